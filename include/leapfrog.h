@@ -368,6 +368,159 @@ int lf_last_cuda_error(const lf_ctx* ctx);
 int lf_delta_step_static(const float* w_up, const float* delta_up, const float* a_l,
                          float* delta_l, int N, void* cuda_stream);
 
+/* ================================================================================================
+ * Layer operators in 16 bits: the dense layer of Eq. z / a with a residual path, its backward pass
+ * (Eq. bp2 .. bp4), the root-mean-square norm in front of it, and activations kept in 8 bits.
+ * They take tensors of any number of rows (`tokens`), so they need no lf_ctx; a handle of their
+ * own (lf_ops) holds the stream, the workspace and the status word.
+ *
+ * Matrices are row-major, one row per token, every pointer but s 16-byte aligned.  Widths (n_in, n_out,
+ * n) are multiples of 8.  A leading dimension ld_* counts elements from one row to the next; 0
+ * stands for the width (contiguous rows), any other value must be at least the width and a
+ * multiple of 8 (of 4 for LF_F32).  Weights w [n_out][n_in], their gradients and the 8-bit arrays
+ * are contiguous.  Bias, gain and their gradients are float32.  Every element is computed in fp32
+ * from the stored inputs and rounded once, on its way out.
+ *
+ * 8-bit form of a matrix [tokens][n]:  q [tokens][n] bytes, s [tokens][(n + 31) / 32] bytes.  Groups
+ * of 32 consecutive columns of a row (the last one may be shorter) share the power of two 2^e, e >=
+ * -127 the smallest integer with max|v| <= 448 * 2^e; s holds e + 127 and q the e4m3 numbers
+ * nearest to v * 2^-e (ties to even).  The value q * 2^e has four significant bits, so it is exact
+ * in bf16 and the tensor cores can take it as it is.  A group that holds an infinity or a NaN gets
+ * s = 255 and reads back as NaN throughout.
+ *
+ * tokens = 0 is legal everywhere (matrices over tokens may then be NULL): nothing is written, except
+ * that gradients summed over tokens are set to zero.  An output may be the very matrix (same address, same leading dimension) that
+ * `residual`, `add` or `dres` names, and h or y of lf_rms_norm may be its x or residual; other
+ * overlaps of outputs with inputs are not allowed.  Results do not depend on timing: sums are added in
+ * a fixed order.
+ * ================================================================================================ */
+typedef struct lf_ops lf_ops;
+
+enum lf_dtype { LF_F32 = 0, LF_BF16 = 1, LF_F16 = 2 };
+
+/* Activations of the layer operators: enum lf_activation and these.  Here sigma' is taken from the
+ * pre-activation z (for the three of lf_activation too). */
+enum lf_layer_activation {
+    LF_ACT_NONE = 3, /* sigma(t) = t                                                           */
+    LF_ACT_SILU = 4, /* sigma(t) = t / (1 + e^{-t})                                            */
+    LF_ACT_GELU = 5  /* sigma(t) = t/2 (1 + tanh(sqrt(2/pi) (t + 0.044715 t^3)))               */
+};
+
+typedef struct lf_linear_args {      /* y = sigma(x w^T + bias) + residual                     */
+    int dtype;                       /* of x, w, residual, y: LF_BF16 or LF_F16                */
+    int act;
+    int tokens, n_in, n_out;
+    const void* x; long long ld_x;   /* [tokens][n_in]                                         */
+    const void* w;                   /* [n_out][n_in]                                          */
+    const float* bias;               /* [n_out] or NULL                                        */
+    const void* residual; long long ld_residual;   /* [tokens][n_out] or NULL                  */
+    void* y; long long ld_y;         /* [tokens][n_out]                                        */
+    unsigned char *q, *s;            /* both or neither: z = x w^T + bias in 8 bits            */
+} lf_linear_args;
+
+typedef struct lf_linear_grad_x_args {   /* dx = (dz w) (.) sigma'(z) + add                    */
+    int dtype;                       /* of dz, w, add, dx: LF_BF16 or LF_F16                   */
+    int act;                         /* sigma of the layer below, whose pre-activation z is    */
+    int tokens, n_in, n_out;
+    const void* dz; long long ld_dz; /* [tokens][n_out]                                        */
+    const void* w;                   /* [n_out][n_in]                                          */
+    const unsigned char *q, *s;      /* z [tokens][n_in] in 8 bits; both NULL: sigma' = 1 (act LF_ACT_NONE) */
+    const void* add; long long ld_add;   /* [tokens][n_in] or NULL                             */
+    void* dx; long long ld_dx;       /* [tokens][n_in]                                         */
+} lf_linear_grad_x_args;
+
+typedef struct lf_linear_grad_w_args {   /* gw = dz^T x,  gb = sum of dz over tokens           */
+    int dtype;                       /* of dz, x: LF_BF16 or LF_F16                            */
+    int gw_dtype;                    /* of gw: LF_F32 or dtype                                 */
+    int act;                         /* x = sigma(z), z from q and s (rounded to dtype as the layer itself does) */
+    int tokens, n_in, n_out;
+    const void* dz; long long ld_dz; /* [tokens][n_out]                                        */
+    const void* x; long long ld_x;   /* [tokens][n_in], or NULL with ...                       */
+    const unsigned char *q, *s;      /* ... z [tokens][n_in] in 8 bits                         */
+    void* gw;                        /* [n_out][n_in]                                          */
+    float* gb;                       /* [n_out] or NULL                                        */
+} lf_linear_grad_w_args;
+
+typedef struct lf_rms_norm_args {    /* h = x + residual;  y = h / sqrt(mean h^2 + eps) (.) gain */
+    int dtype;                       /* of x, residual, h, y: any                              */
+    int tokens, n;                   /* n <= 16384                                             */
+    float eps;                       /* >= 0, finite                                           */
+    const void* x; long long ld_x;
+    const void* residual; long long ld_residual;   /* or NULL                                  */
+    const float* gain;               /* [n]                                                    */
+    void* h; long long ld_h;         /* or NULL                                                */
+    void* y; long long ld_y;         /* or NULL (then q, s are needed)                         */
+    unsigned char *q, *s;            /* both or neither: y in 8 bits, from the unrounded y     */
+} lf_rms_norm_args;
+
+typedef struct lf_rms_norm_backward_args {
+    /* with r = 1 / sqrt(mean h^2 + eps), u = gain (.) dy:
+     *   dh = r (u - h r mean(u (.) h r)) + dres,   dgain = sum over tokens of dy (.) h r           */
+    int dtype;                       /* of dy, h, dres, dh: any                                */
+    int tokens, n;
+    float eps;
+    const void* dy; long long ld_dy;
+    const void* h; long long ld_h;
+    const float* gain;
+    const void* dres; long long ld_dres;   /* gradient that reaches h along the residual path, or NULL */
+    void* dh; long long ld_dh;
+    float* dgain;                    /* [n] or NULL                                            */
+} lf_rms_norm_backward_args;
+
+typedef struct lf_ops_stats {
+    int sm_count;
+    int launches;                    /* kernels launched by the last call                      */
+    int form;                        /* enum lf_linear_form of the last matrix product         */
+    int splits;                      /* parts its contraction was split into                   */
+    unsigned int device_status;      /* status word read by the last lf_ops_sync (0 = clean)   */
+    long long workspace_bytes;
+} lf_ops_stats;
+
+enum lf_linear_form {
+    LF_FORM_STREAM = 1, /* few tokens: weights streamed once through warp-wide products        */
+    LF_FORM_SPLIT = 2,  /* 128 x 128 tiles, the contraction split over a thread-block cluster  */
+    LF_FORM_PAIRS = 3   /* 256 x 256 tiles of CTA pairs, persistent                            */
+};
+
+/*
+ * Create a handle on the current CUDA device with `workspace_bytes` of device memory; calls on it
+ * never allocate.  lf_ops_workspace(tokens, n_in) gives what any call with at most so many tokens
+ * and input columns needs (of it, tokens * n_in * 2 bytes are for lf_linear_grad_w from 8 bits; the
+ * rest is a fixed amount).  Work is enqueued on the handle's stream (lf_ops_set_stream; initially
+ * the legacy default stream) with the handle's device current, and calls of one handle that may
+ * overlap on the GPU must be ordered by the caller: they share the workspace.  Options:
+ * LF_OPT_WAIT_BUDGET_US, and LF_OPT_WITHHOLD = 1 (test hook: a producer of the matrix products arms
+ * a stage it never loads).
+ * Errors of every call: LF_ENULL (a required pointer, or one of a pair that comes together),
+ * LF_EINVAL (types, sizes, leading dimensions, activations), LF_EALIGN, LF_ECAPACITY (the workspace
+ * is too small; nothing is run), LF_ECUDA (lf_ops_last_cuda_error), LF_ENOMEM (create).
+ */
+int lf_ops_create(lf_ops** out, long long workspace_bytes);
+long long lf_ops_workspace(long long tokens, long long n_in);
+int lf_ops_set_stream(lf_ops* ops, void* cuda_stream);
+int lf_ops_set_option(lf_ops* ops, int key, long long value);
+int lf_ops_get_stats(lf_ops* ops, lf_ops_stats* out);
+int lf_ops_last_cuda_error(const lf_ops* ops);
+/* Wait for the handle's stream and read the status word: LF_ETIMEOUT, LF_ECUDA or LF_OK. */
+int lf_ops_sync(lf_ops* ops);
+int lf_ops_destroy(lf_ops* ops);
+
+int lf_linear(lf_ops* ops, const lf_linear_args* args);
+int lf_linear_grad_x(lf_ops* ops, const lf_linear_grad_x_args* args);
+int lf_linear_grad_w(lf_ops* ops, const lf_linear_grad_w_args* args);
+int lf_rms_norm(lf_ops* ops, const lf_rms_norm_args* args);
+int lf_rms_norm_backward(lf_ops* ops, const lf_rms_norm_backward_args* args);
+
+/* x [tokens][n] -> 8 bits.  Any dtype. */
+int lf_pack8(lf_ops* ops, int dtype, int tokens, int n, const void* x, long long ld_x, unsigned char* q,
+             unsigned char* s);
+/* x = sigma(value), rounded to dtype; a value beyond dtype's range becomes its largest finite number. */
+int lf_unpack8(lf_ops* ops, int dtype, int act, int tokens, int n, const unsigned char* q, const unsigned char* s,
+               void* x, long long ld_x);
+/* dz = dy (.) sigma'(value): what reaches the pre-activation of a layer whose output got the gradient dy. */
+int lf_act_backward(lf_ops* ops, int dtype, int act, int tokens, int n, const void* dy, long long ld_dy,
+                    const unsigned char* q, const unsigned char* s, void* dz, long long ld_dz);
+
 /* Static English text for a status code. */
 const char* lf_strerror(int status);
 

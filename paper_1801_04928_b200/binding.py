@@ -30,11 +30,17 @@ LF_FUSED_TILING_AUTO, LF_FUSED_TILING_CLUSTERS, LF_FUSED_TILING_COLUMNS = 0, 1, 
 LF_ACT_SIGMOID, LF_ACT_TANH, LF_ACT_RELU = 0, 1, 2
 LF_COST_QUADRATIC, LF_COST_CROSS_ENTROPY = 0, 1
 LF_TC_TILING_AUTO, LF_TC_TILING_ONE_SM, LF_TC_TILING_TWO_SM = 0, 1, 2
+LF_F32, LF_BF16, LF_F16 = 0, 1, 2
+LF_ACT_NONE, LF_ACT_SILU, LF_ACT_GELU = 3, 4, 5
+LF_FORM_STREAM, LF_FORM_SPLIT, LF_FORM_PAIRS = 1, 2, 3
 LF_DELTA_MATH_AUTO, LF_DELTA_MATH_FP32, LF_DELTA_MATH_3XTF32, LF_DELTA_MATH_TF32_BF16 = 0, 1, 2, 3
 
 EXPORTS = ("lf_create", "lf_create_widths", "lf_set_stream", "lf_set_option", "lf_forward", "lf_backward",
            "lf_backward_sgd", "lf_grad_w", "lf_backward_host", "lf_sync", "lf_owner", "lf_get_stats", "lf_last_cuda_error",
-           "lf_strerror", "lf_version", "lf_destroy", "lf_delta_step_static")
+           "lf_strerror", "lf_version", "lf_destroy", "lf_delta_step_static",
+           "lf_ops_create", "lf_ops_workspace", "lf_ops_set_stream", "lf_ops_set_option", "lf_ops_get_stats",
+           "lf_ops_last_cuda_error", "lf_ops_sync", "lf_ops_destroy", "lf_linear", "lf_linear_grad_x", "lf_linear_grad_w",
+           "lf_rms_norm", "lf_rms_norm_backward", "lf_pack8", "lf_unpack8", "lf_act_backward")
 
 
 class lf_stats(ctypes.Structure):
@@ -47,6 +53,26 @@ class lf_stats(ctypes.Structure):
                 ("delta_math", ctypes.c_int), ("gw_tiling", ctypes.c_int), ("delta_tiling", ctypes.c_int), ("cost", ctypes.c_int), ("activation", ctypes.c_int),
                 ("shard_rank", ctypes.c_int), ("shard_count", ctypes.c_int),
                 ("fused_tiling", ctypes.c_int), ("last_backward_ms", ctypes.c_float)]
+
+
+def _struct(name: str, *fields):
+    """A C struct from (type letter, names) pairs: i int, l long long, f float, p pointer."""
+    kinds = {"i": ctypes.c_int, "l": ctypes.c_longlong, "f": ctypes.c_float, "p": ctypes.c_void_p, "u": ctypes.c_uint}
+    return type(name, (ctypes.Structure,), {"_fields_": [(n, kinds[k]) for k, names in fields for n in names.split()]})
+
+
+# the argument structs of the layer operators, field by field as in include/leapfrog.h
+lf_linear_args = _struct("lf_linear_args", ("i", "dtype act tokens n_in n_out"), ("p", "x"), ("l", "ld_x"), ("p", "w bias residual"),
+                         ("l", "ld_residual"), ("p", "y"), ("l", "ld_y"), ("p", "q s"))
+lf_linear_grad_x_args = _struct("lf_linear_grad_x_args", ("i", "dtype act tokens n_in n_out"), ("p", "dz"), ("l", "ld_dz"), ("p", "w q s add"),
+                                ("l", "ld_add"), ("p", "dx"), ("l", "ld_dx"))
+lf_linear_grad_w_args = _struct("lf_linear_grad_w_args", ("i", "dtype gw_dtype act tokens n_in n_out"), ("p", "dz"), ("l", "ld_dz"), ("p", "x"),
+                                ("l", "ld_x"), ("p", "q s gw gb"))
+lf_rms_norm_args = _struct("lf_rms_norm_args", ("i", "dtype tokens n"), ("f", "eps"), ("p", "x"), ("l", "ld_x"), ("p", "residual"),
+                           ("l", "ld_residual"), ("p", "gain h"), ("l", "ld_h"), ("p", "y"), ("l", "ld_y"), ("p", "q s"))
+lf_rms_norm_backward_args = _struct("lf_rms_norm_backward_args", ("i", "dtype tokens n"), ("f", "eps"), ("p", "dy"), ("l", "ld_dy"), ("p", "h"),
+                                    ("l", "ld_h"), ("p", "gain dres"), ("l", "ld_dres"), ("p", "dh"), ("l", "ld_dh"), ("p", "dgain"))
+lf_ops_stats = _struct("lf_ops_stats", ("i", "sm_count launches form splits"), ("u", "device_status"), ("l", "workspace_bytes"))
 
 
 def _load() -> ctypes.CDLL:
@@ -74,9 +100,23 @@ def _load() -> ctypes.CDLL:
     lib.lf_version.argtypes = []
     lib.lf_destroy.argtypes = [vp]
     lib.lf_delta_step_static.argtypes = [vp, vp, vp, vp, i, vp]
+    lib.lf_ops_create.argtypes = [ctypes.POINTER(vp), ll]
+    lib.lf_ops_workspace.argtypes = [ll, ll]
+    lib.lf_ops_set_stream.argtypes = [vp, vp]
+    lib.lf_ops_set_option.argtypes = [vp, i, ll]
+    lib.lf_ops_get_stats.argtypes = [vp, ctypes.POINTER(lf_ops_stats)]
+    lib.lf_ops_last_cuda_error.argtypes = [vp]
+    lib.lf_ops_sync.argtypes = [vp]
+    lib.lf_ops_destroy.argtypes = [vp]
+    for name in ("lf_linear", "lf_linear_grad_x", "lf_linear_grad_w", "lf_rms_norm", "lf_rms_norm_backward"):
+        getattr(lib, name).argtypes = [vp, ctypes.c_void_p]
+    lib.lf_pack8.argtypes = [vp, i, i, i, vp, ll, vp, vp]
+    lib.lf_unpack8.argtypes = [vp, i, i, i, i, vp, vp, vp, ll]
+    lib.lf_act_backward.argtypes = [vp, i, i, i, i, vp, ll, vp, vp, vp, ll]
     for name in EXPORTS:
         if name != "lf_strerror":
             getattr(lib, name).restype = i
+    lib.lf_ops_workspace.restype = ll
     return lib
 
 
@@ -304,6 +344,304 @@ class Leapfrog:
     def close(self):
         if self._h is not None:
             lf_destroy(self._h)
+            self._h = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---- layer operators ----------------------------------------------------------------------------
+
+def lf_ops_create(workspace_bytes: int):
+    """Returns (status, handle)."""
+    h = ctypes.c_void_p(None)
+    rc = _lib.lf_ops_create(ctypes.byref(h), int(workspace_bytes))
+    return rc, h
+
+
+def lf_ops_workspace(tokens: int, n_in: int) -> int:
+    """Bytes of workspace that every call with at most `tokens` rows and `n_in` input columns can run in."""
+    return _lib.lf_ops_workspace(int(tokens), int(n_in))
+
+
+def lf_ops_set_stream(ops, cuda_stream: int | None) -> int:
+    return _lib.lf_ops_set_stream(ops, ctypes.c_void_p(cuda_stream or None))
+
+
+def lf_ops_set_option(ops, key: int, value: int) -> int:
+    return _lib.lf_ops_set_option(ops, int(key), int(value))
+
+
+def lf_ops_get_stats(ops):
+    """Returns (status, dict)."""
+    st = lf_ops_stats()
+    rc = _lib.lf_ops_get_stats(ops, ctypes.byref(st))
+    return rc, {f: getattr(st, f) for f, _ in lf_ops_stats._fields_}
+
+
+def lf_ops_last_cuda_error(ops) -> int:
+    return _lib.lf_ops_last_cuda_error(ops)
+
+
+def lf_ops_sync(ops) -> int:
+    return _lib.lf_ops_sync(ops)
+
+
+def lf_ops_destroy(ops) -> int:
+    return _lib.lf_ops_destroy(ops)
+
+
+def _by_struct(name):
+    fn = getattr(_lib, name)
+
+    def call(ops, args) -> int:
+        return fn(ops, None if args is None else ctypes.addressof(args))
+    call.__name__ = name
+    call.__doc__ = f"{name}(ops, args): `args` is a {name}_args."
+    return call
+
+
+lf_linear = _by_struct("lf_linear")
+lf_linear_grad_x = _by_struct("lf_linear_grad_x")
+lf_linear_grad_w = _by_struct("lf_linear_grad_w")
+lf_rms_norm = _by_struct("lf_rms_norm")
+lf_rms_norm_backward = _by_struct("lf_rms_norm_backward")
+
+
+def lf_pack8(ops, dtype: int, tokens: int, n: int, x, ld_x: int, q, s) -> int:
+    return _lib.lf_pack8(ops, dtype, tokens, n, _ptr(x), ld_x, _ptr(q), _ptr(s))
+
+
+def lf_unpack8(ops, dtype: int, act: int, tokens: int, n: int, q, s, x, ld_x: int) -> int:
+    return _lib.lf_unpack8(ops, dtype, act, tokens, n, _ptr(q), _ptr(s), _ptr(x), ld_x)
+
+
+def lf_act_backward(ops, dtype: int, act: int, tokens: int, n: int, dy, ld_dy: int, q, s, dz, ld_dz: int) -> int:
+    return _lib.lf_act_backward(ops, dtype, act, tokens, n, _ptr(dy), ld_dy, _ptr(q), _ptr(s), _ptr(dz), ld_dz)
+
+
+_TYPES = {}              # torch dtype -> enum lf_dtype, filled on first use
+
+
+def _types() -> dict:
+    import torch
+    _TYPES.update({torch.float32: LF_F32, torch.bfloat16: LF_BF16, torch.float16: LF_F16, torch.uint8: -1})
+    return _TYPES
+
+
+def _refuse(where: str, name: str, problem: str):
+    raise LeapfrogError(LF_EINVAL, f"{where}: argument {name}: {problem}")
+
+
+class Operators:
+    """Owns one ``lf_ops``: the layer operators on torch tensors.
+
+    Matrices are 2-D, [tokens, width], with unit stride along a row; their rows may be further apart than
+    the width (a slice of columns of a wider matrix).  Results go into the tensors that are passed in.
+    Raises :class:`LeapfrogError` on any non-zero status and on tensors whose type, device, shape or
+    layout does not fit.  ``stream``: a cudaStream_t as an int; None is the legacy default stream.
+    """
+
+    def __init__(self, workspace_bytes: int | None = None, stream: int | None = None):
+        rc, self._h = lf_ops_create(lf_ops_workspace(0, 0) if workspace_bytes is None else workspace_bytes)
+        if rc != LF_OK:
+            self._h = None
+            raise LeapfrogError(rc, "lf_ops_create")
+        self._types = _types()
+        if stream is not None:
+            self.set_stream(stream)
+
+    def _check(self, rc: int, where: str):
+        if rc != LF_OK:
+            raise LeapfrogError(rc, where, lf_ops_last_cuda_error(self._h))
+
+    def set_stream(self, cuda_stream: int | None):
+        self._check(lf_ops_set_stream(self._h, cuda_stream), "lf_ops_set_stream")
+
+    def set_option(self, key: int, value: int):
+        self._check(lf_ops_set_option(self._h, key, value), "lf_ops_set_option")
+
+    def sync(self):
+        self._check(lf_ops_sync(self._h), "lf_ops_sync")
+
+    def stats(self) -> dict:
+        rc, d = lf_ops_get_stats(self._h)
+        self._check(rc, "lf_ops_get_stats")
+        return d
+
+    # -- marshalling: what a tensor has to be; answers its address (and row stride) --
+    def _type(self, t, name: str, where: str) -> int:
+        code = self._types.get(t.dtype, -1)
+        if code < 0:
+            _refuse(where, name, f"dtype {t.dtype} (float32, bfloat16 or float16 needed)")
+        return code
+
+    @staticmethod
+    def _mat(t, rows: int, cols: int, dtype, name: str, where: str):
+        """(address, leading dimension) of a [rows, cols] matrix."""
+        if t is None:
+            return None, 0
+        if t.dtype is dtype and t.is_cuda:
+            shape = t.shape
+            if len(shape) == 2 and shape[0] == rows and shape[1] == cols:
+                step, unit = t.stride()
+                if unit == 1 and (step >= cols or rows <= 1):
+                    return t.data_ptr(), (step if rows > 1 else 0)
+                _refuse(where, name, f"strides {tuple(t.stride())} (unit stride along rows that do not overlap needed)")
+            _refuse(where, name, f"shape {tuple(shape)}, ({rows}, {cols}) needed")
+        _refuse(where, name, f"{t.dtype} on {t.device} ({dtype} on a CUDA device needed)")
+
+    @staticmethod
+    def _flat(t, n: int, dtype, name: str, where: str):
+        """Address of a contiguous tensor of n elements."""
+        if t is None:
+            return None
+        if t.dtype is dtype and t.is_cuda and t.numel() == n and t.is_contiguous():
+            return t.data_ptr()
+        _refuse(where, name, f"{t.dtype} {tuple(t.shape)} on {t.device}, contiguous: {t.is_contiguous()} "
+                             f"({n} contiguous elements of {dtype} on a CUDA device needed)")
+
+    def _eight(self, q, s, rows: int, cols: int, where: str):
+        if q is None and s is None:
+            return None, None
+        import torch
+        return (self._flat(q, rows * cols, torch.uint8, "q", where),
+                self._flat(s, rows * ((cols + 31) // 32), torch.uint8, "s", where))
+
+    @staticmethod
+    def _shape(t, name: str, where: str):
+        if t.dim() != 2:
+            _refuse(where, name, f"{t.dim()} dimensions (2 needed)")
+        return t.shape
+
+    def linear(self, x, w, y, bias=None, residual=None, act: int = LF_ACT_NONE, q=None, s=None):
+        """y = act(x w^T + bias) + residual; with q and s also z = x w^T + bias in 8 bits."""
+        where = "lf_linear"
+        code = self._type(x, "x", where)
+        m, k = self._shape(x, "x", where)
+        n = self._shape(w, "w", where)[0]
+        t, f32 = x.dtype, _FLOAT32 or self._f32()
+        xp, ldx = self._mat(x, m, k, t, "x", where)
+        rp, ldr = self._mat(residual, m, n, t, "residual", where)
+        yp, ldy = self._mat(y, m, n, t, "y", where)
+        self._w(w, n, k, where)
+        qp, sp = self._eight(q, s, m, n, where)
+        a = lf_linear_args(code, act, m, k, n, xp, ldx, self._flat(w, n * k, t, "w", where), self._flat(bias, n, f32, "bias", where),
+                           rp, ldr, yp, ldy, qp, sp)
+        self._check(_lib.lf_linear(self._h, ctypes.addressof(a)), where)
+
+    def linear_grad_x(self, dz, w, dx, q=None, s=None, act: int = LF_ACT_NONE, add=None):
+        """dx = (dz w) * act'(z) + add, z [tokens, n_in] given in 8 bits by q and s."""
+        where = "lf_linear_grad_x"
+        code = self._type(dz, "dz", where)
+        m, n = self._shape(dz, "dz", where)
+        k = self._shape(w, "w", where)[1]
+        t = dz.dtype
+        zp, ldz = self._mat(dz, m, n, t, "dz", where)
+        ap, lda = self._mat(add, m, k, t, "add", where)
+        xp, ldx = self._mat(dx, m, k, t, "dx", where)
+        self._w(w, n, k, where)
+        qp, sp = self._eight(q, s, m, k, where)
+        a = lf_linear_grad_x_args(code, act, m, k, n, zp, ldz, self._flat(w, n * k, t, "w", where), qp, sp, ap, lda, xp, ldx)
+        self._check(_lib.lf_linear_grad_x(self._h, ctypes.addressof(a)), where)
+
+    def linear_grad_w(self, dz, gw, gb=None, x=None, q=None, s=None, act: int = LF_ACT_NONE):
+        """gw = dz^T x, gb = column sums of dz; x given, or act(z) from 8 bits.  gw: float32 or dz's type."""
+        where = "lf_linear_grad_w"
+        code = self._type(dz, "dz", where)
+        gcode = self._type(gw, "gw", where)
+        m, n = self._shape(dz, "dz", where)
+        k = self._shape(gw, "gw", where)[1]
+        t, f32 = dz.dtype, _FLOAT32 or self._f32()
+        zp, ldz = self._mat(dz, m, n, t, "dz", where)
+        xp, ldx = self._mat(x, m, k, t, "x", where)
+        self._w(gw, n, k, where, "gw")
+        qp, sp = self._eight(q, s, m, k, where)
+        a = lf_linear_grad_w_args(code, gcode, act, m, k, n, zp, ldz, xp, ldx, qp, sp, self._flat(gw, n * k, gw.dtype, "gw", where),
+                                  self._flat(gb, n, f32, "gb", where))
+        self._check(_lib.lf_linear_grad_w(self._h, ctypes.addressof(a)), where)
+
+    def rms_norm(self, x, gain, y=None, residual=None, h=None, q=None, s=None, eps: float = 1e-5):
+        """h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain, in x's type and / or in 8 bits (q, s)."""
+        where = "lf_rms_norm"
+        code = self._type(x, "x", where)
+        m, n = self._shape(x, "x", where)
+        t = x.dtype
+        xp, ldx = self._mat(x, m, n, t, "x", where)
+        rp, ldr = self._mat(residual, m, n, t, "residual", where)
+        hp, ldh = self._mat(h, m, n, t, "h", where)
+        yp, ldy = self._mat(y, m, n, t, "y", where)
+        qp, sp = self._eight(q, s, m, n, where)
+        a = lf_rms_norm_args(code, m, n, eps, xp, ldx, rp, ldr, self._flat(gain, n, _FLOAT32 or self._f32(), "gain", where),
+                             hp, ldh, yp, ldy, qp, sp)
+        self._check(_lib.lf_rms_norm(self._h, ctypes.addressof(a)), where)
+
+    def rms_norm_backward(self, dy, h, gain, dh, dgain=None, dres=None, eps: float = 1e-5):
+        """Gradient of y = h / sqrt(mean(h^2) + eps) * gain with respect to h (plus dres) and gain."""
+        where = "lf_rms_norm_backward"
+        code = self._type(h, "h", where)
+        m, n = self._shape(h, "h", where)
+        t, f32 = h.dtype, _FLOAT32 or self._f32()
+        yp, ldy = self._mat(dy, m, n, t, "dy", where)
+        hp, ldh = self._mat(h, m, n, t, "h", where)
+        rp, ldr = self._mat(dres, m, n, t, "dres", where)
+        dp, ldd = self._mat(dh, m, n, t, "dh", where)
+        a = lf_rms_norm_backward_args(code, m, n, eps, yp, ldy, hp, ldh, self._flat(gain, n, f32, "gain", where), rp, ldr, dp, ldd,
+                                      self._flat(dgain, n, f32, "dgain", where))
+        self._check(_lib.lf_rms_norm_backward(self._h, ctypes.addressof(a)), where)
+
+    def pack8(self, x, q, s):
+        """x [tokens, n] in 8 bits: q [tokens, n], s [tokens, ceil(n / 32)]."""
+        where = "lf_pack8"
+        code = self._type(x, "x", where)
+        m, n = self._shape(x, "x", where)
+        xp, ldx = self._mat(x, m, n, x.dtype, "x", where)
+        qp, sp = self._eight(q, s, m, n, where)
+        self._check(_lib.lf_pack8(self._h, code, m, n, xp, ldx, qp, sp), where)
+
+    def unpack8(self, q, s, x, act: int = LF_ACT_NONE):
+        """x = act(value of q and s)."""
+        where = "lf_unpack8"
+        code = self._type(x, "x", where)
+        m, n = self._shape(x, "x", where)
+        xp, ldx = self._mat(x, m, n, x.dtype, "x", where)
+        qp, sp = self._eight(q, s, m, n, where)
+        self._check(_lib.lf_unpack8(self._h, code, act, m, n, qp, sp, xp, ldx), where)
+
+    def act_backward(self, dy, q, s, dz, act: int = LF_ACT_NONE):
+        """dz = dy * act'(value of q and s)."""
+        where = "lf_act_backward"
+        code = self._type(dy, "dy", where)
+        m, n = self._shape(dy, "dy", where)
+        yp, ldy = self._mat(dy, m, n, dy.dtype, "dy", where)
+        zp, ldz = self._mat(dz, m, n, dy.dtype, "dz", where)
+        qp, sp = self._eight(q, s, m, n, where)
+        self._check(_lib.lf_act_backward(self._h, code, act, m, n, yp, ldy, qp, sp, zp, ldz), where)
+
+    @staticmethod
+    def _f32():
+        global _FLOAT32
+        import torch
+        _FLOAT32 = torch.float32
+        return _FLOAT32
+
+    @staticmethod
+    def _w(w, n: int, k: int, where: str, name: str = "w"):
+        if w.dim() != 2 or w.shape[0] != n or w.shape[1] != k:
+            _refuse(where, name, f"shape {tuple(w.shape)}, ({n}, {k}) needed")
+
+    def close(self):
+        if self._h is not None:
+            lf_ops_destroy(self._h)
             self._h = None
 
     def __enter__(self):

@@ -19,7 +19,8 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libleapfrog.so")
 
 SOURCES = ["lf_api.cu", "lf_kernels_b1.cu", "lf_kernels_batch.cu", "lf_persistent.cu", "lf_columns.cu",
-           "lf_gemm_tf32.cu", "lf_delta_gemm_tc.cu"]
+           "lf_gemm_tf32.cu", "lf_delta_gemm_tc.cu", "lf_ops_api.cu", "lf_rows.cu", "lf_linear_tc.cu",
+           "lf_linear_stream.cu"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v", "-I", INCLUDE, "-I", CSRC]

@@ -1,0 +1,182 @@
+// Device helpers of the layer operators: rows of fp32 / bf16 / f16 as fp32 vectors of eight, the
+// activations and their derivatives from the pre-activation, and the 8-bit form (e4m3 numbers, one
+// power-of-two scale for 32 columns).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "leapfrog.h"
+
+namespace lfrow {
+
+// ---- eight consecutive elements <-> fp32 ----------------------------------------------------------
+__device__ __forceinline__ float2 unpack2(unsigned v, __nv_bfloat16)
+{
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+}
+__device__ __forceinline__ float2 unpack2(unsigned v, __half)
+{
+    return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+__device__ __forceinline__ unsigned pack2(float lo, float hi, __nv_bfloat16)
+{
+    unsigned r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ unsigned pack2(float lo, float hi, __half)
+{
+    unsigned r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <typename T>
+struct vec8 {      // 16-bit types: one 128-bit access
+    uint4 u;
+    __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+        const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2(w[i], T());
+            v[2 * i] = f.x; v[2 * i + 1] = f.y;
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[8])
+    {
+        u = make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()), pack2(v[6], v[7], T()));
+    }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = u; }
+};
+template <>
+struct vec8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p)
+    {
+        a = reinterpret_cast<const float4*>(p)[0];
+        b = reinterpret_cast<const float4*>(p)[1];
+    }
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    __device__ __forceinline__ void set(const float (&v)[8])
+    {
+        a = make_float4(v[0], v[1], v[2], v[3]);
+        b = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    __device__ __forceinline__ void store(float* p) const
+    {
+        reinterpret_cast<float4*>(p)[0] = a;
+        reinterpret_cast<float4*>(p)[1] = b;
+    }
+};
+// the largest finite number of a type (what lf_unpack8 saturates to)
+__device__ __forceinline__ float max_finite(float) { return 3.402823466e38f; }
+__device__ __forceinline__ float max_finite(__nv_bfloat16) { return 3.389531389e38f; }
+__device__ __forceinline__ float max_finite(__half) { return 65504.f; }
+__device__ __forceinline__ float clamp_keep_nan(float v, float m)
+{
+    return v > m ? m : (v < -m ? -m : v);
+}
+
+// ---- activations from the pre-activation ----------------------------------------------------------
+// FAST: e^t and the quotient from the special-function unit (about 1e-6 relative, far below the
+// rounding of a 16-bit result); otherwise the correctly scaled library functions, for fp32 results.
+template <bool FAST>
+__device__ __forceinline__ float sigmoid(float t)
+{
+    return FAST ? __fdividef(1.0f, 1.0f + __expf(-t)) : 1.0f / (1.0f + expf(-t));
+}
+constexpr float GELU_C = 1.5957691216057308f;            // 2 sqrt(2 / pi)
+constexpr float GELU_D = GELU_C * 0.044715f;
+template <bool FAST>
+__device__ __forceinline__ float act(float z, int kind)
+{
+    switch (kind) {
+        case LF_ACT_SIGMOID: return sigmoid<FAST>(z);
+        case LF_ACT_TANH: return tanhf(z);
+        case LF_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+        case LF_ACT_SILU: return z * sigmoid<FAST>(z);
+        case LF_ACT_GELU: return z * sigmoid<FAST>(z * (GELU_C + GELU_D * z * z));   // (1 + tanh u) / 2 = sigmoid(2 u)
+        default: return z;
+    }
+}
+template <bool FAST>
+__device__ __forceinline__ float act_prime(float z, int kind)
+{
+    switch (kind) {
+        case LF_ACT_SIGMOID: { const float a = sigmoid<FAST>(z); return a * (1.f - a); }
+        case LF_ACT_TANH: { const float t = tanhf(z); return 1.f - t * t; }
+        case LF_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+        case LF_ACT_SILU: { const float a = sigmoid<FAST>(z); return a + z * a * (1.f - a); }
+        case LF_ACT_GELU: {
+            const float a = sigmoid<FAST>(z * (GELU_C + GELU_D * z * z));
+            return a + z * a * (1.f - a) * (GELU_C + 3.f * GELU_D * z * z);
+        }
+        default: return 1.f;
+    }
+}
+
+// ---- 8 bits -------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// the scale byte of a group from the bits of its largest magnitude (NaN > infinity > finite as integers):
+// amax = m 2^E, e = E - 8 for m <= 1.75 (448 = 1.75 * 2^8), else E - 7, at least -127
+__device__ __forceinline__ unsigned scale_byte(unsigned amax_bits)
+{
+    if (amax_bits >= 0x7F800000u) return 255u;
+    const int b = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return b > 0 ? (unsigned)b : 0u;
+}
+__device__ __forceinline__ float inv_scale(unsigned byte)     // 2^-e; NaN for a group that is not finite
+{
+    return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((254u - byte) << 23);
+}
+__device__ __forceinline__ float scale(unsigned byte)         // 2^e
+{
+    return __uint_as_float(byte == 255u ? 0x7FC00000u : (byte == 0u ? 0x00400000u : byte << 23));
+}
+__device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d)
+{
+    unsigned short lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (unsigned)lo | ((unsigned)hi << 16);
+}
+__device__ __forceinline__ void from_e4m3x4(unsigned q, float s, float& a, float& b, float& c, float& d)
+{
+    unsigned h0, h1;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h0) : "h"((unsigned short)(q & 0xFFFFu)));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h1) : "h"((unsigned short)(q >> 16)));
+    const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
+    const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+    a = f0.x * s; b = f0.y * s; c = f1.x * s; d = f1.y * s;
+}
+// eight columns held by one lane; the four lanes of a group are neighbours (lane & ~3)
+__device__ __forceinline__ unsigned group_byte(const float (&v)[8])
+{
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    return scale_byte(m);
+}
+__device__ __forceinline__ uint2 quantize8(const float (&v)[8], unsigned byte)
+{
+    const float r = inv_scale(byte);
+    return make_uint2(to_e4m3x4(v[0] * r, v[1] * r, v[2] * r, v[3] * r), to_e4m3x4(v[4] * r, v[5] * r, v[6] * r, v[7] * r));
+}
+__device__ __forceinline__ void dequantize8(uint2 q, unsigned byte, float (&v)[8])
+{
+    const float s = scale(byte);
+    from_e4m3x4(q.x, s, v[0], v[1], v[2], v[3]);
+    from_e4m3x4(q.y, s, v[4], v[5], v[6], v[7]);
+}
+
+}  // namespace lfrow

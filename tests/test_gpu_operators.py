@@ -1,0 +1,639 @@
+"""The layer operators on the GPU against their definitions in 64 bits: values, 8-bit forms, gradients (the
+formula's and central differences'), ragged sizes, strides, aliases, streams, empty inputs, values that are not
+finite, refusals and waits that run out."""
+import pytest
+import torch
+
+import operators_ref as R
+import paper_1801_04928_b200 as lf
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+GUARD = 512
+
+
+def _rand(g, *shape, std=1.0, dtype=F32):
+    return torch.empty(shape, device="cuda").normal_(0.0, std, generator=g).to(dtype)
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+class Out:
+    """An output matrix, NaN-filled (0xA5 bytes for integers), with guard bands around it."""
+
+    def __init__(self, rows, cols, dtype, ld=None):
+        ld = ld or cols
+        self.raw = torch.empty(rows * ld + 2 * GUARD, dtype=dtype, device="cuda")
+        self.fill = 0xA5 if dtype == torch.uint8 else float("nan")
+        self.raw.fill_(self.fill)
+        self.t = self.raw[GUARD:GUARD + rows * ld].view(rows, ld)[:, :cols]
+        self.ld, self.rows, self.cols = ld, rows, cols
+
+    def check(self):
+        def clean(v):
+            return bool(((v == 0xA5) if v.dtype == torch.uint8 else v.isnan()).all())
+        assert clean(self.raw[:GUARD]) and clean(self.raw[GUARD + self.rows * self.ld:]), "written outside the matrix"
+        if self.ld > self.cols:
+            assert clean(self.raw[GUARD:GUARD + self.rows * self.ld].view(self.rows, self.ld)[:, self.cols:]), "written between rows"
+
+
+@pytest.fixture(scope="module")
+def ops():
+    with lf.Operators(lf.lf_ops_workspace(8192, 4096)) as o:
+        yield o
+
+
+def _groups(n):
+    return (n + 31) // 32
+
+
+def _check_packed(name, q, s, ref, err):
+    """q, s stand for values within `err` of ref: the scale is right for them up to that error, and a value is half a
+    step of the format away at most (2^-4 relative; 2^-10 of the scale where e4m3 is subnormal)."""
+    e = s.to(R.D) - 127
+    amax_hi, amax_lo = _amax(ref.abs() + err), _amax((ref.abs() - err).clamp(min=0))
+    assert bool((amax_lo <= 448 * torch.exp2(e)).all()), f"{name}: a scale is too small"
+    assert bool(((amax_hi > 224 * torch.exp2(e)) | (s == 0)).all()), f"{name}: a scale is too large"
+    v = R.unpack8(q, s)
+    step = torch.exp2(R.columns(e, ref.shape[1]))
+    R.check(name, v, ref, err + 2.0 ** -4 * (ref.abs() + err) + 2.0 ** -10 * step)
+
+
+def _amax(v):
+    rows, n = v.shape
+    pad = torch.zeros(rows, _groups(n) * 32, dtype=v.dtype, device=v.device)
+    pad[:, :n] = v
+    return pad.view(rows, -1, 32).amax(-1)
+
+
+# ---- dense layer, forward ----------------------------------------------------------------------------
+
+def _linear(ops, M, K, N, dtype, act, bias=True, residual=True, ckpt=True, ld_extra=0, form=None, seed=0):
+    g = _gen(1000 * M + 10 * K + N + seed)
+    x = Out(M, K, dtype, K + ld_extra)
+    x.t.copy_(_rand(g, M, K, dtype=dtype))
+    w = _rand(g, N, K, std=K ** -0.5, dtype=dtype)
+    b = _rand(g, N, std=0.3) if bias else None
+    r = Out(M, N, dtype, N + 2 * ld_extra)
+    r.t.copy_(_rand(g, M, N, dtype=dtype))
+    y = Out(M, N, dtype, N + ld_extra)
+    q, s = Out(M, N, torch.uint8), Out(M, _groups(N), torch.uint8)
+    ops.linear(x.t, w, y.t, bias=b, residual=r.t if residual else None, act=act, q=q.t if ckpt else None, s=s.t if ckpt else None)
+    ops.sync()
+    if form:
+        assert ops.stats()["form"] == form, ops.stats()
+    for o in (x, r, y, q, s):
+        o.check()
+    z = x.t.to(R.D) @ w.to(R.D).t()
+    err = R.product_err(x.t.to(R.D), w.to(R.D).t(), 1.0)
+    if bias:
+        z = z + b.to(R.D)
+        err = err + 2.0 ** -23 * (z.abs() + b.abs().to(R.D))
+    a = R.act(z, act)
+    # the error of z through sigma, and 4e-6 for e^t and the quotient
+    yerr = R.LIP1[act] * err + 4e-6 * (a.abs() + (1 if act == R.TANH else 0))
+    ref = a
+    if residual:
+        ref = a + r.t.to(R.D)
+        yerr = yerr + 2.0 ** -24 * ref.abs()
+    R.check(f"y {M}x{K}x{N}", y.t, ref, R.rounded(ref, dtype, yerr))
+    if ckpt:
+        _check_packed(f"z8 {M}x{K}x{N}", q.t, s.t, z, err)
+
+
+@pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
+@pytest.mark.parametrize("K,N,dtype,act", [(8, 8, BF16, R.NONE), (4096, 40, BF16, R.GELU), (520, 1032, F16, R.SILU),
+                                           (1024, 72, F16, R.RELU), (2056, 4096, BF16, R.TANH), (264, 264, F16, R.SIGMOID)])
+def test_linear_few_tokens(ops, M, K, N, dtype, act):
+    _linear(ops, M, K, N, dtype, act, form=lf.LF_FORM_STREAM)
+
+
+@pytest.mark.parametrize("M,K,N,dtype,act", [(17, 8, 8, BF16, R.NONE), (17, 64, 136, F16, R.GELU), (127, 72, 128, BF16, R.SILU),
+                                             (128, 1024, 1024, BF16, R.GELU), (129, 520, 264, F16, R.RELU), (70, 4096, 40, BF16, R.TANH),
+                                             (256, 4104, 256, F16, R.SIGMOID), (509, 2048, 1024, BF16, R.NONE), (200, 16384, 64, BF16, R.GELU)])
+def test_linear_split_tiles(ops, M, K, N, dtype, act):
+    _linear(ops, M, K, N, dtype, act, form=lf.LF_FORM_SPLIT)
+
+
+@pytest.mark.parametrize("M,K,N,dtype,act", [(2049, 72, 1288, BF16, R.GELU), (1537, 1024, 1800, F16, R.SILU), (4097, 8, 776, BF16, R.RELU),
+                                             (2048, 2048, 2048, BF16, R.NONE), (5000, 520, 1032, F16, R.TANH)])
+def test_linear_pairs(ops, M, K, N, dtype, act):
+    _linear(ops, M, K, N, dtype, act, form=lf.LF_FORM_PAIRS)
+
+
+@pytest.mark.parametrize("M,K,N", [(3, 264, 72), (130, 264, 200), (2050, 136, 1400)])
+@pytest.mark.parametrize("bias,residual,ckpt,ld", [(False, False, False, 0), (True, False, True, 8), (False, True, False, 24), (True, True, True, 40)])
+def test_linear_options_and_strides(ops, M, K, N, bias, residual, ckpt, ld):
+    _linear(ops, M, K, N, BF16, R.GELU, bias, residual, ckpt, ld)
+
+
+@pytest.mark.parametrize("M,K,N", [(5, 512, 96), (300, 512, 96), (2100, 128, 1304)])
+def test_linear_adds_into_its_residual_and_repeats_bitwise(ops, M, K, N):
+    g = _gen(5)
+    x, w, r = _rand(g, M, K, dtype=BF16), _rand(g, N, K, std=0.05, dtype=BF16), _rand(g, M, N, dtype=BF16)
+    y = torch.empty_like(r)
+    ops.linear(x, w, y, residual=r, act=R.SILU)
+    for _ in range(3):
+        r2 = r.clone()
+        ops.linear(x, w, r2, residual=r2, act=R.SILU)
+        assert torch.equal(r2, y)
+
+
+def test_linear_row_does_not_depend_on_its_neighbours_being_finite(ops):
+    # a token with infinities or NaN spoils its own row only; in 8 bits, its own groups only
+    for M, K, N in ((4, 256, 96), (40, 256, 96), (2100, 256, 1304)):
+        g = _gen(6)
+        x, w = _rand(g, M, K, dtype=BF16), _rand(g, N, K, std=0.05, dtype=BF16)
+        y, y2 = (torch.empty(M, N, dtype=BF16, device="cuda") for _ in range(2))
+        q, s, q2, s2 = (torch.empty(M, c, dtype=torch.uint8, device="cuda") for c in (N, _groups(N), N, _groups(N)))
+        ops.linear(x, w, y, q=q, s=s)
+        x2 = x.clone()
+        x2[1, 3] = float("nan")
+        x2[2, 5] = float("inf")
+        ops.linear(x2, w, y2, q=q2, s=s2)
+        others = [i for i in range(M) if i not in (1, 2)]
+        assert torch.equal(y[others], y2[others]) and torch.equal(q[others], q2[others]) and torch.equal(s[others], s2[others])
+        assert y2[1].isnan().all() and not y2[2].isfinite().any()
+        assert bool((s2[1:3] == 255).all())
+        v = torch.empty_like(y)
+        ops.unpack8(q2, s2, v)
+        assert v[1:3].isnan().all() and v[others].isfinite().all()
+
+
+# ---- dense layer, backward ----------------------------------------------------------------------------
+
+def _backward(ops, M, K, N, dtype, act, gw_dtype, eight=True, add=False, ld_extra=0, forms=(None, None)):
+    g = _gen(77 + 1000 * M + 10 * K + N)
+    dz = Out(M, N, dtype, N + ld_extra)
+    dz.t.copy_(_rand(g, M, N, std=0.1, dtype=dtype))
+    w = _rand(g, N, K, std=N ** -0.5, dtype=dtype)
+    z32 = _rand(g, M, K, std=1.5)
+    x = Out(M, K, dtype, K + ld_extra)
+    x.t.copy_(z32.to(dtype))
+    q, s = R.pack8(z32)
+    zv = R.unpack8(q, s) if eight else None
+    addm = Out(M, K, dtype, K + 3 * ld_extra)
+    addm.t.copy_(_rand(g, M, K, std=0.1, dtype=dtype))
+    dx, gw, gb = Out(M, K, dtype, K + 2 * ld_extra), Out(N, K, gw_dtype), Out(1, N, F32)
+    ops.linear_grad_x(dz.t, w, dx.t, q=q if eight else None, s=s if eight else None, act=act if eight else R.NONE, add=addm.t if add else None)
+    if forms[0]:
+        assert ops.stats()["form"] == forms[0], ops.stats()
+    if eight:
+        ops.linear_grad_w(dz.t, gw.t, gb=gb.t.view(-1), q=q, s=s, act=act)
+    else:
+        ops.linear_grad_w(dz.t, gw.t, gb=gb.t.view(-1), x=x.t)
+    if forms[1]:
+        assert ops.stats()["form"] == forms[1], ops.stats()
+    ops.sync()
+    for o in (dz, x, addm, dx, gw, gb):
+        o.check()
+    d64, w64 = dz.t.to(R.D), w.to(R.D)
+    t = d64 @ w64
+    err = R.product_err(d64, w64)
+    if eight:
+        sp = R.act_prime(zv, act)
+        err = err * sp.abs() + 8e-6 * t.abs()
+        t = t * sp
+    if add:
+        t = t + addm.t.to(R.D)
+        err = err + 2.0 ** -24 * t.abs()
+    R.check("dx", dx.t, t, R.rounded(t, dtype, err))
+    # the layer's input as it enters the products: sigma(z) rounded to 16 bits
+    if eight:
+        a = R.act(zv, act)
+        aerr = torch.zeros_like(a) if act in (R.NONE, R.RELU) else R.rounded(a, dtype, 4e-6 * (a.abs() + 1))
+        if dtype == F16:
+            aerr = aerr + R.TINY[F16]
+    else:
+        a, aerr = x.t.to(R.D), None
+    ref = d64.t() @ a
+    gerr = R.product_err(d64.t(), a) + (d64.abs().t() @ aerr if aerr is not None else 0)
+    R.check("gw", gw.t, ref, R.rounded(ref, gw_dtype, gerr))
+    col = d64.sum(0)
+    R.check("gb", gb.t.view(-1), col, (M / 16 + 16) * 2.0 ** -23 * d64.abs().sum(0) + 1e-30)
+
+
+@pytest.mark.parametrize("M,K,N,dtype,act,gw", [
+    (1, 8, 8, BF16, R.GELU, F32), (3, 72, 40, F16, R.NONE, F32), (64, 64, 64, BF16, R.SILU, BF16), (65, 520, 136, F16, R.SIGMOID, F16),
+    (70, 1032, 520, BF16, R.RELU, F32), (129, 256, 1024, F16, R.TANH, F32), (1000, 136, 264, BF16, R.GELU, BF16), (4100, 72, 136, BF16, R.NONE, F32),
+    (2047, 520, 1032, F16, R.SILU, F16)])
+def test_backward_from_eight_bits(ops, M, K, N, dtype, act, gw):
+    _backward(ops, M, K, N, dtype, act, gw)
+
+
+@pytest.mark.parametrize("M,K,N,dtype,act,gw", [
+    (2049, 1288, 1800, BF16, R.GELU, BF16), (1800, 1544, 2056, F16, R.NONE, F32), (2300, 2048, 1536, BF16, R.RELU, F32)])
+def test_backward_pairs(ops, M, K, N, dtype, act, gw):
+    _backward(ops, M, K, N, dtype, act, gw, forms=(lf.LF_FORM_PAIRS, lf.LF_FORM_PAIRS))
+
+
+@pytest.mark.parametrize("M,K,N,dtype,gw", [(33, 136, 72, BF16, F32), (300, 1032, 264, F16, F16), (2100, 1400, 1512, BF16, F32)])
+@pytest.mark.parametrize("ld", [0, 24])
+def test_backward_from_sixteen_bits(ops, M, K, N, dtype, gw, ld):
+    _backward(ops, M, K, N, dtype, R.NONE, gw, eight=False, add=True, ld_extra=ld)
+
+
+def test_weight_gradient_over_many_tokens_keeps_fp32(ops):
+    # 8192 tokens, all terms positive: truncation in the accumulator would show as a bias of 2^-23 per
+    # instruction; chunks of 512 tokens added in registers stay below 32 * 2^-23 plus 16 roundings
+    g = _gen(9)
+    for n_out, n_in in ((64, 72), (2304, 2304)):
+        M = 8192
+        dz = (0.5 + torch.rand(M, n_out, device="cuda", generator=g)).to(BF16)
+        x = (0.5 + torch.rand(M, n_in, device="cuda", generator=g)).to(BF16)
+        gw = torch.empty(n_out, n_in, device="cuda")
+        ops.linear_grad_w(dz, gw, x=x)
+        ref = dz.to(R.D).t() @ x.to(R.D)
+        R.check("gw", gw, ref, (32 + 16) * 2.0 ** -23 * ref)
+
+
+@pytest.mark.parametrize("M,K,N", [(5, 16, 24), (40, 16, 24)])
+@pytest.mark.parametrize("act", [R.GELU, R.SILU, R.SIGMOID, R.TANH, R.NONE])
+def test_gradients_against_central_differences(ops, M, K, N, act):
+    # C = sum(dy * (sigma(x w^T + b))) in 64 bits; the pre-activation goes through 8 bits, so the network
+    # differentiated is the one whose z is the stored value: z = z8 + (x - x0) w^T + ...
+    g = _gen(10 + act)
+    x, w, b = _rand(g, M, K, dtype=BF16), _rand(g, N, K, std=0.4, dtype=BF16), _rand(g, N, std=0.2)
+    dy = _rand(g, M, N, dtype=BF16)
+    y = torch.empty(M, N, dtype=BF16, device="cuda")
+    q, s = torch.empty(M, N, dtype=torch.uint8, device="cuda"), torch.empty(M, _groups(N), dtype=torch.uint8, device="cuda")
+    ops.linear(x, w, y, bias=b, act=act, q=q, s=s)
+    dz, dx = torch.empty_like(y), torch.empty_like(x)
+    gw, gb = torch.empty(N, K, device="cuda"), torch.empty(N, device="cuda")
+    ops.act_backward(dy, q, s, dz, act=act)
+    ops.linear_grad_x(dz, w, dx)
+    ops.linear_grad_w(dz, gw, gb=gb, x=x)
+    ops.sync()
+    z8, x0, w0, d64 = R.unpack8(q, s), x.to(R.D), w.to(R.D), dy.to(R.D)
+
+    def cost(dxv, dwv, dbv):
+        return (d64 * R.act(z8 + dxv @ w0.t() + x0 @ dwv.t() + dbv, act)).sum().item()
+
+    h = 1e-4
+    zx, zw, zb = torch.zeros_like(x0), torch.zeros_like(w0), torch.zeros(N, dtype=R.D, device="cuda")
+    # dz is rounded to bf16, dx once more: 2^-8 of the sums of magnitudes; differences are exact to h^2
+    mag = d64.abs() * R.LIP1[act]
+    for got, zero, bound, slot in ((dx, zx, mag @ w0.abs(), 0), (gw, zw, mag.t() @ x0.abs(), 1), (gb, zb, mag.sum(0), 2)):
+        for i in range(0, zero.numel(), max(1, zero.numel() // 24)):
+            step = [zx, zw, zb]
+            step[slot] = zero.clone()
+            step[slot].view(-1)[i] = h
+            up = cost(*step)
+            step[slot].view(-1)[i] = -h
+            fd = (up - cost(*step)) / (2 * h)
+            assert abs(got.reshape(-1)[i].item() - fd) <= 2.0 ** -8 * bound.reshape(-1)[i].item() + 1e-6, (slot, i)
+
+
+# ---- norm ---------------------------------------------------------------------------------------------
+
+NORM_SHAPES = [(1, 8), (1, 4096), (3, 40), (300, 256), (301, 264), (17, 520), (310, 1032), (5, 2056), (300, 4096), (300, 4104), (9, 8192),
+               (297, 8200), (2, 16384), (299, 16384)]
+
+
+def _norm(ops, M, n, dtype, residual, ckpt, with_y=True, ld=0, eps=1e-5):
+    g = _gen(3 * M + n)
+    x, r = Out(M, n, dtype, n + ld), Out(M, n, dtype, n + 2 * ld)
+    x.t.copy_(_rand(g, M, n, std=2.0, dtype=dtype))
+    r.t.copy_(_rand(g, M, n, dtype=dtype))
+    gain = 1 + _rand(g, n, std=0.2)
+    h, y = Out(M, n, dtype, n + ld), Out(M, n, dtype, n + 3 * ld)
+    q, s = Out(M, n, torch.uint8), Out(M, _groups(n), torch.uint8)
+    ops.rms_norm(x.t, gain, y.t if with_y else None, residual=r.t if residual else None, h=h.t if residual else None,
+                 q=q.t if ckpt else None, s=s.t if ckpt else None, eps=eps)
+    ops.sync()
+    for o in (x, r, h, y, q, s):
+        o.check()
+    h64 = x.t.to(R.D) + (r.t.to(R.D) if residual else 0)
+    ref = h64 / (h64.square().mean(1, keepdim=True) + eps).sqrt() * gain.to(R.D)
+    # the sum of squares has n terms in at most n / 32 + 16 additions per partial sum; half of its error reaches y
+    err = (n / 64 + 16) * 2.0 ** -24 * ref.abs() + 2.0 ** -22 * ref.abs()
+    if residual:
+        R.check("h", h.t, h64, R.rounded(h64, dtype, 2.0 ** -24 * h64.abs()))
+    if with_y:
+        R.check("y", y.t, ref, R.rounded(ref, dtype, err))
+    if ckpt:
+        _check_packed("y8", q.t, s.t, ref, err)
+
+
+@pytest.mark.parametrize("M,n", NORM_SHAPES)
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_norm(ops, M, n, dtype):
+    _norm(ops, M, n, dtype, True, True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("residual,ckpt,with_y,ld", [(False, False, True, 0), (False, True, False, 8), (True, False, True, 16), (True, True, False, 0)])
+def test_norm_options_and_strides(ops, dtype, residual, ckpt, with_y, ld):
+    for M, n in ((4, 1032), (333, 264)):
+        _norm(ops, M, n, dtype, residual, ckpt, with_y, ld)
+
+
+def test_norm_of_zero_rows_and_rows_that_are_not_finite(ops):
+    x = torch.ones(6, 256, dtype=BF16, device="cuda")
+    x[1] = 0
+    x[2, 7] = float("inf")
+    x[3, 9] = float("nan")
+    x[4] = 3e38                       # the sum of squares overflows fp32, as the definition in fp32 does
+    gain = torch.ones(256, device="cuda")
+    y = torch.empty_like(x)
+    q, s = torch.empty(6, 256, dtype=torch.uint8, device="cuda"), torch.empty(6, 8, dtype=torch.uint8, device="cuda")
+    ops.rms_norm(x, gain, y, q=q, s=s, eps=0.0)
+    ops.sync()
+    assert y[0].eq(1).all() and y[5].eq(1).all()
+    assert y[1].isnan().all() and y[2].isnan().any() and y[3].isnan().all() and y[4].eq(0).all()    # 0 / 0, inf, NaN, 3e38 / inf
+    assert bool((s[1] == 255).all()) and bool((s[3] == 255).all()) and bool((s[4] == 0).all())
+    ops.rms_norm(x, gain, y, q=q, s=s, eps=1e-6)
+    ops.sync()
+    assert y[1].eq(0).all() and bool((q[1] == 0).all()) and bool((s[1] == 0).all())
+    # h and y may be written over x and residual
+    a, b = torch.randn(5, 264, device="cuda").to(BF16), torch.randn(5, 264, device="cuda").to(BF16)
+    h, y = torch.empty_like(a), torch.empty_like(a)
+    g = torch.rand(264, device="cuda")
+    ops.rms_norm(a, g, y, residual=b, h=h)
+    a2, b2 = a.clone(), b.clone()
+    ops.rms_norm(a2, g, a2, residual=b2, h=b2)
+    assert torch.equal(a2, y) and torch.equal(b2, h)
+
+
+def _norm_backward(ops, M, n, dtype, dres, dgain=True, ld=0, eps=1e-5):
+    g = _gen(5 * M + n)
+    h, dy, r = Out(M, n, dtype, n + ld), Out(M, n, dtype, n + 2 * ld), Out(M, n, dtype, n + ld)
+    h.t.copy_(_rand(g, M, n, std=2.0, dtype=dtype))
+    dy.t.copy_(_rand(g, M, n, std=0.3, dtype=dtype))
+    r.t.copy_(_rand(g, M, n, std=0.3, dtype=dtype))
+    gain = 1 + _rand(g, n, std=0.2)
+    dh, dg = Out(M, n, dtype, n + 3 * ld), Out(1, n, F32)
+    ops.rms_norm_backward(dy.t, h.t, gain, dh.t, dg.t.view(-1) if dgain else None, dres=r.t if dres else None, eps=eps)
+    ops.sync()
+    for o in (h, dy, r, dh, dg):
+        o.check()
+    h64, y64, g64 = h.t.to(R.D), dy.t.to(R.D), gain.to(R.D)
+    rstd = (h64.square().mean(1, keepdim=True) + eps).rsqrt()
+    hn, u = h64 * rstd, y64 * g64
+    ref = rstd * (u - hn * (u * hn).mean(1, keepdim=True))
+    # both row sums have errors of (n / 32 + 16) additions, relative to their sums of magnitudes
+    k = (n / 32 + 16) * 2.0 ** -24
+    err = k * (ref.abs() + rstd * hn.abs() * (u * hn).abs().mean(1, keepdim=True) * 2) + 2.0 ** -21 * rstd * (u.abs() + hn.abs() * (u * hn).abs().mean(1, keepdim=True))
+    if dres:
+        ref = ref + r.t.to(R.D)
+        err = err + 2.0 ** -24 * ref.abs()
+    R.check("dh", dh.t, ref, R.rounded(ref, dtype, err))
+    if dgain:
+        terms = (y64 * hn).abs().sum(0)
+        R.check("dgain", dg.t.view(-1), (y64 * hn).sum(0), (M / 8 + 340 + n / 64) * 2.0 ** -24 * terms + 1e-30)
+    else:
+        assert dg.t.isnan().all()
+
+
+@pytest.mark.parametrize("M,n", NORM_SHAPES + [(2000, 1024), (5000, 72)])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_norm_backward(ops, M, n, dtype):
+    _norm_backward(ops, M, n, dtype, True)
+
+
+@pytest.mark.parametrize("dres,dgain,ld", [(False, True, 8), (True, False, 0), (False, False, 16)])
+def test_norm_backward_options_and_strides(ops, dres, dgain, ld):
+    for M, n, dtype in ((4, 1032, BF16), (333, 264, F32)):
+        _norm_backward(ops, M, n, dtype, dres, dgain, ld)
+
+
+def test_norm_backward_against_central_differences(ops):
+    g = _gen(11)
+    h, dy, gain = _rand(g, 3, 40), _rand(g, 3, 40), 1 + _rand(g, 40, std=0.2)
+    dh, dg = torch.empty_like(h), torch.empty(40, device="cuda")
+    ops.rms_norm_backward(dy, h, gain, dh, dg, eps=1e-3)
+    ops.sync()
+    h64, y64, g64 = h.to(R.D), dy.to(R.D), gain.to(R.D)
+
+    def cost(hv, gv):
+        return (y64 * hv / (hv.square().mean(1, keepdim=True) + 1e-3).sqrt() * gv).sum().item()
+
+    for i in range(0, 120, 7):
+        e = torch.zeros(120, dtype=R.D, device="cuda")
+        e[i] = 1e-5
+        e = e.view(3, 40)
+        fd = (cost(h64 + e, g64) - cost(h64 - e, g64)) / 2e-5
+        assert abs(dh.view(-1)[i].item() - fd) <= 1e-5 * (1 + abs(fd))
+    for i in range(0, 40, 5):
+        e = torch.zeros(40, dtype=R.D, device="cuda")
+        e[i] = 1e-5
+        fd = (cost(h64, g64 + e) - cost(h64, g64 - e)) / 2e-5
+        assert abs(dg[i].item() - fd) <= 1e-5 * (1 + abs(fd))
+
+
+# ---- 8 bits -------------------------------------------------------------------------------------------
+
+def _awkward(g, M, n, dtype):
+    """Magnitudes over the whole range of the type, zeros, group maxima on and next to 448 * 2^e."""
+    big = {BF16: 120, F16: 14, F32: 120}[dtype]
+    low = {BF16: -126, F16: -20, F32: -140}[dtype]
+    v = _rand(g, M, n) * torch.exp2(torch.empty(M, 1, device="cuda").uniform_(low, big, generator=g))
+    v = v * torch.exp2(torch.empty(M, n, device="cuda").uniform_(-12, 0, generator=g))
+    v[:, ::5] = 0
+    if M > 2:
+        v[1] = 0
+        v[2] = torch.tensor([448.0, 449.0, 447.0, 1.0], device="cuda").repeat((n + 3) // 4)[:n]
+    return v.to(dtype)
+
+
+@pytest.mark.parametrize("M,n", [(1, 8), (3, 32), (4, 40), (33, 264), (300, 1032), (5, 4096), (1000, 2056)])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_pack_and_unpack_are_the_definition(ops, M, n, dtype):
+    g = _gen(M + n)
+    for ld in (0, 8):
+        x = Out(M, n, dtype, n + ld)
+        x.t.copy_(_awkward(g, M, n, dtype))
+        q, s, v = Out(M, n, torch.uint8), Out(M, _groups(n), torch.uint8), Out(M, n, dtype, n + 2 * ld)
+        ops.pack8(x.t, q.t, s.t)
+        ops.unpack8(q.t, s.t, v.t)
+        ops.sync()
+        for o in (x, q, s, v):
+            o.check()
+        rq, rs = R.pack8(x.t)
+        assert torch.equal(s.t, rs)
+        same = (q.t == rq) | ((q.t & 0x7F == 0) & (rq & 0x7F == 0))      # either zero
+        assert bool(same.all())
+        big = float(torch.finfo(dtype).max)
+        assert torch.equal(v.t, R.unpack8(q.t, s.t).clamp(-big, big).to(dtype))
+
+
+def test_groups_that_are_not_finite_read_back_as_nan(ops):
+    for dtype in (BF16, F16, F32):
+        x = torch.ones(2, 72, dtype=dtype, device="cuda")
+        x[0, 33] = float("inf")
+        x[1, 70] = float("nan")
+        q, s, v = torch.empty(2, 72, dtype=torch.uint8, device="cuda"), torch.empty(2, 3, dtype=torch.uint8, device="cuda"), torch.empty_like(x)
+        ops.pack8(x, q, s)
+        ops.unpack8(q, s, v)
+        ops.sync()
+        assert s.tolist() == [[119, 255, 119], [119, 119, 255]]
+        assert v[0, 32:64].isnan().all() and v[1, 64:].isnan().all()
+        assert v[0, :32].eq(1).all() and v[0, 64:].eq(1).all() and v[1, :64].eq(1).all()
+
+
+@pytest.mark.parametrize("act", [R.NONE, R.SILU, R.GELU, R.SIGMOID, R.TANH, R.RELU])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_activation_and_derivative_from_eight_bits(ops, act, dtype):
+    g = _gen(act)
+    for M, n in ((3, 40), (257, 1032)):
+        z = _rand(g, M, n, std=4.0)
+        z[0, :8] = torch.tensor([0.0, -0.0, 30.0, -30.0, 100.0, -100.0, 8.0, -8.0])
+        q, s = R.pack8(z)
+        v = R.unpack8(q, s)
+        a, dy, dz = Out(M, n, dtype, n + 8), _rand(g, M, n, dtype=dtype), Out(M, n, dtype, n + 16)
+        ops.unpack8(q, s, a.t, act=act)
+        ops.act_backward(dy, q, s, dz.t, act=act)
+        ops.sync()
+        a.check(); dz.check()
+        f = 1e-6 if dtype == F32 else 8e-6      # correctly scaled functions; special-function unit
+        ref = R.act(v, act)
+        R.check("a", a.t, ref, R.rounded(ref, dtype, (f + R.exponent_err(v, act)) * ref.abs() + 1e-37))
+        ref = dy.to(R.D) * R.act_prime(v, act)
+        # sigma' is made of terms up to 1 + |z| that cancel in the tails
+        R.check("dz", dz.t, ref, R.rounded(ref, dtype, f * dy.to(R.D).abs() * (1 + v.abs()) * (2 if act in (R.TANH, R.GELU) else 1)))
+
+
+# ---- empty inputs, large offsets, streams, refusals, waits ----------------------------------------------
+
+def test_no_tokens(ops):
+    e = lambda n, t=BF16: torch.empty(0, n, dtype=t, device="cuda")   # noqa: E731
+    w, u8 = torch.ones(16, 24, dtype=BF16, device="cuda"), torch.uint8
+    ops.linear(e(24), w, e(16), q=e(16, u8), s=e(1, u8))
+    ops.linear_grad_x(e(16), w, e(24), q=e(24, u8), s=e(1, u8), act=R.GELU)
+    for t in (F32, BF16):
+        gw, gb = torch.full((16, 24), 7.0, dtype=t, device="cuda"), torch.full((16,), 7.0, device="cuda")
+        ops.linear_grad_w(e(16), gw, gb=gb, x=e(24))
+        assert gw.eq(0).all() and gb.eq(0).all()
+    ops.rms_norm(e(24), torch.ones(24, device="cuda"), e(24))
+    dg = torch.full((24,), 7.0, device="cuda")
+    ops.rms_norm_backward(e(24), e(24), torch.ones(24, device="cuda"), e(24), dg)
+    assert dg.eq(0).all()
+    ops.pack8(e(24), e(24, u8), e(1, u8))
+    ops.unpack8(e(24, u8), e(1, u8), e(24))
+    ops.act_backward(e(24), e(24, u8), e(1, u8), e(24), act=R.RELU)
+    ops.sync()
+
+
+def test_offsets_beyond_32_bits(ops):
+    # 140000 x 16384 elements are more than 2^31; the last rows are compared
+    M, N, K = 140000, 16384, 8
+    g = _gen(12)
+    x, w = _rand(g, M, K, dtype=BF16), _rand(g, N, K, std=0.3, dtype=BF16)
+    y = torch.empty(M, N, dtype=BF16, device="cuda")
+    q, s = torch.empty(M, N, dtype=torch.uint8, device="cuda"), torch.empty(M, N // 32, dtype=torch.uint8, device="cuda")
+    ops.linear(x, w, y, q=q, s=s)
+    ops.sync()
+    last = slice(M - 64, M)
+    ref = x[last].to(R.D) @ w.to(R.D).t()
+    err = R.product_err(x[last].to(R.D), w.to(R.D).t())
+    R.check("y", y[last], ref, R.rounded(ref, BF16, err))
+    _check_packed("z8", q[last], s[last], ref, err)
+    del q, s
+    gain = torch.ones(N, device="cuda")
+    n = torch.empty_like(y)
+    q, s = torch.empty(M, N, dtype=torch.uint8, device="cuda"), torch.empty(M, N // 32, dtype=torch.uint8, device="cuda")
+    ops.rms_norm(y, gain, n, q=q, s=s)
+    ops.sync()
+    h = y[last].to(R.D)
+    ref = h / (h.square().mean(1, keepdim=True) + 1e-5).sqrt()
+    R.check("norm", n[last], ref, R.rounded(ref, BF16, 1e-4 * ref.abs()))
+    ops.rms_norm_backward(n, y, gain, n)
+    ops.unpack8(q, s, y)
+    ops.sync()
+    assert torch.equal(y[last], R.unpack8(q[last], s[last]).to(BF16))
+    assert n[last].isfinite().all()
+
+
+def test_work_goes_to_the_stream_that_was_set():
+    st = torch.cuda.Stream()
+    M, K, N = 300, 512, 264
+    g = _gen(13)
+    x, w = _rand(g, M, K, dtype=BF16), _rand(g, N, K, std=0.05, dtype=BF16)
+    y, y2 = (torch.zeros(M, N, dtype=BF16, device="cuda") for _ in range(2))
+    torch.cuda.synchronize()
+    with lf.Operators(stream=st.cuda_stream) as o:
+        graph = torch.cuda.CUDAGraph()          # calls allocate nothing, so they can be captured
+        o.linear(x, w, y)
+        st.synchronize()
+        with torch.cuda.graph(graph, stream=st):
+            o.set_stream(torch.cuda.current_stream().cuda_stream)
+            o.linear(x, w, y2)
+        assert y2.eq(0).all()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2) and bool((y != 0).any())
+        o.set_stream(None)
+
+
+@pytest.mark.parametrize("M,K,N", [(200, 1024, 264), (2049, 512, 1288)])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(M, K, N):
+    g = _gen(14)
+    x, w = _rand(g, M, K, dtype=BF16), _rand(g, N, K, std=0.05, dtype=BF16)
+    y, y2 = (torch.empty(M, N, dtype=BF16, device="cuda") for _ in range(2))
+    with lf.Operators() as o:
+        o.linear(x, w, y)
+        o.sync()
+        o.set_option(lf.LF_OPT_WAIT_BUDGET_US, 20000)
+        o.set_option(lf.LF_OPT_WITHHOLD, 1)
+        o.linear(x, w, y2)
+        assert lf.lf_ops_sync(o._h) == lf.LF_ETIMEOUT
+        assert o.stats()["device_status"] != 0
+        o.set_option(lf.LF_OPT_WITHHOLD, 0)
+        o.linear(x, w, y2)
+        o.sync()
+        assert o.stats()["device_status"] == 0
+        assert torch.equal(y, y2)
+
+
+def test_refusals(ops):
+    t = lambda *s, d=BF16: torch.zeros(*s, dtype=d, device="cuda")   # noqa: E731
+    u8 = torch.uint8
+    x, w, y = t(4, 64), t(32, 64), t(4, 32)
+
+    def refused(status, f, *a, **k):
+        with pytest.raises(lf.LeapfrogError) as e:
+            f(*a, **k)
+        assert e.value.status == status, e.value
+
+    for bad in (t(4, 64, d=F32), t(4, 64, d=R.D), t(4, 72), t(64), x.cpu(), t(64, 4).t()):
+        refused(lf.LF_EINVAL, ops.linear, bad, w, y)
+    refused(lf.LF_EINVAL, ops.linear, x, w, t(4, 32, d=F16))
+    refused(lf.LF_EINVAL, ops.linear, x, w, t(5, 32))
+    refused(lf.LF_EINVAL, ops.linear, x, w, y, bias=t(32))                       # bias is float32
+    refused(lf.LF_EINVAL, ops.linear, x, w, y, act=6)
+    refused(lf.LF_EINVAL, ops.linear, x, w, y, act=-1)
+    refused(lf.LF_EINVAL, ops.linear, t(4, 60), t(32, 60), y)                    # width not a multiple of 8
+    refused(lf.LF_EINVAL, ops.linear, t(4, 68)[:, :64], w, y)                    # rows not 16-byte aligned
+    refused(lf.LF_EALIGN, ops.linear, t(4 * 64 + 8)[4:260].view(4, 64), w, y)
+    refused(lf.LF_ENULL, ops.linear, x, w, y, q=t(4, 32, d=u8))
+    refused(lf.LF_EINVAL, ops.linear, x, w, y, q=t(4, 32, d=u8), s=t(4, 2, d=u8))
+    refused(lf.LF_EINVAL, ops.linear, x, t(32, 64)[:, :64].t().contiguous(), y)
+    dz, dx, gw = t(4, 32), t(4, 64), t(32, 64, d=F32)
+    q, s = t(4, 64, d=u8), t(4, 2, d=u8)
+    refused(lf.LF_EINVAL, ops.linear_grad_x, dz, w, dx, act=R.GELU)              # sigma' needs z
+    refused(lf.LF_EINVAL, ops.linear_grad_w, dz, gw, x=x, q=q, s=s)              # one form of the input
+    refused(lf.LF_EINVAL, ops.linear_grad_w, dz, gw, x=x, act=R.GELU)
+    refused(lf.LF_ENULL, ops.linear_grad_w, dz, gw)
+    refused(lf.LF_EINVAL, ops.linear_grad_w, dz, t(32, 64, d=F16), x=x)
+    with lf.Operators() as small:
+        refused(lf.LF_ECAPACITY, small.linear_grad_w, dz, gw, q=q, s=s)
+        small.linear_grad_w(dz, gw, x=x)
+        small.sync()
+    gain = t(64, d=F32)
+    refused(lf.LF_ENULL, ops.rms_norm, x, gain)                                  # nothing to write
+    refused(lf.LF_EINVAL, ops.rms_norm, x, gain, t(4, 64), eps=-1.0)
+    refused(lf.LF_EINVAL, ops.rms_norm, x, gain, t(4, 64), eps=float("nan"))
+    refused(lf.LF_EINVAL, ops.rms_norm, t(1, 16392), t(16392, d=F32), t(1, 16392))
+    refused(lf.LF_EINVAL, ops.rms_norm_backward, x, x, t(72, d=F32), x)
+    refused(lf.LF_ENULL, ops.pack8, x, q, None)
+    refused(lf.LF_EINVAL, ops.unpack8, q, s, x, act=17)
+    refused(lf.LF_EINVAL, ops.act_backward, x, q, s, t(4, 64, d=F16))
+    refused(lf.LF_EINVAL, ops.set_option, lf.LF_OPT_WITHHOLD, 2)
+    refused(lf.LF_EINVAL, ops.set_option, lf.LF_OPT_VARIANT, 1)
+    refused(lf.LF_EINVAL, lf.Operators, 1024)
+    ops.sync()
