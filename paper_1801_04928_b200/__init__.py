@@ -24,6 +24,8 @@ def __getattr__(name):
     if name in ("build", "binding"):
         return importlib.import_module("." + name, __name__)
     try:
-        return getattr(_binding(), name)
+        value = getattr(_binding(), name)
+        globals()[name] = value         # the next look-up finds it without coming here
+        return value
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None

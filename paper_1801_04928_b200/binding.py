@@ -429,17 +429,8 @@ def lf_act_backward(ops, dtype: int, act: int, tokens: int, n: int, dy, ld_dy: i
     return _lib.lf_act_backward(ops, dtype, act, tokens, n, _ptr(dy), ld_dy, _ptr(q), _ptr(s), _ptr(dz), ld_dz)
 
 
-_TYPES = {}              # torch dtype -> enum lf_dtype, filled on first use
-
-
-def _types() -> dict:
-    import torch
-    _TYPES.update({torch.float32: LF_F32, torch.bfloat16: LF_BF16, torch.float16: LF_F16, torch.uint8: -1})
-    return _TYPES
-
-
-def _refuse(where: str, name: str, problem: str):
-    raise LeapfrogError(LF_EINVAL, f"{where}: argument {name}: {problem}")
+def _entry(name: str) -> int:
+    return ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value
 
 
 class Operators:
@@ -449,6 +440,7 @@ class Operators:
     the width (a slice of columns of a wider matrix).  Results go into the tensors that are passed in.
     Raises :class:`LeapfrogError` on any non-zero status and on tensors whose type, device, shape or
     layout does not fit.  ``stream``: a cudaStream_t as an int; None is the legacy default stream.
+    The tensors are checked and turned into C arguments by the native module ``_marshal``.
     """
 
     def __init__(self, workspace_bytes: int | None = None, stream: int | None = None):
@@ -456,13 +448,22 @@ class Operators:
         if rc != LF_OK:
             self._h = None
             raise LeapfrogError(rc, "lf_ops_create")
-        self._types = _types()
+        import torch  # noqa: F401  (its libraries have to be loaded before the module that uses them)
+        from . import _marshal
+        self._m = _marshal
+        self._a = self._h.value
         if stream is not None:
             self.set_stream(stream)
 
     def _check(self, rc: int, where: str):
         if rc != LF_OK:
             raise LeapfrogError(rc, where, lf_ops_last_cuda_error(self._h))
+
+    def _raise(self, where: str, failed):
+        status, problem = failed
+        if problem is not None:
+            raise LeapfrogError(status, f"{where}: {problem}")
+        raise LeapfrogError(status, where, lf_ops_last_cuda_error(self._h) if status == LF_ECUDA else 0)
 
     def set_stream(self, cuda_stream: int | None):
         self._check(lf_ops_set_stream(self._h, cuda_stream), "lf_ops_set_stream")
@@ -478,171 +479,59 @@ class Operators:
         self._check(rc, "lf_ops_get_stats")
         return d
 
-    # -- marshalling: what a tensor has to be; answers its address (and row stride) --
-    def _type(self, t, name: str, where: str) -> int:
-        code = self._types.get(t.dtype, -1)
-        if code < 0:
-            _refuse(where, name, f"dtype {t.dtype} (float32, bfloat16 or float16 needed)")
-        return code
-
-    @staticmethod
-    def _mat(t, rows: int, cols: int, dtype, name: str, where: str):
-        """(address, leading dimension) of a [rows, cols] matrix."""
-        if t is None:
-            return None, 0
-        if t.dtype is dtype and t.is_cuda:
-            shape = t.shape
-            if len(shape) == 2 and shape[0] == rows and shape[1] == cols:
-                step, unit = t.stride()
-                if unit == 1 and (step >= cols or rows <= 1):
-                    return t.data_ptr(), (step if rows > 1 else 0)
-                _refuse(where, name, f"strides {tuple(t.stride())} (unit stride along rows that do not overlap needed)")
-            _refuse(where, name, f"shape {tuple(shape)}, ({rows}, {cols}) needed")
-        _refuse(where, name, f"{t.dtype} on {t.device} ({dtype} on a CUDA device needed)")
-
-    @staticmethod
-    def _flat(t, n: int, dtype, name: str, where: str):
-        """Address of a contiguous tensor of n elements."""
-        if t is None:
-            return None
-        if t.dtype is dtype and t.is_cuda and t.numel() == n and t.is_contiguous():
-            return t.data_ptr()
-        _refuse(where, name, f"{t.dtype} {tuple(t.shape)} on {t.device}, contiguous: {t.is_contiguous()} "
-                             f"({n} contiguous elements of {dtype} on a CUDA device needed)")
-
-    def _eight(self, q, s, rows: int, cols: int, where: str):
-        if q is None and s is None:
-            return None, None
-        import torch
-        return (self._flat(q, rows * cols, torch.uint8, "q", where),
-                self._flat(s, rows * ((cols + 31) // 32), torch.uint8, "s", where))
-
-    @staticmethod
-    def _shape(t, name: str, where: str):
-        if t.dim() != 2:
-            _refuse(where, name, f"{t.dim()} dimensions (2 needed)")
-        return t.shape
-
-    def linear(self, x, w, y, bias=None, residual=None, act: int = LF_ACT_NONE, q=None, s=None):
+    def linear(self, x, w, y, bias=None, residual=None, act: int = LF_ACT_NONE, q=None, s=None, _f=_entry("lf_linear")):
         """y = act(x w^T + bias) + residual; with q and s also z = x w^T + bias in 8 bits."""
-        where = "lf_linear"
-        code = self._type(x, "x", where)
-        m, k = self._shape(x, "x", where)
-        n = self._shape(w, "w", where)[0]
-        t, f32 = x.dtype, _FLOAT32 or self._f32()
-        xp, ldx = self._mat(x, m, k, t, "x", where)
-        rp, ldr = self._mat(residual, m, n, t, "residual", where)
-        yp, ldy = self._mat(y, m, n, t, "y", where)
-        self._w(w, n, k, where)
-        qp, sp = self._eight(q, s, m, n, where)
-        a = lf_linear_args(code, act, m, k, n, xp, ldx, self._flat(w, n * k, t, "w", where), self._flat(bias, n, f32, "bias", where),
-                           rp, ldr, yp, ldy, qp, sp)
-        self._check(_lib.lf_linear(self._h, ctypes.addressof(a)), where)
+        failed = self._m.linear(_f, self._a, x, w, y, bias, residual, act, q, s)
+        if failed is not None:
+            self._raise("lf_linear", failed)
 
-    def linear_grad_x(self, dz, w, dx, q=None, s=None, act: int = LF_ACT_NONE, add=None):
+    def linear_grad_x(self, dz, w, dx, q=None, s=None, act: int = LF_ACT_NONE, add=None, _f=_entry("lf_linear_grad_x")):
         """dx = (dz w) * act'(z) + add, z [tokens, n_in] given in 8 bits by q and s."""
-        where = "lf_linear_grad_x"
-        code = self._type(dz, "dz", where)
-        m, n = self._shape(dz, "dz", where)
-        k = self._shape(w, "w", where)[1]
-        t = dz.dtype
-        zp, ldz = self._mat(dz, m, n, t, "dz", where)
-        ap, lda = self._mat(add, m, k, t, "add", where)
-        xp, ldx = self._mat(dx, m, k, t, "dx", where)
-        self._w(w, n, k, where)
-        qp, sp = self._eight(q, s, m, k, where)
-        a = lf_linear_grad_x_args(code, act, m, k, n, zp, ldz, self._flat(w, n * k, t, "w", where), qp, sp, ap, lda, xp, ldx)
-        self._check(_lib.lf_linear_grad_x(self._h, ctypes.addressof(a)), where)
+        failed = self._m.linear_grad_x(_f, self._a, dz, w, dx, q, s, act, add)
+        if failed is not None:
+            self._raise("lf_linear_grad_x", failed)
 
-    def linear_grad_w(self, dz, gw, gb=None, x=None, q=None, s=None, act: int = LF_ACT_NONE):
+    def linear_grad_w(self, dz, gw, gb=None, x=None, q=None, s=None, act: int = LF_ACT_NONE, _f=_entry("lf_linear_grad_w")):
         """gw = dz^T x, gb = column sums of dz; x given, or act(z) from 8 bits.  gw: float32 or dz's type."""
-        where = "lf_linear_grad_w"
-        code = self._type(dz, "dz", where)
-        gcode = self._type(gw, "gw", where)
-        m, n = self._shape(dz, "dz", where)
-        k = self._shape(gw, "gw", where)[1]
-        t, f32 = dz.dtype, _FLOAT32 or self._f32()
-        zp, ldz = self._mat(dz, m, n, t, "dz", where)
-        xp, ldx = self._mat(x, m, k, t, "x", where)
-        self._w(gw, n, k, where, "gw")
-        qp, sp = self._eight(q, s, m, k, where)
-        a = lf_linear_grad_w_args(code, gcode, act, m, k, n, zp, ldz, xp, ldx, qp, sp, self._flat(gw, n * k, gw.dtype, "gw", where),
-                                  self._flat(gb, n, f32, "gb", where))
-        self._check(_lib.lf_linear_grad_w(self._h, ctypes.addressof(a)), where)
+        failed = self._m.linear_grad_w(_f, self._a, dz, gw, gb, x, q, s, act)
+        if failed is not None:
+            self._raise("lf_linear_grad_w", failed)
 
-    def rms_norm(self, x, gain, y=None, residual=None, h=None, q=None, s=None, eps: float = 1e-5):
+    def rms_norm(self, x, gain, y=None, residual=None, h=None, q=None, s=None, eps: float = 1e-5, _f=_entry("lf_rms_norm")):
         """h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain, in x's type and / or in 8 bits (q, s)."""
-        where = "lf_rms_norm"
-        code = self._type(x, "x", where)
-        m, n = self._shape(x, "x", where)
-        t = x.dtype
-        xp, ldx = self._mat(x, m, n, t, "x", where)
-        rp, ldr = self._mat(residual, m, n, t, "residual", where)
-        hp, ldh = self._mat(h, m, n, t, "h", where)
-        yp, ldy = self._mat(y, m, n, t, "y", where)
-        qp, sp = self._eight(q, s, m, n, where)
-        a = lf_rms_norm_args(code, m, n, eps, xp, ldx, rp, ldr, self._flat(gain, n, _FLOAT32 or self._f32(), "gain", where),
-                             hp, ldh, yp, ldy, qp, sp)
-        self._check(_lib.lf_rms_norm(self._h, ctypes.addressof(a)), where)
+        failed = self._m.rms_norm(_f, self._a, x, gain, y, residual, h, q, s, eps)
+        if failed is not None:
+            self._raise("lf_rms_norm", failed)
 
-    def rms_norm_backward(self, dy, h, gain, dh, dgain=None, dres=None, eps: float = 1e-5):
+    def rms_norm_backward(self, dy, h, gain, dh, dgain=None, dres=None, eps: float = 1e-5, _f=_entry("lf_rms_norm_backward")):
         """Gradient of y = h / sqrt(mean(h^2) + eps) * gain with respect to h (plus dres) and gain."""
-        where = "lf_rms_norm_backward"
-        code = self._type(h, "h", where)
-        m, n = self._shape(h, "h", where)
-        t, f32 = h.dtype, _FLOAT32 or self._f32()
-        yp, ldy = self._mat(dy, m, n, t, "dy", where)
-        hp, ldh = self._mat(h, m, n, t, "h", where)
-        rp, ldr = self._mat(dres, m, n, t, "dres", where)
-        dp, ldd = self._mat(dh, m, n, t, "dh", where)
-        a = lf_rms_norm_backward_args(code, m, n, eps, yp, ldy, hp, ldh, self._flat(gain, n, f32, "gain", where), rp, ldr, dp, ldd,
-                                      self._flat(dgain, n, f32, "dgain", where))
-        self._check(_lib.lf_rms_norm_backward(self._h, ctypes.addressof(a)), where)
+        failed = self._m.rms_norm_backward(_f, self._a, dy, h, gain, dh, dgain, dres, eps)
+        if failed is not None:
+            self._raise("lf_rms_norm_backward", failed)
 
-    def pack8(self, x, q, s):
+    def pack8(self, x, q, s, _f=_entry("lf_pack8")):
         """x [tokens, n] in 8 bits: q [tokens, n], s [tokens, ceil(n / 32)]."""
-        where = "lf_pack8"
-        code = self._type(x, "x", where)
-        m, n = self._shape(x, "x", where)
-        xp, ldx = self._mat(x, m, n, x.dtype, "x", where)
-        qp, sp = self._eight(q, s, m, n, where)
-        self._check(_lib.lf_pack8(self._h, code, m, n, xp, ldx, qp, sp), where)
+        failed = self._m.pack8(_f, self._a, x, q, s)
+        if failed is not None:
+            self._raise("lf_pack8", failed)
 
-    def unpack8(self, q, s, x, act: int = LF_ACT_NONE):
+    def unpack8(self, q, s, x, act: int = LF_ACT_NONE, _f=_entry("lf_unpack8")):
         """x = act(value of q and s)."""
-        where = "lf_unpack8"
-        code = self._type(x, "x", where)
-        m, n = self._shape(x, "x", where)
-        xp, ldx = self._mat(x, m, n, x.dtype, "x", where)
-        qp, sp = self._eight(q, s, m, n, where)
-        self._check(_lib.lf_unpack8(self._h, code, act, m, n, qp, sp, xp, ldx), where)
+        failed = self._m.unpack8(_f, self._a, q, s, x, act)
+        if failed is not None:
+            self._raise("lf_unpack8", failed)
 
-    def act_backward(self, dy, q, s, dz, act: int = LF_ACT_NONE):
+    def act_backward(self, dy, q, s, dz, act: int = LF_ACT_NONE, _f=_entry("lf_act_backward")):
         """dz = dy * act'(value of q and s)."""
-        where = "lf_act_backward"
-        code = self._type(dy, "dy", where)
-        m, n = self._shape(dy, "dy", where)
-        yp, ldy = self._mat(dy, m, n, dy.dtype, "dy", where)
-        zp, ldz = self._mat(dz, m, n, dy.dtype, "dz", where)
-        qp, sp = self._eight(q, s, m, n, where)
-        self._check(_lib.lf_act_backward(self._h, code, act, m, n, yp, ldy, qp, sp, zp, ldz), where)
-
-    @staticmethod
-    def _f32():
-        global _FLOAT32
-        import torch
-        _FLOAT32 = torch.float32
-        return _FLOAT32
-
-    @staticmethod
-    def _w(w, n: int, k: int, where: str, name: str = "w"):
-        if w.dim() != 2 or w.shape[0] != n or w.shape[1] != k:
-            _refuse(where, name, f"shape {tuple(w.shape)}, ({n}, {k}) needed")
+        failed = self._m.act_backward(_f, self._a, dy, q, s, dz, act)
+        if failed is not None:
+            self._raise("lf_act_backward", failed)
 
     def close(self):
         if self._h is not None:
             lf_ops_destroy(self._h)
             self._h = None
+            self._a = 0               # further calls answer LF_ENULL
 
     def __enter__(self):
         return self

@@ -1,4 +1,5 @@
-"""Build ``libleapfrog.so`` in-tree with nvcc for sm_100a.
+"""Build ``libleapfrog.so`` in-tree with nvcc for sm_100a, and ``_marshal.so`` with g++ (tensor marshalling
+of the layer operators, against the installed torch's headers).
 
 Run as ``python -m paper_1801_04928_b200.build`` or call :func:`build`.  The shared library
 lands beside this file; nothing is installed elsewhere and nothing is compiled at import time.
@@ -24,6 +25,29 @@ SOURCES = ["lf_api.cu", "lf_kernels_b1.cu", "lf_kernels_batch.cu", "lf_persisten
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v", "-I", INCLUDE, "-I", CSRC]
+
+
+MARSHAL_SRC = os.path.join(CSRC, "lf_marshal.cpp")
+MARSHAL = os.path.join(PKG, "_marshal.so")
+
+
+def _build_marshal(force: bool) -> None:
+    if not force and not _stale(MARSHAL, [MARSHAL_SRC, os.path.join(INCLUDE, "leapfrog.h")]):
+        return
+    import sysconfig
+    import importlib.util
+    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
+    inc = os.path.join(torch_dir, "include")
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    # no run path: torch is loaded before the module, which finds its libraries by name
+    r = subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", MARSHAL_SRC, "-o", tmp, "-I", INCLUDE,
+                        "-I", sysconfig.get_paths()["include"], "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"),
+                        "-I", os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"),
+                        "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10"],
+                       capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on lf_marshal.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, MARSHAL)
 
 
 def _nvcc() -> str:
@@ -61,8 +85,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
                 sys.stderr.write(r.stderr)
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        marshal = ex.submit(_build_marshal, force)
         objs = list(ex.map(compile_one, SOURCES))
+        marshal.result()
     if force or _stale(LIB, objs):
         tmp = LIB + f".tmp{os.getpid()}"
         r = subprocess.run([nvcc, "-shared", "-o", tmp, *objs, "-gencode",

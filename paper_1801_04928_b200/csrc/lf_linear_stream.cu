@@ -129,7 +129,9 @@ __global__ void __launch_bounds__(SR_WARPS * 32, 2) k_linear_stream(const lf_pro
                 if (in) p.q[(size_t)tok * p.N + col] = (unsigned char)(to_e4m3x4(v * inv_scale(b), 0.f, 0.f, 0.f) & 0xFFu);
                 if (lane == 0) p.s[(size_t)tok * ((p.N + 31) / 32) + (n0 >> 5)] = (unsigned char)b;
             }
-            v = act<true>(v, p.act);
+            float two[2] = {v, 0.f};
+            act_n<true, 2>(two, p.act);
+            v = two[0];
             if (in) {
                 if (p.add) v += (float)static_cast<const T*>(p.add)[(size_t)tok * p.ld_add + col];
                 static_cast<T*>(p.d)[(size_t)tok * p.ld_d + col] = (T)v;

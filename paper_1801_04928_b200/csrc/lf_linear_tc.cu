@@ -34,16 +34,22 @@ constexpr int LT_STAGE_BYTES = 2 * LT_BLOCK_BYTES;
 constexpr int LT_STAGES = 6;
 constexpr int LT_THREADS = 320;                          // producer, issuer, eight epilogue warps
 constexpr int LT_CHUNK = 8;                              // K stages per accumulator of an fp32 result
+constexpr int LP_RING_BYTES = LT_STAGES * LT_STAGE_BYTES;   // pairs: six stages of two blocks, or four of three
 constexpr int LP_EPI_BYTES = 8 * 4096;                   // pairs: 32 rows x 128 bytes per epilogue warp
+constexpr int LP_THREADS = 384;                          // pairs: a warpgroup with producer and issuer, two for the epilogue
+constexpr int LP_REGS_LOW = 56, LP_REGS_HIGH = 224;      // 56 + 2 * 224 = 3 * 168: what the block was launched with
+constexpr int LP_AHEAD = 4;                              // 512 x 256 tiles: stages by which block 0 runs ahead
 constexpr int LS_LD = 132;                               // split tiles: padded row of the fp32 tile in shared memory
-constexpr size_t LP_SMEM = (size_t)LT_STAGES * LT_STAGE_BYTES + LP_EPI_BYTES + 1024 + 512;
-constexpr size_t LS_SMEM = (size_t)LT_STAGES * LT_STAGE_BYTES + 1024 + 512;
-static_assert(128 * LS_LD * 4 <= LT_STAGES * LT_STAGE_BYTES, "the fp32 tile overlays the operand ring");
+constexpr size_t LP_SMEM = (size_t)LP_RING_BYTES + LP_EPI_BYTES + 1024 + 512;
+constexpr int LS_STAGES = 4;
+constexpr int LS_TILE_BYTES = 128 * LS_LD * 4;
+constexpr size_t LS_SMEM = (size_t)LS_STAGES * LT_STAGE_BYTES + LS_TILE_BYTES + 1024 + 512;
 
 struct LtParams {
     int M, N, K;
     int tiles_m, tiles_n;
-    int splits, stages_per_split;      // split tiles
+    int band;                          // pairs: tile rows of a band of the schedule
+    int stages_per_split;      // split tiles
     int act;
     unsigned idesc;
     const float* bias;
@@ -151,12 +157,10 @@ template <bool MN, bool PAIR>
 __device__ __forceinline__ void lt_load(unsigned dst, const CUtensorMap* map, unsigned bar, int mn, int k)
 {
     if (MN) {
-        if (PAIR) {
-            lfptx::tma_load_2d_pair(dst, map, bar, mn, k);
-            lfptx::tma_load_2d_pair(dst + 8192, map, bar, mn + 64, k);
-        } else {
-            lfptx::tma_load_2d(dst, map, bar, mn, k);
-            lfptx::tma_load_2d(dst + 8192, map, bar, mn + 64, k);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (PAIR) lfptx::tma_load_2d_pair(dst + i * 8192, map, bar, mn + i * 64, k);
+            else lfptx::tma_load_2d(dst + i * 8192, map, bar, mn + i * 64, k);
         }
     } else {
         if (PAIR) lfptx::tma_load_2d_pair(dst, map, bar, k, mn);
@@ -176,30 +180,6 @@ __device__ __forceinline__ void epi_bias8(float (&v)[8], const LtParams& P, int 
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += b[k];
 }
-template <typename T>
-__device__ __forceinline__ void epi_add8(float (&v)[8], const LtParams& P, int row, int col)
-{
-    if (!P.add) return;
-    float r[8];
-    vec8<T> rv;
-    rv.load(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col);
-    rv.get(r);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += r[k];
-}
-__device__ __forceinline__ void epi_act8(float (&v)[8], int kind)
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = act<true>(v[k], kind);
-}
-__device__ __forceinline__ void epi_prime8(float (&v)[8], uint2 q, unsigned byte, int kind)
-{
-    float z[8];
-    dequantize8(q, byte, z);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= act_prime<true>(z[k], kind);
-}
-
 // ================================================================================================
 // CTA pairs, 256 x 256 tiles
 // ================================================================================================
@@ -207,22 +187,148 @@ __device__ __forceinline__ void epi_prime8(float (&v)[8], uint2 q, unsigned byte
 // tiles worked on at one time share both operands in L2
 __device__ __forceinline__ void lp_tile(int t, const LtParams& P, int& tm, int& tn)
 {
-    const int per_band = 8 * P.tiles_n, band = t / per_band, in = t - band * per_band;
-    const int rows = min(8, P.tiles_m - band * 8);
+    const int per_band = P.band * P.tiles_n, band = t / per_band, in = t - band * per_band;
+    const int rows = min(P.band, P.tiles_m - band * P.band);
     tn = in / rows;
-    tm = band * 8 + (in - tn * rows);
+    tm = band * P.band + (in - tn * rows);
 }
 
-template <int PROD, typename T, typename OUT>
-__global__ void __launch_bounds__(LT_THREADS, 1)
+// What the epilogue reads for 32 columns of its row, fetched a step ahead of its use.
+struct lp_operands {
+    uint2 q[4];            // GRAD_X: 8-bit pre-activations ...
+    unsigned s;            // ... and their scale
+    uint4 add[4];          // residual, 16-bit
+    float4 bias;           // FORWARD, columns 4 * lane ..: brings the line into L1, where the broadcast loads find it
+};
+struct lp_place {
+    int row0, col0, lane;
+    unsigned char* blk;    // this warp's 32 x 128 bytes of shared memory
+    size_t groups;         // 8-bit scales per row
+    lp_operands next;
+};
+template <int PROD, typename T>
+__device__ __forceinline__ void lp_fetch(lp_operands& o, const LtParams& P, const lp_place& e, int j)
+{
+    if (PROD == LF_PROD_GRAD_W) return;
+    const int row = e.row0 + e.lane, col = e.col0 + j * 32;
+    if (PROD == LF_PROD_FORWARD && j == 0 && P.bias && e.col0 + 4 * e.lane < P.N)
+        asm volatile("ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o.bias.x), "=f"(o.bias.y), "=f"(o.bias.z), "=f"(o.bias.w)
+                     : "l"(P.bias + e.col0 + 4 * e.lane));
+#pragma unroll
+    for (int g = 0; g < 4; ++g) { o.q[g] = make_uint2(0, 0); o.add[g] = make_uint4(0, 0, 0, 0); }
+    o.s = 0;
+    if (row >= P.M) return;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        if (col + 8 * g >= P.N) continue;
+        if (PROD == LF_PROD_GRAD_X && P.q) o.q[g] = *reinterpret_cast<const uint2*>(P.q + (size_t)row * P.N + col + 8 * g);
+        if (P.add) o.add[g] = *reinterpret_cast<const uint4*>(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col + 8 * g);
+    }
+    if (PROD == LF_PROD_GRAD_X && P.q && col < P.N) o.s = P.s[(size_t)row * e.groups + (col >> 5)];
+}
+// Epilogue of 32 rows x NC columns, a row per lane.  One copy per activation, straight-line: the accumulator's
+// registers need constant indices, and choosing the activation per eight columns cost 1100 cycles for 32.
+template <int PROD, typename T, typename OUT, int KIND, int NC>
+__device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, lp_place& e)
+{
+    const int lane = e.lane, row = e.row0 + lane;
+#pragma unroll
+    for (int j = 0; j < NC / 32; ++j) {                         // 32 columns at a time
+        const int col = e.col0 + j * 32;
+        const int valid = row < P.M ? min(32, P.N - col) : 0;   // a multiple of 8, or not positive
+        float* v = acc + 32 * j;
+        const lp_operands now = e.next;
+        if (j < NC / 32 - 1) lp_fetch<PROD, T>(e.next, P, e, j + 1);
+        if (PROD == LF_PROD_FORWARD) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (col + 8 * g < P.N) epi_bias8(*reinterpret_cast<float(*)[8]>(v + 8 * g), P, col + 8 * g);
+            if (P.q && valid > 0) {
+                unsigned m = 0;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) if (i < valid) m = max(m, abs_bits(v[i]));
+                const unsigned b = scale_byte(m);
+                unsigned char* qp = P.q + (size_t)row * P.N + col;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (8 * g < valid)
+                        *reinterpret_cast<uint2*>(qp + 8 * g) = quantize8(*reinterpret_cast<float(*)[8]>(v + 8 * g), b);
+                P.s[(size_t)row * e.groups + (col >> 5)] = (unsigned char)b;
+            }
+            act_all<true, 32, KIND>(v);
+        }
+        if (PROD == LF_PROD_GRAD_X && KIND != LF_ACT_NONE) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float z[8];
+                dequantize8(now.q[g], now.s, z);
+                prime_all<true, 8, KIND>(v + 8 * g, z);
+            }
+        }
+        if (PROD != LF_PROD_GRAD_W && P.add) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                vec8<T> rv;
+                float r[8];
+                rv.u = now.add[g];
+                rv.get(r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * g + i] += r[i];
+            }
+        }
+        constexpr int PER = sizeof(OUT) == 2 ? 2 : 1;            // blocks of 32 columns per stored line
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float(&w)[8] = *reinterpret_cast<const float(*)[8]>(v + 8 * g);
+            // 16-byte units of a 128-byte line, turned by the row so that neither side meets a bank twice
+            if (sizeof(OUT) == 2) {
+                vec8<T> o;
+                o.set(w);
+                *reinterpret_cast<uint4*>(e.blk + lane * 128 + ((((j & 1) * 4 + g) ^ (lane & 7)) << 4)) = o.u;
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    *reinterpret_cast<float4*>(e.blk + lane * 128 + (((g * 2 + u) ^ (lane & 7)) << 4)) =
+                        make_float4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+            }
+        }
+        if (j % PER == PER - 1) {                               // a line of every row is complete: whole lines go out
+            __syncwarp();
+            constexpr int UC = 16 / (int)sizeof(OUT);           // columns of a 16-byte unit
+            const int cu = col - (PER - 1) * 32 + (lane & 7) * UC, r0 = e.row0 + (lane >> 3);
+            const unsigned char* from = e.blk + (lane >> 3) * 128;
+            OUT* to = static_cast<OUT*>(P.d) + (size_t)r0 * P.ld_d + cu;
+            const size_t step = (size_t)4 * P.ld_d;
+            uint4 u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)                         // row (lane >> 3) + 4 i: its turn alternates
+                u[i] = *reinterpret_cast<const uint4*>(from + i * 512 + (((lane & 7) ^ (((lane >> 3) + 4 * i) & 7)) << 4));
+            if (cu < P.N) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (r0 + 4 * i < P.M) *reinterpret_cast<uint4*>(to + i * step) = u[i];
+            }
+            __syncwarp();
+        }
+    }
+}
+
+// MB: 128-row blocks per CTA.  MB = 1: 256 x 256 tiles, the two accumulators alternate between tiles (or
+// chunks).  MB = 2: 512 x 256 tiles, one accumulator per block.
+template <int PROD, typename T, typename OUT, int MB>
+__global__ void __launch_bounds__(LP_THREADS, 1)
 k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_d, const LtParams P)
+               const LtParams P)
 {
     constexpr bool A_MN = PROD == LF_PROD_GRAD_W, B_MN = PROD != LF_PROD_FORWARD;
     constexpr bool PROMOTE = sizeof(OUT) == 4;
+    constexpr int STAGES = MB == 2 ? 4 : 6;
+    constexpr unsigned STAGE_BYTES = (unsigned)(MB + 1) * LT_BLOCK_BYTES;
+    constexpr int NC = 128;                                  // columns of an epilogue warp
+    static_assert(STAGES * STAGE_BYTES == LP_RING_BYTES, "both forms use the whole ring");
     extern __shared__ unsigned char lt_smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lt_smem_raw) + 1023u) & ~(uintptr_t)1023u);
-    unsigned char* epi = ring + (size_t)LT_STAGES * LT_STAGE_BYTES;
+    unsigned char* epi = ring + LP_RING_BYTES;
     LtShared* sh = reinterpret_cast<LtShared*>(epi + LP_EPI_BYTES);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -233,7 +339,7 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int chunk = PROMOTE ? LT_CHUNK : n_k;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < LT_STAGES; ++i) {
+        for (int i = 0; i < STAGES; ++i) {
             lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
             lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
         }
@@ -256,7 +362,10 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     lfptx::tc_fence_after();
     const unsigned tmem_base = sh->tmem_base;
 
-    if (warp == 0) {
+    // registers move from the first warpgroup to the two that hold accumulators
+    if (warp < 4) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LP_REGS_LOW));
+      if (warp == 0) {
         // ------------------------------ TMA producer: this CTA's halves -------------------------
         if (lane == 0) {
             unsigned it = 0;
@@ -264,81 +373,137 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
                 int tm, tn;
                 lp_tile(t, P, tm, tn);
-                const int m0 = tm * 256 + (int)rank * 128, n0 = tn * 256 + (int)rank * 128;
+                const int m0 = (tm * 2 + (int)rank) * (MB * 128), n0 = tn * 256 + (int)rank * 128;
                 for (int ks = 0; ks < n_k; ++ks, ++it) {
-                    const unsigned st = it % LT_STAGES, use = it / LT_STAGES;
+                    const unsigned st = it % STAGES, use = it / STAGES;
                     if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->empty[st]), (use - 1) & 1u, P, sh)) { ok = false; break; }
                     const unsigned lbar = lfptx::smem_u32(&sh->full[st]);
                     if (P.withhold && pair == 0 && rank == 1 && it == 0) continue;    // test hook
-                    if (rank == 0) lfptx::mbar_arrive_expect_tx(lbar, 2u * LT_STAGE_BYTES);
+                    if (rank == 0) lfptx::mbar_arrive_expect_tx(lbar, 2u * STAGE_BYTES);
                     const unsigned bar = lfptx::map_to_cta(lbar, 0);
-                    const unsigned dst = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
-                    lt_load<A_MN, true>(dst, &map_a, bar, m0, ks * LT_BK);
-                    lt_load<B_MN, true>(dst + LT_BLOCK_BYTES, &map_b, bar, n0, ks * LT_BK);
+                    const unsigned dst = lfptx::smem_u32(ring + (size_t)st * STAGE_BYTES);
+#pragma unroll
+                    for (int b = 0; b < MB; ++b) lt_load<A_MN, true>(dst + b * LT_BLOCK_BYTES, &map_a, bar, m0 + b * 128, ks * LT_BK);
+                    lt_load<B_MN, true>(dst + MB * LT_BLOCK_BYTES, &map_b, bar, n0, ks * LT_BK);
                 }
             }
             sh->prog_it = it;
         }
-    } else if (warp == 1) {
+      } else if (warp == 1) {
         // ------------------------------ MMA issuer (leader CTA) ---------------------------------
         if (lane == 0 && rank == 0) {
-            unsigned it = 0, c = 0;             // c counts accumulator fills
+            auto full_wait = [&](unsigned it) {
+                const bool ok = lt_wait(lfptx::smem_u32(&sh->full[it % STAGES]), (it / STAGES) & 1u, P, sh);
+                lfptx::tc_fence_after();
+                return ok;
+            };
+            auto acc_wait = [&](unsigned c) {           // fill c of the accumulators: buffer c & 1
+                const bool ok = (c >> 1) == 0 || lt_wait(lfptx::smem_u32(&sh->acc_empty[c & 1u]), ((c >> 1) - 1) & 1u, P, sh);
+                lfptx::tc_fence_after();
+                return ok;
+            };
+            auto products = [&](unsigned it, int b, unsigned buffer, bool first) {      // block b of a stage
+                const unsigned st_addr = lfptx::smem_u32(ring + (size_t)(it % STAGES) * STAGE_BYTES);
+                const unsigned a_addr = st_addr + b * LT_BLOCK_BYTES, b_addr = st_addr + MB * LT_BLOCK_BYTES;
+#pragma unroll
+                for (int kk = 0; kk < LT_BK / 16; ++kk)
+                    lt_mma<true>(tmem_base + buffer * 256u, lt_desc<A_MN>(a_addr + lt_step<A_MN>(kk)),
+                                 lt_desc<B_MN>(b_addr + lt_step<B_MN>(kk)), P.idesc, (!first || kk > 0) ? 1u : 0u);
+            };
+            auto release = [&](unsigned it) { lt_commit<true>(lfptx::smem_u32(&sh->empty[it % STAGES])); };
+            auto filled = [&](unsigned c) { lt_commit<true>(lfptx::smem_u32(&sh->acc_full[c & 1u])); };
+            unsigned it = 0, c = 0;             // stages consumed, accumulators filled
             bool ok = true;
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
-                for (int k0 = 0; k0 < n_k && ok; k0 += chunk, ++c) {
-                    const unsigned ab = c & 1u, ab_use = c >> 1;
-                    if (ab_use > 0 && !lt_wait(lfptx::smem_u32(&sh->acc_empty[ab]), (ab_use - 1) & 1u, P, sh)) { ok = false; break; }
-                    lfptx::tc_fence_after();
-                    const unsigned d_tmem = tmem_base + ab * 256u;
-                    const int k1 = min(k0 + chunk, n_k);
-                    for (int ks = k0; ks < k1; ++ks, ++it) {
-                        const unsigned st = it % LT_STAGES, use = it / LT_STAGES;
-                        if (!lt_wait(lfptx::smem_u32(&sh->full[st]), use & 1u, P, sh)) { ok = false; break; }
-                        lfptx::tc_fence_after();
-                        const unsigned a_addr = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
-                        const unsigned b_addr = a_addr + LT_BLOCK_BYTES;
-#pragma unroll
-                        for (int kk = 0; kk < LT_BK / 16; ++kk)
-                            lt_mma<true>(d_tmem, lt_desc<A_MN>(a_addr + lt_step<A_MN>(kk)), lt_desc<B_MN>(b_addr + lt_step<B_MN>(kk)),
-                                         P.idesc, (ks > k0 || kk > 0) ? 1u : 0u);
-                        lt_commit<true>(lfptx::smem_u32(&sh->empty[st]));
+                if (MB == 1) {
+                    for (int k0 = 0; k0 < n_k && ok; k0 += chunk, ++c) {
+                        if (!acc_wait(c)) { ok = false; break; }
+                        const int k1 = min(k0 + chunk, n_k);
+                        for (int ks = k0; ks < k1; ++ks, ++it) {
+                            if (!full_wait(it)) { ok = false; break; }
+                            products(it, 0, c & 1u, ks == k0);
+                            release(it);
+                        }
+                        if (ok) filled(c);
                     }
-                    if (ok) lt_commit<true>(lfptx::smem_u32(&sh->acc_full[ab]));
+                } else {
+                    // Both accumulators belong to this tile, so the epilogue can only run beside the products if one
+                    // block is ahead of the other: the first stages are multiplied for block 0 before block
+                    // 1's accumulator is asked for, the last ones for block 0 before block 1, whose
+                    // products then cover block 0's epilogue.
+                    const int head = min(LP_AHEAD, n_k), tail = min(LP_AHEAD, n_k - head), mid_end = n_k - tail;
+                    if (!acc_wait(c)) break;
+                    for (int ks = 0; ks < head && ok; ++ks) {
+                        ok = full_wait(it + ks);
+                        if (ok) products(it + ks, 0, 0u, ks == 0);
+                    }
+                    if (ok && n_k == head) filled(c);
+                    if (!ok || !acc_wait(c + 1)) break;
+                    for (int ks = 0; ks < head; ++ks) {
+                        products(it + ks, 1, 1u, ks == 0);
+                        release(it + ks);
+                    }
+                    for (int ks = head; ks < mid_end && ok; ++ks) {
+                        ok = full_wait(it + ks);
+                        if (!ok) break;
+                        products(it + ks, 0, 0u, false);
+                        products(it + ks, 1, 1u, false);
+                        release(it + ks);
+                    }
+                    for (int ks = mid_end; ks < n_k && ok; ++ks) {
+                        ok = full_wait(it + ks);
+                        if (ok) products(it + ks, 0, 0u, false);
+                    }
+                    if (!ok) break;
+                    if (tail > 0) filled(c);
+                    for (int ks = mid_end; ks < n_k; ++ks) {
+                        products(it + ks, 1, 1u, false);
+                        release(it + ks);
+                    }
+                    filled(c + 1);
+                    it += n_k;
+                    c += 2;
                 }
             }
         }
+      }
     } else {
-        // ------------------------------ epilogue (warps 2..9 of both CTAs) ----------------------
-        // A warp has one 32-lane quadrant (32 rows) and one half (128 columns) of the tile; a lane has a
-        // row.  Results leave through a 32 x 128-byte block in shared memory and a TMA store, which
-        // clips ragged edges.
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(LP_REGS_HIGH));
+        // ------------------------------ epilogue (warps 4..11 of both CTAs) ----------------------
+        // A warp has one 32-lane quadrant (32 rows) and one half (NC columns) of an accumulator; a lane has a row.
+        // It takes the columns into registers and hands the accumulator back before it works on
+        // them.  Results are turned through a 32 x 128-byte block in shared memory, so that a warp
+        // stores whole lines (a TMA store of the block instead made the next block wait for its read:
+        // 6000 to 9000 cycles per accumulator against 2000).
+        const int quad = warp & 3, half = (warp - 4) >> 2;
         const unsigned leader_acc_empty = lfptx::map_to_cta(lfptx::smem_u32(&sh->acc_empty[0]), 0);
-        unsigned char* blk = epi + (warp - 2) * 4096;
-        const unsigned blk_addr = lfptx::smem_u32(blk);
-        constexpr int OC = 128 / (int)sizeof(OUT);             // columns of a stored block: 64 or 32
+        unsigned char* blk = epi + (warp - 4) * 4096;
+        const size_t groups = (size_t)((P.N + 31) / 32);
         unsigned c = 0;
         bool ok = true;
-        for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+        for (int tb = pair * MB; ok; tb += (tb % MB == MB - 1) ? n_pairs * MB - (MB - 1) : 1) {     // tile, block
+            if (tb / MB >= n_tiles) break;
             int tm, tn;
-            lp_tile(t, P, tm, tn);
-            const int row0 = tm * 256 + (int)rank * 128 + quad * 32, row = row0 + lane;
-            const int col0 = tn * 256 + half * 128;
-            const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * 128u;
-            float acc[PROMOTE ? 128 : 1];
+            lp_tile(tb / MB, P, tm, tn);
+            const int row0 = (tm * 2 + (int)rank) * (MB * 128) + (tb % MB) * 128 + quad * 32;
+            const int col0 = tn * 256 + half * NC;
+            const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * (unsigned)NC;
+            lp_place e = {row0, col0, lane, blk, groups, {}};
+            lp_fetch<PROD, T>(e.next, P, e, 0);                  // on its way while the accumulator is waited for
+            float acc[NC];
             if (PROMOTE) {
 #pragma unroll
-                for (int i = 0; i < 128; ++i) acc[(PROMOTE ? i : 0)] = 0.f;
+                for (int i = 0; i < NC; ++i) acc[i] = 0.f;
                 for (int k0 = 0; k0 < n_k; k0 += chunk, ++c) {
                     const unsigned ab = c & 1u;
                     if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) { ok = false; break; }
                     lfptx::tc_fence_after();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < NC / 16; ++j) {
                         unsigned r[16];
                         lfptx::tmem_ld16(lane_addr + ab * 256u + j * 16, r);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[(PROMOTE ? j * 16 + i : 0)] += __uint_as_float(r[i]);
+                        for (int i = 0; i < 16; ++i) acc[j * 16 + i] += __uint_as_float(r[i]);
                     }
                     lfptx::tc_fence_before();
                     __syncwarp();
@@ -346,86 +511,24 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 }
                 if (!ok) break;
             } else {
-                if (!lt_wait(lfptx::smem_u32(&sh->acc_full[c & 1u]), (c >> 1) & 1u, P, sh)) break;
+                const unsigned ab = c & 1u;
+                if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) break;
+                ++c;
                 lfptx::tc_fence_after();
-            }
-#pragma unroll (PROMOTE ? 4 : 1)
-            for (int j = 0; j < 128 / OC; ++j) {
-                const int colj = col0 + j * OC;
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // blk is free again
+                lfptx::tmem_ld_row(lane_addr + ab * 256u, acc);
+                lfptx::tc_fence_before();
                 __syncwarp();
-#pragma unroll
-                for (int h = 0; h < OC / 32; ++h) {            // 32 columns at a time
-                    const int col = colj + h * 32;
-                    float v[32];
-                    if (PROMOTE) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = acc[(PROMOTE ? j * 32 + i : 0)];
-                    } else {
-                        unsigned r[32];
-                        lfptx::tmem_ld32(lane_addr + (c & 1u) * 256u + j * OC + h * 32, r);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-                    }
-                    const int valid = row < P.M ? min(32, P.N - col) : 0;    // a multiple of 8
-                    if (PROD == LF_PROD_FORWARD) {
-#pragma unroll
-                        for (int g = 0; g < 4; ++g)
-                            if (col + 8 * g < P.N) epi_bias8(*reinterpret_cast<float(*)[8]>(v + 8 * g), P, col + 8 * g);
-                        if (P.q && valid > 0) {
-                            unsigned m = 0;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) if (i < valid) m = max(m, abs_bits(v[i]));
-                            const unsigned b = scale_byte(m);
-                            unsigned char* qp = P.q + (size_t)row * P.N + col;
-#pragma unroll
-                            for (int g = 0; g < 4; ++g)
-                                if (8 * g < valid)
-                                    *reinterpret_cast<uint2*>(qp + 8 * g) = quantize8(*reinterpret_cast<float(*)[8]>(v + 8 * g), b);
-                            P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)] = (unsigned char)b;
-                        }
-                    }
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        float(&w)[8] = *reinterpret_cast<float(*)[8]>(v + 8 * g);
-                        if (PROD == LF_PROD_FORWARD) epi_act8(w, P.act);
-                        if (PROD == LF_PROD_GRAD_X && P.q && 8 * g < valid)
-                            epi_prime8(w, *reinterpret_cast<const uint2*>(P.q + (size_t)row * P.N + col + 8 * g),
-                                       P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)], P.act);
-                        if (PROD != LF_PROD_GRAD_W && 8 * g < valid) epi_add8<T>(w, P, row, col + 8 * g);
-                        // 16-byte units of a 128-byte line, turned as the 128-byte swizzle has them
-                        if (sizeof(OUT) == 2) {
-                            vec8<T> o;
-                            o.set(w);
-                            const int unit = h * 4 + g;
-                            *reinterpret_cast<uint4*>(blk + lane * 128 + ((unit ^ (lane & 7)) << 4)) = o.u;
-                        } else {
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                const int unit = g * 2 + u;
-                                *reinterpret_cast<float4*>(blk + lane * 128 + ((unit ^ (lane & 7)) << 4)) =
-                                    make_float4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
-                            }
-                        }
-                    }
-                }
-                if (!PROMOTE && j == 128 / OC - 1) {           // the accumulator has been read
-                    lfptx::tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) lt_arrive_cluster(leader_acc_empty + (c & 1u) * 8u);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    if (row0 < P.M && colj < P.N)
-                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-                                     ::"l"(&map_d), "r"(blk_addr), "r"(colj), "r"(row0) : "memory");
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                }
+                if (lane == 0) lt_arrive_cluster(leader_acc_empty + ab * 8u);
             }
-            if (!PROMOTE) ++c;
+            switch (PROD == LF_PROD_GRAD_W || (PROD == LF_PROD_GRAD_X && !P.q) ? LF_ACT_NONE : P.act) {
+                case LF_ACT_SIGMOID: lp_finish<PROD, T, OUT, LF_ACT_SIGMOID, NC>(acc, P, e); break;
+                case LF_ACT_TANH: lp_finish<PROD, T, OUT, LF_ACT_TANH, NC>(acc, P, e); break;
+                case LF_ACT_RELU: lp_finish<PROD, T, OUT, LF_ACT_RELU, NC>(acc, P, e); break;
+                case LF_ACT_SILU: lp_finish<PROD, T, OUT, LF_ACT_SILU, NC>(acc, P, e); break;
+                case LF_ACT_GELU: lp_finish<PROD, T, OUT, LF_ACT_GELU, NC>(acc, P, e); break;
+                default: lp_finish<PROD, T, OUT, LF_ACT_NONE, NC>(acc, P, e); break;
+            }
         }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 
     // Neither CTA may leave (or free tensor memory) while the other can still reach it.
@@ -441,14 +544,14 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const unsigned it_l = sh->prog_it, it_p = lt_ld_cluster_u32(lfptx::map_to_cta(lfptx::smem_u32(&sh->prog_it), 1));
             const unsigned hi = max(it_l, it_p), lo = min(it_l, it_p);
             for (unsigned j = lo; j < hi; ++j) {
-                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
-                if (j >= it_l) lfptx::mbar_arrive_expect_tx(bar, (unsigned)LT_STAGE_BYTES);   // only the peer loaded
-                else lt_complete_tx(bar, (unsigned)LT_STAGE_BYTES);                           // only the leader loaded
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % STAGES]);
+                if (j >= it_l) lfptx::mbar_arrive_expect_tx(bar, STAGE_BYTES);                // only the peer loaded
+                else lt_complete_tx(bar, STAGE_BYTES);                                        // only the leader loaded
             }
             const unsigned long long t0 = lfptx::globaltimer_ns();
-            for (unsigned j = hi > LT_STAGES ? hi - LT_STAGES : 0; j < hi; ++j) {
-                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
-                while (!lfptx::mbar_try_wait(bar, (j / LT_STAGES) & 1u) && lfptx::globaltimer_ns() - t0 < 50000000ull) { }
+            for (unsigned j = hi > STAGES ? hi - STAGES : 0; j < hi; ++j) {
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % STAGES]);
+                while (!lfptx::mbar_try_wait(bar, (j / STAGES) & 1u) && lfptx::globaltimer_ns() - t0 < 50000000ull) { }
             }
         }
     }
@@ -462,7 +565,13 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // ================================================================================================
 // Split tiles: one CTA per 128 x 128 tile and part of the contraction, a cluster per tile
 // ================================================================================================
-template <int PROD, typename T, typename OUT>
+// The parts of a tile meet in distributed shared memory: every part leaves its fp32 tile beside its operand ring,
+// and after a cluster barrier each CTA adds its share of the rows, R = 128 / splits, from all parts,
+// every load issued before the first addition.  (One part after the other cost 7000 to 11000 cycles,
+// storing registers into the owners' shared memory, 16 bytes a row, 5000.)
+// The epilogue warps go through their code once before the accumulator is complete, with nothing to load or store:
+// a launch this short meets its instructions and parameters cold, 2400 cycles otherwise spent at its end.
+template <int PROD, typename T, typename OUT, int SPLITS>
 __global__ void __launch_bounds__(LT_THREADS, 1)
 k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const LtParams P)
 {
@@ -470,19 +579,27 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     constexpr bool PROMOTE = sizeof(OUT) == 4;
     extern __shared__ unsigned char lt_smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lt_smem_raw) + 1023u) & ~(uintptr_t)1023u);
-    LtShared* sh = reinterpret_cast<LtShared*>(ring + (size_t)LT_STAGES * LT_STAGE_BYTES);
-    float* tile = reinterpret_cast<float*>(ring);            // [128][LS_LD], once every product is done
+    float* tile = reinterpret_cast<float*>(ring + (size_t)LS_STAGES * LT_STAGE_BYTES);     // [128][LS_LD]
+    LtShared* sh = reinterpret_cast<LtShared*>(ring + (size_t)LS_STAGES * LT_STAGE_BYTES + LS_TILE_BYTES);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int part = (int)(blockIdx.x % (unsigned)P.splits), t = (int)(blockIdx.x / (unsigned)P.splits);
+    const int part = (int)(blockIdx.x % (unsigned)SPLITS), t = (int)(blockIdx.x / (unsigned)SPLITS);
     const int tn = t / P.tiles_m, tm = t - tn * P.tiles_m;
     const int n_k_all = (P.K + LT_BK - 1) / LT_BK;
     const int ks0 = part * P.stages_per_split;
     const int n_k = max(0, min(P.stages_per_split, n_k_all - ks0));
     const int chunk = PROMOTE ? LT_CHUNK : (n_k > 0 ? n_k : 1);
 
+    auto load_stage = [&](int ks) {                    // one thread; stage ks of this part into its slot
+        const unsigned st = (unsigned)ks % LS_STAGES, bar = lfptx::smem_u32(&sh->full[st]);
+        lfptx::mbar_arrive_expect_tx(bar, LT_STAGE_BYTES);
+        if (P.withhold && blockIdx.x == 0 && ks == 0) return;                       // test hook
+        const unsigned dst = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
+        lt_load<A_MN, false>(dst, &map_a, bar, tm * 128, (ks0 + ks) * LT_BK);
+        lt_load<B_MN, false>(dst + LT_BLOCK_BYTES, &map_b, bar, tn * 128, (ks0 + ks) * LT_BK);
+    };
     if (threadIdx.x == 0) {
-        for (int i = 0; i < LT_STAGES; ++i) {
+        for (int i = 0; i < LS_STAGES; ++i) {
             lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
             lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
         }
@@ -492,6 +609,7 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
         sh->abort_flag = 0u;
         lfptx::mbar_fence_init();
+        for (int ks = 0; ks < min(n_k, LS_STAGES); ++ks) load_stage(ks);            // under the rest of the set-up
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -503,25 +621,19 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     lfptx::tc_fence_after();
     const unsigned tmem_base = sh->tmem_base;
 
-    float acc[64];
     if (warp == 0) {
         if (lane == 0) {
-            unsigned it = 0;
-            for (int ks = 0; ks < n_k; ++ks, ++it) {
-                const unsigned st = it % LT_STAGES, use = it / LT_STAGES;
-                if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->empty[st]), (use - 1) & 1u, P, sh)) break;
-                const unsigned bar = lfptx::smem_u32(&sh->full[st]);
-                lfptx::mbar_arrive_expect_tx(bar, LT_STAGE_BYTES);
-                if (P.withhold && blockIdx.x == 0 && it == 0) continue;              // test hook
-                const unsigned dst = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
-                lt_load<A_MN, false>(dst, &map_a, bar, tm * 128, (ks0 + ks) * LT_BK);
-                lt_load<B_MN, false>(dst + LT_BLOCK_BYTES, &map_b, bar, tn * 128, (ks0 + ks) * LT_BK);
+            int ks = LS_STAGES;
+            for (; ks < n_k; ++ks) {
+                if (!lt_wait(lfptx::smem_u32(&sh->empty[ks % LS_STAGES]), (unsigned)(ks / LS_STAGES - 1) & 1u, P, sh)) break;
+                load_stage(ks);
             }
             // after giving up: do not let the CTA go on under loads that are still landing
             if (sh->abort_flag) {
                 const unsigned long long t0 = lfptx::globaltimer_ns();
-                for (unsigned j = it > LT_STAGES ? it - LT_STAGES : 0; j < it; ++j)
-                    while (!lfptx::mbar_try_wait(lfptx::smem_u32(&sh->full[j % LT_STAGES]), (j / LT_STAGES) & 1u) &&
+                const int n = min(ks, n_k);
+                for (int j = max(0, n - LS_STAGES); j < n; ++j)
+                    while (!lfptx::mbar_try_wait(lfptx::smem_u32(&sh->full[j % LS_STAGES]), (unsigned)(j / LS_STAGES) & 1u) &&
                            lfptx::globaltimer_ns() - t0 < 50000000ull) { }
             }
         }
@@ -535,7 +647,7 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 lfptx::tc_fence_after();
                 const int k1 = min(k0 + chunk, n_k);
                 for (int ks = k0; ks < k1; ++ks, ++it) {
-                    const unsigned st = it % LT_STAGES, use = it / LT_STAGES;
+                    const unsigned st = it % LS_STAGES, use = it / LS_STAGES;
                     if (!lt_wait(lfptx::smem_u32(&sh->full[st]), use & 1u, P, sh)) { ok = false; break; }
                     lfptx::tc_fence_after();
                     const unsigned a_addr = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
@@ -549,83 +661,115 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 if (ok) lt_commit<false>(lfptx::smem_u32(&sh->acc_full[ab]));
             }
         }
-    } else {
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+    }
+    __syncwarp();
+    constexpr int R = 128 / SPLITS, RP = SPLITS >= 4 ? 16 / SPLITS : 4;     // rows of this CTA at most, and rows a warp takes at a time
+    const int share = min(R, (P.M - tm * 128 + SPLITS - 1) / SPLITS);     // rows of this CTA: its part of those that exist
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        if (pass == 1) {
+            if (warp >= 2) {
+                const int quad = warp & 3, half = (warp - 2) >> 2;
+                float acc[64];
 #pragma unroll
-        for (int i = 0; i < 64; ++i) acc[i] = 0.f;
-        unsigned c = 0;
-        for (int k0 = 0; k0 < n_k; k0 += chunk, ++c) {
-            const unsigned ab = c & 1u;
-            if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) break;
-            lfptx::tc_fence_after();
+                for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+                unsigned c = 0;
+                for (int k0 = 0; k0 < n_k; k0 += chunk, ++c) {
+                    const unsigned ab = c & 1u;
+                    if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) break;
+                    lfptx::tc_fence_after();
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                unsigned r[32];
-                lfptx::tmem_ld32(tmem_base + ((unsigned)(quad * 32) << 16) + ab * 128u + half * 64u + j * 32, r);
+                    for (int j = 0; j < 2; ++j) {
+                        unsigned r[32];
+                        lfptx::tmem_ld32(tmem_base + ((unsigned)(quad * 32) << 16) + ab * 128u + half * 64u + j * 32, r);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) acc[j * 32 + i] += __uint_as_float(r[i]);
+                        for (int i = 0; i < 32; ++i) acc[j * 32 + i] += __uint_as_float(r[i]);
+                    }
+                    lfptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->acc_empty[ab]));
+                }
+                float* to = tile + (quad * 32 + lane) * LS_LD + half * 64;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    *reinterpret_cast<float4*>(to + 4 * i) = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
             }
             lfptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->acc_empty[ab]));
+            if (SPLITS > 1) lfptx::cluster_sync_all();
+            else __syncthreads();
         }
-        // every product of this CTA is done (the last accumulator was complete), so the ring is free
-        if (!sh->abort_flag) {
-            float* to = tile + (quad * 32 + lane) * LS_LD + half * 64;
+        if (warp < 2) continue;
+        // This CTA's rows.  A lane takes four columns, a warp a row (its loads from another CTA are whole lines),
+        // RP rows at a time.
+        const int rows = pass == 0 ? 8 * RP : share;
+#pragma unroll 1
+        for (int r0 = (warp - 2) * RP; r0 < rows; r0 += 8 * RP) {
+            const int col = tn * 128 + lane * 4;
+            float4 x[RP][SPLITS];
+            const float* at = tile + min(part * share + r0, 128 - RP) * LS_LD + lane * 4;   // (rows past the share are not used)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                *reinterpret_cast<float4*>(to + 4 * i) = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
-        }
-    }
-    lfptx::tc_fence_before();
-    __syncthreads();
-    if (P.splits > 1) lfptx::cluster_sync_all();
-    if (warp >= 2 && !sh->abort_flag) {
-        // this CTA finishes 128 / splits rows; a lane takes eight columns, half a warp a row
-        const int tid = threadIdx.x - 64;
-        const int rows = 128 / P.splits;
-        const unsigned tile_addr = lfptx::smem_u32(tile);
-        for (int u = tid; u < rows * 16; u += 256) {           // (a multiple of 256: whole warps)
-            const int r = part * rows + (u >> 4), cv = (u & 15) * 8;
-            const int row = tm * 128 + r, col = tn * 128 + cv;
-            float v[8];
+            for (int p = 0; p < SPLITS; ++p) {
+                const unsigned from = SPLITS > 1 && pass == 1 ? lfptx::map_to_cta(lfptx::smem_u32(at), (unsigned)p) : lfptx::smem_u32(at);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = 0.f;
-            const unsigned at = tile_addr + (unsigned)(r * LS_LD + cv) * 4u;
-            for (int p = 0; p < P.splits; ++p) {               // parts in order: the sum does not depend on timing
-                const unsigned from = P.splits > 1 ? lfptx::map_to_cta(at, (unsigned)p) : at;
-                const float4 x = lt_ld_cluster_f4(from), y = lt_ld_cluster_f4(from + 16);
-                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-                v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+                for (int h = 0; h < RP; ++h)
+                    x[h][p] = SPLITS > 1 ? lt_ld_cluster_f4(from + h * (LS_LD * 4)) : *reinterpret_cast<const float4*>(at + h * LS_LD);
             }
-            const bool in = row < P.M && col < P.N;
-            if (PROD == LF_PROD_FORWARD) {
-                if (in) epi_bias8(v, P, col);
-                if (P.q) {
-                    float z[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) z[k] = in ? v[k] : 0.f;
-                    const unsigned b = group_byte(z);
-                    if (in) {
-                        *reinterpret_cast<uint2*>(P.q + (size_t)row * P.N + col) = quantize8(z, b);
-                        if ((col & 31) == 0) P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)] = (unsigned char)b;
-                    }
+            for (int h = 0; h < RP; ++h) {
+                const int row = tm * 128 + part * share + r0 + h;
+                const bool in = pass == 1 && r0 + h < share && row < P.M && col < P.N && !sh->abort_flag;
+                uint2 radd = make_uint2(0, 0);
+                unsigned zq = 0, zs = 0;
+                if (in && PROD != LF_PROD_GRAD_W && P.add)
+                    radd = *reinterpret_cast<const uint2*>(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col);
+                if (in && PROD == LF_PROD_GRAD_X && P.q) {
+                    zq = *reinterpret_cast<const unsigned*>(P.q + (size_t)row * P.N + col);
+                    zs = P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)];
                 }
-                epi_act8(v, P.act);
+                float v[4] = {x[h][0].x, x[h][0].y, x[h][0].z, x[h][0].w};
+#pragma unroll
+                for (int p = 1; p < SPLITS; ++p) {                  // parts in order: the sum does not depend on timing
+                    v[0] += x[h][p].x; v[1] += x[h][p].y; v[2] += x[h][p].z; v[3] += x[h][p].w;
+                }
+                if (PROD == LF_PROD_FORWARD) {
+                    if (in && P.bias) {
+                        const float4 b = *reinterpret_cast<const float4*>(P.bias + col);
+                        v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
+                    }
+                    if (P.q) {
+                        unsigned m = in ? max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3]))) : 0u;
+#pragma unroll
+                        for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                        const unsigned b = scale_byte(m);
+                        const float is = inv_scale(b);
+                        if (in) {
+                            *reinterpret_cast<unsigned*>(P.q + (size_t)row * P.N + col) = to_e4m3x4(v[0] * is, v[1] * is, v[2] * is, v[3] * is);
+                            if ((col & 31) == 0) P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)] = (unsigned char)b;
+                        }
+                    }
+                    act_n<true, 4>(v, P.act);
+                }
+                if (PROD == LF_PROD_GRAD_X && P.q) {
+                    float z[4];
+                    from_e4m3x4(zq, scale(zs), z[0], z[1], z[2], z[3]);
+                    prime_n<true, 4>(v, z, P.act);
+                }
+                if (PROD != LF_PROD_GRAD_W && P.add) {
+                    const float2 f0 = unpack2(radd.x, T()), f1 = unpack2(radd.y, T());
+                    v[0] += f0.x; v[1] += f0.y; v[2] += f1.x; v[3] += f1.y;
+                }
+                if (in) {
+                    OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
+                    if (sizeof(OUT) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
+                    else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                }
             }
-            if (!in) continue;
-            if (PROD == LF_PROD_GRAD_X && P.q)
-                epi_prime8(v, *reinterpret_cast<const uint2*>(P.q + (size_t)row * P.N + col),
-                           P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)], P.act);
-            if (PROD != LF_PROD_GRAD_W) epi_add8<T>(v, P, row, col);
-            vec8<OUT> o;
-            o.set(v);
-            o.store(static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col);
         }
     }
-    if (P.splits > 1) lfptx::cluster_sync_all();               // the other parts have read this CTA's tile
-    else __syncthreads();
+    // no CTA may leave while another one reads its tile
+    if (SPLITS > 1) lfptx::cluster_sync_all();
     if (warp == 1) {
+        __syncwarp();
         lfptx::tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
     }
@@ -646,10 +790,10 @@ lf_encode_fn lt_encode()
 }
 
 // row-major [rows][cols] matrix, boxes of `bc` columns x `br` rows in the 128-byte swizzle
-bool lt_map(CUtensorMap* m, CUtensorMapDataType type, int esize, const void* base, int rows, int cols, long long ld, int bc, int br)
+bool lt_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, int rows, int cols, long long ld, int bc, int br)
 {
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)ld * (cuuint64_t)esize};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
     cuuint32_t box[2] = {(cuuint32_t)bc, (cuuint32_t)br};
     cuuint32_t estr[2] = {1, 1};
     return lt_encode()(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -657,48 +801,61 @@ bool lt_map(CUtensorMap* m, CUtensorMapDataType type, int esize, const void* bas
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-typedef void (*lt_pair_kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const LtParams);
-typedef void (*lt_split_kernel)(const CUtensorMap, const CUtensorMap, const LtParams);
+typedef void (*lt_kernel)(const CUtensorMap, const CUtensorMap, const LtParams);
 
+// Kernel of a product: index = prod * 2 + (f16); 6 and 7: grad_w with an fp32 result.  Pairs: tile 0 256 x 256,
+// 1 512 x 256 (16-bit results).
+constexpr int LT_KERNELS = 8;
+enum lt_tile { LT_256x256 = 0, LT_512x256 = 1, LT_TILES = 2 };
 template <int PROD, typename T, typename OUT>
-struct lt_kernels {
-    static lt_pair_kernel pair() { return k_product_pair<PROD, T, OUT>; }
-    static lt_split_kernel split() { return k_product_split<PROD, T, OUT>; }
-};
-
-// kernel of a product; index = prod * 2 + (f16), 6 and 7: grad_w with an fp32 result
-lt_pair_kernel lt_pick_pair(int i)
+lt_kernel lt_pair_of(int tile)
 {
-    switch (i) {
-        case 0: return lt_kernels<LF_PROD_FORWARD, __nv_bfloat16, __nv_bfloat16>::pair();
-        case 1: return lt_kernels<LF_PROD_FORWARD, __half, __half>::pair();
-        case 2: return lt_kernels<LF_PROD_GRAD_X, __nv_bfloat16, __nv_bfloat16>::pair();
-        case 3: return lt_kernels<LF_PROD_GRAD_X, __half, __half>::pair();
-        case 4: return lt_kernels<LF_PROD_GRAD_W, __nv_bfloat16, __nv_bfloat16>::pair();
-        case 5: return lt_kernels<LF_PROD_GRAD_W, __half, __half>::pair();
-        case 6: return lt_kernels<LF_PROD_GRAD_W, __nv_bfloat16, float>::pair();
-        default: return lt_kernels<LF_PROD_GRAD_W, __half, float>::pair();
+    if constexpr (sizeof(OUT) == 2)
+        if (tile == LT_512x256) return k_product_pair<PROD, T, OUT, 2>;
+    return tile == LT_256x256 ? k_product_pair<PROD, T, OUT, 1> : nullptr;
+}
+template <int PROD, typename T, typename OUT>
+lt_kernel lt_split_of(int splits)
+{
+    switch (splits) {
+        case 1: return k_product_split<PROD, T, OUT, 1>;
+        case 2: return k_product_split<PROD, T, OUT, 2>;
+        case 4: return k_product_split<PROD, T, OUT, 4>;
+        default: return k_product_split<PROD, T, OUT, 8>;
     }
 }
-lt_split_kernel lt_pick_split(int i)
+lt_kernel lt_pick_pair(int i, int tile)
 {
     switch (i) {
-        case 0: return lt_kernels<LF_PROD_FORWARD, __nv_bfloat16, __nv_bfloat16>::split();
-        case 1: return lt_kernels<LF_PROD_FORWARD, __half, __half>::split();
-        case 2: return lt_kernels<LF_PROD_GRAD_X, __nv_bfloat16, __nv_bfloat16>::split();
-        case 3: return lt_kernels<LF_PROD_GRAD_X, __half, __half>::split();
-        case 4: return lt_kernels<LF_PROD_GRAD_W, __nv_bfloat16, __nv_bfloat16>::split();
-        case 5: return lt_kernels<LF_PROD_GRAD_W, __half, __half>::split();
-        case 6: return lt_kernels<LF_PROD_GRAD_W, __nv_bfloat16, float>::split();
-        default: return lt_kernels<LF_PROD_GRAD_W, __half, float>::split();
+        case 0: return lt_pair_of<LF_PROD_FORWARD, __nv_bfloat16, __nv_bfloat16>(tile);
+        case 1: return lt_pair_of<LF_PROD_FORWARD, __half, __half>(tile);
+        case 2: return lt_pair_of<LF_PROD_GRAD_X, __nv_bfloat16, __nv_bfloat16>(tile);
+        case 3: return lt_pair_of<LF_PROD_GRAD_X, __half, __half>(tile);
+        case 4: return lt_pair_of<LF_PROD_GRAD_W, __nv_bfloat16, __nv_bfloat16>(tile);
+        case 5: return lt_pair_of<LF_PROD_GRAD_W, __half, __half>(tile);
+        case 6: return lt_pair_of<LF_PROD_GRAD_W, __nv_bfloat16, float>(tile);
+        default: return lt_pair_of<LF_PROD_GRAD_W, __half, float>(tile);
+    }
+}
+lt_kernel lt_pick_split(int i, int splits)
+{
+    switch (i) {
+        case 0: return lt_split_of<LF_PROD_FORWARD, __nv_bfloat16, __nv_bfloat16>(splits);
+        case 1: return lt_split_of<LF_PROD_FORWARD, __half, __half>(splits);
+        case 2: return lt_split_of<LF_PROD_GRAD_X, __nv_bfloat16, __nv_bfloat16>(splits);
+        case 3: return lt_split_of<LF_PROD_GRAD_X, __half, __half>(splits);
+        case 4: return lt_split_of<LF_PROD_GRAD_W, __nv_bfloat16, __nv_bfloat16>(splits);
+        case 5: return lt_split_of<LF_PROD_GRAD_W, __half, __half>(splits);
+        case 6: return lt_split_of<LF_PROD_GRAD_W, __nv_bfloat16, float>(splits);
+        default: return lt_split_of<LF_PROD_GRAD_W, __half, float>(splits);
     }
 }
 
-void lt_cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int grid, int cluster, size_t smem, cudaStream_t s)
+void lt_cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int grid, int threads, int cluster, size_t smem, cudaStream_t s)
 {
     *cfg = cudaLaunchConfig_t{};
     cfg->gridDim = dim3((unsigned)grid);
-    cfg->blockDim = dim3(LT_THREADS);
+    cfg->blockDim = dim3((unsigned)threads);
     cfg->dynamicSmemBytes = smem;
     cfg->stream = s;
     at->id = cudaLaunchAttributeClusterDimension;
@@ -715,19 +872,55 @@ int lf_product_tc_init(lf_ops* o)
 {
     if (!lt_encode()) return LF_ECUDA;
     o->max_pairs = 0;
-    for (int i = 0; i < 8; ++i) {
-        if (cudaFuncSetAttribute(lt_pick_pair(i), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LP_SMEM) != cudaSuccess ||
-            cudaFuncSetAttribute(lt_pick_split(i), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LS_SMEM) != cudaSuccess)
-            return LF_ECUDA;
-        cudaLaunchConfig_t cfg;
-        cudaLaunchAttribute at[1];
-        lt_cluster_config(&cfg, at, 32, 2, LP_SMEM, nullptr);
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, lt_pick_pair(i), &cfg) != cudaSuccess) return LF_ECUDA;
-        if (i == 0 || n < o->max_pairs) o->max_pairs = n;
+    for (int i = 0; i < LT_KERNELS; ++i) {
+        for (int splits = 1; splits <= 8; splits *= 2)
+            if (cudaFuncSetAttribute(lt_pick_split(i, splits), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LS_SMEM) != cudaSuccess) return LF_ECUDA;
+        for (int tile = 0; tile < LT_TILES; ++tile) {
+            const lt_kernel f = lt_pick_pair(i, tile);
+            if (!f) continue;
+            if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LP_SMEM) != cudaSuccess) return LF_ECUDA;
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute at[1];
+            lt_cluster_config(&cfg, at, 32, LP_THREADS, 2, LP_SMEM, nullptr);
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return LF_ECUDA;
+            if ((i == 0 && tile == 0) || n < o->max_pairs) o->max_pairs = n;
+        }
     }
     return LF_OK;
 }
+
+namespace {
+
+struct lt_choice { int splits, tile; };      // splits = 0: CTA pairs
+
+// The form with the least estimated time, in SM cycles; constants measured on B200 (widths 512 .. 16384, 17 .. 8192
+// tokens).  A 64-deep stage costs a 256 x 256 pair tile 568 cycles, a 512 x 256 one 1024 and a 128 x 128 tile 560
+// (an instruction takes as long for 128 columns as for 256); switching tiles 600, 5000 and, where the
+// parts of a split tile meet, 1500 and the bytes from the other parts at 14 a cycle.
+lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
+{
+    auto waves = [](long long units, int at_once) { return (double)((units + at_once - 1) / at_once); };
+    lt_choice best = {1, 0};
+    double least = 1e30;
+    auto offer = [&](lt_choice c, double cycles) { if (cycles < least) { least = cycles; best = c; } };
+    const long long m128 = (p.M + 127) / 128, m256 = (p.M + 255) / 256, m512 = (p.M + 511) / 512;
+    const long long n128 = (p.N + 127) / 128, n256 = (p.N + 255) / 256;
+    const double rows = p.M < 128 ? p.M / 128.0 : 1.0;
+    for (int splits = 1; splits <= 8 && splits <= n_k; splits *= 2) {
+        const double part = (double)((n_k + splits - 1) / splits);
+        const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
+        const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
+        offer({splits, 0}, waves(m128 * n128 * splits, at_once) * (part * 560.0 + meet + 6500.0));
+    }
+    if (o->max_pairs > 0) {
+        offer({0, LT_256x256}, waves(m256 * n256, o->max_pairs) * (n_k * 568.0 + 600.0) + 10000.0);
+        if (p.out_dtype != LF_F32) offer({0, LT_512x256}, waves(m512 * n256, o->max_pairs) * (n_k * 1024.0 + 5000.0) + 10000.0);
+    }
+    return best;
+}
+
+}  // namespace
 
 int lf_product_tc(lf_ops* o, const lf_product& p)
 {
@@ -750,38 +943,33 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
     if (a_mn) idesc |= 1u << 15;
     if (b_mn) idesc |= 1u << 16;
 
-    alignas(64) CUtensorMap map_a, map_b, map_d;
-    bool ok = a_mn ? lt_map(&map_a, in_type, 2, p.a, p.K, p.M, p.ld_a, 64, 64) : lt_map(&map_a, in_type, 2, p.a, p.M, p.K, p.ld_a, 64, 128);
-    ok = ok && (b_mn ? lt_map(&map_b, in_type, 2, p.b, p.K, p.N, p.ld_b, 64, 64) : lt_map(&map_b, in_type, 2, p.b, p.N, p.K, p.ld_b, 64, 128));
-
     const int n_k = (p.K + LT_BK - 1) / LT_BK;
-    const long long pair_tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256);
+    const lt_choice c = lt_choose(o, p, n_k);
+    alignas(64) CUtensorMap map_a, map_b;
+    const bool ok = (a_mn ? lt_map(&map_a, in_type, p.a, p.K, p.M, p.ld_a, 64, 64) : lt_map(&map_a, in_type, p.a, p.M, p.K, p.ld_a, 64, 128)) &&
+                    (b_mn ? lt_map(&map_b, in_type, p.b, p.K, p.N, p.ld_b, 64, 64) : lt_map(&map_b, in_type, p.b, p.N, p.K, p.ld_b, 64, 128));
+    if (!ok) { o->last_cuda_error = (int)cudaErrorInvalidValue; return LF_ECUDA; }
+
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute at[1];
-    if (o->max_pairs > 0 && pair_tiles * 2 >= o->max_pairs) {
-        P.tiles_m = (p.M + 255) / 256; P.tiles_n = (p.N + 255) / 256;
+    if (c.splits == 0) {
+        const int bm = c.tile == LT_512x256 ? 512 : 256;
+        P.tiles_m = (p.M + bm - 1) / bm; P.tiles_n = (p.N + 255) / 256;
         P.idesc = idesc | (256u >> 3) << 17 | (256u >> 4) << 24;
-        ok = ok && (out32 ? lt_map(&map_d, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, p.d, p.M, p.N, p.ld_d, 32, 32)
-                          : lt_map(&map_d, in_type, 2, p.d, p.M, p.N, p.ld_d, 64, 32));
-        if (!ok) { o->last_cuda_error = (int)cudaErrorInvalidValue; return LF_ECUDA; }
-        const int pairs = pair_tiles < o->max_pairs ? (int)pair_tiles : o->max_pairs;
-        lt_cluster_config(&cfg, at, 2 * pairs, 2, LP_SMEM, o->stream);
-        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_pair(kernel), map_a, map_b, map_d, P));
+        P.band = 2048 / bm;
+        const int tiles = P.tiles_m * P.tiles_n, pairs = tiles < o->max_pairs ? tiles : o->max_pairs;
+        lt_cluster_config(&cfg, at, 2 * pairs, LP_THREADS, 2, LP_SMEM, o->stream);
+        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_pair(kernel, c.tile), map_a, map_b, P));
         o->stats.form = LF_FORM_PAIRS;
         o->stats.splits = 1;
     } else {
-        if (!ok) { o->last_cuda_error = (int)cudaErrorInvalidValue; return LF_ECUDA; }
         P.tiles_m = (p.M + 127) / 128; P.tiles_n = (p.N + 127) / 128;
         P.idesc = idesc | (128u >> 3) << 17 | (128u >> 4) << 24;
-        const long long tiles = (long long)P.tiles_m * P.tiles_n;
-        int splits = 1;
-        while (splits < 8 && tiles * splits * 2 <= o->sm_count && n_k >= splits * 4) splits *= 2;
-        P.splits = splits;
-        P.stages_per_split = (n_k + splits - 1) / splits;
-        lt_cluster_config(&cfg, at, (int)(tiles * splits), splits, LS_SMEM, o->stream);
-        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_split(kernel), map_a, map_b, P));
+        P.stages_per_split = (n_k + c.splits - 1) / c.splits;
+        lt_cluster_config(&cfg, at, P.tiles_m * P.tiles_n * c.splits, LT_THREADS, c.splits, LS_SMEM, o->stream);
+        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_split(kernel, c.splits), map_a, map_b, P));
         o->stats.form = LF_FORM_SPLIT;
-        o->stats.splits = splits;
+        o->stats.splits = c.splits;
     }
     o->stats.launches += 1;
     return LF_OK;

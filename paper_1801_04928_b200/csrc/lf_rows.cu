@@ -266,11 +266,13 @@ __global__ void __launch_bounds__(256) k_unpack8(const unsigned char* q, const u
             float d[8];
             o.load(dy + (size_t)row * ld_dy + 8 * i);
             o.get(d);
+            prime_n<FAST, 8>(d, v, kind);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = d[k] * act_prime<FAST>(v[k], kind);
+            for (int k = 0; k < 8; ++k) v[k] = d[k];
         } else {
+            act_n<FAST, 8>(v, kind);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = clamp_keep_nan(act<FAST>(v[k], kind), max_finite(T()));
+            for (int k = 0; k < 8; ++k) v[k] = clamp_keep_nan(v[k], max_finite(T()));
         }
         o.set(v);
         o.store(x + (size_t)row * ld + 8 * i);

@@ -86,40 +86,121 @@ __device__ __forceinline__ float clamp_keep_nan(float v, float m)
 }
 
 // ---- activations from the pre-activation ----------------------------------------------------------
-// FAST: e^t and the quotient from the special-function unit (about 1e-6 relative, far below the
-// rounding of a 16-bit result); otherwise the correctly scaled library functions, for fp32 results.
-template <bool FAST>
-__device__ __forceinline__ float sigmoid(float t)
+// Two elements at a time: multiplies and additions as packed fp32 (fma.rn.f32x2), which halves their issue slots.
+// FAST: e^t and the reciprocal from the special-function unit (about 1e-6 relative, far below the
+// rounding of a 16-bit result); otherwise the library functions, for fp32 results.
+__device__ __forceinline__ float2 f2(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float ex2(float t)
 {
-    return FAST ? __fdividef(1.0f, 1.0f + __expf(-t)) : 1.0f / (1.0f + expf(-t));
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
+}
+__device__ __forceinline__ float rcp(float t)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
+}
+constexpr float LOG2E = 1.4426950408889634f;
+// 1 / (1 + 2^t): the logistic function of -t ln 2
+__device__ __forceinline__ float2 logistic2(float2 t)
+{
+    const float2 d = add2(f2(1.f), make_float2(ex2(t.x), ex2(t.y)));
+    return make_float2(rcp(d.x), rcp(d.y));
 }
 constexpr float GELU_C = 1.5957691216057308f;            // 2 sqrt(2 / pi)
 constexpr float GELU_D = GELU_C * 0.044715f;
+// a = sigmoid(g(z)) of the three activations built on it: g(z) = z, or GELU's cubic, as (1 + tanh u) / 2 = sigmoid(2 u)
 template <bool FAST>
-__device__ __forceinline__ float act(float z, int kind)
+__device__ __forceinline__ float2 sigmoid_of(float2 z, float2 zz, bool cubic)
 {
-    switch (kind) {
-        case LF_ACT_SIGMOID: return sigmoid<FAST>(z);
-        case LF_ACT_TANH: return tanhf(z);
-        case LF_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-        case LF_ACT_SILU: return z * sigmoid<FAST>(z);
-        case LF_ACT_GELU: return z * sigmoid<FAST>(z * (GELU_C + GELU_D * z * z));   // (1 + tanh u) / 2 = sigmoid(2 u)
-        default: return z;
+    if (FAST) {
+        const float2 p = cubic ? fma2(zz, f2(-LOG2E * GELU_D), f2(-LOG2E * GELU_C)) : f2(-LOG2E);
+        return logistic2(mul2(z, p));
+    }
+    const float2 t = cubic ? mul2(z, fma2(zz, f2(GELU_D), f2(GELU_C))) : z;
+    return make_float2(1.0f / (1.0f + expf(-t.x)), 1.0f / (1.0f + expf(-t.y)));
+}
+// tanh z = 1 - 2 / (1 + e^{2 z}); below 1/16, where that cancels, the Taylor polynomial (next term 17/315 z^7: 3e-9 relative)
+__device__ __forceinline__ float tanh_fast(float z)
+{
+    const float t = fmaf(-2.f, rcp(1.f + ex2(2.f * LOG2E * z)), 1.f), zz = z * z;
+    return fabsf(z) < 0.0625f ? z * fmaf(zz, fmaf(zz, 2.f / 15.f, -1.f / 3.f), 1.f) : t;
+}
+template <bool FAST, int KIND>
+__device__ __forceinline__ float2 act2(float2 z)
+{
+    if (KIND == LF_ACT_SIGMOID) return sigmoid_of<FAST>(z, z, false);
+    if (KIND == LF_ACT_TANH) return FAST ? make_float2(tanh_fast(z.x), tanh_fast(z.y)) : make_float2(tanhf(z.x), tanhf(z.y));
+    if (KIND == LF_ACT_RELU) return make_float2(z.x < 0.f ? 0.f : z.x, z.y < 0.f ? 0.f : z.y);     // NaN stays
+    if (KIND == LF_ACT_SILU) return mul2(z, sigmoid_of<FAST>(z, z, false));
+    if (KIND == LF_ACT_GELU) return mul2(z, sigmoid_of<FAST>(z, mul2(z, z), true));
+    return z;
+}
+template <bool FAST, int KIND>
+__device__ __forceinline__ float2 act_prime2(float2 z)
+{
+    if (KIND == LF_ACT_TANH || KIND == LF_ACT_SIGMOID) {
+        // even functions of z: a (1 - a) with a = sigmoid(-|z|) <= 1/2, where 1 - a does not cancel; tanh' = 4 a (1 - a) at 2 z
+        const float k = KIND == LF_ACT_TANH ? 2.f : 1.f;
+        const float2 a = sigmoid_of<FAST>(make_float2(-k * fabsf(z.x), -k * fabsf(z.y)), z, false);
+        return mul2(mul2(a, f2(k * k)), fma2(a, f2(-1.f), f2(1.f)));
+    }
+    if (KIND == LF_ACT_RELU) return make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
+    if (KIND == LF_ACT_NONE) return f2(1.f);
+    // a + z a (1 - a) g'(z)
+    const float2 zz = mul2(z, z);
+    const float2 a = sigmoid_of<FAST>(z, zz, KIND == LF_ACT_GELU);
+    const float2 na = fma2(a, f2(-1.f), f2(1.f));
+    const float2 zn = KIND == LF_ACT_GELU ? mul2(mul2(z, na), fma2(zz, f2(3.f * GELU_D), f2(GELU_C))) : mul2(z, na);
+    return fma2(a, zn, a);
+}
+// run-time choice outside of the loop over NE elements
+template <bool FAST, int NE, int KIND>
+__device__ __forceinline__ void act_all(float* v)
+{
+#pragma unroll
+    for (int i = 0; i < NE; i += 2) {
+        const float2 r = act2<FAST, KIND>(make_float2(v[i], v[i + 1]));
+        v[i] = r.x; v[i + 1] = r.y;
     }
 }
-template <bool FAST>
-__device__ __forceinline__ float act_prime(float z, int kind)
+template <bool FAST, int NE>
+__device__ __forceinline__ void act_n(float* v, int kind)
 {
     switch (kind) {
-        case LF_ACT_SIGMOID: { const float a = sigmoid<FAST>(z); return a * (1.f - a); }
-        case LF_ACT_TANH: { const float t = tanhf(z); return 1.f - t * t; }
-        case LF_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-        case LF_ACT_SILU: { const float a = sigmoid<FAST>(z); return a + z * a * (1.f - a); }
-        case LF_ACT_GELU: {
-            const float a = sigmoid<FAST>(z * (GELU_C + GELU_D * z * z));
-            return a + z * a * (1.f - a) * (GELU_C + 3.f * GELU_D * z * z);
-        }
-        default: return 1.f;
+        case LF_ACT_SIGMOID: act_all<FAST, NE, LF_ACT_SIGMOID>(v); break;
+        case LF_ACT_TANH: act_all<FAST, NE, LF_ACT_TANH>(v); break;
+        case LF_ACT_RELU: act_all<FAST, NE, LF_ACT_RELU>(v); break;
+        case LF_ACT_SILU: act_all<FAST, NE, LF_ACT_SILU>(v); break;
+        case LF_ACT_GELU: act_all<FAST, NE, LF_ACT_GELU>(v); break;
+        default: break;
+    }
+}
+// d *= sigma'(z)
+template <bool FAST, int NE, int KIND>
+__device__ __forceinline__ void prime_all(float* d, const float* z)
+{
+#pragma unroll
+    for (int i = 0; i < NE; i += 2) {
+        const float2 r = mul2(make_float2(d[i], d[i + 1]), act_prime2<FAST, KIND>(make_float2(z[i], z[i + 1])));
+        d[i] = r.x; d[i + 1] = r.y;
+    }
+}
+template <bool FAST, int NE>
+__device__ __forceinline__ void prime_n(float* d, const float* z, int kind)
+{
+    switch (kind) {
+        case LF_ACT_SIGMOID: prime_all<FAST, NE, LF_ACT_SIGMOID>(d, z); break;
+        case LF_ACT_TANH: prime_all<FAST, NE, LF_ACT_TANH>(d, z); break;
+        case LF_ACT_RELU: prime_all<FAST, NE, LF_ACT_RELU>(d, z); break;
+        case LF_ACT_SILU: prime_all<FAST, NE, LF_ACT_SILU>(d, z); break;
+        case LF_ACT_GELU: prime_all<FAST, NE, LF_ACT_GELU>(d, z); break;
+        default: break;
     }
 }
 
@@ -155,7 +236,8 @@ __device__ __forceinline__ void from_e4m3x4(unsigned q, float s, float& a, float
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h1) : "h"((unsigned short)(q >> 16)));
     const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
     const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-    a = f0.x * s; b = f0.y * s; c = f1.x * s; d = f1.y * s;
+    const float2 g0 = __fmul2_rn(f0, make_float2(s, s)), g1 = __fmul2_rn(f1, make_float2(s, s));
+    a = g0.x; b = g0.y; c = g1.x; d = g1.y;
 }
 // eight columns held by one lane; the four lanes of a group are neighbours (lane & ~3)
 __device__ __forceinline__ unsigned group_byte(const float (&v)[8])
