@@ -77,6 +77,8 @@ __global__ void __launch_bounds__(SR_WARPS * 32, 2) k_linear_stream(const lf_pro
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.f;
 
+    lf_grid_wait();
+    lf_grid_release();
     for (int c = c0; c < c1; c += SR_UNROLL) {
         uint4 a[SR_UNROLL][4], b[SR_UNROLL][TT];
 #pragma unroll
@@ -150,13 +152,15 @@ cudaError_t stream_go(const lf_product& p, int sm_count, cudaStream_t s, int* sp
     while (splits < 8 && tiles * splits < 2 * sm_count && chunks >= splits * 2 * SR_WARPS * 2 * SR_UNROLL) splits *= 2;
     *splits_out = splits;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     cfg.gridDim = dim3((unsigned)(tiles * splits));
     cfg.blockDim = dim3(SR_WARPS * 32);
     cfg.stream = s;
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)splits; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.attrs = at; cfg.numAttrs = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = 2;
     if (p.M <= 8) return cudaLaunchKernelEx(&cfg, k_linear_stream<T, 1>, p, splits);
     return cudaLaunchKernelEx(&cfg, k_linear_stream<T, 2>, p, splits);
 }

@@ -361,6 +361,8 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     lfptx::cluster_sync_all();       // the peer's barriers exist before anything can arrive on them
     lfptx::tc_fence_after();
     const unsigned tmem_base = sh->tmem_base;
+    lf_grid_wait();                  // (by every thread: the bounded waits below do not count the time until then)
+    lf_grid_release();
 
     // registers move from the first warpgroup to the two that hold accumulators
     if (warp < 4) {
@@ -609,6 +611,7 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
         sh->abort_flag = 0u;
         lfptx::mbar_fence_init();
+        lf_grid_wait();
         for (int ks = 0; ks < min(n_k, LS_STAGES); ++ks) load_stage(ks);            // under the rest of the set-up
     }
     if (warp == 1) {
@@ -620,6 +623,8 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     __syncthreads();
     lfptx::tc_fence_after();
     const unsigned tmem_base = sh->tmem_base;
+    lf_grid_wait();
+    lf_grid_release();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -858,12 +863,14 @@ void lt_cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int gri
     cfg->blockDim = dim3((unsigned)threads);
     cfg->dynamicSmemBytes = smem;
     cfg->stream = s;
-    at->id = cudaLaunchAttributeClusterDimension;
-    at->val.clusterDim.x = (unsigned)cluster;
-    at->val.clusterDim.y = 1;
-    at->val.clusterDim.z = 1;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cluster;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg->attrs = at;
-    cfg->numAttrs = 1;
+    cfg->numAttrs = 2;
 }
 
 }  // namespace
@@ -880,7 +887,7 @@ int lf_product_tc_init(lf_ops* o)
             if (!f) continue;
             if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LP_SMEM) != cudaSuccess) return LF_ECUDA;
             cudaLaunchConfig_t cfg;
-            cudaLaunchAttribute at[1];
+            cudaLaunchAttribute at[2];
             lt_cluster_config(&cfg, at, 32, LP_THREADS, 2, LP_SMEM, nullptr);
             int n = 0;
             if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return LF_ECUDA;
@@ -951,7 +958,7 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
     if (!ok) { o->last_cuda_error = (int)cudaErrorInvalidValue; return LF_ECUDA; }
 
     cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     if (c.splits == 0) {
         const int bm = c.tile == LT_512x256 ? 512 : 256;
         P.tiles_m = (p.M + bm - 1) / bm; P.tiles_n = (p.N + 255) / 256;

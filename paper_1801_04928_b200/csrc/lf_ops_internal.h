@@ -37,6 +37,30 @@ constexpr size_t LF_OPS_FIXED_BYTES = (size_t)LF_OPS_PARTIAL_ROWS * LF_OPS_MAX_N
         }                                                       \
     } while (0)
 
+// Kernels of the layer operators may be launched while the kernel before them is still running: each waits for it
+// (lf_grid_wait) before it touches global memory and lets the next one be launched (lf_grid_release) as
+// soon as its own blocks are under way, so that only the set-up overlaps.
+#ifdef __CUDACC__
+__device__ __forceinline__ void lf_grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void lf_grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t lf_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+#endif
+
 inline size_t lf_groups(int n) { return ((size_t)n + 31) / 32; }
 
 typedef CUresult (*lf_encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,

@@ -36,6 +36,8 @@ __global__ void __launch_bounds__(TPR) k_rms_norm(const lf_rms_norm_args a)
     __shared__ float red[TPR / 32];
     const int nv = a.n >> 3;
     const size_t gpr = (size_t)((a.n + 31) / 32);
+    lf_grid_wait();
+    lf_grid_release();
     for (int row = blockIdx.x; row < a.tokens; row += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + (size_t)row * a.ld_x;
         vec8<T> xv[VPT], rv[VPT];
@@ -100,75 +102,148 @@ __global__ void __launch_bounds__(TPR) k_rms_norm(const lf_rms_norm_args a)
 }
 
 // ---- dh = r (u - h r mean(u h r)) + dres, partial column sums of dy h r -----------------------------
-template <typename T, int TPR, int VPT>
-__global__ void __launch_bounds__(TPR) k_rms_norm_backward(const lf_rms_norm_backward_args a, float* partial)
+// Groups of TPR threads take a row at a time and walk down the matrix.  The rows ahead are on their way into shared
+// memory meanwhile (cp.async; a thread copies exactly what it will read itself, so the ring needs no
+// barriers), which keeps the memory busy through the row's two phases: with the row loaded into registers at
+// the top of the loop instead, 16384 x 8192 took 283 us, 3.8 TB/s.  Both row sums share one exchange, in
+// buffers that alternate, so a row has one barrier.  The gain's gradient stays in registers, eight
+// columns per vector; the groups of a block add theirs at the end, one partial row per block.
+__device__ __forceinline__ void cp_async16(unsigned dst, const void* src)
 {
-    __shared__ float red[TPR / 32], red2[TPR / 32];
-    const int nv = a.n >> 3;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+template <typename T, int TPR, int VPT, int GROUPS>
+__global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms_norm_backward_args a, float* partial, int depth)
+{
+    extern __shared__ __align__(16) unsigned char ring[];      // [depth][tensor][VPT][thread] pieces of eight elements
+    __shared__ float2 red[2][GROUPS][TPR / 32];
+    constexpr int PIECE = 8 * (int)sizeof(T), THREADS = TPR * GROUPS;
+    const int nv = a.n >> 3, t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+    const int tensors = a.dres ? 3 : 2;
+    const unsigned slot_bytes = (unsigned)(tensors * VPT) * THREADS * PIECE;
+    auto piece = [&](int slot, int tensor, int j) { return ring + (size_t)slot * slot_bytes + ((size_t)(tensor * VPT + j) * THREADS + threadIdx.x) * PIECE; };
+    const int stride = gridDim.x * GROUPS, first = blockIdx.x * GROUPS + g;
+    auto fetch = [&](int row, int slot) {
+        if (row < a.tokens) {
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const int i = j * TPR + t;
+                if (i >= nv) continue;
+                const T* src[3] = {static_cast<const T*>(a.h) + (size_t)row * a.ld_h, static_cast<const T*>(a.dy) + (size_t)row * a.ld_dy,
+                                   static_cast<const T*>(a.dres) + (size_t)row * a.ld_dres};
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    if (k == 2 && tensors < 3) continue;
+                    const unsigned dst = (unsigned)__cvta_generic_to_shared(piece(slot, k, j));
+#pragma unroll
+                    for (int c = 0; c < PIECE / 16; ++c) cp_async16(dst + 16 * c, src[k] + 8 * i + c * (16 / (int)sizeof(T)));
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    lf_grid_wait();
+    for (int d = 0; d < depth - 1; ++d) fetch(first + d * stride, d);
     float dg[VPT][8];
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
         for (int k = 0; k < 8; ++k) dg[j][k] = 0.f;
-    for (int row = blockIdx.x; row < a.tokens; row += gridDim.x) {
-        vec8<T> hv[VPT], yv[VPT], rv[VPT];
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int i = j * TPR + threadIdx.x;
-            hv[j].zero(); yv[j].zero(); rv[j].zero();
-            if (i < nv) {
-                hv[j].load(static_cast<const T*>(a.h) + (size_t)row * a.ld_h + 8 * i);
-                yv[j].load(static_cast<const T*>(a.dy) + (size_t)row * a.ld_dy + 8 * i);
-                if (a.dres) rv[j].load(static_cast<const T*>(a.dres) + (size_t)row * a.ld_dres + 8 * i);
-            }
-        }
+    // every group of the block makes the same number of steps: the barrier is the block's
+    const int steps = (a.tokens - blockIdx.x * GROUPS + stride - 1) / stride;
+    int slot = 0;
+    for (int st = 0; st < steps; ++st) {
+        const int row = first + st * stride;
+        int ahead = slot + depth - 1;
+        if (ahead >= depth) ahead -= depth;
+        fetch(row + (depth - 1) * stride, ahead);
+        // all but the newest depth - 1 groups of copies have landed
+        if (depth == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        const bool live = row < a.tokens;
+        vec8<T> hv[VPT], yv[VPT];
         float ss = 0.f, su = 0.f;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int i = j * TPR + threadIdx.x;
-            float h[8], y[8], g[8];
+            const int i = j * TPR + t;
+            hv[j].zero(); yv[j].zero();
+            if (!live || i >= nv) continue;
+            hv[j].load(reinterpret_cast<const T*>(piece(slot, 0, j)));
+            yv[j].load(reinterpret_cast<const T*>(piece(slot, 1, j)));
+            float h[8], y[8], gn[8];
             vec8<float> gv;
-            gv.zero();
-            if (i < nv) gv.load(a.gain + 8 * i);
-            gv.get(g);
+            gv.load(a.gain + 8 * i);
+            gv.get(gn);
             hv[j].get(h);
             yv[j].get(y);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 ss = fmaf(h[k], h[k], ss);
-                su = fmaf(g[k] * y[k], h[k], su);
+                su = fmaf(gn[k] * y[k], h[k], su);
             }
         }
-        ss = row_sum<TPR>(ss, red);
-        su = row_sum<TPR>(su, red2);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+            su += __shfl_xor_sync(0xFFFFFFFFu, su, o);
+        }
+        if (TPR > 32) {
+            if ((threadIdx.x & 31) == 0) red[st & 1][g][t >> 5] = make_float2(ss, su);
+            __syncthreads();
+            ss = su = 0.f;
+#pragma unroll
+            for (int i = 0; i < TPR / 32; ++i) { const float2 p = red[st & 1][g][i]; ss += p.x; su += p.y; }
+        }
         const float r = 1.0f / sqrtf(ss / (float)a.n + a.eps);
         const float c = su * r * r / (float)a.n;         // mean(u h r) r
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int i = j * TPR + threadIdx.x;
-            if (i >= nv) continue;
-            float h[8], y[8], g[8], d[8];
+            const int i = j * TPR + t;
+            if (!live || i >= nv) continue;
+            float h[8], y[8], gn[8], d[8];
             vec8<float> gv;
+            vec8<T> o;
             gv.load(a.gain + 8 * i);
-            gv.get(g);
+            gv.get(gn);
             hv[j].get(h);
             yv[j].get(y);
-            rv[j].get(d);
+            if (a.dres) { o.load(reinterpret_cast<const T*>(piece(slot, 2, j))); o.get(d); }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 dg[j][k] = fmaf(y[k], h[k] * r, dg[j][k]);
-                const float t = r * (g[k] * y[k] - h[k] * c);
-                d[k] = a.dres ? t + d[k] : t;
+                const float v = r * (gn[k] * y[k] - h[k] * c);
+                d[k] = a.dres ? v + d[k] : v;
             }
-            vec8<T> o;
             o.set(d);
             o.store(static_cast<T*>(a.dh) + (size_t)row * a.ld_dh + 8 * i);
         }
+        if (++slot == depth) slot = 0;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    lf_grid_release();
     if (partial) {
+        if (GROUPS > 1) {
+            // add the groups' sums in group order (the ring is free; it holds at least eight floats per thread and vector)
+            float* all = reinterpret_cast<float*>(ring);
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < VPT; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) all[(size_t)(j * 8 + k) * THREADS + threadIdx.x] = dg[j][k];
+            __syncthreads();
+            if (g > 0) return;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int o = 1; o < GROUPS; ++o) dg[j][k] += all[(size_t)(j * 8 + k) * THREADS + o * TPR + t];
+        }
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int i = j * TPR + threadIdx.x;
+            const int i = j * TPR + t;
             if (i < nv) {
                 vec8<float> o;
                 o.set(dg[j]);
@@ -178,22 +253,23 @@ __global__ void __launch_bounds__(TPR) k_rms_norm_backward(const lf_rms_norm_bac
     }
 }
 
-// out[c] = sum over the rows of partial[rows][n], in row order per thread group, then across groups
-__global__ void __launch_bounds__(256) k_sum_rows(const float* partial, int rows, int n, float* out)
+// out[c] = sum over the rows of partial[rows][n]: a block has 32 columns and 32 runs of rows, added in a fixed order
+__global__ void __launch_bounds__(1024) k_sum_rows(const float* partial, int rows, int n, float* out)
 {
-    __shared__ float red[8][33];
+    __shared__ float red[32][33];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
     float v = 0.f;
-    if (c < n)
-        for (int r = g; r < rows; r += 8) v += partial[(size_t)r * n + c];
+    lf_grid_wait();
+    if (c < n) {
+#pragma unroll 8
+        for (int r = g; r < rows; r += 32) v += partial[(size_t)r * n + c];
+    }
     red[g][threadIdx.x & 31] = v;
     __syncthreads();
-    if (g == 0 && c < n) {
-        float t = 0.f;
+    v = red[threadIdx.x & 31][g];            // column g, run (lane)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t += red[i][threadIdx.x & 31];
-        out[c] = t;
-    }
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if ((threadIdx.x & 31) == 0 && blockIdx.x * 32 + g < n) out[blockIdx.x * 32 + g] = v;
 }
 
 // column sums of a 16-bit matrix: a block takes 256 columns (a warp all of them, eight per lane) and every
@@ -204,6 +280,8 @@ __global__ void __launch_bounds__(256) k_colsum16(const T* x, long long ld, int 
     __shared__ float red[8][256];
     const int c = blockIdx.x * 256 + (threadIdx.x & 31) * 8, w = threadIdx.x >> 5;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    lf_grid_wait();
+    lf_grid_release();
     if (c < n) {
 #pragma unroll 4
         for (int r = blockIdx.y * 8 + w; r < tokens; r += gridDim.y * 8) {
@@ -228,54 +306,99 @@ __global__ void __launch_bounds__(256) k_colsum16(const T* x, long long ld, int 
 }
 
 // ---- 8-bit form -------------------------------------------------------------------------------------
-// Threads run along the row (blockIdx.x) and take every gridDim.y-th row.
+// Threads run along the row (blockIdx.x) and take every gridDim.y-th row, ROWS_AT_ONCE of them at a time, all loads
+// ahead of the first use.
+constexpr int ROWS_AT_ONCE = 4;
 template <typename T>
 __global__ void __launch_bounds__(256) k_pack8(const T* x, long long ld, int tokens, int n, unsigned char* q, unsigned char* s)
 {
     const int i = blockIdx.x * 256 + threadIdx.x, nv = n >> 3;
     if ((i & ~31) >= nv) return;             // whole warps only: the group maximum is taken across lanes
     const size_t gpr = (size_t)((n + 31) / 32);
-    for (int row = blockIdx.y; row < tokens; row += gridDim.y) {
-        vec8<T> v;
-        v.zero();
-        if (i < nv) v.load(x + (size_t)row * ld + 8 * i);
-        float f[8];
-        v.get(f);
-        const unsigned b = group_byte(f);
-        if (i < nv) {
-            *reinterpret_cast<uint2*>(q + (size_t)row * n + 8 * i) = quantize8(f, b);
-            if ((i & 3) == 0) s[(size_t)row * gpr + (i >> 2)] = (unsigned char)b;
+    lf_grid_wait();
+    lf_grid_release();
+    for (int row0 = blockIdx.y; row0 < tokens; row0 += ROWS_AT_ONCE * gridDim.y) {
+        vec8<T> v[ROWS_AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+            const int row = row0 + u * gridDim.y;
+            v[u].zero();
+            if (i < nv && row < tokens) v[u].load(x + (size_t)row * ld + 8 * i);
+        }
+#pragma unroll
+        for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+            const int row = row0 + u * gridDim.y;
+            float f[8];
+            v[u].get(f);
+            const unsigned b = group_byte(f);
+            if (i < nv && row < tokens) {
+                *reinterpret_cast<uint2*>(q + (size_t)row * n + 8 * i) = quantize8(f, b);
+                if ((i & 3) == 0) s[(size_t)row * gpr + (i >> 2)] = (unsigned char)b;
+            }
         }
     }
 }
 
 // GRAD = false: x = sigma(value);  GRAD = true: x = dy * sigma'(value)
+template <typename T, bool GRAD, int KIND>
+__device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsigned char* s, const T* dy, long long ld_dy, int tokens, int n,
+                                            T* x, long long ld)
+{
+    constexpr bool FAST = sizeof(T) == 2;
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= (n >> 3)) return;
+    const size_t gpr = (size_t)((n + 31) / 32);
+    for (int row0 = blockIdx.y; row0 < tokens; row0 += ROWS_AT_ONCE * gridDim.y) {
+        uint2 qv[ROWS_AT_ONCE];
+        unsigned sv[ROWS_AT_ONCE];
+        vec8<T> dv[ROWS_AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+            const int row = row0 + u * gridDim.y;
+            qv[u] = make_uint2(0, 0);
+            sv[u] = 0;
+            dv[u].zero();
+            if (row < tokens) {
+                qv[u] = *reinterpret_cast<const uint2*>(q + (size_t)row * n + 8 * i);
+                sv[u] = s[(size_t)row * gpr + (i >> 2)];
+                if (GRAD) dv[u].load(dy + (size_t)row * ld_dy + 8 * i);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+            const int row = row0 + u * gridDim.y;
+            if (row >= tokens) break;
+            float v[8];
+            dequantize8(qv[u], sv[u], v);
+            vec8<T> o;
+            if (GRAD) {
+                float d[8];
+                dv[u].get(d);
+                prime_all<FAST, 8, KIND>(d, v);
+                o.set(d);
+            } else {
+                act_all<FAST, 8, KIND>(v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = clamp_keep_nan(v[k], max_finite(T()));
+                o.set(v);
+            }
+            o.store(x + (size_t)row * ld + 8 * i);
+        }
+    }
+}
 template <typename T, bool GRAD>
 __global__ void __launch_bounds__(256) k_unpack8(const unsigned char* q, const unsigned char* s, const T* dy,
                                                  long long ld_dy, int tokens, int n, int kind, T* x, long long ld)
 {
-    constexpr bool FAST = sizeof(T) == 2;
-    const int i = blockIdx.x * 256 + threadIdx.x, nv = n >> 3;
-    if (i >= nv) return;
-    const size_t gpr = (size_t)((n + 31) / 32);
-    for (int row = blockIdx.y; row < tokens; row += gridDim.y) {
-        float v[8];
-        dequantize8(*reinterpret_cast<const uint2*>(q + (size_t)row * n + 8 * i), s[(size_t)row * gpr + (i >> 2)], v);
-        vec8<T> o;
-        if (GRAD) {
-            float d[8];
-            o.load(dy + (size_t)row * ld_dy + 8 * i);
-            o.get(d);
-            prime_n<FAST, 8>(d, v, kind);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = d[k];
-        } else {
-            act_n<FAST, 8>(v, kind);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = clamp_keep_nan(v[k], max_finite(T()));
-        }
-        o.set(v);
-        o.store(x + (size_t)row * ld + 8 * i);
+    lf_grid_wait();
+    lf_grid_release();
+    switch (kind) {
+        case LF_ACT_SIGMOID: unpack_rows<T, GRAD, LF_ACT_SIGMOID>(q, s, dy, ld_dy, tokens, n, x, ld); break;
+        case LF_ACT_TANH: unpack_rows<T, GRAD, LF_ACT_TANH>(q, s, dy, ld_dy, tokens, n, x, ld); break;
+        case LF_ACT_RELU: unpack_rows<T, GRAD, LF_ACT_RELU>(q, s, dy, ld_dy, tokens, n, x, ld); break;
+        case LF_ACT_SILU: unpack_rows<T, GRAD, LF_ACT_SILU>(q, s, dy, ld_dy, tokens, n, x, ld); break;
+        case LF_ACT_GELU: unpack_rows<T, GRAD, LF_ACT_GELU>(q, s, dy, ld_dy, tokens, n, x, ld); break;
+        default: unpack_rows<T, GRAD, LF_ACT_NONE>(q, s, dy, ld_dy, tokens, n, x, ld); break;
     }
 }
 
@@ -291,46 +414,54 @@ dim3 row_grid(int tokens, int n, int sm_count)
 // Threads per row: four vectors per thread when there are rows enough to fill the device, otherwise
 // one, so that a few rows are read by as many threads as they have vectors.
 template <template <typename, int, int> class F, typename T, typename... A>
-void pick_row_shape(int n, bool many, A&&... args)
+cudaError_t pick_row_shape(int n, bool many, A&&... args)
 {
     const int nv = n >> 3;
     if (many) {
-        if (nv <= 32) F<T, 32, 1>::go(args...);
-        else if (nv <= 64) F<T, 32, 2>::go(args...);
-        else if (nv <= 128) F<T, 32, 4>::go(args...);
-        else if (nv <= 256) F<T, 64, 4>::go(args...);
-        else if (nv <= 512) F<T, 128, 4>::go(args...);
-        else if (nv <= 1024) F<T, 256, 4>::go(args...);
-        else F<T, 512, 4>::go(args...);
+        if (nv <= 32) return F<T, 32, 1>::go(args...);
+        else if (nv <= 64) return F<T, 32, 2>::go(args...);
+        else if (nv <= 128) return F<T, 32, 4>::go(args...);
+        else if (nv <= 256) return F<T, 64, 4>::go(args...);
+        else if (nv <= 512) return F<T, 128, 4>::go(args...);
+        else if (nv <= 1024) return F<T, 256, 4>::go(args...);
+        else return F<T, 512, 4>::go(args...);
     } else {
-        if (nv <= 32) F<T, 32, 1>::go(args...);
-        else if (nv <= 128) F<T, 128, 1>::go(args...);
-        else if (nv <= 512) F<T, 512, 1>::go(args...);
-        else if (nv <= 1024) F<T, 512, 2>::go(args...);
-        else F<T, 512, 4>::go(args...);
+        if (nv <= 32) return F<T, 32, 1>::go(args...);
+        else if (nv <= 128) return F<T, 128, 1>::go(args...);
+        else if (nv <= 512) return F<T, 512, 1>::go(args...);
+        else if (nv <= 1024) return F<T, 512, 2>::go(args...);
+        else return F<T, 512, 4>::go(args...);
     }
 }
 
 template <typename T, int TPR, int VPT>
 struct norm_go {
-    static void go(const lf_rms_norm_args& a, int sm_count, cudaStream_t s)
+    static cudaError_t go(const lf_rms_norm_args& a, int sm_count, cudaStream_t s)
     {
         const int per_sm = 2048 / TPR < 16 ? 2048 / TPR : 16;
         const int grid = a.tokens < sm_count * per_sm ? a.tokens : sm_count * per_sm;
-        k_rms_norm<T, TPR, VPT><<<grid, TPR, 0, s>>>(a);
+        return lf_launch(k_rms_norm<T, TPR, VPT>, dim3(grid), TPR, 0, s, a);
     }
 };
+// A block has about 256 threads: several rows side by side where a row takes fewer.  The ring is as deep as shared
+// memory allows with two blocks per multiprocessor, up to four rows.
 template <typename T, int TPR, int VPT>
 struct norm_backward_go {
-    static void go(const lf_rms_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* grid_out)
+    static cudaError_t go(const lf_rms_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* grid_out)
     {
-        const int per_sm = 1024 / TPR < 8 ? 1024 / TPR : 8;
-        // partial sums: one row per block, within the fixed workspace
-        long long most = (long long)(LF_OPS_FIXED_BYTES / sizeof(float)) / a.n;
-        if (most > (long long)sm_count * per_sm) most = (long long)sm_count * per_sm;
-        const int grid = a.tokens < most ? a.tokens : (int)most;
-        k_rms_norm_backward<T, TPR, VPT><<<grid, TPR, 0, s>>>(a, a.dgain ? partial : nullptr);
+        constexpr int GROUPS = TPR >= 256 ? 1 : 256 / TPR;
+        const auto kernel = k_rms_norm_backward<T, TPR, VPT, GROUPS>;
+        const size_t slot = (size_t)(a.dres ? 3 : 2) * VPT * TPR * GROUPS * 8 * sizeof(T), most = 110 * 1024;
+        const long long blocks = ((long long)a.tokens + GROUPS - 1) / GROUPS;
+        const int at_most = 2 * sm_count < LF_OPS_PARTIAL_ROWS ? 2 * sm_count : LF_OPS_PARTIAL_ROWS;
+        const int grid = blocks < at_most ? (int)blocks : at_most;
+        int depth = 4;
+        while (depth > 1 && slot * depth > most) --depth;
+        if (depth == 1 && slot * 2 <= 220 * 1024) depth = 2;       // one block per multiprocessor, two rows in flight
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(slot * depth));
+        if (e != cudaSuccess) return e;
         *grid_out = grid;
+        return lf_launch(kernel, dim3(grid), TPR * GROUPS, slot * depth, s, a, a.dgain ? partial : nullptr, depth);
     }
 };
 
@@ -339,10 +470,14 @@ struct norm_backward_go {
 cudaError_t lfk_rms_norm(const lf_rms_norm_args& a, int sm_count, cudaStream_t s)
 {
     const bool many = a.tokens >= 2 * sm_count;
-    if (a.dtype == LF_F32) pick_row_shape<norm_go, float>(a.n, many, a, sm_count, s);
-    else if (a.dtype == LF_BF16) pick_row_shape<norm_go, __nv_bfloat16>(a.n, many, a, sm_count, s);
-    else pick_row_shape<norm_go, __half>(a.n, many, a, sm_count, s);
-    return cudaGetLastError();
+    if (a.dtype == LF_F32) return pick_row_shape<norm_go, float>(a.n, many, a, sm_count, s);
+    if (a.dtype == LF_BF16) return pick_row_shape<norm_go, __nv_bfloat16>(a.n, many, a, sm_count, s);
+    return pick_row_shape<norm_go, __half>(a.n, many, a, sm_count, s);
+}
+
+static cudaError_t sum_rows(const float* partial, int rows, int n, float* out, cudaStream_t s)
+{
+    return lf_launch(k_sum_rows, dim3((unsigned)ceil_div(n, 32)), 1024, 0, s, partial, rows, n, out);
 }
 
 cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s,
@@ -350,41 +485,41 @@ cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* par
 {
     const bool many = a.tokens >= 2 * sm_count;
     int grid = 0;
-    if (a.dtype == LF_F32) pick_row_shape<norm_backward_go, float>(a.n, many, a, partial, sm_count, s, &grid);
-    else if (a.dtype == LF_BF16) pick_row_shape<norm_backward_go, __nv_bfloat16>(a.n, many, a, partial, sm_count, s, &grid);
-    else pick_row_shape<norm_backward_go, __half>(a.n, many, a, partial, sm_count, s, &grid);
+    cudaError_t e;
+    if (a.dtype == LF_F32) e = pick_row_shape<norm_backward_go, float>(a.n, many, a, partial, sm_count, s, &grid);
+    else if (a.dtype == LF_BF16) e = pick_row_shape<norm_backward_go, __nv_bfloat16>(a.n, many, a, partial, sm_count, s, &grid);
+    else e = pick_row_shape<norm_backward_go, __half>(a.n, many, a, partial, sm_count, s, &grid);
     *launches = 1;
-    if (a.dgain) {
-        k_sum_rows<<<ceil_div(a.n, 32), 256, 0, s>>>(partial, grid, a.n, a.dgain);
+    if (e == cudaSuccess && a.dgain) {
+        e = sum_rows(partial, grid, a.n, a.dgain, s);
         *launches = 2;
     }
-    return cudaGetLastError();
+    return e;
 }
 
 cudaError_t lfk_pack8(int dtype, int tokens, int n, const void* x, long long ld, unsigned char* q, unsigned char* s8,
                       int sm_count, cudaStream_t s)
 {
     const dim3 g = row_grid(tokens, n, sm_count);
-    if (dtype == LF_F32) k_pack8<float><<<g, 256, 0, s>>>(static_cast<const float*>(x), ld, tokens, n, q, s8);
-    else if (dtype == LF_BF16) k_pack8<__nv_bfloat16><<<g, 256, 0, s>>>(static_cast<const __nv_bfloat16*>(x), ld, tokens, n, q, s8);
-    else k_pack8<__half><<<g, 256, 0, s>>>(static_cast<const __half*>(x), ld, tokens, n, q, s8);
-    return cudaGetLastError();
+    if (dtype == LF_F32) return lf_launch(k_pack8<float>, g, 256, 0, s, static_cast<const float*>(x), ld, tokens, n, q, s8);
+    if (dtype == LF_BF16) return lf_launch(k_pack8<__nv_bfloat16>, g, 256, 0, s, static_cast<const __nv_bfloat16*>(x), ld, tokens, n, q, s8);
+    return lf_launch(k_pack8<__half>, g, 256, 0, s, static_cast<const __half*>(x), ld, tokens, n, q, s8);
 }
 
+template <typename T, bool GRAD>
+static cudaError_t unpack_of(int act, int tokens, int n, const void* dy, long long ld_dy, const unsigned char* q, const unsigned char* s8,
+                             void* x, long long ld, int sm_count, cudaStream_t s)
+{
+    return lf_launch(k_unpack8<T, GRAD>, row_grid(tokens, n, sm_count), 256, 0, s, q, s8, static_cast<const T*>(dy), ld_dy, tokens, n, act,
+                     static_cast<T*>(x), ld);
+}
 template <bool GRAD>
 static cudaError_t unpack_any(int dtype, int act, int tokens, int n, const void* dy, long long ld_dy, const unsigned char* q,
                               const unsigned char* s8, void* x, long long ld, int sm_count, cudaStream_t s)
 {
-    const dim3 g = row_grid(tokens, n, sm_count);
-    if (dtype == LF_F32)
-        k_unpack8<float, GRAD><<<g, 256, 0, s>>>(q, s8, static_cast<const float*>(dy), ld_dy, tokens, n, act, static_cast<float*>(x), ld);
-    else if (dtype == LF_BF16)
-        k_unpack8<__nv_bfloat16, GRAD><<<g, 256, 0, s>>>(q, s8, static_cast<const __nv_bfloat16*>(dy), ld_dy, tokens, n, act,
-                                                         static_cast<__nv_bfloat16*>(x), ld);
-    else
-        k_unpack8<__half, GRAD><<<g, 256, 0, s>>>(q, s8, static_cast<const __half*>(dy), ld_dy, tokens, n, act,
-                                                  static_cast<__half*>(x), ld);
-    return cudaGetLastError();
+    if (dtype == LF_F32) return unpack_of<float, GRAD>(act, tokens, n, dy, ld_dy, q, s8, x, ld, sm_count, s);
+    if (dtype == LF_BF16) return unpack_of<__nv_bfloat16, GRAD>(act, tokens, n, dy, ld_dy, q, s8, x, ld, sm_count, s);
+    return unpack_of<__half, GRAD>(act, tokens, n, dy, ld_dy, q, s8, x, ld, sm_count, s);
 }
 
 cudaError_t lfk_unpack8(int dtype, int act, int tokens, int n, const unsigned char* q, const unsigned char* s8, void* x,
@@ -405,18 +540,18 @@ cudaError_t lfk_colsum16(int dtype, int tokens, int n, const void* x, long long 
 {
     const int bx = ceil_div(n, 256);
     long long by = ceil_div((long long)sm_count * 4, bx);
-    const long long most = (long long)(LF_OPS_FIXED_BYTES / sizeof(float)) / n, rows8 = ceil_div(tokens, 8);
+    const long long most = (long long)(LF_OPS_FIXED_BYTES / sizeof(float)) / n, rows16 = ceil_div(tokens, 128);
     if (by > most) by = most;
-    if (by > rows8) by = rows8;
+    if (by > rows16) by = rows16;             // at least 16 rows per warp
     if (by < 1) by = 1;
     const dim3 g((unsigned)bx, (unsigned)by);
     float* to = by == 1 ? out : partial;
-    if (dtype == LF_BF16) k_colsum16<__nv_bfloat16><<<g, 256, 0, s>>>(static_cast<const __nv_bfloat16*>(x), ld, tokens, n, to);
-    else k_colsum16<__half><<<g, 256, 0, s>>>(static_cast<const __half*>(x), ld, tokens, n, to);
+    cudaError_t e = dtype == LF_BF16 ? lf_launch(k_colsum16<__nv_bfloat16>, g, 256, 0, s, static_cast<const __nv_bfloat16*>(x), ld, tokens, n, to)
+                                     : lf_launch(k_colsum16<__half>, g, 256, 0, s, static_cast<const __half*>(x), ld, tokens, n, to);
     *launches += 1;
-    if (by > 1) {
-        k_sum_rows<<<ceil_div(n, 32), 256, 0, s>>>(partial, (int)by, n, out);
+    if (e == cudaSuccess && by > 1) {
+        e = sum_rows(partial, (int)by, n, out, s);
         *launches += 1;
     }
-    return cudaGetLastError();
+    return e;
 }
