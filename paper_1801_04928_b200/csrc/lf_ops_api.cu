@@ -10,7 +10,6 @@ namespace {
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 constexpr int MAX_TOKENS = 1 << 30;      // row counters of the kernels are ints with room for a grid stride
-constexpr int MAX_WIDTH = 1 << 24;
 
 // Collects the findings of one call; the order of precedence is the header's.
 struct checker {
@@ -26,7 +25,7 @@ struct checker {
     void type(int t) { ok(t == LF_F32 || t == LF_BF16 || t == LF_F16); }
     void type16(int t) { ok(t == LF_BF16 || t == LF_F16); }
     void act(int a) { ok(a >= LF_ACT_SIGMOID && a <= LF_ACT_GELU); }
-    void width(int n) { ok(n >= 8 && n <= MAX_WIDTH && (n & 7) == 0); }
+    void width(int n) { ok(n >= 8 && n <= LF_OPS_MAX_WIDTH && (n & 7) == 0); }
     // the stride of a matrix's rows; 0 = contiguous
     void ld(long long l, int n, int dtype) { ok(l == 0 || (l >= n && l % (dtype == LF_F32 ? 4 : 8) == 0 && l < (1ll << 36))); }
     int result() const { return null_ ? LF_ENULL : invalid ? LF_EINVAL : misaligned ? LF_EALIGN : LF_OK; }
@@ -62,9 +61,11 @@ int lf_ops_create(lf_ops** out, long long workspace_bytes)
     o->ws_bytes = (size_t)workspace_bytes;
     bool ok = cudaMalloc(&o->ws, o->ws_bytes) == cudaSuccess;
     ok = ok && cudaMalloc(&o->status_dev, sizeof(unsigned)) == cudaSuccess;
+    ok = ok && cudaMalloc(&o->counters, LF_OPS_COUNTERS * sizeof(unsigned)) == cudaSuccess;
+    ok = ok && cudaMemset(o->counters, 0, LF_OPS_COUNTERS * sizeof(unsigned)) == cudaSuccess;
     ok = ok && cudaMallocHost(&o->status_host, sizeof(unsigned)) == cudaSuccess;
     ok = ok && cudaMemset(o->status_dev, 0, sizeof(unsigned)) == cudaSuccess;
-    ok = ok && lf_product_tc_init(o) == LF_OK;
+    ok = ok && lf_product_tc_init(o) == LF_OK && lf_linear_stream_init() == LF_OK;
     if (!ok) {
         const cudaError_t e = cudaGetLastError();
         lf_ops_destroy(o);
@@ -127,6 +128,7 @@ int lf_ops_destroy(lf_ops* o)
     if (!o) return LF_ENULL;
     cudaStreamSynchronize(o->stream);
     if (o->ws) cudaFree(o->ws);
+    if (o->counters) cudaFree(o->counters);
     if (o->status_dev) cudaFree(o->status_dev);
     if (o->status_host) cudaFreeHost(o->status_host);
     delete o;
@@ -153,7 +155,8 @@ int lf_linear(lf_ops* o, const lf_linear_args* a)
     p.add = a->residual; p.ld_add = ld_or(a->ld_residual, a->n_out);
     p.q = a->q; p.s = a->s;
     if (a->tokens <= LF_STREAM_MAX_TOKENS) {
-        LF_OPS_TRY(o, lfk_linear_stream(p, o->sm_count, o->stream, &o->stats.splits));
+        LF_OPS_TRY(o, lfk_linear_stream(p, o->sm_count, o->stream));
+        o->stats.splits = 1;
         o->stats.form = LF_FORM_STREAM;
         o->stats.launches = 1;
         return LF_OK;
@@ -207,13 +210,13 @@ int lf_linear_grad_w(lf_ops* o, const lf_linear_grad_w_args* a)
     if (a->q) {
         if (LF_OPS_FIXED_BYTES + (size_t)a->tokens * a->n_in * 2 > o->ws_bytes) return LF_ECAPACITY;
         void* to = o->ws + LF_OPS_FIXED_BYTES;
-        LF_OPS_TRY(o, lfk_unpack8(a->dtype, a->act, a->tokens, a->n_in, a->q, a->s, to, a->n_in, o->sm_count, o->stream));
-        o->stats.launches += 1;
         x = to; ld_x = a->n_in;
     }
-    if (a->gb)
-        LF_OPS_TRY(o, lfk_colsum16(a->dtype, a->tokens, a->n_out, a->dz, ld_or(a->ld_dz, a->n_out), a->gb,
-                                   reinterpret_cast<float*>(o->ws), o->sm_count, o->stream, &o->stats.launches));
+    if (a->q || a->gb) {
+        LF_OPS_TRY(o, lfk_grad_w_prepare(*a, ld_or(a->ld_dz, a->n_out), o->ws + LF_OPS_FIXED_BYTES, reinterpret_cast<float*>(o->ws), o->counters,
+                                         o->sm_count, o->stream));
+        o->stats.launches += 1;
+    }
     lf_product p = {};
     p.prod = LF_PROD_GRAD_W; p.dtype = a->dtype; p.out_dtype = a->gw_dtype; p.act = LF_ACT_NONE;
     p.M = a->n_out; p.N = a->n_in; p.K = a->tokens;

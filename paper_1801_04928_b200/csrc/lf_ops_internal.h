@@ -14,6 +14,7 @@ struct lf_ops {
     cudaStream_t stream;
     unsigned char* ws;          // workspace: fixed part first, then the unpacked layer input
     size_t ws_bytes;
+    unsigned* counters;         // LF_OPS_COUNTERS words, zero between calls
     unsigned* status_dev;
     unsigned* status_host;
     long long wait_budget_us;
@@ -27,6 +28,9 @@ struct lf_ops {
 constexpr int LF_OPS_MAX_NORM = 16384;
 constexpr int LF_OPS_PARTIAL_ROWS = 320;
 constexpr size_t LF_OPS_FIXED_BYTES = (size_t)LF_OPS_PARTIAL_ROWS * LF_OPS_MAX_NORM * sizeof(float);
+
+constexpr int LF_OPS_MAX_WIDTH = 1 << 24;
+constexpr int LF_OPS_COUNTERS = LF_OPS_MAX_WIDTH / 256;      // one per 256 columns of a bias gradient
 
 #define LF_OPS_TRY(o, expr)                                     \
     do {                                                        \
@@ -78,9 +82,10 @@ cudaError_t lfk_unpack8(int dtype, int act, int tokens, int n, const unsigned ch
 cudaError_t lfk_act_backward(int dtype, int act, int tokens, int n, const void* dy, long long ld_dy,
                              const unsigned char* q, const unsigned char* s8, void* dz, long long ld_dz, int sm_count,
                              cudaStream_t s);
-// column sums of a 16-bit matrix in fp32, fixed order; partial: LF_OPS_FIXED_BYTES of scratch
-cudaError_t lfk_colsum16(int dtype, int tokens, int n, const void* x, long long ld, float* out, float* partial,
-                         int sm_count, cudaStream_t s, int* launches);
+// grad_w's bias gradient (where a.gb) and its input from 8 bits into x (where a.q), in one launch; partial:
+// LF_OPS_FIXED_BYTES of scratch, counters: LF_OPS_COUNTERS words that are zero between calls
+cudaError_t lfk_grad_w_prepare(const lf_linear_grad_w_args& a, long long ld_dz, void* x, float* partial, unsigned* counters, int sm_count,
+                               cudaStream_t s);
 
 // ---- matrix products -----------------------------------------------------------------------------
 // What a product is for: which operands are transposed and what its epilogue does.
@@ -104,4 +109,5 @@ int lf_product_tc_init(lf_ops* o);              // opts the kernels in, finds ma
 int lf_product_tc(lf_ops* o, const lf_product& p);
 // few tokens, forward only
 constexpr int LF_STREAM_MAX_TOKENS = 16;
-cudaError_t lfk_linear_stream(const lf_product& p, int sm_count, cudaStream_t s, int* splits);
+int lf_linear_stream_init();
+cudaError_t lfk_linear_stream(const lf_product& p, int sm_count, cudaStream_t s);

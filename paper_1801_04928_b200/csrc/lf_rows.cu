@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(TPR) k_rms_norm(const lf_rms_norm_args a)
                 for (int k = 0; k < 8; ++k) h[j][k] = 0.f;
             }
             if (a.q) {                       // all lanes of a warp take part: j * TPR + 32 w is uniform
-                const unsigned b = group_byte(h[j]);
+                const unsigned b = group_byte<8>(h[j]);
                 if (i < nv) {
                     *reinterpret_cast<uint2*>(a.q + (size_t)row * a.n + 8 * i) = quantize8(h[j], b);
                     if ((i & 3) == 0) a.s[(size_t)row * gpr + (i >> 2)] = (unsigned char)b;
@@ -272,19 +272,20 @@ __global__ void __launch_bounds__(1024) k_sum_rows(const float* partial, int row
     if ((threadIdx.x & 31) == 0 && blockIdx.x * 32 + g < n) out[blockIdx.x * 32 + g] = v;
 }
 
-// column sums of a 16-bit matrix: a block takes 256 columns (a warp all of them, eight per lane) and every
-// gridDim.y-th run of rows
+// Column sums of a 16-bit matrix: a block takes 256 columns (a warp all of them, eight per lane) and run `by` of n_by
+// runs of rows.  The block that finishes a column group last -- a counter per group says which one, and
+// goes back to zero -- adds the runs, in their order.
 template <typename T>
-__global__ void __launch_bounds__(256) k_colsum16(const T* x, long long ld, int tokens, int n, float* partial)
+__device__ __forceinline__ void colsum_block(const T* x, long long ld, int tokens, int n, float* partial, unsigned* counters, float* out,
+                                             int bx, int by, int n_by)
 {
     __shared__ float red[8][256];
-    const int c = blockIdx.x * 256 + (threadIdx.x & 31) * 8, w = threadIdx.x >> 5;
+    __shared__ unsigned last;
+    const int c = bx * 256 + (threadIdx.x & 31) * 8, w = threadIdx.x >> 5;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    lf_grid_wait();
-    lf_grid_release();
     if (c < n) {
-#pragma unroll 4
-        for (int r = blockIdx.y * 8 + w; r < tokens; r += gridDim.y * 8) {
+#pragma unroll 8
+        for (int r = by * 8 + w; r < tokens; r += n_by * 8) {
             vec8<T> xv;
             float f[8];
             xv.load(x + (size_t)r * ld + c);
@@ -296,120 +297,187 @@ __global__ void __launch_bounds__(256) k_colsum16(const T* x, long long ld, int 
 #pragma unroll
     for (int k = 0; k < 8; ++k) red[w][(threadIdx.x & 31) * 8 + k] = v[k];
     __syncthreads();
-    const int col = blockIdx.x * 256 + threadIdx.x;
-    if (col < n) {
-        float t = 0.f;
+    const int col = bx * 256 + threadIdx.x;
+    float t = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t += red[i][threadIdx.x];
-        partial[(size_t)blockIdx.y * n + col] = t;
+    for (int i = 0; i < 8; ++i) t += red[i][threadIdx.x];
+    if (n_by == 1) {
+        if (col < n) out[col] = t;
+        return;
+    }
+    if (col < n) partial[(size_t)by * n + col] = t;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const unsigned k = atomicAdd(&counters[bx], 1u);
+        last = k == (unsigned)(n_by - 1);
+        if (last) counters[bx] = 0u;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    if (col < n) {
+        t = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < n_by; ++i) t += __ldcg(partial + (size_t)i * n + col);
+        out[col] = t;
     }
 }
 
 // ---- 8-bit form -------------------------------------------------------------------------------------
-// Threads run along the row (blockIdx.x) and take every gridDim.y-th row, ROWS_AT_ONCE of them at a time, all loads
-// ahead of the first use.
+// Threads run along the row, W columns each (16 in 256-bit accesses where widths, strides and addresses allow it, else
+// 8), and take every n_by-th row, ROWS_AT_ONCE of them at a time, all loads ahead of the first use.
 constexpr int ROWS_AT_ONCE = 4;
-template <typename T>
+template <int W> struct bytes_of;                // W e4m3 numbers
+template <> struct bytes_of<16> { typedef uint4 type; };
+template <> struct bytes_of<8> { typedef uint2 type; };
+__device__ __forceinline__ void quantize(const float (&v)[8], unsigned byte, uint2& q) { q = quantize8(v, byte); }
+__device__ __forceinline__ void quantize(const float (&v)[16], unsigned byte, uint4& q)
+{
+    const float r = inv_scale(byte);
+    q = make_uint4(to_e4m3x4(v[0] * r, v[1] * r, v[2] * r, v[3] * r), to_e4m3x4(v[4] * r, v[5] * r, v[6] * r, v[7] * r),
+                   to_e4m3x4(v[8] * r, v[9] * r, v[10] * r, v[11] * r), to_e4m3x4(v[12] * r, v[13] * r, v[14] * r, v[15] * r));
+}
+__device__ __forceinline__ void dequantize(uint2 q, unsigned byte, float (&v)[8]) { dequantize8(q, byte, v); }
+__device__ __forceinline__ void dequantize(uint4 q, unsigned byte, float (&v)[16])
+{
+    const float s = scale(byte);
+    from_e4m3x4(q.x, s, v[0], v[1], v[2], v[3]);
+    from_e4m3x4(q.y, s, v[4], v[5], v[6], v[7]);
+    from_e4m3x4(q.z, s, v[8], v[9], v[10], v[11]);
+    from_e4m3x4(q.w, s, v[12], v[13], v[14], v[15]);
+}
+
+template <typename T, int W>
 __global__ void __launch_bounds__(256) k_pack8(const T* x, long long ld, int tokens, int n, unsigned char* q, unsigned char* s)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x, nv = n >> 3;
+    typedef typename bytes_of<W>::type Q;
+    const int i = blockIdx.x * 256 + threadIdx.x, nv = n / W;
     if ((i & ~31) >= nv) return;             // whole warps only: the group maximum is taken across lanes
     const size_t gpr = (size_t)((n + 31) / 32);
     lf_grid_wait();
     lf_grid_release();
     for (int row0 = blockIdx.y; row0 < tokens; row0 += ROWS_AT_ONCE * gridDim.y) {
-        vec8<T> v[ROWS_AT_ONCE];
+        typename piece_of<T, W>::type v[ROWS_AT_ONCE];
 #pragma unroll
         for (int u = 0; u < ROWS_AT_ONCE; ++u) {
             const int row = row0 + u * gridDim.y;
             v[u].zero();
-            if (i < nv && row < tokens) v[u].load(x + (size_t)row * ld + 8 * i);
+            if (i < nv && row < tokens) v[u].load(x + (size_t)row * ld + W * i);
         }
 #pragma unroll
         for (int u = 0; u < ROWS_AT_ONCE; ++u) {
             const int row = row0 + u * gridDim.y;
-            float f[8];
+            float f[W];
             v[u].get(f);
-            const unsigned b = group_byte(f);
+            const unsigned b = group_byte<W>(f);
             if (i < nv && row < tokens) {
-                *reinterpret_cast<uint2*>(q + (size_t)row * n + 8 * i) = quantize8(f, b);
-                if ((i & 3) == 0) s[(size_t)row * gpr + (i >> 2)] = (unsigned char)b;
+                Q qv;
+                quantize(f, b, qv);
+                *reinterpret_cast<Q*>(q + (size_t)row * n + W * i) = qv;
+                if ((i & (32 / W - 1)) == 0) s[(size_t)row * gpr + i / (32 / W)] = (unsigned char)b;
             }
         }
     }
 }
 
 // GRAD = false: x = sigma(value);  GRAD = true: x = dy * sigma'(value)
-template <typename T, bool GRAD, int KIND>
+template <typename T, bool GRAD, int KIND, int W>
 __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsigned char* s, const T* dy, long long ld_dy, int tokens, int n,
-                                            T* x, long long ld)
+                                            T* x, long long ld, int bx, int by, int n_by)
 {
+    typedef typename bytes_of<W>::type Q;
     constexpr bool FAST = sizeof(T) == 2;
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= (n >> 3)) return;
+    const int i = bx * 256 + threadIdx.x;
+    if (i >= n / W) return;
     const size_t gpr = (size_t)((n + 31) / 32);
-    for (int row0 = blockIdx.y; row0 < tokens; row0 += ROWS_AT_ONCE * gridDim.y) {
-        uint2 qv[ROWS_AT_ONCE];
+    for (int row0 = by; row0 < tokens; row0 += ROWS_AT_ONCE * n_by) {
+        Q qv[ROWS_AT_ONCE];
         unsigned sv[ROWS_AT_ONCE];
-        vec8<T> dv[ROWS_AT_ONCE];
+        typename piece_of<T, W>::type dv[ROWS_AT_ONCE];
 #pragma unroll
         for (int u = 0; u < ROWS_AT_ONCE; ++u) {
-            const int row = row0 + u * gridDim.y;
-            qv[u] = make_uint2(0, 0);
-            sv[u] = 0;
-            dv[u].zero();
+            const int row = row0 + u * n_by;
             if (row < tokens) {
-                qv[u] = *reinterpret_cast<const uint2*>(q + (size_t)row * n + 8 * i);
-                sv[u] = s[(size_t)row * gpr + (i >> 2)];
-                if (GRAD) dv[u].load(dy + (size_t)row * ld_dy + 8 * i);
+                qv[u] = *reinterpret_cast<const Q*>(q + (size_t)row * n + W * i);
+                sv[u] = s[(size_t)row * gpr + i / (32 / W)];
+                if (GRAD) dv[u].load(dy + (size_t)row * ld_dy + W * i);
             }
         }
 #pragma unroll
         for (int u = 0; u < ROWS_AT_ONCE; ++u) {
-            const int row = row0 + u * gridDim.y;
+            const int row = row0 + u * n_by;
             if (row >= tokens) break;
-            float v[8];
-            dequantize8(qv[u], sv[u], v);
-            vec8<T> o;
+            float v[W];
+            dequantize(qv[u], sv[u], v);
+            typename piece_of<T, W>::type o;
             if (GRAD) {
-                float d[8];
+                float d[W];
                 dv[u].get(d);
-                prime_all<FAST, 8, KIND>(d, v);
+                prime_all<FAST, W, KIND>(d, v);
                 o.set(d);
             } else {
-                act_all<FAST, 8, KIND>(v);
+                act_all<FAST, W, KIND>(v);
+                if (sv[u] >= overflow_byte(T())) {       // (no activation leaves the range its argument is in)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = clamp_keep_nan(v[k], max_finite(T()));
+                    for (int k = 0; k < W; ++k) v[k] = clamp_keep_nan(v[k], max_finite(T()));
+                }
                 o.set(v);
             }
-            o.store(x + (size_t)row * ld + 8 * i);
+            o.store(x + (size_t)row * ld + W * i);
         }
     }
 }
-template <typename T, bool GRAD>
+template <typename T, bool GRAD, int W>
+__device__ __forceinline__ void unpack_block(const unsigned char* q, const unsigned char* s, const T* dy, long long ld_dy, int tokens, int n,
+                                             int kind, T* x, long long ld, int bx, int by, int n_by)
+{
+    switch (kind) {
+        case LF_ACT_SIGMOID: unpack_rows<T, GRAD, LF_ACT_SIGMOID, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
+        case LF_ACT_TANH: unpack_rows<T, GRAD, LF_ACT_TANH, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
+        case LF_ACT_RELU: unpack_rows<T, GRAD, LF_ACT_RELU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
+        case LF_ACT_SILU: unpack_rows<T, GRAD, LF_ACT_SILU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
+        case LF_ACT_GELU: unpack_rows<T, GRAD, LF_ACT_GELU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
+        default: unpack_rows<T, GRAD, LF_ACT_NONE, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
+    }
+}
+template <typename T, bool GRAD, int W>
 __global__ void __launch_bounds__(256) k_unpack8(const unsigned char* q, const unsigned char* s, const T* dy,
                                                  long long ld_dy, int tokens, int n, int kind, T* x, long long ld)
 {
     lf_grid_wait();
     lf_grid_release();
-    switch (kind) {
-        case LF_ACT_SIGMOID: unpack_rows<T, GRAD, LF_ACT_SIGMOID>(q, s, dy, ld_dy, tokens, n, x, ld); break;
-        case LF_ACT_TANH: unpack_rows<T, GRAD, LF_ACT_TANH>(q, s, dy, ld_dy, tokens, n, x, ld); break;
-        case LF_ACT_RELU: unpack_rows<T, GRAD, LF_ACT_RELU>(q, s, dy, ld_dy, tokens, n, x, ld); break;
-        case LF_ACT_SILU: unpack_rows<T, GRAD, LF_ACT_SILU>(q, s, dy, ld_dy, tokens, n, x, ld); break;
-        case LF_ACT_GELU: unpack_rows<T, GRAD, LF_ACT_GELU>(q, s, dy, ld_dy, tokens, n, x, ld); break;
-        default: unpack_rows<T, GRAD, LF_ACT_NONE>(q, s, dy, ld_dy, tokens, n, x, ld); break;
+    unpack_block<T, GRAD, W>(q, s, dy, ld_dy, tokens, n, kind, x, ld, blockIdx.x, blockIdx.y, gridDim.y);
+}
+
+// What a weight gradient needs beside its product, in one launch: the column sums of dz (the first sum_x * sum_y
+// blocks) and the layer's input unpacked (the others).
+template <typename T, int W>
+__global__ void __launch_bounds__(256) k_grad_w_prepare(const T* dz, long long ld_dz, int tokens, int n_out, float* partial, unsigned* counters,
+                                                        float* gb, int sum_x, int sum_y, const unsigned char* q, const unsigned char* s, int n_in,
+                                                        int kind, T* x, int unpack_x, int unpack_y)
+{
+    lf_grid_wait();
+    lf_grid_release();
+    const int b = blockIdx.x, sums = sum_x * sum_y;
+    if (b < sums) {
+        colsum_block(dz, ld_dz, tokens, n_out, partial, counters, gb, b % sum_x, b / sum_x, sum_y);
+    } else {
+        const int u = b - sums;
+        unpack_block<T, false, W>(q, s, nullptr, 0, tokens, n_in, kind, x, n_in, u % unpack_x, u / unpack_x, unpack_y);
     }
 }
 
-dim3 row_grid(int tokens, int n, int sm_count)
+dim3 row_grid(int tokens, int n, int w, int sm_count)
 {
-    const int bx = ceil_div(n >> 3, 256);
+    const int bx = ceil_div(n / w, 256);
     int by = ceil_div((long long)sm_count * 16, bx);
     if (by > tokens) by = tokens;
     if (by > 65535) by = 65535;
     return dim3((unsigned)bx, (unsigned)by);
 }
+// whether 256-bit accesses fit a matrix of this width, row stride and address (8-bit rows: 128-bit ones)
+inline bool wide(int n, long long ld, const void* p) { return (n & 15) == 0 && (ld & 15) == 0 && (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 
 // Threads per row: four vectors per thread when there are rows enough to fill the device, otherwise
 // one, so that a few rows are read by as many threads as they have vectors.
@@ -497,20 +565,28 @@ cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* par
     return e;
 }
 
+template <typename T>
+static cudaError_t pack_of(int tokens, int n, const void* x, long long ld, unsigned char* q, unsigned char* s8, int sm_count, cudaStream_t s)
+{
+    if (wide(n, ld, x)) return lf_launch(k_pack8<T, 16>, row_grid(tokens, n, 16, sm_count), 256, 0, s, static_cast<const T*>(x), ld, tokens, n, q, s8);
+    return lf_launch(k_pack8<T, 8>, row_grid(tokens, n, 8, sm_count), 256, 0, s, static_cast<const T*>(x), ld, tokens, n, q, s8);
+}
 cudaError_t lfk_pack8(int dtype, int tokens, int n, const void* x, long long ld, unsigned char* q, unsigned char* s8,
                       int sm_count, cudaStream_t s)
 {
-    const dim3 g = row_grid(tokens, n, sm_count);
-    if (dtype == LF_F32) return lf_launch(k_pack8<float>, g, 256, 0, s, static_cast<const float*>(x), ld, tokens, n, q, s8);
-    if (dtype == LF_BF16) return lf_launch(k_pack8<__nv_bfloat16>, g, 256, 0, s, static_cast<const __nv_bfloat16*>(x), ld, tokens, n, q, s8);
-    return lf_launch(k_pack8<__half>, g, 256, 0, s, static_cast<const __half*>(x), ld, tokens, n, q, s8);
+    if (dtype == LF_F32) return pack_of<float>(tokens, n, x, ld, q, s8, sm_count, s);
+    if (dtype == LF_BF16) return pack_of<__nv_bfloat16>(tokens, n, x, ld, q, s8, sm_count, s);
+    return pack_of<__half>(tokens, n, x, ld, q, s8, sm_count, s);
 }
 
 template <typename T, bool GRAD>
 static cudaError_t unpack_of(int act, int tokens, int n, const void* dy, long long ld_dy, const unsigned char* q, const unsigned char* s8,
                              void* x, long long ld, int sm_count, cudaStream_t s)
 {
-    return lf_launch(k_unpack8<T, GRAD>, row_grid(tokens, n, sm_count), 256, 0, s, q, s8, static_cast<const T*>(dy), ld_dy, tokens, n, act,
+    if (wide(n, ld, x) && (!GRAD || wide(n, ld_dy, dy)))
+        return lf_launch(k_unpack8<T, GRAD, 16>, row_grid(tokens, n, 16, sm_count), 256, 0, s, q, s8, static_cast<const T*>(dy), ld_dy, tokens, n, act,
+                         static_cast<T*>(x), ld);
+    return lf_launch(k_unpack8<T, GRAD, 8>, row_grid(tokens, n, 8, sm_count), 256, 0, s, q, s8, static_cast<const T*>(dy), ld_dy, tokens, n, act,
                      static_cast<T*>(x), ld);
 }
 template <bool GRAD>
@@ -535,23 +611,26 @@ cudaError_t lfk_act_backward(int dtype, int act, int tokens, int n, const void* 
     return unpack_any<true>(dtype, act, tokens, n, dy, ld_dy, q, s8, dz, ld_dz, sm_count, s);
 }
 
-cudaError_t lfk_colsum16(int dtype, int tokens, int n, const void* x, long long ld, float* out, float* partial,
-                         int sm_count, cudaStream_t s, int* launches)
+cudaError_t lfk_grad_w_prepare(const lf_linear_grad_w_args& a, long long ld_dz, void* x, float* partial, unsigned* counters, int sm_count,
+                               cudaStream_t s)
 {
-    const int bx = ceil_div(n, 256);
-    long long by = ceil_div((long long)sm_count * 4, bx);
-    const long long most = (long long)(LF_OPS_FIXED_BYTES / sizeof(float)) / n, rows16 = ceil_div(tokens, 128);
-    if (by > most) by = most;
-    if (by > rows16) by = rows16;             // at least 16 rows per warp
-    if (by < 1) by = 1;
-    const dim3 g((unsigned)bx, (unsigned)by);
-    float* to = by == 1 ? out : partial;
-    cudaError_t e = dtype == LF_BF16 ? lf_launch(k_colsum16<__nv_bfloat16>, g, 256, 0, s, static_cast<const __nv_bfloat16*>(x), ld, tokens, n, to)
-                                     : lf_launch(k_colsum16<__half>, g, 256, 0, s, static_cast<const __half*>(x), ld, tokens, n, to);
-    *launches += 1;
-    if (e == cudaSuccess && by > 1) {
-        e = sum_rows(partial, (int)by, n, out, s);
-        *launches += 1;
+    int sum_x = 0, sum_y = 0;
+    dim3 u(0, 0);
+    if (a.gb) {
+        sum_x = ceil_div(a.n_out, 256);
+        long long by = ceil_div((long long)sm_count * 4, sum_x);
+        const long long most = (long long)(LF_OPS_FIXED_BYTES / sizeof(float)) / a.n_out, rows = ceil_div(a.tokens, 128);
+        if (by > most) by = most;
+        if (by > rows) by = rows;              // at least 16 rows per warp
+        sum_y = by < 1 ? 1 : (int)by;
     }
-    return e;
+    const bool w16 = wide(a.n_in, a.n_in, x);
+    if (a.q) u = row_grid(a.tokens, a.n_in, w16 ? 16 : 8, sm_count);
+    const dim3 grid((unsigned)(sum_x * sum_y) + u.x * u.y);
+    if (a.dtype == LF_BF16)
+        return lf_launch(w16 ? k_grad_w_prepare<__nv_bfloat16, 16> : k_grad_w_prepare<__nv_bfloat16, 8>, grid, 256, 0, s,
+                         static_cast<const __nv_bfloat16*>(a.dz), ld_dz, a.tokens, a.n_out, partial, counters, a.gb, sum_x, sum_y, a.q, a.s, a.n_in,
+                         a.act, static_cast<__nv_bfloat16*>(x), (int)u.x, (int)u.y);
+    return lf_launch(w16 ? k_grad_w_prepare<__half, 16> : k_grad_w_prepare<__half, 8>, grid, 256, 0, s, static_cast<const __half*>(a.dz), ld_dz,
+                     a.tokens, a.n_out, partial, counters, a.gb, sum_x, sum_y, a.q, a.s, a.n_in, a.act, static_cast<__half*>(x), (int)u.x, (int)u.y);
 }

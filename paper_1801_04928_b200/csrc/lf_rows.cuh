@@ -76,10 +76,74 @@ struct vec8<float> {
         reinterpret_cast<float4*>(p)[1] = b;
     }
 };
+// ---- sixteen consecutive elements in 256-bit accesses (32-byte aligned) -----------------------------
+__device__ __forceinline__ void ld256(const void* p, unsigned (&r)[8])
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
+}
+__device__ __forceinline__ void st256(void* p, const unsigned (&r)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+template <typename T>
+struct vec16 {
+    unsigned u[8];
+    __device__ __forceinline__ void load(const T* p) { ld256(p, u); }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = 0;
+    }
+    __device__ __forceinline__ void get(float (&v)[16]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = unpack2(u[i], T());
+            v[2 * i] = f.x; v[2 * i + 1] = f.y;
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[16])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = pack2(v[2 * i], v[2 * i + 1], T());
+    }
+    __device__ __forceinline__ void store(T* p) const { st256(p, u); }
+};
+template <>
+struct vec16<float> {
+    unsigned a[8], b[8];
+    __device__ __forceinline__ void load(const float* p) { ld256(p, a); ld256(p + 8, b); }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = b[i] = 0;
+    }
+    __device__ __forceinline__ void get(float (&v)[16]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { v[i] = __uint_as_float(a[i]); v[8 + i] = __uint_as_float(b[i]); }
+    }
+    __device__ __forceinline__ void set(const float (&v)[16])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { a[i] = __float_as_uint(v[i]); b[i] = __float_as_uint(v[8 + i]); }
+    }
+    __device__ __forceinline__ void store(float* p) const { st256(p, a); st256(p + 8, b); }
+};
+// a lane's piece of a row: W = 16 or 8 columns
+template <typename T, int W> struct piece_of { typedef vec16<T> type; };
+template <typename T> struct piece_of<T, 8> { typedef vec8<T> type; };
+
 // the largest finite number of a type (what lf_unpack8 saturates to)
 __device__ __forceinline__ float max_finite(float) { return 3.402823466e38f; }
 __device__ __forceinline__ float max_finite(__nv_bfloat16) { return 3.389531389e38f; }
 __device__ __forceinline__ float max_finite(__half) { return 65504.f; }
+// the smallest scale byte of a group whose values may lie beyond the type: 448 * 2^e > max_finite
+__device__ __forceinline__ unsigned overflow_byte(float) { return 127u + 120u; }
+__device__ __forceinline__ unsigned overflow_byte(__nv_bfloat16) { return 127u + 120u; }
+__device__ __forceinline__ unsigned overflow_byte(__half) { return 127u + 8u; }
 __device__ __forceinline__ float clamp_keep_nan(float v, float m)
 {
     return v > m ? m : (v < -m ? -m : v);
@@ -159,16 +223,19 @@ __device__ __forceinline__ float2 act_prime2(float2 z)
     const float2 zn = KIND == LF_ACT_GELU ? mul2(mul2(z, na), fma2(zz, f2(3.f * GELU_D), f2(GELU_C))) : mul2(z, na);
     return fma2(a, zn, a);
 }
-// run-time choice outside of the loop over NE elements
+// Over NE elements.  (Half of the exponentials as a polynomial on the multiply-add units, to relieve the
+// special-function unit, was 5 % slower: the issue slots are as scarce.)
 template <bool FAST, int NE, int KIND>
 __device__ __forceinline__ void act_all(float* v)
 {
 #pragma unroll
     for (int i = 0; i < NE; i += 2) {
-        const float2 r = act2<FAST, KIND>(make_float2(v[i], v[i + 1]));
+        const float2 z = make_float2(v[i], v[i + 1]);
+        const float2 r = act2<FAST, KIND>(z);
         v[i] = r.x; v[i + 1] = r.y;
     }
 }
+// ... with the choice of the activation at run time, outside of the loop
 template <bool FAST, int NE>
 __device__ __forceinline__ void act_n(float* v, int kind)
 {
@@ -187,7 +254,8 @@ __device__ __forceinline__ void prime_all(float* d, const float* z)
 {
 #pragma unroll
     for (int i = 0; i < NE; i += 2) {
-        const float2 r = mul2(make_float2(d[i], d[i + 1]), act_prime2<FAST, KIND>(make_float2(z[i], z[i + 1])));
+        const float2 zi = make_float2(z[i], z[i + 1]);
+        const float2 r = mul2(make_float2(d[i], d[i + 1]), act_prime2<FAST, KIND>(zi));
         d[i] = r.x; d[i + 1] = r.y;
     }
 }
@@ -239,14 +307,15 @@ __device__ __forceinline__ void from_e4m3x4(unsigned q, float s, float& a, float
     const float2 g0 = __fmul2_rn(f0, make_float2(s, s)), g1 = __fmul2_rn(f1, make_float2(s, s));
     a = g0.x; b = g0.y; c = g1.x; d = g1.y;
 }
-// eight columns held by one lane; the four lanes of a group are neighbours (lane & ~3)
-__device__ __forceinline__ unsigned group_byte(const float (&v)[8])
+// W columns held by one lane; the 32 / W lanes of a group are neighbours
+template <int W>
+__device__ __forceinline__ unsigned group_byte(const float (&v)[W])
 {
     unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    for (int i = 0; i < W; ++i) m = max(m, abs_bits(v[i]));
+#pragma unroll
+    for (int o = 1; o < 32 / W; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
     return scale_byte(m);
 }
 __device__ __forceinline__ uint2 quantize8(const float (&v)[8], unsigned byte)
