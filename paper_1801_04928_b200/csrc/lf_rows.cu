@@ -144,11 +144,11 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
     };
     lf_grid_wait();
     for (int d = 0; d < depth - 1; ++d) fetch(first + d * stride, d);
-    float dg[VPT][8];
+    float2 dg[VPT][4];                       // packed fp32 throughout: the row's arithmetic is what limits the copies' rate
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dg[j][k] = 0.f;
+        for (int k = 0; k < 4; ++k) dg[j][k] = f2(0.f);
     // every group of the block makes the same number of steps: the barrier is the block's
     const int steps = (a.tokens - blockIdx.x * GROUPS + stride - 1) / stride;
     int slot = 0;
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
         const bool live = row < a.tokens;
         vec8<T> hv[VPT], yv[VPT];
-        float ss = 0.f, su = 0.f;
+        float2 ss2 = f2(0.f), su2 = f2(0.f);
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int i = j * TPR + t;
@@ -179,11 +179,13 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
             hv[j].get(h);
             yv[j].get(y);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                ss = fmaf(h[k], h[k], ss);
-                su = fmaf(gn[k] * y[k], h[k], su);
+            for (int k = 0; k < 8; k += 2) {
+                const float2 hk = make_float2(h[k], h[k + 1]);
+                ss2 = fma2(hk, hk, ss2);
+                su2 = fma2(mul2(make_float2(gn[k], gn[k + 1]), make_float2(y[k], y[k + 1])), hk, su2);
             }
         }
+        float ss = ss2.x + ss2.y, su = su2.x + su2.y;
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
             ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
@@ -211,10 +213,12 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
             yv[j].get(y);
             if (a.dres) { o.load(reinterpret_cast<const T*>(piece(slot, 2, j))); o.get(d); }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                dg[j][k] = fmaf(y[k], h[k] * r, dg[j][k]);
-                const float v = r * (gn[k] * y[k] - h[k] * c);
-                d[k] = a.dres ? v + d[k] : v;
+            for (int k = 0; k < 8; k += 2) {
+                const float2 hk = make_float2(h[k], h[k + 1]), yk = make_float2(y[k], y[k + 1]);
+                dg[j][k / 2] = fma2(yk, mul2(hk, f2(r)), dg[j][k / 2]);
+                const float2 in = fma2(hk, f2(-c), mul2(make_float2(gn[k], gn[k + 1]), yk));       // u - h r mean(u h r)
+                const float2 v = a.dres ? fma2(in, f2(r), make_float2(d[k], d[k + 1])) : mul2(in, f2(r));
+                d[k] = v.x; d[k + 1] = v.y;
             }
             o.set(d);
             o.store(static_cast<T*>(a.dh) + (size_t)row * a.ld_dh + 8 * i);
@@ -226,28 +230,28 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
     if (partial) {
         if (GROUPS > 1) {
             // add the groups' sums in group order (the ring is free; it holds at least eight floats per thread and vector)
-            float* all = reinterpret_cast<float*>(ring);
+            float2* all = reinterpret_cast<float2*>(ring);
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < VPT; ++j)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) all[(size_t)(j * 8 + k) * THREADS + threadIdx.x] = dg[j][k];
+                for (int k = 0; k < 4; ++k) all[(size_t)(j * 4 + k) * THREADS + threadIdx.x] = dg[j][k];
             __syncthreads();
             if (g > 0) return;
 #pragma unroll
             for (int j = 0; j < VPT; ++j)
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int o = 1; o < GROUPS; ++o) dg[j][k] += all[(size_t)(j * 8 + k) * THREADS + o * TPR + t];
+                    for (int o = 1; o < GROUPS; ++o) dg[j][k] = add2(dg[j][k], all[(size_t)(j * 4 + k) * THREADS + o * TPR + t]);
         }
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int i = j * TPR + t;
             if (i < nv) {
-                vec8<float> o;
-                o.set(dg[j]);
-                o.store(partial + (size_t)blockIdx.x * a.n + 8 * i);
+                float4* to = reinterpret_cast<float4*>(partial + (size_t)blockIdx.x * a.n + 8 * i);
+                to[0] = make_float4(dg[j][0].x, dg[j][0].y, dg[j][1].x, dg[j][1].y);
+                to[1] = make_float4(dg[j][2].x, dg[j][2].y, dg[j][3].x, dg[j][3].y);
             }
         }
     }
@@ -327,7 +331,7 @@ __device__ __forceinline__ void colsum_block(const T* x, long long ld, int token
 // ---- 8-bit form -------------------------------------------------------------------------------------
 // Threads run along the row, W columns each (16 in 256-bit accesses where widths, strides and addresses allow it, else
 // 8), and take every n_by-th row, ROWS_AT_ONCE of them at a time, all loads ahead of the first use.
-constexpr int ROWS_AT_ONCE = 4;
+constexpr int ROWS_AT_ONCE = 4, ROWS_GRAD = 2;       // (two where a second matrix is read: registers)
 template <int W> struct bytes_of;                // W e4m3 numbers
 template <> struct bytes_of<16> { typedef uint4 type; };
 template <> struct bytes_of<8> { typedef uint2 type; };
@@ -388,15 +392,16 @@ __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsign
 {
     typedef typename bytes_of<W>::type Q;
     constexpr bool FAST = sizeof(T) == 2;
+    constexpr int ROWS = GRAD ? ROWS_GRAD : ROWS_AT_ONCE;
     const int i = bx * 256 + threadIdx.x;
     if (i >= n / W) return;
     const size_t gpr = (size_t)((n + 31) / 32);
-    for (int row0 = by; row0 < tokens; row0 += ROWS_AT_ONCE * n_by) {
-        Q qv[ROWS_AT_ONCE];
-        unsigned sv[ROWS_AT_ONCE];
-        typename piece_of<T, W>::type dv[ROWS_AT_ONCE];
+    for (int row0 = by; row0 < tokens; row0 += ROWS * n_by) {
+        Q qv[ROWS];
+        unsigned sv[ROWS];
+        typename piece_of<T, W>::type dv[ROWS];
 #pragma unroll
-        for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+        for (int u = 0; u < ROWS; ++u) {
             const int row = row0 + u * n_by;
             if (row < tokens) {
                 qv[u] = *reinterpret_cast<const Q*>(q + (size_t)row * n + W * i);
@@ -405,7 +410,7 @@ __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsign
             }
         }
 #pragma unroll
-        for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+        for (int u = 0; u < ROWS; ++u) {
             const int row = row0 + u * n_by;
             if (row >= tokens) break;
             float v[W];
