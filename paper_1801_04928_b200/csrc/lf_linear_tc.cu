@@ -32,7 +32,7 @@ constexpr int LT_BK = 64;
 constexpr int LT_BLOCK_BYTES = 128 * LT_BK * 2;          // 16 KiB: 128 rows (or columns) x 64 contraction steps
 constexpr int LT_STAGE_BYTES = 2 * LT_BLOCK_BYTES;
 constexpr int LT_STAGES = 6;
-constexpr int LT_THREADS = 320;                          // producer, issuer, eight epilogue warps
+constexpr int LS_THREADS = 512;                          // split tiles: producer, issuer, eight warps that read the accumulator; all finish
 constexpr int LT_CHUNK = 8;                              // K stages per accumulator of an fp32 result
 constexpr int LP_RING_BYTES = LT_STAGES * LT_STAGE_BYTES;   // pairs: six stages of two blocks, or four of three
 constexpr int LP_EPI_BYTES = 8 * 4096;                   // pairs: 32 rows x 128 bytes per epilogue warp
@@ -339,6 +339,8 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int chunk = PROMOTE ? LT_CHUNK : n_k;
 
     if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
         for (int i = 0; i < STAGES; ++i) {
             lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
             lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
@@ -574,7 +576,7 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // The epilogue warps go through their code once before the accumulator is complete, with nothing to load or store:
 // a launch this short meets its instructions and parameters cold, 2400 cycles otherwise spent at its end.
 template <int PROD, typename T, typename OUT, int SPLITS>
-__global__ void __launch_bounds__(LT_THREADS, 1)
+__global__ void __launch_bounds__(LS_THREADS, 1)
 k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const LtParams P)
 {
     constexpr bool A_MN = PROD == LF_PROD_GRAD_W, B_MN = PROD != LF_PROD_FORWARD;
@@ -601,6 +603,8 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         lt_load<B_MN, false>(dst + LT_BLOCK_BYTES, &map_b, bar, tn * 128, (ks0 + ks) * LT_BK);
     };
     if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
         for (int i = 0; i < LS_STAGES; ++i) {
             lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
             lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
@@ -668,12 +672,12 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
     }
     __syncwarp();
-    constexpr int R = 128 / SPLITS, RP = SPLITS >= 4 ? 16 / SPLITS : 4;     // rows of this CTA at most, and rows a warp takes at a time
+    constexpr int R = 128 / SPLITS, RP = SPLITS == 8 ? 1 : 2;     // rows of this CTA at most, and rows a warp takes at a time
     const int share = min(R, (P.M - tm * 128 + SPLITS - 1) / SPLITS);     // rows of this CTA: its part of those that exist
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
         if (pass == 1) {
-            if (warp >= 2) {
+            if (warp >= 2 && warp < 10) {
                 const int quad = warp & 3, half = (warp - 2) >> 2;
                 float acc[64];
 #pragma unroll
@@ -703,12 +707,11 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if (SPLITS > 1) lfptx::cluster_sync_all();
             else __syncthreads();
         }
-        if (warp < 2) continue;
         // This CTA's rows.  A lane takes four columns, a warp a row (its loads from another CTA are whole lines),
         // RP rows at a time.
-        const int rows = pass == 0 ? 8 * RP : share;
+        const int rows = pass == 0 ? 16 * RP : share;
 #pragma unroll 1
-        for (int r0 = (warp - 2) * RP; r0 < rows; r0 += 8 * RP) {
+        for (int r0 = warp * RP; r0 < rows; r0 += 16 * RP) {
             const int col = tn * 128 + lane * 4;
             float4 x[RP][SPLITS];
             const float* at = tile + min(part * share + r0, 128 - RP) * LS_LD + lane * 4;   // (rows past the share are not used)
@@ -973,7 +976,7 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
         P.tiles_m = (p.M + 127) / 128; P.tiles_n = (p.N + 127) / 128;
         P.idesc = idesc | (128u >> 3) << 17 | (128u >> 4) << 24;
         P.stages_per_split = (n_k + c.splits - 1) / c.splits;
-        lt_cluster_config(&cfg, at, P.tiles_m * P.tiles_n * c.splits, LT_THREADS, c.splits, LS_SMEM, o->stream);
+        lt_cluster_config(&cfg, at, P.tiles_m * P.tiles_n * c.splits, LS_THREADS, c.splits, LS_SMEM, o->stream);
         LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_split(kernel, c.splits), map_a, map_b, P));
         o->stats.form = LF_FORM_SPLIT;
         o->stats.splits = c.splits;
