@@ -673,6 +673,7 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
     __syncwarp();
     constexpr int R = 128 / SPLITS, RP = SPLITS == 8 ? 1 : 2;     // rows of this CTA at most, and rows a warp takes at a time
+    bool arrived = false;
     const int share = min(R, (P.M - tm * 128 + SPLITS - 1) / SPLITS);     // rows of this CTA: its part of those that exist
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
@@ -721,6 +722,10 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 #pragma unroll
                 for (int h = 0; h < RP; ++h)
                     x[h][p] = SPLITS > 1 ? lt_ld_cluster_f4(from + h * (LS_LD * 4)) : *reinterpret_cast<const float4*>(at + h * LS_LD);
+            }
+            if (SPLITS > 1 && pass == 1 && r0 + 16 * RP >= rows) {             // this warp reads nothing more of the other parts
+                asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+                arrived = true;
             }
 #pragma unroll
             for (int h = 0; h < RP; ++h) {
@@ -775,7 +780,10 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
     }
     // no CTA may leave while another one reads its tile
-    if (SPLITS > 1) lfptx::cluster_sync_all();
+    if (SPLITS > 1) {
+        if (!arrived) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
     if (warp == 1) {
         __syncwarp();
         lfptx::tc_fence_after();
