@@ -32,7 +32,7 @@ LF_COST_QUADRATIC, LF_COST_CROSS_ENTROPY = 0, 1
 LF_TC_TILING_AUTO, LF_TC_TILING_ONE_SM, LF_TC_TILING_TWO_SM = 0, 1, 2
 LF_F32, LF_BF16, LF_F16 = 0, 1, 2
 LF_ACT_NONE, LF_ACT_SILU, LF_ACT_GELU = 3, 4, 5
-LF_FORM_STREAM, LF_FORM_SPLIT, LF_FORM_PAIRS = 1, 2, 3
+LF_FORM_STREAM, LF_FORM_SPLIT, LF_FORM_PAIRS, LF_FORM_SPLIT_PAIRS = 1, 2, 3, 4
 LF_DELTA_MATH_AUTO, LF_DELTA_MATH_FP32, LF_DELTA_MATH_3XTF32, LF_DELTA_MATH_TF32_BF16 = 0, 1, 2, 3
 
 EXPORTS = ("lf_create", "lf_create_widths", "lf_set_stream", "lf_set_option", "lf_forward", "lf_backward",

@@ -43,6 +43,10 @@ constexpr int LS_LD = 132;                               // split tiles: padded 
 constexpr size_t LP_SMEM = (size_t)LP_RING_BYTES + LP_EPI_BYTES + 1024 + 512;
 constexpr int LS_STAGES = 4;
 constexpr int LS_TILE_BYTES = 128 * LS_LD * 4;
+constexpr int LPS_SPLITS = 2;
+constexpr int LD_PS = 260;                               // split pairs: padded row of a CTA's 128 x 256 fp32 tile
+constexpr size_t LPS_SMEM = (size_t)LT_STAGES * LT_STAGE_BYTES + 1024 + 512;
+static_assert(128 * LD_PS * 4 <= LT_STAGES * LT_STAGE_BYTES, "the fp32 tile overlays the operand ring");
 constexpr size_t LS_SMEM = (size_t)LS_STAGES * LT_STAGE_BYTES + LS_TILE_BYTES + 1024 + 512;
 
 struct LtParams {
@@ -569,6 +573,53 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // ================================================================================================
 // Split tiles: one CTA per 128 x 128 tile and part of the contraction, a cluster per tile
 // ================================================================================================
+// Finishes four columns of a row, which a warp's lanes hold side by side (eight neighbours make an 8-bit scale group);
+// `in`: the elements exist.
+template <int PROD, typename T, typename OUT>
+__device__ __forceinline__ void ls_finish4(float (&v)[4], const LtParams& P, int row, int col, bool in)
+{
+                    uint2 radd = make_uint2(0, 0);
+                    unsigned zq = 0, zs = 0;
+                    if (in && PROD != LF_PROD_GRAD_W && P.add)
+                        radd = *reinterpret_cast<const uint2*>(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col);
+                    if (in && PROD == LF_PROD_GRAD_X && P.q) {
+                        zq = *reinterpret_cast<const unsigned*>(P.q + (size_t)row * P.N + col);
+                        zs = P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)];
+                    }
+                    if (PROD == LF_PROD_FORWARD) {
+                        if (in && P.bias) {
+                            const float4 b = *reinterpret_cast<const float4*>(P.bias + col);
+                            v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
+                        }
+                        if (P.q) {
+                            unsigned m = in ? max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3]))) : 0u;
+    #pragma unroll
+                            for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                            const unsigned b = scale_byte(m);
+                            const float is = inv_scale(b);
+                            if (in) {
+                                *reinterpret_cast<unsigned*>(P.q + (size_t)row * P.N + col) = to_e4m3x4(v[0] * is, v[1] * is, v[2] * is, v[3] * is);
+                                if ((col & 31) == 0) P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)] = (unsigned char)b;
+                            }
+                        }
+                        act_n<true, 4>(v, P.act);
+                    }
+                    if (PROD == LF_PROD_GRAD_X && P.q) {
+                        float z[4];
+                        from_e4m3x4(zq, scale(zs), z[0], z[1], z[2], z[3]);
+                        prime_n<true, 4>(v, z, P.act);
+                    }
+                    if (PROD != LF_PROD_GRAD_W && P.add) {
+                        const float2 f0 = unpack2(radd.x, T()), f1 = unpack2(radd.y, T());
+                        v[0] += f0.x; v[1] += f0.y; v[2] += f1.x; v[3] += f1.y;
+                    }
+                    if (in) {
+                        OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
+                        if (sizeof(OUT) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
+                        else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                    }
+}
+
 // The parts of a tile meet in distributed shared memory: every part leaves its fp32 tile beside its operand ring,
 // and after a cluster barrier each CTA adds its share of the rows, R = 128 / splits, from all parts,
 // every load issued before the first addition.  (One part after the other cost 7000 to 11000 cycles,
@@ -731,51 +782,12 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             for (int h = 0; h < RP; ++h) {
                 const int row = tm * 128 + part * share + r0 + h;
                 const bool in = pass == 1 && r0 + h < share && row < P.M && col < P.N && !sh->abort_flag;
-                uint2 radd = make_uint2(0, 0);
-                unsigned zq = 0, zs = 0;
-                if (in && PROD != LF_PROD_GRAD_W && P.add)
-                    radd = *reinterpret_cast<const uint2*>(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col);
-                if (in && PROD == LF_PROD_GRAD_X && P.q) {
-                    zq = *reinterpret_cast<const unsigned*>(P.q + (size_t)row * P.N + col);
-                    zs = P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)];
-                }
                 float v[4] = {x[h][0].x, x[h][0].y, x[h][0].z, x[h][0].w};
 #pragma unroll
                 for (int p = 1; p < SPLITS; ++p) {                  // parts in order: the sum does not depend on timing
                     v[0] += x[h][p].x; v[1] += x[h][p].y; v[2] += x[h][p].z; v[3] += x[h][p].w;
                 }
-                if (PROD == LF_PROD_FORWARD) {
-                    if (in && P.bias) {
-                        const float4 b = *reinterpret_cast<const float4*>(P.bias + col);
-                        v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
-                    }
-                    if (P.q) {
-                        unsigned m = in ? max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3]))) : 0u;
-#pragma unroll
-                        for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                        const unsigned b = scale_byte(m);
-                        const float is = inv_scale(b);
-                        if (in) {
-                            *reinterpret_cast<unsigned*>(P.q + (size_t)row * P.N + col) = to_e4m3x4(v[0] * is, v[1] * is, v[2] * is, v[3] * is);
-                            if ((col & 31) == 0) P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)] = (unsigned char)b;
-                        }
-                    }
-                    act_n<true, 4>(v, P.act);
-                }
-                if (PROD == LF_PROD_GRAD_X && P.q) {
-                    float z[4];
-                    from_e4m3x4(zq, scale(zs), z[0], z[1], z[2], z[3]);
-                    prime_n<true, 4>(v, z, P.act);
-                }
-                if (PROD != LF_PROD_GRAD_W && P.add) {
-                    const float2 f0 = unpack2(radd.x, T()), f1 = unpack2(radd.y, T());
-                    v[0] += f0.x; v[1] += f0.y; v[2] += f1.x; v[3] += f1.y;
-                }
-                if (in) {
-                    OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
-                    if (sizeof(OUT) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
-                    else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
-                }
+                ls_finish4<PROD, T, OUT>(v, P, row, col, in);
             }
         }
     }
@@ -788,6 +800,181 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         __syncwarp();
         lfptx::tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
+    }
+}
+
+// ================================================================================================
+// Split pairs: 256 x 256 tiles of CTA pairs, the contraction split over the two pairs of a cluster
+// ================================================================================================
+// For outputs with too few 256 x 256 tiles to fill the device and too many bytes of operands for 128 x 128 ones: a
+// stage costs a pair 568 cycles for four times the products of a 128 x 128 tile's 560.  The parts meet as
+// above (the fp32 tile of a CTA, 128 x 256, overlays its operand ring here: every product that reads
+// the ring is done when the accumulator is).  16-bit results only.  512 x 4096 x 4096: 19 us, against 27 with either
+// of the other forms.  (Four pairs to a cluster leave 60 multiprocessors idle -- 15 such clusters are resident -- and were
+// never ahead.)
+template <int PROD, typename T>
+__global__ void __launch_bounds__(LS_THREADS, 1)
+k_product_pair_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const LtParams P)
+{
+    constexpr bool A_MN = PROD == LF_PROD_GRAD_W, B_MN = PROD != LF_PROD_FORWARD;
+    constexpr int SPLITS = LPS_SPLITS, CTAS = 2 * SPLITS;
+    extern __shared__ unsigned char lt_smem_raw[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lt_smem_raw) + 1023u) & ~(uintptr_t)1023u);
+    float* tile = reinterpret_cast<float*>(ring);            // [128][LD_PS], once every product is done
+    LtShared* sh = reinterpret_cast<LtShared*>(ring + (size_t)LT_STAGES * LT_STAGE_BYTES);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int member = (int)lfptx::cluster_ctarank(), part = member >> 1, rank = member & 1;
+    const unsigned leader = (unsigned)(member & ~1);
+    const int t = (int)(blockIdx.x / (unsigned)CTAS);
+    const int tn = t / P.tiles_m, tm = t - tn * P.tiles_m;
+    const int n_k_all = (P.K + LT_BK - 1) / LT_BK;
+    const int ks0 = part * P.stages_per_split;
+    const int n_k = max(0, min(P.stages_per_split, n_k_all - ks0));
+    const int row_base = tm * 256 + rank * 128;
+
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+        for (int i = 0; i < LT_STAGES; ++i) {
+            lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
+            lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
+        }
+        lfptx::mbar_init(lfptx::smem_u32(&sh->acc_full[0]), 1);
+        sh->abort_flag = 0u;
+        sh->prog_it = 0u;
+        lfptx::mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(lfptx::smem_u32(&sh->tmem_base)), "r"(256u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    lfptx::tc_fence_before();
+    __syncthreads();
+    lfptx::cluster_sync_all();       // the pair's barriers exist before anything can arrive on them
+    lfptx::tc_fence_after();
+    const unsigned tmem_base = sh->tmem_base;
+    lf_grid_wait();
+    lf_grid_release();
+
+    const unsigned short both = (unsigned short)(3u << leader);
+    auto commit = [&](unsigned bar) {
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"(both) : "memory");
+    };
+    if (warp == 0) {
+        if (lane == 0) {
+            int ks = 0;
+            for (; ks < n_k; ++ks) {
+                const unsigned st = (unsigned)ks % LT_STAGES, use = (unsigned)ks / LT_STAGES;
+                if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->empty[st]), (use - 1) & 1u, P, sh)) break;
+                const unsigned lbar = lfptx::smem_u32(&sh->full[st]);
+                if (P.withhold && blockIdx.x == 1 && ks == 0) continue;                   // test hook
+                if (rank == 0) lfptx::mbar_arrive_expect_tx(lbar, 2u * LT_STAGE_BYTES);
+                const unsigned bar = lfptx::map_to_cta(lbar, leader);
+                const unsigned dst = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
+                lt_load<A_MN, true>(dst, &map_a, bar, row_base, (ks0 + ks) * LT_BK);
+                lt_load<B_MN, true>(dst + LT_BLOCK_BYTES, &map_b, bar, tn * 256 + rank * 128, (ks0 + ks) * LT_BK);
+            }
+            sh->prog_it = (unsigned)ks;
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            bool ok = true;
+            for (int ks = 0; ks < n_k; ++ks) {
+                const unsigned st = (unsigned)ks % LT_STAGES, use = (unsigned)ks / LT_STAGES;
+                if (!lt_wait(lfptx::smem_u32(&sh->full[st]), use & 1u, P, sh)) { ok = false; break; }
+                lfptx::tc_fence_after();
+                const unsigned a_addr = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
+                const unsigned b_addr = a_addr + LT_BLOCK_BYTES;
+#pragma unroll
+                for (int kk = 0; kk < LT_BK / 16; ++kk)
+                    lt_mma<true>(tmem_base, lt_desc<A_MN>(a_addr + lt_step<A_MN>(kk)), lt_desc<B_MN>(b_addr + lt_step<B_MN>(kk)), P.idesc,
+                                 (ks > 0 || kk > 0) ? 1u : 0u);
+                commit(lfptx::smem_u32(&sh->empty[st]));
+            }
+            if (ok && n_k > 0) commit(lfptx::smem_u32(&sh->acc_full[0]));
+        }
+    }
+    __syncwarp();
+    // this CTA's rows: its part of those that exist
+    constexpr int R = 128 / SPLITS, RP = 2;
+    const int share = min(R, max(0, (P.M - row_base + SPLITS - 1) / SPLITS));
+    bool gave_up = false;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        if (pass == 1) {
+            if (warp >= 2 && warp < 10) {
+                const int quad = warp & 3, half = (warp - 2) >> 2;
+                const bool ok = n_k > 0 && lt_wait(lfptx::smem_u32(&sh->acc_full[0]), 0u, P, sh);
+                lfptx::tc_fence_after();
+                float* to = tile + (quad * 32 + lane) * LD_PS + half * 128;
+#pragma unroll 1
+                for (int j = 0; j < 4 && (ok || n_k == 0); ++j) {
+                    unsigned r[32];
+                    if (ok) lfptx::tmem_ld32(tmem_base + ((unsigned)(quad * 32) << 16) + half * 128u + j * 32, r);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<float4*>(to + j * 32 + 4 * i) =
+                            ok ? make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]), __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]))
+                               : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
+            lfptx::tc_fence_before();
+            lfptx::cluster_sync_all();
+            gave_up = sh->abort_flag != 0u;
+        }
+        const int units = pass == 0 ? 16 * RP : share * 2;      // row, half of the columns
+#pragma unroll 1
+        for (int u0 = warp * RP; u0 < units; u0 += 16 * RP) {
+            float4 x[RP][SPLITS];
+#pragma unroll
+            for (int h = 0; h < RP; ++h) {
+                const int row = min(part * share + ((u0 + h) >> 1), 127);      // (units past the share are not used)
+                const unsigned at = lfptx::smem_u32(tile + row * LD_PS + ((u0 + h) & 1) * 128 + lane * 4);
+#pragma unroll
+                for (int p = 0; p < SPLITS; ++p)
+                    x[h][p] = lt_ld_cluster_f4(pass == 1 ? lfptx::map_to_cta(at, (unsigned)(2 * p + rank)) : at);
+            }
+#pragma unroll
+            for (int h = 0; h < RP; ++h) {
+                const int u = u0 + h, row = row_base + part * share + (u >> 1), col = tn * 256 + (u & 1) * 128 + lane * 4;
+                float v[4] = {x[h][0].x, x[h][0].y, x[h][0].z, x[h][0].w};
+#pragma unroll
+                for (int p = 1; p < SPLITS; ++p) {                             // parts in order: the sum does not depend on timing
+                    v[0] += x[h][p].x; v[1] += x[h][p].y; v[2] += x[h][p].z; v[3] += x[h][p].w;
+                }
+                ls_finish4<PROD, T, T>(v, P, row, col, pass == 1 && u < units && row < P.M && col < P.N && !gave_up);
+            }
+        }
+    }
+    // No CTA may leave (or free tensor memory) while another one reads its tile or the pair's products can reach it.
+    lfptx::tc_fence_before();
+    __syncthreads();
+    lfptx::cluster_sync_all();
+    if (threadIdx.x == 0 && rank == 0) {
+        // given up: as in the persistent form, the loads of both CTAs that are on their way are waited for, with a limit
+        const bool any = sh->abort_flag != 0u || lt_ld_cluster_u32(lfptx::map_to_cta(lfptx::smem_u32((const void*)&sh->abort_flag), leader + 1)) != 0u;
+        if (any) {
+            const unsigned it_l = sh->prog_it, it_p = lt_ld_cluster_u32(lfptx::map_to_cta(lfptx::smem_u32(&sh->prog_it), leader + 1));
+            const unsigned hi = max(it_l, it_p), lo = min(it_l, it_p);
+            for (unsigned j = lo; j < hi; ++j) {
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
+                if (j >= it_l) lfptx::mbar_arrive_expect_tx(bar, LT_STAGE_BYTES);
+                else lt_complete_tx(bar, LT_STAGE_BYTES);
+            }
+            const unsigned long long t0 = lfptx::globaltimer_ns();
+            for (unsigned j = hi > LT_STAGES ? hi - LT_STAGES : 0; j < hi; ++j) {
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
+                while (!lfptx::mbar_try_wait(bar, (j / LT_STAGES) & 1u) && lfptx::globaltimer_ns() - t0 < 50000000ull) { }
+            }
+        }
+    }
+    lfptx::cluster_sync_all();
+    if (warp == 1) {
+        lfptx::tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
     }
 }
 
@@ -853,6 +1040,18 @@ lt_kernel lt_pick_pair(int i, int tile)
         default: return lt_pair_of<LF_PROD_GRAD_W, __half, float>(tile);
     }
 }
+lt_kernel lt_pick_pair_split(int i)
+{
+    switch (i) {
+        case 0: return k_product_pair_split<LF_PROD_FORWARD, __nv_bfloat16>;
+        case 1: return k_product_pair_split<LF_PROD_FORWARD, __half>;
+        case 2: return k_product_pair_split<LF_PROD_GRAD_X, __nv_bfloat16>;
+        case 3: return k_product_pair_split<LF_PROD_GRAD_X, __half>;
+        case 4: return k_product_pair_split<LF_PROD_GRAD_W, __nv_bfloat16>;
+        case 5: return k_product_pair_split<LF_PROD_GRAD_W, __half>;
+        default: return nullptr;
+    }
+}
 lt_kernel lt_pick_split(int i, int splits)
 {
     switch (i) {
@@ -889,20 +1088,25 @@ void lt_cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int gri
 int lf_product_tc_init(lf_ops* o)
 {
     if (!lt_encode()) return LF_ECUDA;
-    o->max_pairs = 0;
+    o->max_pairs = o->max_pair_splits = -1;
     for (int i = 0; i < LT_KERNELS; ++i) {
         for (int splits = 1; splits <= 8; splits *= 2)
             if (cudaFuncSetAttribute(lt_pick_split(i, splits), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LS_SMEM) != cudaSuccess) return LF_ECUDA;
-        for (int tile = 0; tile < LT_TILES; ++tile) {
-            const lt_kernel f = lt_pick_pair(i, tile);
-            if (!f) continue;
-            if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LP_SMEM) != cudaSuccess) return LF_ECUDA;
+        auto resident = [&](lt_kernel f, int threads, int cluster, size_t smem, int* least) {
+            if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute at[2];
-            lt_cluster_config(&cfg, at, 32, LP_THREADS, 2, LP_SMEM, nullptr);
+            lt_cluster_config(&cfg, at, 32, threads, cluster, smem, nullptr);
             int n = 0;
-            if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return LF_ECUDA;
-            if ((i == 0 && tile == 0) || n < o->max_pairs) o->max_pairs = n;
+            if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return false;
+            if (*least < 0 || n < *least) *least = n;
+            return true;
+        };
+        if (const lt_kernel f = lt_pick_pair_split(i))
+            if (!resident(f, LS_THREADS, 2 * LPS_SPLITS, LPS_SMEM, &o->max_pair_splits)) return LF_ECUDA;
+        for (int tile = 0; tile < LT_TILES; ++tile) {
+            const lt_kernel f = lt_pick_pair(i, tile);
+            if (f && !resident(f, LP_THREADS, 2, LP_SMEM, &o->max_pairs)) return LF_ECUDA;
         }
     }
     return LF_OK;
@@ -910,7 +1114,7 @@ int lf_product_tc_init(lf_ops* o)
 
 namespace {
 
-struct lt_choice { int splits, tile; };      // splits = 0: CTA pairs
+struct lt_choice { int splits, tile; };      // splits = 0: CTA pairs on `tile`; < 0: split pairs; else split tiles
 
 // The form with the least estimated time, in SM cycles; constants measured on B200 (widths 512 .. 16384, 17 .. 8192
 // tokens).  A 64-deep stage costs a 256 x 256 pair tile 568 cycles, a 512 x 256 one 1024 and a 128 x 128 tile 560
@@ -930,6 +1134,10 @@ lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
         const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
         const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
         offer({splits, 0}, waves(m128 * n128 * splits, at_once) * (part * 560.0 + meet + 6500.0));
+    }
+    if (o->max_pair_splits > 0 && n_k >= LPS_SPLITS && p.out_dtype != LF_F32) {
+        const double part = (double)((n_k + LPS_SPLITS - 1) / LPS_SPLITS), meet = 2000.0 + 65536.0 * rows / 14.0;
+        offer({-LPS_SPLITS, 0}, waves(m256 * n256, o->max_pair_splits) * (part * 568.0 + meet + 9000.0));
     }
     if (o->max_pairs > 0) {
         offer({0, LT_256x256}, waves(m256 * n256, o->max_pairs) * (n_k * 568.0 + 600.0) + 10000.0);
@@ -970,7 +1178,15 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
 
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute at[2];
-    if (c.splits == 0) {
+    if (c.splits < 0) {
+        P.tiles_m = (p.M + 255) / 256; P.tiles_n = (p.N + 255) / 256;
+        P.idesc = idesc | (256u >> 3) << 17 | (256u >> 4) << 24;
+        P.stages_per_split = (n_k + LPS_SPLITS - 1) / LPS_SPLITS;
+        lt_cluster_config(&cfg, at, P.tiles_m * P.tiles_n * 2 * LPS_SPLITS, LS_THREADS, 2 * LPS_SPLITS, LPS_SMEM, o->stream);
+        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_pair_split(kernel), map_a, map_b, P));
+        o->stats.form = LF_FORM_SPLIT_PAIRS;
+        o->stats.splits = LPS_SPLITS;
+    } else if (c.splits == 0) {
         const int bm = c.tile == LT_512x256 ? 512 : 256;
         P.tiles_m = (p.M + bm - 1) / bm; P.tiles_n = (p.N + 255) / 256;
         P.idesc = idesc | (256u >> 3) << 17 | (256u >> 4) << 24;

@@ -11,6 +11,7 @@ struct lf_ops {
     int device;
     int sm_count;
     int max_pairs;              // CTA pairs of the 256 x 256 tile kernels that are resident at once (0: none)
+    int max_pair_splits;        // resident clusters of the split pair kernels
     cudaStream_t stream;
     unsigned char* ws;          // workspace: fixed part first, then the unpacked layer input
     size_t ws_bytes;

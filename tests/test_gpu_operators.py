@@ -126,6 +126,12 @@ def test_linear_pairs(ops, M, K, N, dtype, act):
     _linear(ops, M, K, N, dtype, act, form=lf.LF_FORM_PAIRS)
 
 
+@pytest.mark.parametrize("M,K,N,dtype,act", [(512, 4096, 3976, BF16, R.GELU), (400, 4104, 4096, F16, R.NONE), (1900, 4096, 1000, BF16, R.SIGMOID),
+                                             (2048, 8200, 1024, F16, R.RELU)])
+def test_linear_split_pairs(ops, M, K, N, dtype, act):
+    _linear(ops, M, K, N, dtype, act, form=lf.LF_FORM_SPLIT_PAIRS)
+
+
 @pytest.mark.parametrize("M,K,N", [(3, 264, 72), (130, 264, 200), (2050, 136, 1400)])
 @pytest.mark.parametrize("bias,residual,ckpt,ld", [(False, False, False, 0), (True, False, True, 8), (False, True, False, 24), (True, True, True, 40)])
 def test_linear_options_and_strides(ops, M, K, N, bias, residual, ckpt, ld):
@@ -236,6 +242,12 @@ def test_backward_pairs(ops, M, K, N, dtype, act, gw):
 @pytest.mark.parametrize("ld", [0, 24])
 def test_backward_from_sixteen_bits(ops, M, K, N, dtype, gw, ld):
     _backward(ops, M, K, N, dtype, R.NONE, gw, eight=False, add=True, ld_extra=ld)
+
+
+@pytest.mark.parametrize("M,K,N,dtype,act,gw,forms", [
+    (500, 4000, 4096, BF16, R.GELU, BF16, (lf.LF_FORM_SPLIT_PAIRS, None)), (4096, 2048, 1024, F16, R.SILU, F16, (None, lf.LF_FORM_SPLIT_PAIRS))])
+def test_backward_split_pairs(ops, M, K, N, dtype, act, gw, forms):
+    _backward(ops, M, K, N, dtype, act, gw, forms=forms)
 
 
 def test_weight_gradient_over_many_tokens_keeps_fp32(ops):
@@ -570,7 +582,7 @@ def test_work_goes_to_the_stream_that_was_set():
         o.set_stream(None)
 
 
-@pytest.mark.parametrize("M,K,N", [(200, 1024, 264), (2049, 512, 1288)])
+@pytest.mark.parametrize("M,K,N", [(200, 1024, 264), (2049, 512, 1288), (4096, 512, 4096), (512, 4096, 4096)])
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(M, K, N):
     g = _gen(14)
     x, w = _rand(g, M, K, dtype=BF16), _rand(g, N, K, std=0.05, dtype=BF16)
