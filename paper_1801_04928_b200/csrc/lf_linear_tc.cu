@@ -1118,8 +1118,9 @@ struct lt_choice { int splits, tile; };      // splits = 0: CTA pairs on `tile`;
 
 // The form with the least estimated time, in SM cycles; constants measured on B200 (widths 512 .. 16384, 17 .. 8192
 // tokens).  A 64-deep stage costs a 256 x 256 pair tile 568 cycles, a 512 x 256 one 1024 and a 128 x 128 tile 560
-// (an instruction takes as long for 128 columns as for 256); switching tiles 600, 5000 and, where the
-// parts of a split tile meet, 1500 and the bytes from the other parts at 14 a cycle.
+// (an instruction takes as long for 128 columns as for 256); switching tiles costs 600 or 5000 and, where the
+// parts of a split tile meet, 1500 and the bytes from the other parts at 14 a cycle; the rest is the launch, the first
+// loads and the last epilogue.
 lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
 {
     auto waves = [](long long units, int at_once) { return (double)((units + at_once - 1) / at_once); };
@@ -1133,15 +1134,15 @@ lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
         const double part = (double)((n_k + splits - 1) / splits);
         const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
         const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
-        offer({splits, 0}, waves(m128 * n128 * splits, at_once) * (part * 560.0 + meet + 6500.0));
+        offer({splits, 0}, waves(m128 * n128 * splits, at_once) * (part * 560.0 + meet + 6300.0 + 3200.0 / splits));
     }
     if (o->max_pair_splits > 0 && n_k >= LPS_SPLITS && p.out_dtype != LF_F32) {
         const double part = (double)((n_k + LPS_SPLITS - 1) / LPS_SPLITS), meet = 2000.0 + 65536.0 * rows / 14.0;
-        offer({-LPS_SPLITS, 0}, waves(m256 * n256, o->max_pair_splits) * (part * 568.0 + meet + 9000.0));
+        offer({-LPS_SPLITS, 0}, waves(m256 * n256, o->max_pair_splits) * (part * 568.0 + meet + 11500.0));
     }
     if (o->max_pairs > 0) {
-        offer({0, LT_256x256}, waves(m256 * n256, o->max_pairs) * (n_k * 568.0 + 600.0) + 10000.0);
-        if (p.out_dtype != LF_F32) offer({0, LT_512x256}, waves(m512 * n256, o->max_pairs) * (n_k * 1024.0 + 5000.0) + 10000.0);
+        offer({0, LT_256x256}, waves(m256 * n256, o->max_pairs) * (n_k * 568.0 + 600.0) + 14000.0);
+        if (p.out_dtype != LF_F32) offer({0, LT_512x256}, waves(m512 * n256, o->max_pairs) * (n_k * 1024.0 + 5000.0) + 14000.0);
     }
     return best;
 }

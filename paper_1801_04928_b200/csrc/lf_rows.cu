@@ -330,7 +330,8 @@ __device__ __forceinline__ void colsum_block(const T* x, long long ld, int token
 
 // ---- 8-bit form -------------------------------------------------------------------------------------
 // Threads run along the row, W columns each (16 in 256-bit accesses where widths, strides and addresses allow it, else
-// 8), and take every n_by-th row, ROWS_AT_ONCE of them at a time, all loads ahead of the first use.
+// 8); a block has 256 / lanes rows side by side, lanes = 2^lanes_log2 >= the row's pieces (at most 256: wider rows take
+// several blocks), and walks down the matrix, ROWS_AT_ONCE rows at a time, all loads ahead of the first use.
 constexpr int ROWS_AT_ONCE = 4, ROWS_GRAD = 2;       // (two where a second matrix is read: registers)
 template <int W> struct bytes_of;                // W e4m3 numbers
 template <> struct bytes_of<16> { typedef uint4 type; };
@@ -353,25 +354,28 @@ __device__ __forceinline__ void dequantize(uint4 q, unsigned byte, float (&v)[16
 }
 
 template <typename T, int W>
-__global__ void __launch_bounds__(256) k_pack8(const T* x, long long ld, int tokens, int n, unsigned char* q, unsigned char* s)
+__global__ void __launch_bounds__(256) k_pack8(const T* x, long long ld, int tokens, int n, unsigned char* q, unsigned char* s, int lanes_log2)
 {
     typedef typename bytes_of<W>::type Q;
-    const int i = blockIdx.x * 256 + threadIdx.x, nv = n / W;
-    if ((i & ~31) >= nv) return;             // whole warps only: the group maximum is taken across lanes
+    const int i = blockIdx.x * 256 + (threadIdx.x & ((1 << lanes_log2) - 1)), nv = n / W;
+    const int first = blockIdx.y * (256 >> lanes_log2) + (threadIdx.x >> lanes_log2), stride = gridDim.y * (256 >> lanes_log2);
+    const int steps = (tokens - (int)blockIdx.y * (256 >> lanes_log2) + ROWS_AT_ONCE * stride - 1) / (ROWS_AT_ONCE * stride);   // the block's: the group
+                                                                                                             // maximum is taken across lanes
     const size_t gpr = (size_t)((n + 31) / 32);
     lf_grid_wait();
     lf_grid_release();
-    for (int row0 = blockIdx.y; row0 < tokens; row0 += ROWS_AT_ONCE * gridDim.y) {
+    for (int step = 0; step < steps; ++step) {
+        const int row0 = first + step * ROWS_AT_ONCE * stride;
         typename piece_of<T, W>::type v[ROWS_AT_ONCE];
 #pragma unroll
         for (int u = 0; u < ROWS_AT_ONCE; ++u) {
-            const int row = row0 + u * gridDim.y;
+            const int row = row0 + u * stride;
             v[u].zero();
             if (i < nv && row < tokens) v[u].load(x + (size_t)row * ld + W * i);
         }
 #pragma unroll
         for (int u = 0; u < ROWS_AT_ONCE; ++u) {
-            const int row = row0 + u * gridDim.y;
+            const int row = row0 + u * stride;
             float f[W];
             v[u].get(f);
             const unsigned b = group_byte<W>(f);
@@ -388,21 +392,22 @@ __global__ void __launch_bounds__(256) k_pack8(const T* x, long long ld, int tok
 // GRAD = false: x = sigma(value);  GRAD = true: x = dy * sigma'(value)
 template <typename T, bool GRAD, int KIND, int W>
 __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsigned char* s, const T* dy, long long ld_dy, int tokens, int n,
-                                            T* x, long long ld, int bx, int by, int n_by)
+                                            T* x, long long ld, int bx, int by, int n_by, int lanes_log2)
 {
     typedef typename bytes_of<W>::type Q;
     constexpr bool FAST = sizeof(T) == 2;
     constexpr int ROWS = GRAD ? ROWS_GRAD : ROWS_AT_ONCE;
-    const int i = bx * 256 + threadIdx.x;
+    const int i = bx * 256 + (threadIdx.x & ((1 << lanes_log2) - 1));
     if (i >= n / W) return;
+    const int first = by * (256 >> lanes_log2) + (threadIdx.x >> lanes_log2), stride = n_by * (256 >> lanes_log2);
     const size_t gpr = (size_t)((n + 31) / 32);
-    for (int row0 = by; row0 < tokens; row0 += ROWS * n_by) {
+    for (int row0 = first; row0 < tokens; row0 += ROWS * stride) {
         Q qv[ROWS];
         unsigned sv[ROWS];
         typename piece_of<T, W>::type dv[ROWS];
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-            const int row = row0 + u * n_by;
+            const int row = row0 + u * stride;
             if (row < tokens) {
                 qv[u] = *reinterpret_cast<const Q*>(q + (size_t)row * n + W * i);
                 sv[u] = s[(size_t)row * gpr + i / (32 / W)];
@@ -411,7 +416,7 @@ __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsign
         }
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-            const int row = row0 + u * n_by;
+            const int row = row0 + u * stride;
             if (row >= tokens) break;
             float v[W];
             dequantize(qv[u], sv[u], v);
@@ -435,24 +440,24 @@ __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsign
 }
 template <typename T, bool GRAD, int W>
 __device__ __forceinline__ void unpack_block(const unsigned char* q, const unsigned char* s, const T* dy, long long ld_dy, int tokens, int n,
-                                             int kind, T* x, long long ld, int bx, int by, int n_by)
+                                             int kind, T* x, long long ld, int bx, int by, int n_by, int lanes_log2)
 {
     switch (kind) {
-        case LF_ACT_SIGMOID: unpack_rows<T, GRAD, LF_ACT_SIGMOID, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
-        case LF_ACT_TANH: unpack_rows<T, GRAD, LF_ACT_TANH, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
-        case LF_ACT_RELU: unpack_rows<T, GRAD, LF_ACT_RELU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
-        case LF_ACT_SILU: unpack_rows<T, GRAD, LF_ACT_SILU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
-        case LF_ACT_GELU: unpack_rows<T, GRAD, LF_ACT_GELU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
-        default: unpack_rows<T, GRAD, LF_ACT_NONE, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by); break;
+        case LF_ACT_SIGMOID: unpack_rows<T, GRAD, LF_ACT_SIGMOID, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by, lanes_log2); break;
+        case LF_ACT_TANH: unpack_rows<T, GRAD, LF_ACT_TANH, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by, lanes_log2); break;
+        case LF_ACT_RELU: unpack_rows<T, GRAD, LF_ACT_RELU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by, lanes_log2); break;
+        case LF_ACT_SILU: unpack_rows<T, GRAD, LF_ACT_SILU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by, lanes_log2); break;
+        case LF_ACT_GELU: unpack_rows<T, GRAD, LF_ACT_GELU, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by, lanes_log2); break;
+        default: unpack_rows<T, GRAD, LF_ACT_NONE, W>(q, s, dy, ld_dy, tokens, n, x, ld, bx, by, n_by, lanes_log2); break;
     }
 }
 template <typename T, bool GRAD, int W>
 __global__ void __launch_bounds__(256) k_unpack8(const unsigned char* q, const unsigned char* s, const T* dy,
-                                                 long long ld_dy, int tokens, int n, int kind, T* x, long long ld)
+                                                 long long ld_dy, int tokens, int n, int kind, T* x, long long ld, int lanes_log2)
 {
     lf_grid_wait();
     lf_grid_release();
-    unpack_block<T, GRAD, W>(q, s, dy, ld_dy, tokens, n, kind, x, ld, blockIdx.x, blockIdx.y, gridDim.y);
+    unpack_block<T, GRAD, W>(q, s, dy, ld_dy, tokens, n, kind, x, ld, blockIdx.x, blockIdx.y, gridDim.y, lanes_log2);
 }
 
 // What a weight gradient needs beside its product, in one launch: the column sums of dz (the first sum_x * sum_y
@@ -460,7 +465,7 @@ __global__ void __launch_bounds__(256) k_unpack8(const unsigned char* q, const u
 template <typename T, int W>
 __global__ void __launch_bounds__(256) k_grad_w_prepare(const T* dz, long long ld_dz, int tokens, int n_out, float* partial, unsigned* counters,
                                                         float* gb, int sum_x, int sum_y, const unsigned char* q, const unsigned char* s, int n_in,
-                                                        int kind, T* x, int unpack_x, int unpack_y)
+                                                        int kind, T* x, int unpack_x, int unpack_y, int lanes_log2)
 {
     lf_grid_wait();
     lf_grid_release();
@@ -469,15 +474,20 @@ __global__ void __launch_bounds__(256) k_grad_w_prepare(const T* dz, long long l
         colsum_block(dz, ld_dz, tokens, n_out, partial, counters, gb, b % sum_x, b / sum_x, sum_y);
     } else {
         const int u = b - sums;
-        unpack_block<T, false, W>(q, s, nullptr, 0, tokens, n_in, kind, x, n_in, u % unpack_x, u / unpack_x, unpack_y);
+        unpack_block<T, false, W>(q, s, nullptr, 0, tokens, n_in, kind, x, n_in, u % unpack_x, u / unpack_x, unpack_y, lanes_log2);
     }
 }
 
-dim3 row_grid(int tokens, int n, int w, int sm_count)
+// grid of the row kernels for pieces of w columns, and how many threads share a row
+dim3 row_grid(int tokens, int n, int w, int sm_count, int* lanes_log2)
 {
-    const int bx = ceil_div(n / w, 256);
+    const int pieces = (n + w - 1) / w;
+    int log2 = 2;                              // (a scale group's lanes at least)
+    while (log2 < 8 && (1 << log2) < pieces) ++log2;
+    *lanes_log2 = log2;
+    const int bx = ceil_div(pieces, 256), rows = ceil_div(tokens, 256 >> log2);
     int by = ceil_div((long long)sm_count * 16, bx);
-    if (by > tokens) by = tokens;
+    if (by > rows) by = rows;
     if (by > 65535) by = 65535;
     return dim3((unsigned)bx, (unsigned)by);
 }
@@ -573,8 +583,10 @@ cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* par
 template <typename T>
 static cudaError_t pack_of(int tokens, int n, const void* x, long long ld, unsigned char* q, unsigned char* s8, int sm_count, cudaStream_t s)
 {
-    if (wide(n, ld, x)) return lf_launch(k_pack8<T, 16>, row_grid(tokens, n, 16, sm_count), 256, 0, s, static_cast<const T*>(x), ld, tokens, n, q, s8);
-    return lf_launch(k_pack8<T, 8>, row_grid(tokens, n, 8, sm_count), 256, 0, s, static_cast<const T*>(x), ld, tokens, n, q, s8);
+    int lanes;
+    const int w = wide(n, ld, x) ? 16 : 8;
+    const dim3 grid = row_grid(tokens, n, w, sm_count, &lanes);
+    return lf_launch(w == 16 ? k_pack8<T, 16> : k_pack8<T, 8>, grid, 256, 0, s, static_cast<const T*>(x), ld, tokens, n, q, s8, lanes);
 }
 cudaError_t lfk_pack8(int dtype, int tokens, int n, const void* x, long long ld, unsigned char* q, unsigned char* s8,
                       int sm_count, cudaStream_t s)
@@ -588,11 +600,11 @@ template <typename T, bool GRAD>
 static cudaError_t unpack_of(int act, int tokens, int n, const void* dy, long long ld_dy, const unsigned char* q, const unsigned char* s8,
                              void* x, long long ld, int sm_count, cudaStream_t s)
 {
-    if (wide(n, ld, x) && (!GRAD || wide(n, ld_dy, dy)))
-        return lf_launch(k_unpack8<T, GRAD, 16>, row_grid(tokens, n, 16, sm_count), 256, 0, s, q, s8, static_cast<const T*>(dy), ld_dy, tokens, n, act,
-                         static_cast<T*>(x), ld);
-    return lf_launch(k_unpack8<T, GRAD, 8>, row_grid(tokens, n, 8, sm_count), 256, 0, s, q, s8, static_cast<const T*>(dy), ld_dy, tokens, n, act,
-                     static_cast<T*>(x), ld);
+    int lanes;
+    const int w = wide(n, ld, x) && (!GRAD || wide(n, ld_dy, dy)) ? 16 : 8;
+    const dim3 grid = row_grid(tokens, n, w, sm_count, &lanes);
+    return lf_launch(w == 16 ? k_unpack8<T, GRAD, 16> : k_unpack8<T, GRAD, 8>, grid, 256, 0, s, q, s8, static_cast<const T*>(dy), ld_dy, tokens, n,
+                     act, static_cast<T*>(x), ld, lanes);
 }
 template <bool GRAD>
 static cudaError_t unpack_any(int dtype, int act, int tokens, int n, const void* dy, long long ld_dy, const unsigned char* q,
@@ -630,12 +642,13 @@ cudaError_t lfk_grad_w_prepare(const lf_linear_grad_w_args& a, long long ld_dz, 
         sum_y = by < 1 ? 1 : (int)by;
     }
     const bool w16 = wide(a.n_in, a.n_in, x);
-    if (a.q) u = row_grid(a.tokens, a.n_in, w16 ? 16 : 8, sm_count);
+    int lanes = 8;
+    if (a.q) u = row_grid(a.tokens, a.n_in, w16 ? 16 : 8, sm_count, &lanes);
     const dim3 grid((unsigned)(sum_x * sum_y) + u.x * u.y);
     if (a.dtype == LF_BF16)
         return lf_launch(w16 ? k_grad_w_prepare<__nv_bfloat16, 16> : k_grad_w_prepare<__nv_bfloat16, 8>, grid, 256, 0, s,
                          static_cast<const __nv_bfloat16*>(a.dz), ld_dz, a.tokens, a.n_out, partial, counters, a.gb, sum_x, sum_y, a.q, a.s, a.n_in,
-                         a.act, static_cast<__nv_bfloat16*>(x), (int)u.x, (int)u.y);
+                         a.act, static_cast<__nv_bfloat16*>(x), (int)u.x, (int)u.y, lanes);
     return lf_launch(w16 ? k_grad_w_prepare<__half, 16> : k_grad_w_prepare<__half, 8>, grid, 256, 0, s, static_cast<const __half*>(a.dz), ld_dz,
-                     a.tokens, a.n_out, partial, counters, a.gb, sum_x, sum_y, a.q, a.s, a.n_in, a.act, static_cast<__half*>(x), (int)u.x, (int)u.y);
+                     a.tokens, a.n_out, partial, counters, a.gb, sum_x, sum_y, a.q, a.s, a.n_in, a.act, static_cast<__half*>(x), (int)u.x, (int)u.y, lanes);
 }

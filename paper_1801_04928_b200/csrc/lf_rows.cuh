@@ -190,16 +190,18 @@ __device__ __forceinline__ float2 sigmoid_of(float2 z, float2 zz, bool cubic)
     return make_float2(1.0f / (1.0f + expf(-t.x)), 1.0f / (1.0f + expf(-t.y)));
 }
 // tanh z = 1 - 2 / (1 + e^{2 z}); below 1/16, where that cancels, the Taylor polynomial (next term 17/315 z^7: 3e-9 relative)
-__device__ __forceinline__ float tanh_fast(float z)
+__device__ __forceinline__ float2 tanh_fast(float2 z)
 {
-    const float t = fmaf(-2.f, rcp(1.f + ex2(2.f * LOG2E * z)), 1.f), zz = z * z;
-    return fabsf(z) < 0.0625f ? z * fmaf(zz, fmaf(zz, 2.f / 15.f, -1.f / 3.f), 1.f) : t;
+    const float2 zz = mul2(z, z), r = logistic2(mul2(z, f2(2.f * LOG2E)));
+    const float2 t = fma2(r, f2(-2.f), f2(1.f));
+    const float2 p = fma2(mul2(z, zz), fma2(zz, f2(2.f / 15.f), f2(-1.f / 3.f)), z);
+    return make_float2(fabsf(z.x) < 0.0625f ? p.x : t.x, fabsf(z.y) < 0.0625f ? p.y : t.y);
 }
 template <bool FAST, int KIND>
 __device__ __forceinline__ float2 act2(float2 z)
 {
     if (KIND == LF_ACT_SIGMOID) return sigmoid_of<FAST>(z, z, false);
-    if (KIND == LF_ACT_TANH) return FAST ? make_float2(tanh_fast(z.x), tanh_fast(z.y)) : make_float2(tanhf(z.x), tanhf(z.y));
+    if (KIND == LF_ACT_TANH) return FAST ? tanh_fast(z) : make_float2(tanhf(z.x), tanhf(z.y));
     if (KIND == LF_ACT_RELU) return make_float2(z.x < 0.f ? 0.f : z.x, z.y < 0.f ? 0.f : z.y);     // NaN stays
     if (KIND == LF_ACT_SILU) return mul2(z, sigmoid_of<FAST>(z, z, false));
     if (KIND == LF_ACT_GELU) return mul2(z, sigmoid_of<FAST>(z, mul2(z, z), true));
