@@ -573,51 +573,160 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // ================================================================================================
 // Split tiles: one CTA per 128 x 128 tile and part of the contraction, a cluster per tile
 // ================================================================================================
-// Finishes four columns of a row, which a warp's lanes hold side by side (eight neighbours make an 8-bit scale group);
-// `in`: the elements exist.
-template <int PROD, typename T, typename OUT>
-__device__ __forceinline__ void ls_finish4(float (&v)[4], const LtParams& P, int row, int col, bool in)
+// What is left to do for a CTA's share of a tile's rows: add the parts, bias, 8 bits, activation, residual, store.  A
+// piece is 128 columns of a row, half a warp's: a lane has columns 4 i .. and 64 + 4 i .., so that every
+// access is a whole line, also to another CTA's tile, and eight neighbours hold an 8-bit scale group.  With eight
+// parts a CTA has 16 rows, one for each warp: then a piece is a whole warp's (NK = 1: columns 4 i alone).
+struct ls_share {
+    const float* tile;         // [row][ld] fp32, the share's first row
+    int ld;
+    int row0, rows;            // first row of the share in the matrix, number of rows
+    int col0;                  // first column of the tile
+    int peer0, peer_step;      // CTA of the cluster that holds part p: peer0 + p * peer_step
+    int live;                  // 0: a dry run, nothing is loaded or stored
+    int leave;                 // arrive at the cluster's barrier as soon as the last part has been read
+};
+struct ls_operands {           // what a piece reads of the layer's matrices, fetched a piece ahead
+    unsigned q[2], s[2];
+    uint2 add[2];
+};
+template <int PROD, typename T, int NK>
+__device__ __forceinline__ void ls_fetch(ls_operands& o, const LtParams& P, const ls_share& e, int row, int col)
 {
-                    uint2 radd = make_uint2(0, 0);
-                    unsigned zq = 0, zs = 0;
-                    if (in && PROD != LF_PROD_GRAD_W && P.add)
-                        radd = *reinterpret_cast<const uint2*>(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col);
-                    if (in && PROD == LF_PROD_GRAD_X && P.q) {
-                        zq = *reinterpret_cast<const unsigned*>(P.q + (size_t)row * P.N + col);
-                        zs = P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)];
-                    }
-                    if (PROD == LF_PROD_FORWARD) {
-                        if (in && P.bias) {
-                            const float4 b = *reinterpret_cast<const float4*>(P.bias + col);
-                            v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
-                        }
-                        if (P.q) {
-                            unsigned m = in ? max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3]))) : 0u;
-    #pragma unroll
-                            for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                            const unsigned b = scale_byte(m);
-                            const float is = inv_scale(b);
-                            if (in) {
-                                *reinterpret_cast<unsigned*>(P.q + (size_t)row * P.N + col) = to_e4m3x4(v[0] * is, v[1] * is, v[2] * is, v[3] * is);
-                                if ((col & 31) == 0) P.s[(size_t)row * ((P.N + 31) / 32) + (col >> 5)] = (unsigned char)b;
-                            }
-                        }
-                        act_n<true, 4>(v, P.act);
-                    }
-                    if (PROD == LF_PROD_GRAD_X && P.q) {
-                        float z[4];
-                        from_e4m3x4(zq, scale(zs), z[0], z[1], z[2], z[3]);
-                        prime_n<true, 4>(v, z, P.act);
-                    }
-                    if (PROD != LF_PROD_GRAD_W && P.add) {
-                        const float2 f0 = unpack2(radd.x, T()), f1 = unpack2(radd.y, T());
-                        v[0] += f0.x; v[1] += f0.y; v[2] += f1.x; v[3] += f1.y;
-                    }
-                    if (in) {
-                        OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
-                        if (sizeof(OUT) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
-                        else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
-                    }
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+        const int c = col + 64 * k;
+        o.q[k] = o.s[k] = 0;
+        o.add[k] = make_uint2(0, 0);
+        if (PROD == LF_PROD_GRAD_W || !e.live || row >= e.row0 + e.rows || row >= P.M || c >= P.N) continue;
+        if (PROD == LF_PROD_GRAD_X && P.q) {
+            o.q[k] = *reinterpret_cast<const unsigned*>(P.q + (size_t)row * P.N + c);
+            o.s[k] = P.s[(size_t)row * ((P.N + 31) / 32) + (c >> 5)];
+        }
+        if (P.add) o.add[k] = *reinterpret_cast<const uint2*>(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + c);
+    }
+}
+// HALVES: pieces per row.  One copy per activation: the choice stands outside of the loop.
+template <int PROD, typename T, typename OUT, int SPLITS, int HALVES, int KIND>
+__device__ __forceinline__ void ls_rows(const LtParams& P, const ls_share& e, ls_operands now)
+{
+    constexpr int NK = SPLITS == 8 ? 1 : 2, SIDE = NK;         // column groups of a lane, pieces a warp has side by side
+    static_assert(HALVES == 1 || NK == 2, "two halves of a row are two pieces");
+    const int lane = threadIdx.x & 31, i = NK == 1 ? lane : lane & 15;
+    const int u0 = (threadIdx.x >> 5) * SIDE + (NK == 1 ? 0 : lane >> 4);
+    const int half = HALVES == 2 ? (lane >> 4) : 0;
+    const int col = e.col0 + half * 128 + 4 * i;
+    const bool in0 = col < P.N, in1 = NK == 2 && col + 64 < P.N;
+    float2 bias[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
+    if (PROD == LF_PROD_FORWARD && P.bias) {
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+            if (k ? in1 : in0) {
+                const float4 b = *reinterpret_cast<const float4*>(P.bias + col + 64 * k);
+                bias[2 * k] = make_float2(b.x, b.y);
+                bias[2 * k + 1] = make_float2(b.z, b.w);
+            }
+    }
+    const size_t groups = (size_t)((P.N + 31) / 32);
+    const int pieces = e.rows * HALVES, steps = (pieces + 16 * SIDE - 1) / (16 * SIDE);      // 16 warps
+    const bool reads = P.add != nullptr || (PROD == LF_PROD_GRAD_X && KIND != LF_ACT_NONE);
+    if (SPLITS > 1 && e.leave && steps == 0) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+#pragma unroll 1
+    for (int st = 0; st < steps; ++st) {
+        const int u = u0 + st * 16 * SIDE, r = HALVES == 2 ? u >> 1 : u;
+        const float* at = e.tile + r * e.ld + half * 128 + 4 * i;
+        float4 x[SPLITS][2];
+#pragma unroll
+        for (int p = 0; p < SPLITS; ++p) {
+            x[p][0] = x[p][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (u >= pieces) continue;                         // (reading along cost S = 8 twice the traffic between CTAs)
+            if (SPLITS == 1) {
+                x[p][0] = *reinterpret_cast<const float4*>(at);
+                if (NK == 2) x[p][1] = *reinterpret_cast<const float4*>(at + 64);
+            } else {
+                const unsigned from = lfptx::map_to_cta(lfptx::smem_u32(at), (unsigned)(e.peer0 + p * e.peer_step));
+                x[p][0] = lt_ld_cluster_f4(from);
+                if (NK == 2) x[p][1] = lt_ld_cluster_f4(from + 256);
+            }
+        }
+        if (SPLITS > 1 && e.leave && st + 1 == steps) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        const ls_operands mine = now;
+        const int row = e.row0 + r, row_next = e.row0 + (HALVES == 2 ? (u + 32) >> 1 : u + 16 * SIDE);
+        if (reads && st + 1 < steps) ls_fetch<PROD, T, NK>(now, P, e, row_next, col);
+        float v[4 * NK];
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {                         // parts in order: the sum does not depend on timing
+            float2 lo = make_float2(x[0][k].x, x[0][k].y), hi = make_float2(x[0][k].z, x[0][k].w);
+#pragma unroll
+            for (int p = 1; p < SPLITS; ++p) {
+                lo = add2(lo, make_float2(x[p][k].x, x[p][k].y));
+                hi = add2(hi, make_float2(x[p][k].z, x[p][k].w));
+            }
+            if (PROD == LF_PROD_FORWARD) { lo = add2(lo, bias[2 * k]); hi = add2(hi, bias[2 * k + 1]); }
+            v[4 * k] = lo.x; v[4 * k + 1] = lo.y; v[4 * k + 2] = hi.x; v[4 * k + 3] = hi.y;
+        }
+        const bool have = e.live && u < pieces && row < P.M;
+        if (PROD == LF_PROD_FORWARD && P.q) {
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const bool in = have && (k ? in1 : in0);
+                const float* w = v + 4 * k;
+                unsigned m = in ? max(max(abs_bits(w[0]), abs_bits(w[1])), max(abs_bits(w[2]), abs_bits(w[3]))) : 0u;
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                const unsigned b = scale_byte(m);
+                const float is = inv_scale(b);
+                if (in) {
+                    const int c = col + 64 * k;
+                    *reinterpret_cast<unsigned*>(P.q + (size_t)row * P.N + c) = to_e4m3x4(w[0] * is, w[1] * is, w[2] * is, w[3] * is);
+                    if ((c & 31) == 0) P.s[(size_t)row * groups + (c >> 5)] = (unsigned char)b;
+                }
+            }
+        }
+        if (PROD == LF_PROD_FORWARD) act_all<true, 4 * NK, KIND>(v);
+        if (PROD == LF_PROD_GRAD_X && KIND != LF_ACT_NONE) {
+            float z[4 * NK];
+#pragma unroll
+            for (int k = 0; k < NK; ++k)
+                from_e4m3x4(mine.q[k], scale(mine.s[k]), z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]);
+            prime_all<true, 4 * NK, KIND>(v, z);
+        }
+        OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            float* w = v + 4 * k;
+            if (PROD != LF_PROD_GRAD_W && P.add) {
+                const float2 f0 = unpack2(mine.add[k].x, T()), f1 = unpack2(mine.add[k].y, T());
+                w[0] += f0.x; w[1] += f0.y; w[2] += f1.x; w[3] += f1.y;
+            }
+            if (have && (k ? in1 : in0)) {
+                if (sizeof(OUT) == 2) *reinterpret_cast<uint2*>(to + 64 * k) = make_uint2(pack2(w[0], w[1], T()), pack2(w[2], w[3], T()));
+                else *reinterpret_cast<float4*>(to + 64 * k) = make_float4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+}
+template <int PROD, typename T, typename OUT, int SPLITS, int HALVES>
+__device__ __forceinline__ void ls_finish(const LtParams& P, const ls_share& e, const ls_operands& first)
+{
+    switch (PROD == LF_PROD_GRAD_W || (PROD == LF_PROD_GRAD_X && !P.q) ? LF_ACT_NONE : P.act) {
+        case LF_ACT_SIGMOID: ls_rows<PROD, T, OUT, SPLITS, HALVES, LF_ACT_SIGMOID>(P, e, first); break;
+        case LF_ACT_TANH: ls_rows<PROD, T, OUT, SPLITS, HALVES, LF_ACT_TANH>(P, e, first); break;
+        case LF_ACT_RELU: ls_rows<PROD, T, OUT, SPLITS, HALVES, LF_ACT_RELU>(P, e, first); break;
+        case LF_ACT_SILU: ls_rows<PROD, T, OUT, SPLITS, HALVES, LF_ACT_SILU>(P, e, first); break;
+        case LF_ACT_GELU: ls_rows<PROD, T, OUT, SPLITS, HALVES, LF_ACT_GELU>(P, e, first); break;
+        default: ls_rows<PROD, T, OUT, SPLITS, HALVES, LF_ACT_NONE>(P, e, first); break;
+    }
+}
+// the first piece's operands, on their way while the accumulator is waited for
+template <int PROD, typename T, int SPLITS, int HALVES>
+__device__ __forceinline__ ls_operands ls_first(const LtParams& P, const ls_share& e)
+{
+    constexpr int NK = SPLITS == 8 ? 1 : 2;
+    const int lane = threadIdx.x & 31, u = (threadIdx.x >> 5) * NK + (NK == 1 ? 0 : lane >> 4);
+    ls_operands o;
+    ls_fetch<PROD, T, NK>(o, P, e, e.row0 + (HALVES == 2 ? u >> 1 : u), e.col0 + (HALVES == 2 ? (lane >> 4) * 128 : 0) + 4 * (NK == 1 ? lane : lane & 15));
+    return o;
 }
 
 // The parts of a tile meet in distributed shared memory: every part leaves its fp32 tile beside its operand ring,
@@ -723,9 +832,11 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
     }
     __syncwarp();
-    constexpr int R = 128 / SPLITS, RP = SPLITS == 8 ? 1 : 2;     // rows of this CTA at most, and rows a warp takes at a time
-    bool arrived = false;
-    const int share = min(R, (P.M - tm * 128 + SPLITS - 1) / SPLITS);     // rows of this CTA: its part of those that exist
+    // this CTA's rows: its part of those that exist
+    constexpr int R = 128 / SPLITS;
+    const int share = min(R, (P.M - tm * 128 + SPLITS - 1) / SPLITS);
+    ls_share e = {tile + part * share * LS_LD, LS_LD, tm * 128 + part * share, share, tn * 128, 0, 1, 1, 0};
+    const ls_operands first = ls_first<PROD, T, SPLITS, 1>(P, e);
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
         if (pass == 1) {
@@ -759,43 +870,15 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if (SPLITS > 1) lfptx::cluster_sync_all();
             else __syncthreads();
         }
-        // This CTA's rows.  A lane takes four columns, a warp a row (its loads from another CTA are whole lines),
-        // RP rows at a time.
-        const int rows = pass == 0 ? 16 * RP : share;
-#pragma unroll 1
-        for (int r0 = warp * RP; r0 < rows; r0 += 16 * RP) {
-            const int col = tn * 128 + lane * 4;
-            float4 x[RP][SPLITS];
-            const float* at = tile + min(part * share + r0, 128 - RP) * LS_LD + lane * 4;   // (rows past the share are not used)
-#pragma unroll
-            for (int p = 0; p < SPLITS; ++p) {
-                const unsigned from = SPLITS > 1 && pass == 1 ? lfptx::map_to_cta(lfptx::smem_u32(at), (unsigned)p) : lfptx::smem_u32(at);
-#pragma unroll
-                for (int h = 0; h < RP; ++h)
-                    x[h][p] = SPLITS > 1 ? lt_ld_cluster_f4(from + h * (LS_LD * 4)) : *reinterpret_cast<const float4*>(at + h * LS_LD);
-            }
-            if (SPLITS > 1 && pass == 1 && r0 + 16 * RP >= rows) {             // this warp reads nothing more of the other parts
-                asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-                arrived = true;
-            }
-#pragma unroll
-            for (int h = 0; h < RP; ++h) {
-                const int row = tm * 128 + part * share + r0 + h;
-                const bool in = pass == 1 && r0 + h < share && row < P.M && col < P.N && !sh->abort_flag;
-                float v[4] = {x[h][0].x, x[h][0].y, x[h][0].z, x[h][0].w};
-#pragma unroll
-                for (int p = 1; p < SPLITS; ++p) {                  // parts in order: the sum does not depend on timing
-                    v[0] += x[h][p].x; v[1] += x[h][p].y; v[2] += x[h][p].z; v[3] += x[h][p].w;
-                }
-                ls_finish4<PROD, T, OUT>(v, P, row, col, in);
-            }
-        }
+        e.live = pass == 1 && !sh->abort_flag;
+        e.rows = pass == 1 ? share : min(share, 1);
+        e.peer0 = pass == 1 ? 0 : part;                          // (a dry run reads its own CTA's memory only)
+        e.peer_step = pass == 1 ? 1 : 0;
+        e.leave = pass;
+        ls_finish<PROD, T, OUT, SPLITS, 1>(P, e, first);
     }
     // no CTA may leave while another one reads its tile
-    if (SPLITS > 1) {
-        if (!arrived) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
+    if (SPLITS > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (warp == 1) {
         __syncwarp();
         lfptx::tc_fence_after();
@@ -899,9 +982,10 @@ k_product_pair_split(const __grid_constant__ CUtensorMap map_a, const __grid_con
     }
     __syncwarp();
     // this CTA's rows: its part of those that exist
-    constexpr int R = 128 / SPLITS, RP = 2;
+    constexpr int R = 128 / SPLITS;
     const int share = min(R, max(0, (P.M - row_base + SPLITS - 1) / SPLITS));
-    bool gave_up = false;
+    ls_share e = {tile + part * share * LD_PS, LD_PS, row_base + part * share, share, tn * 256, rank, 2, 1, 0};
+    const ls_operands first = ls_first<PROD, T, SPLITS, 2>(P, e);
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
         if (pass == 1) {
@@ -923,36 +1007,18 @@ k_product_pair_split(const __grid_constant__ CUtensorMap map_a, const __grid_con
             }
             lfptx::tc_fence_before();
             lfptx::cluster_sync_all();
-            gave_up = sh->abort_flag != 0u;
         }
-        const int units = pass == 0 ? 16 * RP : share * 2;      // row, half of the columns
-#pragma unroll 1
-        for (int u0 = warp * RP; u0 < units; u0 += 16 * RP) {
-            float4 x[RP][SPLITS];
-#pragma unroll
-            for (int h = 0; h < RP; ++h) {
-                const int row = min(part * share + ((u0 + h) >> 1), 127);      // (units past the share are not used)
-                const unsigned at = lfptx::smem_u32(tile + row * LD_PS + ((u0 + h) & 1) * 128 + lane * 4);
-#pragma unroll
-                for (int p = 0; p < SPLITS; ++p)
-                    x[h][p] = lt_ld_cluster_f4(pass == 1 ? lfptx::map_to_cta(at, (unsigned)(2 * p + rank)) : at);
-            }
-#pragma unroll
-            for (int h = 0; h < RP; ++h) {
-                const int u = u0 + h, row = row_base + part * share + (u >> 1), col = tn * 256 + (u & 1) * 128 + lane * 4;
-                float v[4] = {x[h][0].x, x[h][0].y, x[h][0].z, x[h][0].w};
-#pragma unroll
-                for (int p = 1; p < SPLITS; ++p) {                             // parts in order: the sum does not depend on timing
-                    v[0] += x[h][p].x; v[1] += x[h][p].y; v[2] += x[h][p].z; v[3] += x[h][p].w;
-                }
-                ls_finish4<PROD, T, T>(v, P, row, col, pass == 1 && u < units && row < P.M && col < P.N && !gave_up);
-            }
-        }
+        // (a dry run reads its own CTA's memory only, which holds operands still: nothing is kept of it)
+        e.live = pass == 1 && sh->abort_flag == 0u;
+        e.rows = pass == 1 ? share : min(share, 1);
+        e.peer0 = pass == 1 ? rank : member;
+        e.peer_step = pass == 1 ? 2 : 0;
+        e.leave = pass;
+        ls_finish<PROD, T, T, SPLITS, 2>(P, e, first);
     }
     // No CTA may leave (or free tensor memory) while another one reads its tile or the pair's products can reach it.
     lfptx::tc_fence_before();
-    __syncthreads();
-    lfptx::cluster_sync_all();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (threadIdx.x == 0 && rank == 0) {
         // given up: as in the persistent form, the loads of both CTAs that are on their way are waited for, with a limit
         const bool any = sh->abort_flag != 0u || lt_ld_cluster_u32(lfptx::map_to_cta(lfptx::smem_u32((const void*)&sh->abort_flag), leader + 1)) != 0u;
