@@ -60,6 +60,7 @@ struct LtParams {
     const void* add; long long ld_add;
     void* d; long long ld_d;
     unsigned char *q, *s;
+    int wide_q, wide_s, wide_add;      // 256-bit accesses to q and add, 32-bit ones to s, fit a lane's place
     unsigned* status;
     unsigned long long budget_ns;
     int withhold;
@@ -172,18 +173,6 @@ __device__ __forceinline__ void lt_load(unsigned dst, const CUtensorMap* map, un
     }
 }
 
-// ---- epilogue on eight columns of one row -----------------------------------------------------------
-// FORWARD, first half: z = D + bias (in place)
-__device__ __forceinline__ void epi_bias8(float (&v)[8], const LtParams& P, int col)
-{
-    if (!P.bias) return;
-    float b[8];
-    vec8<float> bv;
-    bv.load(P.bias + col);
-    bv.get(b);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += b[k];
-}
 // ================================================================================================
 // CTA pairs, 256 x 256 tiles
 // ================================================================================================
@@ -199,43 +188,62 @@ __device__ __forceinline__ void lp_tile(int t, const LtParams& P, int& tm, int& 
 
 // What the epilogue reads for 32 columns of its row, fetched a step ahead of its use.
 struct lp_operands {
-    uint2 q[4];            // GRAD_X: 8-bit pre-activations ...
+    unsigned q[8];         // GRAD_X: 8-bit pre-activations ...
     unsigned s;            // ... and their scale
-    uint4 add[4];          // residual, 16-bit
-    float4 bias;           // FORWARD, columns 4 * lane ..: brings the line into L1, where the broadcast loads find it
+    unsigned add[16];      // residual, 16-bit
 };
 struct lp_place {
     int row0, col0, lane;
     unsigned char* blk;    // this warp's 32 x 128 bytes of shared memory
     size_t groups;         // 8-bit scales per row
+    bool full;             // every row and column of the block exists
+    float4 bias;           // FORWARD: of columns col0 + 4 * lane ..
     lp_operands next;
 };
+// (256-bit accesses where a lane's 32 or 64 bytes allow them: its row is a line of its own, so every access less
+// is 32 transactions less)
 template <int PROD, typename T>
 __device__ __forceinline__ void lp_fetch(lp_operands& o, const LtParams& P, const lp_place& e, int j)
 {
     if (PROD == LF_PROD_GRAD_W) return;
     const int row = e.row0 + e.lane, col = e.col0 + j * 32;
-    if (PROD == LF_PROD_FORWARD && j == 0 && P.bias && e.col0 + 4 * e.lane < P.N)
-        asm volatile("ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o.bias.x), "=f"(o.bias.y), "=f"(o.bias.z), "=f"(o.bias.w)
-                     : "l"(P.bias + e.col0 + 4 * e.lane));
+    if (PROD == LF_PROD_GRAD_X && P.q && row < P.M && col < P.N) {
+        const unsigned char* from = P.q + (size_t)row * P.N + col;
+        if (e.full && P.wide_q) {
+            ld256(from, o.q);
+        } else {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) { o.q[g] = make_uint2(0, 0); o.add[g] = make_uint4(0, 0, 0, 0); }
-    o.s = 0;
-    if (row >= P.M) return;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        if (col + 8 * g >= P.N) continue;
-        if (PROD == LF_PROD_GRAD_X && P.q) o.q[g] = *reinterpret_cast<const uint2*>(P.q + (size_t)row * P.N + col + 8 * g);
-        if (P.add) o.add[g] = *reinterpret_cast<const uint4*>(static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col + 8 * g);
+            for (int g = 0; g < 4; ++g)
+                if (col + 8 * g < P.N) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(from + 8 * g);
+                    o.q[2 * g] = v.x; o.q[2 * g + 1] = v.y;
+                }
+        }
+        o.s = P.s[(size_t)row * e.groups + (col >> 5)];
     }
-    if (PROD == LF_PROD_GRAD_X && P.q && col < P.N) o.s = P.s[(size_t)row * e.groups + (col >> 5)];
+    if (P.add && row < P.M && col < P.N) {
+        const T* from = static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col;
+        if (e.full && P.wide_add) {
+            ld256(from, *reinterpret_cast<unsigned(*)[8]>(o.add));
+            ld256(from + 16, *reinterpret_cast<unsigned(*)[8]>(o.add + 8));
+        } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (col + 8 * g < P.N) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(from + 8 * g);
+                    o.add[4 * g] = v.x; o.add[4 * g + 1] = v.y; o.add[4 * g + 2] = v.z; o.add[4 * g + 3] = v.w;
+                }
+        }
+    }
 }
 // Epilogue of 32 rows x NC columns, a row per lane.  One copy per activation, straight-line: the accumulator's
 // registers need constant indices, and choosing the activation per eight columns cost 1100 cycles for 32.
 template <int PROD, typename T, typename OUT, int KIND, int NC>
 __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, lp_place& e)
 {
+    static_assert(NC == 128, "four scales of a row are one word");
     const int lane = e.lane, row = e.row0 + lane;
+    unsigned scales = 0;
 #pragma unroll
     for (int j = 0; j < NC / 32; ++j) {                         // 32 columns at a time
         const int col = e.col0 + j * 32;
@@ -244,20 +252,46 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
         const lp_operands now = e.next;
         if (j < NC / 32 - 1) lp_fetch<PROD, T>(e.next, P, e, j + 1);
         if (PROD == LF_PROD_FORWARD) {
+            if (P.bias) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                if (col + 8 * g < P.N) epi_bias8(*reinterpret_cast<float(*)[8]>(v + 8 * g), P, col + 8 * g);
+                for (int g = 0; g < 8; ++g) {                   // lane 8 j + g holds the bias of these four columns
+                    const int from = 8 * j + g;
+                    const float2 lo = add2(make_float2(v[4 * g], v[4 * g + 1]), make_float2(__shfl_sync(0xFFFFFFFFu, e.bias.x, from), __shfl_sync(0xFFFFFFFFu, e.bias.y, from)));
+                    const float2 hi = add2(make_float2(v[4 * g + 2], v[4 * g + 3]), make_float2(__shfl_sync(0xFFFFFFFFu, e.bias.z, from), __shfl_sync(0xFFFFFFFFu, e.bias.w, from)));
+                    v[4 * g] = lo.x; v[4 * g + 1] = lo.y; v[4 * g + 2] = hi.x; v[4 * g + 3] = hi.y;
+                }
+            }
             if (P.q && valid > 0) {
                 unsigned m = 0;
+                if (valid == 32) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) if (i < valid) m = max(m, abs_bits(v[i]));
+                    for (int i = 0; i < 32; ++i) m = max(m, abs_bits(v[i]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) if (i < valid) m = max(m, abs_bits(v[i]));
+                }
                 const unsigned b = scale_byte(m);
                 unsigned char* qp = P.q + (size_t)row * P.N + col;
+                if (e.full && P.wide_q) {
+                    unsigned w[8];
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    if (8 * g < valid)
-                        *reinterpret_cast<uint2*>(qp + 8 * g) = quantize8(*reinterpret_cast<float(*)[8]>(v + 8 * g), b);
-                P.s[(size_t)row * e.groups + (col >> 5)] = (unsigned char)b;
+                    for (int g = 0; g < 4; ++g) {
+                        const uint2 q8 = quantize8(*reinterpret_cast<float(*)[8]>(v + 8 * g), b);
+                        w[2 * g] = q8.x; w[2 * g + 1] = q8.y;
+                    }
+                    st256(qp, w);
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        if (8 * g < valid)
+                            *reinterpret_cast<uint2*>(qp + 8 * g) = quantize8(*reinterpret_cast<float(*)[8]>(v + 8 * g), b);
+                }
+                if (e.full && P.wide_s) {                       // four scales at once
+                    scales |= b << (8 * j);
+                    if (j == NC / 32 - 1) *reinterpret_cast<unsigned*>(P.s + (size_t)row * e.groups + (e.col0 >> 5)) = scales;
+                } else {
+                    P.s[(size_t)row * e.groups + (col >> 5)] = (unsigned char)b;
+                }
             }
             act_all<true, 32, KIND>(v);
         }
@@ -265,19 +299,18 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 float z[8];
-                dequantize8(now.q[g], now.s, z);
+                dequantize8(make_uint2(now.q[2 * g], now.q[2 * g + 1]), now.s, z);
                 prime_all<true, 8, KIND>(v + 8 * g, z);
             }
         }
         if (PROD != LF_PROD_GRAD_W && P.add) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                vec8<T> rv;
-                float r[8];
-                rv.u = now.add[g];
-                rv.get(r);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[8 * g + i] += r[i];
+                for (int i = 0; i < 4; ++i) {
+                    const float2 r = add2(make_float2(v[8 * g + 2 * i], v[8 * g + 2 * i + 1]), unpack2(now.add[4 * g + i], T()));
+                    v[8 * g + 2 * i] = r.x; v[8 * g + 2 * i + 1] = r.y;
+                }
             }
         }
         constexpr int PER = sizeof(OUT) == 2 ? 2 : 1;            // blocks of 32 columns per stored line
@@ -496,7 +529,8 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const int row0 = (tm * 2 + (int)rank) * (MB * 128) + (tb % MB) * 128 + quad * 32;
             const int col0 = tn * 256 + half * NC;
             const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * (unsigned)NC;
-            lp_place e = {row0, col0, lane, blk, groups, {}};
+            lp_place e = {row0, col0, lane, blk, groups, row0 + 32 <= P.M && col0 + NC <= P.N, make_float4(0.f, 0.f, 0.f, 0.f), {}};
+            if (PROD == LF_PROD_FORWARD && P.bias && col0 + 4 * lane < P.N) e.bias = *reinterpret_cast<const float4*>(P.bias + col0 + 4 * lane);
             lp_fetch<PROD, T>(e.next, P, e, 0);                  // on its way while the accumulator is waited for
             float acc[NC];
             if (PROMOTE) {
@@ -1228,6 +1262,9 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
     P.bias = p.bias; P.add = p.add; P.ld_add = p.ld_add;
     P.d = p.d; P.ld_d = p.ld_d;
     P.q = p.q; P.s = p.s;
+    P.wide_q = (p.N & 31) == 0 && (reinterpret_cast<uintptr_t>(p.q) & 31) == 0;
+    P.wide_s = (p.N & 127) == 0 && (reinterpret_cast<uintptr_t>(p.s) & 3) == 0;
+    P.wide_add = (p.ld_add & 15) == 0 && (reinterpret_cast<uintptr_t>(p.add) & 31) == 0;
     P.status = o->status_dev;
     P.budget_ns = (unsigned long long)o->wait_budget_us * 1000ull;
     P.withhold = o->withhold;
