@@ -205,7 +205,6 @@ struct lp_place {
 template <int PROD, typename T>
 __device__ __forceinline__ void lp_fetch(lp_operands& o, const LtParams& P, const lp_place& e, int j)
 {
-    if (PROD == LF_PROD_GRAD_W) return;
     const int row = e.row0 + e.lane, col = e.col0 + j * 32;
     if (PROD == LF_PROD_GRAD_X && P.q && row < P.M && col < P.N) {
         const unsigned char* from = P.q + (size_t)row * P.N + col;
@@ -237,8 +236,9 @@ __device__ __forceinline__ void lp_fetch(lp_operands& o, const LtParams& P, cons
     }
 }
 // Epilogue of 32 rows x NC columns, a row per lane.  One copy per activation, straight-line: the accumulator's
-// registers need constant indices, and choosing the activation per eight columns cost 1100 cycles for 32.
-template <int PROD, typename T, typename OUT, int KIND, int NC>
+// registers need constant indices, and choosing the activation per eight columns cost 1100 cycles for 32.  And one
+// copy without 8-bit values and residual (OPERANDS = false), which then holds no registers for them.
+template <int PROD, typename T, typename OUT, int KIND, int NC, bool OPERANDS>
 __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, lp_place& e)
 {
     static_assert(NC == 128, "four scales of a row are one word");
@@ -250,7 +250,7 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
         const int valid = row < P.M ? min(32, P.N - col) : 0;   // a multiple of 8, or not positive
         float* v = acc + 32 * j;
         const lp_operands now = e.next;
-        if (j < NC / 32 - 1) lp_fetch<PROD, T>(e.next, P, e, j + 1);
+        if (OPERANDS && j < NC / 32 - 1) lp_fetch<PROD, T>(e.next, P, e, j + 1);
         if (PROD == LF_PROD_FORWARD) {
             if (P.bias) {
 #pragma unroll
@@ -261,7 +261,7 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
                     v[4 * g] = lo.x; v[4 * g + 1] = lo.y; v[4 * g + 2] = hi.x; v[4 * g + 3] = hi.y;
                 }
             }
-            if (P.q && valid > 0) {
+            if (OPERANDS && P.q && valid > 0) {
                 unsigned m = 0;
                 if (valid == 32) {
 #pragma unroll
@@ -295,7 +295,7 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
             }
             act_all<true, 32, KIND>(v);
         }
-        if (PROD == LF_PROD_GRAD_X && KIND != LF_ACT_NONE) {
+        if (OPERANDS && PROD == LF_PROD_GRAD_X && KIND != LF_ACT_NONE) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 float z[8];
@@ -303,7 +303,7 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
                 prime_all<true, 8, KIND>(v + 8 * g, z);
             }
         }
-        if (PROD != LF_PROD_GRAD_W && P.add) {
+        if (OPERANDS && P.add) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
 #pragma unroll
@@ -531,7 +531,8 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * (unsigned)NC;
             lp_place e = {row0, col0, lane, blk, groups, row0 + 32 <= P.M && col0 + NC <= P.N, make_float4(0.f, 0.f, 0.f, 0.f), {}};
             if (PROD == LF_PROD_FORWARD && P.bias && col0 + 4 * lane < P.N) e.bias = *reinterpret_cast<const float4*>(P.bias + col0 + 4 * lane);
-            lp_fetch<PROD, T>(e.next, P, e, 0);                  // on its way while the accumulator is waited for
+            const bool operands = PROD != LF_PROD_GRAD_W && (P.q || P.add);
+            if (operands) lp_fetch<PROD, T>(e.next, P, e, 0);   // on its way while the accumulator is waited for
             float acc[NC];
             if (PROMOTE) {
 #pragma unroll
@@ -562,14 +563,31 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 __syncwarp();
                 if (lane == 0) lt_arrive_cluster(leader_acc_empty + ab * 8u);
             }
-            switch (PROD == LF_PROD_GRAD_W || (PROD == LF_PROD_GRAD_X && !P.q) ? LF_ACT_NONE : P.act) {
-                case LF_ACT_SIGMOID: lp_finish<PROD, T, OUT, LF_ACT_SIGMOID, NC>(acc, P, e); break;
-                case LF_ACT_TANH: lp_finish<PROD, T, OUT, LF_ACT_TANH, NC>(acc, P, e); break;
-                case LF_ACT_RELU: lp_finish<PROD, T, OUT, LF_ACT_RELU, NC>(acc, P, e); break;
-                case LF_ACT_SILU: lp_finish<PROD, T, OUT, LF_ACT_SILU, NC>(acc, P, e); break;
-                case LF_ACT_GELU: lp_finish<PROD, T, OUT, LF_ACT_GELU, NC>(acc, P, e); break;
-                default: lp_finish<PROD, T, OUT, LF_ACT_NONE, NC>(acc, P, e); break;
+            const int act = PROD == LF_PROD_GRAD_W || (PROD == LF_PROD_GRAD_X && !P.q) ? LF_ACT_NONE : P.act;
+            if constexpr (PROD != LF_PROD_GRAD_W) {
+                if (operands) {
+                    switch (act) {
+                        case LF_ACT_SIGMOID: lp_finish<PROD, T, OUT, LF_ACT_SIGMOID, NC, true>(acc, P, e); break;
+                        case LF_ACT_TANH: lp_finish<PROD, T, OUT, LF_ACT_TANH, NC, true>(acc, P, e); break;
+                        case LF_ACT_RELU: lp_finish<PROD, T, OUT, LF_ACT_RELU, NC, true>(acc, P, e); break;
+                        case LF_ACT_SILU: lp_finish<PROD, T, OUT, LF_ACT_SILU, NC, true>(acc, P, e); break;
+                        case LF_ACT_GELU: lp_finish<PROD, T, OUT, LF_ACT_GELU, NC, true>(acc, P, e); break;
+                        default: lp_finish<PROD, T, OUT, LF_ACT_NONE, NC, true>(acc, P, e); break;
+                    }
+                    continue;
+                }
             }
+            if constexpr (PROD == LF_PROD_FORWARD) {
+                switch (act) {
+                    case LF_ACT_SIGMOID: lp_finish<PROD, T, OUT, LF_ACT_SIGMOID, NC, false>(acc, P, e); continue;
+                    case LF_ACT_TANH: lp_finish<PROD, T, OUT, LF_ACT_TANH, NC, false>(acc, P, e); continue;
+                    case LF_ACT_RELU: lp_finish<PROD, T, OUT, LF_ACT_RELU, NC, false>(acc, P, e); continue;
+                    case LF_ACT_SILU: lp_finish<PROD, T, OUT, LF_ACT_SILU, NC, false>(acc, P, e); continue;
+                    case LF_ACT_GELU: lp_finish<PROD, T, OUT, LF_ACT_GELU, NC, false>(acc, P, e); continue;
+                    default: break;
+                }
+            }
+            lp_finish<PROD, T, OUT, LF_ACT_NONE, NC, false>(acc, P, e);
         }
     }
 
