@@ -53,6 +53,7 @@ struct LtParams {
     int M, N, K;
     int tiles_m, tiles_n;
     int band;                          // pairs: tile rows of a band of the schedule
+    int width;                         // pairs: columns of a tile, a multiple of 32 up to 256
     int stages_per_split;      // split tiles
     int act;
     unsigned idesc;
@@ -157,13 +158,15 @@ __device__ __forceinline__ float4 lt_ld_cluster_f4(unsigned addr)
     return v;
 }
 
-// One operand block of a stage: `mn` the first row/column, `k` the first contraction step.
+// One operand block of a stage: `mn` the first row/column, `k` the first contraction step; `cols` as many as are
+// needed of its 128 (of an MN-major block, in boxes of 64; of a K-major one, what the map's box says).
 template <bool MN, bool PAIR>
-__device__ __forceinline__ void lt_load(unsigned dst, const CUtensorMap* map, unsigned bar, int mn, int k)
+__device__ __forceinline__ void lt_load(unsigned dst, const CUtensorMap* map, unsigned bar, int mn, int k, int cols = 128)
 {
     if (MN) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+            if (i * 64 >= cols) break;
             if (PAIR) lfptx::tma_load_2d_pair(dst + i * 8192, map, bar, mn + i * 64, k);
             else lfptx::tma_load_2d(dst + i * 8192, map, bar, mn + i * 64, k);
         }
@@ -193,7 +196,7 @@ struct lp_operands {
     unsigned add[16];      // residual, 16-bit
 };
 struct lp_place {
-    int row0, col0, lane;
+    int row0, col0, end, lane;     // (end: past the tile's last column)
     unsigned char* blk;    // this warp's 32 x 128 bytes of shared memory
     size_t groups;         // 8-bit scales per row
     bool full;             // every row and column of the block exists
@@ -206,21 +209,21 @@ template <int PROD, typename T>
 __device__ __forceinline__ void lp_fetch(lp_operands& o, const LtParams& P, const lp_place& e, int j)
 {
     const int row = e.row0 + e.lane, col = e.col0 + j * 32;
-    if (PROD == LF_PROD_GRAD_X && P.q && row < P.M && col < P.N) {
+    if (PROD == LF_PROD_GRAD_X && P.q && row < P.M && col < e.end) {
         const unsigned char* from = P.q + (size_t)row * P.N + col;
         if (e.full && P.wide_q) {
             ld256(from, o.q);
         } else {
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                if (col + 8 * g < P.N) {
+                if (col + 8 * g < e.end) {
                     const uint2 v = *reinterpret_cast<const uint2*>(from + 8 * g);
                     o.q[2 * g] = v.x; o.q[2 * g + 1] = v.y;
                 }
         }
         o.s = P.s[(size_t)row * e.groups + (col >> 5)];
     }
-    if (P.add && row < P.M && col < P.N) {
+    if (P.add && row < P.M && col < e.end) {
         const T* from = static_cast<const T*>(P.add) + (size_t)row * P.ld_add + col;
         if (e.full && P.wide_add) {
             ld256(from, *reinterpret_cast<unsigned(*)[8]>(o.add));
@@ -228,7 +231,7 @@ __device__ __forceinline__ void lp_fetch(lp_operands& o, const LtParams& P, cons
         } else {
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                if (col + 8 * g < P.N) {
+                if (col + 8 * g < e.end) {
                     const uint4 v = *reinterpret_cast<const uint4*>(from + 8 * g);
                     o.add[4 * g] = v.x; o.add[4 * g + 1] = v.y; o.add[4 * g + 2] = v.z; o.add[4 * g + 3] = v.w;
                 }
@@ -247,7 +250,8 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
 #pragma unroll
     for (int j = 0; j < NC / 32; ++j) {                         // 32 columns at a time
         const int col = e.col0 + j * 32;
-        const int valid = row < P.M ? min(32, P.N - col) : 0;   // a multiple of 8, or not positive
+        if (j % 2 == 0 && col >= e.end) break;                  // a narrower tile, or the last one
+        const int valid = row < P.M ? min(32, e.end - col) : 0;   // a multiple of 8, or not positive
         float* v = acc + 32 * j;
         const lp_operands now = e.next;
         if (OPERANDS && j < NC / 32 - 1) lp_fetch<PROD, T>(e.next, P, e, j + 1);
@@ -286,7 +290,7 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
                         if (8 * g < valid)
                             *reinterpret_cast<uint2*>(qp + 8 * g) = quantize8(*reinterpret_cast<float(*)[8]>(v + 8 * g), b);
                 }
-                if (e.full && P.wide_s) {                       // four scales at once
+                if (e.full && P.wide_s && (e.col0 & 127) == 0) {                       // four scales at once
                     scales |= b << (8 * j);
                     if (j == NC / 32 - 1) *reinterpret_cast<unsigned*>(P.s + (size_t)row * e.groups + (e.col0 >> 5)) = scales;
                 } else {
@@ -340,7 +344,7 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
 #pragma unroll
             for (int i = 0; i < 8; ++i)                         // row (lane >> 3) + 4 i: its turn alternates
                 u[i] = *reinterpret_cast<const uint4*>(from + i * 512 + (((lane & 7) ^ (((lane >> 3) + 4 * i) & 7)) << 4));
-            if (cu < P.N) {
+            if (cu < e.end) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (r0 + 4 * i < P.M) *reinterpret_cast<uint4*>(to + i * step) = u[i];
@@ -374,6 +378,8 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int n_tiles = P.tiles_m * P.tiles_n;
     const int n_k = (P.K + LT_BK - 1) / LT_BK;
     const int chunk = PROMOTE ? LT_CHUNK : n_k;
+    // bytes that this CTA's loads of a stage bring
+    const unsigned stage_bytes = MB * LT_BLOCK_BYTES + (unsigned)(B_MN ? (P.width > 128 ? 128 : 64) : P.width / 2) * (LT_BK * 2);
 
     if (threadIdx.x == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
@@ -414,18 +420,18 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
                 int tm, tn;
                 lp_tile(t, P, tm, tn);
-                const int m0 = (tm * 2 + (int)rank) * (MB * 128), n0 = tn * 256 + (int)rank * 128;
+                const int m0 = (tm * 2 + (int)rank) * (MB * 128), n0 = tn * P.width + (int)rank * (P.width / 2);
                 for (int ks = 0; ks < n_k; ++ks, ++it) {
                     const unsigned st = it % STAGES, use = it / STAGES;
                     if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->empty[st]), (use - 1) & 1u, P, sh)) { ok = false; break; }
                     const unsigned lbar = lfptx::smem_u32(&sh->full[st]);
                     if (P.withhold && pair == 0 && rank == 1 && it == 0) continue;    // test hook
-                    if (rank == 0) lfptx::mbar_arrive_expect_tx(lbar, 2u * STAGE_BYTES);
+                    if (rank == 0) lfptx::mbar_arrive_expect_tx(lbar, 2u * stage_bytes);
                     const unsigned bar = lfptx::map_to_cta(lbar, 0);
                     const unsigned dst = lfptx::smem_u32(ring + (size_t)st * STAGE_BYTES);
 #pragma unroll
                     for (int b = 0; b < MB; ++b) lt_load<A_MN, true>(dst + b * LT_BLOCK_BYTES, &map_a, bar, m0 + b * 128, ks * LT_BK);
-                    lt_load<B_MN, true>(dst + MB * LT_BLOCK_BYTES, &map_b, bar, n0, ks * LT_BK);
+                    lt_load<B_MN, true>(dst + MB * LT_BLOCK_BYTES, &map_b, bar, n0, ks * LT_BK, P.width / 2);
                 }
             }
             sh->prog_it = it;
@@ -527,9 +533,9 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int tm, tn;
             lp_tile(tb / MB, P, tm, tn);
             const int row0 = (tm * 2 + (int)rank) * (MB * 128) + (tb % MB) * 128 + quad * 32;
-            const int col0 = tn * 256 + half * NC;
+            const int col0 = tn * P.width + half * NC, end = min(P.N, (tn + 1) * P.width);
             const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * (unsigned)NC;
-            lp_place e = {row0, col0, lane, blk, groups, row0 + 32 <= P.M && col0 + NC <= P.N, make_float4(0.f, 0.f, 0.f, 0.f), {}};
+            lp_place e = {row0, col0, end, lane, blk, groups, row0 + 32 <= P.M && col0 + NC <= end, make_float4(0.f, 0.f, 0.f, 0.f), {}};
             if (PROD == LF_PROD_FORWARD && P.bias && col0 + 4 * lane < P.N) e.bias = *reinterpret_cast<const float4*>(P.bias + col0 + 4 * lane);
             const bool operands = PROD != LF_PROD_GRAD_W && (P.q || P.add);
             if (operands) lp_fetch<PROD, T>(e.next, P, e, 0);   // on its way while the accumulator is waited for
@@ -605,8 +611,8 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const unsigned hi = max(it_l, it_p), lo = min(it_l, it_p);
             for (unsigned j = lo; j < hi; ++j) {
                 const unsigned bar = lfptx::smem_u32(&sh->full[j % STAGES]);
-                if (j >= it_l) lfptx::mbar_arrive_expect_tx(bar, STAGE_BYTES);                // only the peer loaded
-                else lt_complete_tx(bar, STAGE_BYTES);                                        // only the leader loaded
+                if (j >= it_l) lfptx::mbar_arrive_expect_tx(bar, stage_bytes);                // only the peer loaded
+                else lt_complete_tx(bar, stage_bytes);                                        // only the leader loaded
             }
             const unsigned long long t0 = lfptx::globaltimer_ns();
             for (unsigned j = hi > STAGES ? hi - STAGES : 0; j < hi; ++j) {
@@ -1232,35 +1238,59 @@ int lf_product_tc_init(lf_ops* o)
 
 namespace {
 
-struct lt_choice { int splits, tile; };      // splits = 0: CTA pairs on `tile`; < 0: split pairs; else split tiles
+struct lt_choice { int splits, tile, width; };      // splits = 0: CTA pairs on `tile`, `width` columns wide; < 0: split pairs; else split tiles
 
-// The form with the least estimated time, in SM cycles; constants measured on B200 (widths 512 .. 16384, 17 .. 8192
-// tokens).  A 64-deep stage costs a 256 x 256 pair tile 568 cycles, a 512 x 256 one 1024 and a 128 x 128 tile 560
-// (an instruction takes as long for 128 columns as for 256); switching tiles costs 600 or 5000 and, where the
-// parts of a split tile meet, 1500 and the bytes from the other parts at 14 a cycle; the rest is the launch, the first
-// loads and the last epilogue.
+// The form with the least estimated time, in SM cycles; constants measured on B200 (widths 72 .. 16384, 17 .. 8192
+// tokens).  A 64-deep stage costs what is most of: its products (a pair: 2 cycles per column and 128-row block of a
+// CTA), a multiprocessor's own fetch at 57 bytes a cycle, and all multiprocessors' fetch at 7600 bytes a cycle from
+// L2, which is what limits 256 x 256 tiles when all are busy.  Rows that do not begin on a 32-byte sector cost a fetch
+// five sectors for four (6998 x 1976 -> 6744: 293,000 cycles, 6998 x 1984 -> 6744: 220,000).  Narrower tiles only pay where
+// they fill the last wave better (408 x 4576 -> 12728: 49 us with 512 x 192 tiles, 55 with 256 x 256); their MN-major operand
+// comes in boxes of 64 columns per CTA, so they are taken for the forward product.  Switching tiles
+// costs 600, but no tile takes less than its epilogue, or with 512 rows 4300 and the epilogue, of which little
+// runs beside the products there; where the parts of a split tile meet, 1500 and the bytes from the other parts at 14 a
+// cycle; the rest is the launch, the first loads and the last epilogue.
 lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
 {
     auto waves = [](long long units, int at_once) { return (double)((units + at_once - 1) / at_once); };
-    lt_choice best = {1, 0};
+    lt_choice best = {1, 0, 0};
     double least = 1e30;
     auto offer = [&](lt_choice c, double cycles) { if (cycles < least) { least = cycles; best = c; } };
     const long long m128 = (p.M + 127) / 128, m256 = (p.M + 255) / 256, m512 = (p.M + 511) / 512;
     const long long n128 = (p.N + 127) / 128, n256 = (p.N + 255) / 256;
     const double rows = p.M < 128 ? p.M / 128.0 : 1.0;
+    auto sectors = [](const void* base, long long ld) { return ((reinterpret_cast<uintptr_t>(base) | (uintptr_t)(2 * ld)) & 31) ? 1.25 : 1.0; };
+    const double row_a = 128.0 * sectors(p.a, p.ld_a), row_b = 128.0 * sectors(p.b, p.ld_b);      // a row of a stage, as fetched
+    // a stage of `a` rows of A and `b` of B per CTA, `ctas` of them at work
+    auto stage = [&](double products, int a, int b, double ctas) {
+        const double bytes = a * row_a + b * row_b, own = bytes / 57.0, all = bytes * ctas / 7600.0;
+        return products > own ? (products > all ? products : all) : (own > all ? own : all);
+    };
+    auto busy = [](long long units, int at_once) { return (double)(units < at_once ? units : at_once); };
     for (int splits = 1; splits <= 8 && splits <= n_k; splits *= 2) {
         const double part = (double)((n_k + splits - 1) / splits);
         const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
         const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
-        offer({splits, 0}, waves(m128 * n128 * splits, at_once) * (part * 560.0 + meet + 6300.0 + 3200.0 / splits));
+        const long long ctas = m128 * n128 * splits;
+        offer({splits, 0, 0}, waves(ctas, at_once) * (part * stage(256.0, 128, 128, busy(ctas, at_once)) + meet + 6300.0 + 3200.0 / splits));
     }
     if (o->max_pair_splits > 0 && n_k >= LPS_SPLITS && p.out_dtype != LF_F32) {
         const double part = (double)((n_k + LPS_SPLITS - 1) / LPS_SPLITS), meet = 2000.0 + 65536.0 * rows / 14.0;
-        offer({-LPS_SPLITS, 0}, waves(m256 * n256, o->max_pair_splits) * (part * 568.0 + meet + 11500.0));
+        const long long tiles = m256 * n256;
+        offer({-LPS_SPLITS, 0, 0}, waves(tiles, o->max_pair_splits) *
+              (part * stage(512.0, 128, 128, 2.0 * LPS_SPLITS * busy(tiles, o->max_pair_splits)) + meet + 11500.0));
     }
+    // epilogue of 128 rows x 256 columns: as it is, an activation, 8-bit values one way or the other
+    const double epilogue = p.q ? 10000.0 : p.prod == LF_PROD_FORWARD && p.act != LF_ACT_NONE ? 7500.0 : 3700.0;
     if (o->max_pairs > 0) {
-        offer({0, LT_256x256}, waves(m256 * n256, o->max_pairs) * (n_k * 568.0 + 600.0) + 14000.0);
-        if (p.out_dtype != LF_F32) offer({0, LT_512x256}, waves(m512 * n256, o->max_pairs) * (n_k * 1024.0 + 5000.0) + 14000.0);
+        for (int width = 256; width >= (p.prod == LF_PROD_FORWARD ? 160 : 256); width -= 32) {
+            const long long n = (p.N + width - 1) / width, t256 = m256 * n, t512 = m512 * n;
+            const double products = n_k * stage(2.0 * width, 128, width / 2, 2.0 * busy(t256, o->max_pairs));
+            offer({0, LT_256x256, width}, waves(t256, o->max_pairs) * ((products > epilogue ? products : epilogue) + 600.0) + 14000.0);
+            if (p.out_dtype != LF_F32)
+                offer({0, LT_512x256, width}, waves(t512, o->max_pairs) *
+                      (n_k * stage(4.0 * width, 256, width / 2, 2.0 * busy(t512, o->max_pairs)) + 4300.0 + epilogue) + 14000.0);
+        }
     }
     return best;
 }
@@ -1295,7 +1325,7 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
     const lt_choice c = lt_choose(o, p, n_k);
     alignas(64) CUtensorMap map_a, map_b;
     const bool ok = (a_mn ? lt_map(&map_a, in_type, p.a, p.K, p.M, p.ld_a, 64, 64) : lt_map(&map_a, in_type, p.a, p.M, p.K, p.ld_a, 64, 128)) &&
-                    (b_mn ? lt_map(&map_b, in_type, p.b, p.K, p.N, p.ld_b, 64, 64) : lt_map(&map_b, in_type, p.b, p.N, p.K, p.ld_b, 64, 128));
+                    (b_mn ? lt_map(&map_b, in_type, p.b, p.K, p.N, p.ld_b, 64, 64) : lt_map(&map_b, in_type, p.b, p.N, p.K, p.ld_b, 64, c.splits == 0 ? c.width / 2 : 128));
     if (!ok) { o->last_cuda_error = (int)cudaErrorInvalidValue; return LF_ECUDA; }
 
     cudaLaunchConfig_t cfg;
@@ -1310,8 +1340,9 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
         o->stats.splits = LPS_SPLITS;
     } else if (c.splits == 0) {
         const int bm = c.tile == LT_512x256 ? 512 : 256;
-        P.tiles_m = (p.M + bm - 1) / bm; P.tiles_n = (p.N + 255) / 256;
-        P.idesc = idesc | (256u >> 3) << 17 | (256u >> 4) << 24;
+        P.width = c.width;
+        P.tiles_m = (p.M + bm - 1) / bm; P.tiles_n = (p.N + c.width - 1) / c.width;
+        P.idesc = idesc | ((unsigned)c.width >> 3) << 17 | (256u >> 4) << 24;
         P.band = 2048 / bm;
         const int tiles = P.tiles_m * P.tiles_n, pairs = tiles < o->max_pairs ? tiles : o->max_pairs;
         lt_cluster_config(&cfg, at, 2 * pairs, LP_THREADS, 2, LP_SMEM, o->stream);
