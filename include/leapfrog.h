@@ -479,7 +479,7 @@ typedef struct lf_ops_stats {
 enum lf_linear_form {
     LF_FORM_STREAM = 1, /* few tokens: weights streamed once through warp-wide products        */
     LF_FORM_SPLIT = 2,  /* 128 x 128 tiles, the contraction split over a thread-block cluster  */
-    LF_FORM_PAIRS = 3,  /* 256 x 256 or 512 x 256 tiles of CTA pairs, persistent               */
+    LF_FORM_PAIRS = 3,  /* 256- or 512-row tiles of CTA pairs, up to 256 wide, persistent     */
     LF_FORM_SPLIT_PAIRS = 4 /* 256 x 256 tiles of CTA pairs, the contraction split over a cluster */
 };
 

@@ -6,7 +6,8 @@
 // split the contraction of a tile of up to 32 output columns, and every warp keeps SR_DEPTH - 1 steps
 // of loads in flight, on into the next tile.  A tile has as many columns as make the tiles come out even
 // over the multiprocessors (4096 columns: 147 blocks of 28; 128 of 32 left a seventh of the memory
-// rate unused), or a whole 8-bit scale group where z is kept.
+// rate unused), or a whole 8-bit scale group where z is kept.  One token, 4096 -> 4096 bf16: 7.3 us with its launch,
+// 4.6 TB/s (a plain copy of the weights' bytes: 5.1 us); with the ring in registers 11 us.  16 tokens, 1032 -> 4104: 4.7.
 #include "lf_ops_internal.h"
 #include "lf_ptx.cuh"
 #include "lf_rows.cuh"

@@ -4,16 +4,22 @@
 //   grad_x   A = dz [tokens][n_out], B = w^T (w read MN-major): dx = D (.) sigma'(z from 8 bits) + add
 //   grad_w   A = dz^T, B = x^T (both MN-major, the contraction runs over tokens):  gw = D
 // Every operand is used where it lies; what differs is the box TMA fetches and the descriptor's
-// majorness.  A K stage is 64 deep; a CTA fetches a 128 x 64 block of A and one of B (16 KiB each, 128-byte
-// swizzle) per stage, six stages in flight.
+// majorness.  A K stage is 64 deep; a block of operand is 128 x 64 (16 KiB, 128-byte swizzle).
 //
-// Two forms.  CTA pairs (k_product_pair): tcgen05.mma.cta_group::2 on 256 x 256 tiles, each CTA fetching half
-// of both operands, so a stage of 512 tensor-core cycles needs 32 KiB per CTA; persistent, two
-// accumulators in tensor memory, so the epilogue of a tile runs under the next tile's products.  Split tiles
-// (k_product_split): one CTA per 128 x 128 tile and part of the contraction; the CTAs of a tile form
-// a cluster and add their parts through distributed shared memory, each finishing its share of the rows.
-// The first form needs the fewest operand bytes per product, the second fills the device when
-// there are few tiles.
+// Three kernels, chosen by an estimate of each one's time (lt_choose):
+//   CTA pairs (k_product_pair): tcgen05.mma.cta_group::2, persistent.  256 x 256 tiles with two accumulators that take
+//     turns, so that the epilogue of a tile runs under the next tile's products, or 512 x 256 tiles, an accumulator for
+//     each 256 rows, which fetch 24 KiB for what 256 x 256 tiles fetch 32; the forward product's may be narrower.
+//   Split tiles (k_product_split): one CTA per 128 x 128 tile and part of the contraction (1, 2, 4 or 8 parts); the
+//     CTAs of a tile form a cluster, add their parts through distributed shared memory, and each finishes its
+//     share of the rows.  Fills the device where there are few tiles.
+//   Split pairs (k_product_pair_split): 256 x 256 tiles of CTA pairs, two pairs to a cluster and half of the
+//     contraction each, for what lies between.
+// What bounds them: large products the chip's power limit (8192 x 4096 -> 16384 in a loop: 1.35 PFLOP/s without an
+// activation, 1.28 with GELU; the tensor cores are at work 85 % of the time in a single launch); middle ones the fetch
+// of operands from L2; small ones launch, first loads and the meeting of the parts (5 to 6 us for a small layer, of
+// which 2.3 is the launch).  Copies that reach several CTAs of a cluster at once would relieve the fetch; they are
+// left out because operands may be any memory that the caller's device can address.
 //
 // The tensor core adds into its accumulator by truncation.  Results that are rounded to 16 bits do not see
 // it; an fp32 weight gradient over thousands of tokens would (about 1e-5 relative after 512
@@ -177,9 +183,9 @@ __device__ __forceinline__ void lt_load(unsigned dst, const CUtensorMap* map, un
 }
 
 // ================================================================================================
-// CTA pairs, 256 x 256 tiles
+// CTA pairs
 // ================================================================================================
-// tile of a persistent schedule: bands of eight row blocks, column by column inside a band, so that the
+// tile of a persistent schedule: bands of 2048 rows, column by column inside a band, so that the
 // tiles worked on at one time share both operands in L2
 __device__ __forceinline__ void lp_tile(int t, const LtParams& P, int& tm, int& tn)
 {
@@ -355,7 +361,10 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
 }
 
 // MB: 128-row blocks per CTA.  MB = 1: 256 x 256 tiles, the two accumulators alternate between tiles (or
-// chunks).  MB = 2: 512 x 256 tiles, one accumulator per block.
+// chunks).  MB = 2: 512 x 256 tiles, one accumulator per block: a 64-deep stage takes 1024 cycles for twice the
+// products of MB = 1's 568 (8192 x 4096 -> 16384 without an activation: 813 us in a loop, 841 with MB = 1).
+// Epilogue of 128 rows x 256 columns: 3700 cycles as it is, 7500 with GELU (half of it exponentials and
+// reciprocals), 10000 with 8-bit values.  8192 x 1024 -> 4096: 53 us, with GELU 63, with GELU, checkpoint and residual 90.
 template <int PROD, typename T, typename OUT, int MB>
 __global__ void __launch_bounds__(LP_THREADS, 1)
 k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -631,6 +640,11 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // ================================================================================================
 // Split tiles: one CTA per 128 x 128 tile and part of the contraction, a cluster per tile
 // ================================================================================================
+// Bound by latency: of 5.4 us for 70 x 520 -> 1024 (8 parts; floor 0.2) the launch is 2.3, the rest set-up, first loads,
+// meeting of the parts and store, one after another.  Distributed shared memory gives a multiprocessor 14 bytes a
+// cycle, so 64 KB from the other parts are 4300 cycles: rows that do not exist are not exchanged (32 tokens, 4096 -> 4096:
+// 10.8 us against 14.2).  509 x 4096 -> 1024 with 4 parts: 11.1 us, with 2: 14.9.
+//
 // What is left to do for a CTA's share of a tile's rows: add the parts, bias, 8 bits, activation, residual, store.  A
 // piece is 128 columns of a row, half a warp's: a lane has columns 4 i .. and 64 + 4 i .., so that every
 // access is a whole line, also to another CTA's tile, and eight neighbours hold an 8-bit scale group.  With eight

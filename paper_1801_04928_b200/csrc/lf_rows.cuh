@@ -1,4 +1,4 @@
-// Device helpers of the layer operators: rows of fp32 / bf16 / f16 as fp32 vectors of eight, the
+// Device helpers of the layer operators: rows of fp32 / bf16 / f16 as fp32 vectors of 8 or 16, the
 // activations and their derivatives from the pre-activation, and the 8-bit form (e4m3 numbers, one
 // power-of-two scale for 32 columns).
 #pragma once
