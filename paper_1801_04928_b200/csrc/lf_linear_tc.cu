@@ -1261,9 +1261,9 @@ struct lt_choice { int splits, tile, width; };      // splits = 0: CTA pairs on 
 // five sectors for four (6998 x 1976 -> 6744: 293,000 cycles, 6998 x 1984 -> 6744: 220,000).  Narrower tiles only pay where
 // they fill the last wave better (408 x 4576 -> 12728: 49 us with 512 x 192 tiles, 55 with 256 x 256); their MN-major operand
 // comes in boxes of 64 columns per CTA, so they are taken for the forward product.  Switching tiles
-// costs 600, but no tile takes less than its epilogue, or with 512 rows 4300 and the epilogue, of which little
+// costs 600, but no tile takes less than the epilogue before it, or with 512 rows 4300 and the epilogue, of which little
 // runs beside the products there; where the parts of a split tile meet, 1500 and the bytes from the other parts at 14 a
-// cycle; the rest is the launch, the first loads and the last epilogue.
+// cycle; the rest is the launch, the first loads and the last epilogue (a split tile's: 128 columns, more warps).
 lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
 {
     auto waves = [](long long units, int at_once) { return (double)((units + at_once - 1) / at_once); };
@@ -1281,26 +1281,26 @@ lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
         return products > own ? (products > all ? products : all) : (own > all ? own : all);
     };
     auto busy = [](long long units, int at_once) { return (double)(units < at_once ? units : at_once); };
+    // epilogue of 128 rows x 256 columns: as it is, an activation, 8-bit values one way or the other
+    const double epilogue = p.q ? 10000.0 : p.prod == LF_PROD_FORWARD && p.act != LF_ACT_NONE ? 7500.0 : 3700.0;
     for (int splits = 1; splits <= 8 && splits <= n_k; splits *= 2) {
         const double part = (double)((n_k + splits - 1) / splits);
         const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
         const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
         const long long ctas = m128 * n128 * splits;
-        offer({splits, 0, 0}, waves(ctas, at_once) * (part * stage(256.0, 128, 128, busy(ctas, at_once)) + meet + 6300.0 + 3200.0 / splits));
+        offer({splits, 0, 0}, waves(ctas, at_once) * (part * stage(256.0, 128, 128, busy(ctas, at_once)) + meet + 6300.0 + 0.86 * epilogue / splits));
     }
     if (o->max_pair_splits > 0 && n_k >= LPS_SPLITS && p.out_dtype != LF_F32) {
         const double part = (double)((n_k + LPS_SPLITS - 1) / LPS_SPLITS), meet = 2000.0 + 65536.0 * rows / 14.0;
         const long long tiles = m256 * n256;
         offer({-LPS_SPLITS, 0, 0}, waves(tiles, o->max_pair_splits) *
-              (part * stage(512.0, 128, 128, 2.0 * LPS_SPLITS * busy(tiles, o->max_pair_splits)) + meet + 11500.0));
+              (part * stage(512.0, 128, 128, 2.0 * LPS_SPLITS * busy(tiles, o->max_pair_splits)) + meet + 9600.0 + 0.5 * epilogue));
     }
-    // epilogue of 128 rows x 256 columns: as it is, an activation, 8-bit values one way or the other
-    const double epilogue = p.q ? 10000.0 : p.prod == LF_PROD_FORWARD && p.act != LF_ACT_NONE ? 7500.0 : 3700.0;
     if (o->max_pairs > 0) {
         for (int width = 256; width >= (p.prod == LF_PROD_FORWARD ? 160 : 256); width -= 32) {
             const long long n = (p.N + width - 1) / width, t256 = m256 * n, t512 = m512 * n;
             const double products = n_k * stage(2.0 * width, 128, width / 2, 2.0 * busy(t256, o->max_pairs));
-            offer({0, LT_256x256, width}, waves(t256, o->max_pairs) * ((products > epilogue ? products : epilogue) + 600.0) + 14000.0);
+            offer({0, LT_256x256, width}, products + 600.0 + (waves(t256, o->max_pairs) - 1.0) * ((products > epilogue ? products : epilogue) + 600.0) + 10300.0 + epilogue);
             if (p.out_dtype != LF_F32)
                 offer({0, LT_512x256, width}, waves(t512, o->max_pairs) *
                       (n_k * stage(4.0 * width, 256, width / 2, 2.0 * busy(t512, o->max_pairs)) + 4300.0 + epilogue) + 14000.0);

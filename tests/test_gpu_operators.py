@@ -126,6 +126,17 @@ def test_linear_pairs(ops, M, K, N, dtype, act):
     _linear(ops, M, K, N, dtype, act, form=lf.LF_FORM_PAIRS)
 
 
+# tiles of 160, 192 and 224 columns, 256 and 512 rows
+@pytest.mark.parametrize("M,K,N,dtype,act,ckpt", [
+    (409, 72, 4760, BF16, R.GELU, False), (1036, 200, 2096, F16, R.SILU, True), (312, 64, 6384, BF16, R.NONE, False), (273, 248, 6368, BF16, R.NONE, True),
+    (268, 72, 7424, F16, R.TANH, False), (262, 200, 7432, BF16, R.GELU, True), (2026, 64, 2432, BF16, R.SIGMOID, False), (814, 64, 5440, F16, R.NONE, True),
+    (1682, 64, 2912, BF16, R.RELU, False), (641, 64, 6776, BF16, R.GELU, True), (1062, 64, 4808, F16, R.GELU, False), (591, 64, 7592, BF16, R.NONE, True),
+    (408, 1160, 12728, BF16, R.SILU, True), (1453, 12328, 1960, BF16, R.GELU, False)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_linear_narrow_pair_tiles(ops, M, K, N, dtype, act, ckpt, residual):
+    _linear(ops, M, K, N, dtype, act, residual=residual, ckpt=ckpt, ld_extra=8 if residual else 0, form=lf.LF_FORM_PAIRS)
+
+
 @pytest.mark.parametrize("M,K,N,dtype,act", [(512, 4096, 3976, BF16, R.GELU), (400, 4104, 4096, F16, R.NONE), (1900, 4096, 1000, BF16, R.SIGMOID),
                                              (2048, 8200, 1024, F16, R.RELU)])
 def test_linear_split_pairs(ops, M, K, N, dtype, act):
