@@ -49,20 +49,30 @@ constexpr int LF_OPS_COUNTERS = LF_OPS_MAX_WIDTH / 256;      // one per 256 colu
 __device__ __forceinline__ void lf_grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void lf_grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// in clusters of `cluster` blocks
 template <typename... P, typename... A>
-cudaError_t lf_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args)
+cudaError_t lf_launch_clusters(void (*kernel)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, A... args)
 {
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+template <typename... P, typename... A>
+cudaError_t lf_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args)
+{
+    return lf_launch_clusters(kernel, grid, threads, smem, 1, s, args...);
 }
 #endif
 

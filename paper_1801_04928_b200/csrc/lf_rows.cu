@@ -3,6 +3,7 @@
 // by memory once there are rows enough; a lane holds 8 or 16 consecutive columns (one 128- or 256-bit access
 // in 16 bits), the lanes of an 8-bit scale group are neighbours.  A few rows cost a launch, 2.2 to 2.5 us.
 #include "lf_ops_internal.h"
+#include "lf_ptx.cuh"
 #include "lf_rows.cuh"
 
 namespace {
@@ -117,8 +118,12 @@ __device__ __forceinline__ void cp_async16(unsigned dst, const void* src)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-template <typename T, int TPR, int VPT, int GROUPS>
-__global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms_norm_backward_args a, float* partial, int depth)
+// ONE: the grid is one cluster, which adds the gain's gradient through distributed shared memory (`sums` is the gradient then,
+// else the partial rows): a launch instead of two.  Up to eight blocks and 4096 columns: one row of 4096 and 64 of 248 3.6 us
+// instead of 5.7, 8 of 2048 4.5 instead of 5.9; wider rows gain nothing (8 of 8192: 6.2 against 5.7, 6 of 14432: 10.6, 10.9).
+constexpr int NORM_CLUSTER = 8;
+template <typename T, int TPR, int VPT, int GROUPS, bool ONE>
+__global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms_norm_backward_args a, float* sums, int depth)
 {
     extern __shared__ __align__(16) unsigned char ring[];      // [depth][tensor][VPT][thread] pieces of eight elements
     __shared__ float2 red[2][GROUPS][TPR / 32];
@@ -232,9 +237,10 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     lf_grid_release();
-    if (partial) {
+    if (sums) {
+        float* mine = reinterpret_cast<float*>(ring);           // (free soon; it holds at least eight floats per thread and vector)
         if (GROUPS > 1) {
-            // add the groups' sums in group order (the ring is free; it holds at least eight floats per thread and vector)
+            // add the groups' sums in group order
             float2* all = reinterpret_cast<float2*>(ring);
             __syncthreads();
 #pragma unroll
@@ -242,22 +248,44 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
 #pragma unroll
                 for (int k = 0; k < 4; ++k) all[(size_t)(j * 4 + k) * THREADS + threadIdx.x] = dg[j][k];
             __syncthreads();
-            if (g > 0) return;
+            if (!ONE && g > 0) return;
 #pragma unroll
             for (int j = 0; j < VPT; ++j)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int o = 1; o < GROUPS; ++o) dg[j][k] = add2(dg[j][k], all[(size_t)(j * 4 + k) * THREADS + o * TPR + t]);
+                    for (int o = 1; o < GROUPS; ++o)
+                        if (!ONE || g == 0) dg[j][k] = add2(dg[j][k], all[(size_t)(j * 4 + k) * THREADS + o * TPR + t]);
         }
+        if (ONE) __syncthreads();
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int i = j * TPR + t;
-            if (i < nv) {
-                float4* to = reinterpret_cast<float4*>(partial + (size_t)blockIdx.x * a.n + 8 * i);
+            if (i < nv && (!ONE || g == 0)) {
+                float4* to = reinterpret_cast<float4*>((ONE ? mine : sums + (size_t)blockIdx.x * a.n) + 8 * i);
                 to[0] = make_float4(dg[j][0].x, dg[j][0].y, dg[j][1].x, dg[j][1].y);
                 to[1] = make_float4(dg[j][2].x, dg[j][2].y, dg[j][3].x, dg[j][3].y);
             }
+        }
+        if (ONE) {
+            // every block adds the blocks' sums of its share of the columns, in block order
+            __syncwarp();
+            lfptx::cluster_sync_all();
+            const unsigned from = lfptx::smem_u32(mine);
+            for (int v = (int)blockIdx.x * THREADS + (int)threadIdx.x; v < a.n / 4; v += (int)gridDim.x * THREADS) {
+                float4 p[NORM_CLUSTER];
+#pragma unroll
+                for (unsigned c = 0; c < NORM_CLUSTER; ++c)
+                    if (c < gridDim.x)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                     : "=f"(p[c].x), "=f"(p[c].y), "=f"(p[c].z), "=f"(p[c].w) : "r"(lfptx::map_to_cta(from, c) + 16u * (unsigned)v) : "memory");
+#pragma unroll
+                for (unsigned c = 1; c < NORM_CLUSTER; ++c)
+                    if (c < gridDim.x) { p[0].x += p[c].x; p[0].y += p[c].y; p[0].z += p[c].z; p[0].w += p[c].w; }
+                *reinterpret_cast<float4*>(sums + 4 * v) = p[0];
+            }
+            __syncwarp();
+            lfptx::cluster_sync_all();                          // nobody leaves while its sums are being read
         }
     }
 }
@@ -540,14 +568,25 @@ struct norm_backward_go {
     static cudaError_t go(const lf_rms_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* grid_out)
     {
         constexpr int GROUPS = TPR >= 256 ? 1 : 256 / TPR;
-        const auto kernel = k_rms_norm_backward<T, TPR, VPT, GROUPS>;
         const size_t slot = (size_t)(a.dres ? 3 : 2) * VPT * TPR * GROUPS * 8 * sizeof(T), most = 110 * 1024;
         const long long blocks = ((long long)a.tokens + GROUPS - 1) / GROUPS;
-        const int at_most = 2 * sm_count < LF_OPS_PARTIAL_ROWS ? 2 * sm_count : LF_OPS_PARTIAL_ROWS;
-        const int grid = blocks < at_most ? (int)blocks : at_most;
         int depth = 4;
         while (depth > 1 && slot * depth > most) --depth;
         if (depth == 1 && slot * 2 <= 220 * 1024) depth = 2;       // one block per multiprocessor, two rows in flight
+        if constexpr (VPT == 1) {                                  // (few rows of up to 4096 columns)
+            if (a.dgain && blocks <= NORM_CLUSTER) {
+                const auto kernel = k_rms_norm_backward<T, TPR, VPT, GROUPS, true>;
+                cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)slot);
+                if (e != cudaSuccess) return e;
+                int grid = 1;
+                while (grid < blocks) grid *= 2;
+                *grid_out = 0;
+                return lf_launch_clusters(kernel, dim3(grid), TPR * GROUPS, slot, grid, s, a, a.dgain, 1);      // a row each: a ring of one
+            }
+        }
+        const auto kernel = k_rms_norm_backward<T, TPR, VPT, GROUPS, false>;
+        const int at_most = 2 * sm_count < LF_OPS_PARTIAL_ROWS ? 2 * sm_count : LF_OPS_PARTIAL_ROWS;
+        const int grid = blocks < at_most ? (int)blocks : at_most;
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(slot * depth));
         if (e != cudaSuccess) return e;
         *grid_out = grid;
@@ -580,7 +619,7 @@ cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* par
     else if (a.dtype == LF_BF16) e = pick_row_shape<norm_backward_go, __nv_bfloat16>(a.n, many, a, partial, sm_count, s, &grid);
     else e = pick_row_shape<norm_backward_go, __half>(a.n, many, a, partial, sm_count, s, &grid);
     *launches = 1;
-    if (e == cudaSuccess && a.dgain) {
+    if (e == cudaSuccess && a.dgain && grid > 0) {
         e = sum_rows(partial, grid, a.n, a.dgain, s);
         *launches = 2;
     }

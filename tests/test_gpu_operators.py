@@ -425,6 +425,15 @@ def test_norm_backward_options_and_strides(ops, dres, dgain, ld):
         _norm_backward(ops, M, n, dtype, dres, dgain, ld)
 
 
+# one cluster of up to eight blocks, with one to eight rows each
+@pytest.mark.parametrize("M,n", [(1, 4096), (2, 8), (3, 264), (5, 4088), (8, 2048), (8, 4096), (11, 520), (16, 1024), (64, 248)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dres", [False, True])
+def test_norm_backward_of_few_rows_is_one_launch(ops, M, n, dtype, dres):
+    _norm_backward(ops, M, n, dtype, dres)
+    assert ops.stats()["launches"] == 1
+
+
 def test_norm_backward_against_central_differences(ops):
     g = _gen(11)
     h, dy, gain = _rand(g, 3, 40), _rand(g, 3, 40), 1 + _rand(g, 40, std=0.2)
