@@ -310,6 +310,7 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
             for (int g = 0; g < 4; ++g) {
                 float z[8];
                 dequantize8(make_uint2(now.q[2 * g], now.q[2 * g + 1]), now.s, z);
+                prime_range<8>(z, now.s);
                 prime_all<true, 8, KIND>(v + 8 * g, z);
             }
         }
@@ -759,8 +760,10 @@ __device__ __forceinline__ void ls_rows(const LtParams& P, const ls_share& e, ls
         if (PROD == LF_PROD_GRAD_X && KIND != LF_ACT_NONE) {
             float z[4 * NK];
 #pragma unroll
-            for (int k = 0; k < NK; ++k)
+            for (int k = 0; k < NK; ++k) {
                 from_e4m3x4(mine.q[k], scale(mine.s[k]), z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]);
+                prime_range<4>(z + 4 * k, mine.s[k]);
+            }
             prime_all<true, 4 * NK, KIND>(v, z);
         }
         OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;

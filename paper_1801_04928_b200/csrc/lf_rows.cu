@@ -459,6 +459,7 @@ __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsign
             if (GRAD) {
                 float d[W];
                 dv[u].get(d);
+                prime_range<W>(v, sv[u]);
                 prime_all<FAST, W, KIND>(d, v);
                 o.set(d);
             } else {

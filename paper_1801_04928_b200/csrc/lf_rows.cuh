@@ -207,6 +207,7 @@ __device__ __forceinline__ float2 act2(float2 z)
     if (KIND == LF_ACT_GELU) return mul2(z, sigmoid_of<FAST>(z, mul2(z, z), true));
     return z;
 }
+// |z| <= 2^37 or NaN (prime_range): GELU's cubic is finite there
 template <bool FAST, int KIND>
 __device__ __forceinline__ float2 act_prime2(float2 z)
 {
@@ -330,6 +331,16 @@ __device__ __forceinline__ void dequantize8(uint2 q, unsigned byte, float (&v)[8
     const float s = scale(byte);
     from_e4m3x4(q.x, s, v[0], v[1], v[2], v[3]);
     from_e4m3x4(q.y, s, v[4], v[5], v[6], v[7]);
+}
+// Values that sigma' is taken at: beyond 2^37 it is 0 or 1 to the last bit for every activation, and a finite z a (1 - a) g'(z)
+// needs |z| < 1e13 for GELU.  Up to e = 28 no value is beyond 448 * 2^28 < 2^37.
+template <int NE>
+__device__ __forceinline__ void prime_range(float* z, unsigned byte)
+{
+    if (byte > 127u + 28u) {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) z[i] = clamp_keep_nan(z[i], 137438953472.0f);
+    }
 }
 
 }  // namespace lfrow

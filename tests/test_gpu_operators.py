@@ -530,6 +530,47 @@ def test_activation_and_derivative_from_eight_bits(ops, act, dtype):
         R.check("dz", dz.t, ref, R.rounded(ref, dtype, f * dy.to(R.D).abs() * (1 + v.abs()) * (2 if act in (R.TANH, R.GELU) else 1)))
 
 
+# every magnitude of which the 8-bit form is kept: sigma is 0, +-1 or its argument there and sigma' 0 or 1, all of them exactly
+LARGE = (1e10, 1e11, 3e11, 1e13, 2e13, 1e14, 1e19, 2e19, 1e20, 1e30, 3.4e38)
+
+
+def _large(M, n):
+    v = torch.tensor(LARGE, device="cuda").repeat_interleave(2)[torch.arange(M, device="cuda") % (2 * len(LARGE))]
+    sign = 1 - 2 * ((torch.arange(n, device="cuda")[None, :] + torch.arange(M, device="cuda")[:, None]) % 2)
+    q, s = R.pack8(v[:, None] * sign)
+    assert 247 in s                            # 3.4e38 is kept as 256 * 2^120, beyond fp32
+    up = sign > 0
+    return q, s, up, R.unpack8(q, s)
+
+
+@pytest.mark.parametrize("act", [R.NONE, R.SILU, R.GELU, R.SIGMOID, R.TANH, R.RELU])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_derivative_at_the_largest_values(ops, act, dtype):
+    for M, n in ((22, 40), (44, 64)):
+        q, s, up, _ = _large(M, n)
+        dy, dz = _rand(_gen(act), M, n, dtype=dtype), torch.empty(M, n, dtype=dtype, device="cuda")
+        ops.act_backward(dy, q, s, dz, act=act)
+        ops.sync()
+        slope = torch.ones_like(dy) if act == R.NONE else torch.zeros_like(dy) if act in (R.TANH, R.SIGMOID) else up.to(dtype)
+        assert torch.equal(dz, dy * slope)
+
+
+@pytest.mark.parametrize("act", [R.SILU, R.GELU, R.SIGMOID, R.TANH, R.RELU])
+@pytest.mark.parametrize("M,K,N,form", [(44, 136, 72, lf.LF_FORM_SPLIT), (70, 136, 4096, lf.LF_FORM_SPLIT), (2049, 1288, 1800, lf.LF_FORM_PAIRS),
+                                        (500, 4000, 4096, lf.LF_FORM_SPLIT_PAIRS)])
+def test_gradient_through_the_derivative_at_the_largest_values(ops, act, M, K, N, form):
+    q, s, up, _ = _large(M, K)
+    g = _gen(M)
+    dz, w = _rand(g, M, N, dtype=BF16), _rand(g, N, K, std=N ** -0.5, dtype=BF16)
+    dx = torch.empty(M, K, dtype=BF16, device="cuda")
+    ops.linear_grad_x(dz, w, dx, q=q, s=s, act=act)
+    assert ops.stats()["form"] == form
+    ops.sync()
+    ref = dz.to(R.D) @ w.to(R.D)
+    ref = torch.where(up, ref, 0 * ref) if act not in (R.TANH, R.SIGMOID) else 0 * ref
+    R.check("dx", dx, ref, R.rounded(ref, BF16, torch.where(ref != 0, R.product_err(dz.to(R.D), w.to(R.D)), 0 * ref)))
+
+
 # ---- empty inputs, large offsets, streams, refusals, waits ----------------------------------------------
 
 def test_no_tokens(ops):
