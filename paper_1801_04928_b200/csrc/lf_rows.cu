@@ -463,8 +463,9 @@ __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsign
                 prime_all<FAST, W, KIND>(d, v);
                 o.set(d);
             } else {
+                act_range<W>(v, sv[u]);
                 act_all<FAST, W, KIND>(v);
-                if (sv[u] >= overflow_byte(T())) {       // (no activation leaves the range its argument is in)
+                if (sv[u] >= overflow_byte(T())) {       // (no activation of a finite value leaves the range that value is in)
 #pragma unroll
                     for (int k = 0; k < W; ++k) v[k] = clamp_keep_nan(v[k], max_finite(T()));
                 }

@@ -332,6 +332,18 @@ __device__ __forceinline__ void dequantize8(uint2 q, unsigned byte, float (&v)[8
     from_e4m3x4(q.x, s, v[0], v[1], v[2], v[3]);
     from_e4m3x4(q.y, s, v[4], v[5], v[6], v[7]);
 }
+// The ends of the range, where products of fp32 numbers overflow although sigma and sigma' are finite.  Both look at
+// the group's scale byte first, which settles it for all but a few groups.
+// Values that sigma is applied to: with e = 120 the largest e4m3 numbers stand for 2^128 and more; they
+// become the largest fp32 number, so that SiLU and GELU of the negative ones are 0 and not -infinity * 0.
+template <int NE>
+__device__ __forceinline__ void act_range(float* v, unsigned byte)
+{
+    if (byte >= 127u + 120u) {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) v[i] = clamp_keep_nan(v[i], 3.402823466e38f);
+    }
+}
 // Values that sigma' is taken at: beyond 2^37 it is 0 or 1 to the last bit for every activation, and a finite z a (1 - a) g'(z)
 // needs |z| < 1e13 for GELU.  Up to e = 28 no value is beyond 448 * 2^28 < 2^37.
 template <int NE>

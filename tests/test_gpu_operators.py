@@ -545,6 +545,21 @@ def _large(M, n):
 
 @pytest.mark.parametrize("act", [R.NONE, R.SILU, R.GELU, R.SIGMOID, R.TANH, R.RELU])
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_activation_of_the_largest_values(ops, act, dtype):
+    for M, n in ((22, 40), (44, 64)):
+        q, s, up, v = _large(M, n)
+        big = float(torch.finfo(dtype).max)
+        v = v.clamp(-big, big).to(dtype)
+        a = torch.empty_like(v)
+        ops.unpack8(q, s, a, act=act)
+        ops.sync()
+        low = {R.NONE: v, R.TANH: -torch.ones_like(v)}.get(act, torch.zeros_like(v))
+        high = torch.ones_like(v) if act in (R.TANH, R.SIGMOID) else v
+        assert torch.equal(a, torch.where(up, high, low))
+
+
+@pytest.mark.parametrize("act", [R.NONE, R.SILU, R.GELU, R.SIGMOID, R.TANH, R.RELU])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
 def test_derivative_at_the_largest_values(ops, act, dtype):
     for M, n in ((22, 40), (44, 64)):
         q, s, up, _ = _large(M, n)
