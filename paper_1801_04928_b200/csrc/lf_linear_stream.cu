@@ -17,6 +17,10 @@ namespace {
 using namespace lfrow;
 
 constexpr int SR_ROWS = 32, SR_DEPTH = 4;
+// The products add into their accumulator by truncation, 1.0e-7 of a sum of one sign per instruction: an accumulator takes
+// 512 steps, 1024 instructions, and the fills are added with round-to-nearest.  (LONG: more than one fill, contractions
+// beyond 16384 per warp; over 2^20 terms f16 results were 4.2e-4 and 5.6e-4 short without.)
+constexpr int SR_FILL = 512;
 
 template <typename T>
 __device__ __forceinline__ void mma16816(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1, T);
@@ -41,7 +45,7 @@ __device__ __forceinline__ void copy16(unsigned dst, const void* src, bool valid
 }
 
 // TT: blocks of eight tokens (1 or 2)
-template <typename T, int TT, int WARPS>
+template <typename T, int TT, int WARPS, bool LONG>
 __global__ void __launch_bounds__(WARPS * 32, 1) k_linear_stream(const lf_product p, int rows)
 {
     // [tile parity][warp][token][column]: 33 words a row keep the lanes of a fragment on different banks; before
@@ -96,37 +100,53 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_linear_stream(const lf_produc
     for (int d = 0; d < SR_DEPTH - 1; ++d) fetch(d);
     int parity = 0, slot = 0;
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, parity ^= 1) {
-        float acc[2][TT][4];
+        float sum[2][TT][4];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int j = 0; j < TT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.f;
-        for (int c = c0; c < c1; ++c) {
-            fetch(slot == 0 ? SR_DEPTH - 1 : slot - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(SR_DEPTH - 1) : "memory");
-            const unsigned char* from = sr_raw + (size_t)(slot * PIECES) * (THREADS * 16) + threadIdx.x * 16;
-            uint4 a[4], b[TT];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const uint4*>(from + r * (THREADS * 16));
-#pragma unroll
-            for (int j = 0; j < TT; ++j) b[j] = *reinterpret_cast<const uint4*>(from + (4 + j) * (THREADS * 16));
+                for (int i = 0; i < 4; ++i) sum[m][j][i] = 0.f;
+        int c = c0;
+        do {
+            float acc[2][TT][4];
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int j = 0; j < TT; ++j) {
-                    mma16816(acc[m][j], a[2 * m].x, a[2 * m + 1].x, a[2 * m].y, a[2 * m + 1].y, b[j].x, b[j].y, T());
-                    mma16816(acc[m][j], a[2 * m].z, a[2 * m + 1].z, a[2 * m].w, a[2 * m + 1].w, b[j].z, b[j].w, T());
-                }
-            if (++slot == SR_DEPTH) slot = 0;
-        }
+                for (int j = 0; j < TT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.f;
+            for (const int to = LONG ? min(c + SR_FILL, c1) : c1; c < to; ++c) {
+                fetch(slot == 0 ? SR_DEPTH - 1 : slot - 1);
+                asm volatile("cp.async.wait_group %0;" ::"n"(SR_DEPTH - 1) : "memory");
+                const unsigned char* from = sr_raw + (size_t)(slot * PIECES) * (THREADS * 16) + threadIdx.x * 16;
+                uint4 a[4], b[TT];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const uint4*>(from + r * (THREADS * 16));
+#pragma unroll
+                for (int j = 0; j < TT; ++j) b[j] = *reinterpret_cast<const uint4*>(from + (4 + j) * (THREADS * 16));
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int j = 0; j < TT; ++j) {
+                        mma16816(acc[m][j], a[2 * m].x, a[2 * m + 1].x, a[2 * m].y, a[2 * m + 1].y, b[j].x, b[j].y, T());
+                        mma16816(acc[m][j], a[2 * m].z, a[2 * m + 1].z, a[2 * m].w, a[2 * m + 1].w, b[j].z, b[j].w, T());
+                    }
+                if (++slot == SR_DEPTH) slot = 0;
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < TT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[m][j][i] = LONG ? sum[m][j][i] + acc[m][j][i] : acc[m][j][i];
+        } while (LONG && c < c1);
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int j = 0; j < TT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) red[parity][warp][j * 8 + 2 * t + (i & 1)][m * 16 + g + 8 * (i >> 1)] = acc[m][j][i];
+                for (int i = 0; i < 4; ++i) red[parity][warp][j * 8 + 2 * t + (i & 1)][m * 16 + g + 8 * (i >> 1)] = sum[m][j][i];
         __syncthreads();
         // a warp takes a token at a time, a lane a column; the sums are added in warp order
         const int col = tile * rows + lane;
@@ -166,18 +186,24 @@ cudaError_t stream_go(const lf_product& p, int sm_count, cudaStream_t s)
         if (rows < 8) rows = 8;              // a load covers eight rows
     }
     const int tiles = (p.N + rows - 1) / rows;
-    return lf_launch(k_linear_stream<T, TT, WARPS>, dim3((unsigned)(tiles < sm_count ? tiles : sm_count)), WARPS * 32, stream_smem<TT, WARPS>(), s, p, rows);
+    return lf_launch((p.K + 31) / 32 > WARPS * SR_FILL ? k_linear_stream<T, TT, WARPS, true> : k_linear_stream<T, TT, WARPS, false>, dim3((unsigned)(tiles < sm_count ? tiles : sm_count)), WARPS * 32, stream_smem<TT, WARPS>(), s, p, rows);
 }
 
 }  // namespace
 
+namespace {
+template <typename T, int TT, int WARPS>
+bool stream_ready()
+{
+    constexpr int bytes = (int)stream_smem<TT, WARPS>();
+    return cudaFuncSetAttribute(k_linear_stream<T, TT, WARPS, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess &&
+           cudaFuncSetAttribute(k_linear_stream<T, TT, WARPS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+}
+}  // namespace
+
 int lf_linear_stream_init()
 {
-    constexpr int one = (int)stream_smem<1, 16>(), two = (int)stream_smem<2, 12>();
-    return cudaFuncSetAttribute(k_linear_stream<__nv_bfloat16, 1, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, one) == cudaSuccess &&
-                   cudaFuncSetAttribute(k_linear_stream<__half, 1, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, one) == cudaSuccess &&
-                   cudaFuncSetAttribute(k_linear_stream<__nv_bfloat16, 2, 12>, cudaFuncAttributeMaxDynamicSharedMemorySize, two) == cudaSuccess &&
-                   cudaFuncSetAttribute(k_linear_stream<__half, 2, 12>, cudaFuncAttributeMaxDynamicSharedMemorySize, two) == cudaSuccess
+    return stream_ready<__nv_bfloat16, 1, 16>() && stream_ready<__half, 1, 16>() && stream_ready<__nv_bfloat16, 2, 12>() && stream_ready<__half, 2, 12>()
                ? LF_OK : LF_ECUDA;
 }
 

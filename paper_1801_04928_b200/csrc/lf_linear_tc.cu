@@ -21,10 +21,12 @@
 // which 2.3 is the launch).  Copies that reach several CTAs of a cluster at once would relieve the fetch; they are
 // left out because operands may be any memory that the caller's device can address.
 //
-// The tensor core adds into its accumulator by truncation.  Results that are rounded to 16 bits do not see
-// it; an fp32 weight gradient over thousands of tokens would (about 1e-5 relative after 512
-// instructions), so there an accumulator only takes CHUNK stages (32 instructions) and the chunks are added in
-// registers with round-to-nearest.
+// The tensor core adds into its accumulator by truncation: over terms of one sign 1.0e-7 of the sum per instruction
+// (16 terms), always towards zero.  An accumulator therefore takes a limited number of stages (lt_fill), and the fills are
+// added in registers with round-to-nearest: 8 stages, 3e-6, for an fp32 result, which a weight gradient over thousands of
+// tokens would show; 256 stages, 1.0e-4, for f16 and 1024, 4.1e-4, for bf16, less than half of the smallest half
+// unit of those types (2.4e-4, 2.0e-3).  Only contractions beyond 16384 and 65536 have more than one fill, in copies of
+// the kernels made for them.  (Without a limit f16 results were 4.2e-4 short over 65536 terms, 8.4e-4 over 2^20 in eight parts.)
 // All waits are bounded; on expiry the status word is raised and the launch drains and ends.
 #include "lf_ops_internal.h"
 #include "lf_ptx.cuh"
@@ -39,7 +41,6 @@ constexpr int LT_BLOCK_BYTES = 128 * LT_BK * 2;          // 16 KiB: 128 rows (or
 constexpr int LT_STAGE_BYTES = 2 * LT_BLOCK_BYTES;
 constexpr int LT_STAGES = 6;
 constexpr int LS_THREADS = 512;                          // split tiles: producer, issuer, eight warps that read the accumulator; all finish
-constexpr int LT_CHUNK = 8;                              // K stages per accumulator of an fp32 result
 constexpr int LP_RING_BYTES = LT_STAGES * LT_STAGE_BYTES;   // pairs: six stages of two blocks, or four of three
 constexpr int LP_EPI_BYTES = 8 * 4096;                   // pairs: 32 rows x 128 bytes per epilogue warp
 constexpr int LP_THREADS = 384;                          // pairs: a warpgroup with producer and issuer, two for the epilogue
@@ -54,6 +55,11 @@ constexpr int LD_PS = 260;                               // split pairs: padded 
 constexpr size_t LPS_SMEM = (size_t)LT_STAGES * LT_STAGE_BYTES + 1024 + 512;
 static_assert(128 * LD_PS * 4 <= LT_STAGES * LT_STAGE_BYTES, "the fp32 tile overlays the operand ring");
 constexpr size_t LS_SMEM = (size_t)LS_STAGES * LT_STAGE_BYTES + LS_TILE_BYTES + 1024 + 512;
+
+// K stages that one accumulator takes of a result of type OUT
+template <typename OUT> struct lt_fill { static constexpr int stages = 8; };
+template <> struct lt_fill<__half> { static constexpr int stages = 256; };
+template <> struct lt_fill<__nv_bfloat16> { static constexpr int stages = 1024; };
 
 struct LtParams {
     int M, N, K;
@@ -362,17 +368,18 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
 }
 
 // MB: 128-row blocks per CTA.  MB = 1: 256 x 256 tiles, the two accumulators alternate between tiles (or
-// chunks).  MB = 2: 512 x 256 tiles, one accumulator per block: a 64-deep stage takes 1024 cycles for twice the
+// fills).  MB = 2: 512 x 256 tiles, one accumulator per block: a 64-deep stage takes 1024 cycles for twice the
 // products of MB = 1's 568 (8192 x 4096 -> 16384 without an activation: 813 us in a loop, 841 with MB = 1).
 // Epilogue of 128 rows x 256 columns: 3700 cycles as it is, 7500 with GELU (half of it exponentials and
 // reciprocals), 10000 with 8-bit values.  8192 x 1024 -> 4096: 53 us, with GELU 63, with GELU, checkpoint and residual 90.
-template <int PROD, typename T, typename OUT, int MB>
+// FILL: K stages per accumulator (MB = 1), or 0: one accumulator takes the whole contraction.
+template <int PROD, typename T, typename OUT, int MB, int FILL>
 __global__ void __launch_bounds__(LP_THREADS, 1)
 k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const LtParams P)
 {
     constexpr bool A_MN = PROD == LF_PROD_GRAD_W, B_MN = PROD != LF_PROD_FORWARD;
-    constexpr bool PROMOTE = sizeof(OUT) == 4;
+    static_assert(MB == 1 || FILL == 0, "with 512 rows both accumulators belong to one tile");
     constexpr int STAGES = MB == 2 ? 4 : 6;
     constexpr unsigned STAGE_BYTES = (unsigned)(MB + 1) * LT_BLOCK_BYTES;
     constexpr int NC = 128;                                  // columns of an epilogue warp
@@ -387,7 +394,7 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
     const int n_tiles = P.tiles_m * P.tiles_n;
     const int n_k = (P.K + LT_BK - 1) / LT_BK;
-    const int chunk = PROMOTE ? LT_CHUNK : n_k;
+    const int fill = FILL ? FILL : n_k;
     // bytes that this CTA's loads of a stage bring
     const unsigned stage_bytes = MB * LT_BLOCK_BYTES + (unsigned)(B_MN ? (P.width > 128 ? 128 : 64) : P.width / 2) * (LT_BK * 2);
 
@@ -473,9 +480,9 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bool ok = true;
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
                 if (MB == 1) {
-                    for (int k0 = 0; k0 < n_k && ok; k0 += chunk, ++c) {
+                    for (int k0 = 0; k0 < n_k && ok; k0 += fill, ++c) {
                         if (!acc_wait(c)) { ok = false; break; }
-                        const int k1 = min(k0 + chunk, n_k);
+                        const int k1 = min(k0 + fill, n_k);
                         for (int ks = k0; ks < k1; ++ks, ++it) {
                             if (!full_wait(it)) { ok = false; break; }
                             products(it, 0, c & 1u, ks == k0);
@@ -550,10 +557,10 @@ k_product_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const bool operands = PROD != LF_PROD_GRAD_W && (P.q || P.add);
             if (operands) lp_fetch<PROD, T>(e.next, P, e, 0);   // on its way while the accumulator is waited for
             float acc[NC];
-            if (PROMOTE) {
+            if (FILL) {
 #pragma unroll
                 for (int i = 0; i < NC; ++i) acc[i] = 0.f;
-                for (int k0 = 0; k0 < n_k; k0 += chunk, ++c) {
+                for (int k0 = 0; k0 < n_k; k0 += fill, ++c) {
                     const unsigned ab = c & 1u;
                     if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) { ok = false; break; }
                     lfptx::tc_fence_after();
@@ -810,12 +817,11 @@ __device__ __forceinline__ ls_operands ls_first(const LtParams& P, const ls_shar
 // storing registers into the owners' shared memory, 16 bytes a row, 5000.)
 // The epilogue warps go through their code once before the accumulator is complete, with nothing to load or store:
 // a launch this short meets its instructions and parameters cold, 2400 cycles otherwise spent at its end.
-template <int PROD, typename T, typename OUT, int SPLITS>
+template <int PROD, typename T, typename OUT, int SPLITS, int FILL>
 __global__ void __launch_bounds__(LS_THREADS, 1)
 k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const LtParams P)
 {
     constexpr bool A_MN = PROD == LF_PROD_GRAD_W, B_MN = PROD != LF_PROD_FORWARD;
-    constexpr bool PROMOTE = sizeof(OUT) == 4;
     extern __shared__ unsigned char lt_smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lt_smem_raw) + 1023u) & ~(uintptr_t)1023u);
     float* tile = reinterpret_cast<float*>(ring + (size_t)LS_STAGES * LT_STAGE_BYTES);     // [128][LS_LD]
@@ -827,7 +833,7 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const int n_k_all = (P.K + LT_BK - 1) / LT_BK;
     const int ks0 = part * P.stages_per_split;
     const int n_k = max(0, min(P.stages_per_split, n_k_all - ks0));
-    const int chunk = PROMOTE ? LT_CHUNK : (n_k > 0 ? n_k : 1);
+    const int fill = FILL ? FILL : (n_k > 0 ? n_k : 1);
 
     auto load_stage = [&](int ks) {                    // one thread; stage ks of this part into its slot
         const unsigned st = (unsigned)ks % LS_STAGES, bar = lfptx::smem_u32(&sh->full[st]);
@@ -885,11 +891,11 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (lane == 0) {
             unsigned it = 0, c = 0;
             bool ok = true;
-            for (int k0 = 0; k0 < n_k && ok; k0 += chunk, ++c) {
+            for (int k0 = 0; k0 < n_k && ok; k0 += fill, ++c) {
                 const unsigned ab = c & 1u, ab_use = c >> 1;
                 if (ab_use > 0 && !lt_wait(lfptx::smem_u32(&sh->acc_empty[ab]), (ab_use - 1) & 1u, P, sh)) break;
                 lfptx::tc_fence_after();
-                const int k1 = min(k0 + chunk, n_k);
+                const int k1 = min(k0 + fill, n_k);
                 for (int ks = k0; ks < k1; ++ks, ++it) {
                     const unsigned st = it % LS_STAGES, use = it / LS_STAGES;
                     if (!lt_wait(lfptx::smem_u32(&sh->full[st]), use & 1u, P, sh)) { ok = false; break; }
@@ -921,7 +927,7 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 #pragma unroll
                 for (int i = 0; i < 64; ++i) acc[i] = 0.f;
                 unsigned c = 0;
-                for (int k0 = 0; k0 < n_k; k0 += chunk, ++c) {
+                for (int k0 = 0; k0 < n_k; k0 += fill, ++c) {
                     const unsigned ab = c & 1u;
                     if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) break;
                     lfptx::tc_fence_after();
@@ -967,7 +973,7 @@ k_product_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // For outputs with too few 256 x 256 tiles to fill the device and too many bytes of operands for 128 x 128 ones: a
 // stage costs a pair 568 cycles for four times the products of a 128 x 128 tile's 560.  The parts meet as
 // above (the fp32 tile of a CTA, 128 x 256, overlays its operand ring here: every product that reads
-// the ring is done when the accumulator is).  16-bit results only.  512 x 4096 x 4096: 19 us, against 27 with either
+// the ring is done when the accumulator is).  16-bit results only, and no more stages a part than one accumulator takes.  512 x 4096 x 4096: 19 us, against 27 with either
 // of the other forms.  (Four pairs to a cluster leave 60 multiprocessors idle -- 15 such clusters are resident -- and were
 // never ahead.)
 template <int PROD, typename T>
@@ -1148,25 +1154,37 @@ bool lt_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, int rows
 typedef void (*lt_kernel)(const CUtensorMap, const CUtensorMap, const LtParams);
 
 // Kernel of a product: index = prod * 2 + (f16); 6 and 7: grad_w with an fp32 result.  Pairs: tile 0 256 x 256,
-// 1 512 x 256 (16-bit results).
-constexpr int LT_KERNELS = 8;
-enum lt_tile { LT_256x256 = 0, LT_512x256 = 1, LT_TILES = 2 };
+// 1 512 x 256 (16-bit results), 2 256 x 256 with more than one fill of the accumulator.  Split tiles: splits = 1, 2, 4, 8, and
+// LT_LONG_SPLITS for eight parts of more than one fill.
+constexpr int LT_KERNELS = 8, LT_LONG_SPLITS = 16;
+enum lt_tile { LT_256x256 = 0, LT_512x256 = 1, LT_256x256_LONG = 2, LT_TILES = 3 };
 template <int PROD, typename T, typename OUT>
 lt_kernel lt_pair_of(int tile)
 {
-    if constexpr (sizeof(OUT) == 2)
-        if (tile == LT_512x256) return k_product_pair<PROD, T, OUT, 2>;
-    return tile == LT_256x256 ? k_product_pair<PROD, T, OUT, 1> : nullptr;
+    constexpr int FILL = lt_fill<OUT>::stages;
+    if constexpr (sizeof(OUT) == 2) {
+        if (tile == LT_512x256) return k_product_pair<PROD, T, OUT, 2, 0>;
+        if (tile == LT_256x256_LONG) return k_product_pair<PROD, T, OUT, 1, FILL>;
+        return k_product_pair<PROD, T, OUT, 1, 0>;
+    }
+    return tile == LT_256x256 ? k_product_pair<PROD, T, OUT, 1, FILL> : nullptr;
 }
 template <int PROD, typename T, typename OUT>
 lt_kernel lt_split_of(int splits)
 {
+    constexpr int FILL = lt_fill<OUT>::stages, SHORT = sizeof(OUT) == 2 ? 0 : FILL;
     switch (splits) {
-        case 1: return k_product_split<PROD, T, OUT, 1>;
-        case 2: return k_product_split<PROD, T, OUT, 2>;
-        case 4: return k_product_split<PROD, T, OUT, 4>;
-        default: return k_product_split<PROD, T, OUT, 8>;
+        case 1: return k_product_split<PROD, T, OUT, 1, SHORT>;
+        case 2: return k_product_split<PROD, T, OUT, 2, SHORT>;
+        case 4: return k_product_split<PROD, T, OUT, 4, SHORT>;
+        case 8: return k_product_split<PROD, T, OUT, 8, SHORT>;
+        default: return k_product_split<PROD, T, OUT, 8, FILL>;
     }
+}
+// stages that one accumulator takes without being added up
+int lt_one_fill(const lf_product& p)
+{
+    return p.out_dtype == LF_F32 ? 1 << 30 : p.out_dtype == LF_F16 ? lt_fill<__half>::stages : lt_fill<__nv_bfloat16>::stages;
 }
 lt_kernel lt_pick_pair(int i, int tile)
 {
@@ -1231,7 +1249,7 @@ int lf_product_tc_init(lf_ops* o)
     if (!lt_encode()) return LF_ECUDA;
     o->max_pairs = o->max_pair_splits = -1;
     for (int i = 0; i < LT_KERNELS; ++i) {
-        for (int splits = 1; splits <= 8; splits *= 2)
+        for (int splits = 1; splits <= LT_LONG_SPLITS; splits *= 2)
             if (cudaFuncSetAttribute(lt_pick_split(i, splits), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LS_SMEM) != cudaSuccess) return LF_ECUDA;
         auto resident = [&](lt_kernel f, int threads, int cluster, size_t smem, int* least) {
             if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
@@ -1286,14 +1304,16 @@ lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
     auto busy = [](long long units, int at_once) { return (double)(units < at_once ? units : at_once); };
     // epilogue of 128 rows x 256 columns: as it is, an activation, 8-bit values one way or the other
     const double epilogue = p.q ? 10000.0 : p.prod == LF_PROD_FORWARD && p.act != LF_ACT_NONE ? 7500.0 : 3700.0;
+    const int one_fill = lt_one_fill(p);
     for (int splits = 1; splits <= 8 && splits <= n_k; splits *= 2) {
         const double part = (double)((n_k + splits - 1) / splits);
+        if (part > one_fill && splits < 8) continue;
         const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
         const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
         const long long ctas = m128 * n128 * splits;
         offer({splits, 0, 0}, waves(ctas, at_once) * (part * stage(256.0, 128, 128, busy(ctas, at_once)) + meet + 6300.0 + 0.86 * epilogue / splits));
     }
-    if (o->max_pair_splits > 0 && n_k >= LPS_SPLITS && p.out_dtype != LF_F32) {
+    if (o->max_pair_splits > 0 && n_k >= LPS_SPLITS && n_k <= LPS_SPLITS * one_fill && p.out_dtype != LF_F32) {
         const double part = (double)((n_k + LPS_SPLITS - 1) / LPS_SPLITS), meet = 2000.0 + 65536.0 * rows / 14.0;
         const long long tiles = m256 * n256;
         offer({-LPS_SPLITS, 0, 0}, waves(tiles, o->max_pair_splits) *
@@ -1304,7 +1324,7 @@ lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
             const long long n = (p.N + width - 1) / width, t256 = m256 * n, t512 = m512 * n;
             const double products = n_k * stage(2.0 * width, 128, width / 2, 2.0 * busy(t256, o->max_pairs));
             offer({0, LT_256x256, width}, products + 600.0 + (waves(t256, o->max_pairs) - 1.0) * ((products > epilogue ? products : epilogue) + 600.0) + 10300.0 + epilogue);
-            if (p.out_dtype != LF_F32)
+            if (p.out_dtype != LF_F32 && n_k <= one_fill)
                 offer({0, LT_512x256, width}, waves(t512, o->max_pairs) *
                       (n_k * stage(4.0 * width, 256, width / 2, 2.0 * busy(t512, o->max_pairs)) + 4300.0 + epilogue) + 14000.0);
         }
@@ -1340,6 +1360,7 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
 
     const int n_k = (p.K + LT_BK - 1) / LT_BK;
     const lt_choice c = lt_choose(o, p, n_k);
+    const int one_fill = lt_one_fill(p);
     alignas(64) CUtensorMap map_a, map_b;
     const bool ok = (a_mn ? lt_map(&map_a, in_type, p.a, p.K, p.M, p.ld_a, 64, 64) : lt_map(&map_a, in_type, p.a, p.M, p.K, p.ld_a, 64, 128)) &&
                     (b_mn ? lt_map(&map_b, in_type, p.b, p.K, p.N, p.ld_b, 64, 64) : lt_map(&map_b, in_type, p.b, p.N, p.K, p.ld_b, 64, c.splits == 0 ? c.width / 2 : 128));
@@ -1363,7 +1384,7 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
         P.band = 2048 / bm;
         const int tiles = P.tiles_m * P.tiles_n, pairs = tiles < o->max_pairs ? tiles : o->max_pairs;
         lt_cluster_config(&cfg, at, 2 * pairs, LP_THREADS, 2, LP_SMEM, o->stream);
-        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_pair(kernel, c.tile), map_a, map_b, P));
+        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_pair(kernel, c.tile == LT_256x256 && n_k > one_fill ? LT_256x256_LONG : c.tile), map_a, map_b, P));
         o->stats.form = LF_FORM_PAIRS;
         o->stats.splits = 1;
     } else {
@@ -1371,7 +1392,7 @@ int lf_product_tc(lf_ops* o, const lf_product& p)
         P.idesc = idesc | (128u >> 3) << 17 | (128u >> 4) << 24;
         P.stages_per_split = (n_k + c.splits - 1) / c.splits;
         lt_cluster_config(&cfg, at, P.tiles_m * P.tiles_n * c.splits, LS_THREADS, c.splits, LS_SMEM, o->stream);
-        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_split(kernel, c.splits), map_a, map_b, P));
+        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, lt_pick_split(kernel, P.stages_per_split > one_fill ? LT_LONG_SPLITS : c.splits), map_a, map_b, P));
         o->stats.form = LF_FORM_SPLIT;
         o->stats.splits = c.splits;
     }

@@ -275,6 +275,61 @@ def test_weight_gradient_over_many_tokens_keeps_fp32(ops):
         R.check("gw", gw, ref, (32 + 16) * 2.0 ** -23 * ref)
 
 
+def _one_sign(g, rows, cols, dtype, scale=1.0, dim=0):
+    """Positive numbers, every row (or column) with a magnitude of its own, so that the sums spread over the roundings."""
+    v = 0.75 + 0.5 * torch.rand(rows, cols, device="cuda", generator=g)
+    v *= torch.exp2(torch.rand((rows, 1) if dim == 0 else (1, cols), device="cuda", generator=g)) * scale
+    return v.to(dtype)
+
+
+def _check_long(name, got, ref, terms):
+    """Sums of terms of one sign: an accumulator takes 1024 instructions for f16, 4096 for bf16, each truncated by a unit of 2^-23 at most;
+    fills, parts and warps are added with round-to-nearest.  The bound does not grow with the contraction as truncation over all
+    of it would, which the mean of the errors shows: the type's own rounding averages out (4 standard deviations of its mean)."""
+    dtype = got.dtype
+    rel = (1024 if dtype == F16 else 4096) * 2.0 ** -23 + (terms / 16384 + 16) * 2.0 ** -24
+    R.check(name, got, ref, R.rounded(ref, dtype, rel * ref))
+    mean = ((got.to(R.D) - ref) / ref).mean().item()
+    assert abs(mean) <= rel + 4 * R.HALF_ULP[dtype] / (3 * ref.numel()) ** 0.5, mean
+
+
+@pytest.mark.parametrize("M,K,N,dtype,form", [(4, 1 << 20, 512, F16, lf.LF_FORM_STREAM), (12, 1 << 20, 256, F16, lf.LF_FORM_STREAM),
+                                              (5, (1 << 18) + 8 * 77, 264, BF16, lf.LF_FORM_STREAM),
+                                              (32, 1 << 20, 128, F16, lf.LF_FORM_SPLIT), (40, (1 << 20) + 72, 136, BF16, lf.LF_FORM_SPLIT),
+                                              (2048, 1 << 16, 2048, F16, lf.LF_FORM_PAIRS), (2050, 66568, 2048, BF16, lf.LF_FORM_PAIRS)])
+def test_long_contractions_in_sixteen_bits(ops, M, K, N, dtype, form):
+    g = _gen(21)
+    x, w = _one_sign(g, M, K, dtype), _one_sign(g, N, K, dtype, 64 / K)
+    y = torch.empty(M, N, dtype=dtype, device="cuda")
+    ops.linear(x, w, y)
+    ops.sync()
+    assert ops.stats()["form"] == form
+    m = min(M, 64)
+    _check_long("y", y[-m:], x[-m:].to(R.D) @ w.to(R.D).t(), K)
+
+
+@pytest.mark.parametrize("M,K,N,form", [(64, 128, 1 << 20, lf.LF_FORM_SPLIT), (2048, 2048, 1 << 16, lf.LF_FORM_PAIRS)])
+def test_long_contractions_in_sixteen_bits_grad_x(ops, M, K, N, form):
+    g = _gen(22)
+    dz, w = _one_sign(g, M, N, F16), _one_sign(g, N, K, F16, 64 / N, dim=1)
+    dx = torch.empty(M, K, dtype=F16, device="cuda")
+    ops.linear_grad_x(dz, w, dx)
+    ops.sync()
+    assert ops.stats()["form"] == form
+    _check_long("dx", dx[:64], dz[:64].to(R.D) @ w.to(R.D), N)
+
+
+@pytest.mark.parametrize("M,K,N,form", [(1 << 20, 512, 512, lf.LF_FORM_SPLIT), (1 << 17, 2048, 2048, lf.LF_FORM_PAIRS)])
+def test_long_contractions_in_sixteen_bits_grad_w(ops, M, K, N, form):
+    g = _gen(23)
+    dz, x = _one_sign(g, M, N, F16, 64 / M, dim=1), _one_sign(g, M, K, F16, dim=1)
+    gw = torch.empty(N, K, dtype=F16, device="cuda")
+    ops.linear_grad_w(dz, gw, x=x)
+    ops.sync()
+    assert ops.stats()["form"] == form
+    _check_long("gw", gw[:64], dz[:, :64].to(R.D).t() @ x.to(R.D), M)
+
+
 @pytest.mark.parametrize("M,K,N", [(5, 16, 24), (40, 16, 24)])
 @pytest.mark.parametrize("act", [R.GELU, R.SILU, R.SIGMOID, R.TANH, R.NONE])
 def test_gradients_against_central_differences(ops, M, K, N, act):
