@@ -487,7 +487,7 @@ enum lf_linear_form {
  * Create a handle on the current CUDA device with `workspace_bytes` of device memory; calls on it
  * never allocate.  lf_ops_workspace(tokens, n_in) gives what any call with at most so many tokens
  * and input columns needs (of it, tokens * n_in * 2 bytes are for lf_linear_grad_w from 8 bits; the
- * rest is a fixed amount).  Work is enqueued on the handle's stream (lf_ops_set_stream; initially
+ * rest is a fixed amount).  lf_ops_create waits for the legacy default stream.  Work is enqueued on the handle's stream (lf_ops_set_stream; initially
  * the legacy default stream) with the handle's device current, and calls of one handle that may
  * overlap on the GPU must be ordered by the caller: they share the workspace.  Options:
  * LF_OPT_WAIT_BUDGET_US, and LF_OPT_WITHHOLD = 1 (test hook: a producer of the matrix products arms

@@ -713,6 +713,22 @@ def test_work_goes_to_the_stream_that_was_set():
         o.set_stream(None)
 
 
+def test_a_new_handle_is_ready_for_any_stream():
+    # what create queues (counters and the status word set to zero) is done when it returns, whatever was queued before it
+    st = torch.cuda.Stream()
+    g = _gen(15)
+    dz, x = _rand(g, 3000, 520, dtype=BF16), _rand(g, 3000, 64, dtype=BF16)
+    gw, gb = torch.empty(520, 64, device="cuda"), torch.empty(520, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)             # 0.1 s of the default stream
+    with lf.Operators(stream=st.cuda_stream) as o:
+        assert torch.cuda.default_stream().query()
+        o.linear_grad_w(dz, gw, gb=gb, x=x)
+        o.sync()
+    ref = dz.to(R.D).sum(0)
+    R.check("gb", gb, ref, (3000 / 16 + 16) * 2.0 ** -23 * dz.to(R.D).abs().sum(0))
+
+
 @pytest.mark.parametrize("M,K,N", [(200, 1024, 264), (2049, 512, 1288), (4096, 512, 4096), (512, 4096, 4096)])
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(M, K, N):
     g = _gen(14)
