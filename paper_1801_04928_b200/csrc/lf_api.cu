@@ -403,6 +403,8 @@ int lf_create_widths(lf_ctx** out, int L, const int* widths, int B, int k)
         ok = ok && cudaMemset(c->counters, 0, counter_bytes) == cudaSuccess;
         ok = ok && cudaMemset(c->sync_words, 0, c->sync_words_count * sizeof(unsigned)) == cudaSuccess;
         ok = ok && cudaMemset(c->status_dev, 0, sizeof(unsigned)) == cudaSuccess;
+        // (the memsets are only queued, on a stream that the context's own need not wait for)
+        ok = ok && cudaStreamSynchronize(nullptr) == cudaSuccess;
         *c->status_host = 0;
     }
     c->wstreams = new (std::nothrow) cudaStream_t[c->keff]();

@@ -152,3 +152,23 @@ def test_binding_refuses_buffers_of_the_wrong_size_or_type():
             assert e.value.status == lf.LF_EINVAL
         with pytest.raises(lf.LeapfrogError):
             ctx.backward_host(t["w"], t["z"], t["a"], t["y"], t["delta"], t["gw"], t["gb"])   # device tensors
+
+
+def test_a_new_context_is_ready_for_any_stream():
+    # what create queues (barrier counters and the status word set to zero) is done when it returns, whatever was
+    # queued before it
+    L, N, k = 6, 1024, 2
+    t = _buffers(L, N)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)             # 0.1 s of the default stream
+    with lf.Leapfrog(L, N, 1, k, stream=st.cuda_stream) as ctx:
+        assert torch.cuda.default_stream().query()
+        ctx.forward(t["w"], t["b"], t["x"], t["z"], t["a"])
+        ctx.backward(t["w"], t["z"], t["a"], t["y"], t["delta"], t["gw"], t["gb"])
+        ctx.sync()
+    first = {n: t[n].clone() for n in ("delta", "gw", "gb")}
+    with lf.Leapfrog(L, N, 1, k, stream=st.cuda_stream) as ctx:
+        ctx.backward(t["w"], t["z"], t["a"], t["y"], t["delta"], t["gw"], t["gb"])
+        ctx.sync()
+    assert all(torch.equal(first[n], t[n]) for n in first)
