@@ -4,11 +4,14 @@
 // the library's entry points arrive as addresses.
 //
 // Every function takes (entry point, handle, tensors and numbers ...) and returns None, or (status, text) for a
-// refusal (text says what was wrong) and for a status of the library (text is None).
+// refusal (text says what was wrong) and for a status of the library (text is None).  No C++ exception leaves them:
+// what a tensor throws when it is asked for a size, a stride or an address becomes a refusal.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <exception>
+#include <new>
 #include <string>
 
 #include "leapfrog.h"
@@ -39,7 +42,9 @@ struct call {
     const at::Tensor* tensor(PyObject* o, const char* name)
     {
         if (!THPVariable_Check(o)) { refuse(name, "not a tensor"); return nullptr; }
-        return &THPVariable_Unpack(o);
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.layout() != at::kStrided || t.is_nested() || !t.has_storage()) { refuse(name, "not a dense tensor with memory of its own"); return nullptr; }
+        return &t;
     }
     // enum lf_dtype of a tensor that sets the call's type; -1 after a refusal
     int type(const at::Tensor* t, const char* name)
@@ -292,7 +297,21 @@ PyObject* m_act_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_act_backward)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), dtype, act, m, n, yp, ldy, q, s, zp, ldz));
 }
 
-#define LF_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(m_##name)), METH_FASTCALL, nullptr}
+template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
+PyObject* entry(PyObject* self, PyObject* const* v, Py_ssize_t nargs) noexcept
+{
+    try {
+        return F(self, v, nargs);
+    } catch (const std::bad_alloc&) {
+        return PyErr_NoMemory();
+    } catch (const c10::Error& e) {
+        return PyErr_Occurred() ? nullptr : Py_BuildValue("(is)", (int)LF_EINVAL, e.what_without_backtrace());
+    } catch (const std::exception& e) {
+        return PyErr_Occurred() ? nullptr : Py_BuildValue("(is)", (int)LF_EINVAL, e.what());
+    }
+}
+
+#define LF_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(entry<m_##name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LF_METHOD(linear),    LF_METHOD(linear_grad_x), LF_METHOD(linear_grad_w), LF_METHOD(rms_norm), LF_METHOD(rms_norm_backward),
                          LF_METHOD(pack8),     LF_METHOD(unpack8),       LF_METHOD(act_backward),  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "tensor marshalling of the layer operators", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -796,3 +796,21 @@ def test_refusals(ops):
     refused(lf.LF_EINVAL, ops.set_option, lf.LF_OPT_VARIANT, 1)
     refused(lf.LF_EINVAL, lf.Operators, 1024)
     ops.sync()
+
+
+@pytest.mark.filterwarnings("ignore:Sparse CSR")
+def test_tensors_without_memory_of_their_own_are_refused(ops):
+    # inside vmap a tensor has no address; the process goes on and the message names the argument
+    x, q, s = torch.zeros(3, 4, 64, dtype=BF16, device="cuda"), torch.zeros(4, 64, dtype=torch.uint8, device="cuda"), torch.zeros(4, 2, dtype=torch.uint8, device="cuda")
+
+    def call(v):
+        ops.pack8(v, q, s)
+        return v
+
+    with pytest.raises(lf.LeapfrogError, match="argument x") as e:
+        torch.vmap(call)(x)
+    assert e.value.status == lf.LF_EINVAL
+    with pytest.raises(lf.LeapfrogError, match="argument x"):
+        ops.pack8(x[0].to_sparse_csr(), q, s)
+    ops.pack8(x[0], q, s)
+    ops.sync()

@@ -4,6 +4,8 @@ import ctypes
 import os
 import re
 import subprocess
+import sys
+import textwrap
 
 import pytest
 import torch
@@ -99,3 +101,38 @@ def test_reference_derivatives_by_differences_and_their_bounds(kind):
     fd = (R.act(z + h, kind) - R.act(z - h, kind)) / (2 * h)
     assert (d - fd).abs().max().item() < 1e-7
     assert d.abs().max().item() <= R.LIP1[kind]
+
+
+def _without_gpu(code):
+    """Run `code` in a process of its own, with `o` an Operators that has no handle: calls end at their checks of tensors."""
+    head = """
+        import torch, paper_1801_04928_b200 as lf
+        from paper_1801_04928_b200 import _marshal
+        o = object.__new__(lf.Operators)
+        o._h, o._a, o._m, o._device = None, 0, _marshal, 0
+        def refused(f, *a, **k):
+            try:
+                f(*a, **k)
+            except lf.LeapfrogError as e:
+                assert e.status == lf.LF_EINVAL, e
+                return str(e)
+            raise AssertionError("not refused")
+    """
+    r = subprocess.run([sys.executable, "-c", textwrap.dedent(head) + textwrap.dedent(code)], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, (r.returncode, r.stdout, r.stderr[-3000:])
+
+
+@pytest.mark.parametrize("make", ["m.to_sparse()", "m.to_sparse_csr()", "torch.nested.nested_tensor([m, m[:2]])",
+                                  "torch.nested.nested_tensor([m, m[:2]], layout=torch.jagged)", "m.to(torch.float32).to_mkldnn()"])
+def test_tensors_without_plain_memory_are_refused_and_do_not_end_the_process(make):
+    _without_gpu(f"""
+        import warnings
+        warnings.simplefilter("ignore")
+        m, byte = torch.ones(4, 8, dtype=torch.bfloat16), torch.zeros(4, 8, dtype=torch.uint8)
+        odd, gain = {make}, torch.ones(8)
+        calls = [(o.linear, odd, m, m), (o.linear, m, odd, m), (o.linear, m, m, odd), (o.linear_grad_x, odd, m, m), (o.linear_grad_x, m, odd, m),
+                 (o.linear_grad_w, odd, m), (o.linear_grad_w, m, odd), (o.rms_norm, odd, gain, m), (o.rms_norm_backward, m, odd, gain, m),
+                 (o.pack8, odd, byte, byte), (o.unpack8, byte, byte, odd), (o.act_backward, odd, byte, byte, m)]
+        for f, *a in calls:
+            assert "argument" in refused(f, *a)
+    """)
