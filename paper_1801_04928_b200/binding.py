@@ -72,7 +72,7 @@ lf_rms_norm_args = _struct("lf_rms_norm_args", ("i", "dtype tokens n"), ("f", "e
                            ("l", "ld_residual"), ("p", "gain h"), ("l", "ld_h"), ("p", "y"), ("l", "ld_y"), ("p", "q s"))
 lf_rms_norm_backward_args = _struct("lf_rms_norm_backward_args", ("i", "dtype tokens n"), ("f", "eps"), ("p", "dy"), ("l", "ld_dy"), ("p", "h"),
                                     ("l", "ld_h"), ("p", "gain dres"), ("l", "ld_dres"), ("p", "dh"), ("l", "ld_dh"), ("p", "dgain"))
-lf_ops_stats = _struct("lf_ops_stats", ("i", "sm_count launches form splits"), ("u", "device_status"), ("l", "workspace_bytes"))
+lf_ops_stats = _struct("lf_ops_stats", ("i", "sm_count launches form splits"), ("u", "device_status"), ("i", "device"), ("l", "workspace_bytes"))
 
 
 def _load() -> ctypes.CDLL:
@@ -439,7 +439,8 @@ class Operators:
     Matrices are 2-D, [tokens, width], with unit stride along a row; their rows may be further apart than
     the width (a slice of columns of a wider matrix).  Results go into the tensors that are passed in.
     Raises :class:`LeapfrogError` on any non-zero status and on tensors whose type, device, shape or
-    layout does not fit.  ``stream``: a cudaStream_t as an int; None is the legacy default stream.
+    layout does not fit: they are on the GPU that was current when the handle was made, and work is put there
+    whichever is current at the call.  ``stream``: a cudaStream_t as an int; None is the legacy default stream.
     The tensors are checked and turned into C arguments by the native module ``_marshal``.
     """
 
@@ -452,6 +453,7 @@ class Operators:
         from . import _marshal
         self._m = _marshal
         self._a = self._h.value
+        self._device = self.stats()["device"]
         if stream is not None:
             self.set_stream(stream)
 
@@ -481,49 +483,49 @@ class Operators:
 
     def linear(self, x, w, y, bias=None, residual=None, act: int = LF_ACT_NONE, q=None, s=None, _f=_entry("lf_linear")):
         """y = act(x w^T + bias) + residual; with q and s also z = x w^T + bias in 8 bits."""
-        failed = self._m.linear(_f, self._a, x, w, y, bias, residual, act, q, s)
+        failed = self._m.linear(_f, self._a, x, w, y, bias, residual, act, q, s, self._device)
         if failed is not None:
             self._raise("lf_linear", failed)
 
     def linear_grad_x(self, dz, w, dx, q=None, s=None, act: int = LF_ACT_NONE, add=None, _f=_entry("lf_linear_grad_x")):
         """dx = (dz w) * act'(z) + add, z [tokens, n_in] given in 8 bits by q and s."""
-        failed = self._m.linear_grad_x(_f, self._a, dz, w, dx, q, s, act, add)
+        failed = self._m.linear_grad_x(_f, self._a, dz, w, dx, q, s, act, add, self._device)
         if failed is not None:
             self._raise("lf_linear_grad_x", failed)
 
     def linear_grad_w(self, dz, gw, gb=None, x=None, q=None, s=None, act: int = LF_ACT_NONE, _f=_entry("lf_linear_grad_w")):
         """gw = dz^T x, gb = column sums of dz; x given, or act(z) from 8 bits.  gw: float32 or dz's type."""
-        failed = self._m.linear_grad_w(_f, self._a, dz, gw, gb, x, q, s, act)
+        failed = self._m.linear_grad_w(_f, self._a, dz, gw, gb, x, q, s, act, self._device)
         if failed is not None:
             self._raise("lf_linear_grad_w", failed)
 
     def rms_norm(self, x, gain, y=None, residual=None, h=None, q=None, s=None, eps: float = 1e-5, _f=_entry("lf_rms_norm")):
         """h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain, in x's type and / or in 8 bits (q, s)."""
-        failed = self._m.rms_norm(_f, self._a, x, gain, y, residual, h, q, s, eps)
+        failed = self._m.rms_norm(_f, self._a, x, gain, y, residual, h, q, s, eps, self._device)
         if failed is not None:
             self._raise("lf_rms_norm", failed)
 
     def rms_norm_backward(self, dy, h, gain, dh, dgain=None, dres=None, eps: float = 1e-5, _f=_entry("lf_rms_norm_backward")):
         """Gradient of y = h / sqrt(mean(h^2) + eps) * gain with respect to h (plus dres) and gain."""
-        failed = self._m.rms_norm_backward(_f, self._a, dy, h, gain, dh, dgain, dres, eps)
+        failed = self._m.rms_norm_backward(_f, self._a, dy, h, gain, dh, dgain, dres, eps, self._device)
         if failed is not None:
             self._raise("lf_rms_norm_backward", failed)
 
     def pack8(self, x, q, s, _f=_entry("lf_pack8")):
         """x [tokens, n] in 8 bits: q [tokens, n], s [tokens, ceil(n / 32)]."""
-        failed = self._m.pack8(_f, self._a, x, q, s)
+        failed = self._m.pack8(_f, self._a, x, q, s, self._device)
         if failed is not None:
             self._raise("lf_pack8", failed)
 
     def unpack8(self, q, s, x, act: int = LF_ACT_NONE, _f=_entry("lf_unpack8")):
         """x = act(value of q and s)."""
-        failed = self._m.unpack8(_f, self._a, q, s, x, act)
+        failed = self._m.unpack8(_f, self._a, q, s, x, act, self._device)
         if failed is not None:
             self._raise("lf_unpack8", failed)
 
     def act_backward(self, dy, q, s, dz, act: int = LF_ACT_NONE, _f=_entry("lf_act_backward")):
         """dz = dy * act'(value of q and s)."""
-        failed = self._m.act_backward(_f, self._a, dy, q, s, dz, act)
+        failed = self._m.act_backward(_f, self._a, dy, q, s, dz, act, self._device)
         if failed is not None:
             self._raise("lf_act_backward", failed)
 

@@ -21,7 +21,9 @@ namespace {
 constexpr long long ROWS_MOST = 0x7FFFFFFF;
 
 struct call {
+    const int device;                // the handle's: the last argument
     std::string problem;
+    explicit call(PyObject* d) : device((int)PyLong_AsLong(d)) {}
 
     bool refuse(const char* name, const std::string& what)
     {
@@ -39,6 +41,7 @@ struct call {
         s += t.device().str();
         return s;
     }
+    bool here(const at::Tensor& t) const { return t.is_cuda() && t.device().index() == device; }
     const at::Tensor* tensor(PyObject* o, const char* name)
     {
         if (!THPVariable_Check(o)) { refuse(name, "not a tensor"); return nullptr; }
@@ -76,8 +79,8 @@ struct call {
         if (o == Py_None) return true;
         const at::Tensor* t = tensor(o, name);
         if (!t) return false;
-        if (t->scalar_type() != st || !t->is_cuda() || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols)
-            return refuse(name, said(*t) + ", " + c10::toString(st) + " (" + std::to_string(rows) + ", " + std::to_string(cols) + ") on a CUDA device needed");
+        if (t->scalar_type() != st || !here(*t) || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols)
+            return refuse(name, said(*t) + ", " + c10::toString(st) + " (" + std::to_string(rows) + ", " + std::to_string(cols) + ") on cuda:" + std::to_string(device) + " needed");
         if (cols > 1 && t->stride(1) != 1) return refuse(name, said(*t) + " (unit stride along rows needed)");
         if (rows > 1) {
             if (t->stride(0) < cols) return refuse(name, said(*t) + " (rows overlap)");
@@ -97,8 +100,8 @@ struct call {
         if (o == Py_None) return true;
         const at::Tensor* t = tensor(o, name);
         if (!t) return false;
-        if (t->scalar_type() != st || !t->is_cuda() || t->numel() != n || !t->is_contiguous())
-            return refuse(name, said(*t) + ", " + std::to_string(n) + " contiguous elements of " + c10::toString(st) + " on a CUDA device needed");
+        if (t->scalar_type() != st || !here(*t) || t->numel() != n || !t->is_contiguous())
+            return refuse(name, said(*t) + ", " + std::to_string(n) + " contiguous elements of " + c10::toString(st) + " on cuda:" + std::to_string(device) + " needed");
         *p = t->const_data_ptr();
         return true;
     }
@@ -133,11 +136,11 @@ void* address(PyObject* o) { return PyLong_AsVoidPtr(o); }
     }
 #define LF_NUMBERS_OK if (PyErr_Occurred()) return nullptr
 
-// linear(f, ops, x, w, y, bias, residual, act, q, s)
+// linear(f, ops, x, w, y, bias, residual, act, q, s, device)
 PyObject* m_linear(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(10);
-    call c;
+    LF_EXPECT(11);
+    call c(v[10]);
     lf_linear_args a = {};
     const at::Tensor *x = c.tensor(v[2], "x"), *w = c.tensor(v[3], "w");
     int k = 0, wn = 0;
@@ -157,11 +160,11 @@ PyObject* m_linear(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_linear)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
 }
 
-// linear_grad_x(f, ops, dz, w, dx, q, s, act, add)
+// linear_grad_x(f, ops, dz, w, dx, q, s, act, add, device)
 PyObject* m_linear_grad_x(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(9);
-    call c;
+    LF_EXPECT(10);
+    call c(v[9]);
     lf_linear_grad_x_args a = {};
     const at::Tensor *dz = c.tensor(v[2], "dz"), *w = c.tensor(v[3], "w");
     int wn = 0;
@@ -179,11 +182,11 @@ PyObject* m_linear_grad_x(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_linear_grad_x)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
 }
 
-// linear_grad_w(f, ops, dz, gw, gb, x, q, s, act)
+// linear_grad_w(f, ops, dz, gw, gb, x, q, s, act, device)
 PyObject* m_linear_grad_w(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(9);
-    call c;
+    LF_EXPECT(10);
+    call c(v[9]);
     lf_linear_grad_w_args a = {};
     const at::Tensor *dz = c.tensor(v[2], "dz"), *gw = c.tensor(v[3], "gw");
     int wn = 0;
@@ -202,11 +205,11 @@ PyObject* m_linear_grad_w(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_linear_grad_w)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
 }
 
-// rms_norm(f, ops, x, gain, y, residual, h, q, s, eps)
+// rms_norm(f, ops, x, gain, y, residual, h, q, s, eps, device)
 PyObject* m_rms_norm(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(10);
-    call c;
+    LF_EXPECT(11);
+    call c(v[10]);
     lf_rms_norm_args a = {};
     const at::Tensor* x = c.tensor(v[2], "x");
     a.dtype = c.type(x, "x");
@@ -222,11 +225,11 @@ PyObject* m_rms_norm(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_rms_norm)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
 }
 
-// rms_norm_backward(f, ops, dy, h, gain, dh, dgain, dres, eps)
+// rms_norm_backward(f, ops, dy, h, gain, dh, dgain, dres, eps, device)
 PyObject* m_rms_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(9);
-    call c;
+    LF_EXPECT(10);
+    call c(v[9]);
     lf_rms_norm_backward_args a = {};
     const at::Tensor* h = c.tensor(v[3], "h");
     a.dtype = c.type(h, "h");
@@ -242,13 +245,14 @@ PyObject* m_rms_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_rms_norm_backward)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
 }
 
-// pack8(f, ops, x, q, s)
+// pack8(f, ops, x, q, s, device)
 PyObject* m_pack8(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(5);
-    call c;
+    LF_EXPECT(6);
+    call c(v[5]);
     const at::Tensor* x = c.tensor(v[2], "x");
     const int dtype = c.type(x, "x");
+    LF_NUMBERS_OK;
     int m, n;
     c.shape(x, "x", &m, &n);
     if (!c.problem.empty()) return c.refused();
@@ -259,11 +263,11 @@ PyObject* m_pack8(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_pack8)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), dtype, m, n, xp, ld, q, s));
 }
 
-// unpack8(f, ops, q, s, x, act)
+// unpack8(f, ops, q, s, x, act, device)
 PyObject* m_unpack8(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(6);
-    call c;
+    LF_EXPECT(7);
+    call c(v[6]);
     const at::Tensor* x = c.tensor(v[4], "x");
     const int dtype = c.type(x, "x"), act = (int)number(v[5]);
     LF_NUMBERS_OK;
@@ -277,11 +281,11 @@ PyObject* m_unpack8(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_unpack8)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), dtype, act, m, n, q, s, xp, ld));
 }
 
-// act_backward(f, ops, dy, q, s, dz, act)
+// act_backward(f, ops, dy, q, s, dz, act, device)
 PyObject* m_act_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
 {
-    LF_EXPECT(7);
-    call c;
+    LF_EXPECT(8);
+    call c(v[7]);
     const at::Tensor* dy = c.tensor(v[2], "dy");
     const int dtype = c.type(dy, "dy"), act = (int)number(v[6]);
     LF_NUMBERS_OK;

@@ -31,6 +31,20 @@ struct checker {
     int result() const { return null_ ? LF_ENULL : invalid ? LF_EINVAL : misaligned ? LF_EALIGN : LF_OK; }
 };
 
+// The handle's device, current while an entry point runs.
+struct on_device {
+    int before = -1;
+    cudaError_t error;
+    explicit on_device(const lf_ops* o)
+    {
+        int now = -1;
+        error = cudaGetDevice(&now);
+        if (error == cudaSuccess && now != o->device && (error = cudaSetDevice(o->device)) == cudaSuccess) before = now;
+    }
+    ~on_device() { if (before >= 0) cudaSetDevice(before); }
+};
+#define LF_OPS_DEVICE(o) const on_device on_device__(o); LF_OPS_TRY(o, on_device__.error)
+
 inline long long ld_or(long long l, int n) { return l ? l : n; }
 
 }  // namespace
@@ -75,6 +89,7 @@ int lf_ops_create(lf_ops** out, long long workspace_bytes)
     }
     *o->status_host = 0;
     o->stats.sm_count = o->sm_count;
+    o->stats.device = dev;
     o->stats.workspace_bytes = workspace_bytes;
     *out = o;
     return LF_OK;
@@ -115,6 +130,7 @@ int lf_ops_last_cuda_error(const lf_ops* o) { return o ? o->last_cuda_error : 0;
 int lf_ops_sync(lf_ops* o)
 {
     if (!o) return LF_ENULL;
+    LF_OPS_DEVICE(o);
     LF_OPS_TRY(o, cudaMemcpyAsync(o->status_host, o->status_dev, sizeof(unsigned), cudaMemcpyDeviceToHost, o->stream));
     LF_OPS_TRY(o, cudaStreamSynchronize(o->stream));
     o->stats.device_status = *o->status_host;
@@ -128,6 +144,7 @@ int lf_ops_sync(lf_ops* o)
 int lf_ops_destroy(lf_ops* o)
 {
     if (!o) return LF_ENULL;
+    const on_device there(o);
     cudaStreamSynchronize(o->stream);
     if (o->ws) cudaFree(o->ws);
     if (o->counters) cudaFree(o->counters);
@@ -145,6 +162,7 @@ int lf_linear(lf_ops* o, const lf_linear_args* a)
     c.matrix(a->x); c.require(a->w); c.matrix(a->y); c.optional(a->bias); c.optional(a->residual); c.both(a->q, a->s);
     c.ld(a->ld_x, a->n_in, a->dtype); c.ld(a->ld_residual, a->n_out, a->dtype); c.ld(a->ld_y, a->n_out, a->dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     if (a->tokens == 0) return LF_OK;
     lf_product p = {};
@@ -175,6 +193,7 @@ int lf_linear_grad_x(lf_ops* o, const lf_linear_grad_x_args* a)
     c.ok(a->q || c.empty || a->act == LF_ACT_NONE);   // sigma' needs the pre-activation
     c.ld(a->ld_dz, a->n_out, a->dtype); c.ld(a->ld_add, a->n_in, a->dtype); c.ld(a->ld_dx, a->n_in, a->dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     if (a->tokens == 0) return LF_OK;
     lf_product p = {};
@@ -200,6 +219,7 @@ int lf_linear_grad_w(lf_ops* o, const lf_linear_grad_w_args* a)
     c.ok(!a->x || a->act == LF_ACT_NONE);         // x is already an activation
     c.ld(a->ld_dz, a->n_out, a->dtype); c.ld(a->ld_x, a->n_in, a->dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     const size_t gw_bytes = (size_t)a->n_out * a->n_in * (a->gw_dtype == LF_F32 ? 4 : 2);
     if (a->tokens == 0) {
@@ -238,6 +258,7 @@ int lf_rms_norm(lf_ops* o, const lf_rms_norm_args* args)
     if (!a.y) c.matrix(a.q);
     c.ld(a.ld_x, a.n, a.dtype); c.ld(a.ld_residual, a.n, a.dtype); c.ld(a.ld_h, a.n, a.dtype); c.ld(a.ld_y, a.n, a.dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     if (a.tokens == 0) return LF_OK;
     a.ld_x = ld_or(a.ld_x, a.n); a.ld_residual = ld_or(a.ld_residual, a.n); a.ld_h = ld_or(a.ld_h, a.n); a.ld_y = ld_or(a.ld_y, a.n);
@@ -255,6 +276,7 @@ int lf_rms_norm_backward(lf_ops* o, const lf_rms_norm_backward_args* args)
     c.matrix(a.dy); c.matrix(a.h); c.require(a.gain); c.matrix(a.dh); c.optional(a.dres); c.optional(a.dgain);
     c.ld(a.ld_dy, a.n, a.dtype); c.ld(a.ld_h, a.n, a.dtype); c.ld(a.ld_dres, a.n, a.dtype); c.ld(a.ld_dh, a.n, a.dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     if (a.tokens == 0) {
         if (a.dgain) LF_OPS_TRY(o, cudaMemsetAsync(a.dgain, 0, (size_t)a.n * sizeof(float), o->stream));
@@ -272,6 +294,7 @@ int lf_pack8(lf_ops* o, int dtype, int tokens, int n, const void* x, long long l
     c.type(dtype); c.width(n); c.matrix(x); c.matrix(q); c.bytes(s);
     c.ld(ld_x, n, dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     if (tokens == 0) return LF_OK;
     LF_OPS_TRY(o, lfk_pack8(dtype, tokens, n, x, ld_or(ld_x, n), q, s, o->sm_count, o->stream));
@@ -287,6 +310,7 @@ int lf_unpack8(lf_ops* o, int dtype, int act, int tokens, int n, const unsigned 
     c.type(dtype); c.act(act); c.width(n); c.matrix(x); c.matrix(q); c.bytes(s);
     c.ld(ld_x, n, dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     if (tokens == 0) return LF_OK;
     LF_OPS_TRY(o, lfk_unpack8(dtype, act, tokens, n, q, s, x, ld_or(ld_x, n), o->sm_count, o->stream));
@@ -302,6 +326,7 @@ int lf_act_backward(lf_ops* o, int dtype, int act, int tokens, int n, const void
     c.type(dtype); c.act(act); c.width(n); c.matrix(dy); c.matrix(q); c.matrix(dz); c.bytes(s);
     c.ld(ld_dy, n, dtype); c.ld(ld_dz, n, dtype);
     if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
     o->stats.launches = 0;
     if (tokens == 0) return LF_OK;
     LF_OPS_TRY(o, lfk_act_backward(dtype, act, tokens, n, dy, ld_or(ld_dy, n), q, s, dz, ld_or(ld_dz, n), o->sm_count, o->stream));

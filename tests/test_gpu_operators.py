@@ -814,3 +814,19 @@ def test_tensors_without_memory_of_their_own_are_refused(ops):
         ops.pack8(x[0].to_sparse_csr(), q, s)
     ops.pack8(x[0], q, s)
     ops.sync()
+
+
+def test_tensors_of_another_device_are_refused():
+    with lf.Operators() as o:
+        assert o.stats()["device"] == torch.cuda.current_device()
+        x, w, y = (torch.zeros(r, c, dtype=BF16, device="cuda") for r, c in ((4, 64), (32, 64), (4, 32)))
+        gain, byte = torch.ones(64, device="cuda"), torch.zeros(4, 64, dtype=torch.uint8, device="cuda")
+        scales = torch.zeros(4, 2, dtype=torch.uint8, device="cuda")
+        o.linear(x, w, y)
+        o.sync()
+        o._device += 1                         # as if the handle were another GPU's
+        for f, *a in ((o.linear, x, w, y), (o.linear_grad_x, y, w, x), (o.linear_grad_w, y, w), (o.rms_norm, x, gain, x),
+                      (o.rms_norm_backward, x, x, gain, x), (o.pack8, x, byte, scales), (o.unpack8, byte, scales, x), (o.act_backward, x, byte, scales, x)):
+            with pytest.raises(lf.LeapfrogError, match=f"cuda:{o._device} needed") as e:
+                f(*a)
+            assert e.value.status == lf.LF_EINVAL
