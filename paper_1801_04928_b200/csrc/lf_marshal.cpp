@@ -10,6 +10,8 @@
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <limits.h>
+
 #include <exception>
 #include <new>
 #include <string>
@@ -118,6 +120,14 @@ struct call {
     {
         return flat(q, "q", (long long)rows * cols, at::kByte, qp) & flat(s, "s", (long long)rows * ((cols + 31) / 32), at::kByte, sp);
     }
+    // a number for an int of the library: one that is too large is refused, not cut
+    int number(PyObject* o, const char* name)
+    {
+        int beyond = 0;
+        const long n = PyLong_AsLongAndOverflow(o, &beyond);
+        if (beyond || n < INT_MIN || n > INT_MAX) { refuse(name, "out of range"); return 0; }
+        return (int)n;
+    }
     PyObject* answer(int rc)
     {
         if (rc == LF_OK) Py_RETURN_NONE;
@@ -126,7 +136,6 @@ struct call {
     PyObject* refused() { return Py_BuildValue("(is)", (int)LF_EINVAL, problem.c_str()); }
 };
 
-long number(PyObject* o) { return PyLong_AsLong(o); }
 void* address(PyObject* o) { return PyLong_AsVoidPtr(o); }
 
 #define LF_EXPECT(n)                                                                     \
@@ -145,7 +154,7 @@ PyObject* m_linear(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     const at::Tensor *x = c.tensor(v[2], "x"), *w = c.tensor(v[3], "w");
     int k = 0, wn = 0;
     a.dtype = c.type(x, "x");
-    a.act = (int)number(v[7]);
+    a.act = c.number(v[7], "act");
     LF_NUMBERS_OK;
     c.shape(x, "x", &a.tokens, &a.n_in);
     c.shape(w, "w", &wn, &k);
@@ -169,7 +178,7 @@ PyObject* m_linear_grad_x(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     const at::Tensor *dz = c.tensor(v[2], "dz"), *w = c.tensor(v[3], "w");
     int wn = 0;
     a.dtype = c.type(dz, "dz");
-    a.act = (int)number(v[7]);
+    a.act = c.number(v[7], "act");
     LF_NUMBERS_OK;
     c.shape(dz, "dz", &a.tokens, &a.n_out);
     c.shape(w, "w", &wn, &a.n_in);
@@ -192,7 +201,7 @@ PyObject* m_linear_grad_w(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     int wn = 0;
     a.dtype = c.type(dz, "dz");
     a.gw_dtype = c.type(gw, "gw");
-    a.act = (int)number(v[8]);
+    a.act = c.number(v[8], "act");
     LF_NUMBERS_OK;
     c.shape(dz, "dz", &a.tokens, &a.n_out);
     c.shape(gw, "gw", &wn, &a.n_in);
@@ -269,7 +278,7 @@ PyObject* m_unpack8(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     LF_EXPECT(7);
     call c(v[6]);
     const at::Tensor* x = c.tensor(v[4], "x");
-    const int dtype = c.type(x, "x"), act = (int)number(v[5]);
+    const int dtype = c.type(x, "x"), act = c.number(v[5], "act");
     LF_NUMBERS_OK;
     int m, n;
     c.shape(x, "x", &m, &n);
@@ -287,7 +296,7 @@ PyObject* m_act_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     LF_EXPECT(8);
     call c(v[7]);
     const at::Tensor* dy = c.tensor(v[2], "dy");
-    const int dtype = c.type(dy, "dy"), act = (int)number(v[6]);
+    const int dtype = c.type(dy, "dy"), act = c.number(v[6], "act");
     LF_NUMBERS_OK;
     int m, n;
     c.shape(dy, "dy", &m, &n);

@@ -136,3 +136,18 @@ def test_tensors_without_plain_memory_are_refused_and_do_not_end_the_process(mak
         for f, *a in calls:
             assert "argument" in refused(f, *a)
     """)
+
+
+def test_activations_beyond_an_int_are_refused():
+    _without_gpu("""
+        m, byte = torch.ones(4, 8, dtype=torch.bfloat16), torch.zeros(4, 8, dtype=torch.uint8)
+        for act in (2 ** 32, 2 ** 32 + 3, -2 ** 32, 2 ** 31, -2 ** 31 - 1, 2 ** 64, -2 ** 80):
+            for f, *a in ((o.linear, m, m, m), (o.linear_grad_x, m, m, m), (o.linear_grad_w, m, m), (o.unpack8, byte, byte, m), (o.act_backward, m, byte, byte, m)):
+                assert "argument act: out of range" in refused(f, *a, act=act)
+        try:
+            o.linear(m, m, m, act="gelu")
+        except TypeError:
+            pass
+        else:
+            raise AssertionError("a text is no activation")
+    """)
