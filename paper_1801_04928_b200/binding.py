@@ -440,7 +440,10 @@ class Operators:
     the width (a slice of columns of a wider matrix).  Results go into the tensors that are passed in.
     Raises :class:`LeapfrogError` on any non-zero status and on tensors whose type, device, shape or
     layout does not fit: they are on the GPU that was current when the handle was made, and work is put there
-    whichever is current at the call.  ``stream``: a cudaStream_t as an int; None is the legacy default stream.
+    whichever is current at the call.  ``stream``: a cudaStream_t as an int; None is the legacy default
+    stream (torch's current stream is not looked at).  Nothing is recorded for autograd: the gradients are operators
+    of their own.  Outputs are marked as modified, and one that is still a lazy copy of another tensor gets
+    memory of its own first, by a copy on torch's current stream, which then has to be the handle's.
     The tensors are checked and turned into C arguments by the native module ``_marshal``.
     """
 

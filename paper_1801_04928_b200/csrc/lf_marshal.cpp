@@ -15,6 +15,7 @@
 #include <exception>
 #include <new>
 #include <string>
+#include <type_traits>
 
 #include "leapfrog.h"
 
@@ -25,6 +26,8 @@ constexpr long long ROWS_MOST = 0x7FFFFFFF;
 struct call {
     const int device;                // the handle's: the last argument
     std::string problem;
+    const at::Tensor* written[6];    // outputs of the call
+    int n_written = 0;
     explicit call(PyObject* d) : device((int)PyLong_AsLong(d)) {}
 
     bool refuse(const char* name, const std::string& what)
@@ -91,9 +94,21 @@ struct call {
         *p = t->const_data_ptr();
         return true;
     }
+    // an output: memory that it shares with a lazy copy becomes its own, and its version goes up when the call is accepted
+    void* output(PyObject* o)
+    {
+        if (o == Py_None) return nullptr;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        written[n_written++] = &t;
+        return t.mutable_data_ptr();
+    }
     bool mat(PyObject* o, const char* name, int rows, int cols, at::ScalarType st, void** p, long long* ld)
     {
-        return mat(o, name, rows, cols, st, const_cast<const void**>(p), ld);
+        const void* as_input;
+        *p = nullptr;
+        if (!mat(o, name, rows, cols, st, &as_input, ld)) return false;
+        *p = output(o);
+        return true;
     }
     // contiguous tensor of n elements
     bool flat(PyObject* o, const char* name, long long n, at::ScalarType st, const void** p)
@@ -111,9 +126,11 @@ struct call {
     bool flat(PyObject* o, const char* name, long long n, at::ScalarType st, U** p)
     {
         const void* v;
-        const bool ok = flat(o, name, n, st, &v);
-        *p = static_cast<U*>(const_cast<void*>(v));
-        return ok;
+        *p = nullptr;
+        if (!flat(o, name, n, st, &v)) return false;
+        if constexpr (std::is_const_v<U>) *p = static_cast<U*>(v);
+        else *p = static_cast<U*>(output(o));
+        return true;
     }
     template <typename U>
     bool eight(PyObject* q, PyObject* s, int rows, int cols, U** qp, U** sp)
@@ -130,7 +147,11 @@ struct call {
     }
     PyObject* answer(int rc)
     {
-        if (rc == LF_OK) Py_RETURN_NONE;
+        if (rc == LF_OK) {
+            for (int i = 0; i < n_written; ++i)
+                if (!written[i]->is_inference()) written[i]->unsafeGetTensorImpl()->bump_version();      // (those have no version)
+            Py_RETURN_NONE;
+        }
         return Py_BuildValue("(iO)", rc, Py_None);
     }
     PyObject* refused() { return Py_BuildValue("(is)", (int)LF_EINVAL, problem.c_str()); }
@@ -284,7 +305,7 @@ PyObject* m_unpack8(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     c.shape(x, "x", &m, &n);
     if (!c.problem.empty()) return c.refused();
     void* xp;
-    unsigned char *q, *s;
+    const unsigned char *q, *s;
     long long ld;
     if (!(c.mat(v[4], "x", m, n, x->scalar_type(), &xp, &ld) && c.eight(v[2], v[3], m, n, &q, &s))) return c.refused();
     return c.answer(reinterpret_cast<decltype(&lf_unpack8)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), dtype, act, m, n, q, s, xp, ld));
@@ -303,7 +324,7 @@ PyObject* m_act_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     if (!c.problem.empty()) return c.refused();
     const void* yp;
     void* zp;
-    unsigned char *q, *s;
+    const unsigned char *q, *s;
     long long ldy, ldz;
     if (!(c.mat(v[2], "dy", m, n, dy->scalar_type(), &yp, &ldy) && c.mat(v[5], "dz", m, n, dy->scalar_type(), &zp, &ldz) && c.eight(v[3], v[4], m, n, &q, &s)))
         return c.refused();

@@ -830,3 +830,52 @@ def test_tensors_of_another_device_are_refused():
             with pytest.raises(lf.LeapfrogError, match=f"cuda:{o._device} needed") as e:
                 f(*a)
             assert e.value.status == lf.LF_EINVAL
+
+
+def _written(ops):
+    """Every operator as (call, outputs, inputs)."""
+    t = lambda r, c, d=BF16: torch.zeros(r, c, dtype=d, device="cuda")     # noqa: E731
+    byte = torch.uint8
+    x, w, y, dz, dx, r, h = t(4, 64), t(32, 64), t(4, 32), t(4, 32), t(4, 64), t(4, 64), t(4, 64)
+    gw, gb, bias, gain, dg = t(32, 64, F32), torch.zeros(32, device="cuda"), torch.zeros(32, device="cuda"), torch.ones(64, device="cuda"), torch.zeros(64, device="cuda")
+    qy, sy, qx, sx = t(4, 32, byte), t(4, 1, byte), t(4, 64, byte), t(4, 2, byte)
+    return [(lambda: ops.linear(x, w, y, bias=bias, residual=dz, q=qy, s=sy), (y, qy, sy), (x, w, bias, dz)),
+            (lambda: ops.linear_grad_x(dz, w, dx, q=qx, s=sx, act=R.GELU, add=r), (dx,), (dz, w, qx, sx, r)),
+            (lambda: ops.linear_grad_w(dz, gw, gb=gb, q=qx, s=sx, act=R.GELU), (gw, gb), (dz, qx, sx)),
+            (lambda: ops.linear_grad_w(dz, gw, gb=gb, x=x), (gw, gb), (dz, x)),
+            (lambda: ops.rms_norm(x, gain, dx, residual=r, h=h, q=qx, s=sx), (dx, h, qx, sx), (x, gain, r)),
+            (lambda: ops.rms_norm_backward(x, h, gain, dx, dg, dres=r), (dx, dg), (x, h, gain, r)),
+            (lambda: ops.pack8(x, qx, sx), (qx, sx), (x,)),
+            (lambda: ops.unpack8(qx, sx, dx), (dx,), (qx, sx)),
+            (lambda: ops.act_backward(x, qx, sx, dx, act=R.RELU), (dx,), (x, qx, sx))]
+
+
+def test_outputs_are_marked_as_written(ops):
+    # what autograd goes by to see that a tensor it has kept was overwritten
+    for call, outputs, inputs in _written(ops):
+        before = [v._version for v in outputs + inputs]
+        call()
+        assert [v._version for v in outputs] == [b + 1 for b in before[:len(outputs)]]
+        assert [v._version for v in inputs] == before[len(outputs):]
+    with torch.inference_mode():
+        for call, _, _ in _written(ops):
+            call()
+    ops.sync()
+    kept, q, s = torch.zeros(4, 64, device="cuda", requires_grad=True), torch.zeros(4, 64, dtype=torch.uint8, device="cuda"), torch.full((4, 2), 127, dtype=torch.uint8, device="cuda")
+    mid = kept * 1.0
+    out = mid.square().sum()                   # its gradient needs mid
+    ops.unpack8(q, s, mid.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.backward()
+
+
+def test_a_lazy_copy_is_not_written_through(ops):
+    x = torch.ones(4, 64, dtype=BF16, device="cuda")
+    q, s = torch.empty(4, 64, dtype=torch.uint8, device="cuda"), torch.empty(4, 2, dtype=torch.uint8, device="cuda")
+    ops.pack8(x, q, s)
+    lazy, q2, s2 = torch._lazy_clone(x), torch._lazy_clone(q), torch._lazy_clone(s)
+    ops.unpack8(q2, s2, lazy, act=R.TANH)      # reads two lazy copies and writes a third
+    ops.pack8(lazy, q2, s2)
+    ops.sync()
+    assert x.eq(1).all() and lazy.eq(0.76171875).all()                     # tanh 1 in bf16
+    assert torch.equal(R.unpack8(q, s), x.to(R.D)) and bool((R.unpack8(q2, s2) != 1).all())
