@@ -453,7 +453,10 @@ class Operators:
             self._h = None
             raise LeapfrogError(rc, "lf_ops_create")
         import torch  # noqa: F401  (its libraries have to be loaded before the module that uses them)
-        from . import _marshal
+        try:
+            from . import _marshal
+        except ImportError as exc:
+            raise ImportError(f"_marshal.so is missing or does not fit this torch; run python -m {__package__}.build ({exc})") from exc
         self._m = _marshal
         self._a = self._h.value
         self._device = self.stats()["device"]

@@ -1,15 +1,17 @@
 """Build ``libleapfrog.so`` in-tree with nvcc for sm_100a, and ``_marshal.so`` with g++ (tensor marshalling
-of the layer operators, against the installed torch's headers).
+of the layer operators, against the installed torch's headers; without torch it is left out and the C library alone is built).
 
 Run as ``python -m paper_1801_04928_b200.build`` or call :func:`build`.  The shared library
 lands beside this file; nothing is installed elsewhere and nothing is compiled at import time.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -32,11 +34,13 @@ MARSHAL = os.path.join(PKG, "_marshal.so")
 
 
 def _build_marshal(force: bool) -> None:
+    spec = importlib.util.find_spec("torch")
+    if spec is None or spec.origin is None:
+        sys.stderr.write("torch not found: _marshal.so, the layer operators on torch tensors, is not built\n")
+        return
+    torch_dir = os.path.dirname(spec.origin)
     if not force and not _stale(MARSHAL, [MARSHAL_SRC, os.path.join(INCLUDE, "leapfrog.h")]):
         return
-    import sysconfig
-    import importlib.util
-    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
     inc = os.path.join(torch_dir, "include")
     tmp = MARSHAL + f".tmp{os.getpid()}"
     # no run path: torch is loaded before the module, which finds its libraries by name
@@ -88,7 +92,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
     with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         marshal = ex.submit(_build_marshal, force)
         objs = list(ex.map(compile_one, SOURCES))
-        marshal.result()
     if force or _stale(LIB, objs):
         tmp = LIB + f".tmp{os.getpid()}"
         r = subprocess.run([nvcc, "-shared", "-o", tmp, *objs, "-gencode",
@@ -96,6 +99,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
         os.replace(tmp, LIB)
+    marshal.result()                 # (last: what goes wrong there does not keep the library from being linked)
     return LIB
 
 

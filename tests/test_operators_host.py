@@ -151,3 +151,13 @@ def test_activations_beyond_an_int_are_refused():
         else:
             raise AssertionError("a text is no activation")
     """)
+
+
+def test_the_library_is_built_without_torch(monkeypatch, tmp_path, capsys):
+    import importlib.util
+    from paper_1801_04928_b200 import build
+    find = importlib.util.find_spec
+    monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: None if name == "torch" else find(name, *a))
+    monkeypatch.setattr(build, "MARSHAL", str(tmp_path / "_marshal.so"))
+    assert build.build() == build.LIB and os.path.exists(build.LIB)
+    assert not os.path.exists(build.MARSHAL) and "torch not found" in capsys.readouterr().err
