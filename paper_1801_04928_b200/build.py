@@ -39,7 +39,12 @@ def _build_marshal(force: bool) -> None:
         sys.stderr.write("torch not found: _marshal.so, the layer operators on torch tensors, is not built\n")
         return
     torch_dir = os.path.dirname(spec.origin)
-    if not force and not _stale(MARSHAL, [MARSHAL_SRC, os.path.join(INCLUDE, "leapfrog.h")]):
+    # the module fits the torch and the Python it was built against: others make it stale
+    version = os.path.join(torch_dir, "version.py")
+    against = f"{sys.version}\n{torch_dir}\n" + (open(version).read() if os.path.exists(version) else "")
+    stamp = os.path.join(OBJ, os.path.basename(MARSHAL) + ".torch")
+    same = os.path.exists(stamp) and open(stamp).read() == against
+    if not force and same and not _stale(MARSHAL, [MARSHAL_SRC, os.path.join(INCLUDE, "leapfrog.h")]):
         return
     inc = os.path.join(torch_dir, "include")
     tmp = MARSHAL + f".tmp{os.getpid()}"
@@ -52,6 +57,8 @@ def _build_marshal(force: bool) -> None:
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed on lf_marshal.cpp:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, MARSHAL)
+    with open(stamp, "w") as f:
+        f.write(against)
 
 
 def _nvcc() -> str:

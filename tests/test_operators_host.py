@@ -161,3 +161,29 @@ def test_the_library_is_built_without_torch(monkeypatch, tmp_path, capsys):
     monkeypatch.setattr(build, "MARSHAL", str(tmp_path / "_marshal.so"))
     assert build.build() == build.LIB and os.path.exists(build.LIB)
     assert not os.path.exists(build.MARSHAL) and "torch not found" in capsys.readouterr().err
+
+
+def test_the_tensor_module_is_rebuilt_for_another_torch(monkeypatch, tmp_path):
+    import importlib.util
+    import types
+    from paper_1801_04928_b200 import build
+    home, runs = tmp_path / "torch", []
+    home.mkdir()
+    (home / "version.py").write_text("__version__ = '1'")
+
+    def compiler(cmd, **kw):
+        runs.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+        return types.SimpleNamespace(returncode=0, stdout="", stderr="")
+
+    monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: types.SimpleNamespace(origin=str(home / "__init__.py")))
+    monkeypatch.setattr(build, "OBJ", str(tmp_path))
+    monkeypatch.setattr(build, "MARSHAL", str(tmp_path / "_marshal.so"))
+    monkeypatch.setattr(build.subprocess, "run", compiler)
+    build._build_marshal(False)
+    build._build_marshal(False)
+    assert len(runs) == 1
+    (home / "version.py").write_text("__version__ = '2'")
+    build._build_marshal(False)
+    build._build_marshal(False)
+    assert len(runs) == 2 and str(home / "lib") in runs[1]
