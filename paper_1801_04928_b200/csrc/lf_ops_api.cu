@@ -81,7 +81,7 @@ int lf_ops_create(lf_ops** out, long long workspace_bytes)
     ok = ok && cudaMemset(o->status_dev, 0, sizeof(unsigned)) == cudaSuccess;
     // (the memsets are only queued, on a stream that the handle's own need not wait for)
     ok = ok && cudaStreamSynchronize(nullptr) == cudaSuccess;
-    ok = ok && lf_product_tc_init(o) == LF_OK && lf_linear_stream_init() == LF_OK;
+    ok = ok && lf_product_tc_init(o) == LF_OK && lf_linear_stream_init() == LF_OK && lf_rows_init() == LF_OK;
     if (!ok) {
         const cudaError_t e = cudaGetLastError();
         lf_ops_destroy(o);

@@ -83,6 +83,7 @@ typedef CUresult (*lf_encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 // ---- launchers: sizes and pointers are checked by the caller ------------------------------------
+int lf_rows_init();                 // opts the kernels in
 cudaError_t lfk_rms_norm(const lf_rms_norm_args& a, int sm_count, cudaStream_t s);
 cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s,
                                   int* launches);

@@ -567,36 +567,63 @@ struct norm_go {
 // memory allows with two blocks per multiprocessor, up to four rows.
 template <typename T, int TPR, int VPT>
 struct norm_backward_go {
+    static constexpr int GROUPS = TPR >= 256 ? 1 : 256 / TPR;
+    static constexpr size_t slot(bool dres) { return (size_t)(dres ? 3 : 2) * VPT * TPR * GROUPS * 8 * sizeof(T); }
+    static int depth(bool dres)
+    {
+        const size_t most = 110 * 1024;
+        int d = 4;
+        while (d > 1 && slot(dres) * d > most) --d;
+        if (d == 1 && slot(dres) * 2 <= 220 * 1024) d = 2;         // one block per multiprocessor, two rows in flight
+        return d;
+    }
     static cudaError_t go(const lf_rms_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* grid_out)
     {
-        constexpr int GROUPS = TPR >= 256 ? 1 : 256 / TPR;
-        const size_t slot = (size_t)(a.dres ? 3 : 2) * VPT * TPR * GROUPS * 8 * sizeof(T), most = 110 * 1024;
         const long long blocks = ((long long)a.tokens + GROUPS - 1) / GROUPS;
-        int depth = 4;
-        while (depth > 1 && slot * depth > most) --depth;
-        if (depth == 1 && slot * 2 <= 220 * 1024) depth = 2;       // one block per multiprocessor, two rows in flight
         if constexpr (VPT == 1) {                                  // (few rows of up to 4096 columns)
             if (a.dgain && blocks <= NORM_CLUSTER) {
-                const auto kernel = k_rms_norm_backward<T, TPR, VPT, GROUPS, true>;
-                cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)slot);
-                if (e != cudaSuccess) return e;
                 int grid = 1;
                 while (grid < blocks) grid *= 2;
                 *grid_out = 0;
-                return lf_launch_clusters(kernel, dim3(grid), TPR * GROUPS, slot, grid, s, a, a.dgain, 1);      // a row each: a ring of one
+                return lf_launch_clusters(k_rms_norm_backward<T, TPR, VPT, GROUPS, true>, dim3(grid), TPR * GROUPS, slot(a.dres), grid, s, a, a.dgain,
+                                          1);                      // a row each: a ring of one
             }
         }
-        const auto kernel = k_rms_norm_backward<T, TPR, VPT, GROUPS, false>;
         const int at_most = 2 * sm_count < LF_OPS_PARTIAL_ROWS ? 2 * sm_count : LF_OPS_PARTIAL_ROWS;
-        const int grid = blocks < at_most ? (int)blocks : at_most;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(slot * depth));
-        if (e != cudaSuccess) return e;
+        const int grid = blocks < at_most ? (int)blocks : at_most, d = depth(a.dres);
         *grid_out = grid;
-        return lf_launch(kernel, dim3(grid), TPR * GROUPS, slot * depth, s, a, a.dgain ? partial : nullptr, depth);
+        return lf_launch(k_rms_norm_backward<T, TPR, VPT, GROUPS, false>, dim3(grid), TPR * GROUPS, slot(a.dres) * d, s, a, a.dgain ? partial : nullptr, d);
+    }
+};
+// The shared memory that a kernel may be launched with, with dres and without, is set once: it belongs to the
+// kernel and not to a call, which another thread's call could take it away from.
+template <typename T, int TPR, int VPT>
+struct norm_backward_ready {
+    typedef norm_backward_go<T, TPR, VPT> shape;
+    static cudaError_t go()
+    {
+        const size_t with = shape::slot(true) * shape::depth(true), without = shape::slot(false) * shape::depth(false);
+        cudaError_t e = cudaFuncSetAttribute(k_rms_norm_backward<T, TPR, VPT, shape::GROUPS, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)(with > without ? with : without));
+        if constexpr (VPT == 1)
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(k_rms_norm_backward<T, TPR, VPT, shape::GROUPS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shape::slot(true));
+        return e;
     }
 };
 
 }  // namespace
+
+int lf_rows_init()
+{
+    for (int n = 256; n <= LF_OPS_MAX_NORM; n *= 2)                // every shape that pick_row_shape has
+        for (int many = 0; many < 2; ++many)
+            if (pick_row_shape<norm_backward_ready, float>(n, many != 0) != cudaSuccess ||
+                pick_row_shape<norm_backward_ready, __nv_bfloat16>(n, many != 0) != cudaSuccess ||
+                pick_row_shape<norm_backward_ready, __half>(n, many != 0) != cudaSuccess)
+                return LF_ECUDA;
+    return LF_OK;
+}
 
 cudaError_t lfk_rms_norm(const lf_rms_norm_args& a, int sm_count, cudaStream_t s)
 {

@@ -489,6 +489,29 @@ def test_norm_backward_of_few_rows_is_one_launch(ops, M, n, dtype, dres):
     assert ops.stats()["launches"] == 1
 
 
+def test_norm_backward_from_several_threads():
+    # handles of their own, calls with and without dres (which need different shared memory) at the same time
+    import threading
+    refusals = []
+
+    def work(dres):
+        with lf.Operators() as o:
+            h, gain = torch.ones(4, 16384, dtype=BF16, device="cuda"), torch.ones(16384, device="cuda")
+            dh = torch.empty_like(h)
+            a = lf.lf_rms_norm_backward_args(dtype=lf.LF_BF16, tokens=4, n=16384, eps=1e-5, dy=h.data_ptr(), h=h.data_ptr(), gain=gain.data_ptr(),
+                                             dres=h.data_ptr() if dres else None, dh=dh.data_ptr())
+            torch.cuda.synchronize()
+            refusals.extend(rc for rc in (lf.lf_rms_norm_backward(o._h, a) for _ in range(3000)) if rc != lf.LF_OK)     # (ctypes lets threads run)
+            o.sync()
+
+    threads = [threading.Thread(target=work, args=(i % 2 == 0,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not refusals, (len(refusals), refusals[0])
+
+
 def test_norm_backward_against_central_differences(ops):
     g = _gen(11)
     h, dy, gain = _rand(g, 3, 40), _rand(g, 3, 40), 1 + _rand(g, 40, std=0.2)
