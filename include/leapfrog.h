@@ -389,10 +389,10 @@ int lf_delta_step_static(const float* w_up, const float* delta_up, const float* 
  * s = 255 and reads back as NaN throughout.
  *
  * tokens = 0 is legal everywhere (matrices over tokens may then be NULL): nothing is written, except
- * that gradients summed over tokens are set to zero.  An output may be the very matrix (same address, same leading dimension) that
- * `residual`, `add` or `dres` names, and h or y of lf_rms_norm may be its x or residual; other
- * overlaps of outputs with inputs are not allowed.  Results do not depend on timing: sums are added in
- * a fixed order.
+ * that gradients summed over tokens are set to zero.  An output may be the very matrix (same address,
+ * same leading dimension) that `residual`, `add` or `dres` names; h or y of lf_rms_norm may be its x or
+ * residual, and dh of lf_rms_norm_backward its dy or h.  Other overlaps of outputs with inputs are not
+ * allowed.  Results do not depend on timing: sums are added in a fixed order.
  * ================================================================================================ */
 typedef struct lf_ops lf_ops;
 

@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(TPR) k_rms_norm(const lf_rms_norm_args a)
 // ---- dh = r (u - h r mean(u h r)) + dres, partial column sums of dy h r -----------------------------
 // Groups of TPR threads take a row at a time and walk down the matrix.  The rows ahead are on their way into shared
 // memory meanwhile (cp.async; a thread copies exactly what it will read itself, so the ring needs no
-// barriers), which keeps the memory busy through the row's two phases: with the row loaded into registers at
+// barriers, and dh may be h, dy or dres), which keeps the memory busy through the row's two phases: with the row loaded into registers at
 // the top of the loop instead, 16384 x 8192 took 283 us, 3.8 TB/s.  Both row sums share one exchange, in
 // buffers that alternate, so a row has one barrier.  The gain's gradient stays in registers, eight
 // columns per vector; the groups of a block add theirs at the end, one partial row per block.  16384 x 8192 bf16 with

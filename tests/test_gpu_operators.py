@@ -489,6 +489,26 @@ def test_norm_backward_of_few_rows_is_one_launch(ops, M, n, dtype, dres):
     assert ops.stats()["launches"] == 1
 
 
+@pytest.mark.parametrize("M,n,dtype", [(1, 4096, BF16), (5, 264, F16), (300, 4096, BF16), (2000, 1032, F32), (299, 16384, F32)])
+@pytest.mark.parametrize("ld", [0, 16])
+def test_norm_backward_over_one_of_its_inputs(ops, M, n, dtype, ld):
+    g = _gen(M)
+    t = [Out(M, n, dtype, n + ld) for _ in range(3)]
+    for o in t:
+        o.t.copy_(_rand(g, M, n, dtype=dtype))
+    gain = 1 + _rand(g, n, std=0.2)
+    want, dg, dg2 = torch.empty(M, n, dtype=dtype, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    ops.rms_norm_backward(t[0].t, t[1].t, gain, want, dg, dres=t[2].t)
+    for over in range(3):
+        kept = [o.t.clone() for o in t]
+        ops.rms_norm_backward(t[0].t, t[1].t, gain, t[over].t, dg2, dres=t[2].t)
+        ops.sync()
+        assert torch.equal(t[over].t, want) and torch.equal(dg, dg2)
+        for o, k in zip(t, kept):
+            o.check()
+            o.t.copy_(k)
+
+
 def test_norm_backward_from_several_threads():
     # handles of their own, calls with and without dres (which need different shared memory) at the same time
     import threading
@@ -713,6 +733,71 @@ def test_offsets_beyond_32_bits(ops):
     ops.sync()
     assert torch.equal(y[last], R.unpack8(q[last], s[last]).to(BF16))
     assert n[last].isfinite().all()
+
+
+def test_gradients_and_packing_beyond_32_bits():
+    # the same 140000 x 16384 in every matrix over tokens of the other operators.  What is summed over tokens comes from
+    # the last 64 rows alone, so that a row fetched from elsewhere shows.
+    M, N, K, L = 140000, 16384, 8, 64
+    last = slice(M - L, M)
+    g = _gen(16)
+    empty = lambda *s, d=BF16: torch.empty(*s, dtype=d, device="cuda")   # noqa: E731
+    wide, byte = empty(M, N), torch.uint8
+    for i in range(0, M, 20000):
+        wide[i:i + 20000].normal_(0.0, 1.0, generator=g)
+    with lf.Operators(lf.lf_ops_workspace(M, N)) as o:
+        q, s, out = empty(M, N, d=byte), empty(M, N // 32, d=byte), torch.full((M, N), float("nan"), dtype=BF16, device="cuda")
+        o.pack8(wide, q, s)
+        o.act_backward(wide, q, s, out, act=R.GELU)
+        o.sync()
+        rq, rs = R.pack8(wide[last])
+        assert torch.equal(s[last], rs) and bool(((q[last] == rq) | ((q[last] & 0x7F == 0) & (rq & 0x7F == 0))).all())
+        z = R.unpack8(q[last], s[last])
+        w64 = wide[last].to(R.D)
+        ref = w64 * R.act_prime(z, R.GELU)
+        R.check("dz", out[last], ref, R.rounded(ref, BF16, 16e-6 * w64.abs() * (1 + z.abs())))
+        # dx [M, N] = (dz w) * gelu'(z) + add
+        dz, w = _rand(g, M, K, dtype=BF16), _rand(g, K, N, std=0.3, dtype=BF16)
+        out.fill_(float("nan"))
+        o.linear_grad_x(dz, w, out, q=q, s=s, act=R.GELU, add=wide)
+        o.sync()
+        d64 = dz[last].to(R.D)
+        t, sp = d64 @ w.to(R.D), R.act_prime(z, R.GELU)
+        ref = t * sp + w64
+        R.check("dx", out[last], ref, R.rounded(ref, BF16, R.product_err(d64, w.to(R.D)) * sp.abs() + 8e-6 * t.abs() + 2.0 ** -24 * ref.abs()))
+        # gw [K, N] from 8 bits, through the workspace
+        dz[:M - L] = 0
+        gw, gb = empty(K, N, d=F32), empty(K, d=F32)
+        o.linear_grad_w(dz, gw, gb=gb, q=q, s=s)
+        o.sync()
+        R.check("gw", gw, d64.t() @ z, R.rounded(d64.t() @ z, F32, R.product_err(d64.t(), z)))
+        R.check("gb", gb, d64.sum(0), (L + 340) * 2.0 ** -24 * d64.abs().sum(0))
+        del q, s, dz
+        # gw [N, K] and gb [N] with a wide dz
+        x = _rand(g, M, K, dtype=BF16)
+        wide[:M - L] = 0
+        gw, gb = empty(N, K, d=F32), empty(N, d=F32)
+        o.linear_grad_w(wide, gw, gb=gb, x=x)
+        o.sync()
+        x64 = x[last].to(R.D)
+        R.check("gw", gw, w64.t() @ x64, R.rounded(w64.t() @ x64, F32, R.product_err(w64.t(), x64)))
+        R.check("gb", gb, w64.sum(0), (L + 340) * 2.0 ** -24 * w64.abs().sum(0))
+        # norm backward: dy (zero but for the last rows), h, dh
+        h = empty(M, N)
+        for i in range(0, M, 20000):
+            h[i:i + 20000].normal_(0.0, 1.0, generator=g)
+        gain, dg = 1 + _rand(g, N, std=0.2), empty(N, d=F32)
+        out.fill_(float("nan"))
+        o.rms_norm_backward(wide, h, gain, out, dg)
+        o.sync()
+    assert out[:M - L:1000].eq(0).all()
+    h64, g64 = h[last].to(R.D), gain.to(R.D)
+    rstd = (h64.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+    hn, u = h64 * rstd, w64 * g64
+    ref = rstd * (u - hn * (u * hn).mean(1, keepdim=True))
+    mag = rstd * (u.abs() + hn.abs() * (u * hn).abs().mean(1, keepdim=True))
+    R.check("dh", out[last], ref, R.rounded(ref, BF16, ((N / 32 + 16) * 2.0 ** -23 + 2.0 ** -21) * mag))
+    R.check("dgain", dg, (w64 * hn).sum(0), (L + 340 + N / 64) * 2.0 ** -24 * (w64 * hn).abs().sum(0))
 
 
 def test_work_goes_to_the_stream_that_was_set():
