@@ -153,10 +153,12 @@ struct lf_ctx {
 inline bool lf_layer_owned(const lf_ctx* c, int l) { return (c->L - l) % c->shard_count == c->shard_rank; }
 inline int lf_layer_worker(const lf_ctx* c, int l) { return ((c->L - l) / c->shard_count) % c->keff; }
 
+// (the error is taken back: pending, it would be reported as another call's)
 #define LF_CUDA_TRY(ctx, expr)                                  \
     do {                                                        \
         cudaError_t e__ = (expr);                               \
         if (e__ != cudaSuccess) {                               \
+            cudaGetLastError();                                 \
             (ctx)->last_cuda_error = (int)e__;                  \
             return LF_ECUDA;                                    \
         }                                                       \

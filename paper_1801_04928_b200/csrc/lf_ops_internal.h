@@ -33,10 +33,12 @@ constexpr size_t LF_OPS_FIXED_BYTES = (size_t)LF_OPS_PARTIAL_ROWS * LF_OPS_MAX_N
 constexpr int LF_OPS_MAX_WIDTH = 1 << 24;
 constexpr int LF_OPS_COUNTERS = LF_OPS_MAX_WIDTH / 256;      // one per 256 columns of a bias gradient
 
+// (the error is taken back: pending, it would be reported as another call's)
 #define LF_OPS_TRY(o, expr)                                     \
     do {                                                        \
         cudaError_t e__ = (expr);                               \
         if (e__ != cudaSuccess) {                               \
+            cudaGetLastError();                                 \
             (o)->last_cuda_error = (int)e__;                    \
             return LF_ECUDA;                                    \
         }                                                       \

@@ -1,6 +1,11 @@
 """The layer operators on the GPU against their definitions in 64 bits: values, 8-bit forms, gradients (the
 formula's and central differences'), ragged sizes, strides, aliases, streams, empty inputs, values that are not
 finite, refusals and waits that run out."""
+import os
+import subprocess
+import sys
+import textwrap
+
 import pytest
 import torch
 
@@ -11,6 +16,7 @@ pytestmark = pytest.mark.gpu
 
 BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
 GUARD = 512
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def _rand(g, *shape, std=1.0, dtype=F32):
@@ -987,3 +993,46 @@ def test_a_lazy_copy_is_not_written_through(ops):
     ops.sync()
     assert x.eq(1).all() and lazy.eq(0.76171875).all()                     # tanh 1 in bf16
     assert torch.equal(R.unpack8(q, s), x.to(R.D)) and bool((R.unpack8(q2, s2) != 1).all())
+
+
+@pytest.mark.parametrize("first", ["o.sync()", "ctx.sync()"])
+def test_a_call_that_cuda_refuses_is_not_reported_by_the_next_one(first):
+    # waiting for a stream that is being captured is refused (and ends the capture); what follows knows nothing of it.  In a
+    # process of its own, for the capture's sake.
+    code = f"""
+        import torch, paper_1801_04928_b200 as lf, lf_inputs
+        L, N = 3, 256
+        t = {{k: v.cuda() for k, v in lf_inputs.make_inputs(L, N, 1, "uniform", 7, "cpu").items()}}
+        new = lambda *s: torch.empty(s, device="cuda")
+        z, a, delta, gw, gb = new(L, 1, N), new(L + 1, 1, N), new(L, 1, N), new(L, N, N), new(L, N)
+        o, ctx = lf.Operators(), lf.Leapfrog(L, N, 1, 2)
+        x, w, y = new(20, 64).bfloat16(), new(64, 64).bfloat16(), new(20, 64).bfloat16()
+        variants = (lf.LF_VARIANT_STREAMS, lf.LF_VARIANT_FUSED)
+        for v in variants:                     # (first launches set kernels up)
+            ctx.set_option(lf.LF_OPT_VARIANT, v)
+            ctx.forward(t["w"], t["b"], t["x"], z, a)
+            ctx.backward(t["w"], z, a, t["y"], delta, gw, gb)
+        for v in variants:
+            st, seen = torch.cuda.Stream(), None
+            try:
+                with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=st):
+                    o.set_stream(st.cuda_stream)
+                    ctx.set_stream(st.cuda_stream)
+                    try:
+                        {first}
+                    except lf.LeapfrogError as e:
+                        seen = e.status
+            except RuntimeError:
+                pass
+            assert seen == lf.LF_ECUDA, seen
+            o.set_stream(None)
+            ctx.set_stream(None)
+            ctx.set_option(lf.LF_OPT_VARIANT, v)
+            ctx.forward(t["w"], t["b"], t["x"], z, a)
+            ctx.backward(t["w"], z, a, t["y"], delta, gw, gb)
+            o.linear(x, w, y)
+            ctx.sync()
+            o.sync()
+    """
+    r = subprocess.run([sys.executable, "-c", textwrap.dedent(code)], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
