@@ -488,9 +488,10 @@ enum lf_linear_form {
  * Create a handle on the current CUDA device with `workspace_bytes` of device memory; calls on it
  * never allocate.  lf_ops_workspace(tokens, n_in) gives what any call with at most so many tokens
  * and input columns needs (of it, tokens * n_in * 2 bytes are for lf_linear_grad_w from 8 bits; the
- * rest is a fixed amount).  lf_ops_create waits for the legacy default stream.  Work is enqueued on
- * the handle's stream (lf_ops_set_stream, a stream of the handle's device; initially the legacy default
- * stream); a call makes the handle's device current while it runs.  Calls of one handle that may
+ * rest is a fixed amount), or LF_EINVAL beyond 2^30 tokens or 2^24 columns, which no call takes.
+ * lf_ops_create waits for the legacy default stream.  Work is enqueued on the handle's stream
+ * (lf_ops_set_stream, a stream of the handle's device; initially the legacy default stream); a call
+ * makes the handle's device current while it runs.  Calls of one handle that may
  * overlap on the GPU must be ordered by the caller: they share the workspace.  Options:
  * LF_OPT_WAIT_BUDGET_US, and LF_OPT_WITHHOLD = 1 (test hook: a producer of the matrix products arms
  * a stage it never loads).

@@ -53,7 +53,7 @@ extern "C" {
 
 long long lf_ops_workspace(long long tokens, long long n_in)
 {
-    if (tokens < 0 || n_in < 0) return LF_EINVAL;
+    if (tokens < 0 || n_in < 0 || tokens > MAX_TOKENS || n_in > LF_OPS_MAX_WIDTH) return LF_EINVAL;      // (also: the product fits)
     return (long long)LF_OPS_FIXED_BYTES + ((tokens * n_in * 2 + 255) / 256) * 256;
 }
 

@@ -187,3 +187,9 @@ def test_the_tensor_module_is_rebuilt_for_another_torch(monkeypatch, tmp_path):
     build._build_marshal(False)
     build._build_marshal(False)
     assert len(runs) == 2 and str(home / "lib") in runs[1]
+
+
+def test_workspace_beyond_any_call_is_refused():
+    assert lf.lf_ops_workspace(1 << 30, 1 << 24) == lf.lf_ops_workspace(0, 0) + (1 << 55)
+    for tokens, n_in in (((1 << 30) + 1, 8), (8, (1 << 24) + 8), (1 << 40, 1 << 24), (1 << 62, 2), (1 << 32, 1 << 31), (8, -1)):
+        assert lf.lf_ops_workspace(tokens, n_in) == lf.LF_EINVAL
