@@ -386,7 +386,7 @@ int lf_delta_step_static(const float* w_up, const float* delta_up, const float* 
  * -127 the smallest integer with max|v| <= 448 * 2^e; s holds e + 127 and q the e4m3 numbers
  * nearest to v * 2^-e (ties to even).  The value q * 2^e has four significant bits, so it is exact
  * in bf16 and the tensor cores can take it as it is.  A group that holds an infinity or a NaN gets
- * s = 255 and reads back as NaN throughout.
+ * s = 255 and reads back as NaN throughout; sigma and sigma' of it are NaN (LF_ACT_NONE does not look).
  *
  * tokens = 0 is legal everywhere (matrices over tokens may then be NULL): nothing is written, except
  * that gradients summed over tokens are set to zero.  An output may be the very matrix (same address,

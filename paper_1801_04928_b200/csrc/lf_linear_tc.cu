@@ -315,9 +315,8 @@ __device__ __forceinline__ void lp_finish(float (&acc)[NC], const LtParams& P, l
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 float z[8];
-                dequantize8(make_uint2(now.q[2 * g], now.q[2 * g + 1]), now.s, z);
-                prime_range<8>(z, now.s);
-                prime_all<true, 8, KIND>(v + 8 * g, z);
+                dequantize8(make_uint2(now.q[2 * g], now.q[2 * g + 1]), prime_byte(now.s), z);
+                prime_all<true, 8, KIND>(v + 8 * g, z, prime_nan(now.s));
             }
         }
         if (OPERANDS && P.add) {
@@ -768,10 +767,9 @@ __device__ __forceinline__ void ls_rows(const LtParams& P, const ls_share& e, ls
             float z[4 * NK];
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
-                from_e4m3x4(mine.q[k], scale(mine.s[k]), z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]);
-                prime_range<4>(z + 4 * k, mine.s[k]);
+                from_e4m3x4(mine.q[k], scale(prime_byte(mine.s[k])), z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]);
+                prime_all<true, 4, KIND>(v + 4 * k, z + 4 * k, prime_nan(mine.s[k]));
             }
-            prime_all<true, 4 * NK, KIND>(v, z);
         }
         OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
 #pragma unroll

@@ -424,6 +424,21 @@ __global__ void __launch_bounds__(256) k_pack8(const T* x, long long ld, int tok
     }
 }
 
+// sigma of a piece of W columns that may lie beyond a type, one element after the other: few groups are like that, and their
+// comparisons in the loop below cost it registers and 3 % of its time.  A value beyond fp32 (e = 120) is the largest fp32 number
+// to sigma, so that SiLU and GELU of a negative one are 0 and not -infinity * 0; a result beyond T is T's largest number.
+template <typename T, int KIND, int W>
+__device__ __noinline__ void unpack_saturated(const unsigned char* q, unsigned byte, T* x)
+{
+#pragma unroll 1
+    for (int k = 0; k < W; ++k) {
+        float v, none[3];
+        from_e4m3x4(q[k], scale(byte), v, none[0], none[1], none[2]);
+        v = act2<sizeof(T) == 2, KIND>(f2(clamp_keep_nan(v, max_finite(0.f)))).x;
+        x[k] = (T)clamp_keep_nan(v, max_finite(T()));
+    }
+}
+
 // GRAD = false: x = sigma(value);  GRAD = true: x = dy * sigma'(value)
 template <typename T, bool GRAD, int KIND, int W>
 __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsigned char* s, const T* dy, long long ld_dy, int tokens, int n,
@@ -453,22 +468,20 @@ __device__ __forceinline__ void unpack_rows(const unsigned char* q, const unsign
         for (int u = 0; u < ROWS; ++u) {
             const int row = row0 + u * stride;
             if (row >= tokens) break;
+            if (!GRAD && sv[u] >= overflow_byte(T())) {
+                unpack_saturated<T, KIND, W>(q + (size_t)row * n + W * i, sv[u], x + (size_t)row * ld + W * i);
+                continue;
+            }
             float v[W];
-            dequantize(qv[u], sv[u], v);
+            dequantize(qv[u], GRAD ? prime_byte(sv[u]) : sv[u], v);
             typename piece_of<T, W>::type o;
             if (GRAD) {
                 float d[W];
                 dv[u].get(d);
-                prime_range<W>(v, sv[u]);
-                prime_all<FAST, W, KIND>(d, v);
+                prime_all<FAST, W, KIND>(d, v, prime_nan(sv[u]));
                 o.set(d);
             } else {
-                act_range<W>(v, sv[u]);
                 act_all<FAST, W, KIND>(v);
-                if (sv[u] >= overflow_byte(T())) {       // (no activation of a finite value leaves the range that value is in)
-#pragma unroll
-                    for (int k = 0; k < W; ++k) v[k] = clamp_keep_nan(v[k], max_finite(T()));
-                }
                 o.set(v);
             }
             o.store(x + (size_t)row * ld + W * i);

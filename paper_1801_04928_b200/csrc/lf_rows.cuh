@@ -207,9 +207,9 @@ __device__ __forceinline__ float2 act2(float2 z)
     if (KIND == LF_ACT_GELU) return mul2(z, sigmoid_of<FAST>(z, mul2(z, z), true));
     return z;
 }
-// |z| <= 2^37 or NaN (prime_range): GELU's cubic is finite there
+// |z| <= 448 * 2^28 (prime_byte) or NaN; `nan`: 0, or NaN where z is not a number
 template <bool FAST, int KIND>
-__device__ __forceinline__ float2 act_prime2(float2 z)
+__device__ __forceinline__ float2 act_prime2(float2 z, float nan)
 {
     if (KIND == LF_ACT_TANH || KIND == LF_ACT_SIGMOID) {
         // even functions of z: a (1 - a) with a = sigmoid(-|z|) <= 1/2, where 1 - a does not cancel; tanh' = 4 a (1 - a) at 2 z
@@ -217,7 +217,7 @@ __device__ __forceinline__ float2 act_prime2(float2 z)
         const float2 a = sigmoid_of<FAST>(make_float2(-k * fabsf(z.x), -k * fabsf(z.y)), z, false);
         return mul2(mul2(a, f2(k * k)), fma2(a, f2(-1.f), f2(1.f)));
     }
-    if (KIND == LF_ACT_RELU) return make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
+    if (KIND == LF_ACT_RELU) return make_float2(z.x > 0.f ? 1.f : nan, z.y > 0.f ? 1.f : nan);
     if (KIND == LF_ACT_NONE) return f2(1.f);
     // a + z a (1 - a) g'(z)
     const float2 zz = mul2(z, z);
@@ -253,28 +253,15 @@ __device__ __forceinline__ void act_n(float* v, int kind)
 }
 // d *= sigma'(z)
 template <bool FAST, int NE, int KIND>
-__device__ __forceinline__ void prime_all(float* d, const float* z)
+__device__ __forceinline__ void prime_all(float* d, const float* z, float nan)
 {
 #pragma unroll
     for (int i = 0; i < NE; i += 2) {
         const float2 zi = make_float2(z[i], z[i + 1]);
-        const float2 r = mul2(make_float2(d[i], d[i + 1]), act_prime2<FAST, KIND>(zi));
+        const float2 r = mul2(make_float2(d[i], d[i + 1]), act_prime2<FAST, KIND>(zi, nan));
         d[i] = r.x; d[i + 1] = r.y;
     }
 }
-template <bool FAST, int NE>
-__device__ __forceinline__ void prime_n(float* d, const float* z, int kind)
-{
-    switch (kind) {
-        case LF_ACT_SIGMOID: prime_all<FAST, NE, LF_ACT_SIGMOID>(d, z); break;
-        case LF_ACT_TANH: prime_all<FAST, NE, LF_ACT_TANH>(d, z); break;
-        case LF_ACT_RELU: prime_all<FAST, NE, LF_ACT_RELU>(d, z); break;
-        case LF_ACT_SILU: prime_all<FAST, NE, LF_ACT_SILU>(d, z); break;
-        case LF_ACT_GELU: prime_all<FAST, NE, LF_ACT_GELU>(d, z); break;
-        default: break;
-    }
-}
-
 // ---- 8 bits -------------------------------------------------------------------------------------
 __device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 // the scale byte of a group from the bits of its largest magnitude (NaN > infinity > finite as integers):
@@ -293,6 +280,11 @@ __device__ __forceinline__ float scale(unsigned byte)         // 2^e
 {
     return __uint_as_float(byte == 255u ? 0x7FC00000u : (byte == 0u ? 0x00400000u : byte << 23));
 }
+// The byte whose scale sigma' is taken with: at most 2^28, so that GELU's cubic stays finite (z a (1 - a) g'(z) needs |z| < 1e13).
+// From e = 28 on every value but zero is beyond 2^19, where sigma' is 0 or 1 to the last bit for all activations.
+__device__ __forceinline__ unsigned prime_byte(unsigned byte) { return byte < 127u + 28u || byte == 255u ? byte : 127u + 28u; }
+// what is added to the rectifier's sigma', a comparison, which does not see NaN
+__device__ __forceinline__ float prime_nan(unsigned byte) { return byte == 255u ? __uint_as_float(0x7FC00000u) : 0.f; }
 __device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d)
 {
     unsigned short lo, hi;
@@ -332,27 +324,4 @@ __device__ __forceinline__ void dequantize8(uint2 q, unsigned byte, float (&v)[8
     from_e4m3x4(q.x, s, v[0], v[1], v[2], v[3]);
     from_e4m3x4(q.y, s, v[4], v[5], v[6], v[7]);
 }
-// The ends of the range, where products of fp32 numbers overflow although sigma and sigma' are finite.  Both look at
-// the group's scale byte first, which settles it for all but a few groups.
-// Values that sigma is applied to: with e = 120 the largest e4m3 numbers stand for 2^128 and more; they
-// become the largest fp32 number, so that SiLU and GELU of the negative ones are 0 and not -infinity * 0.
-template <int NE>
-__device__ __forceinline__ void act_range(float* v, unsigned byte)
-{
-    if (byte >= 127u + 120u) {
-#pragma unroll
-        for (int i = 0; i < NE; ++i) v[i] = clamp_keep_nan(v[i], 3.402823466e38f);
-    }
-}
-// Values that sigma' is taken at: beyond 2^37 it is 0 or 1 to the last bit for every activation, and a finite z a (1 - a) g'(z)
-// needs |z| < 1e13 for GELU.  Up to e = 28 no value is beyond 448 * 2^28 < 2^37.
-template <int NE>
-__device__ __forceinline__ void prime_range(float* z, unsigned byte)
-{
-    if (byte > 127u + 28u) {
-#pragma unroll
-        for (int i = 0; i < NE; ++i) z[i] = clamp_keep_nan(z[i], 137438953472.0f);
-    }
-}
-
 }  // namespace lfrow

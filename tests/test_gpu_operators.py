@@ -612,6 +612,33 @@ def test_groups_that_are_not_finite_read_back_as_nan(ops):
         assert v[0, :32].eq(1).all() and v[0, 64:].eq(1).all() and v[1, :64].eq(1).all()
 
 
+@pytest.mark.parametrize("act", [R.SILU, R.GELU, R.SIGMOID, R.TANH, R.RELU])
+def test_gradients_through_groups_that_are_not_finite_are_nan(ops, act):
+    # what z was is not known there: a gradient that looks like a number would hide it
+    for dtype in (BF16, F16, F32):
+        z, dy = torch.ones(3, 72, dtype=dtype, device="cuda"), torch.ones(3, 72, dtype=dtype, device="cuda")
+        z[0, 33], z[1, 70] = float("inf"), float("nan")
+        q, s, dz = torch.empty(3, 72, dtype=torch.uint8, device="cuda"), torch.empty(3, 3, dtype=torch.uint8, device="cuda"), torch.empty_like(z)
+        ops.pack8(z, q, s)
+        ops.act_backward(dy, q, s, dz, act=act)
+        ops.sync()
+        bad = torch.zeros(3, 72, dtype=torch.bool, device="cuda")
+        bad[0, 32:64] = bad[1, 64:] = True
+        assert torch.equal(dz.isnan(), bad)
+    for M, K, N, form in ((40, 136, 72, lf.LF_FORM_SPLIT), (2049, 1288, 1800, lf.LF_FORM_PAIRS), (500, 4000, 4096, lf.LF_FORM_SPLIT_PAIRS)):
+        g = _gen(M)
+        z, dz, w = _rand(g, M, K, dtype=BF16), _rand(g, M, N, dtype=BF16), _rand(g, N, K, std=N ** -0.5, dtype=BF16)
+        z[3, 40], z[M - 1, K - 1] = float("inf"), float("nan")
+        q, s, dx = torch.empty(M, K, dtype=torch.uint8, device="cuda"), torch.empty(M, _groups(K), dtype=torch.uint8, device="cuda"), torch.empty_like(z)
+        ops.pack8(z, q, s)
+        ops.linear_grad_x(dz, w, dx, q=q, s=s, act=act)
+        ops.sync()
+        assert ops.stats()["form"] == form
+        bad = torch.zeros(M, K, dtype=torch.bool, device="cuda")
+        bad[3, 32:64] = bad[M - 1, (K - 1) // 32 * 32:] = True
+        assert torch.equal(dx.isnan(), bad)
+
+
 @pytest.mark.parametrize("act", [R.NONE, R.SILU, R.GELU, R.SIGMOID, R.TANH, R.RELU])
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 def test_activation_and_derivative_from_eight_bits(ops, act, dtype):
