@@ -379,13 +379,18 @@ int lf_delta_step_static(const float* w_up, const float* delta_up, const float* 
  * stands for the width (contiguous rows), any other value must be at least the width and a
  * multiple of 8 (of 4 for LF_F32).  Weights w [n_out][n_in], their gradients and the 8-bit arrays
  * are contiguous.  Bias, gain and their gradients are float32.  Every element is computed in fp32
- * from the stored inputs and rounded once, on its way out.
+ * from the stored inputs and rounded once, on its way out, with one exception: lf_linear_grad_w from
+ * 8 bits rounds sigma(z) to `dtype` before the product (16-bit operands are what the tensor cores take, and
+ * what the layer itself was given).  Products are added in fp32 accumulators that truncate: up to 1e-7 of
+ * a sum of one sign for 16 terms, at most 3e-6 in fp32 results, 1e-4 in f16 and 4e-4 in bf16 ones,
+ * however long the contraction.
  *
  * 8-bit form of a matrix [tokens][n]:  q [tokens][n] bytes, s [tokens][(n + 31) / 32] bytes.  Groups
  * of 32 consecutive columns of a row (the last one may be shorter) share the power of two 2^e, e >=
  * -127 the smallest integer with max|v| <= 448 * 2^e; s holds e + 127 and q the e4m3 numbers
- * nearest to v * 2^-e (ties to even).  The value q * 2^e has four significant bits, so it is exact
- * in bf16 and the tensor cores can take it as it is.  A group that holds an infinity or a NaN gets
+ * nearest to v * 2^-e (ties to even).  The value q * 2^e has four significant bits, so the tensor
+ * cores can take it as it is: it is exact in bf16 from s = 3 up (below, its last bits may be smaller than
+ * bf16's smallest number), and in f16 where that type's range holds it.  A group that holds an infinity or a NaN gets
  * s = 255 and reads back as NaN throughout; sigma and sigma' of it are NaN (LF_ACT_NONE does not look).
  *
  * tokens = 0 is legal everywhere (matrices over tokens may then be NULL): nothing is written, except

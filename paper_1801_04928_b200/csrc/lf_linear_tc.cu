@@ -16,7 +16,7 @@
 //   Split pairs (k_product_pair_split): 256 x 256 tiles of CTA pairs, two pairs to a cluster and half of the
 //     contraction each, for what lies between.
 // What bounds them: large products the chip's power limit (8192 x 4096 -> 16384 in a loop: 1.35 PFLOP/s without an
-// activation, 1.28 with GELU; the tensor cores are at work 85 % of the time in a single launch); middle ones the fetch
+// activation, 1.25 to 1.33 with GELU, by the card; the tensor cores are at work 85 % of the time in a single launch); middle ones the fetch
 // of operands from L2; small ones launch, first loads and the meeting of the parts (5 to 6 us for a small layer, of
 // which 2.3 is the launch).  Copies that reach several CTAs of a cluster at once would relieve the fetch; they are
 // left out because operands may be any memory that the caller's device can address.
@@ -1305,7 +1305,7 @@ lt_choice lt_choose(const lf_ops* o, const lf_product& p, int n_k)
     const int one_fill = lt_one_fill(p);
     for (int splits = 1; splits <= 8 && splits <= n_k; splits *= 2) {
         const double part = (double)((n_k + splits - 1) / splits);
-        if (part > one_fill && splits < 8) continue;
+        if (part > one_fill && splits < 8) continue;               // (of more than one fill there are copies of eight parts)
         const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
         const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
         const long long ctas = m128 * n128 * splits;

@@ -32,8 +32,8 @@ __device__ __forceinline__ float row_sum(float v, float* red)
 // A block of TPR threads takes one row at a time, VPT vectors of eight columns per thread: the row stays
 // in registers between the sum and the scaling, so x and residual are read once.  With few rows a row has as many
 // threads as vectors (one row of 4096: 2.6 us, a launch), with many four vectors per thread, for fewer
-// barriers and more loads in flight.  Bound by memory: 16384 x 4096 bf16 with residual, h, y and y in 8 bits 95 us,
-// 6.35 TB/s.
+// barriers and more loads in flight.  Bound by memory: 16384 x 4096 bf16 with residual, h, y and y in 8 bits 95 to
+// 102 us by the card, 6.0 to 6.35 TB/s.
 template <typename T, int TPR, int VPT>
 __global__ void __launch_bounds__(TPR) k_rms_norm(const lf_rms_norm_args a)
 {
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(TPR) k_rms_norm(const lf_rms_norm_args a)
 // the top of the loop instead, 16384 x 8192 took 283 us, 3.8 TB/s.  Both row sums share one exchange, in
 // buffers that alternate, so a row has one barrier.  The gain's gradient stays in registers, eight
 // columns per vector; the groups of a block add theirs at the end, one partial row per block.  16384 x 8192 bf16 with
-// dres: 200 us, 5.4 TB/s; what is left is the chain load, sums, barrier, results of a row, of which a
+// dres: 194 to 208 us by the card, 5.2 to 5.5 TB/s; what is left is the chain load, sums, barrier, results of a row, of which a
 // multiprocessor overlaps two (blocks of 512 threads: 212 us; one block with a ring twice as deep: 265).
 __device__ __forceinline__ void cp_async16(unsigned dst, const void* src)
 {
@@ -365,8 +365,8 @@ __device__ __forceinline__ void colsum_block(const T* x, long long ld, int token
 // Threads run along the row, W columns each (16 in 256-bit accesses where widths, strides and addresses allow it, else
 // 8); a block has 256 / lanes rows side by side, lanes = 2^lanes_log2 >= the row's pieces (at most 256: wider rows take
 // several blocks), and walks down the matrix, ROWS_AT_ONCE rows at a time, all loads ahead of the first use.
-// 8192 x 16384 bf16: packed in 61 us (6.7 TB/s), read back in 64 (6.3), as GELU in 79 (5.1: the unit for exponentials
-// and reciprocals is 81 % busy), applied to a gradient with GELU' in 115 (5.9).
+// 8192 x 16384 bf16: packed in 61 to 64 us (6.4 to 6.7 TB/s), read back in 65 (6.2), as GELU in 73 (5.6: the unit for
+// exponentials and reciprocals is 82 % busy), applied to a gradient with GELU' in 112 (6.0).
 constexpr int ROWS_AT_ONCE = 4, ROWS_GRAD = 2;       // (two where a second matrix is read: registers)
 template <int W> struct bytes_of;                // W e4m3 numbers
 template <> struct bytes_of<16> { typedef uint4 type; };
@@ -511,7 +511,9 @@ __global__ void __launch_bounds__(256) k_unpack8(const unsigned char* q, const u
 }
 
 // What a weight gradient needs beside its product, in one launch: the column sums of dz (the first sum_x * sum_y
-// blocks) and the layer's input unpacked (the others).
+// blocks) and the layer's input unpacked (the others).  sigma(z) is rounded to T here, which the product's operands are: it is the
+// number that the layer was given in the forward pass.  The gradient is then 2.8e-4 off the one of an exact sigma (f16, 70 x 520 ->
+// 1024) where its own rounding is 2.1e-4, in bf16 (8192 x 16384 -> 4096) 1.9e-3 where that is 1.7e-3.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) k_grad_w_prepare(const T* dz, long long ld_dz, int tokens, int n_out, float* partial, unsigned* counters,
                                                         float* gb, int sum_x, int sum_y, const unsigned char* q, const unsigned char* s, int n_in,
