@@ -336,6 +336,24 @@ def test_long_contractions_in_sixteen_bits_grad_w(ops, M, K, N, form):
     _check_long("gw", gw[:64], dz[:, :64].to(R.D).t() @ x.to(R.D), M)
 
 
+# one fill of the accumulator and a little, with everything that the epilogues do (16384 terms of f16 and 65536 of bf16 a part, 16384 a warp)
+@pytest.mark.parametrize("M,K,N,dtype,act,form", [
+    (5, 262160, 72, BF16, R.GELU, lf.LF_FORM_STREAM), (13, 196680, 40, F16, R.SILU, lf.LF_FORM_STREAM), (40, 131080, 136, F16, R.TANH, lf.LF_FORM_SPLIT),
+    (1030, 16392, 2056, F16, R.GELU, lf.LF_FORM_PAIRS), (1030, 16392, 3080, F16, R.NONE, lf.LF_FORM_PAIRS), (1030, 65600, 2056, BF16, R.SILU, lf.LF_FORM_PAIRS)])
+@pytest.mark.parametrize("options", [False, True])
+def test_long_contractions_and_their_epilogues(ops, M, K, N, dtype, act, form, options):
+    _linear(ops, M, K, N, dtype, act, residual=options, ckpt=options, ld_extra=8 if options else 0, form=form)
+
+
+@pytest.mark.parametrize("M,K,N,dtype,act,gw,forms", [
+    (1030, 2056, 16392, F16, R.GELU, F16, (lf.LF_FORM_PAIRS, None)), (1030, 2056, 65544, BF16, R.RELU, BF16, (lf.LF_FORM_PAIRS, None)),
+    (40, 136, 131080, F16, R.SIGMOID, F32, (lf.LF_FORM_SPLIT, None)), (131080, 72, 64, F16, R.NONE, F16, (None, lf.LF_FORM_SPLIT)),
+    (16400, 1544, 2056, F16, R.TANH, F16, (None, lf.LF_FORM_PAIRS))])
+def test_long_contractions_backward(ops, M, K, N, dtype, act, gw, forms):
+    with lf.Operators(lf.lf_ops_workspace(M, K)) as o:
+        _backward(o, M, K, N, dtype, act, gw, add=act != R.GELU, forms=forms)
+
+
 @pytest.mark.parametrize("M,K,N", [(5, 16, 24), (40, 16, 24)])
 @pytest.mark.parametrize("act", [R.GELU, R.SILU, R.SIGMOID, R.TANH, R.NONE])
 def test_gradients_against_central_differences(ops, M, K, N, act):
