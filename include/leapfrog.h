@@ -382,7 +382,7 @@ int lf_delta_step_static(const float* w_up, const float* delta_up, const float* 
  * from the stored inputs and rounded once, on its way out, with one exception: lf_linear_grad_w from
  * 8 bits rounds sigma(z) to `dtype` before the product (16-bit operands are what the tensor cores take, and
  * what the layer itself was given).  Products are added in fp32 accumulators that truncate: up to 1e-7 of
- * a sum of one sign for 16 terms, at most 3e-6 in fp32 results, 1e-4 in f16 and 4e-4 in bf16 ones,
+ * a sum of one sign for 16 terms, at most 3e-6 in fp32 results, 2e-4 in f16 and 4e-4 in bf16 ones,
  * however long the contraction.
  *
  * 8-bit form of a matrix [tokens][n]:  q [tokens][n] bytes, s [tokens][(n + 31) / 32] bytes.  Groups

@@ -24,9 +24,10 @@
 // The tensor core adds into its accumulator by truncation: over terms of one sign 1.0e-7 of the sum per instruction
 // (16 terms), always towards zero.  An accumulator therefore takes a limited number of stages (lt_fill), and the fills are
 // added in registers with round-to-nearest: 8 stages, 3e-6, for an fp32 result, which a weight gradient over thousands of
-// tokens would show; 256 stages, 1.0e-4, for f16 and 1024, 4.1e-4, for bf16, less than half of the smallest half
-// unit of those types (2.4e-4, 2.0e-3).  Only contractions beyond 16384 and 65536 have more than one fill, in copies of
-// the kernels made for them.  (Without a limit f16 results were 4.2e-4 short over 65536 terms, 8.4e-4 over 2^20 in eight parts.)
+// tokens would show; 512 stages, 2.0e-4, for f16 and 1024, 4.1e-4, for bf16, below the smallest half unit of those
+// types (2.4e-4, 2.0e-3).  Only contractions beyond 32768 and 65536 have more than one fill, in copies of
+// the kernels made for them.  (Without a limit f16 results were 4.2e-4 short over 65536 terms, 8.4e-4 over 2^20 in eight parts.  With 256
+// stages 2048 x 28672 -> 8192 took 890 us instead of 700, as only 256-row tiles have an accumulator to spare.)
 // All waits are bounded; on expiry the status word is raised and the launch drains and ends.
 #include "lf_ops_internal.h"
 #include "lf_ptx.cuh"
@@ -58,7 +59,7 @@ constexpr size_t LS_SMEM = (size_t)LS_STAGES * LT_STAGE_BYTES + LS_TILE_BYTES + 
 
 // K stages that one accumulator takes of a result of type OUT
 template <typename OUT> struct lt_fill { static constexpr int stages = 8; };
-template <> struct lt_fill<__half> { static constexpr int stages = 256; };
+template <> struct lt_fill<__half> { static constexpr int stages = 512; };
 template <> struct lt_fill<__nv_bfloat16> { static constexpr int stages = 1024; };
 
 struct LtParams {
