@@ -530,6 +530,105 @@ int lf_unpack8(lf_ops* ops, int dtype, int act, int tokens, int n, const unsigne
 int lf_act_backward(lf_ops* ops, int dtype, int act, int tokens, int n, const void* dy, long long ld_dy,
                     const unsigned char* q, const unsigned char* s, void* dz, long long ld_dz);
 
+/* ================================================================================================
+ * Layer norm, products in 8 bits with a scale for each block of 128, and the loss against a teacher's
+ * top logits: the output layer of a network that learns from a larger one.  Same handle, same rules as above
+ * (rows, strides, alignment, tokens = 0, order of additions) but where said otherwise.
+ *
+ * Blocks of 128.  An operand of such a product is a matrix of e4m3 bytes, rows along the contraction, row stride ld a
+ * multiple of 16 bytes (0 stands for the width rounded up to one; what lies behind a row's end is neither read nor
+ * written).  128 consecutive values of a row, or a tile of 128 rows x 128 columns, share a float32 scale; blocks and tiles
+ * at the end may be smaller.  Scales of rows: [ceil(width / 128)][rows] (a line for each block of the contraction);
+ * scales of tiles: [ceil(rows / 128)][ceil(width / 128)].  lf_pack_blocks, lf_pack_tiles and lf_layer_norm make the scale the power
+ * of two 2^e, e >= -126 the smallest integer with max|v| <= 448 * 2^e, and the bytes the e4m3 numbers nearest to v * 2^-e (ties
+ * to even); a block that holds an infinity or a NaN gets a NaN for its scale.  lf_product_blocks takes any
+ * float32 numbers as scales.
+ * ================================================================================================ */
+typedef struct lf_layer_norm_args {  /* h = x + residual, m = mean h, r = 1 / sqrt(mean (h - m)^2 + eps);  y = (h - m) r (.) gain + bias */
+    int dtype;                       /* of x, residual, h, y: any                              */
+    int tokens, n;                   /* n <= 16384                                             */
+    float eps;                       /* >= 0, finite                                           */
+    const void* x; long long ld_x;
+    const void* residual; long long ld_residual;   /* or NULL                                  */
+    const float* gain;               /* [n]                                                    */
+    const float* bias;               /* [n] or NULL                                            */
+    void* h; long long ld_h;         /* or NULL                                                */
+    void* y; long long ld_y;         /* or NULL (then q, s are needed)                         */
+    unsigned char* q; long long ld_q;   /* q and s both or neither: y in blocks of 128 along its rows, */
+    float* s;                        /*   from the unrounded y                                  */
+    float *mean, *rstd;              /* [tokens], m and r; both or neither                     */
+} lf_layer_norm_args;                /* h or y may be x or residual                            */
+
+typedef struct lf_layer_norm_backward_args {
+    /* with c = (h - m) r, u = gain (.) dy:
+     *   dh = r (u - mean u - c mean(u (.) c)) + dres,   dgain = sum over tokens of dy (.) c,   dbias = sum over tokens of dy */
+    int dtype;                       /* of dy, h, dres, dh: any                                */
+    int tokens, n;
+    const void* dy; long long ld_dy;
+    const void* h; long long ld_h;
+    const float* gain;
+    const float *mean, *rstd;        /* as lf_layer_norm wrote them                            */
+    const void* dres; long long ld_dres;   /* gradient that reaches h along the residual path, or NULL */
+    void* dh; long long ld_dh;
+    float *dgain, *dbias;            /* [n], each or NULL                                      */
+} lf_layer_norm_backward_args;       /* dh may be dy, h or dres                                */
+
+typedef struct lf_pack_blocks_args {
+    int dtype;                       /* of x: any                                              */
+    int tokens, n;
+    const void* x; long long ld_x;   /* [tokens][n]                                            */
+    unsigned char* q; long long ld_q;   /* [tokens][n], q and s both or neither                */
+    float* s;                        /* lf_pack_blocks [ceil(n/128)][tokens]; lf_pack_tiles [ceil(tokens/128)][ceil(n/128)] */
+    unsigned char* qt; long long ld_qt; /* [n][tokens], qt and st both or neither: the transposed matrix */
+    float* st;                       /* lf_pack_blocks [ceil(tokens/128)][n] (blocks along a column of x); lf_pack_tiles [ceil(n/128)][ceil(tokens/128)] */
+} lf_pack_blocks_args;               /* one pair at least                                      */
+
+typedef struct lf_product_blocks_args {
+    /* d[i][j] = sum over blocks c of sa[c][i] sb[c][j] sum over k of block c of a[i][k] b[j][k], + bias[j] + add[i][j].
+     * The product of two scales is formed first, in fp32; a block's 128 terms are added by the tensor cores, the blocks in
+     * fp32 with round-to-nearest, in their order. */
+    int out_dtype;                   /* of d and add: any (add: not LF_F32)                    */
+    int tokens, n_in, n_out;         /* rows of a and d; contraction (any length); columns of d: a multiple of 8 */
+    const unsigned char* a; long long ld_a; const float* sa;   /* [tokens][n_in], scales of rows */
+    const unsigned char* b; long long ld_b; const float* sb;   /* [n_out][n_in], scales of rows or, where b_tiles != 0, of tiles */
+    int b_tiles;
+    const float* bias;               /* [n_out] or NULL                                        */
+    const void* add; long long ld_add;   /* [tokens][n_out] or NULL                            */
+    void* d; long long ld_d;         /* [tokens][n_out]                                        */
+} lf_product_blocks_args;
+
+typedef struct lf_distill_args {
+    /* p = softmax over a token's entries k of value[k] / T,  q = softmax over the vocabulary of z / T:
+     *   loss = weight T^2 sum over k of p_k (ln p_k - ln q_index[k]),   lse = ln sum over v of e^(z_v / T),
+     *   dz_v = weight T (q_v - sum of p_k with index[k] = v).
+     * An entry whose index is negative or whose value is -infinity does not exist; of a token without entries loss
+     * and dz are 0.  An index may come several times.  One beyond the vocabulary makes the token's loss and dz NaN.  A token of
+     * weight 0 has loss and dz 0 whatever its logits hold. */
+    int dtype;                       /* of z, dz: any                                          */
+    int tokens, vocab, top;          /* vocab: any number from 1, top: 1 .. LF_DISTILL_MAX_TOP */
+    float temperature;               /* T, > 0, finite                                         */
+    const void* z; long long ld_z;   /* [tokens][vocab]; rows may begin at any element, ld any number >= vocab (0: vocab) */
+    const int* index;                /* [tokens][top]                                          */
+    const float* value;              /* [tokens][top], the teacher's logits                    */
+    const float* weight;             /* [tokens] or NULL (1): the token's weight; lf_distill_backward: times the gradient of its loss */
+    float* loss;                     /* [tokens]; not used by lf_distill_backward              */
+    float* lse;                      /* [tokens]; lf_distill: written, or NULL; lf_distill_backward: read */
+    void* dz; long long ld_dz;       /* [tokens][vocab], as z; lf_distill: or NULL (gradient of the sum of the losses).  May be z itself */
+} lf_distill_args;
+
+#define LF_DISTILL_MAX_TOP 512
+
+int lf_layer_norm(lf_ops* ops, const lf_layer_norm_args* args);
+int lf_layer_norm_backward(lf_ops* ops, const lf_layer_norm_backward_args* args);
+int lf_pack_blocks(lf_ops* ops, const lf_pack_blocks_args* args);
+/* the same for weights: a scale for each tile of 128 x 128, which serves the transposed matrix too */
+int lf_pack_tiles(lf_ops* ops, const lf_pack_blocks_args* args);
+int lf_product_blocks(lf_ops* ops, const lf_product_blocks_args* args);
+/* loss, lse and, where dz is given, the gradient, with z read once from memory */
+int lf_distill(lf_ops* ops, const lf_distill_args* args);
+/* dz from z and lse */
+int lf_distill_backward(lf_ops* ops, const lf_distill_args* args);
+
 /* Static English text for a status code. */
 const char* lf_strerror(int status);
 

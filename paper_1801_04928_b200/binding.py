@@ -33,6 +33,7 @@ LF_TC_TILING_AUTO, LF_TC_TILING_ONE_SM, LF_TC_TILING_TWO_SM = 0, 1, 2
 LF_F32, LF_BF16, LF_F16 = 0, 1, 2
 LF_ACT_NONE, LF_ACT_SILU, LF_ACT_GELU = 3, 4, 5
 LF_FORM_STREAM, LF_FORM_SPLIT, LF_FORM_PAIRS, LF_FORM_SPLIT_PAIRS = 1, 2, 3, 4
+LF_DISTILL_MAX_TOP = 512
 LF_DELTA_MATH_AUTO, LF_DELTA_MATH_FP32, LF_DELTA_MATH_3XTF32, LF_DELTA_MATH_TF32_BF16 = 0, 1, 2, 3
 
 EXPORTS = ("lf_create", "lf_create_widths", "lf_set_stream", "lf_set_option", "lf_forward", "lf_backward",
@@ -40,7 +41,8 @@ EXPORTS = ("lf_create", "lf_create_widths", "lf_set_stream", "lf_set_option", "l
            "lf_strerror", "lf_version", "lf_destroy", "lf_delta_step_static",
            "lf_ops_create", "lf_ops_workspace", "lf_ops_set_stream", "lf_ops_set_option", "lf_ops_get_stats",
            "lf_ops_last_cuda_error", "lf_ops_sync", "lf_ops_destroy", "lf_linear", "lf_linear_grad_x", "lf_linear_grad_w",
-           "lf_rms_norm", "lf_rms_norm_backward", "lf_pack8", "lf_unpack8", "lf_act_backward")
+           "lf_rms_norm", "lf_rms_norm_backward", "lf_pack8", "lf_unpack8", "lf_act_backward",
+           "lf_layer_norm", "lf_layer_norm_backward", "lf_pack_blocks", "lf_pack_tiles", "lf_product_blocks", "lf_distill", "lf_distill_backward")
 
 
 class lf_stats(ctypes.Structure):
@@ -72,6 +74,17 @@ lf_rms_norm_args = _struct("lf_rms_norm_args", ("i", "dtype tokens n"), ("f", "e
                            ("l", "ld_residual"), ("p", "gain h"), ("l", "ld_h"), ("p", "y"), ("l", "ld_y"), ("p", "q s"))
 lf_rms_norm_backward_args = _struct("lf_rms_norm_backward_args", ("i", "dtype tokens n"), ("f", "eps"), ("p", "dy"), ("l", "ld_dy"), ("p", "h"),
                                     ("l", "ld_h"), ("p", "gain dres"), ("l", "ld_dres"), ("p", "dh"), ("l", "ld_dh"), ("p", "dgain"))
+lf_layer_norm_args = _struct("lf_layer_norm_args", ("i", "dtype tokens n"), ("f", "eps"), ("p", "x"), ("l", "ld_x"), ("p", "residual"),
+                             ("l", "ld_residual"), ("p", "gain bias h"), ("l", "ld_h"), ("p", "y"), ("l", "ld_y"), ("p", "q"), ("l", "ld_q"),
+                             ("p", "s mean rstd"))
+lf_layer_norm_backward_args = _struct("lf_layer_norm_backward_args", ("i", "dtype tokens n"), ("p", "dy"), ("l", "ld_dy"), ("p", "h"), ("l", "ld_h"),
+                                      ("p", "gain mean rstd dres"), ("l", "ld_dres"), ("p", "dh"), ("l", "ld_dh"), ("p", "dgain dbias"))
+lf_pack_blocks_args = _struct("lf_pack_blocks_args", ("i", "dtype tokens n"), ("p", "x"), ("l", "ld_x"), ("p", "q"), ("l", "ld_q"), ("p", "s qt"),
+                              ("l", "ld_qt"), ("p", "st"))
+lf_product_blocks_args = _struct("lf_product_blocks_args", ("i", "out_dtype tokens n_in n_out"), ("p", "a"), ("l", "ld_a"), ("p", "sa b"), ("l", "ld_b"),
+                                 ("p", "sb"), ("i", "b_tiles"), ("p", "bias add"), ("l", "ld_add"), ("p", "d"), ("l", "ld_d"))
+lf_distill_args = _struct("lf_distill_args", ("i", "dtype tokens vocab top"), ("f", "temperature"), ("p", "z"), ("l", "ld_z"),
+                          ("p", "index value weight loss lse dz"), ("l", "ld_dz"))
 lf_ops_stats = _struct("lf_ops_stats", ("i", "sm_count launches form splits"), ("u", "device_status"), ("i", "device"), ("l", "workspace_bytes"))
 
 
@@ -108,7 +121,8 @@ def _load() -> ctypes.CDLL:
     lib.lf_ops_last_cuda_error.argtypes = [vp]
     lib.lf_ops_sync.argtypes = [vp]
     lib.lf_ops_destroy.argtypes = [vp]
-    for name in ("lf_linear", "lf_linear_grad_x", "lf_linear_grad_w", "lf_rms_norm", "lf_rms_norm_backward"):
+    for name in ("lf_linear", "lf_linear_grad_x", "lf_linear_grad_w", "lf_rms_norm", "lf_rms_norm_backward", "lf_layer_norm",
+                 "lf_layer_norm_backward", "lf_pack_blocks", "lf_pack_tiles", "lf_product_blocks", "lf_distill", "lf_distill_backward"):
         getattr(lib, name).argtypes = [vp, ctypes.c_void_p]
     lib.lf_pack8.argtypes = [vp, i, i, i, vp, ll, vp, vp]
     lib.lf_unpack8.argtypes = [vp, i, i, i, i, vp, vp, vp, ll]
@@ -400,13 +414,13 @@ def lf_ops_destroy(ops) -> int:
     return _lib.lf_ops_destroy(ops)
 
 
-def _by_struct(name):
+def _by_struct(name, args_name=None):
     fn = getattr(_lib, name)
 
     def call(ops, args) -> int:
         return fn(ops, None if args is None else ctypes.addressof(args))
     call.__name__ = name
-    call.__doc__ = f"{name}(ops, args): `args` is a {name}_args."
+    call.__doc__ = f"{name}(ops, args): `args` is a {args_name or name + '_args'}."
     return call
 
 
@@ -415,6 +429,13 @@ lf_linear_grad_x = _by_struct("lf_linear_grad_x")
 lf_linear_grad_w = _by_struct("lf_linear_grad_w")
 lf_rms_norm = _by_struct("lf_rms_norm")
 lf_rms_norm_backward = _by_struct("lf_rms_norm_backward")
+lf_layer_norm = _by_struct("lf_layer_norm")
+lf_layer_norm_backward = _by_struct("lf_layer_norm_backward")
+lf_pack_blocks = _by_struct("lf_pack_blocks")
+lf_pack_tiles = _by_struct("lf_pack_tiles", "lf_pack_blocks_args")
+lf_product_blocks = _by_struct("lf_product_blocks")
+lf_distill = _by_struct("lf_distill")
+lf_distill_backward = _by_struct("lf_distill_backward", "lf_distill_args")
 
 
 def lf_pack8(ops, dtype: int, tokens: int, n: int, x, ld_x: int, q, s) -> int:
@@ -534,6 +555,55 @@ class Operators:
         failed = self._m.act_backward(_f, self._a, dy, q, s, dz, act, self._device)
         if failed is not None:
             self._raise("lf_act_backward", failed)
+
+    def layer_norm(self, x, gain, bias=None, y=None, residual=None, h=None, q=None, s=None, mean=None, rstd=None, eps: float = 1e-5,
+                   _f=_entry("lf_layer_norm")):
+        """h = x + residual; y = (h - mean(h)) * rstd * gain + bias, rstd = 1 / sqrt(mean((h - mean(h))^2) + eps), in x's type and / or in
+        8 bits (q [tokens, n], s [ceil(n / 128), tokens]); mean, rstd [tokens]: what the backward pass reads."""
+        failed = self._m.layer_norm(_f, self._a, x, gain, bias, y, residual, h, q, s, mean, rstd, eps, self._device)
+        if failed is not None:
+            self._raise("lf_layer_norm", failed)
+
+    def layer_norm_backward(self, dy, h, gain, mean, rstd, dh, dgain=None, dbias=None, dres=None, _f=_entry("lf_layer_norm_backward")):
+        """Gradient of layer_norm's y with respect to h (plus dres), gain and bias."""
+        failed = self._m.layer_norm_backward(_f, self._a, dy, h, gain, mean, rstd, dh, dgain, dbias, dres, self._device)
+        if failed is not None:
+            self._raise("lf_layer_norm_backward", failed)
+
+    def pack_blocks(self, x, q=None, s=None, qt=None, st=None, _f=_entry("lf_pack_blocks")):
+        """x [tokens, n] in 8 bits with a scale for each 128 of a row: q [tokens, n], s [ceil(n / 128), tokens]; and / or its transpose with a
+        scale for each 128 tokens: qt [n, tokens], st [ceil(tokens / 128), n].  Rows of q and qt begin 16 bytes apart or a multiple."""
+        failed = self._m.pack_blocks(_f, self._a, x, q, s, qt, st, self._device)
+        if failed is not None:
+            self._raise("lf_pack_blocks", failed)
+
+    def pack_tiles(self, w, q=None, s=None, qt=None, st=None, _f=_entry("lf_pack_tiles")):
+        """w [rows, n] in 8 bits with a scale for each tile of 128 x 128: q [rows, n], s [ceil(rows / 128), ceil(n / 128)]; and / or its
+        transpose, qt [n, rows], st [ceil(n / 128), ceil(rows / 128)]."""
+        failed = self._m.pack_tiles(_f, self._a, w, q, s, qt, st, self._device)
+        if failed is not None:
+            self._raise("lf_pack_tiles", failed)
+
+    def product_blocks(self, a, sa, b, sb, d, bias=None, add=None, _f=_entry("lf_product_blocks")):
+        """d = a b^T + bias + add of 8-bit matrices a [tokens, n_in], b [n_out, n_in]; sa [ceil(n_in / 128), tokens], sb
+        [ceil(n_in / 128), n_out] (pack_blocks) or [ceil(n_out / 128), ceil(n_in / 128)] (pack_tiles).  The layer's three products:
+        x and w give y; dz and w's transpose give dx; the transposes of dz and x give w's gradient."""
+        failed = self._m.product_blocks(_f, self._a, a, sa, b, sb, d, bias, add, self._device)
+        if failed is not None:
+            self._raise("lf_product_blocks", failed)
+
+    def distill(self, z, index, value, loss, lse=None, weight=None, dz=None, temperature: float = 1.0, _f=_entry("lf_distill")):
+        """loss [tokens] of logits z [tokens, vocab] against the teacher's top logits value [tokens, top] at index (int32; negative: no
+        entry): weight T^2 KL(softmax(value / T) || softmax(z / T)); lse [tokens] for the backward pass; dz: the gradient at once."""
+        failed = self._m.distill(_f, self._a, z, index, value, loss, lse, weight, dz, temperature, self._device)
+        if failed is not None:
+            self._raise("lf_distill", failed)
+
+    def distill_backward(self, z, index, value, lse, dz, weight=None, temperature: float = 1.0, _f=_entry("lf_distill_backward")):
+        """dz of the losses that distill gave; weight: times the gradient of each token's loss."""
+        failed = self._m.distill_backward(_f, self._a, z, index, value, None, lse, weight, dz, temperature, self._device)
+        if failed is not None:
+            self._raise("lf_distill_backward", failed)
 
     def close(self):
         if self._h is not None:

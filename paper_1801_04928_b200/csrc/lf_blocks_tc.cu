@@ -1,0 +1,651 @@
+// Products of 8-bit operands with a scale for each block of 128 of the contraction, on the 5th-generation tensor cores:
+//     D[m][n] = sum_c sa[c][m] sb(c, n) sum_{k in block c} A[m][k] B[n][k] + bias[n] + add[m][n]
+// sb(c, n) is one number for 128 columns (tiles of weights) or one for each column (gradients of weights).
+// A stage is one block: 128 e4m3 numbers are 128 bytes, a row of an operand block in the 128-byte swizzle, four
+// instructions of 32 each.  The products of a block start a new accumulator; the warps that finish the tile take it from tensor
+// memory, multiply it by the scales and add it to their own fp32 registers with round-to-nearest, while the tensor cores fill
+// the other accumulator with the next block.  So scales are any fp32 numbers and nothing but 128 terms is ever added
+// by the tensor core's truncating adder.
+//
+// Two kernels, chosen by an estimate of each one's time (lb_choose):
+//   CTA pairs (k_blocks_pair): tcgen05.mma.cta_group::2, 256 x 256 tiles, persistent.  A CTA's 128 x 256 fp32
+//     sums fill half of its registers, which is why tiles are not larger.
+//   Split tiles (k_blocks_split): one CTA per 128 x 128 tile and part of the contraction (1, 2, 4 or 8 parts), whose
+//     CTAs form a cluster and add their parts through distributed shared memory.
+// All waits are bounded; on expiry the status word is raised and the launch drains and ends.
+#include "lf_ops_internal.h"
+#include "lf_product_tc.cuh"
+#include "lf_ptx.cuh"
+#include "lf_rows.cuh"
+
+namespace {
+
+using namespace lfrow;
+
+constexpr int LB_BK = 128;                               // a block of the contraction, bytes and numbers
+constexpr int LB_RING_BYTES = LT_STAGES * LT_STAGE_BYTES;
+constexpr int LB_EPI_BYTES = 8 * 4096;                   // 32 rows x 128 bytes per warp that finishes
+constexpr int LB_THREADS = 384;                          // a warpgroup with producer and issuer, two that finish
+constexpr int LB_REGS_LOW = 56, LB_REGS_HIGH = 224;      // 56 + 2 * 224 = 3 * 168: what the block was launched with
+constexpr size_t LB_SMEM = (size_t)LB_RING_BYTES + LB_EPI_BYTES + 1024 + 512;
+constexpr int LBS_THREADS = 512, LBS_STAGES = 4, LBS_LD = 132;
+constexpr int LBS_TILE_BYTES = 128 * LBS_LD * 4;
+constexpr int LBS_SCALE_BYTES = 8 * 2 * 64 * 4;          // column scales of two blocks per warp
+constexpr size_t LBS_SMEM = (size_t)LBS_STAGES * LT_STAGE_BYTES + LBS_TILE_BYTES + LBS_SCALE_BYTES + 1024 + 512;
+
+struct LbParams {
+    int M, N, K;
+    int tiles_m, tiles_n, band;
+    int stages_per_split;
+    unsigned idesc;
+    const float *sa, *sb;
+    const float* bias;
+    const void* add; long long ld_add;
+    void* d; long long ld_d;
+    int wide_add;                      // 256-bit accesses fit add
+    unsigned* status;
+    unsigned long long budget_ns;
+    int withhold;
+};
+
+template <bool PAIR>
+__device__ __forceinline__ void lb_mma(unsigned d_tmem, unsigned long long a, unsigned long long b, unsigned idesc, unsigned acc)
+{
+    if (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// the four instructions of a stage
+template <bool PAIR>
+__device__ __forceinline__ void lb_products(unsigned d_tmem, unsigned a_addr, unsigned b_addr, unsigned idesc)
+{
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+        lb_mma<PAIR>(d_tmem, lt_desc<false>(a_addr + lt_step<false>(kk)), lt_desc<false>(b_addr + lt_step<false>(kk)), idesc, kk > 0 ? 1u : 0u);
+}
+
+template <typename OUT> struct half_of { typedef OUT type; };          // type of `add`
+template <> struct half_of<float> { typedef __nv_bfloat16 type; };     // (none there)
+
+// acc += scale * the 32 columns of an accumulator in t; ROWS: the scales of the columns lie in shared memory
+template <bool ROWS>
+__device__ __forceinline__ void lb_scale_add(float* acc, const float* t, float sa, const float4* sb)
+{
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+        float2 lo, hi;
+        if (ROWS) {
+            const float4 b = sb[g];
+            lo = mul2(f2(sa), make_float2(b.x, b.y));
+            hi = mul2(f2(sa), make_float2(b.z, b.w));
+        } else {
+            lo = hi = f2(sa);
+        }
+        const float2 r0 = fma2(lo, make_float2(t[4 * g], t[4 * g + 1]), make_float2(acc[4 * g], acc[4 * g + 1]));
+        const float2 r1 = fma2(hi, make_float2(t[4 * g + 2], t[4 * g + 3]), make_float2(acc[4 * g + 2], acc[4 * g + 3]));
+        acc[4 * g] = r0.x; acc[4 * g + 1] = r0.y; acc[4 * g + 2] = r1.x; acc[4 * g + 3] = r1.y;
+    }
+}
+
+// ================================================================================================
+// CTA pairs
+// ================================================================================================
+// 32 rows x 128 columns of a tile, a row per lane: bias, residual, and whole lines out through the warp's 32 x 128
+// bytes of shared memory.
+template <typename OUT>
+__device__ __forceinline__ void lb_finish(float (&acc)[128], const LbParams& P, int row0, int col0, unsigned char* blk)
+{
+    typedef typename half_of<OUT>::type H;
+    const int lane = threadIdx.x & 31, row = row0 + lane;
+    float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (P.bias && col0 + 4 * lane < P.N) bias = *reinterpret_cast<const float4*>(P.bias + col0 + 4 * lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {                                // 32 columns at a time
+        const int col = col0 + 32 * j;
+        if (j % 2 == 0 && col >= P.N) break;
+        float* v = acc + 32 * j;
+        if (P.bias) {
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {                        // lane 8 j + g holds the bias of these four columns
+                v[4 * g] += __shfl_sync(0xFFFFFFFFu, bias.x, 8 * j + g);
+                v[4 * g + 1] += __shfl_sync(0xFFFFFFFFu, bias.y, 8 * j + g);
+                v[4 * g + 2] += __shfl_sync(0xFFFFFFFFu, bias.z, 8 * j + g);
+                v[4 * g + 3] += __shfl_sync(0xFFFFFFFFu, bias.w, 8 * j + g);
+            }
+        }
+        if (sizeof(OUT) == 2 && P.add && row < P.M) {
+            const H* from = static_cast<const H*>(P.add) + (size_t)row * P.ld_add + col;
+            unsigned r[16];
+            if (P.wide_add && col + 32 <= P.N) {
+                ld256(from, *reinterpret_cast<unsigned(*)[8]>(r));
+                ld256(from + 16, *reinterpret_cast<unsigned(*)[8]>(r + 8));
+            } else {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    uint4 u = make_uint4(0, 0, 0, 0);
+                    if (col + 8 * g < P.N) u = *reinterpret_cast<const uint4*>(from + 8 * g);
+                    r[4 * g] = u.x; r[4 * g + 1] = u.y; r[4 * g + 2] = u.z; r[4 * g + 3] = u.w;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 f = unpack2(r[i], H());
+                v[2 * i] += f.x; v[2 * i + 1] += f.y;
+            }
+        }
+        constexpr int PER = sizeof(OUT) == 2 ? 2 : 1;            // blocks of 32 columns per stored line
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float(&w)[8] = *reinterpret_cast<const float(*)[8]>(v + 8 * g);
+            // 16-byte units of a 128-byte line, turned by the row so that neither side meets a bank twice
+            if (sizeof(OUT) == 2) {
+                vec8<H> o;
+                o.set(w);
+                *reinterpret_cast<uint4*>(blk + lane * 128 + ((((j & 1) * 4 + g) ^ (lane & 7)) << 4)) = o.u;
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    *reinterpret_cast<float4*>(blk + lane * 128 + (((g * 2 + u) ^ (lane & 7)) << 4)) = make_float4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+            }
+        }
+        if (j % PER == PER - 1) {                               // a line of every row is complete: whole lines go out
+            __syncwarp();
+            constexpr int UC = 16 / (int)sizeof(OUT);           // columns of a 16-byte unit
+            const int cu = col - (PER - 1) * 32 + (lane & 7) * UC, r0 = row0 + (lane >> 3);
+            const unsigned char* from = blk + (lane >> 3) * 128;
+            OUT* to = static_cast<OUT*>(P.d) + (size_t)r0 * P.ld_d + cu;
+            const size_t step = (size_t)4 * P.ld_d;
+            uint4 u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)                         // row (lane >> 3) + 4 i: its turn alternates
+                u[i] = *reinterpret_cast<const uint4*>(from + i * 512 + (((lane & 7) ^ (((lane >> 3) + 4 * i) & 7)) << 4));
+            if (cu < P.N) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (r0 + 4 * i < P.M) *reinterpret_cast<uint4*>(to + i * step) = u[i];
+            }
+            __syncwarp();
+        }
+    }
+}
+
+template <typename OUT, bool ROWS>
+__global__ void __launch_bounds__(LB_THREADS, 1)
+k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const LbParams P)
+{
+    extern __shared__ unsigned char lb_smem_raw[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lb_smem_raw) + 1023u) & ~(uintptr_t)1023u);
+    unsigned char* epi = ring + LB_RING_BYTES;
+    LtShared* sh = reinterpret_cast<LtShared*>(epi + LB_EPI_BYTES);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned rank = lfptx::cluster_ctarank();
+    const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+    const int n_tiles = P.tiles_m * P.tiles_n;
+    const int n_k = (P.K + LB_BK - 1) / LB_BK;
+
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+        for (int i = 0; i < LT_STAGES; ++i) {
+            lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
+            lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            lfptx::mbar_init(lfptx::smem_u32(&sh->acc_full[i]), 1);
+            lfptx::mbar_init(lfptx::smem_u32(&sh->acc_empty[i]), 16);   // eight finishing warps of each CTA
+        }
+        sh->abort_flag = 0u;
+        sh->prog_it = 0u;
+        lfptx::mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(lfptx::smem_u32(&sh->tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    lfptx::tc_fence_before();
+    __syncthreads();
+    lfptx::cluster_sync_all();       // the peer's barriers exist before anything can arrive on them
+    lfptx::tc_fence_after();
+    const unsigned tmem_base = sh->tmem_base;
+    lf_grid_wait();                  // (by every thread: the bounded waits below do not count the time until then)
+    lf_grid_release();
+
+    if (warp < 4) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LB_REGS_LOW));
+      if (warp == 0) {
+        // ------------------------------ TMA producer: this CTA's halves -------------------------
+        if (lane == 0) {
+            unsigned it = 0;
+            bool ok = true;
+            for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+                int tm, tn;
+                lp_tile(t, P, tm, tn);
+                const int m0 = (tm * 2 + (int)rank) * 128, n0 = (tn * 2 + (int)rank) * 128;
+                for (int ks = 0; ks < n_k; ++ks, ++it) {
+                    const unsigned st = it % LT_STAGES, use = it / LT_STAGES;
+                    if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->empty[st]), (use - 1) & 1u, P, sh)) { ok = false; break; }
+                    const unsigned lbar = lfptx::smem_u32(&sh->full[st]);
+                    if (P.withhold && pair == 0 && rank == 1 && it == 0) continue;    // test hook
+                    if (rank == 0) lfptx::mbar_arrive_expect_tx(lbar, 2u * LT_STAGE_BYTES);
+                    const unsigned bar = lfptx::map_to_cta(lbar, 0);
+                    const unsigned dst = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
+                    lt_load<false, true>(dst, &map_a, bar, m0, ks * LB_BK);
+                    lt_load<false, true>(dst + LT_BLOCK_BYTES, &map_b, bar, n0, ks * LB_BK);
+                }
+            }
+            sh->prog_it = it;
+        }
+      } else if (warp == 1) {
+        // ------------------------------ MMA issuer (leader CTA) ---------------------------------
+        if (lane == 0 && rank == 0) {
+            unsigned it = 0;                    // stages, and accumulators, one for each
+            bool ok = true;
+            for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+                for (int ks = 0; ks < n_k; ++ks, ++it) {
+                    const unsigned ab = it & 1u, use = it >> 1, st = it % LT_STAGES;
+                    if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->acc_empty[ab]), (use - 1) & 1u, P, sh)) { ok = false; break; }
+                    if (!lt_wait(lfptx::smem_u32(&sh->full[st]), (it / LT_STAGES) & 1u, P, sh)) { ok = false; break; }
+                    lfptx::tc_fence_after();
+                    const unsigned a_addr = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
+                    lb_products<true>(tmem_base + ab * 256u, a_addr, a_addr + LT_BLOCK_BYTES, P.idesc);
+                    lt_commit<true>(lfptx::smem_u32(&sh->empty[st]));
+                    lt_commit<true>(lfptx::smem_u32(&sh->acc_full[ab]));
+                }
+            }
+        }
+      }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(LB_REGS_HIGH));
+        // ------------------------------ scales and epilogue (warps 4..11 of both CTAs) -----------
+        // A warp has one 32-lane quadrant (32 rows) and one half (128 columns, one tile of weights) of the accumulators.
+        const int quad = warp & 3, half = (warp - 4) >> 2;
+        const unsigned leader_acc_empty = lfptx::map_to_cta(lfptx::smem_u32(&sh->acc_empty[0]), 0);
+        unsigned char* blk = epi + (warp - 4) * 4096;
+        unsigned c = 0;
+        bool ok = true;
+        for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+            int tm, tn;
+            lp_tile(t, P, tm, tn);
+            const int row0 = (tm * 2 + (int)rank) * 128 + quad * 32, col0 = tn * 256 + half * 128, row = row0 + lane;
+            const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * 128u;
+            // scales of the next block, on their way while this one's products are waited for
+            const float* sa = P.sa + (row < P.M ? row : 0);
+            const float* sb = ROWS ? P.sb + min(col0 + 4 * lane, P.N - 4) : P.sb + (size_t)min(col0 >> 7, (P.N - 1) >> 7) * n_k;
+            const size_t sb_step = ROWS ? (size_t)P.N : 1;
+            float sa_next = *sa;
+            float4 sb_next = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (ROWS) sb_next = *reinterpret_cast<const float4*>(sb);
+            else sb_next.x = *sb;
+            float acc[128];
+#pragma unroll
+            for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+#pragma unroll 1
+            for (int ks = 0; ks < n_k; ++ks, ++c) {
+                const unsigned ab = c & 1u;
+                const float s = ROWS ? sa_next : sa_next * sb_next.x;
+                float4* mine = reinterpret_cast<float4*>(blk + (ks & 1) * 512);
+                if (ROWS) mine[lane] = sb_next;
+                if (ks + 1 < n_k) {
+                    sa += P.M;
+                    sb += sb_step;
+                    sa_next = *sa;
+                    if (ROWS) sb_next = *reinterpret_cast<const float4*>(sb);
+                    else sb_next.x = *sb;
+                }
+                if (ROWS) __syncwarp();
+                if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) { ok = false; break; }
+                lfptx::tc_fence_after();
+                float r[2][32];
+                const unsigned from = lane_addr + ab * 256u;
+                lfptx::tmem_ld32_async(from, r[0]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    lfptx::tmem_wait_ld32(r[j & 1]);
+                    if (j < 3) {
+                        lfptx::tmem_ld32_async(from + 32 * (j + 1), r[(j + 1) & 1]);
+                    } else {
+                        lfptx::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) lt_arrive_cluster(leader_acc_empty + ab * 8u);
+                    }
+                    lb_scale_add<ROWS>(acc + 32 * j, r[j & 1], s, mine + 8 * j);
+                }
+            }
+            if (!ok) break;
+            __syncwarp();
+            lb_finish<OUT>(acc, P, row0, col0, blk);
+        }
+    }
+
+    // Neither CTA may leave (or free tensor memory) while the other can still reach it.
+    lfptx::tc_fence_before();
+    __syncthreads();
+    lfptx::cluster_sync_all();
+    if (threadIdx.x == 0 && rank == 0) {
+        // A launch that was given up: wait, with a limit, for the operand loads of both CTAs that are still on
+        // their way.  All of them are credited to the leader's barriers; a phase that only one CTA
+        // loaded for is first given what it would otherwise wait for.
+        const bool gave_up = sh->abort_flag != 0u || lt_ld_cluster_u32(lfptx::map_to_cta(lfptx::smem_u32((const void*)&sh->abort_flag), 1)) != 0u;
+        if (gave_up) {
+            const unsigned it_l = sh->prog_it, it_p = lt_ld_cluster_u32(lfptx::map_to_cta(lfptx::smem_u32(&sh->prog_it), 1));
+            const unsigned hi = max(it_l, it_p), lo = min(it_l, it_p);
+            for (unsigned j = lo; j < hi; ++j) {
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
+                if (j >= it_l) lfptx::mbar_arrive_expect_tx(bar, LT_STAGE_BYTES);                // only the peer loaded
+                else lt_complete_tx(bar, LT_STAGE_BYTES);                                        // only the leader loaded
+            }
+            const unsigned long long t0 = lfptx::globaltimer_ns();
+            for (unsigned j = hi > LT_STAGES ? hi - LT_STAGES : 0; j < hi; ++j) {
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
+                while (!lfptx::mbar_try_wait(bar, (j / LT_STAGES) & 1u) && lfptx::globaltimer_ns() - t0 < 50000000ull) { }
+            }
+        }
+    }
+    lfptx::cluster_sync_all();
+    if (warp == 1) {
+        lfptx::tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    }
+}
+
+// ================================================================================================
+// Split tiles
+// ================================================================================================
+// Every part leaves its fp32 tile in shared memory; after a cluster barrier each CTA adds its share of the rows that exist
+// from all parts, in their order.  A row is a warp's: a lane has four columns.
+template <typename OUT, bool ROWS, int SPLITS>
+__global__ void __launch_bounds__(LBS_THREADS, 1)
+k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const LbParams P)
+{
+    typedef typename half_of<OUT>::type H;
+    extern __shared__ unsigned char lb_smem_raw[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lb_smem_raw) + 1023u) & ~(uintptr_t)1023u);
+    float* tile = reinterpret_cast<float*>(ring + (size_t)LBS_STAGES * LT_STAGE_BYTES);     // [128][LBS_LD]
+    unsigned char* scales = reinterpret_cast<unsigned char*>(tile) + LBS_TILE_BYTES;
+    LtShared* sh = reinterpret_cast<LtShared*>(scales + LBS_SCALE_BYTES);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int part = (int)(blockIdx.x % (unsigned)SPLITS), t = (int)(blockIdx.x / (unsigned)SPLITS);
+    const int tn = t / P.tiles_m, tm = t - tn * P.tiles_m;
+    const int n_k_all = (P.K + LB_BK - 1) / LB_BK;
+    const int ks0 = part * P.stages_per_split;
+    const int n_k = max(0, min(P.stages_per_split, n_k_all - ks0));
+
+    auto load_stage = [&](int ks) {                    // one thread; stage ks of this part into its slot
+        const unsigned st = (unsigned)ks % LBS_STAGES, bar = lfptx::smem_u32(&sh->full[st]);
+        lfptx::mbar_arrive_expect_tx(bar, LT_STAGE_BYTES);
+        if (P.withhold && blockIdx.x == 0 && ks == 0) return;                       // test hook
+        const unsigned dst = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
+        lt_load<false, false>(dst, &map_a, bar, tm * 128, (ks0 + ks) * LB_BK);
+        lt_load<false, false>(dst + LT_BLOCK_BYTES, &map_b, bar, tn * 128, (ks0 + ks) * LB_BK);
+    };
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+        for (int i = 0; i < LBS_STAGES; ++i) {
+            lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
+            lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            lfptx::mbar_init(lfptx::smem_u32(&sh->acc_full[i]), 1);
+            lfptx::mbar_init(lfptx::smem_u32(&sh->acc_empty[i]), 8);
+        }
+        sh->abort_flag = 0u;
+        lfptx::mbar_fence_init();
+        lf_grid_wait();
+        for (int ks = 0; ks < min(n_k, LBS_STAGES); ++ks) load_stage(ks);            // under the rest of the set-up
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(lfptx::smem_u32(&sh->tmem_base)), "r"(256u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    lfptx::tc_fence_before();
+    __syncthreads();
+    lfptx::tc_fence_after();
+    const unsigned tmem_base = sh->tmem_base;
+    lf_grid_wait();
+    lf_grid_release();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int ks = LBS_STAGES;
+            for (; ks < n_k; ++ks) {
+                if (!lt_wait(lfptx::smem_u32(&sh->empty[ks % LBS_STAGES]), (unsigned)(ks / LBS_STAGES - 1) & 1u, P, sh)) break;
+                load_stage(ks);
+            }
+            // after giving up: do not let the CTA go on under loads that are still landing
+            if (sh->abort_flag) {
+                const unsigned long long t0 = lfptx::globaltimer_ns();
+                const int n = min(ks, n_k);
+                for (int j = max(0, n - LBS_STAGES); j < n; ++j)
+                    while (!lfptx::mbar_try_wait(lfptx::smem_u32(&sh->full[j % LBS_STAGES]), (unsigned)(j / LBS_STAGES) & 1u) &&
+                           lfptx::globaltimer_ns() - t0 < 50000000ull) { }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            for (int ks = 0; ks < n_k; ++ks) {
+                const unsigned ab = (unsigned)ks & 1u, use = (unsigned)ks >> 1, st = (unsigned)ks % LBS_STAGES;
+                if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->acc_empty[ab]), (use - 1) & 1u, P, sh)) break;
+                if (!lt_wait(lfptx::smem_u32(&sh->full[st]), (unsigned)(ks / LBS_STAGES) & 1u, P, sh)) break;
+                lfptx::tc_fence_after();
+                const unsigned a_addr = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
+                lb_products<false>(tmem_base + ab * 128u, a_addr, a_addr + LT_BLOCK_BYTES, P.idesc);
+                lt_commit<false>(lfptx::smem_u32(&sh->empty[st]));
+                lt_commit<false>(lfptx::smem_u32(&sh->acc_full[ab]));
+            }
+        }
+    } else if (warp < 10) {
+        const int quad = warp & 3, half = (warp - 2) >> 2, row = tm * 128 + quad * 32 + lane, col0 = tn * 128 + half * 64;
+        const float* sa = P.sa + (size_t)ks0 * P.M + min(row, P.M - 1);
+        const float* sb = ROWS ? P.sb + (size_t)ks0 * P.N + min(col0 + 2 * lane, P.N - 2) : P.sb + (size_t)tn * n_k_all + ks0;
+        const size_t sb_step = ROWS ? (size_t)P.N : 1;
+        float acc[64], sa_next = 0.f;
+        float2 sb_next = f2(0.f);
+#pragma unroll
+        for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+        auto scales_of = [&]() {
+            sa_next = *sa;
+            if (ROWS) sb_next = *reinterpret_cast<const float2*>(sb);
+            else sb_next.x = *sb;
+        };
+        if (n_k > 0) scales_of();
+#pragma unroll 1
+        for (int ks = 0; ks < n_k; ++ks) {
+            const unsigned ab = (unsigned)ks & 1u;
+            const float s = ROWS ? sa_next : sa_next * sb_next.x;
+            float2* mine = reinterpret_cast<float2*>(scales + (warp - 2) * 512 + (ks & 1) * 256);
+            if (ROWS) mine[lane] = sb_next;
+            if (ks + 1 < n_k) {
+                sa += P.M;
+                sb += sb_step;
+                scales_of();
+            }
+            if (ROWS) __syncwarp();
+            if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), ((unsigned)ks >> 1) & 1u, P, sh)) break;
+            lfptx::tc_fence_after();
+            float r[64];
+            lfptx::tmem_ld_row(tmem_base + ((unsigned)(quad * 32) << 16) + ab * 128u + half * 64u, r);
+            lfptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->acc_empty[ab]));
+            lb_scale_add<ROWS>(acc, r, s, reinterpret_cast<const float4*>(mine));
+            lb_scale_add<ROWS>(acc + 32, r + 32, s, reinterpret_cast<const float4*>(mine) + 8);
+        }
+        float* to = tile + (quad * 32 + lane) * LBS_LD + half * 64;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            *reinterpret_cast<float4*>(to + 4 * i) = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
+    }
+    __syncwarp();
+    lfptx::tc_fence_before();
+    __syncthreads();
+    if (SPLITS > 1) lfptx::cluster_sync_all();
+    // this CTA's rows: its part of those that exist
+    constexpr int R = 128 / SPLITS, SIDE = SPLITS == 8 ? 1 : 2;       // rows that a warp has in flight
+    const int share = min(R, (P.M - tm * 128 + SPLITS - 1) / SPLITS);
+    const int col = tn * 128 + 4 * lane;
+    const bool live = sh->abort_flag == 0u && col < P.N;
+    float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (P.bias && live) bias = *reinterpret_cast<const float4*>(P.bias + col);
+    for (int r0 = warp * SIDE; r0 < share; r0 += 16 * SIDE) {
+        float4 x[SIDE][SPLITS];
+        uint2 res[SIDE];
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i) {
+            const int r = part * share + r0 + i, row = tm * 128 + r;
+            res[i] = make_uint2(0, 0);
+            if (r0 + i >= share) continue;
+#pragma unroll
+            for (int p = 0; p < SPLITS; ++p) {
+                const float* at = tile + r * LBS_LD + 4 * lane;
+                if (SPLITS == 1) x[i][p] = *reinterpret_cast<const float4*>(at);
+                else x[i][p] = lt_ld_cluster_f4(lfptx::map_to_cta(lfptx::smem_u32(at), (unsigned)p));
+            }
+            if (sizeof(OUT) == 2 && P.add && live && row < P.M) res[i] = *reinterpret_cast<const uint2*>(static_cast<const H*>(P.add) + (size_t)row * P.ld_add + col);
+        }
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i) {
+            const int row = tm * 128 + part * share + r0 + i;
+            if (r0 + i >= share || !live || row >= P.M) continue;
+            float4 v = x[i][0];
+#pragma unroll
+            for (int p = 1; p < SPLITS; ++p) { v.x += x[i][p].x; v.y += x[i][p].y; v.z += x[i][p].z; v.w += x[i][p].w; }
+            v.x += bias.x; v.y += bias.y; v.z += bias.z; v.w += bias.w;
+            OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
+            if (sizeof(OUT) == 2) {
+                if (P.add) {
+                    const float2 f0 = unpack2(res[i].x, H()), f1 = unpack2(res[i].y, H());
+                    v.x += f0.x; v.y += f0.y; v.z += f1.x; v.w += f1.y;
+                }
+                *reinterpret_cast<uint2*>(to) = make_uint2(pack2(v.x, v.y, H()), pack2(v.z, v.w, H()));
+            } else {
+                *reinterpret_cast<float4*>(to) = v;
+            }
+        }
+    }
+    // no CTA may leave while another one reads its tile
+    __syncwarp();
+    if (SPLITS > 1) lfptx::cluster_sync_all();
+    else __syncthreads();
+    if (warp == 1) {
+        lfptx::tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
+    }
+}
+
+typedef void (*lb_kernel)(const CUtensorMap, const CUtensorMap, const LbParams);
+
+// kernel of a result type and kind of column scales; splits = 0: CTA pairs
+template <typename OUT, bool ROWS>
+lb_kernel lb_of(int splits)
+{
+    switch (splits) {
+        case 0: return k_blocks_pair<OUT, ROWS>;
+        case 1: return k_blocks_split<OUT, ROWS, 1>;
+        case 2: return k_blocks_split<OUT, ROWS, 2>;
+        case 4: return k_blocks_split<OUT, ROWS, 4>;
+        default: return k_blocks_split<OUT, ROWS, 8>;
+    }
+}
+lb_kernel lb_pick(int out_dtype, bool rows, int splits)
+{
+    if (out_dtype == LF_F32) return rows ? lb_of<float, true>(splits) : lb_of<float, false>(splits);
+    if (out_dtype == LF_BF16) return rows ? lb_of<__nv_bfloat16, true>(splits) : lb_of<__nv_bfloat16, false>(splits);
+    return rows ? lb_of<__half, true>(splits) : lb_of<__half, false>(splits);
+}
+
+// Parts of a split tile, or 0 for CTA pairs: the least estimated time in SM cycles.
+int lb_choose(const lf_ops* o, const lf_product_blocks_args& a, int n_k)
+{
+    auto waves = [](long long units, int at_once) { return (double)((units + at_once - 1) / at_once); };
+    const long long m128 = (a.tokens + 127) / 128, n128 = (a.n_out + 127) / 128, tiles = ((a.tokens + 255) / 256) * (long long)((a.n_out + 255) / 256);
+    const double rows = a.tokens < 128 ? a.tokens / 128.0 : 1.0;
+    int best = 1;
+    double least = 1e30;
+    for (int splits = 1; splits <= 8 && splits <= n_k; splits *= 2) {
+        const double part = (double)((n_k + splits - 1) / splits);
+        const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
+        const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
+        const double cycles = waves(m128 * n128 * splits, at_once) * (part * 600.0 + meet + 9000.0);
+        if (cycles < least) { least = cycles; best = splits; }
+    }
+    if (o->max_block_pairs > 0 && waves(tiles, o->max_block_pairs) * (n_k * 750.0 + 4000.0) + 10000.0 < least) best = 0;
+    return best;
+}
+
+}  // namespace
+
+int lf_blocks_tc_init(lf_ops* o)
+{
+    o->max_block_pairs = -1;
+    for (int type = 0; type < 3; ++type)
+        for (int rows = 0; rows < 2; ++rows) {
+            const int out = type == 0 ? LF_F32 : type == 1 ? LF_BF16 : LF_F16;
+            for (int splits = 1; splits <= 8; splits *= 2)
+                if (cudaFuncSetAttribute(lb_pick(out, rows, splits), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LBS_SMEM) != cudaSuccess) return LF_ECUDA;
+            const lb_kernel f = lb_pick(out, rows, 0);
+            if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LB_SMEM) != cudaSuccess) return LF_ECUDA;
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute at[2];
+            lt_cluster_config(&cfg, at, 32, LB_THREADS, 2, LB_SMEM, nullptr);
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return LF_ECUDA;
+            if (o->max_block_pairs < 0 || n < o->max_block_pairs) o->max_block_pairs = n;
+        }
+    return LF_OK;
+}
+
+int lf_blocks_tc(lf_ops* o, const lf_product_blocks_args& a)
+{
+    const int n_k = (a.n_in + LB_BK - 1) / LB_BK;
+    LbParams P = {};
+    P.M = a.tokens; P.N = a.n_out; P.K = a.n_in;
+    P.sa = a.sa; P.sb = a.sb;
+    P.bias = a.bias; P.add = a.add; P.ld_add = a.ld_add;
+    P.d = a.d; P.ld_d = a.ld_d;
+    P.wide_add = (a.ld_add & 15) == 0 && (reinterpret_cast<uintptr_t>(a.add) & 31) == 0;
+    P.status = o->status_dev;
+    P.budget_ns = (unsigned long long)o->wait_budget_us * 1000ull;
+    P.withhold = o->withhold;
+    const unsigned idesc = 1u << 4;                                 // fp32 accumulator; A and B: e4m3 (0), both K-major
+    alignas(64) CUtensorMap map_a, map_b;
+    if (!lt_map(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.a, a.tokens, a.n_in, a.ld_a, LB_BK, 128) ||
+        !lt_map(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.b, a.n_out, a.n_in, a.ld_b, LB_BK, 128)) {
+        o->last_cuda_error = (int)cudaErrorInvalidValue;
+        return LF_ECUDA;
+    }
+    const int splits = lb_choose(o, a, n_k);
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute at[2];
+    const lb_kernel f = lb_pick(a.out_dtype, a.b_tiles == 0, splits);
+    if (splits == 0) {
+        P.tiles_m = (P.M + 255) / 256; P.tiles_n = (P.N + 255) / 256;
+        P.idesc = idesc | (256u >> 3) << 17 | (256u >> 4) << 24;
+        P.band = 8;
+        const long long tiles = (long long)P.tiles_m * P.tiles_n;
+        const int pairs = tiles < o->max_block_pairs ? (int)tiles : o->max_block_pairs;
+        lt_cluster_config(&cfg, at, 2 * pairs, LB_THREADS, 2, LB_SMEM, o->stream);
+        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, f, map_a, map_b, P));
+        o->stats.form = LF_FORM_PAIRS;
+        o->stats.splits = 1;
+    } else {
+        P.tiles_m = (P.M + 127) / 128; P.tiles_n = (P.N + 127) / 128;
+        P.idesc = idesc | (128u >> 3) << 17 | (128u >> 4) << 24;
+        P.stages_per_split = (n_k + splits - 1) / splits;
+        lt_cluster_config(&cfg, at, P.tiles_m * P.tiles_n * splits, LBS_THREADS, splits, LBS_SMEM, o->stream);
+        LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, f, map_a, map_b, P));
+        o->stats.form = LF_FORM_SPLIT;
+        o->stats.splits = splits;
+    }
+    o->stats.launches += 1;
+    return LF_OK;
+}

@@ -1,0 +1,434 @@
+// The loss of a network against a teacher's top logits, and its gradient:
+//     loss = w T^2 sum_k p_k (ln p_k - ln q_{i_k}),   dz_v = w T (q_v - sum of p_k with i_k = v)
+// with p the softmax of the teacher's entries and q the softmax of the whole row of logits, both at temperature T.
+//
+// Mathematics: ln p_k - ln q_i = (t_k - z_i) / T + lse(z) - lse(t), so the loss needs of a row only its largest
+// value m, the sum s of e^((z - m) / T), taken together in one pass with s rescaled where m grows, and the picked
+// logits.  lse and loss are differences of numbers larger than themselves: what there is one of per row is in 64 bits.
+//
+// Bound by memory: the loss reads a row once, the gradient reads it and writes one.  A row is cut into parts, a block
+// each, which are a cluster and meet once, over distributed shared memory, with their m and s.  Where the gradient is
+// written too, a part keeps what it has read in shared memory, so that the row is read from memory once.
+// The teacher's entries are one warp's work beside the others' pass over the row; the dense part of the gradient is
+// written first, then the entries that fall into the part are put right.
+#include <math_constants.h>
+
+#include "lf_ops_internal.h"
+#include "lf_ptx.cuh"
+#include "lf_rows.cuh"
+
+namespace {
+
+using namespace lfrow;
+
+constexpr int DT_THREADS = 288;                 // eight warps for the row, one for the teacher's entries
+constexpr int DT_ROW_THREADS = 256;
+constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
+constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
+constexpr int DT_STAGE_BYTES = 64 * 1024;       // of a part that stays in shared memory
+
+// ---- 16 bytes of a row -------------------------------------------------------------------------------
+template <typename T>
+struct piece16 {
+    static constexpr int N = 16 / (int)sizeof(T);
+    uint4 u;
+    __device__ __forceinline__ void get(float (&v)[N]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            vec8<T> w;
+            w.u = u;
+            w.get(v);
+        } else {
+            v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[N])
+    {
+        if constexpr (sizeof(T) == 2) {
+            vec8<T> w;
+            w.set(v);
+            u = w.u;
+        } else {
+            u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        }
+    }
+};
+__device__ __forceinline__ unsigned minus_infinity(float) { return 0xFF800000u; }
+__device__ __forceinline__ unsigned minus_infinity(__nv_bfloat16) { return 0xFF80FF80u; }
+__device__ __forceinline__ unsigned minus_infinity(__half) { return 0xFC00FC00u; }
+__device__ __forceinline__ uint4 ld16(const void* p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// The part of a row that a block has: elements [e0, e1), of which pieces [0, pieces) of 16 aligned bytes begin at `body`; fewer than a
+// piece's elements lie before and behind them.
+template <typename T>
+struct part_of {
+    long long e0, e1, body;
+    int pieces, edge;           // edge: elements before and behind
+    __device__ __forceinline__ part_of(const T* row, int vocab, int part, int parts)
+    {
+        constexpr int N = 16 / (int)sizeof(T);
+        const long long per = ((vocab + parts - 1) / parts + N - 1) / N * N;
+        e0 = min((long long)vocab, per * part);
+        e1 = min((long long)vocab, e0 + per);
+        const int off = (int)((reinterpret_cast<uintptr_t>(row + e0) & 15u) / sizeof(T));
+        body = min(e1, e0 + (off ? N - off : 0));
+        pieces = (int)((e1 - body) / N);
+        edge = (int)(e1 - e0) - pieces * N;
+    }
+    // element of the i-th one that is in no piece
+    __device__ __forceinline__ long long at_edge(int i) const
+    {
+        const int before = (int)(body - e0);
+        return i < before ? e0 + i : body + (long long)pieces * (16 / (int)sizeof(T)) + (i - before);
+    }
+};
+
+// ---- running maximum and sum of e^((z - m) / T); c = log2(e) / T --------------------------------------
+struct online {
+    float m, s;
+    __device__ __forceinline__ void clear() { m = -CUDART_INF_F; s = 0.f; }
+    template <int N>
+    __device__ __forceinline__ void add(const float (&v)[N], float c)
+    {
+        float top = v[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+        const float now = fmaxf(m, top), about = now == -CUDART_INF_F ? 0.f : now;
+        s *= ex2((m - about) * c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s += ex2((v[i] - about) * c);
+        m = now;
+    }
+    __device__ __forceinline__ void join(float m2, float s2, float c)
+    {
+        const float now = fmaxf(m, m2), about = now == -CUDART_INF_F ? 0.f : now;
+        s = s * ex2((m - about) * c) + s2 * ex2((m2 - about) * c);
+        m = now;
+    }
+};
+
+struct entries {                       // the teacher's, of one token
+    int at[LF_DISTILL_MAX_TOP];
+    float p[LF_DISTILL_MAX_TOP];       // 0: not there
+    float z[LF_DISTILL_MAX_TOP];       // the student's logit
+    double base;                       // sum_k p_k (t_k - z_k) / T - lse(t)
+    int any, bad;                      // entries at all; an index beyond the vocabulary
+};
+// By one warp.  A sum over lanes adds in a fixed order.
+template <typename T>
+__device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, int token, const T* z, bool loss)
+{
+    const int lane = threadIdx.x & 31;
+    const int* index = a.index + (size_t)token * a.top;
+    const float* value = a.value + (size_t)token * a.top;
+    float top = -CUDART_INF_F;
+    int bad = 0, any = 0;
+    for (int k = lane; k < a.top; k += 32) {
+        const int i = index[k];
+        const float t = value[k];
+        const bool there = i >= 0 && t != -CUDART_INF_F;
+        const bool beyond = there && i >= a.vocab;
+        bad |= beyond;
+        any |= there;
+        e.at[k] = there && !beyond ? i : -1;
+        e.p[k] = there ? t : -CUDART_INF_F;
+        e.z[k] = there && !beyond ? (float)z[i] : 0.f;
+        if (there) top = fmaxf(top, t);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    bad = __any_sync(0xFFFFFFFFu, bad);
+    any = __any_sync(0xFFFFFFFFu, any);
+    const float inv_t = 1.0f / a.temperature;
+    double sum = 0.0, dot = 0.0;
+    for (int k = lane; k < a.top; k += 32) {
+        const float t = e.p[k];
+        float p = 0.f;
+        if (t != -CUDART_INF_F) {
+            p = expf((t - top) * inv_t);
+            sum += (double)p;
+            // (a weight that fp32 does not tell from zero has no part in the loss, whatever logit it falls on)
+            if (loss && p != 0.f) dot += (double)p * ((double)t - (double)e.z[k]);
+        }
+        e.p[k] = p;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+    }
+    const float inv = (float)(1.0 / sum);
+    for (int k = lane; k < a.top; k += 32) e.p[k] = e.at[k] >= 0 ? e.p[k] * inv : 0.f;
+    if (lane == 0) {
+        const double tau = (double)a.temperature;
+        e.any = any;
+        e.bad = bad;
+        e.base = loss ? dot / (sum * tau) - ((double)top / tau + log(sum)) : 0.0;
+    }
+}
+// dz of the entries that fall on elements [e0, e1): the first of several on one element adds them up, in their order
+template <typename T, typename F>
+__device__ __forceinline__ void put_right(const entries& e, int top, long long e0, long long e1, T* dz, float wt, F q_of)
+{
+    for (int k = threadIdx.x; k < top; k += DT_THREADS) {
+        const int at = e.at[k];
+        if (at < e0 || at >= e1) continue;
+        float p = 0.f;
+        bool first = true;
+        for (int j = 0; j < top; ++j) {
+            if (e.at[j] != at) continue;
+            if (j < k) { first = false; break; }
+            p += e.p[j];
+        }
+        if (first) dz[at] = (T)(wt * (q_of(e.z[k]) - p));
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* to, const float (&v)[16 / sizeof(T)], bool aligned)
+{
+    if (aligned) {
+        piece16<T> o;
+        o.set(v);
+        *reinterpret_cast<uint4*>(to) = o.u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16 / (int)sizeof(T); ++i) to[i] = (T)v[i];
+    }
+}
+
+// Loss, lse and, with GRAD, the gradient.  A cluster of `parts` blocks has a token; `staged` pieces of a part stay in shared memory.
+template <typename T, bool GRAD>
+__global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a, int parts, int staged)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    extern __shared__ __align__(16) uint4 stage[];
+    __shared__ entries ent;
+    __shared__ float2 warp_ms[8];
+    __shared__ float2 part_ms;
+    const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
+    const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
+    const part_of<T> mine(z, a.vocab, part, parts);
+    const float c = LOG2E / a.temperature;
+    lf_grid_wait();
+    lf_grid_release();
+    online o;
+    o.clear();
+    if (tid < DT_ROW_THREADS) {
+        const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
+        const int kept = GRAD ? min(staged, mine.pieces) : 0;
+        if (GRAD) {
+            // (a thread reads what it copied itself)
+            for (int i = tid; i < kept; i += DT_ROW_THREADS) cp_async16(lfptx::smem_u32(stage + i), from + i);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        float v[DT_UNROLL * N];
+        auto take = [&](const uint4 (&r)[DT_UNROLL]) {
+#pragma unroll
+            for (int u = 0; u < DT_UNROLL; ++u) {
+                piece16<T> p;
+                p.u = r[u];
+                p.get(*reinterpret_cast<float(*)[N]>(v + u * N));
+            }
+            o.add(v, c);
+        };
+        const unsigned none = minus_infinity(T());
+        // what is not kept, and the elements outside of pieces
+        for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS * DT_UNROLL) {
+            uint4 r[DT_UNROLL];
+#pragma unroll
+            for (int u = 0; u < DT_UNROLL; ++u) {
+                const int at = i + u * DT_ROW_THREADS;
+                r[u] = at < mine.pieces ? ld16(from + at) : make_uint4(none, none, none, none);
+            }
+            take(r);
+        }
+        if (tid < mine.edge) {
+            const float one[1] = {(float)z[mine.at_edge(tid)]};
+            o.add(one, c);
+        }
+        if (GRAD) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            for (int i = tid; i < kept; i += DT_ROW_THREADS * DT_UNROLL) {
+                uint4 r[DT_UNROLL];
+#pragma unroll
+                for (int u = 0; u < DT_UNROLL; ++u) {
+                    const int at = i + u * DT_ROW_THREADS;
+                    r[u] = at < kept ? stage[at] : make_uint4(none, none, none, none);
+                }
+                take(r);
+            }
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, o.m, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, o.s, d);
+            o.join(m2, s2, c);
+        }
+        if ((tid & 31) == 0) warp_ms[tid >> 5] = make_float2(o.m, o.s);
+    } else if (GRAD || part == 0) {
+        teacher<T>(ent, a, token, z, part == 0);
+    }
+    __syncthreads();
+    o.clear();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) o.join(warp_ms[w].x, warp_ms[w].y, c);
+    if (parts > 1) {
+        if (tid == 0) part_ms = make_float2(o.m, o.s);
+        __syncwarp();
+        lfptx::cluster_sync_all();             // (also: every part has read the logits that the loss needs)
+        const unsigned at = lfptx::smem_u32(&part_ms);
+        o.clear();
+        for (int q = 0; q < parts; ++q) {
+            float2 ms;
+            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ms.x), "=f"(ms.y) : "r"(lfptx::map_to_cta(at, (unsigned)q)) : "memory");
+            o.join(ms.x, ms.y, c);
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    }
+    const float w = a.weight ? a.weight[token] : 1.f;
+    if (part == 0 && tid == 0) {
+        const double lse = (double)o.m / (double)a.temperature + log((double)o.s);
+        if (a.lse) a.lse[token] = (float)lse;
+        double loss = (ent.base + lse) * (double)a.temperature * (double)a.temperature * (double)w;
+        if (ent.bad) loss = CUDART_NAN;
+        a.loss[token] = w == 0.f || !ent.any ? 0.f : (float)loss;
+    }
+    if (GRAD) {
+        T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
+        const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !ent.any;
+        const float wt = none ? 0.f : ent.bad ? CUDART_NAN_F : w * a.temperature, f = wt / o.s, m = o.m;
+        if (tid < DT_ROW_THREADS) {
+            const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
+            const int kept = min(staged, mine.pieces);
+            auto give = [&](int i, uint4 r) {
+                piece16<T> p;
+                float v[N];
+                p.u = r;
+                p.get(v);
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] = none ? 0.f : f * ex2((v[k] - m) * c);
+                store_piece<T>(dz + mine.body + (long long)i * N, v, aligned);
+            };
+#pragma unroll 4
+            for (int i = tid; i < kept; i += DT_ROW_THREADS) give(i, stage[i]);
+#pragma unroll 4
+            for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS) give(i, ld16(from + i));
+            if (tid < mine.edge) {
+                const long long at = mine.at_edge(tid);
+                dz[at] = (T)(none ? 0.f : f * ex2(((float)z[at] - m) * c));
+            }
+        }
+        __syncthreads();
+        if (!none) {
+            const float inv_s = 1.0f / o.s;
+            put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
+        }
+    }
+    __syncwarp();
+    if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
+}
+
+// dz from z and lse: no part of a row needs to know another
+template <typename T>
+__global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distill_args a, int parts)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    __shared__ entries ent;
+    const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
+    const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
+    T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
+    const part_of<T> mine(z, a.vocab, part, parts);
+    lf_grid_wait();
+    lf_grid_release();
+    if (tid >= DT_ROW_THREADS) teacher<T>(ent, a, token, z, false);
+    __syncthreads();                       // (the entries' logits have been read: dz may be z)
+    const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], inv_t = 1.0f / a.temperature;
+    const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !ent.any;
+    const float wt = none ? 0.f : ent.bad ? CUDART_NAN_F : w * a.temperature;
+    auto q_of = [&](float v) { return ex2(fmaf(v, inv_t, -lse) * LOG2E); };
+    if (tid < DT_ROW_THREADS) {
+        const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
+        for (int i = tid; i < mine.pieces; i += DT_ROW_THREADS * DT_UNROLL) {
+            uint4 r[DT_UNROLL];
+#pragma unroll
+            for (int u = 0; u < DT_UNROLL; ++u)
+                if (i + u * DT_ROW_THREADS < mine.pieces) r[u] = ld16(from + i + u * DT_ROW_THREADS);
+#pragma unroll
+            for (int u = 0; u < DT_UNROLL; ++u) {
+                const int at = i + u * DT_ROW_THREADS;
+                if (at >= mine.pieces) break;
+                piece16<T> p;
+                float v[N];
+                p.u = r[u];
+                p.get(v);
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] = none ? 0.f : wt * q_of(v[k]);
+                store_piece<T>(dz + mine.body + (long long)at * N, v, aligned);
+            }
+        }
+        if (tid < mine.edge) {
+            const long long at = mine.at_edge(tid);
+            dz[at] = (T)(none ? 0.f : wt * q_of((float)z[at]));
+        }
+    }
+    __syncthreads();
+    if (!none) put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, q_of);
+}
+
+// A part has as much as stays in shared memory, and there are blocks enough to fill the device, up to eight; parts
+// of fewer than 4 KB are not worth a meeting.
+int parts_for(const lf_distill_args& a, int sm_count, bool grad)
+{
+    const long long bytes = (long long)a.vocab * (a.dtype == LF_F32 ? 4 : 2);
+    int parts = 1;
+    while (parts < DT_MAX_PARTS && bytes / parts > 4096 &&
+           ((grad && bytes / parts > DT_STAGE_BYTES) || (long long)a.tokens * parts < 2 * sm_count))
+        parts *= 2;
+    return parts;
+}
+
+template <typename T>
+cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
+{
+    const int parts = parts_for(a, sm_count, a.dz != nullptr);
+    if (!a.dz) return lf_launch_clusters(k_distill<T, false>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, 0, parts, s, a, parts, 0);
+    const long long pieces = (long long)a.vocab * sizeof(T) / 16 / parts + 2;
+    const int staged = pieces * 16 < DT_STAGE_BYTES ? (int)pieces : DT_STAGE_BYTES / 16;
+    return lf_launch_clusters(k_distill<T, true>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, (size_t)staged * 16, parts, s, a, parts, staged);
+}
+template <typename T>
+cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
+{
+    const long long bytes = (long long)a.vocab * sizeof(T);
+    long long parts = (bytes + 65535) / 65536;                    // (16 pieces a thread)
+    while ((long long)a.tokens * parts < 2 * sm_count && bytes / parts > 4096) parts *= 2;
+    return lf_launch(k_distill_backward<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, 0, s, a, (int)parts);
+}
+
+}  // namespace
+
+int lf_distill_init(lf_ops*)
+{
+    return cudaFuncSetAttribute(k_distill<float, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DT_STAGE_BYTES) == cudaSuccess &&
+                   cudaFuncSetAttribute(k_distill<__nv_bfloat16, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DT_STAGE_BYTES) == cudaSuccess &&
+                   cudaFuncSetAttribute(k_distill<__half, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DT_STAGE_BYTES) == cudaSuccess
+               ? LF_OK : LF_ECUDA;
+}
+
+cudaError_t lfk_distill(const lf_distill_args& a, int sm_count, cudaStream_t s)
+{
+    if (a.dtype == LF_F32) return distill_of<float>(a, sm_count, s);
+    if (a.dtype == LF_BF16) return distill_of<__nv_bfloat16>(a, sm_count, s);
+    return distill_of<__half>(a, sm_count, s);
+}
+cudaError_t lfk_distill_backward(const lf_distill_args& a, int sm_count, cudaStream_t s)
+{
+    if (a.dtype == LF_F32) return distill_backward_of<float>(a, sm_count, s);
+    if (a.dtype == LF_BF16) return distill_backward_of<__nv_bfloat16>(a, sm_count, s);
+    return distill_backward_of<__half>(a, sm_count, s);
+}

@@ -137,6 +137,35 @@ struct call {
     {
         return flat(q, "q", (long long)rows * cols, at::kByte, qp) & flat(s, "s", (long long)rows * ((cols + 31) / 32), at::kByte, sp);
     }
+    // a contiguous float32 [d0][d1] matrix of scales; `or_else`: another shape may fit as well, nothing is refused
+    template <typename U>
+    bool scales(PyObject* o, const char* name, long long d0, long long d1, U** p, bool or_else = false)
+    {
+        *p = nullptr;
+        if (o == Py_None) return true;
+        const at::Tensor* t = tensor(o, name);
+        if (!t) return false;
+        if (t->scalar_type() != at::kFloat || !here(*t) || t->dim() != 2 || t->size(0) != d0 || t->size(1) != d1 || !t->is_contiguous())
+            return or_else ? false : refuse(name, said(*t) + ", contiguous Float (" + std::to_string(d0) + ", " + std::to_string(d1) + ") on cuda:" + std::to_string(device) + " needed");
+        if constexpr (std::is_const_v<U>) *p = static_cast<U*>(t->const_data_ptr());
+        else *p = static_cast<U*>(output(o));
+        return true;
+    }
+    // an 8-bit matrix of which only its type and shape are looked at here
+    template <typename U>
+    bool bytes(PyObject* o, const char* name, int rows, int cols, U** p, long long* ld)
+    {
+        if constexpr (std::is_const_v<U>) {
+            const void* v;
+            if (!mat(o, name, rows, cols, at::kByte, &v, ld)) return false;
+            *p = static_cast<U*>(v);
+        } else {
+            void* v;
+            if (!mat(o, name, rows, cols, at::kByte, &v, ld)) return false;
+            *p = static_cast<U*>(v);
+        }
+        return true;
+    }
     // a number for an int of the library: one that is too large is refused, not cut
     int number(PyObject* o, const char* name)
     {
@@ -331,6 +360,129 @@ PyObject* m_act_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_act_backward)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), dtype, act, m, n, yp, ldy, q, s, zp, ldz));
 }
 
+long long blocks(long long n) { return (n + 127) / 128; }
+
+// layer_norm(f, ops, x, gain, bias, y, residual, h, q, s, mean, rstd, eps, device)
+PyObject* m_layer_norm(PyObject*, PyObject* const* v, Py_ssize_t nargs)
+{
+    LF_EXPECT(14);
+    call c(v[13]);
+    lf_layer_norm_args a = {};
+    const at::Tensor* x = c.tensor(v[2], "x");
+    a.dtype = c.type(x, "x");
+    a.eps = (float)PyFloat_AsDouble(v[12]);
+    LF_NUMBERS_OK;
+    c.shape(x, "x", &a.tokens, &a.n);
+    if (!c.problem.empty()) return c.refused();
+    const at::ScalarType st = x->scalar_type();
+    const bool ok = c.mat(v[2], "x", a.tokens, a.n, st, &a.x, &a.ld_x) && c.flat(v[3], "gain", a.n, at::kFloat, &a.gain) &&
+                    c.flat(v[4], "bias", a.n, at::kFloat, &a.bias) && c.mat(v[5], "y", a.tokens, a.n, st, &a.y, &a.ld_y) &&
+                    c.mat(v[6], "residual", a.tokens, a.n, st, &a.residual, &a.ld_residual) && c.mat(v[7], "h", a.tokens, a.n, st, &a.h, &a.ld_h) &&
+                    c.bytes(v[8], "q", a.tokens, a.n, &a.q, &a.ld_q) && c.scales(v[9], "s", blocks(a.n), a.tokens, &a.s) &&
+                    c.flat(v[10], "mean", a.tokens, at::kFloat, &a.mean) && c.flat(v[11], "rstd", a.tokens, at::kFloat, &a.rstd);
+    if (!ok) return c.refused();
+    return c.answer(reinterpret_cast<decltype(&lf_layer_norm)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
+}
+
+// layer_norm_backward(f, ops, dy, h, gain, mean, rstd, dh, dgain, dbias, dres, device)
+PyObject* m_layer_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs)
+{
+    LF_EXPECT(12);
+    call c(v[11]);
+    lf_layer_norm_backward_args a = {};
+    const at::Tensor* h = c.tensor(v[3], "h");
+    a.dtype = c.type(h, "h");
+    LF_NUMBERS_OK;
+    c.shape(h, "h", &a.tokens, &a.n);
+    if (!c.problem.empty()) return c.refused();
+    const at::ScalarType st = h->scalar_type();
+    const bool ok = c.mat(v[2], "dy", a.tokens, a.n, st, &a.dy, &a.ld_dy) && c.mat(v[3], "h", a.tokens, a.n, st, &a.h, &a.ld_h) &&
+                    c.flat(v[4], "gain", a.n, at::kFloat, &a.gain) && c.flat(v[5], "mean", a.tokens, at::kFloat, &a.mean) &&
+                    c.flat(v[6], "rstd", a.tokens, at::kFloat, &a.rstd) && c.mat(v[7], "dh", a.tokens, a.n, st, &a.dh, &a.ld_dh) &&
+                    c.flat(v[8], "dgain", a.n, at::kFloat, &a.dgain) && c.flat(v[9], "dbias", a.n, at::kFloat, &a.dbias) &&
+                    c.mat(v[10], "dres", a.tokens, a.n, st, &a.dres, &a.ld_dres);
+    if (!ok) return c.refused();
+    return c.answer(reinterpret_cast<decltype(&lf_layer_norm_backward)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
+}
+
+// pack_blocks(f, ops, x, q, s, qt, st, device), pack_tiles the same
+template <bool TILES>
+PyObject* pack_any(PyObject* const* v, Py_ssize_t nargs)
+{
+    LF_EXPECT(8);
+    call c(v[7]);
+    lf_pack_blocks_args a = {};
+    const at::Tensor* x = c.tensor(v[2], "x");
+    a.dtype = c.type(x, "x");
+    LF_NUMBERS_OK;
+    c.shape(x, "x", &a.tokens, &a.n);
+    if (!c.problem.empty()) return c.refused();
+    const long long tb = blocks(a.tokens), nb = blocks(a.n);
+    const bool ok = c.mat(v[2], "x", a.tokens, a.n, x->scalar_type(), &a.x, &a.ld_x) && c.bytes(v[3], "q", a.tokens, a.n, &a.q, &a.ld_q) &&
+                    c.scales(v[4], "s", TILES ? tb : nb, TILES ? nb : a.tokens, &a.s) && c.bytes(v[5], "qt", a.n, a.tokens, &a.qt, &a.ld_qt) &&
+                    c.scales(v[6], "st", TILES ? nb : tb, TILES ? tb : a.n, &a.st);
+    if (!ok) return c.refused();
+    return c.answer(reinterpret_cast<decltype(&lf_pack_blocks)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
+}
+PyObject* m_pack_blocks(PyObject*, PyObject* const* v, Py_ssize_t nargs) { return pack_any<false>(v, nargs); }
+PyObject* m_pack_tiles(PyObject*, PyObject* const* v, Py_ssize_t nargs) { return pack_any<true>(v, nargs); }
+
+// product_blocks(f, ops, a, sa, b, sb, d, bias, add, device)
+PyObject* m_product_blocks(PyObject*, PyObject* const* v, Py_ssize_t nargs)
+{
+    LF_EXPECT(10);
+    call c(v[9]);
+    lf_product_blocks_args a = {};
+    const at::Tensor *x = c.tensor(v[2], "a"), *w = c.tensor(v[4], "b"), *d = c.tensor(v[6], "d");
+    int k = 0;
+    a.out_dtype = c.type(d, "d");
+    LF_NUMBERS_OK;
+    c.shape(x, "a", &a.tokens, &a.n_in);
+    c.shape(w, "b", &a.n_out, &k);
+    if (!c.problem.empty()) return c.refused();
+    const long long kb = blocks(a.n_in);
+    bool ok = c.bytes(v[2], "a", a.tokens, a.n_in, &a.a, &a.ld_a) && c.scales(v[3], "sa", kb, a.tokens, &a.sa) &&
+              (k == a.n_in || c.refuse("b", c.said(*w) + ", rows as long as a's needed")) && c.bytes(v[4], "b", a.n_out, a.n_in, &a.b, &a.ld_b);
+    if (ok && !c.scales(v[5], "sb", kb, a.n_out, &a.sb, true)) {        // (n_out is 8 at least: the two shapes are never the same)
+        a.b_tiles = 1;
+        ok = c.problem.empty() && c.scales(v[5], "sb (scales of rows or, else, of tiles)", blocks(a.n_out), kb, &a.sb);
+    }
+    ok = ok && c.mat(v[6], "d", a.tokens, a.n_out, d->scalar_type(), &a.d, &a.ld_d) && c.flat(v[7], "bias", a.n_out, at::kFloat, &a.bias) &&
+         c.mat(v[8], "add", a.tokens, a.n_out, d->scalar_type(), &a.add, &a.ld_add);
+    if (!ok) return c.refused();
+    return c.answer(reinterpret_cast<decltype(&lf_product_blocks)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
+}
+
+// distill(f, ops, z, index, value, loss, lse, weight, dz, temperature, device); distill_backward the same, loss None
+template <bool BACKWARD>
+PyObject* distill_any(PyObject* const* v, Py_ssize_t nargs)
+{
+    LF_EXPECT(11);
+    call c(v[10]);
+    lf_distill_args a = {};
+    const at::Tensor *z = c.tensor(v[2], "z"), *index = c.tensor(v[3], "index");
+    int rows = 0;
+    a.dtype = c.type(z, "z");
+    a.temperature = (float)PyFloat_AsDouble(v[9]);
+    LF_NUMBERS_OK;
+    c.shape(z, "z", &a.tokens, &a.vocab);
+    c.shape(index, "index", &rows, &a.top);
+    if (!c.problem.empty()) return c.refused();
+    const at::ScalarType st = z->scalar_type();
+    const long long n = (long long)a.tokens * a.top;
+    const float* lse_in = nullptr;
+    const bool ok = c.mat(v[2], "z", a.tokens, a.vocab, st, &a.z, &a.ld_z) && (rows == a.tokens || c.refuse("index", c.said(*index) + ", a row for each of z's needed")) &&
+                    c.flat(v[3], "index", n, at::kInt, &a.index) && c.flat(v[4], "value", n, at::kFloat, &a.value) &&
+                    c.flat(v[5], "loss", a.tokens, at::kFloat, &a.loss) &&
+                    (BACKWARD ? c.flat(v[6], "lse", a.tokens, at::kFloat, &lse_in) : c.flat(v[6], "lse", a.tokens, at::kFloat, &a.lse)) &&
+                    c.flat(v[7], "weight", a.tokens, at::kFloat, &a.weight) && c.mat(v[8], "dz", a.tokens, a.vocab, st, &a.dz, &a.ld_dz);
+    if (!ok) return c.refused();
+    if (BACKWARD) a.lse = const_cast<float*>(lse_in);          // (read only)
+    return c.answer(reinterpret_cast<decltype(&lf_distill)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
+}
+PyObject* m_distill(PyObject*, PyObject* const* v, Py_ssize_t nargs) { return distill_any<false>(v, nargs); }
+PyObject* m_distill_backward(PyObject*, PyObject* const* v, Py_ssize_t nargs) { return distill_any<true>(v, nargs); }
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* entry(PyObject* self, PyObject* const* v, Py_ssize_t nargs) noexcept
 {
@@ -347,7 +499,9 @@ PyObject* entry(PyObject* self, PyObject* const* v, Py_ssize_t nargs) noexcept
 
 #define LF_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(entry<m_##name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LF_METHOD(linear),    LF_METHOD(linear_grad_x), LF_METHOD(linear_grad_w), LF_METHOD(rms_norm), LF_METHOD(rms_norm_backward),
-                         LF_METHOD(pack8),     LF_METHOD(unpack8),       LF_METHOD(act_backward),  {nullptr, nullptr, 0, nullptr}};
+                         LF_METHOD(pack8),     LF_METHOD(unpack8),       LF_METHOD(act_backward),  LF_METHOD(layer_norm),    LF_METHOD(layer_norm_backward),
+                         LF_METHOD(pack_blocks), LF_METHOD(pack_tiles),  LF_METHOD(product_blocks), LF_METHOD(distill), LF_METHOD(distill_backward),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "tensor marshalling of the layer operators", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -28,6 +28,10 @@ struct checker {
     void width(int n) { ok(n >= 8 && n <= LF_OPS_MAX_WIDTH && (n & 7) == 0); }
     // the stride of a matrix's rows; 0 = contiguous
     void ld(long long l, int n, int dtype) { ok(l == 0 || (l >= n && l % (dtype == LF_F32 ? 4 : 8) == 0 && l < (1ll << 36))); }
+    // e4m3 rows: a stride of whole 16-byte pieces; 0 = the width rounded up to them (rows of nothing may lie anywhere)
+    void ld8(long long l, long long n) { ok(l == 0 || n == 0 || (l >= n && l % 16 == 0 && l < (1ll << 36))); }
+    // at an element's boundary
+    void element(const void* p, int dtype) { if (reinterpret_cast<uintptr_t>(p) % (dtype == LF_F32 ? 4 : 2)) misaligned = true; }
     int result() const { return null_ ? LF_ENULL : invalid ? LF_EINVAL : misaligned ? LF_EALIGN : LF_OK; }
 };
 
@@ -46,6 +50,41 @@ struct on_device {
 #define LF_OPS_DEVICE(o) const on_device on_device__(o); LF_OPS_TRY(o, on_device__.error)
 
 inline long long ld_or(long long l, int n) { return l ? l : n; }
+inline long long ld8_or(long long l, long long n) { return l ? l : (n + 15) / 16 * 16; }
+
+int pack_blocks(lf_ops* o, const lf_pack_blocks_args* args, bool tiles)
+{
+    if (!o || !args) return LF_ENULL;
+    lf_pack_blocks_args a = *args;
+    checker c(a.tokens);
+    c.type(a.dtype); c.width(a.n);
+    c.matrix(a.x); c.both(a.q, a.s); c.optional(a.s); c.both(a.qt, a.st); c.optional(a.st);
+    if (!a.qt) c.matrix(a.q);
+    c.ld(a.ld_x, a.n, a.dtype); c.ld8(a.ld_q, a.n); c.ld8(a.ld_qt, a.tokens);
+    if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
+    o->stats.launches = 0;
+    if (a.tokens == 0) return LF_OK;
+    a.ld_x = ld_or(a.ld_x, a.n); a.ld_q = ld8_or(a.ld_q, a.n); a.ld_qt = ld8_or(a.ld_qt, a.tokens);
+    LF_OPS_TRY(o, lfk_pack_blocks(a, tiles, o->stream));
+    o->stats.launches = 1;
+    return LF_OK;
+}
+
+// the checks that both directions of the loss share
+checker distill_checks(const lf_distill_args& a)
+{
+    checker c(a.tokens);
+    c.type(a.dtype); c.ok(a.vocab >= 1 && a.vocab <= 1 << 30); c.ok(a.top >= 1 && a.top <= LF_DISTILL_MAX_TOP);
+    c.ok(a.temperature >= 1e-6f && a.temperature <= 1e6f);        // (1 / T and T^2 stay within fp32; not a NaN)
+    c.ok(a.ld_z == 0 || (a.ld_z >= a.vocab && a.ld_z < (1ll << 36))); c.ok(a.ld_dz == 0 || (a.ld_dz >= a.vocab && a.ld_dz < (1ll << 36)));
+    if (!c.empty && (!a.z || !a.index || !a.value)) c.null_ = true;
+    c.element(a.z, a.dtype); c.element(a.dz, a.dtype);
+    c.element(a.index, LF_F32); c.element(a.value, LF_F32); c.element(a.weight, LF_F32); c.element(a.loss, LF_F32); c.element(a.lse, LF_F32);
+    // in place means row by row
+    c.ok(a.dz != a.z || !a.dz || ld_or(a.ld_z, a.vocab) == ld_or(a.ld_dz, a.vocab) || a.tokens <= 1);
+    return c;
+}
 
 }  // namespace
 
@@ -81,7 +120,8 @@ int lf_ops_create(lf_ops** out, long long workspace_bytes)
     ok = ok && cudaMemset(o->status_dev, 0, sizeof(unsigned)) == cudaSuccess;
     // (the memsets are only queued, on a stream that the handle's own need not wait for)
     ok = ok && cudaStreamSynchronize(nullptr) == cudaSuccess;
-    ok = ok && lf_product_tc_init(o) == LF_OK && lf_linear_stream_init() == LF_OK && lf_rows_init() == LF_OK;
+    ok = ok && lf_product_tc_init(o) == LF_OK && lf_linear_stream_init() == LF_OK && lf_rows_init() == LF_OK && lf_layer_norm_init() == LF_OK &&
+         lf_blocks_tc_init(o) == LF_OK && lf_blocks_stream_init() == LF_OK && lf_distill_init(o) == LF_OK;
     if (!ok) {
         const cudaError_t e = cudaGetLastError();
         lf_ops_destroy(o);
@@ -330,6 +370,113 @@ int lf_act_backward(lf_ops* o, int dtype, int act, int tokens, int n, const void
     o->stats.launches = 0;
     if (tokens == 0) return LF_OK;
     LF_OPS_TRY(o, lfk_act_backward(dtype, act, tokens, n, dy, ld_or(ld_dy, n), q, s, dz, ld_or(ld_dz, n), o->sm_count, o->stream));
+    o->stats.launches = 1;
+    return LF_OK;
+}
+
+int lf_layer_norm(lf_ops* o, const lf_layer_norm_args* args)
+{
+    if (!o || !args) return LF_ENULL;
+    lf_layer_norm_args a = *args;
+    checker c(a.tokens);
+    c.type(a.dtype); c.width(a.n); c.ok(a.n <= LF_OPS_MAX_NORM); c.ok(a.eps >= 0.f && isfinite(a.eps));
+    c.matrix(a.x); c.require(a.gain); c.optional(a.bias); c.optional(a.residual); c.optional(a.h); c.optional(a.y);
+    c.both(a.q, a.s); c.optional(a.s); c.element(a.mean, LF_F32); c.element(a.rstd, LF_F32);
+    if (!c.empty && (a.mean == nullptr) != (a.rstd == nullptr)) c.null_ = true;
+    if (!a.y) c.matrix(a.q);
+    c.ld(a.ld_x, a.n, a.dtype); c.ld(a.ld_residual, a.n, a.dtype); c.ld(a.ld_h, a.n, a.dtype); c.ld(a.ld_y, a.n, a.dtype); c.ld8(a.ld_q, a.n);
+    if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
+    o->stats.launches = 0;
+    if (a.tokens == 0) return LF_OK;
+    a.ld_x = ld_or(a.ld_x, a.n); a.ld_residual = ld_or(a.ld_residual, a.n); a.ld_h = ld_or(a.ld_h, a.n); a.ld_y = ld_or(a.ld_y, a.n);
+    a.ld_q = ld8_or(a.ld_q, a.n);
+    LF_OPS_TRY(o, lfk_layer_norm(a, o->sm_count, o->stream));
+    o->stats.launches = 1;
+    return LF_OK;
+}
+
+int lf_layer_norm_backward(lf_ops* o, const lf_layer_norm_backward_args* args)
+{
+    if (!o || !args) return LF_ENULL;
+    lf_layer_norm_backward_args a = *args;
+    checker c(a.tokens);
+    c.type(a.dtype); c.width(a.n); c.ok(a.n <= LF_OPS_MAX_NORM);
+    c.matrix(a.dy); c.matrix(a.h); c.require(a.gain); c.matrix(a.dh); c.optional(a.dres); c.optional(a.dgain); c.optional(a.dbias);
+    if (!c.empty && (!a.mean || !a.rstd)) c.null_ = true;
+    c.element(a.mean, LF_F32); c.element(a.rstd, LF_F32);
+    c.ld(a.ld_dy, a.n, a.dtype); c.ld(a.ld_h, a.n, a.dtype); c.ld(a.ld_dres, a.n, a.dtype); c.ld(a.ld_dh, a.n, a.dtype);
+    if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
+    o->stats.launches = 0;
+    if (a.tokens == 0) {
+        if (a.dgain) LF_OPS_TRY(o, cudaMemsetAsync(a.dgain, 0, (size_t)a.n * sizeof(float), o->stream));
+        if (a.dbias) LF_OPS_TRY(o, cudaMemsetAsync(a.dbias, 0, (size_t)a.n * sizeof(float), o->stream));
+        return LF_OK;
+    }
+    a.ld_dy = ld_or(a.ld_dy, a.n); a.ld_h = ld_or(a.ld_h, a.n); a.ld_dres = ld_or(a.ld_dres, a.n); a.ld_dh = ld_or(a.ld_dh, a.n);
+    LF_OPS_TRY(o, lfk_layer_norm_backward(a, reinterpret_cast<float*>(o->ws), o->sm_count, o->stream, &o->stats.launches));
+    return LF_OK;
+}
+
+int lf_pack_blocks(lf_ops* o, const lf_pack_blocks_args* args) { return pack_blocks(o, args, false); }
+int lf_pack_tiles(lf_ops* o, const lf_pack_blocks_args* args) { return pack_blocks(o, args, true); }
+
+int lf_product_blocks(lf_ops* o, const lf_product_blocks_args* args)
+{
+    if (!o || !args) return LF_ENULL;
+    lf_product_blocks_args a = *args;
+    checker c(a.tokens);
+    const bool summed = a.n_in > 0;              // nothing to contract: d = bias + add
+    c.type(a.out_dtype); c.width(a.n_out); c.ok(a.n_in >= 0 && a.n_in <= MAX_TOKENS); c.ok(a.out_dtype != LF_F32 || !a.add);
+    if (summed) { c.matrix(a.a); c.matrix(a.sa); c.require(a.b); c.require(a.sb); }
+    c.matrix(a.d); c.optional(a.bias); c.optional(a.add);
+    c.ld8(a.ld_a, a.n_in); c.ld8(a.ld_b, a.n_in);
+    c.ld(a.ld_add, a.n_out, a.out_dtype); c.ld(a.ld_d, a.n_out, a.out_dtype);
+    if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
+    o->stats.launches = 0;
+    if (a.tokens == 0) return LF_OK;
+    a.ld_a = ld8_or(a.ld_a, a.n_in); a.ld_b = ld8_or(a.ld_b, a.n_in);
+    a.ld_add = ld_or(a.ld_add, a.n_out); a.ld_d = ld_or(a.ld_d, a.n_out);
+    if (a.tokens <= LF_STREAM_MAX_TOKENS || !summed) {
+        LF_OPS_TRY(o, lfk_blocks_stream(a, o->sm_count, o->stream));
+        o->stats.splits = 1;
+        o->stats.form = LF_FORM_STREAM;
+        o->stats.launches = 1;
+        return LF_OK;
+    }
+    return lf_blocks_tc(o, a);
+}
+
+int lf_distill(lf_ops* o, const lf_distill_args* args)
+{
+    if (!o || !args) return LF_ENULL;
+    lf_distill_args a = *args;
+    checker c = distill_checks(a);
+    if (!c.empty && !a.loss) c.null_ = true;
+    if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
+    o->stats.launches = 0;
+    if (a.tokens == 0) return LF_OK;
+    a.ld_z = ld_or(a.ld_z, a.vocab); a.ld_dz = ld_or(a.ld_dz, a.vocab);
+    LF_OPS_TRY(o, lfk_distill(a, o->sm_count, o->stream));
+    o->stats.launches = 1;
+    return LF_OK;
+}
+
+int lf_distill_backward(lf_ops* o, const lf_distill_args* args)
+{
+    if (!o || !args) return LF_ENULL;
+    lf_distill_args a = *args;
+    checker c = distill_checks(a);
+    if (!c.empty && (!a.lse || !a.dz)) c.null_ = true;
+    if (const int rc = c.result()) return rc;
+    LF_OPS_DEVICE(o);
+    o->stats.launches = 0;
+    if (a.tokens == 0) return LF_OK;
+    a.ld_z = ld_or(a.ld_z, a.vocab); a.ld_dz = ld_or(a.ld_dz, a.vocab);
+    LF_OPS_TRY(o, lfk_distill_backward(a, o->sm_count, o->stream));
     o->stats.launches = 1;
     return LF_OK;
 }

@@ -12,6 +12,7 @@ struct lf_ops {
     int sm_count;
     int max_pairs;              // CTA pairs of the 256 x 256 tile kernels that are resident at once (0: none)
     int max_pair_splits;        // resident clusters of the split pair kernels
+    int max_block_pairs;        // CTA pairs of the 8-bit kernels that are resident at once
     cudaStream_t stream;
     unsigned char* ws;          // workspace: fixed part first, then the unpacked layer input
     size_t ws_bytes;
@@ -101,6 +102,16 @@ cudaError_t lfk_act_backward(int dtype, int act, int tokens, int n, const void* 
 cudaError_t lfk_grad_w_prepare(const lf_linear_grad_w_args& a, long long ld_dz, void* x, float* partial, unsigned* counters, int sm_count,
                                cudaStream_t s);
 
+// out[c] = sum over the rows of partial[rows][n], c < n_first; columns from n_first on go to out2[c - n_first]
+cudaError_t lfk_sum_rows(const float* partial, int rows, int n, float* out, float* out2, int n_first, cudaStream_t s);
+int lf_layer_norm_init();
+cudaError_t lfk_layer_norm(const lf_layer_norm_args& a, int sm_count, cudaStream_t s);
+cudaError_t lfk_layer_norm_backward(const lf_layer_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* launches);
+cudaError_t lfk_pack_blocks(const lf_pack_blocks_args& a, bool tiles, cudaStream_t s);
+int lf_distill_init(lf_ops* o);
+cudaError_t lfk_distill(const lf_distill_args& a, int sm_count, cudaStream_t s);
+cudaError_t lfk_distill_backward(const lf_distill_args& a, int sm_count, cudaStream_t s);
+
 // ---- matrix products -----------------------------------------------------------------------------
 // What a product is for: which operands are transposed and what its epilogue does.
 enum lf_prod { LF_PROD_FORWARD = 0, LF_PROD_GRAD_X = 1, LF_PROD_GRAD_W = 2 };
@@ -125,3 +136,8 @@ int lf_product_tc(lf_ops* o, const lf_product& p);
 constexpr int LF_STREAM_MAX_TOKENS = 16;
 int lf_linear_stream_init();
 cudaError_t lfk_linear_stream(const lf_product& p, int sm_count, cudaStream_t s);
+// blocks of 128 in 8 bits: sizes, strides (in bytes for a and b) and pointers are checked by the caller
+int lf_blocks_tc_init(lf_ops* o);
+int lf_blocks_tc(lf_ops* o, const lf_product_blocks_args& a);
+int lf_blocks_stream_init();
+cudaError_t lfk_blocks_stream(const lf_product_blocks_args& a, int sm_count, cudaStream_t s);

@@ -10,24 +10,6 @@ namespace {
 
 using namespace lfrow;
 
-inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
-
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* red)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    if (TPR > 32) {
-        __syncthreads();                     // the previous row's partial sums have been read
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = 0.f;
-#pragma unroll
-        for (int i = 0; i < TPR / 32; ++i) v += red[i];
-    }
-    return v;
-}
-
 // ---- h = x + residual, y = h / sqrt(mean h^2 + eps) * gain -------------------------------------------
 // A block of TPR threads takes one row at a time, VPT vectors of eight columns per thread: the row stays
 // in registers between the sum and the scaling, so x and residual are read once.  With few rows a row has as many
@@ -114,10 +96,6 @@ __global__ void __launch_bounds__(TPR) k_rms_norm(const lf_rms_norm_args a)
 // columns per vector; the groups of a block add theirs at the end, one partial row per block.  16384 x 8192 bf16 with
 // dres: 194 to 208 us by the card, 5.2 to 5.5 TB/s; what is left is the chain load, sums, barrier, results of a row, of which a
 // multiprocessor overlaps two (blocks of 512 threads: 212 us; one block with a ring twice as deep: 265).
-__device__ __forceinline__ void cp_async16(unsigned dst, const void* src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 // ONE: the grid is one cluster, which adds the gain's gradient through distributed shared memory (`sums` is the gradient then,
 // else the partial rows): a launch instead of two.  Up to eight blocks and 4096 columns: one row of 4096 and 64 of 248 3.6 us
 // instead of 5.7, 8 of 2048 4.5 instead of 5.9; wider rows gain nothing (8 of 8192: 6.2 against 5.7, 6 of 14432: 10.6, 10.9).
@@ -291,7 +269,8 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_rms_norm_backward(const lf_rms
 }
 
 // out[c] = sum over the rows of partial[rows][n]: a block has 32 columns and 32 runs of rows, added in a fixed order
-__global__ void __launch_bounds__(1024) k_sum_rows(const float* partial, int rows, int n, float* out)
+// (columns from n_first on go to out2; either may be NULL)
+__global__ void __launch_bounds__(1024) k_sum_rows(const float* partial, int rows, int n, float* out, float* out2, int n_first)
 {
     __shared__ float red[32][33];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
@@ -306,7 +285,11 @@ __global__ void __launch_bounds__(1024) k_sum_rows(const float* partial, int row
     v = red[threadIdx.x & 31][g];            // column g, run (lane)
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    if ((threadIdx.x & 31) == 0 && blockIdx.x * 32 + g < n) out[blockIdx.x * 32 + g] = v;
+    const int to = blockIdx.x * 32 + g;
+    if ((threadIdx.x & 31) == 0 && to < n) {
+        if (to < n_first) { if (out) out[to] = v; }
+        else if (out2) out2[to - n_first] = v;
+    }
 }
 
 // Column sums of a 16-bit matrix: a block takes 256 columns (a warp all of them, eight per lane) and run `by` of n_by
@@ -546,29 +529,6 @@ dim3 row_grid(int tokens, int n, int w, int sm_count, int* lanes_log2)
 // whether 256-bit accesses fit a matrix of this width, row stride and address (8-bit rows: 128-bit ones)
 inline bool wide(int n, long long ld, const void* p) { return (n & 15) == 0 && (ld & 15) == 0 && (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 
-// Threads per row: four vectors per thread when there are rows enough to fill the device, otherwise
-// one, so that a few rows are read by as many threads as they have vectors.
-template <template <typename, int, int> class F, typename T, typename... A>
-cudaError_t pick_row_shape(int n, bool many, A&&... args)
-{
-    const int nv = n >> 3;
-    if (many) {
-        if (nv <= 32) return F<T, 32, 1>::go(args...);
-        else if (nv <= 64) return F<T, 32, 2>::go(args...);
-        else if (nv <= 128) return F<T, 32, 4>::go(args...);
-        else if (nv <= 256) return F<T, 64, 4>::go(args...);
-        else if (nv <= 512) return F<T, 128, 4>::go(args...);
-        else if (nv <= 1024) return F<T, 256, 4>::go(args...);
-        else return F<T, 512, 4>::go(args...);
-    } else {
-        if (nv <= 32) return F<T, 32, 1>::go(args...);
-        else if (nv <= 128) return F<T, 128, 1>::go(args...);
-        else if (nv <= 512) return F<T, 512, 1>::go(args...);
-        else if (nv <= 1024) return F<T, 512, 2>::go(args...);
-        else return F<T, 512, 4>::go(args...);
-    }
-}
-
 template <typename T, int TPR, int VPT>
 struct norm_go {
     static cudaError_t go(const lf_rms_norm_args& a, int sm_count, cudaStream_t s)
@@ -648,9 +608,9 @@ cudaError_t lfk_rms_norm(const lf_rms_norm_args& a, int sm_count, cudaStream_t s
     return pick_row_shape<norm_go, __half>(a.n, many, a, sm_count, s);
 }
 
-static cudaError_t sum_rows(const float* partial, int rows, int n, float* out, cudaStream_t s)
+cudaError_t lfk_sum_rows(const float* partial, int rows, int n, float* out, float* out2, int n_first, cudaStream_t s)
 {
-    return lf_launch(k_sum_rows, dim3((unsigned)ceil_div(n, 32)), 1024, 0, s, partial, rows, n, out);
+    return lf_launch(k_sum_rows, dim3((unsigned)ceil_div(n, 32)), 1024, 0, s, partial, rows, n, out, out2, n_first);
 }
 
 cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s,
@@ -664,7 +624,7 @@ cudaError_t lfk_rms_norm_backward(const lf_rms_norm_backward_args& a, float* par
     else e = pick_row_shape<norm_backward_go, __half>(a.n, many, a, partial, sm_count, s, &grid);
     *launches = 1;
     if (e == cudaSuccess && a.dgain && grid > 0) {
-        e = sum_rows(partial, grid, a.n, a.dgain, s);
+        e = lfk_sum_rows(partial, grid, a.n, a.dgain, nullptr, a.n, s);
         *launches = 2;
     }
     return e;

@@ -324,4 +324,48 @@ __device__ __forceinline__ void dequantize8(uint2 q, unsigned byte, float (&v)[8
     from_e4m3x4(q.x, s, v[0], v[1], v[2], v[3]);
     from_e4m3x4(q.y, s, v[4], v[5], v[6], v[7]);
 }
+
+// ---- a row per block or group of threads ---------------------------------------------------------
+inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* red)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if (TPR > 32) {
+        __syncthreads();                     // the previous row's partial sums have been read
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < TPR / 32; ++i) v += red[i];
+    }
+    return v;
+}
+__device__ __forceinline__ void cp_async16(unsigned dst, const void* src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// Threads per row: four vectors per thread when there are rows enough to fill the device, otherwise
+// one, so that a few rows are read by as many threads as they have vectors.
+template <template <typename, int, int> class F, typename T, typename... A>
+cudaError_t pick_row_shape(int n, bool many, A&&... args)
+{
+    const int nv = n >> 3;
+    if (many) {
+        if (nv <= 32) return F<T, 32, 1>::go(args...);
+        else if (nv <= 64) return F<T, 32, 2>::go(args...);
+        else if (nv <= 128) return F<T, 32, 4>::go(args...);
+        else if (nv <= 256) return F<T, 64, 4>::go(args...);
+        else if (nv <= 512) return F<T, 128, 4>::go(args...);
+        else if (nv <= 1024) return F<T, 256, 4>::go(args...);
+        else return F<T, 512, 4>::go(args...);
+    } else {
+        if (nv <= 32) return F<T, 32, 1>::go(args...);
+        else if (nv <= 128) return F<T, 128, 1>::go(args...);
+        else if (nv <= 512) return F<T, 512, 1>::go(args...);
+        else if (nv <= 1024) return F<T, 512, 2>::go(args...);
+        else return F<T, 512, 4>::go(args...);
+    }
+}
 }  // namespace lfrow
