@@ -23,10 +23,17 @@ namespace {
 using namespace lfrow;
 
 constexpr int LB_BK = 128;                               // a block of the contraction, bytes and numbers
-constexpr int LB_RING_BYTES = LT_STAGES * LT_STAGE_BYTES;
-constexpr int LB_EPI_BYTES = 8 * 4096;                   // 32 rows x 128 bytes per warp that finishes
-constexpr int LB_THREADS = 384;                          // a warpgroup with producer and issuer, two that finish
-constexpr int LB_REGS_LOW = 56, LB_REGS_HIGH = 224;      // 56 + 2 * 224 = 3 * 168: what the block was launched with
+constexpr int LB_STAGES = 6;
+constexpr int LB_RING_BYTES = LB_STAGES * LT_STAGE_BYTES;
+// Warps: eight finish, one loads, one issues, and where columns have scales of their own one brings them.  Then registers move
+// to the two warpgroups that finish, 40 + 2 * 232 = 3 * 168, without them 20 to 30 are spilled in the loop (758 us instead of
+// 857 for 4096 x 8192 -> 16384); with one scale for 128 columns 168 do, and 320 threads are faster than 384 (487 against 519 us for 8192 x 4096 -> 16384).
+template <bool ROWS> struct lb_warps { static constexpr int threads = 320, finish = 0, load = 8, issue = 9; };
+template <> struct lb_warps<true> { static constexpr int threads = 384, finish = 4, load = 0, issue = 1, scales = 2, regs_low = 40, regs_high = 232; };
+constexpr int LB_SLOTS = 8;                              // column scales: blocks whose scales lie in shared memory
+constexpr int LB_SLOT_BYTES = (128 + 256) * 4;           // of 128 rows and 256 columns
+constexpr int LB_EPI_BYTES = 8 * 4096;                   // tiles: 32 rows x 128 bytes per warp that finishes
+static_assert(LB_SLOTS * LB_SLOT_BYTES <= LB_EPI_BYTES, "either use of the space fits");
 constexpr size_t LB_SMEM = (size_t)LB_RING_BYTES + LB_EPI_BYTES + 1024 + 512;
 constexpr int LBS_THREADS = 512, LBS_STAGES = 4, LBS_LD = 132;
 constexpr int LBS_TILE_BYTES = 128 * LBS_LD * 4;
@@ -60,35 +67,61 @@ __device__ __forceinline__ void lb_mma(unsigned d_tmem, unsigned long long a, un
                      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                      ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
 }
-// the four instructions of a stage
+// Low word of a K-major operand block's descriptor (lt_desc); the high one is the same for all.  What is added to the
+// address, in 16-byte units, cannot leave its 14 bits: shared memory ends below 256 KB.
+__device__ __forceinline__ unsigned lb_desc_low(unsigned addr) { return (unsigned)lt_desc<false>(addr); }
+// the four instructions of a stage: `a` its first block's descriptor
 template <bool PAIR>
-__device__ __forceinline__ void lb_products(unsigned d_tmem, unsigned a_addr, unsigned b_addr, unsigned idesc)
+__device__ __forceinline__ void lb_products(unsigned d_tmem, unsigned a, unsigned idesc)
 {
+    const unsigned long long high = lt_desc<false>(0) & 0xFFFFFFFF00000000ull;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-        lb_mma<PAIR>(d_tmem, lt_desc<false>(a_addr + lt_step<false>(kk)), lt_desc<false>(b_addr + lt_step<false>(kk)), idesc, kk > 0 ? 1u : 0u);
+    for (unsigned kk = 0; kk < 4; ++kk)
+        lb_mma<PAIR>(d_tmem, high | (a + 2 * kk), high | (a + (LT_BLOCK_BYTES >> 4) + 2 * kk), idesc, kk > 0 ? 1u : 0u);
 }
 
 template <typename OUT> struct half_of { typedef OUT type; };          // type of `add`
 template <> struct half_of<float> { typedef __nv_bfloat16 type; };     // (none there)
 
-// acc += scale * the 32 columns of an accumulator in t; ROWS: the scales of the columns lie in shared memory
-template <bool ROWS>
-__device__ __forceinline__ void lb_scale_add(float* acc, const float* t, float sa, const float4* sb)
+// acc += s * the COLS columns of an accumulator in t, a row of them per lane
+template <int COLS>
+__device__ __forceinline__ void lb_scale_add(float* acc, const float* t, float s)
 {
 #pragma unroll
-    for (int g = 0; g < 8; ++g) {
-        float2 lo, hi;
-        if (ROWS) {
-            const float4 b = sb[g];
-            lo = mul2(f2(sa), make_float2(b.x, b.y));
-            hi = mul2(f2(sa), make_float2(b.z, b.w));
-        } else {
-            lo = hi = f2(sa);
+    for (int i = 0; i < COLS; i += 2) {
+        const float2 r = fma2(f2(s), make_float2(t[i], t[i + 1]), make_float2(acc[i], acc[i + 1]));
+        acc[i] = r.x; acc[i + 1] = r.y;
+    }
+}
+// Where columns have scales of their own, an accumulator is taken in fragments: a lane has two neighbouring columns, 2 (lane % 4), of
+// every eight, of the rows lane / 4 + 0, 8, 16, 24, so that a column's scale serves four rows (a row per lane needed a scale from
+// shared memory for every product).  Of 16 columns: [rows 0, 8 | 16, 24][eight columns][row][column].
+__device__ __forceinline__ void lb_ld_fragments(unsigned from, float* r)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(r[8 * h]), "=f"(r[8 * h + 1]), "=f"(r[8 * h + 2]), "=f"(r[8 * h + 3]), "=f"(r[8 * h + 4]), "=f"(r[8 * h + 5]),
+                       "=f"(r[8 * h + 6]), "=f"(r[8 * h + 7]) : "r"(from + ((unsigned)(16 * h) << 16)) : "memory");
+}
+template <bool FRAGMENTS>
+__device__ __forceinline__ void lb_ld(unsigned from, float (&r)[16])
+{
+    if (FRAGMENTS) lb_ld_fragments(from, r);
+    else lfptx::tmem_ld16_async(from, r);
+}
+// acc += sr[row] * sc[column] * 16 columns in fragments
+__device__ __forceinline__ void lb_scale_add(float* acc, const float* t, const float (&sr)[4], const float2* sc)
+{
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        const float2 s = sc[4 * g];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 8 * (i >> 1) + 4 * g + 2 * (i & 1);
+            const float2 r = fma2(mul2(f2(sr[i]), s), make_float2(t[at], t[at + 1]), make_float2(acc[at], acc[at + 1]));
+            acc[at] = r.x; acc[at + 1] = r.y;
         }
-        const float2 r0 = fma2(lo, make_float2(t[4 * g], t[4 * g + 1]), make_float2(acc[4 * g], acc[4 * g + 1]));
-        const float2 r1 = fma2(hi, make_float2(t[4 * g + 2], t[4 * g + 3]), make_float2(acc[4 * g + 2], acc[4 * g + 3]));
-        acc[4 * g] = r0.x; acc[4 * g + 1] = r0.y; acc[4 * g + 2] = r1.x; acc[4 * g + 3] = r1.y;
     }
 }
 
@@ -174,13 +207,43 @@ __device__ __forceinline__ void lb_finish(float (&acc)[128], const LbParams& P, 
     }
 }
 
+// The same from fragments: a lane stores two columns at a time, four lanes 32 bytes of a row in fp32.
+template <typename OUT>
+__device__ __forceinline__ void lb_finish_fragments(float (&acc)[128], const LbParams& P, int row0, int col0)
+{
+    typedef typename half_of<OUT>::type H;
+    const int lane = threadIdx.x & 31, c0 = col0 + 2 * (lane & 3), r0 = row0 + (lane >> 2);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {                               // eight columns at a time
+        const int col = c0 + 8 * j;
+        if (col >= P.N) break;
+        float2 bias = f2(0.f);
+        if (P.bias) bias = *reinterpret_cast<const float2*>(P.bias + col);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = r0 + 8 * i, at = 16 * (j >> 1) + 8 * (i >> 1) + 4 * (j & 1) + 2 * (i & 1);
+            if (row >= P.M) continue;
+            float2 v = add2(make_float2(acc[at], acc[at + 1]), bias);
+            OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
+            if (sizeof(OUT) == 2) {
+                if (P.add) v = add2(v, unpack2(*reinterpret_cast<const unsigned*>(static_cast<const H*>(P.add) + (size_t)row * P.ld_add + col), H()));
+                *reinterpret_cast<unsigned*>(to) = pack2(v.x, v.y, H());
+            } else {
+                *reinterpret_cast<float2*>(to) = v;
+            }
+        }
+    }
+}
+
 template <typename OUT, bool ROWS>
-__global__ void __launch_bounds__(LB_THREADS, 1)
+__global__ void __launch_bounds__(lb_warps<ROWS>::threads, 1)
 k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const LbParams P)
 {
+    typedef lb_warps<ROWS> W;
     extern __shared__ unsigned char lb_smem_raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lb_smem_raw) + 1023u) & ~(uintptr_t)1023u);
     unsigned char* epi = ring + LB_RING_BYTES;
+    float* slots = reinterpret_cast<float*>(epi);
     LtShared* sh = reinterpret_cast<LtShared*>(epi + LB_EPI_BYTES);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -192,19 +255,20 @@ k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     if (threadIdx.x == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
-        for (int i = 0; i < LT_STAGES; ++i) {
+        for (int i = 0; i < LB_STAGES; ++i) {
             lfptx::mbar_init(lfptx::smem_u32(&sh->full[i]), 1);
             lfptx::mbar_init(lfptx::smem_u32(&sh->empty[i]), 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            lfptx::mbar_init(lfptx::smem_u32(&sh->acc_full[i]), 1);
-            lfptx::mbar_init(lfptx::smem_u32(&sh->acc_empty[i]), 16);   // eight finishing warps of each CTA
+        for (int i = 0; i < 2; ++i) lfptx::mbar_init(lfptx::smem_u32(&sh->acc_empty[i]), 16);   // eight finishing warps of each CTA
+        for (int i = 0; i < LB_SLOTS; ++i) {
+            lfptx::mbar_init(lfptx::smem_u32(&sh->scaled[i]), 1);
+            lfptx::mbar_init(lfptx::smem_u32(&sh->scale_free[i]), 8);
         }
         sh->abort_flag = 0u;
         sh->prog_it = 0u;
         lfptx::mbar_fence_init();
     }
-    if (warp == 1) {
+    if (warp == W::issue) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(lfptx::smem_u32(&sh->tmem_base)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -217,9 +281,9 @@ k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     lf_grid_wait();                  // (by every thread: the bounded waits below do not count the time until then)
     lf_grid_release();
 
-    if (warp < 4) {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LB_REGS_LOW));
-      if (warp == 0) {
+    if (warp < W::finish || warp >= W::finish + 8) {
+      if constexpr (ROWS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W::regs_low));
+      if (warp == W::load) {
         // ------------------------------ TMA producer: this CTA's halves -------------------------
         if (lane == 0) {
             unsigned it = 0;
@@ -229,8 +293,8 @@ k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 lp_tile(t, P, tm, tn);
                 const int m0 = (tm * 2 + (int)rank) * 128, n0 = (tn * 2 + (int)rank) * 128;
                 for (int ks = 0; ks < n_k; ++ks, ++it) {
-                    const unsigned st = it % LT_STAGES, use = it / LT_STAGES;
-                    if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->empty[st]), (use - 1) & 1u, P, sh)) { ok = false; break; }
+                    const unsigned st = it % LB_STAGES, use = it / LB_STAGES;
+                    if (use > 0 && !lt_wait<false>(lfptx::smem_u32(&sh->empty[st]), (use - 1) & 1u, P, sh)) { ok = false; break; }
                     const unsigned lbar = lfptx::smem_u32(&sh->full[st]);
                     if (P.withhold && pair == 0 && rank == 1 && it == 0) continue;    // test hook
                     if (rank == 0) lfptx::mbar_arrive_expect_tx(lbar, 2u * LT_STAGE_BYTES);
@@ -242,85 +306,131 @@ k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             }
             sh->prog_it = it;
         }
-      } else if (warp == 1) {
+      } else if (warp == W::issue) {
         // ------------------------------ MMA issuer (leader CTA) ---------------------------------
+        // One thread, and a stage's products take it little longer than the tensor cores: descriptors are a word counted
+        // up, and the next stage's barrier is looked at while this one's products are being issued.
         if (lane == 0 && rank == 0) {
-            unsigned it = 0;                    // stages, and accumulators, one for each
-            bool ok = true;
+            unsigned it = 0, st = 0, round = 0;      // stages, and accumulators, one for each
+            bool ok = true, there = false;
+            const unsigned first = lb_desc_low(lfptx::smem_u32(ring)), full0 = lfptx::smem_u32(&sh->full[0]), empty0 = lfptx::smem_u32(&sh->empty[0]);
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
                 for (int ks = 0; ks < n_k; ++ks, ++it) {
-                    const unsigned ab = it & 1u, use = it >> 1, st = it % LT_STAGES;
-                    if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->acc_empty[ab]), (use - 1) & 1u, P, sh)) { ok = false; break; }
-                    if (!lt_wait(lfptx::smem_u32(&sh->full[st]), (it / LT_STAGES) & 1u, P, sh)) { ok = false; break; }
+                    const unsigned ab = it & 1u, use = it >> 1;
+                    if (!there && !lt_wait<false>(full0 + 8u * st, round & 1u, P, sh)) { ok = false; break; }
+                    if (use > 0 && !lt_wait<false>(lfptx::smem_u32(&sh->acc_empty[ab]), (use - 1) & 1u, P, sh)) { ok = false; break; }
                     lfptx::tc_fence_after();
-                    const unsigned a_addr = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
-                    lb_products<true>(tmem_base + ab * 256u, a_addr, a_addr + LT_BLOCK_BYTES, P.idesc);
-                    lt_commit<true>(lfptx::smem_u32(&sh->empty[st]));
-                    lt_commit<true>(lfptx::smem_u32(&sh->acc_full[ab]));
+                    lb_products<true>(tmem_base + ab * 256u, first + st * (LT_STAGE_BYTES >> 4), P.idesc);
+                    // the block's products are done: its stage may be loaded again, its accumulator be read
+                    lt_commit<true>(empty0 + 8u * st);
+                    if (++st == LB_STAGES) { st = 0; ++round; }
+                    there = lfptx::mbar_test_wait(full0 + 8u * st, round & 1u);
                 }
             }
         }
       }
-    } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(LB_REGS_HIGH));
-        // ------------------------------ scales and epilogue (warps 4..11 of both CTAs) -----------
-        // A warp has one 32-lane quadrant (32 rows) and one half (128 columns, one tile of weights) of the accumulators.
-        const int quad = warp & 3, half = (warp - 4) >> 2;
-        const unsigned leader_acc_empty = lfptx::map_to_cta(lfptx::smem_u32(&sh->acc_empty[0]), 0);
-        unsigned char* blk = epi + (warp - 4) * 4096;
-        unsigned c = 0;
+      if constexpr (ROWS) if (warp == W::scales) {
+        // ------------------------------ scales of this CTA's rows and of all columns, into slots ------
+        unsigned it = 0;
         bool ok = true;
         for (int t = pair; t < n_tiles && ok; t += n_pairs) {
             int tm, tn;
             lp_tile(t, P, tm, tn);
-            const int row0 = (tm * 2 + (int)rank) * 128 + quad * 32, col0 = tn * 256 + half * 128, row = row0 + lane;
-            const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * 128u;
-            // scales of the next block, on their way while this one's products are waited for
-            const float* sa = P.sa + (row < P.M ? row : 0);
-            const float* sb = ROWS ? P.sb + min(col0 + 4 * lane, P.N - 4) : P.sb + (size_t)min(col0 >> 7, (P.N - 1) >> 7) * n_k;
-            const size_t sb_step = ROWS ? (size_t)P.N : 1;
-            float sa_next = *sa;
-            float4 sb_next = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (ROWS) sb_next = *reinterpret_cast<const float4*>(sb);
-            else sb_next.x = *sb;
+            const int m0 = (tm * 2 + (int)rank) * 128, n0 = tn * 256;
+            float4 next_a, next_b0, next_b1;            // a block ahead
+            auto send_for = [&](int ks) {
+                const float *sa = P.sa + (size_t)ks * P.M, *sb = P.sb + (size_t)ks * P.N;
+                next_a = make_float4(sa[min(m0 + lane, P.M - 1)], sa[min(m0 + 32 + lane, P.M - 1)], sa[min(m0 + 64 + lane, P.M - 1)], sa[min(m0 + 96 + lane, P.M - 1)]);
+                next_b0 = *reinterpret_cast<const float4*>(sb + min(n0 + 4 * lane, P.N - 4));
+                next_b1 = *reinterpret_cast<const float4*>(sb + min(n0 + 128 + 4 * lane, P.N - 4));
+            };
+            send_for(0);
+            for (int ks = 0; ks < n_k; ++ks, ++it) {
+                const unsigned sl = it % LB_SLOTS, use = it / LB_SLOTS;
+                if (use > 0 && !lt_wait<false>(lfptx::smem_u32(&sh->scale_free[sl]), (use - 1) & 1u, P, sh)) { ok = false; break; }
+                float* slot = slots + sl * (LB_SLOT_BYTES / 4);
+                slot[lane] = next_a.x; slot[32 + lane] = next_a.y; slot[64 + lane] = next_a.z; slot[96 + lane] = next_a.w;
+                reinterpret_cast<float4*>(slot + 128)[lane] = next_b0;
+                reinterpret_cast<float4*>(slot + 256)[lane] = next_b1;
+                __syncwarp();
+                if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->scaled[sl]));
+                if (ks + 1 < n_k) send_for(ks + 1);
+            }
+        }
+      }
+    } else {
+        if constexpr (ROWS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W::regs_high));
+        // ------------------------------ scales and epilogue (eight warps of both CTAs) -----------
+        // A warp has one 32-lane quadrant (32 rows) and one half (128 columns, one tile of weights) of the accumulators.
+        const int quad = warp & 3, half = (warp - W::finish) >> 2;
+        const unsigned leader_acc_empty = lfptx::map_to_cta(lfptx::smem_u32(&sh->acc_empty[0]), 0);
+        const unsigned lane_addr = tmem_base + ((unsigned)(quad * 32) << 16) + half * 128u;
+        unsigned char* blk = epi + (warp - W::finish) * 4096;
+        unsigned c = 0, st = 0, round = 0;
+        bool ok = true;
+        for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+            int tm, tn;
+            lp_tile(t, P, tm, tn);
+            const int row0 = (tm * 2 + (int)rank) * 128 + quad * 32, col0 = tn * 256 + half * 128;
+            // one scale for the columns: scales of a block are sent for while the one before it is being added
+            const float *sa = P.sa, *sb = P.sb;
+            float sa_next = 0.f, sb_next = 0.f;
+            if (!ROWS) {
+                sa += min(row0 + lane, P.M - 1);
+                sb += (size_t)min(col0 >> 7, (P.N - 1) >> 7) * n_k;
+                sa_next = *sa;
+                sb_next = *sb;
+            }
             float acc[128];
 #pragma unroll
             for (int i = 0; i < 128; ++i) acc[i] = 0.f;
 #pragma unroll 1
             for (int ks = 0; ks < n_k; ++ks, ++c) {
-                const unsigned ab = c & 1u;
-                const float s = ROWS ? sa_next : sa_next * sb_next.x;
-                float4* mine = reinterpret_cast<float4*>(blk + (ks & 1) * 512);
-                if (ROWS) mine[lane] = sb_next;
-                if (ks + 1 < n_k) {
-                    sa += P.M;
-                    sb += sb_step;
-                    sa_next = *sa;
-                    if (ROWS) sb_next = *reinterpret_cast<const float4*>(sb);
-                    else sb_next.x = *sb;
-                }
-                if (ROWS) __syncwarp();
-                if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), (c >> 1) & 1u, P, sh)) { ok = false; break; }
+                const unsigned ab = c & 1u, from = lane_addr + ab * 256u;
+                float s = 0.f;
+                if (!ROWS) {
+                    s = sa_next * sb_next;
+                    if (ks + 1 < n_k) {
+                        sa += P.M;
+                        ++sb;
+                        sa_next = *sa;
+                        sb_next = *sb;
+                    }
+                } else if (!lt_wait<false>(lfptx::smem_u32(&sh->scaled[c % LB_SLOTS]), (c / LB_SLOTS) & 1u, P, sh)) { ok = false; break; }
+                if (!lt_wait<false>(lfptx::smem_u32(&sh->empty[st]), round & 1u, P, sh)) { ok = false; break; }
+                if (++st == LB_STAGES) { st = 0; ++round; }
                 lfptx::tc_fence_after();
-                float r[2][32];
-                const unsigned from = lane_addr + ab * 256u;
-                lfptx::tmem_ld32_async(from, r[0]);
+                const float* slot = slots + (c % LB_SLOTS) * (LB_SLOT_BYTES / 4);
+                float sr[4] = {0.f, 0.f, 0.f, 0.f};
+                if (ROWS) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    lfptx::tmem_wait_ld32(r[j & 1]);
-                    if (j < 3) {
-                        lfptx::tmem_ld32_async(from + 32 * (j + 1), r[(j + 1) & 1]);
+                    for (int i = 0; i < 4; ++i) sr[i] = slot[quad * 32 + 8 * i + (lane >> 2)];
+                }
+                const float2* sc = reinterpret_cast<const float2*>(slot + 128 + 128 * half) + (lane & 3);
+                // 16 columns at a time, the next ones on their way
+                float r[2][16];
+                lb_ld<ROWS>(from, r[0]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    lfptx::tmem_wait_ld16(r[j & 1]);
+                    if (j < 7) {
+                        lb_ld<ROWS>(from + 16 * (j + 1), r[(j + 1) & 1]);
                     } else {
                         lfptx::tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) lt_arrive_cluster(leader_acc_empty + ab * 8u);
+                        if (lane == 0) lt_arrive_cluster_relaxed(leader_acc_empty + ab * 8u);
                     }
-                    lb_scale_add<ROWS>(acc + 32 * j, r[j & 1], s, mine + 8 * j);
+                    if (ROWS) lb_scale_add(acc + 16 * j, r[j & 1], sr, sc + 8 * j);
+                    else lb_scale_add<16>(acc + 16 * j, r[j & 1], s);
+                }
+                if (ROWS) {
+                    __syncwarp();
+                    if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->scale_free[c % LB_SLOTS]));
                 }
             }
             if (!ok) break;
-            __syncwarp();
-            lb_finish<OUT>(acc, P, row0, col0, blk);
+            if (ROWS) lb_finish_fragments<OUT>(acc, P, row0, col0);
+            else lb_finish<OUT>(acc, P, row0, col0, blk);
         }
     }
 
@@ -337,19 +447,19 @@ k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             const unsigned it_l = sh->prog_it, it_p = lt_ld_cluster_u32(lfptx::map_to_cta(lfptx::smem_u32(&sh->prog_it), 1));
             const unsigned hi = max(it_l, it_p), lo = min(it_l, it_p);
             for (unsigned j = lo; j < hi; ++j) {
-                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % LB_STAGES]);
                 if (j >= it_l) lfptx::mbar_arrive_expect_tx(bar, LT_STAGE_BYTES);                // only the peer loaded
                 else lt_complete_tx(bar, LT_STAGE_BYTES);                                        // only the leader loaded
             }
             const unsigned long long t0 = lfptx::globaltimer_ns();
-            for (unsigned j = hi > LT_STAGES ? hi - LT_STAGES : 0; j < hi; ++j) {
-                const unsigned bar = lfptx::smem_u32(&sh->full[j % LT_STAGES]);
-                while (!lfptx::mbar_try_wait(bar, (j / LT_STAGES) & 1u) && lfptx::globaltimer_ns() - t0 < 50000000ull) { }
+            for (unsigned j = hi > LB_STAGES ? hi - LB_STAGES : 0; j < hi; ++j) {
+                const unsigned bar = lfptx::smem_u32(&sh->full[j % LB_STAGES]);
+                while (!lfptx::mbar_try_wait(bar, (j / LB_STAGES) & 1u) && lfptx::globaltimer_ns() - t0 < 50000000ull) { }
             }
         }
     }
     lfptx::cluster_sync_all();
-    if (warp == 1) {
+    if (warp == W::issue) {
         lfptx::tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
     }
@@ -418,7 +528,7 @@ k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if (lane == 0) {
             int ks = LBS_STAGES;
             for (; ks < n_k; ++ks) {
-                if (!lt_wait(lfptx::smem_u32(&sh->empty[ks % LBS_STAGES]), (unsigned)(ks / LBS_STAGES - 1) & 1u, P, sh)) break;
+                if (!lt_wait<false>(lfptx::smem_u32(&sh->empty[ks % LBS_STAGES]), (unsigned)(ks / LBS_STAGES - 1) & 1u, P, sh)) break;
                 load_stage(ks);
             }
             // after giving up: do not let the CTA go on under loads that are still landing
@@ -434,11 +544,11 @@ k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if (lane == 0) {
             for (int ks = 0; ks < n_k; ++ks) {
                 const unsigned ab = (unsigned)ks & 1u, use = (unsigned)ks >> 1, st = (unsigned)ks % LBS_STAGES;
-                if (use > 0 && !lt_wait(lfptx::smem_u32(&sh->acc_empty[ab]), (use - 1) & 1u, P, sh)) break;
-                if (!lt_wait(lfptx::smem_u32(&sh->full[st]), (unsigned)(ks / LBS_STAGES) & 1u, P, sh)) break;
+                if (use > 0 && !lt_wait<false>(lfptx::smem_u32(&sh->acc_empty[ab]), (use - 1) & 1u, P, sh)) break;
+                if (!lt_wait<false>(lfptx::smem_u32(&sh->full[st]), (unsigned)(ks / LBS_STAGES) & 1u, P, sh)) break;
                 lfptx::tc_fence_after();
                 const unsigned a_addr = lfptx::smem_u32(ring + (size_t)st * LT_STAGE_BYTES);
-                lb_products<false>(tmem_base + ab * 128u, a_addr, a_addr + LT_BLOCK_BYTES, P.idesc);
+                lb_products<false>(tmem_base + ab * 128u, lb_desc_low(a_addr), P.idesc);
                 lt_commit<false>(lfptx::smem_u32(&sh->empty[st]));
                 lt_commit<false>(lfptx::smem_u32(&sh->acc_full[ab]));
             }
@@ -470,15 +580,31 @@ k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 scales_of();
             }
             if (ROWS) __syncwarp();
-            if (!lt_wait(lfptx::smem_u32(&sh->acc_full[ab]), ((unsigned)ks >> 1) & 1u, P, sh)) break;
+            if (!lt_wait<false>(lfptx::smem_u32(&sh->acc_full[ab]), ((unsigned)ks >> 1) & 1u, P, sh)) break;
             lfptx::tc_fence_after();
-            float r[64];
-            lfptx::tmem_ld_row(tmem_base + ((unsigned)(quad * 32) << 16) + ab * 128u + half * 64u, r);
-            lfptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->acc_empty[ab]));
-            lb_scale_add<ROWS>(acc, r, s, reinterpret_cast<const float4*>(mine));
-            lb_scale_add<ROWS>(acc + 32, r + 32, s, reinterpret_cast<const float4*>(mine) + 8);
+            const float4* column = reinterpret_cast<const float4*>(mine);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float r[32];
+                lfptx::tmem_ld32_async(tmem_base + ((unsigned)(quad * 32) << 16) + ab * 128u + half * 64u + 32 * j, r);
+                lfptx::tmem_wait_ld32(r);
+                if (j == 1) {
+                    lfptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->acc_empty[ab]));
+                }
+                if (ROWS) {
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const float4 b = column[8 * j + g];
+                        const float f[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[32 * j + 4 * g + i] = fmaf(s * f[i], r[4 * g + i], acc[32 * j + 4 * g + i]);
+                    }
+                } else {
+                    lb_scale_add<32>(acc + 32 * j, r, s);
+                }
+            }
         }
         float* to = tile + (quad * 32 + lane) * LBS_LD + half * 64;
 #pragma unroll
@@ -542,6 +668,8 @@ k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
 }
 
+int lb_threads(bool rows) { return rows ? lb_warps<true>::threads : lb_warps<false>::threads; }
+
 typedef void (*lb_kernel)(const CUtensorMap, const CUtensorMap, const LbParams);
 
 // kernel of a result type and kind of column scales; splits = 0: CTA pairs
@@ -596,7 +724,7 @@ int lf_blocks_tc_init(lf_ops* o)
             if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LB_SMEM) != cudaSuccess) return LF_ECUDA;
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute at[2];
-            lt_cluster_config(&cfg, at, 32, LB_THREADS, 2, LB_SMEM, nullptr);
+            lt_cluster_config(&cfg, at, 32, lb_threads(rows != 0), 2, LB_SMEM, nullptr);
             int n = 0;
             if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return LF_ECUDA;
             if (o->max_block_pairs < 0 || n < o->max_block_pairs) o->max_block_pairs = n;
@@ -633,7 +761,7 @@ int lf_blocks_tc(lf_ops* o, const lf_product_blocks_args& a)
         P.band = 8;
         const long long tiles = (long long)P.tiles_m * P.tiles_n;
         const int pairs = tiles < o->max_block_pairs ? (int)tiles : o->max_block_pairs;
-        lt_cluster_config(&cfg, at, 2 * pairs, LB_THREADS, 2, LB_SMEM, o->stream);
+        lt_cluster_config(&cfg, at, 2 * pairs, lb_threads(a.b_tiles == 0), 2, LB_SMEM, o->stream);
         LF_OPS_TRY(o, cudaLaunchKernelEx(&cfg, f, map_a, map_b, P));
         o->stats.form = LF_FORM_PAIRS;
         o->stats.splits = 1;

@@ -18,6 +18,8 @@ struct LtShared {
     unsigned long long empty[LT_STAGES];
     unsigned long long acc_full[2];
     unsigned long long acc_empty[2];
+    unsigned long long scaled[8];      // (8-bit blocks: scales of a stage are there ...
+    unsigned long long scale_free[8];  //  ... and have been read)
     unsigned tmem_base;
     volatile unsigned abort_flag;
     unsigned prog_it;                  // stage loads this CTA's producer has issued
@@ -25,14 +27,17 @@ struct LtShared {
 static_assert(sizeof(LtShared) <= 512, "the barrier block must fit into the space reserved for it");
 
 // Bounded wait (acquire at cluster scope: the peer's arrivals count too); false once this CTA has given up.
-template <typename PARAMS>
+// CLUSTER = false: an acquire of this CTA's scope, for barriers that order tensor memory and bulk copies only (which have fences of
+// their own): several times a stage, the wider scope's fences were most of the stage's time.
+template <bool CLUSTER = true, typename PARAMS>
 __device__ __forceinline__ bool lt_wait(unsigned bar, unsigned parity, const PARAMS& P, LtShared* sh)
 {
-    if (lfptx::mbar_try_wait_cluster(bar, parity)) return true;
+    auto done = [&]() { return CLUSTER ? lfptx::mbar_try_wait_cluster(bar, parity) : lfptx::mbar_try_wait(bar, parity); };
+    if (done()) return true;
     if (sh->abort_flag) return false;
     const unsigned long long t0 = lfptx::globaltimer_ns();
     unsigned spins = 0;
-    while (!lfptx::mbar_try_wait_cluster(bar, parity)) {
+    while (!done()) {
         if ((++spins & 15u) == 0u) {
             if (sh->abort_flag) return false;
             if (lfptx::globaltimer_ns() - t0 > P.budget_ns || (((spins & 1023u) == 0u) && *((volatile unsigned*)P.status) != 0u)) {
@@ -75,6 +80,11 @@ __device__ __forceinline__ void lt_commit(unsigned bar)        // PAIR: arrives 
 __device__ __forceinline__ void lt_arrive_cluster(unsigned cluster_bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// the same where no memory that the generic proxy wrote is handed over (the tcgen05 fences order what is)
+__device__ __forceinline__ void lt_arrive_cluster_relaxed(unsigned cluster_bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void lt_complete_tx(unsigned bar, unsigned bytes)
 {
