@@ -2,9 +2,11 @@
 //     loss = w T^2 sum_k p_k (ln p_k - ln q_{i_k}),   dz_v = w T (q_v - sum of p_k with i_k = v)
 // with p the softmax of the teacher's entries and q the softmax of the whole row of logits, both at temperature T.
 //
-// Mathematics: ln p_k - ln q_i = (t_k - z_i) / T + lse(z) - lse(t), so the loss needs of a row only its largest
-// value m, the sum s of e^((z - m) / T), taken together in one pass with s rescaled where m grows, and the picked
-// logits.  lse and loss are differences of numbers larger than themselves: what there is one of per row is in 64 bits.
+// Mathematics: with m and t_m the largest logit and entry, S and P the sums of e^((z - m) / T) and e^((t - t_m) / T),
+//     sum_k p_k (ln p_k - ln q_{i_k}) = sum_k p_k ((t_k - t_m) - (z_{i_k} - m)) / T + ln S - ln P,
+// so the loss needs of a row only m and S, taken together in one pass with S rescaled where m grows, and the picked
+// logits.  Differences come first throughout, so a row of nothing but a type's lowest number is a uniform softmax.  What there is
+// one of per row is in 64 bits.
 //
 // Bound by memory: the loss reads a row once, the gradient reads it and writes one.  A row is cut into parts, a block
 // each, which are a cluster and meet once, over distributed shared memory, with their m and s.  Where the gradient is
@@ -25,7 +27,9 @@ constexpr int DT_THREADS = 288;                 // eight warps for the row, one 
 constexpr int DT_ROW_THREADS = 256;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
-constexpr int DT_STAGE_BYTES = 64 * 1024;       // of a part that stays in shared memory
+constexpr float DT_LARGE_LSE = 65536.f;         // (an eighth of a per cent of the gradient)
+constexpr int DT_STAGE_GROUPS = 4;              // of a part that stay in shared memory
+constexpr int DT_STAGE_BYTES = DT_STAGE_GROUPS * DT_UNROLL * DT_ROW_THREADS * 16;
 
 // ---- 16 bytes of a row -------------------------------------------------------------------------------
 template <typename T>
@@ -89,19 +93,53 @@ struct part_of {
 };
 
 // ---- running maximum and sum of e^((z - m) / T); c = log2(e) / T --------------------------------------
+__device__ __forceinline__ unsigned max2(unsigned a, unsigned b, __nv_bfloat16)
+{
+    const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const unsigned*>(&r);
+}
+__device__ __forceinline__ unsigned max2(unsigned a, unsigned b, __half)
+{
+    const __half2 r = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const unsigned*>(&r);
+}
 struct online {
     float m, s;
     __device__ __forceinline__ void clear() { m = -CUDART_INF_F; s = 0.f; }
-    template <int N>
-    __device__ __forceinline__ void add(const float (&v)[N], float c)
+    // DT_UNROLL pieces; 16-bit maxima two at a time, the rest in packed fp32
+    template <typename T>
+    __device__ __forceinline__ void add(const uint4 (&r)[DT_UNROLL], float c)
     {
-        float top = v[0];
+        constexpr int W = 4 * DT_UNROLL;
+        const unsigned(&w)[W] = reinterpret_cast<const unsigned(&)[W]>(r);
+        float top;
+        if constexpr (sizeof(T) == 2) {
+            unsigned t[4] = {w[0], w[1], w[2], w[3]};
 #pragma unroll
-        for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+            for (int i = 4; i < W; ++i) t[i & 3] = max2(t[i & 3], w[i], T());
+            const float2 f = unpack2(max2(max2(t[0], t[1], T()), max2(t[2], t[3], T()), T()), T());
+            top = fmaxf(f.x, f.y);
+        } else {
+            float t[4] = {__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])};
+#pragma unroll
+            for (int i = 4; i < W; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(w[i]));
+            top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        }
         const float now = fmaxf(m, top), about = now == -CUDART_INF_F ? 0.f : now;
-        s *= ex2((m - about) * c);
+        float2 sum[2] = {make_float2(s * ex2((m - about) * c), 0.f), f2(0.f)};
+        auto pair = [&](int k, float2 v) {
+            const float2 t = mul2(add2(v, f2(-about)), f2(c));
+            sum[k & 1] = add2(sum[k & 1], make_float2(ex2(t.x), ex2(t.y)));
+        };
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s += ex2((v[i] - about) * c);
+            for (int i = 0; i < W; ++i) pair(i, unpack2(w[i], T()));
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i += 2) pair(i >> 1, make_float2(__uint_as_float(w[i]), __uint_as_float(w[i + 1])));
+        }
+        sum[0] = add2(sum[0], sum[1]);
+        s = sum[0].x + sum[0].y;
         m = now;
     }
     __device__ __forceinline__ void join(float m2, float s2, float c)
@@ -110,18 +148,37 @@ struct online {
         s = s * ex2((m - about) * c) + s2 * ex2((m2 - about) * c);
         m = now;
     }
+    __device__ __forceinline__ void add(float v, float c) { join(v, 1.f, c); }
+    // over the row's warps and, where a cluster has it, its parts; in a fixed order
+    __device__ __forceinline__ void join_warps(float2* warp_ms, bool mine, float c)
+    {
+        if (mine) {
+#pragma unroll
+            for (int d = 16; d; d >>= 1) {
+                const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, d);
+                join(m2, s2, c);
+            }
+            if ((threadIdx.x & 31) == 0) warp_ms[threadIdx.x >> 5] = make_float2(m, s);
+        }
+        __syncthreads();
+        clear();
+#pragma unroll
+        for (int w = 0; w < DT_ROW_THREADS / 32; ++w) join(warp_ms[w].x, warp_ms[w].y, c);
+    }
 };
 
 struct entries {                       // the teacher's, of one token
     int at[LF_DISTILL_MAX_TOP];
     float p[LF_DISTILL_MAX_TOP];       // 0: not there
-    float z[LF_DISTILL_MAX_TOP];       // the student's logit
-    double base;                       // sum_k p_k (t_k - z_k) / T - lse(t)
+    float t[LF_DISTILL_MAX_TOP];       // the teacher's logit
+    float z[LF_DISTILL_MAX_TOP];       // the student's
+    double sum;                        // P
+    float top;                         // t_m
     int any, bad;                      // entries at all; an index beyond the vocabulary
 };
 // By one warp.  A sum over lanes adds in a fixed order.
 template <typename T>
-__device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, int token, const T* z, bool loss)
+__device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, int token, const T* z)
 {
     const int lane = threadIdx.x & 31;
     const int* index = a.index + (size_t)token * a.top;
@@ -136,7 +193,7 @@ __device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, in
         bad |= beyond;
         any |= there;
         e.at[k] = there && !beyond ? i : -1;
-        e.p[k] = there ? t : -CUDART_INF_F;
+        e.t[k] = there ? t : -CUDART_INF_F;
         e.z[k] = there && !beyond ? (float)z[i] : 0.f;
         if (there) top = fmaxf(top, t);
     }
@@ -145,31 +202,33 @@ __device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, in
     bad = __any_sync(0xFFFFFFFFu, bad);
     any = __any_sync(0xFFFFFFFFu, any);
     const float inv_t = 1.0f / a.temperature;
-    double sum = 0.0, dot = 0.0;
+    double sum = 0.0;
     for (int k = lane; k < a.top; k += 32) {
-        const float t = e.p[k];
-        float p = 0.f;
-        if (t != -CUDART_INF_F) {
-            p = expf((t - top) * inv_t);
-            sum += (double)p;
-            // (a weight that fp32 does not tell from zero has no part in the loss, whatever logit it falls on)
-            if (loss && p != 0.f) dot += (double)p * ((double)t - (double)e.z[k]);
-        }
+        const float p = e.t[k] != -CUDART_INF_F ? expf((e.t[k] - top) * inv_t) : 0.f;
+        sum += (double)p;
         e.p[k] = p;
     }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
-    }
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
     const float inv = (float)(1.0 / sum);
     for (int k = lane; k < a.top; k += 32) e.p[k] = e.at[k] >= 0 ? e.p[k] * inv : 0.f;
     if (lane == 0) {
-        const double tau = (double)a.temperature;
         e.any = any;
         e.bad = bad;
-        e.base = loss ? dot / (sum * tau) - ((double)top / tau + log(sum)) : 0.0;
+        e.top = top;
+        e.sum = sum;
     }
+}
+// the loss but for weight and T^2, by the same warp; on lane 0
+__device__ __forceinline__ double divergence(const entries& e, int top, double tau, float m, float s)
+{
+    double dot = 0.0;
+    for (int k = threadIdx.x & 31; k < top; k += 32)
+        // (a weight that fp32 does not tell from zero has no part in the loss, whatever logit it falls on)
+        if (e.p[k] != 0.f) dot += (double)e.p[k] * (((double)e.t[k] - (double)e.top) - ((double)e.z[k] - (double)m));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+    return e.bad ? CUDART_NAN : dot / tau + log((double)s) - log(e.sum);
 }
 // dz of the entries that fall on elements [e0, e1): the first of several on one element adds them up, in their order
 template <typename T, typename F>
@@ -201,81 +260,105 @@ __device__ __forceinline__ void store_piece(T* to, const float (&v)[16 / sizeof(
     }
 }
 
+// pieces of dz: f e^((z - m) / T); `none`: zeros, and nothing of z is looked at
+template <typename T>
+__device__ __forceinline__ void gradient_piece(T* to, uint4 u, float m, float c, float f, bool aligned)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    piece16<T> p;
+    float v[N];
+    p.u = u;
+    p.get(v);
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+        const float2 t = mul2(add2(make_float2(v[k], v[k + 1]), f2(-m)), f2(c));
+        const float2 g = mul2(make_float2(ex2(t.x), ex2(t.y)), f2(f));
+        v[k] = g.x; v[k + 1] = g.y;
+    }
+    store_piece<T>(to, v, aligned);
+}
+template <typename T>
+__device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool aligned)
+{
+    const float v[16 / sizeof(T)] = {};
+    for (int i = threadIdx.x; i < mine.pieces; i += DT_THREADS) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
+    if ((int)threadIdx.x < mine.edge) dz[mine.at_edge(threadIdx.x)] = (T)0.f;
+}
+// a thread's pieces of a part that are read where they lie: [from, pieces)
+template <typename T>
+__device__ __forceinline__ void online_part(online& o, const T* z, const part_of<T>& mine, int first, float c)
+{
+    const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
+    const unsigned none = minus_infinity(T());
+    for (int i = first + (int)threadIdx.x; i < mine.pieces; i += DT_ROW_THREADS * DT_UNROLL) {
+        uint4 r[DT_UNROLL];
+#pragma unroll
+        for (int u = 0; u < DT_UNROLL; ++u) {
+            const int at = i + u * DT_ROW_THREADS;
+            r[u] = at < mine.pieces ? ld16(from + at) : make_uint4(none, none, none, none);
+        }
+        o.add<T>(r, c);
+    }
+    if ((int)threadIdx.x < mine.edge) o.add((float)z[mine.at_edge(threadIdx.x)], c);
+}
+
 // Loss, lse and, with GRAD, the gradient.  A cluster of `parts` blocks has a token; `staged` pieces of a part stay in shared memory.
 template <typename T, bool GRAD>
 __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a, int parts, int staged)
 {
-    constexpr int N = 16 / (int)sizeof(T);
+    constexpr int N = 16 / (int)sizeof(T), GROUP = DT_ROW_THREADS * DT_UNROLL;
     extern __shared__ __align__(16) uint4 stage[];
     __shared__ entries ent;
-    __shared__ float2 warp_ms[8];
+    __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
     __shared__ float2 part_ms;
     const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     const part_of<T> mine(z, a.vocab, part, parts);
     const float c = LOG2E / a.temperature;
+    const bool row_warp = tid < DT_ROW_THREADS;
+    const int kept = GRAD ? min(staged, mine.pieces) : 0;
     lf_grid_wait();
     lf_grid_release();
     online o;
     o.clear();
-    if (tid < DT_ROW_THREADS) {
+    if (row_warp) {
         const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-        const int kept = GRAD ? min(staged, mine.pieces) : 0;
         if (GRAD) {
             // (a thread reads what it copied itself)
-            for (int i = tid; i < kept; i += DT_ROW_THREADS) cp_async16(lfptx::smem_u32(stage + i), from + i);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
-        float v[DT_UNROLL * N];
-        auto take = [&](const uint4 (&r)[DT_UNROLL]) {
 #pragma unroll
-            for (int u = 0; u < DT_UNROLL; ++u) {
-                piece16<T> p;
-                p.u = r[u];
-                p.get(*reinterpret_cast<float(*)[N]>(v + u * N));
-            }
-            o.add(v, c);
-        };
-        const unsigned none = minus_infinity(T());
-        // what is not kept, and the elements outside of pieces
-        for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS * DT_UNROLL) {
-            uint4 r[DT_UNROLL];
+            for (int g = 0; g < DT_STAGE_GROUPS; ++g) {
 #pragma unroll
-            for (int u = 0; u < DT_UNROLL; ++u) {
-                const int at = i + u * DT_ROW_THREADS;
-                r[u] = at < mine.pieces ? ld16(from + at) : make_uint4(none, none, none, none);
+                for (int u = 0; u < DT_UNROLL; ++u) {
+                    const int i = g * GROUP + u * DT_ROW_THREADS + tid;
+                    if (i < kept) cp_async16(lfptx::smem_u32(stage + i), from + i);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
             }
-            take(r);
         }
-        if (tid < mine.edge) {
-            const float one[1] = {(float)z[mine.at_edge(tid)]};
-            o.add(one, c);
-        }
+        online_part<T>(o, z, mine, kept, c);
         if (GRAD) {
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            for (int i = tid; i < kept; i += DT_ROW_THREADS * DT_UNROLL) {
+            const unsigned none = minus_infinity(T());
+#pragma unroll
+            for (int g = 0; g < DT_STAGE_GROUPS; ++g) {
+                if (g * GROUP + tid >= kept) break;
+                if (g == 0) asm volatile("cp.async.wait_group %0;" ::"n"(DT_STAGE_GROUPS - 1) : "memory");
+                else if (g == 1) asm volatile("cp.async.wait_group %0;" ::"n"(DT_STAGE_GROUPS - 2) : "memory");
+                else if (g == 2) asm volatile("cp.async.wait_group %0;" ::"n"(DT_STAGE_GROUPS - 3) : "memory");
+                else asm volatile("cp.async.wait_group 0;" ::: "memory");
                 uint4 r[DT_UNROLL];
 #pragma unroll
                 for (int u = 0; u < DT_UNROLL; ++u) {
-                    const int at = i + u * DT_ROW_THREADS;
-                    r[u] = at < kept ? stage[at] : make_uint4(none, none, none, none);
+                    const int i = g * GROUP + u * DT_ROW_THREADS + tid;
+                    r[u] = i < kept ? stage[i] : make_uint4(none, none, none, none);
                 }
-                take(r);
+                o.add<T>(r, c);
             }
         }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, o.m, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, o.s, d);
-            o.join(m2, s2, c);
-        }
-        if ((tid & 31) == 0) warp_ms[tid >> 5] = make_float2(o.m, o.s);
     } else if (GRAD || part == 0) {
-        teacher<T>(ent, a, token, z, part == 0);
+        teacher<T>(ent, a, token, z);
     }
-    __syncthreads();
-    o.clear();
-#pragma unroll
-    for (int w = 0; w < 8; ++w) o.join(warp_ms[w].x, warp_ms[w].y, c);
+    __syncwarp();
+    o.join_warps(warp_ms, row_warp, c);
     if (parts > 1) {
         if (tid == 0) part_ms = make_float2(o.m, o.s);
         __syncwarp();
@@ -291,40 +374,33 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
     const float w = a.weight ? a.weight[token] : 1.f;
-    if (part == 0 && tid == 0) {
-        const double lse = (double)o.m / (double)a.temperature + log((double)o.s);
-        if (a.lse) a.lse[token] = (float)lse;
-        double loss = (ent.base + lse) * (double)a.temperature * (double)a.temperature * (double)w;
-        if (ent.bad) loss = CUDART_NAN;
-        a.loss[token] = w == 0.f || !ent.any ? 0.f : (float)loss;
+    if (part == 0 && !row_warp) {
+        const double tau = (double)a.temperature, kl = divergence(ent, a.top, tau, o.m, o.s);
+        if (tid == DT_ROW_THREADS) {
+            if (a.lse) a.lse[token] = (float)((double)o.m / tau + log((double)o.s));
+            a.loss[token] = w == 0.f || !ent.any ? 0.f : (float)(kl * tau * tau * (double)w);
+        }
     }
     if (GRAD) {
         T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
-        const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !ent.any;
-        const float wt = none ? 0.f : ent.bad ? CUDART_NAN_F : w * a.temperature, f = wt / o.s, m = o.m;
-        if (tid < DT_ROW_THREADS) {
-            const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-            const int kept = min(staged, mine.pieces);
-            auto give = [&](int i, uint4 r) {
-                piece16<T> p;
-                float v[N];
-                p.u = r;
-                p.get(v);
-#pragma unroll
-                for (int k = 0; k < N; ++k) v[k] = none ? 0.f : f * ex2((v[k] - m) * c);
-                store_piece<T>(dz + mine.body + (long long)i * N, v, aligned);
-            };
+        const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
+        if (w == 0.f || !ent.any) {
+            zero_part<T>(dz, mine, aligned);
+        } else {
+            const float wt = ent.bad ? CUDART_NAN_F : w * a.temperature, f = wt / o.s, m = o.m;
+            if (row_warp) {
+                const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
 #pragma unroll 4
-            for (int i = tid; i < kept; i += DT_ROW_THREADS) give(i, stage[i]);
+                for (int i = tid; i < kept; i += DT_ROW_THREADS) gradient_piece<T>(dz + mine.body + (long long)i * N, stage[i], m, c, f, aligned);
 #pragma unroll 4
-            for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS) give(i, ld16(from + i));
-            if (tid < mine.edge) {
-                const long long at = mine.at_edge(tid);
-                dz[at] = (T)(none ? 0.f : f * ex2(((float)z[at] - m) * c));
+                for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS)
+                    gradient_piece<T>(dz + mine.body + (long long)i * N, ld16(from + i), m, c, f, aligned);
+                if (tid < mine.edge) {
+                    const long long at = mine.at_edge(tid);
+                    dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
+                }
             }
-        }
-        __syncthreads();
-        if (!none) {
+            __syncthreads();
             const float inv_s = 1.0f / o.s;
             put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
         }
@@ -333,25 +409,43 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
     if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
 }
 
-// dz from z and lse: no part of a row needs to know another
+// dz from z and lse: no part of a row needs to know another.  Where lse is so large that fp32 does not hold its fraction
+// (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
 template <typename T>
 __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distill_args a, int parts)
 {
     constexpr int N = 16 / (int)sizeof(T);
     __shared__ entries ent;
+    __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
     const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
-    const part_of<T> mine(z, a.vocab, part, parts);
+    const bool row_warp = tid < DT_ROW_THREADS;
     lf_grid_wait();
     lf_grid_release();
-    if (tid >= DT_ROW_THREADS) teacher<T>(ent, a, token, z, false);
+    if (!row_warp) teacher<T>(ent, a, token, z);
     __syncthreads();                       // (the entries' logits have been read: dz may be z)
-    const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], inv_t = 1.0f / a.temperature;
-    const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !ent.any;
-    const float wt = none ? 0.f : ent.bad ? CUDART_NAN_F : w * a.temperature;
-    auto q_of = [&](float v) { return ex2(fmaf(v, inv_t, -lse) * LOG2E); };
-    if (tid < DT_ROW_THREADS) {
+    const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], c = LOG2E / a.temperature;
+    const bool large = fabsf(lse) >= DT_LARGE_LSE;
+    if (large && part > 0) return;
+    const part_of<T> mine(z, a.vocab, part, large ? 1 : parts);
+    const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
+    if (w == 0.f || !ent.any) {
+        zero_part<T>(dz, mine, aligned);
+        return;
+    }
+    const float wt = ent.bad ? CUDART_NAN_F : w * a.temperature;
+    float m = lse * a.temperature, scale = 1.f;        // q = scale e^((z - m) / T)
+    if (large) {
+        online o;
+        o.clear();
+        if (row_warp) online_part<T>(o, z, mine, 0, c);
+        o.join_warps(warp_ms, row_warp, c);
+        m = o.m;
+        scale = 1.0f / o.s;
+    }
+    const float f = wt * scale;
+    if (row_warp) {
         const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
         for (int i = tid; i < mine.pieces; i += DT_ROW_THREADS * DT_UNROLL) {
             uint4 r[DT_UNROLL];
@@ -361,23 +455,16 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
 #pragma unroll
             for (int u = 0; u < DT_UNROLL; ++u) {
                 const int at = i + u * DT_ROW_THREADS;
-                if (at >= mine.pieces) break;
-                piece16<T> p;
-                float v[N];
-                p.u = r[u];
-                p.get(v);
-#pragma unroll
-                for (int k = 0; k < N; ++k) v[k] = none ? 0.f : wt * q_of(v[k]);
-                store_piece<T>(dz + mine.body + (long long)at * N, v, aligned);
+                if (at < mine.pieces) gradient_piece<T>(dz + mine.body + (long long)at * N, r[u], m, c, f, aligned);
             }
         }
         if (tid < mine.edge) {
             const long long at = mine.at_edge(tid);
-            dz[at] = (T)(none ? 0.f : wt * q_of((float)z[at]));
+            dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
         }
     }
     __syncthreads();
-    if (!none) put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, q_of);
+    put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
 }
 
 // A part has as much as stays in shared memory, and there are blocks enough to fill the device, up to eight; parts

@@ -468,6 +468,36 @@ def test_distill_what_is_not_finite(ops, V):
         R.check("dz", dz.t[7:], ref[2], R.rounded(ref[2], F32, err[2]))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [40, 5000, 70001])
+def test_distill_rows_of_the_lowest_number(ops, V, dtype):
+    """Every logit masked with the type's lowest number: a uniform softmax; and rows that are shifted as far, in both calls and in place."""
+    g = _gen(V)
+    low = torch.finfo(dtype).min
+    z = torch.full((4, V), low, dtype=dtype, device="cuda")
+    z[1] = -60000.0
+    z[1, ::2] = -60000.0 + (32 if dtype == F16 else 256)
+    z[2, 7:] = 0
+    index, value = torch.randint(7, V, (4, 5), generator=g, device="cuda").int(), _rand(g, 4, 5)
+    index[:, 4] = index[:, 0]
+    weight = torch.ones(4, device="cuda")
+    q = torch.softmax(z.to(R.D), 1)
+    p = torch.softmax(value.to(R.D), 1)
+    dz_ref = q.scatter_add(1, index.long(), -p)
+    loss_ref = (p * (p.log() - torch.log_softmax(z.to(R.D), 1).gather(1, index.long()))).sum(1)
+    err = 1e-5 * q + 2.0 ** -20 * (p.sum(1, keepdim=True) + 0 * q) * (dz_ref < 0)
+    loss, lse, dz = torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.empty_like(z)
+    ops.distill(z, index, value, loss, lse, weight=weight, dz=dz)
+    R.check("loss", loss[[0, 2, 3]], loss_ref[[0, 2, 3]], 1e-5 * loss_ref[[0, 2, 3]].abs() + 1e-5)
+    R.check("dz", dz, dz_ref, R.rounded(dz_ref, dtype, err))
+    for in_place in (False, True):
+        to = z.clone() if in_place else torch.empty_like(z)
+        ops.distill_backward(to if in_place else z, index, value, lse, to, weight=weight)
+        ops.sync()
+        keep = [0, 2, 3] if dtype == F16 else [0, 1, 2, 3]          # (60000 is not beyond 65536, where lse in fp32 is off by 2^-9)
+        R.check("dz backward", to[keep], dz_ref[keep], R.rounded(dz_ref[keep], dtype, err[keep] + 2.0 ** -7 * q[keep]))
+
+
 def test_distill_gradient_against_differences(ops):
     g = _gen(21)
     M, V, top, tau = 3, 30, 5, 1.7
