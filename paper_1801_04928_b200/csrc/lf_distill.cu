@@ -11,7 +11,7 @@
 // Bound by memory: the loss reads a row once, the gradient reads it and writes one.  A row is cut into parts, a block
 // each, which are a cluster and meet once, over distributed shared memory, with their m and s.  Where the gradient is
 // written too, a part keeps what it has read in shared memory, so that the row is read from memory once.
-// The teacher's entries are one warp's work beside the others' pass over the row; the dense part of the gradient is
+// The teacher's entries are one warp's work and the loss another's, beside the others' passes over the row; the dense part of the gradient is
 // written first, then the entries that fall into the part are put right.
 #include <math_constants.h>
 
@@ -23,13 +23,13 @@ namespace {
 
 using namespace lfrow;
 
-constexpr int DT_THREADS = 288;                 // eight warps for the row, one for the teacher's entries
+constexpr int DT_THREADS = 320;                 // eight warps for the row, one for the teacher's entries, one for the loss
 constexpr int DT_ROW_THREADS = 256;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
 constexpr float DT_LARGE_LSE = 65536.f;         // (an eighth of a per cent of the gradient)
-constexpr int DT_STAGE_GROUPS = 4;              // of a part that stay in shared memory
-constexpr int DT_STAGE_BYTES = DT_STAGE_GROUPS * DT_UNROLL * DT_ROW_THREADS * 16;
+constexpr int DT_PART_BYTES = 32 * 1024;        // of a row that a block of the joint kernel has, where eight parts are enough
+constexpr int DT_STAGE_BYTES = 40 * 1024;       // at most of a part that stays in shared memory
 
 // ---- 16 bytes of a row -------------------------------------------------------------------------------
 template <typename T>
@@ -149,36 +149,66 @@ struct online {
         m = now;
     }
     __device__ __forceinline__ void add(float v, float c) { join(v, 1.f, c); }
-    // over the row's warps and, where a cluster has it, its parts; in a fixed order
+    // over the lanes l ^ 1, ^ 2, ... ^ (LANES / 2), so in a fixed order
+    template <int LANES>
+    __device__ __forceinline__ void join_lanes(float c)
+    {
+#pragma unroll
+        for (int d = LANES / 2; d; d >>= 1) {
+            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, d);
+            join(m2, s2, c);
+        }
+    }
+    // over a block's row warps
     __device__ __forceinline__ void join_warps(float2* warp_ms, bool mine, float c)
     {
         if (mine) {
-#pragma unroll
-            for (int d = 16; d; d >>= 1) {
-                const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, d);
-                join(m2, s2, c);
-            }
+            join_lanes<32>(c);
             if ((threadIdx.x & 31) == 0) warp_ms[threadIdx.x >> 5] = make_float2(m, s);
         }
         __syncthreads();
+        const float2 ms = warp_ms[threadIdx.x & (DT_ROW_THREADS / 32 - 1)];
+        m = ms.x;
+        s = ms.y;
+        join_lanes<DT_ROW_THREADS / 32>(c);
+    }
+    // over the blocks of a cluster, at most eight
+    __device__ __forceinline__ void join_parts(unsigned at, int parts, float c)
+    {
+        const int lane = threadIdx.x & 31;
         clear();
-#pragma unroll
-        for (int w = 0; w < DT_ROW_THREADS / 32; ++w) join(warp_ms[w].x, warp_ms[w].y, c);
+        if ((lane & (DT_MAX_PARTS - 1)) < parts)
+            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m), "=f"(s) : "r"(lfptx::map_to_cta(at, (unsigned)(lane & (DT_MAX_PARTS - 1)))) : "memory");
+        __syncwarp();
+        join_lanes<DT_MAX_PARTS>(c);
     }
 };
 
-struct entries {                       // the teacher's, of one token
-    int at[LF_DISTILL_MAX_TOP];
-    float p[LF_DISTILL_MAX_TOP];       // 0: not there
-    float t[LF_DISTILL_MAX_TOP];       // the teacher's logit
-    float z[LF_DISTILL_MAX_TOP];       // the student's
+struct entry_facts {                   // of a token's entries
     double sum;                        // P
     float top;                         // t_m
     int any, bad;                      // entries at all; an index beyond the vocabulary
 };
-// By one warp.  A sum over lanes adds in a fixed order.
+struct entries {                       // the teacher's, of one token
+    int* at;                           // -1: not there
+    float* p;                          // 0: not there
+    float* t;                          // the teacher's logit
+    float* z;                          // the student's
+    float* total;                      // of the first entry on an element: what all of them have; of others < 0
+    entry_facts* facts;
+    __host__ __device__ static constexpr size_t bytes(int top) { return (size_t)top * 20; }
+    __device__ __forceinline__ entries(void* space, int top, entry_facts* f) : facts(f)
+    {
+        at = static_cast<int*>(space);
+        p = reinterpret_cast<float*>(at + top);
+        t = p + top;
+        z = t + top;
+        total = z + top;
+    }
+};
+// By one warp, in two steps: what is read of the row, and what follows from it.  A sum over lanes adds in a fixed order.
 template <typename T>
-__device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, int token, const T* z)
+__device__ __forceinline__ void gather(const entries& e, const lf_distill_args& a, int token, const T* z)
 {
     const int lane = threadIdx.x & 31;
     const int* index = a.index + (size_t)token * a.top;
@@ -201,7 +231,17 @@ __device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, in
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     bad = __any_sync(0xFFFFFFFFu, bad);
     any = __any_sync(0xFFFFFFFFu, any);
-    const float inv_t = 1.0f / a.temperature;
+    if (lane == 0) {
+        e.facts->any = any;
+        e.facts->bad = bad;
+        e.facts->top = top;
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a)
+{
+    const int lane = threadIdx.x & 31;
+    const float inv_t = 1.0f / a.temperature, top = e.facts->top;
     double sum = 0.0;
     for (int k = lane; k < a.top; k += 32) {
         const float p = e.t[k] != -CUDART_INF_F ? expf((e.t[k] - top) * inv_t) : 0.f;
@@ -210,41 +250,49 @@ __device__ __forceinline__ void teacher(entries& e, const lf_distill_args& a, in
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    const float inv = (float)(1.0 / sum);
+    const float inv = 1.0f / (float)sum;
     for (int k = lane; k < a.top; k += 32) e.p[k] = e.at[k] >= 0 ? e.p[k] * inv : 0.f;
-    if (lane == 0) {
-        e.any = any;
-        e.bad = bad;
-        e.top = top;
-        e.sum = sum;
+    if (lane == 0) e.facts->sum = sum;
+    __syncwarp();
+    // several entries on one element: the first adds them up, in their order
+    for (int k = lane; k < a.top; k += 32) {
+        const int at = e.at[k];
+        float total = 0.f;
+        bool first = at >= 0;
+#pragma unroll 8
+        for (int j = 0; j < a.top; ++j) {
+            const bool same = e.at[j] == at;
+            if (same) total += e.p[j];
+            first &= !(same && j < k);
+        }
+        e.total[k] = first ? total : -1.f;
     }
 }
-// the loss but for weight and T^2, by the same warp; on lane 0
-__device__ __forceinline__ double divergence(const entries& e, int top, double tau, float m, float s)
+// The loss, by one warp.  A weight p that fp32 does not tell from zero has no part in it, whatever logit it falls on.
+__device__ __forceinline__ void loss_of(const entries& e, const lf_distill_args& a, int token, float m, float s)
 {
+    const double tau = (double)a.temperature, log_s = log((double)s);
+    const entry_facts facts = *e.facts;
     double dot = 0.0;
-    for (int k = threadIdx.x & 31; k < top; k += 32)
-        // (a weight that fp32 does not tell from zero has no part in the loss, whatever logit it falls on)
-        if (e.p[k] != 0.f) dot += (double)e.p[k] * (((double)e.t[k] - (double)e.top) - ((double)e.z[k] - (double)m));
+    for (int k = threadIdx.x & 31; k < a.top; k += 32)
+        if (e.p[k] != 0.f) dot += (double)e.p[k] * (((double)e.t[k] - (double)facts.top) - ((double)e.z[k] - (double)m));
 #pragma unroll
     for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
-    return e.bad ? CUDART_NAN : dot / tau + log((double)s) - log(e.sum);
+    if ((threadIdx.x & 31) == 0) {
+        const float w = a.weight ? a.weight[token] : 1.f;
+        const double kl = facts.bad ? CUDART_NAN : dot / tau + log_s - log(facts.sum);
+        if (a.lse) a.lse[token] = (float)((double)m / tau + log_s);
+        a.loss[token] = w == 0.f || !facts.any ? 0.f : (float)(kl * tau * tau * (double)w);
+    }
 }
-// dz of the entries that fall on elements [e0, e1): the first of several on one element adds them up, in their order
+// By the row's threads: dz of the entries that fall on elements [e0, e1)
 template <typename T, typename F>
 __device__ __forceinline__ void put_right(const entries& e, int top, long long e0, long long e1, T* dz, float wt, F q_of)
 {
-    for (int k = threadIdx.x; k < top; k += DT_THREADS) {
+    for (int k = threadIdx.x; k < top; k += DT_ROW_THREADS) {
         const int at = e.at[k];
-        if (at < e0 || at >= e1) continue;
-        float p = 0.f;
-        bool first = true;
-        for (int j = 0; j < top; ++j) {
-            if (e.at[j] != at) continue;
-            if (j < k) { first = false; break; }
-            p += e.p[j];
-        }
-        if (first) dz[at] = (T)(wt * (q_of(e.z[k]) - p));
+        // (NaN, the weight of a list that holds one, is no number below zero)
+        if (at >= e0 && at < e1 && !(e.total[k] < 0.f)) dz[at] = (T)(wt * (q_of(e.z[k]) - e.total[k]));
     }
 }
 template <typename T>
@@ -281,7 +329,7 @@ template <typename T>
 __device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool aligned)
 {
     const float v[16 / sizeof(T)] = {};
-    for (int i = threadIdx.x; i < mine.pieces; i += DT_THREADS) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
+    for (int i = threadIdx.x; i < mine.pieces; i += DT_ROW_THREADS) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
     if ((int)threadIdx.x < mine.edge) dz[mine.at_edge(threadIdx.x)] = (T)0.f;
 }
 // a thread's pieces of a part that are read where they lie: [from, pieces)
@@ -302,13 +350,12 @@ __device__ __forceinline__ void online_part(online& o, const T* z, const part_of
     if ((int)threadIdx.x < mine.edge) o.add((float)z[mine.at_edge(threadIdx.x)], c);
 }
 
-// Loss, lse and, with GRAD, the gradient.  A cluster of `parts` blocks has a token; `staged` pieces of a part stay in shared memory.
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a, int parts, int staged)
+// Loss and lse of a token's row; a cluster of `parts` blocks has a token.
+template <typename T>
+__global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a, int parts)
 {
-    constexpr int N = 16 / (int)sizeof(T), GROUP = DT_ROW_THREADS * DT_UNROLL;
-    extern __shared__ __align__(16) uint4 stage[];
-    __shared__ entries ent;
+    extern __shared__ __align__(16) unsigned char space[];
+    __shared__ entry_facts facts;
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
     __shared__ float2 part_ms;
     const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
@@ -316,94 +363,108 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
     const part_of<T> mine(z, a.vocab, part, parts);
     const float c = LOG2E / a.temperature;
     const bool row_warp = tid < DT_ROW_THREADS;
-    const int kept = GRAD ? min(staged, mine.pieces) : 0;
+    const entries ent(space, a.top, &facts);
     lf_grid_wait();
     lf_grid_release();
     online o;
     o.clear();
     if (row_warp) {
-        const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-        if (GRAD) {
-            // (a thread reads what it copied itself)
-#pragma unroll
-            for (int g = 0; g < DT_STAGE_GROUPS; ++g) {
-#pragma unroll
-                for (int u = 0; u < DT_UNROLL; ++u) {
-                    const int i = g * GROUP + u * DT_ROW_THREADS + tid;
-                    if (i < kept) cp_async16(lfptx::smem_u32(stage + i), from + i);
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            }
-        }
-        online_part<T>(o, z, mine, kept, c);
-        if (GRAD) {
-            const unsigned none = minus_infinity(T());
-#pragma unroll
-            for (int g = 0; g < DT_STAGE_GROUPS; ++g) {
-                if (g * GROUP + tid >= kept) break;
-                if (g == 0) asm volatile("cp.async.wait_group %0;" ::"n"(DT_STAGE_GROUPS - 1) : "memory");
-                else if (g == 1) asm volatile("cp.async.wait_group %0;" ::"n"(DT_STAGE_GROUPS - 2) : "memory");
-                else if (g == 2) asm volatile("cp.async.wait_group %0;" ::"n"(DT_STAGE_GROUPS - 3) : "memory");
-                else asm volatile("cp.async.wait_group 0;" ::: "memory");
-                uint4 r[DT_UNROLL];
-#pragma unroll
-                for (int u = 0; u < DT_UNROLL; ++u) {
-                    const int i = g * GROUP + u * DT_ROW_THREADS + tid;
-                    r[u] = i < kept ? stage[i] : make_uint4(none, none, none, none);
-                }
-                o.add<T>(r, c);
-            }
-        }
-    } else if (GRAD || part == 0) {
-        teacher<T>(ent, a, token, z);
+        online_part<T>(o, z, mine, 0, c);
+    } else if (part == 0 && tid < DT_ROW_THREADS + 32) {
+        gather<T>(ent, a, token, z);
+        weigh(ent, a);
     }
     __syncwarp();
     o.join_warps(warp_ms, row_warp, c);
     if (parts > 1) {
         if (tid == 0) part_ms = make_float2(o.m, o.s);
         __syncwarp();
-        lfptx::cluster_sync_all();             // (also: every part has read the logits that the loss needs)
-        const unsigned at = lfptx::smem_u32(&part_ms);
-        o.clear();
-        for (int q = 0; q < parts; ++q) {
-            float2 ms;
-            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ms.x), "=f"(ms.y) : "r"(lfptx::map_to_cta(at, (unsigned)q)) : "memory");
-            o.join(ms.x, ms.y, c);
+        lfptx::cluster_sync_all();
+        o.join_parts(lfptx::smem_u32(&part_ms), parts, c);
+        __syncwarp();
+        lfptx::cluster_sync_all();             // nobody leaves while its sums are being read
+    }
+    if (part == 0 && tid >= DT_ROW_THREADS + 32) loss_of(ent, a, token, o.m, o.s);
+}
+
+// The same and the gradient, with z read once from memory: a part of a row stays in shared memory between the sums and the
+// gradient (`staged` pieces of it; what is more, of rows beyond 8 * 40 KB, is read again).  Blocks are small and many, so that
+// some load while others add or store.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
+// the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
+template <typename T>
+__global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill_args a, int parts, int staged)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    extern __shared__ __align__(16) unsigned char space[];     // staged pieces, entries
+    __shared__ entry_facts facts;
+    __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
+    __shared__ float2 part_ms;
+    const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
+    const bool row_warp = tid < DT_ROW_THREADS, teacher_warp = !row_warp && tid < DT_ROW_THREADS + 32;
+    const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
+    const part_of<T> mine(z, a.vocab, part, parts);
+    const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
+    const int kept = min(staged, mine.pieces);
+    const float c = LOG2E / a.temperature;
+    uint4* own = reinterpret_cast<uint4*>(space);
+    const entries ent(space + (size_t)staged * 16, a.top, &facts);
+    lf_grid_wait();
+    lf_grid_release();
+    online o;
+    o.clear();
+    if (row_warp) {
+        // (a thread reads what it copied itself)
+        for (int i = tid; i < kept; i += DT_ROW_THREADS) cp_async16(lfptx::smem_u32(own + i), from + i);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        online_part<T>(o, z, mine, kept, c);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        const unsigned none = minus_infinity(T());
+        for (int i = tid; i < kept; i += DT_ROW_THREADS * DT_UNROLL) {
+            uint4 r[DT_UNROLL];
+#pragma unroll
+            for (int u = 0; u < DT_UNROLL; ++u) r[u] = i + u * DT_ROW_THREADS < kept ? own[i + u * DT_ROW_THREADS] : make_uint4(none, none, none, none);
+            o.add<T>(r, c);
         }
+    } else if (teacher_warp) {
+        gather<T>(ent, a, token, z);
+    }
+    __syncwarp();
+    o.join_warps(warp_ms, row_warp, c);
+    if (parts > 1) {
+        if (tid == 0) part_ms = make_float2(o.m, o.s);
+        __syncwarp();
+        lfptx::cluster_sync_all();
+        o.join_parts(lfptx::smem_u32(&part_ms), parts, c);
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
-    const float w = a.weight ? a.weight[token] : 1.f;
-    if (part == 0 && !row_warp) {
-        const double tau = (double)a.temperature, kl = divergence(ent, a.top, tau, o.m, o.s);
-        if (tid == DT_ROW_THREADS) {
-            if (a.lse) a.lse[token] = (float)((double)o.m / tau + log((double)o.s));
-            a.loss[token] = w == 0.f || !ent.any ? 0.f : (float)(kl * tau * tau * (double)w);
+    T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
+    const float w = a.weight ? a.weight[token] : 1.f, wt = w * a.temperature, m = o.m;
+    const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !facts.any;
+    if (teacher_warp) {
+        weigh(ent, a);
+    } else if (row_warp && !none) {
+        const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
+#pragma unroll 2
+        for (int i = tid; i < kept; i += DT_ROW_THREADS) gradient_piece<T>(dz + mine.body + (long long)i * N, own[i], m, c, f, aligned);
+#pragma unroll 2
+        for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS)
+            gradient_piece<T>(dz + mine.body + (long long)i * N, ld16(from + i), m, c, f, aligned);
+        if (tid < mine.edge) {
+            const long long at = mine.at_edge(tid);
+            dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
         }
+    } else if (row_warp) {
+        zero_part<T>(dz, mine, aligned);
     }
-    if (GRAD) {
-        T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
-        const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
-        if (w == 0.f || !ent.any) {
-            zero_part<T>(dz, mine, aligned);
-        } else {
-            const float wt = ent.bad ? CUDART_NAN_F : w * a.temperature, f = wt / o.s, m = o.m;
-            if (row_warp) {
-                const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-#pragma unroll 4
-                for (int i = tid; i < kept; i += DT_ROW_THREADS) gradient_piece<T>(dz + mine.body + (long long)i * N, stage[i], m, c, f, aligned);
-#pragma unroll 4
-                for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS)
-                    gradient_piece<T>(dz + mine.body + (long long)i * N, ld16(from + i), m, c, f, aligned);
-                if (tid < mine.edge) {
-                    const long long at = mine.at_edge(tid);
-                    dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
-                }
-            }
-            __syncthreads();
+    __syncthreads();
+    if (row_warp) {
+        if (!none) {
             const float inv_s = 1.0f / o.s;
-            put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
+            put_right<T>(ent, a.top, mine.e0, mine.e1, dz, facts.bad ? CUDART_NAN_F : wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
         }
+    } else if (!teacher_warp && part == 0) {
+        loss_of(ent, a, token, o.m, o.s);
     }
     __syncwarp();
     if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
@@ -415,26 +476,30 @@ template <typename T>
 __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distill_args a, int parts)
 {
     constexpr int N = 16 / (int)sizeof(T);
-    __shared__ entries ent;
+    extern __shared__ __align__(16) unsigned char space[];
+    __shared__ entry_facts facts;
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
     const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
     const bool row_warp = tid < DT_ROW_THREADS;
+    const entries ent(space, a.top, &facts);
     lf_grid_wait();
     lf_grid_release();
-    if (!row_warp) teacher<T>(ent, a, token, z);
+    const bool teacher_warp = tid >= DT_ROW_THREADS && tid < DT_ROW_THREADS + 32;
+    if (teacher_warp) gather<T>(ent, a, token, z);
     __syncthreads();                       // (the entries' logits have been read: dz may be z)
+    if (teacher_warp) weigh(ent, a);
     const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], c = LOG2E / a.temperature;
     const bool large = fabsf(lse) >= DT_LARGE_LSE;
     if (large && part > 0) return;
     const part_of<T> mine(z, a.vocab, part, large ? 1 : parts);
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
-    if (w == 0.f || !ent.any) {
-        zero_part<T>(dz, mine, aligned);
+    if (w == 0.f || !facts.any) {
+        if (row_warp) zero_part<T>(dz, mine, aligned);
         return;
     }
-    const float wt = ent.bad ? CUDART_NAN_F : w * a.temperature;
+    const float wt = facts.bad ? CUDART_NAN_F : w * a.temperature;
     float m = lse * a.temperature, scale = 1.f;        // q = scale e^((z - m) / T)
     if (large) {
         online o;
@@ -464,29 +529,30 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
         }
     }
     __syncthreads();
-    put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
+    if (row_warp) put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
 }
 
-// A part has as much as stays in shared memory, and there are blocks enough to fill the device, up to eight; parts
-// of fewer than 4 KB are not worth a meeting.
-int parts_for(const lf_distill_args& a, int sm_count, bool grad)
+// Blocks enough to fill the device, up to eight to a row; parts of fewer than 4 KB are not worth a meeting.
+int parts_for(const lf_distill_args& a, int sm_count, long long most)
 {
     const long long bytes = (long long)a.vocab * (a.dtype == LF_F32 ? 4 : 2);
     int parts = 1;
-    while (parts < DT_MAX_PARTS && bytes / parts > 4096 &&
-           ((grad && bytes / parts > DT_STAGE_BYTES) || (long long)a.tokens * parts < 2 * sm_count))
-        parts *= 2;
+    while (parts < DT_MAX_PARTS && bytes / parts > 4096 && (bytes / parts > most || (long long)a.tokens * parts < 2 * sm_count)) parts *= 2;
     return parts;
 }
 
 template <typename T>
 cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
 {
-    const int parts = parts_for(a, sm_count, a.dz != nullptr);
-    if (!a.dz) return lf_launch_clusters(k_distill<T, false>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, 0, parts, s, a, parts, 0);
+    if (!a.dz) {
+        const int parts = parts_for(a, sm_count, 1ll << 40);
+        return lf_launch_clusters(k_distill<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, entries::bytes(a.top), parts, s, a, parts);
+    }
+    const int parts = parts_for(a, sm_count, DT_PART_BYTES);
     const long long pieces = (long long)a.vocab * sizeof(T) / 16 / parts + 2;
     const int staged = pieces * 16 < DT_STAGE_BYTES ? (int)pieces : DT_STAGE_BYTES / 16;
-    return lf_launch_clusters(k_distill<T, true>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, (size_t)staged * 16, parts, s, a, parts, staged);
+    const size_t smem = (size_t)staged * 16 + entries::bytes(a.top);
+    return lf_launch_clusters(k_distill_both<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, smem, parts, s, a, parts, staged);
 }
 template <typename T>
 cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
@@ -494,17 +560,19 @@ cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStre
     const long long bytes = (long long)a.vocab * sizeof(T);
     long long parts = (bytes + 65535) / 65536;                    // (16 pieces a thread)
     while ((long long)a.tokens * parts < 2 * sm_count && bytes / parts > 4096) parts *= 2;
-    return lf_launch(k_distill_backward<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, 0, s, a, (int)parts);
+    return lf_launch(k_distill_backward<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, entries::bytes(a.top), s, a, (int)parts);
+}
+template <typename T>
+bool distill_ready()
+{
+    return cudaFuncSetAttribute(k_distill_both<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(DT_STAGE_BYTES + entries::bytes(LF_DISTILL_MAX_TOP))) == cudaSuccess;
 }
 
 }  // namespace
 
-int lf_distill_init(lf_ops*)
+int lf_distill_init()
 {
-    return cudaFuncSetAttribute(k_distill<float, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DT_STAGE_BYTES) == cudaSuccess &&
-                   cudaFuncSetAttribute(k_distill<__nv_bfloat16, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DT_STAGE_BYTES) == cudaSuccess &&
-                   cudaFuncSetAttribute(k_distill<__half, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DT_STAGE_BYTES) == cudaSuccess
-               ? LF_OK : LF_ECUDA;
+    return distill_ready<float>() && distill_ready<__nv_bfloat16>() && distill_ready<__half>() ? LF_OK : LF_ECUDA;
 }
 
 cudaError_t lfk_distill(const lf_distill_args& a, int sm_count, cudaStream_t s)

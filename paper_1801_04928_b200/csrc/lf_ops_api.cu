@@ -121,7 +121,7 @@ int lf_ops_create(lf_ops** out, long long workspace_bytes)
     // (the memsets are only queued, on a stream that the handle's own need not wait for)
     ok = ok && cudaStreamSynchronize(nullptr) == cudaSuccess;
     ok = ok && lf_product_tc_init(o) == LF_OK && lf_linear_stream_init() == LF_OK && lf_rows_init() == LF_OK && lf_layer_norm_init() == LF_OK &&
-         lf_blocks_tc_init(o) == LF_OK && lf_blocks_stream_init() == LF_OK && lf_distill_init(o) == LF_OK;
+         lf_blocks_tc_init(o) == LF_OK && lf_blocks_stream_init() == LF_OK && lf_distill_init() == LF_OK;
     if (!ok) {
         const cudaError_t e = cudaGetLastError();
         lf_ops_destroy(o);

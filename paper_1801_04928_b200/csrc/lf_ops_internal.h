@@ -108,7 +108,7 @@ int lf_layer_norm_init();
 cudaError_t lfk_layer_norm(const lf_layer_norm_args& a, int sm_count, cudaStream_t s);
 cudaError_t lfk_layer_norm_backward(const lf_layer_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* launches);
 cudaError_t lfk_pack_blocks(const lf_pack_blocks_args& a, bool tiles, cudaStream_t s);
-int lf_distill_init(lf_ops* o);
+int lf_distill_init();
 cudaError_t lfk_distill(const lf_distill_args& a, int sm_count, cudaStream_t s);
 cudaError_t lfk_distill_backward(const lf_distill_args& a, int sm_count, cudaStream_t s);
 
