@@ -11,7 +11,7 @@
 // Bound by memory: the loss reads a row once, the gradient reads it and writes one.  A row is cut into parts, a block
 // each, which are a cluster and meet once, over distributed shared memory, with their m and s.  Where the gradient is
 // written too, a part keeps what it has read in shared memory, so that the row is read from memory once.
-// The teacher's entries are one warp's work and the loss another's, beside the others' passes over the row; the dense part of the gradient is
+// The teacher's entries and the loss are one warp's work, beside the others' passes over the row; the dense part of the gradient is
 // written first, then the entries that fall into the part are put right.
 #include <math_constants.h>
 
@@ -23,7 +23,7 @@ namespace {
 
 using namespace lfrow;
 
-constexpr int DT_THREADS = 320;                 // eight warps for the row, one for the teacher's entries, one for the loss
+constexpr int DT_THREADS = 288;                 // eight warps for the row, one for the teacher's entries and the loss
 constexpr int DT_ROW_THREADS = 256;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
@@ -73,10 +73,10 @@ template <typename T>
 struct part_of {
     long long e0, e1, body;
     int pieces, edge;           // edge: elements before and behind
-    __device__ __forceinline__ part_of(const T* row, int vocab, int part, int parts)
+    // per: elements of a part, a multiple of a piece's
+    __device__ __forceinline__ part_of(const T* row, int vocab, int part, long long per)
     {
         constexpr int N = 16 / (int)sizeof(T);
-        const long long per = ((vocab + parts - 1) / parts + N - 1) / N * N;
         e0 = min((long long)vocab, per * part);
         e1 = min((long long)vocab, e0 + per);
         const int off = (int)((reinterpret_cast<uintptr_t>(row + e0) & 15u) / sizeof(T));
@@ -142,45 +142,54 @@ struct online {
         s = sum[0].x + sum[0].y;
         m = now;
     }
-    __device__ __forceinline__ void join(float m2, float s2, float c)
+    __device__ __forceinline__ void add(float v, float c)
     {
-        const float now = fmaxf(m, m2), about = now == -CUDART_INF_F ? 0.f : now;
-        s = s * ex2((m - about) * c) + s2 * ex2((m2 - about) * c);
+        const float now = fmaxf(m, v), about = now == -CUDART_INF_F ? 0.f : now;
+        s = s * ex2((m - about) * c) + ex2((v - about) * c);
         m = now;
     }
-    __device__ __forceinline__ void add(float v, float c) { join(v, 1.f, c); }
-    // over the lanes l ^ 1, ^ 2, ... ^ (LANES / 2), so in a fixed order
-    template <int LANES>
+    // over the lanes of a warp: the maximum first, then the sums of what is left, in a fixed order
     __device__ __forceinline__ void join_lanes(float c)
     {
+        // (floats in the order of signed integers)
+        const int b = __float_as_int(m), k = __reduce_max_sync(0xFFFFFFFFu, b ^ ((b >> 31) & 0x7FFFFFFF));
+        const float now = __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)), about = now == -CUDART_INF_F ? 0.f : now;
+        s *= ex2((m - about) * c);
 #pragma unroll
-        for (int d = LANES / 2; d; d >>= 1) {
-            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, d);
-            join(m2, s2, c);
-        }
+        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+        m = now;
     }
-    // over a block's row warps
-    __device__ __forceinline__ void join_warps(float2* warp_ms, bool mine, float c)
+    // Over the row's warps of all blocks of a cluster: every warp leaves its own, and after one barrier takes all of them, two a lane.
+    // `mine`: this warp has a share of the row.
+    __device__ __forceinline__ void join_row(float2* warp_ms, bool mine, int parts, float c)
     {
-        if (mine) {
-            join_lanes<32>(c);
-            if ((threadIdx.x & 31) == 0) warp_ms[threadIdx.x >> 5] = make_float2(m, s);
-        }
-        __syncthreads();
-        const float2 ms = warp_ms[threadIdx.x & (DT_ROW_THREADS / 32 - 1)];
-        m = ms.x;
-        s = ms.y;
-        join_lanes<DT_ROW_THREADS / 32>(c);
-    }
-    // over the blocks of a cluster, at most eight
-    __device__ __forceinline__ void join_parts(unsigned at, int parts, float c)
-    {
+        constexpr int WARPS = DT_ROW_THREADS / 32;
         const int lane = threadIdx.x & 31;
-        clear();
-        if ((lane & (DT_MAX_PARTS - 1)) < parts)
-            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m), "=f"(s) : "r"(lfptx::map_to_cta(at, (unsigned)(lane & (DT_MAX_PARTS - 1)))) : "memory");
+        static_assert(WARPS * DT_MAX_PARTS == 64, "two a lane");
+        if (mine) {
+            join_lanes(c);
+            if (lane == 0) warp_ms[threadIdx.x >> 5] = make_float2(m, s);
+        }
         __syncwarp();
-        join_lanes<DT_MAX_PARTS>(c);
+        if (parts > 1) lfptx::cluster_sync_all();
+        else __syncthreads();
+        const unsigned at = lfptx::smem_u32(warp_ms + (lane & (WARPS - 1)));
+        float2 v[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int part = lane / WARPS + 4 * i;
+            v[i] = make_float2(-CUDART_INF_F, 0.f);
+            if (parts == 1) {
+                if (part == 0) v[i] = warp_ms[lane];
+            } else if (part < parts) {
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[i].x), "=f"(v[i].y) : "r"(lfptx::map_to_cta(at, (unsigned)part)) : "memory");
+            }
+        }
+        __syncwarp();
+        const float now = fmaxf(v[0].x, v[1].x), about = now == -CUDART_INF_F ? 0.f : now;
+        s = v[0].y * ex2((v[0].x - about) * c) + v[1].y * ex2((v[1].x - about) * c);
+        m = now;
+        join_lanes(c);
     }
 };
 
@@ -257,15 +266,21 @@ __device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a
     // several entries on one element: the first adds them up, in their order
     for (int k = lane; k < a.top; k += 32) {
         const int at = e.at[k];
-        float total = 0.f;
-        bool first = at >= 0;
+        float total = e.p[k];
+        int others = 0;
 #pragma unroll 8
-        for (int j = 0; j < a.top; ++j) {
-            const bool same = e.at[j] == at;
-            if (same) total += e.p[j];
-            first &= !(same && j < k);
+        for (int j = 0; j < a.top; ++j) others += e.at[j] == at;
+        if (others > 1) {
+            bool first = true;
+            total = 0.f;
+            for (int j = 0; j < a.top; ++j)
+                if (e.at[j] == at) {
+                    total += e.p[j];
+                    first &= j >= k;
+                }
+            if (!first) total = -1.f;
         }
-        e.total[k] = first ? total : -1.f;
+        e.total[k] = total;
     }
 }
 // The loss, by one warp.  A weight p that fp32 does not tell from zero has no part in it, whatever logit it falls on.
@@ -308,22 +323,48 @@ __device__ __forceinline__ void store_piece(T* to, const float (&v)[16 / sizeof(
     }
 }
 
-// pieces of dz: f e^((z - m) / T); `none`: zeros, and nothing of z is looked at
+// a piece of dz: f e^((z - m) / T)
 template <typename T>
-__device__ __forceinline__ void gradient_piece(T* to, uint4 u, float m, float c, float f, bool aligned)
+__device__ __forceinline__ void gradient_piece(float (&v)[16 / sizeof(T)], uint4 u, float m, float c, float f)
 {
-    constexpr int N = 16 / (int)sizeof(T);
     piece16<T> p;
-    float v[N];
     p.u = u;
     p.get(v);
 #pragma unroll
-    for (int k = 0; k < N; k += 2) {
+    for (int k = 0; k < 16 / (int)sizeof(T); k += 2) {
         const float2 t = mul2(add2(make_float2(v[k], v[k + 1]), f2(-m)), f2(c));
         const float2 g = mul2(make_float2(ex2(t.x), ex2(t.y)), f2(f));
         v[k] = g.x; v[k + 1] = g.y;
     }
-    store_piece<T>(to, v, aligned);
+}
+// pieces [first, last) of a part's dz, a thread's of them, from pieces that `at` gives
+template <typename T, typename F>
+__device__ __forceinline__ void gradient_pieces(T* to, int first, int last, float m, float c, float f, bool aligned, F at)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    float v[N];
+    if (aligned) {
+#pragma unroll 4
+        for (int i = first + (int)threadIdx.x; i < last; i += DT_ROW_THREADS) {
+            gradient_piece<T>(v, at(i), m, c, f);
+            piece16<T> o;
+            o.set(v);
+            reinterpret_cast<uint4*>(to)[i] = o.u;
+        }
+    } else {
+        for (int i = first + (int)threadIdx.x; i < last; i += DT_ROW_THREADS) {
+            gradient_piece<T>(v, at(i), m, c, f);
+            store_piece<T>(to + (long long)i * N, v, false);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void gradient_edge(T* dz, const T* z, const part_of<T>& mine, float m, float c, float f)
+{
+    if ((int)threadIdx.x < mine.edge) {
+        const long long at = mine.at_edge(threadIdx.x);
+        dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
+    }
 }
 template <typename T>
 __device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool aligned)
@@ -332,35 +373,42 @@ __device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool al
     for (int i = threadIdx.x; i < mine.pieces; i += DT_ROW_THREADS) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
     if ((int)threadIdx.x < mine.edge) dz[mine.at_edge(threadIdx.x)] = (T)0.f;
 }
-// a thread's pieces of a part that are read where they lie: [from, pieces)
-template <typename T>
-__device__ __forceinline__ void online_part(online& o, const T* z, const part_of<T>& mine, int first, float c)
+// pieces [first, last) of a part, a thread's of them, from pieces that `at` gives, DT_UNROLL at a time
+template <typename T, typename F>
+__device__ __forceinline__ void online_pieces(online& o, int first, int last, float c, F at)
 {
-    const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-    const unsigned none = minus_infinity(T());
-    for (int i = first + (int)threadIdx.x; i < mine.pieces; i += DT_ROW_THREADS * DT_UNROLL) {
-        uint4 r[DT_UNROLL];
+    constexpr int STEP = DT_ROW_THREADS * DT_UNROLL;
+    uint4 r[DT_UNROLL];
+    int i = first + (int)threadIdx.x;
+    for (; i + STEP - DT_ROW_THREADS < last; i += STEP) {
 #pragma unroll
-        for (int u = 0; u < DT_UNROLL; ++u) {
-            const int at = i + u * DT_ROW_THREADS;
-            r[u] = at < mine.pieces ? ld16(from + at) : make_uint4(none, none, none, none);
-        }
+        for (int u = 0; u < DT_UNROLL; ++u) r[u] = at(i + u * DT_ROW_THREADS);
         o.add<T>(r, c);
     }
+    if (i < last) {
+        const unsigned none = minus_infinity(T());
+#pragma unroll
+        for (int u = 0; u < DT_UNROLL; ++u) r[u] = i + u * DT_ROW_THREADS < last ? at(i + u * DT_ROW_THREADS) : make_uint4(none, none, none, none);
+        o.add<T>(r, c);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void online_edge(online& o, const T* z, const part_of<T>& mine, float c)
+{
     if ((int)threadIdx.x < mine.edge) o.add((float)z[mine.at_edge(threadIdx.x)], c);
 }
 
-// Loss and lse of a token's row; a cluster of `parts` blocks has a token.
+// Loss and lse of a token's row; a cluster of 2^log2 blocks has a token, each of them `per` elements.
 template <typename T>
-__global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a, int parts)
+__global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a, int log2, long long per)
 {
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
-    __shared__ float2 part_ms;
-    const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
+    const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
-    const part_of<T> mine(z, a.vocab, part, parts);
+    const part_of<T> mine(z, a.vocab, part, per);
+    const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
     const float c = LOG2E / a.temperature;
     const bool row_warp = tid < DT_ROW_THREADS;
     const entries ent(space, a.top, &facts);
@@ -369,22 +417,18 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
     online o;
     o.clear();
     if (row_warp) {
-        online_part<T>(o, z, mine, 0, c);
-    } else if (part == 0 && tid < DT_ROW_THREADS + 32) {
+        online_pieces<T>(o, 0, mine.pieces, c, [&](int i) { return ld16(from + i); });
+        online_edge<T>(o, z, mine, c);
+    } else if (part == 0) {
         gather<T>(ent, a, token, z);
         weigh(ent, a);
     }
     __syncwarp();
-    o.join_warps(warp_ms, row_warp, c);
-    if (parts > 1) {
-        if (tid == 0) part_ms = make_float2(o.m, o.s);
-        __syncwarp();
-        lfptx::cluster_sync_all();
-        o.join_parts(lfptx::smem_u32(&part_ms), parts, c);
-        __syncwarp();
-        lfptx::cluster_sync_all();             // nobody leaves while its sums are being read
-    }
-    if (part == 0 && tid >= DT_ROW_THREADS + 32) loss_of(ent, a, token, o.m, o.s);
+    o.join_row(warp_ms, row_warp, parts, c);
+    if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (part == 0 && !row_warp) loss_of(ent, a, token, o.m, o.s);
+    __syncwarp();
+    if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
 }
 
 // The same and the gradient, with z read once from memory: a part of a row stays in shared memory between the sums and the
@@ -392,17 +436,15 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
 // some load while others add or store.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
 // the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
 template <typename T>
-__global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill_args a, int parts, int staged)
+__global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill_args a, int log2, long long per, int staged)
 {
-    constexpr int N = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char space[];     // staged pieces, entries
     __shared__ entry_facts facts;
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
-    __shared__ float2 part_ms;
-    const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
-    const bool row_warp = tid < DT_ROW_THREADS, teacher_warp = !row_warp && tid < DT_ROW_THREADS + 32;
+    const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
+    const bool row_warp = tid < DT_ROW_THREADS;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
-    const part_of<T> mine(z, a.vocab, part, parts);
+    const part_of<T> mine(z, a.vocab, part, per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
     const int kept = min(staged, mine.pieces);
     const float c = LOG2E / a.temperature;
@@ -416,45 +458,27 @@ __global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill
         // (a thread reads what it copied itself)
         for (int i = tid; i < kept; i += DT_ROW_THREADS) cp_async16(lfptx::smem_u32(own + i), from + i);
         asm volatile("cp.async.commit_group;" ::: "memory");
-        online_part<T>(o, z, mine, kept, c);
+        online_pieces<T>(o, kept, mine.pieces, c, [&](int i) { return ld16(from + i); });
+        online_edge<T>(o, z, mine, c);
         asm volatile("cp.async.wait_all;" ::: "memory");
-        const unsigned none = minus_infinity(T());
-        for (int i = tid; i < kept; i += DT_ROW_THREADS * DT_UNROLL) {
-            uint4 r[DT_UNROLL];
-#pragma unroll
-            for (int u = 0; u < DT_UNROLL; ++u) r[u] = i + u * DT_ROW_THREADS < kept ? own[i + u * DT_ROW_THREADS] : make_uint4(none, none, none, none);
-            o.add<T>(r, c);
-        }
-    } else if (teacher_warp) {
+        online_pieces<T>(o, 0, kept, c, [&](int i) { return own[i]; });
+    } else {
         gather<T>(ent, a, token, z);
     }
     __syncwarp();
-    o.join_warps(warp_ms, row_warp, c);
-    if (parts > 1) {
-        if (tid == 0) part_ms = make_float2(o.m, o.s);
-        __syncwarp();
-        lfptx::cluster_sync_all();
-        o.join_parts(lfptx::smem_u32(&part_ms), parts, c);
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    }
+    o.join_row(warp_ms, row_warp, parts, c);                     // (every part has read the logits that its entries need)
+    if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
     const float w = a.weight ? a.weight[token] : 1.f, wt = w * a.temperature, m = o.m;
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !facts.any;
-    if (teacher_warp) {
+    if (!row_warp) {
         weigh(ent, a);
-    } else if (row_warp && !none) {
+    } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
-#pragma unroll 2
-        for (int i = tid; i < kept; i += DT_ROW_THREADS) gradient_piece<T>(dz + mine.body + (long long)i * N, own[i], m, c, f, aligned);
-#pragma unroll 2
-        for (int i = kept + tid; i < mine.pieces; i += DT_ROW_THREADS)
-            gradient_piece<T>(dz + mine.body + (long long)i * N, ld16(from + i), m, c, f, aligned);
-        if (tid < mine.edge) {
-            const long long at = mine.at_edge(tid);
-            dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
-        }
-    } else if (row_warp) {
+        gradient_pieces<T>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
+        gradient_pieces<T>(dz + mine.body, kept, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
+        gradient_edge<T>(dz, z, mine, m, c, f);
+    } else {
         zero_part<T>(dz, mine, aligned);
     }
     __syncthreads();
@@ -463,7 +487,7 @@ __global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill
             const float inv_s = 1.0f / o.s;
             put_right<T>(ent, a.top, mine.e0, mine.e1, dz, facts.bad ? CUDART_NAN_F : wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
         }
-    } else if (!teacher_warp && part == 0) {
+    } else if (part == 0) {
         loss_of(ent, a, token, o.m, o.s);
     }
     __syncwarp();
@@ -473,9 +497,8 @@ __global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill
 // dz from z and lse: no part of a row needs to know another.  Where lse is so large that fp32 does not hold its fraction
 // (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
 template <typename T>
-__global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distill_args a, int parts)
+__global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distill_args a, int parts, long long per)
 {
-    constexpr int N = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
@@ -486,14 +509,14 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
     const entries ent(space, a.top, &facts);
     lf_grid_wait();
     lf_grid_release();
-    const bool teacher_warp = tid >= DT_ROW_THREADS && tid < DT_ROW_THREADS + 32;
-    if (teacher_warp) gather<T>(ent, a, token, z);
+    if (!row_warp) gather<T>(ent, a, token, z);
     __syncthreads();                       // (the entries' logits have been read: dz may be z)
-    if (teacher_warp) weigh(ent, a);
+    if (!row_warp) weigh(ent, a);
     const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], c = LOG2E / a.temperature;
     const bool large = fabsf(lse) >= DT_LARGE_LSE;
     if (large && part > 0) return;
-    const part_of<T> mine(z, a.vocab, part, large ? 1 : parts);
+    const part_of<T> mine(z, a.vocab, part, large ? (1ll << 40) : per);
+    const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
     if (w == 0.f || !facts.any) {
         if (row_warp) zero_part<T>(dz, mine, aligned);
@@ -504,55 +527,51 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
     if (large) {
         online o;
         o.clear();
-        if (row_warp) online_part<T>(o, z, mine, 0, c);
-        o.join_warps(warp_ms, row_warp, c);
+        if (row_warp) {
+            online_pieces<T>(o, 0, mine.pieces, c, [&](int i) { return ld16(from + i); });
+            online_edge<T>(o, z, mine, c);
+        }
+        __syncwarp();
+        o.join_row(warp_ms, row_warp, 1, c);
         m = o.m;
         scale = 1.0f / o.s;
     }
     const float f = wt * scale;
     if (row_warp) {
-        const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-        for (int i = tid; i < mine.pieces; i += DT_ROW_THREADS * DT_UNROLL) {
-            uint4 r[DT_UNROLL];
-#pragma unroll
-            for (int u = 0; u < DT_UNROLL; ++u)
-                if (i + u * DT_ROW_THREADS < mine.pieces) r[u] = ld16(from + i + u * DT_ROW_THREADS);
-#pragma unroll
-            for (int u = 0; u < DT_UNROLL; ++u) {
-                const int at = i + u * DT_ROW_THREADS;
-                if (at < mine.pieces) gradient_piece<T>(dz + mine.body + (long long)at * N, r[u], m, c, f, aligned);
-            }
-        }
-        if (tid < mine.edge) {
-            const long long at = mine.at_edge(tid);
-            dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
-        }
+        gradient_pieces<T>(dz + mine.body, 0, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
+        gradient_edge<T>(dz, z, mine, m, c, f);
     }
     __syncthreads();
     if (row_warp) put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
 }
 
-// Blocks enough to fill the device, up to eight to a row; parts of fewer than 4 KB are not worth a meeting.
-int parts_for(const lf_distill_args& a, int sm_count, long long most)
+// elements of a part, whole pieces
+template <typename T>
+long long per_part(const lf_distill_args& a, long long parts)
+{
+    constexpr long long N = 16 / (long long)sizeof(T);
+    return ((a.vocab + parts - 1) / parts + N - 1) / N * N;
+}
+// Blocks of a cluster, as a power of two: enough to fill the device and to have `most` bytes at most, up to eight; parts of fewer than 4 KB
+// are not worth a meeting.
+int parts_log2(const lf_distill_args& a, int sm_count, long long most)
 {
     const long long bytes = (long long)a.vocab * (a.dtype == LF_F32 ? 4 : 2);
-    int parts = 1;
-    while (parts < DT_MAX_PARTS && bytes / parts > 4096 && (bytes / parts > most || (long long)a.tokens * parts < 2 * sm_count)) parts *= 2;
-    return parts;
+    int n = 0;
+    while ((1 << n) < DT_MAX_PARTS && (bytes >> n) > 4096 && ((bytes >> n) > most || ((long long)a.tokens << n) < 2 * sm_count)) ++n;
+    return n;
 }
 
 template <typename T>
 cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
 {
-    if (!a.dz) {
-        const int parts = parts_for(a, sm_count, 1ll << 40);
-        return lf_launch_clusters(k_distill<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, entries::bytes(a.top), parts, s, a, parts);
-    }
-    const int parts = parts_for(a, sm_count, DT_PART_BYTES);
-    const long long pieces = (long long)a.vocab * sizeof(T) / 16 / parts + 2;
-    const int staged = pieces * 16 < DT_STAGE_BYTES ? (int)pieces : DT_STAGE_BYTES / 16;
-    const size_t smem = (size_t)staged * 16 + entries::bytes(a.top);
-    return lf_launch_clusters(k_distill_both<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, smem, parts, s, a, parts, staged);
+    const int log2 = parts_log2(a, sm_count, a.dz ? DT_PART_BYTES : 1ll << 40), parts = 1 << log2;
+    const dim3 grid((unsigned)((long long)a.tokens << log2));
+    const long long per = per_part<T>(a, parts);
+    if (!a.dz) return lf_launch_clusters(k_distill<T>, grid, DT_THREADS, entries::bytes(a.top), parts, s, a, log2, per);
+    const long long bytes = per * (long long)sizeof(T);
+    const int staged = (int)((bytes < DT_STAGE_BYTES ? bytes : DT_STAGE_BYTES) / 16);
+    return lf_launch_clusters(k_distill_both<T>, grid, DT_THREADS, (size_t)staged * 16 + entries::bytes(a.top), parts, s, a, log2, per, staged);
 }
 template <typename T>
 cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
@@ -560,7 +579,7 @@ cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStre
     const long long bytes = (long long)a.vocab * sizeof(T);
     long long parts = (bytes + 65535) / 65536;                    // (16 pieces a thread)
     while ((long long)a.tokens * parts < 2 * sm_count && bytes / parts > 4096) parts *= 2;
-    return lf_launch(k_distill_backward<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, entries::bytes(a.top), s, a, (int)parts);
+    return lf_launch(k_distill_backward<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, entries::bytes(a.top), s, a, (int)parts, per_part<T>(a, parts));
 }
 template <typename T>
 bool distill_ready()
