@@ -23,13 +23,14 @@ namespace {
 
 using namespace lfrow;
 
-constexpr int DT_THREADS = 288;                 // eight warps for the row, one for the teacher's entries and the loss
-constexpr int DT_ROW_THREADS = 256;
+constexpr int DT_ROW_THREADS = 256;             // for the row; beside them a warp for the teacher's entries and the loss
+constexpr int DT_THREADS = DT_ROW_THREADS + 32;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
 constexpr float DT_LARGE_LSE = 65536.f;         // (an eighth of a per cent of the gradient)
+constexpr int DT_BLOCKS = 6;                    // of the joint kernel per multiprocessor
 constexpr int DT_PART_BYTES = 32 * 1024;        // of a row that a block of the joint kernel has, where eight parts are enough
-constexpr int DT_STAGE_BYTES = 40 * 1024;       // at most of a part that stays in shared memory
+constexpr int DT_STAGE_BYTES = DT_PART_BYTES;   // at most of a part that stays in shared memory
 
 // ---- 16 bytes of a row -------------------------------------------------------------------------------
 template <typename T>
@@ -159,13 +160,12 @@ struct online {
         for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
         m = now;
     }
-    // Over the row's warps of all blocks of a cluster: every warp leaves its own, and after one barrier takes all of them, two a lane.
+    // Over the row's warps of all blocks of a cluster: every warp leaves its own, and after one barrier takes all of them, the same ones on a lane.
     // `mine`: this warp has a share of the row.
     __device__ __forceinline__ void join_row(float2* warp_ms, bool mine, int parts, float c)
     {
-        constexpr int WARPS = DT_ROW_THREADS / 32;
+        constexpr int WARPS = DT_ROW_THREADS / 32, EACH = WARPS * DT_MAX_PARTS / 32;
         const int lane = threadIdx.x & 31;
-        static_assert(WARPS * DT_MAX_PARTS == 64, "two a lane");
         if (mine) {
             join_lanes(c);
             if (lane == 0) warp_ms[threadIdx.x >> 5] = make_float2(m, s);
@@ -174,21 +174,25 @@ struct online {
         if (parts > 1) lfptx::cluster_sync_all();
         else __syncthreads();
         const unsigned at = lfptx::smem_u32(warp_ms + (lane & (WARPS - 1)));
-        float2 v[2];
+        float2 v[EACH];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int part = lane / WARPS + 4 * i;
+        for (int i = 0; i < EACH; ++i) {
+            const int part = lane / WARPS + 32 / WARPS * i;
             v[i] = make_float2(-CUDART_INF_F, 0.f);
             if (parts == 1) {
-                if (part == 0) v[i] = warp_ms[lane];
+                if (part == 0) v[i] = warp_ms[lane & (WARPS - 1)];
             } else if (part < parts) {
                 asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[i].x), "=f"(v[i].y) : "r"(lfptx::map_to_cta(at, (unsigned)part)) : "memory");
             }
         }
         __syncwarp();
-        const float now = fmaxf(v[0].x, v[1].x), about = now == -CUDART_INF_F ? 0.f : now;
-        s = v[0].y * ex2((v[0].x - about) * c) + v[1].y * ex2((v[1].x - about) * c);
-        m = now;
+        m = v[0].x;
+#pragma unroll
+        for (int i = 1; i < EACH; ++i) m = fmaxf(m, v[i].x);
+        const float about = m == -CUDART_INF_F ? 0.f : m;
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) s += v[i].y * ex2((v[i].x - about) * c);
         join_lanes(c);
     }
 };
@@ -337,25 +341,30 @@ __device__ __forceinline__ void gradient_piece(float (&v)[16 / sizeof(T)], uint4
         v[k] = g.x; v[k + 1] = g.y;
     }
 }
-// pieces [first, last) of a part's dz, a thread's of them, from pieces that `at` gives
-template <typename T, typename F>
+// pieces [first, last) of a part's dz, a thread's of them, from pieces that `at` gives, BATCH of them before the first is used
+template <typename T, int BATCH, typename F>
 __device__ __forceinline__ void gradient_pieces(T* to, int first, int last, float m, float c, float f, bool aligned, F at)
 {
-    constexpr int N = 16 / (int)sizeof(T);
+    constexpr int N = 16 / (int)sizeof(T), STEP = DT_ROW_THREADS * BATCH;
     float v[N];
+    int i = first + (int)threadIdx.x;
     if (aligned) {
-#pragma unroll 4
-        for (int i = first + (int)threadIdx.x; i < last; i += DT_ROW_THREADS) {
-            gradient_piece<T>(v, at(i), m, c, f);
-            piece16<T> o;
-            o.set(v);
-            reinterpret_cast<uint4*>(to)[i] = o.u;
+        for (; i + STEP - DT_ROW_THREADS < last; i += STEP) {
+            uint4 r[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) r[u] = at(i + u * DT_ROW_THREADS);
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                gradient_piece<T>(v, r[u], m, c, f);
+                piece16<T> o;
+                o.set(v);
+                reinterpret_cast<uint4*>(to)[i + u * DT_ROW_THREADS] = o.u;
+            }
         }
-    } else {
-        for (int i = first + (int)threadIdx.x; i < last; i += DT_ROW_THREADS) {
-            gradient_piece<T>(v, at(i), m, c, f);
-            store_piece<T>(to + (long long)i * N, v, false);
-        }
+    }
+    for (; i < last; i += DT_ROW_THREADS) {
+        gradient_piece<T>(v, at(i), m, c, f);
+        store_piece<T>(to + (long long)i * N, v, aligned);
     }
 }
 template <typename T>
@@ -367,12 +376,17 @@ __device__ __forceinline__ void gradient_edge(T* dz, const T* z, const part_of<T
     }
 }
 template <typename T>
-__device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool aligned)
+__device__ __forceinline__ void fill_part(T* dz, const part_of<T>& mine, float with, bool aligned)
 {
-    const float v[16 / sizeof(T)] = {};
+    float v[16 / sizeof(T)];
+#pragma unroll
+    for (int k = 0; k < 16 / (int)sizeof(T); ++k) v[k] = with;
     for (int i = threadIdx.x; i < mine.pieces; i += DT_ROW_THREADS) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
-    if ((int)threadIdx.x < mine.edge) dz[mine.at_edge(threadIdx.x)] = (T)0.f;
+    if ((int)threadIdx.x < mine.edge) dz[mine.at_edge(threadIdx.x)] = (T)with;
 }
+template <typename T>
+__device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool aligned) { fill_part<T>(dz, mine, 0.f, aligned); }
+
 // pieces [first, last) of a part, a thread's of them, from pieces that `at` gives, DT_UNROLL at a time
 template <typename T, typename F>
 __device__ __forceinline__ void online_pieces(online& o, int first, int last, float c, F at)
@@ -421,22 +435,25 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
         online_edge<T>(o, z, mine, c);
     } else if (part == 0) {
         gather<T>(ent, a, token, z);
-        weigh(ent, a);
     }
     __syncwarp();
     o.join_row(warp_ms, row_warp, parts, c);
     if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    if (part == 0 && !row_warp) loss_of(ent, a, token, o.m, o.s);
+    if (part == 0 && !row_warp) {
+        weigh(ent, a);
+        loss_of(ent, a, token, o.m, o.s);
+    }
     __syncwarp();
     if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
 }
 
 // The same and the gradient, with z read once from memory: a part of a row stays in shared memory between the sums and the
-// gradient (`staged` pieces of it; what is more, of rows beyond 8 * 40 KB, is read again).  Blocks are small and many, so that
-// some load while others add or store.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
+// gradient (`staged` pieces of it; what is more, of rows beyond 8 * 32 KB, is read again).  Blocks are small and many, so that
+// some load while others add or store: 8192 x 131072 bf16 849 us, 5.06 TB/s, with six blocks to a multiprocessor (five: 938, four: 1072); persistent
+// ones with the next part on its way 1345, a row to a block that reads it again from L2 1154.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
 // the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
 template <typename T>
-__global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill_args a, int log2, long long per, int staged)
+__global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf_distill_args a, int log2, long long per, int staged)
 {
     extern __shared__ __align__(16) unsigned char space[];     // staged pieces, entries
     __shared__ entry_facts facts;
@@ -475,8 +492,8 @@ __global__ void __launch_bounds__(DT_THREADS, 5) k_distill_both(const lf_distill
         weigh(ent, a);
     } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
-        gradient_pieces<T>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
-        gradient_pieces<T>(dz + mine.body, kept, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
+        gradient_pieces<T, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
+        gradient_pieces<T, 1>(dz + mine.body, kept, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
         gradient_edge<T>(dz, z, mine, m, c, f);
     } else {
         zero_part<T>(dz, mine, aligned);
@@ -510,7 +527,7 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
     lf_grid_wait();
     lf_grid_release();
     if (!row_warp) gather<T>(ent, a, token, z);
-    __syncthreads();                       // (the entries' logits have been read: dz may be z)
+    if (a.dz == a.z) __syncthreads();      // the entries' logits have been read
     if (!row_warp) weigh(ent, a);
     const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], c = LOG2E / a.temperature;
     const bool large = fabsf(lse) >= DT_LARGE_LSE;
@@ -518,11 +535,11 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
     const part_of<T> mine(z, a.vocab, part, large ? (1ll << 40) : per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
-    if (w == 0.f || !facts.any) {
+    if (w == 0.f) {
         if (row_warp) zero_part<T>(dz, mine, aligned);
         return;
     }
-    const float wt = facts.bad ? CUDART_NAN_F : w * a.temperature;
+    const float wt = w * a.temperature;
     float m = lse * a.temperature, scale = 1.f;        // q = scale e^((z - m) / T)
     if (large) {
         online o;
@@ -538,11 +555,14 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
     }
     const float f = wt * scale;
     if (row_warp) {
-        gradient_pieces<T>(dz + mine.body, 0, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
+        gradient_pieces<T, DT_UNROLL>(dz + mine.body, 0, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
         gradient_edge<T>(dz, z, mine, m, c, f);
     }
     __syncthreads();
-    if (row_warp) put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
+    if (!row_warp) return;
+    if (!facts.any) zero_part<T>(dz, mine, aligned);               // (rare: what was written is written again)
+    else if (facts.bad) fill_part<T>(dz, mine, CUDART_NAN_F, aligned);
+    else put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
 }
 
 // elements of a part, whole pieces

@@ -320,14 +320,65 @@ struct norm_backward_ready {
 
 // ---- blocks of 128 -----------------------------------------------------------------------------------
 // A block of 256 threads takes a tile of 128 x 128 values: a thread has 8 columns of 8 consecutive rows in registers, so
-// that the largest magnitudes of rows, columns or the tile are taken, and both forms written, from one read.  The transposed form
-// is turned in shared memory, in pieces of 8 rows of a column whose place is turned by the column, so that neither side meets
-// a bank twice; it is written a piece of 16 bytes at a time, the last one of a row byte by byte where it is not full.
-template <typename T, bool TILES>
-__global__ void __launch_bounds__(256) k_pack_blocks(const lf_pack_blocks_args a)
+// that the largest magnitudes of rows, columns or the tile are taken, and both forms written, from one read.  Magnitudes are compared as
+// integers, 16-bit ones two at a time.  The transposed form is turned in shared memory, in pieces of 8 rows of a column whose
+// place is turned by the column, so that neither side meets a bank twice; it is written a piece of 16 bytes at a time, the last one of a row byte
+// by byte where it is not full.  Bound by memory.
+template <typename T>
+struct magnitudes {                         // of eight columns
+    static constexpr int N = sizeof(T) == 2 ? 4 : 8;
+    unsigned w[N];
+    static __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return sizeof(T) == 2 ? __vmaxu2(a, b) : max(a, b); }
+    __device__ __forceinline__ void of(const vec8<T>& v)
+    {
+        if constexpr (sizeof(T) == 2) {
+            w[0] = v.u.x & 0x7FFF7FFFu; w[1] = v.u.y & 0x7FFF7FFFu; w[2] = v.u.z & 0x7FFF7FFFu; w[3] = v.u.w & 0x7FFF7FFFu;
+        } else {
+            w[0] = abs_bits(v.a.x); w[1] = abs_bits(v.a.y); w[2] = abs_bits(v.a.z); w[3] = abs_bits(v.a.w);
+            w[4] = abs_bits(v.b.x); w[5] = abs_bits(v.b.y); w[6] = abs_bits(v.b.z); w[7] = abs_bits(v.b.w);
+        }
+    }
+    __device__ __forceinline__ void join(const magnitudes& o)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = larger(w[i], o.w[i]);
+    }
+    __device__ __forceinline__ unsigned largest() const       // still in pairs where they are
+    {
+        unsigned m = w[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = larger(m, w[i]);
+        return m;
+    }
+    // fp32 bits of a magnitude, of the larger one of a pair
+    static __device__ __forceinline__ unsigned bits(unsigned m)
+    {
+        if constexpr (sizeof(T) == 2) {
+            const float2 f = unpack2(max(m & 0xFFFFu, m >> 16), T());
+            return __float_as_uint(f.x);
+        } else {
+            return m;
+        }
+    }
+};
+// column 2 i and 2 i + 1 of eight
+template <typename T>
+__device__ __forceinline__ float2 columns_of(const vec8<T>& v, int i)
 {
-    __shared__ unsigned col_max[8][128];
-    __shared__ __align__(16) unsigned char turned[128 * 128];
+    if constexpr (sizeof(T) == 2) {
+        return unpack2(i == 0 ? v.u.x : i == 1 ? v.u.y : i == 2 ? v.u.z : v.u.w, T());
+    } else {
+        return i == 0 ? make_float2(v.a.x, v.a.y) : i == 1 ? make_float2(v.a.z, v.a.w) : i == 2 ? make_float2(v.b.x, v.b.y) : make_float2(v.b.z, v.b.w);
+    }
+}
+
+// TILES: a scale for the tile; TURN: the transposed form is wanted
+template <typename T, bool TILES, bool TURN>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_pack_blocks(const lf_pack_blocks_args a)
+{
+    typedef magnitudes<T> mags;
+    __shared__ unsigned col_max[TURN || TILES ? 8 : 1][TURN || TILES ? 16 * mags::N : 1];
+    __shared__ __align__(16) unsigned char turned[TURN ? 128 * 128 : 16];
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, warp = threadIdx.x >> 5;
     const unsigned nbx = ((unsigned)a.n + 127) / 128, nby = ((unsigned)a.tokens + 127) / 128;
     const unsigned by = blockIdx.x / nbx, bx = blockIdx.x - by * nbx;
@@ -341,47 +392,36 @@ __global__ void __launch_bounds__(256) k_pack_blocks(const lf_pack_blocks_args a
         v[p].zero();
         if (in && row0 + p < a.tokens) v[p].load(static_cast<const T*>(a.x) + (size_t)(row0 + p) * a.ld_x + col);
     }
-    unsigned rm[8], cm[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) cm[j] = 0;
-#pragma unroll
-    for (int p = 0; p < 8; ++p) {
-        float f[8];
-        v[p].get(f);
-        rm[p] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            rm[p] = max(rm[p], abs_bits(f[j]));
-            cm[j] = max(cm[j], abs_bits(f[j]));
-        }
-    }
     unsigned tile = 0;
     if (TILES) {
-        unsigned m = 0;
+        mags m, o;
+        m.of(v[0]);
 #pragma unroll
-        for (int p = 0; p < 8; ++p) m = max(m, rm[p]);
-        m = __reduce_max_sync(0xFFFFFFFFu, m);
-        if ((threadIdx.x & 31) == 0) col_max[0][warp] = m;
+        for (int p = 1; p < 8; ++p) { o.of(v[p]); m.join(o); }
+        const unsigned w = __reduce_max_sync(0xFFFFFFFFu, mags::bits(m.largest()));
+        if ((threadIdx.x & 31) == 0) col_max[0][warp] = w;
         __syncthreads();
-        m = 0;
+        unsigned t = 0;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) m = max(m, col_max[0][w]);
-        tile = block_byte(m);
+        for (int i = 0; i < 8; ++i) t = max(t, col_max[0][i]);
+        tile = block_byte(t);
         if (threadIdx.x == 0) {
             if (a.s) a.s[(size_t)by * nbx + bx] = scale(tile);
             if (a.st) a.st[(size_t)bx * nby + by] = scale(tile);
         }
     }
-    if (a.q) {
+    if (!TURN || a.q) {
 #pragma unroll
         for (int p = 0; p < 8; ++p) {
             const int row = row0 + p;
             unsigned b = tile;
             if (!TILES) {
-                unsigned m = rm[p];
+                mags m;
+                m.of(v[p]);
+                unsigned w = m.largest();
 #pragma unroll
-                for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                b = block_byte(m);
+                for (int o = 1; o < 16; o <<= 1) w = mags::larger(w, __shfl_xor_sync(0xFFFFFFFFu, w, o));
+                b = block_byte(mags::bits(w));
             }
             if (in && row < a.tokens) {
                 float f[8];
@@ -391,65 +431,82 @@ __global__ void __launch_bounds__(256) k_pack_blocks(const lf_pack_blocks_args a
             }
         }
     }
-    if (a.qt) {
-        unsigned cb[8];
-        if (TILES) {
+    if (!TURN) return;
+    unsigned cb[8];                          // scale bytes of the eight columns
+    if (TILES) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) cb[j] = tile;
-        } else {
+        for (int j = 0; j < 8; ++j) cb[j] = tile;
+    } else {
+        mags m, o;
+        m.of(v[0]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) cm[j] = max(cm[j], __shfl_xor_sync(0xFFFFFFFFu, cm[j], 16));
-            if ((threadIdx.x & 16) == 0) {
-                *reinterpret_cast<uint4*>(&col_max[warp][tx * 8]) = make_uint4(cm[0], cm[1], cm[2], cm[3]);
-                *reinterpret_cast<uint4*>(&col_max[warp][tx * 8 + 4]) = make_uint4(cm[4], cm[5], cm[6], cm[7]);
-            }
-            __syncthreads();
+        for (int p = 1; p < 8; ++p) { o.of(v[p]); m.join(o); }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                unsigned m = 0;
+        for (int i = 0; i < mags::N; ++i) m.w[i] = mags::larger(m.w[i], __shfl_xor_sync(0xFFFFFFFFu, m.w[i], 16));
+        if ((threadIdx.x & 16) == 0) {
 #pragma unroll
-                for (int w = 0; w < 8; ++w) m = max(m, col_max[w][tx * 8 + j]);
-                cb[j] = block_byte(m);
-            }
-            if (ty == 0 && in) {
-                float sc[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sc[j] = scale(cb[j]);
-                vec8<float> o;
-                o.set(sc);
-                o.store(a.st + (size_t)by * a.n + col);
-            }
-        }
-        // a thread's 8 x 8 values, column by column: rows 0 .. 3 and 4 .. 7 of a column are a word each
-        float f[8][8];
-#pragma unroll
-        for (int p = 0; p < 8; ++p) v[p].get(f[p]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float r = inv_scale(cb[j]);
-            const uint2 w = make_uint2(to_e4m3x4(f[0][j] * r, f[1][j] * r, f[2][j] * r, f[3][j] * r),
-                                       to_e4m3x4(f[4][j] * r, f[5][j] * r, f[6][j] * r, f[7][j] * r));
-            *reinterpret_cast<uint2*>(turned + (tx * 8 + j) * 128 + ((ty ^ tx) << 3)) = w;
+            for (int i = 0; i < mags::N; i += 4)
+                *reinterpret_cast<uint4*>(&col_max[warp][tx * mags::N + i]) = make_uint4(m.w[i], m.w[i + 1], m.w[i + 2], m.w[i + 3]);
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int c = k * 32 + (threadIdx.x >> 3), u = threadIdx.x & 7, turn = c >> 3;
-            uint4 w = *reinterpret_cast<const uint4*>(turned + c * 128 + ((u ^ (turn >> 1)) << 4));
-            if (turn & 1) w = make_uint4(w.z, w.w, w.x, w.y);
-            const int to_row = bx * 128 + c, at = by * 128 + u * 16;
-            if (to_row >= a.n || at >= a.tokens) continue;
-            unsigned char* to = a.qt + (size_t)to_row * a.ld_qt + at;
-            if (at + 16 <= a.tokens) {
-                *reinterpret_cast<uint4*>(to) = w;
-            } else {
-                const unsigned b[4] = {w.x, w.y, w.z, w.w};
+        for (int i = 0; i < mags::N; ++i) {
+            unsigned w = 0;
 #pragma unroll
-                for (int i = 0; i < 15; ++i)
-                    if (at + i < a.tokens) to[i] = (unsigned char)(b[i >> 2] >> (8 * (i & 3)));
+            for (int k = 0; k < 8; ++k) w = mags::larger(w, col_max[k][tx * mags::N + i]);
+            if (sizeof(T) == 2) {
+                cb[2 * i & 7] = block_byte(mags::bits(w & 0xFFFFu));
+                cb[(2 * i + 1) & 7] = block_byte(mags::bits(w >> 16));
+            } else {
+                cb[i] = block_byte(w);
             }
         }
+        if (ty == 0 && in) {
+            float sc[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sc[j] = scale(cb[j]);
+            vec8<float> to;
+            to.set(sc);
+            to.store(a.st + (size_t)by * a.n + col);
+        }
     }
+    // a thread's 8 x 8 values, two columns at a time: rows 0 .. 3 and 4 .. 7 of a column are a word each
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 r = make_float2(inv_scale(cb[2 * i]), inv_scale(cb[2 * i + 1]));
+        float2 f[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) f[p] = mul2(columns_of(v[p], i), r);
+        unsigned char* to = turned + (tx * 8 + 2 * i) * 128 + ((ty ^ tx) << 3);
+        *reinterpret_cast<uint2*>(to) = make_uint2(to_e4m3x4(f[0].x, f[1].x, f[2].x, f[3].x), to_e4m3x4(f[4].x, f[5].x, f[6].x, f[7].x));
+        *reinterpret_cast<uint2*>(to + 128) = make_uint2(to_e4m3x4(f[0].y, f[1].y, f[2].y, f[3].y), to_e4m3x4(f[4].y, f[5].y, f[6].y, f[7].y));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int c = k * 32 + (threadIdx.x >> 3), u = threadIdx.x & 7, turn = c >> 3;
+        uint4 w = *reinterpret_cast<const uint4*>(turned + c * 128 + ((u ^ (turn >> 1)) << 4));
+        if (turn & 1) w = make_uint4(w.z, w.w, w.x, w.y);
+        const int to_row = bx * 128 + c, at = by * 128 + u * 16;
+        if (to_row >= a.n || at >= a.tokens) continue;
+        unsigned char* to = a.qt + (size_t)to_row * a.ld_qt + at;
+        if (at + 16 <= a.tokens) {
+            *reinterpret_cast<uint4*>(to) = w;
+        } else {
+            const unsigned b[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 15; ++i)
+                if (at + i < a.tokens) to[i] = (unsigned char)(b[i >> 2] >> (8 * (i & 3)));
+        }
+    }
+}
+
+template <typename T>
+cudaError_t pack_of(const lf_pack_blocks_args& a, bool tiles, cudaStream_t s)
+{
+    const dim3 grid((unsigned)ceil_div(a.n, 128) * (unsigned)ceil_div(a.tokens, 128));       // (2^31 tiles would be 35 TB)
+    if (tiles) return lf_launch(a.qt ? k_pack_blocks<T, true, true> : k_pack_blocks<T, true, false>, grid, 256, 0, s, a);
+    return lf_launch(a.qt ? k_pack_blocks<T, false, true> : k_pack_blocks<T, false, false>, grid, 256, 0, s, a);
 }
 
 }  // namespace
@@ -491,10 +548,7 @@ cudaError_t lfk_layer_norm_backward(const lf_layer_norm_backward_args& a, float*
 
 cudaError_t lfk_pack_blocks(const lf_pack_blocks_args& a, bool tiles, cudaStream_t s)
 {
-    const dim3 grid((unsigned)ceil_div(a.n, 128) * (unsigned)ceil_div(a.tokens, 128));       // (2^31 tiles would be 35 TB)
-    cudaError_t e;
-    if (a.dtype == LF_F32) e = lf_launch(tiles ? k_pack_blocks<float, true> : k_pack_blocks<float, false>, grid, 256, 0, s, a);
-    else if (a.dtype == LF_BF16) e = lf_launch(tiles ? k_pack_blocks<__nv_bfloat16, true> : k_pack_blocks<__nv_bfloat16, false>, grid, 256, 0, s, a);
-    else e = lf_launch(tiles ? k_pack_blocks<__half, true> : k_pack_blocks<__half, false>, grid, 256, 0, s, a);
-    return e;
+    if (a.dtype == LF_F32) return pack_of<float>(a, tiles, s);
+    if (a.dtype == LF_BF16) return pack_of<__nv_bfloat16>(a, tiles, s);
+    return pack_of<__half>(a, tiles, s);
 }
