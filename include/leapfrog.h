@@ -533,7 +533,7 @@ int lf_act_backward(lf_ops* ops, int dtype, int act, int tokens, int n, const vo
 /* ================================================================================================
  * Layer norm, products in 8 bits with a scale for each block of 128, and the loss against a teacher's
  * top logits: the output layer of a network that learns from a larger one.  Same handle, same rules as above
- * (rows, strides, alignment, tokens = 0, order of additions) but where said otherwise.
+ * (rows, strides, alignment, also of scales, tokens = 0, order of additions) but where said otherwise.
  *
  * Blocks of 128.  An operand of such a product is a matrix of e4m3 bytes, rows along the contraction, row stride ld a
  * multiple of 16 bytes (0 stands for the width rounded up to one; what lies behind a row's end is neither read nor
@@ -557,7 +557,7 @@ typedef struct lf_layer_norm_args {  /* h = x + residual, m = mean h, r = 1 / sq
     unsigned char* q; long long ld_q;   /* q and s both or neither: y in blocks of 128 along its rows, */
     float* s;                        /*   from the unrounded y                                  */
     float *mean, *rstd;              /* [tokens], m and r; both or neither                     */
-} lf_layer_norm_args;                /* h or y may be x or residual                            */
+} lf_layer_norm_args;                /* h or y may be x or residual.  Squares are taken in fp32: |h - m| up to 1e17 */
 
 typedef struct lf_layer_norm_backward_args {
     /* with c = (h - m) r, u = gain (.) dy:
@@ -585,8 +585,9 @@ typedef struct lf_pack_blocks_args {
 
 typedef struct lf_product_blocks_args {
     /* d[i][j] = sum over blocks c of sa[c][i] sb[c][j] sum over k of block c of a[i][k] b[j][k], + bias[j] + add[i][j].
-     * The product of two scales is formed first, in fp32; a block's 128 terms are added by the tensor cores, the blocks in
-     * fp32 with round-to-nearest, in their order. */
+     * The product of two scales is formed first, in fp32 (so one that is out of its range makes infinities or NaN); a
+     * block's 128 terms are added by the tensor cores, the blocks in fp32 with round-to-nearest, in a fixed order.  n_in = 0 is
+     * legal: d = bias + add. */
     int out_dtype;                   /* of d and add: any (add: not LF_F32)                    */
     int tokens, n_in, n_out;         /* rows of a and d; contraction (any length); columns of d: a multiple of 8 */
     const unsigned char* a; long long ld_a; const float* sa;   /* [tokens][n_in], scales of rows */
@@ -606,15 +607,15 @@ typedef struct lf_distill_args {
      * weight 0 has loss and dz 0 whatever its logits hold. */
     int dtype;                       /* of z, dz: any                                          */
     int tokens, vocab, top;          /* vocab: any number from 1, top: 1 .. LF_DISTILL_MAX_TOP */
-    float temperature;               /* T, > 0, finite                                         */
+    float temperature;               /* T, 1e-6 .. 1e6                                         */
     const void* z; long long ld_z;   /* [tokens][vocab]; rows may begin at any element, ld any number >= vocab (0: vocab) */
     const int* index;                /* [tokens][top]                                          */
     const float* value;              /* [tokens][top], the teacher's logits                    */
     const float* weight;             /* [tokens] or NULL (1): the token's weight; lf_distill_backward: times the gradient of its loss */
     float* loss;                     /* [tokens]; not used by lf_distill_backward              */
     float* lse;                      /* [tokens]; lf_distill: written, or NULL; lf_distill_backward: read */
-    void* dz; long long ld_dz;       /* [tokens][vocab], as z; lf_distill: or NULL (gradient of the sum of the losses).  May be z itself */
-} lf_distill_args;
+    void* dz; long long ld_dz;       /* [tokens][vocab], as z; lf_distill: or NULL (gradient of the sum of the losses).  May be z itself, same stride */
+} lf_distill_args;                   /* index, value, weight, loss, lse: at the boundary of an element */
 
 #define LF_DISTILL_MAX_TOP 512
 

@@ -27,7 +27,7 @@ constexpr int DT_ROW_THREADS = 256;             // for the row; beside them a wa
 constexpr int DT_THREADS = DT_ROW_THREADS + 32;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
-constexpr float DT_LARGE_LSE = 65536.f;         // (an eighth of a per cent of the gradient)
+constexpr float DT_LARGE_LSE = 1024.f;          // from here on lse in fp32 is off by 3e-5, so much of the gradient
 constexpr int DT_BLOCKS = 6;                    // of the joint kernel per multiprocessor
 constexpr int DT_PART_BYTES = 32 * 1024;        // of a row that a block of the joint kernel has, where eight parts are enough
 constexpr int DT_STAGE_BYTES = DT_PART_BYTES;   // at most of a part that stays in shared memory
@@ -511,8 +511,8 @@ __global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf
     if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
 }
 
-// dz from z and lse: no part of a row needs to know another.  Where lse is so large that fp32 does not hold its fraction
-// (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
+// dz from z and lse: no part of a row needs to know another.  Where lse is so large that fp32 does not hold enough of
+// its fraction (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
 template <typename T>
 __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distill_args a, int parts, long long per)
 {

@@ -33,6 +33,7 @@ template <bool CLUSTER = true, typename PARAMS>
 __device__ __forceinline__ bool lt_wait(unsigned bar, unsigned parity, const PARAMS& P, LtShared* sh)
 {
     auto done = [&]() { return CLUSTER ? lfptx::mbar_try_wait_cluster(bar, parity) : lfptx::mbar_try_wait(bar, parity); };
+    if (!CLUSTER && lfptx::mbar_test_wait(bar, parity)) return true;
     if (done()) return true;
     if (sh->abort_flag) return false;
     const unsigned long long t0 = lfptx::globaltimer_ns();

@@ -733,3 +733,58 @@ def test_a_wait_that_runs_out(M, N, K):
         ops.sync()
         ref, err = O.product(qa.t, sa, qb.t, sb, True)
         R.check("after", d, ref, R.rounded(ref, F32, err))
+
+
+# ---- the layer made of them ----------------------------------------------------------------------------
+
+def _product8(a, b):
+    """a b^T of 64-bit matrices and how far the product of their 8-bit forms may be from it: a value is off by 2^-4 of itself, or by
+    2^-10 of its block's scale, which is less than 1 / 224 of the largest magnitude."""
+    ea, eb = (2.0 ** -4 * v.abs() + 2.0 ** -10 / 224 * v.abs().max() for v in (a, b))
+    return a @ b.t(), ea @ (b.abs() + eb).t() + a.abs() @ eb.t()
+
+
+@pytest.mark.parametrize("tokens,width,vocab", [(3, 64, 264), (130, 264, 1000), (520, 512, 2504)])
+def test_output_layer_gradients(tokens, width, vocab):
+    from paper_1801_04928_b200.output_layer import OutputLayer
+    g = _gen(tokens)
+    with lf.Operators() as ops:
+        layer = OutputLayer(ops, tokens + 5, width, vocab, seed=tokens)
+        layer.master["gain"].add_(_rand(g, width, std=0.2))
+        layer.master["shift"].add_(_rand(g, width, std=0.2))
+        x, r = _rand(g, tokens, width, dtype=BF16), _rand(g, tokens, width, dtype=BF16)
+        index, value = _teacher(g, tokens, vocab, 7)
+        weight = torch.rand(tokens, generator=g, device="cuda")
+        z, loss, dh = torch.empty(tokens, vocab, dtype=BF16, device="cuda"), torch.empty(tokens, device="cuda"), torch.empty_like(x)
+        layer.forward(x, r, z)
+        logits = z.clone()
+        layer.backward(z, index, value, loss, dh, weight=weight, temperature=2.0)
+        ops.sync()
+    p, w = layer.master, layer.master["w"].to(R.D)
+    rh, rm, rr, ry = O.layer_norm(x, p["gain"], p["shift"], r)
+    ref, err = _product8(ry, w)
+    R.check("logits", logits, ref, R.rounded(ref, BF16, 1.001 * err))
+    ref, err = O.distill(logits, index, value, weight, 2.0)
+    R.check("loss", loss, ref[0], R.rounded(ref[0], F32, err[0]))
+    R.check("dz", z, ref[2], R.rounded(ref[2], BF16, err[2]))
+    dz, u, du = z.to(R.D), layer.u[:tokens].to(R.D), layer.du[:tokens]
+    for name, got, (a, b) in (("gw", layer.grad["w"], (dz.t(), u.t())), ("du", du, (dz, w.t()))):
+        ref, err = _product8(a.contiguous(), b.contiguous())
+        R.check(name, got, ref, R.rounded(ref, got.dtype, 1.001 * err))
+    ref, err = O.layer_norm_backward(du, layer.h[:tokens], p["gain"], layer.mean[:tokens], layer.rstd[:tokens])
+    for name, got, a, e in (("dh", dh, ref[0], err[0]), ("gain", layer.grad["gain"], ref[1], err[1]), ("shift", layer.grad["shift"], ref[2], err[2])):
+        R.check(name, got, a, R.rounded(a, got.dtype, e))
+
+
+def test_output_layer_runs():
+    from paper_1801_04928_b200.output_layer import train
+    losses, layer, ops, x, r = train(130, 128, 1000, 8, 3)
+    assert all(math.isfinite(v) and v >= 0 for v in losses)
+    # one token through the few-token kernels: the same sums in another order
+    z, one = torch.empty(130, 1000, dtype=BF16, device="cuda"), torch.empty(1, 1000, dtype=BF16, device="cuda")
+    layer.forward(x, r, z, keep=False)
+    layer.forward(x[5:6], r[5:6], one, keep=False)
+    ops.sync()
+    d = (one[0].double() - z[5].double()).abs()
+    assert bool((d <= 2 * 2.0 ** -8 * z[5].double().abs() + 1e-4).all())
+    ops.close()
