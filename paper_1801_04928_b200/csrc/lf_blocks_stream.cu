@@ -14,6 +14,7 @@ namespace {
 using namespace lfrow;
 
 constexpr int BS_ROWS = 32, BS_DEPTH = 4, BS_STEP = 64;
+constexpr int BS_PREFETCH = 8192;               // bytes of a row of b
 
 __device__ __forceinline__ void mma16832(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
 {
@@ -90,6 +91,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_produc
             for (int i = 0; i < 2; ++i) s_next.x[j][i] = p.sa[(size_t)block * M + min(j * 8 + 2 * t + i, M - 1)];
     };
     rows_of();
+    // The first tile of b into L2 while the kernel before this one runs.  What that one still writes there it writes into L2 as
+    // well, so nothing is read too early; the tile itself is read after the wait.
+    if (threadIdx.x < (unsigned)rows && blockIdx.x * rows + threadIdx.x < (unsigned)N) {
+        const int bytes = min(K & ~15, BS_PREFETCH);
+        if (bytes) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.b + (size_t)(blockIdx.x * rows + threadIdx.x) * p.ld_b), "r"(bytes) : "memory");
+    }
     lf_grid_wait();
     lf_grid_release();
 #pragma unroll

@@ -435,14 +435,12 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
         online_edge<T>(o, z, mine, c);
     } else if (part == 0) {
         gather<T>(ent, a, token, z);
+        weigh(ent, a);
     }
     __syncwarp();
     o.join_row(warp_ms, row_warp, parts, c);
     if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    if (part == 0 && !row_warp) {
-        weigh(ent, a);
-        loss_of(ent, a, token, o.m, o.s);
-    }
+    if (part == 0 && !row_warp) loss_of(ent, a, token, o.m, o.s);
     __syncwarp();
     if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
 }

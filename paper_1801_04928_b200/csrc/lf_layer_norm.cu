@@ -297,8 +297,8 @@ struct norm_backward_go {
     static cudaError_t go(const lf_layer_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* grid_out)
     {
         const long long blocks = ((long long)a.tokens + GROUPS - 1) / GROUPS, room = (long long)(LF_OPS_FIXED_BYTES / (2 * sizeof(float))) / a.n;
-        long long grid = 2 * sm_count;
-        if (grid > room) grid = room;
+        // (wide rows: a block a multiprocessor, and as many partial rows as the workspace holds; 160 blocks of 4096 x 16384 took two rounds, 221 us)
+        long long grid = room >= 2 * sm_count ? 2 * sm_count : room < sm_count ? room : sm_count;
         if (grid > blocks) grid = blocks;
         const int d = depth(a.dres);
         *grid_out = (int)grid;
@@ -372,7 +372,7 @@ __device__ __forceinline__ float2 columns_of(const vec8<T>& v, int i)
     }
 }
 
-// TILES: a scale for the tile; TURN: the transposed form is wanted
+// TILES: a scale for the tile; TURN: the transposed form is wanted (without either: k_pack_rows)
 template <typename T, bool TILES, bool TURN>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_pack_blocks(const lf_pack_blocks_args a)
 {
@@ -501,12 +501,53 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_pack_blocks(con
     }
 }
 
+// Rows alone: a thread has eight columns of four rows, one after the other, and no block needs to know another row.  Shallower than the
+// tiles above, for few rows (509 x 4096: a launch and 0.5 us), and with more loads in flight for many.
+constexpr int PACK_ROWS = 4;
+template <typename T>
+__global__ void __launch_bounds__(256) k_pack_rows(const lf_pack_blocks_args a, int lanes_log2)
+{
+    typedef magnitudes<T> mags;
+    const unsigned nv = (unsigned)a.n >> 3, nbx = (nv + 255) / 256, by = blockIdx.x / nbx, bx = blockIdx.x - by * nbx;
+    const int lanes = 1 << lanes_log2, i = bx * 256 + (threadIdx.x & (lanes - 1));
+    const int row0 = ((int)by * (256 >> lanes_log2) + ((int)threadIdx.x >> lanes_log2)) * PACK_ROWS;
+    lf_grid_wait();
+    lf_grid_release();
+    vec8<T> v[PACK_ROWS];
+#pragma unroll
+    for (int p = 0; p < PACK_ROWS; ++p) {
+        v[p].zero();
+        if (i < (int)nv && row0 + p < a.tokens) v[p].load(static_cast<const T*>(a.x) + (size_t)(row0 + p) * a.ld_x + 8 * i);
+    }
+#pragma unroll
+    for (int p = 0; p < PACK_ROWS; ++p) {
+        const int row = row0 + p;
+        mags m;
+        m.of(v[p]);
+        unsigned w = m.largest();
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) w = mags::larger(w, __shfl_xor_sync(0xFFFFFFFFu, w, o));
+        const unsigned b = block_byte(mags::bits(w));
+        if (i < (int)nv && row < a.tokens) {
+            float f[8];
+            v[p].get(f);
+            *reinterpret_cast<uint2*>(a.q + (size_t)row * a.ld_q + 8 * i) = quantize8(f, b);
+            if ((i & 15) == 0) a.s[(size_t)(i >> 4) * a.tokens + row] = scale(b);
+        }
+    }
+}
+
 template <typename T>
 cudaError_t pack_of(const lf_pack_blocks_args& a, bool tiles, cudaStream_t s)
 {
     const dim3 grid((unsigned)ceil_div(a.n, 128) * (unsigned)ceil_div(a.tokens, 128));       // (2^31 tiles would be 35 TB)
     if (tiles) return lf_launch(a.qt ? k_pack_blocks<T, true, true> : k_pack_blocks<T, true, false>, grid, 256, 0, s, a);
-    return lf_launch(a.qt ? k_pack_blocks<T, false, true> : k_pack_blocks<T, false, false>, grid, 256, 0, s, a);
+    if (a.qt) return lf_launch(k_pack_blocks<T, false, true>, grid, 256, 0, s, a);
+    const int pieces = a.n >> 3;
+    int log2 = 4;                            // (a block's lanes at least)
+    while (log2 < 8 && (1 << log2) < pieces) ++log2;
+    const long long blocks = (long long)ceil_div(pieces, 256) * ceil_div(a.tokens, (256 >> log2) * PACK_ROWS);
+    return lf_launch(k_pack_rows<T>, dim3((unsigned)blocks), 256, 0, s, a, log2);
 }
 
 }  // namespace
