@@ -37,7 +37,7 @@ static_assert(LB_SLOTS * LB_SLOT_BYTES <= LB_EPI_BYTES, "either use of the space
 constexpr size_t LB_SMEM = (size_t)LB_RING_BYTES + LB_EPI_BYTES + 1024 + 512;
 constexpr int LBS_THREADS = 512, LBS_STAGES = 4, LBS_LD = 132;
 constexpr int LBS_TILE_BYTES = 128 * LBS_LD * 4;
-constexpr int LBS_SCALE_BYTES = 8 * 2 * 64 * 4;          // column scales of two blocks per warp
+constexpr int LBS_SCALE_BYTES = 8 * 2 * (32 + 64) * 4;   // scales of a warp's rows and columns, of two blocks
 constexpr size_t LBS_SMEM = (size_t)LBS_STAGES * LT_STAGE_BYTES + LBS_TILE_BYTES + LBS_SCALE_BYTES + 1024 + 512;
 
 struct LbParams {
@@ -207,29 +207,30 @@ __device__ __forceinline__ void lb_finish(float (&acc)[128], const LbParams& P, 
     }
 }
 
-// The same from fragments: a lane stores two columns at a time, four lanes 32 bytes of a row in fp32.
-template <typename OUT>
-__device__ __forceinline__ void lb_finish_fragments(float (&acc)[128], const LbParams& P, int row0, int col0)
+// The same from fragments: a lane stores two columns at a time, four lanes 32 bytes of a row in fp32.  WHOLE: every row and column exists.
+template <typename OUT, bool WHOLE>
+__device__ __forceinline__ void lb_finish_fragments(const float (&acc)[128], const LbParams& P, int row0, int col0)
 {
     typedef typename half_of<OUT>::type H;
     const int lane = threadIdx.x & 31, c0 = col0 + 2 * (lane & 3), r0 = row0 + (lane >> 2);
+    OUT* to[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[i] = static_cast<OUT*>(P.d) + (size_t)(r0 + 8 * i) * P.ld_d + c0;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {                               // eight columns at a time
-        const int col = c0 + 8 * j;
-        if (col >= P.N) break;
+        if (!WHOLE && c0 + 8 * j >= P.N) break;
         float2 bias = f2(0.f);
-        if (P.bias) bias = *reinterpret_cast<const float2*>(P.bias + col);
+        if (P.bias) bias = *reinterpret_cast<const float2*>(P.bias + c0 + 8 * j);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = r0 + 8 * i, at = 16 * (j >> 1) + 8 * (i >> 1) + 4 * (j & 1) + 2 * (i & 1);
-            if (row >= P.M) continue;
+            const int at = 16 * (j >> 1) + 8 * (i >> 1) + 4 * (j & 1) + 2 * (i & 1);
+            if (!WHOLE && r0 + 8 * i >= P.M) continue;
             float2 v = add2(make_float2(acc[at], acc[at + 1]), bias);
-            OUT* to = static_cast<OUT*>(P.d) + (size_t)row * P.ld_d + col;
             if (sizeof(OUT) == 2) {
-                if (P.add) v = add2(v, unpack2(*reinterpret_cast<const unsigned*>(static_cast<const H*>(P.add) + (size_t)row * P.ld_add + col), H()));
-                *reinterpret_cast<unsigned*>(to) = pack2(v.x, v.y, H());
+                if (P.add) v = add2(v, unpack2(*reinterpret_cast<const unsigned*>(static_cast<const H*>(P.add) + (size_t)(r0 + 8 * i) * P.ld_add + c0 + 8 * j), H()));
+                *reinterpret_cast<unsigned*>(to[i] + 8 * j) = pack2(v.x, v.y, H());
             } else {
-                *reinterpret_cast<float2*>(to) = v;
+                *reinterpret_cast<float2*>(to[i] + 8 * j) = v;
             }
         }
     }
@@ -429,8 +430,12 @@ k_blocks_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 }
             }
             if (!ok) break;
-            if (ROWS) lb_finish_fragments<OUT>(acc, P, row0, col0);
-            else lb_finish<OUT>(acc, P, row0, col0, blk);
+            if constexpr (ROWS) {
+                if (row0 + 32 <= P.M && col0 + 128 <= P.N) lb_finish_fragments<OUT, true>(acc, P, row0, col0);
+                else lb_finish_fragments<OUT, false>(acc, P, row0, col0);
+            } else {
+                lb_finish<OUT>(acc, P, row0, col0, blk);
+            }
         }
     }
 
@@ -558,10 +563,11 @@ k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const float* sa = P.sa + (size_t)ks0 * P.M + min(row, P.M - 1);
         const float* sb = ROWS ? P.sb + (size_t)ks0 * P.N + min(col0 + 2 * lane, P.N - 2) : P.sb + (size_t)tn * n_k_all + ks0;
         const size_t sb_step = ROWS ? (size_t)P.N : 1;
-        float acc[64], sa_next = 0.f;
-        float2 sb_next = f2(0.f);
+        float acc[64];
 #pragma unroll
         for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+        float sa_next = 0.f;
+        float2 sb_next = f2(0.f);
         auto scales_of = [&]() {
             sa_next = *sa;
             if (ROWS) sb_next = *reinterpret_cast<const float2*>(sb);
@@ -571,9 +577,12 @@ k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll 1
         for (int ks = 0; ks < n_k; ++ks) {
             const unsigned ab = (unsigned)ks & 1u;
-            const float s = ROWS ? sa_next : sa_next * sb_next.x;
-            float2* mine = reinterpret_cast<float2*>(scales + (warp - 2) * 512 + (ks & 1) * 256);
-            if (ROWS) mine[lane] = sb_next;
+            float* mine = reinterpret_cast<float*>(scales) + ((warp - 2) * 2 + (int)ab) * 96;
+            const float both = sa_next * sb_next.x;
+            if (ROWS) {
+                mine[lane] = sa_next;
+                reinterpret_cast<float2*>(mine + 32)[lane] = sb_next;
+            }
             if (ks + 1 < n_k) {
                 sa += P.M;
                 sb += sb_step;
@@ -582,34 +591,54 @@ k_blocks_split(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (ROWS) __syncwarp();
             if (!lt_wait<false>(lfptx::smem_u32(&sh->acc_full[ab]), ((unsigned)ks >> 1) & 1u, P, sh)) break;
             lfptx::tc_fence_after();
-            const float4* column = reinterpret_cast<const float4*>(mine);
+            float sr[4] = {0.f, 0.f, 0.f, 0.f};
+            if (ROWS) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float r[32];
-                lfptx::tmem_ld32_async(tmem_base + ((unsigned)(quad * 32) << 16) + ab * 128u + half * 64u + 32 * j, r);
-                lfptx::tmem_wait_ld32(r);
-                if (j == 1) {
-                    lfptx::tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->acc_empty[ab]));
+                for (int i = 0; i < 4; ++i) sr[i] = mine[8 * i + (lane >> 2)];
+            }
+            const float2* sc = reinterpret_cast<const float2*>(mine + 32) + (lane & 3);
+            const unsigned from = tmem_base + ((unsigned)(quad * 32) << 16) + ab * 128u + half * 64u;
+            // 32 columns at a time, or of fragments 16, the next ones on their way
+            auto taken = [&]() {
+                lfptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) lfptx::mbar_arrive(lfptx::smem_u32(&sh->acc_empty[ab]));
+            };
+            if constexpr (ROWS) {
+                float r[2][16];
+                lb_ld<true>(from, r[0]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    lfptx::tmem_wait_ld16(r[j & 1]);
+                    if (j < 3) lb_ld<true>(from + 16 * (j + 1), r[(j + 1) & 1]);
+                    else taken();
+                    lb_scale_add(acc + 16 * j, r[j & 1], sr, sc + 8 * j);
                 }
-                if (ROWS) {
+            } else {
 #pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        const float4 b = column[8 * j + g];
-                        const float f[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[32 * j + 4 * g + i] = fmaf(s * f[i], r[4 * g + i], acc[32 * j + 4 * g + i]);
-                    }
-                } else {
-                    lb_scale_add<32>(acc + 32 * j, r, s);
+                for (int j = 0; j < 2; ++j) {
+                    float r[32];
+                    lfptx::tmem_ld32_async(from + 32 * j, r);
+                    lfptx::tmem_wait_ld32(r);
+                    if (j == 1) taken();
+                    lb_scale_add<32>(acc + 32 * j, r, both);
                 }
             }
         }
-        float* to = tile + (quad * 32 + lane) * LBS_LD + half * 64;
+        if (ROWS) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            *reinterpret_cast<float4*>(to + 4 * i) = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 16 * (j >> 1) + 8 * (i >> 1) + 4 * (j & 1) + 2 * (i & 1);
+                    *reinterpret_cast<float2*>(tile + (quad * 32 + 8 * i + (lane >> 2)) * LBS_LD + half * 64 + 8 * j + 2 * (lane & 3)) = make_float2(acc[at], acc[at + 1]);
+                }
+        } else {
+            float* to = tile + (quad * 32 + lane) * LBS_LD + half * 64;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                *reinterpret_cast<float4*>(to + 4 * i) = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
+        }
     }
     __syncwarp();
     lfptx::tc_fence_before();
