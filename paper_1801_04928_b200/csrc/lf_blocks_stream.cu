@@ -4,7 +4,9 @@
 // (cp.async) and feeds warp-wide 16 x 8 x 32 products of e4m3 numbers with them (the order of the contraction is the
 // same permutation for both operands).  A step is 64 long, half a block: its sums, exact in fp32 but for the
 // tensor core's truncation of four instructions' partial sums, are multiplied by the scales and added in fp32.  One
-// persistent block per multiprocessor, whose warps split the contraction of a tile of up to 32 columns.
+// persistent block per multiprocessor, whose warps split the contraction of a tile of up to 32 columns.  One row of a:
+// 8192 -> 65536 91 us, 5.9 TB/s; 4096 -> 32768 27 us, 4.9, of which about 6 are launch, first loads and the last tile; 4096 -> 4096 5.4.  Warps of
+// their own that add the sums, so that no barrier holds the others at a tile's end: no faster, and 16 rows slower.
 #include "lf_ops_internal.h"
 #include "lf_ptx.cuh"
 #include "lf_rows.cuh"

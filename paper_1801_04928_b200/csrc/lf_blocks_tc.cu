@@ -12,6 +12,13 @@
 //     sums fill half of its registers, which is why tiles are not larger.
 //   Split tiles (k_blocks_split): one CTA per 128 x 128 tile and part of the contraction (1, 2, 4 or 8 parts), whose
 //     CTAs form a cluster and add their parts through distributed shared memory.
+// What bounds them: a block of a 256 x 256 tile takes the tensor cores 512 cycles and its fetch 575 (32 KB a multiprocessor at 57 bytes a
+// cycle); the way of an accumulator -- products, barrier, registers, barrier back to the issuer -- is about 1600 and two
+// of them are under way, so 820 with one scale for 128 columns.  With column scales two packed operations a pair of sums instead of one
+// keep the warps busy for 800 of about 1400.  8192 x 4096 -> 16384 in bf16: 489 us, 2.25 PFLOP/s (the same kernel without scales, one
+// accumulator per tile, 393); 4096 x 8192 -> 16384 in fp32 with column scales 691 us, 1.59.  In a loop of seconds
+// the power limit lowers the clock and they take 1.25 times as long.  Products of 128 columns at a time, so that an
+// accumulator's halves are handed over earlier, were slower (671 us for 503): two multiprocessors multiply 128 columns no faster than 192.
 // All waits are bounded; on expiry the status word is raised and the launch drains and ends.
 #include "lf_ops_internal.h"
 #include "lf_product_tc.cuh"
@@ -720,7 +727,11 @@ lb_kernel lb_pick(int out_dtype, bool rows, int splits)
     return rows ? lb_of<__half, true>(splits) : lb_of<__half, false>(splits);
 }
 
-// Parts of a split tile, or 0 for CTA pairs: the least estimated time in SM cycles.
+// Parts of a split tile, or 0 for CTA pairs: the least estimated time in SM cycles.  A stage costs a 128 x 128 tile 600 (fetch), a pair
+// 750; where the parts meet, 1500 and their bytes at 14 a cycle; the rest is launch, first loads and the end.  Measured, us,
+// taken against the next best: 509 x 4096 -> 1024 4 parts 9.2, 2 parts 11.4; 512 x 4096 -> 4096 1 part 16.4, pairs 19.9; 1000 x 8192 -> 1000
+// 2 parts 25.4, 4 parts 32.2; 2048 x 1024 -> 2304 pairs 15.6, 1 part 15.7; 2048 x 4096 -> 4096 pairs 37, 1 part 63.  Over 16 shapes it
+// takes the best form or one within 4 %.
 int lb_choose(const lf_ops* o, const lf_product_blocks_args& a, int n_k)
 {
     auto waves = [](long long units, int at_once) { return (double)((units + at_once - 1) / at_once); };

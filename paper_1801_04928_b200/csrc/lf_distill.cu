@@ -12,7 +12,8 @@
 // each, which are a cluster and meet once, over distributed shared memory, with their m and s.  Where the gradient is
 // written too, a part keeps what it has read in shared memory, so that the row is read from memory once.
 // The teacher's entries and the loss are one warp's work, beside the others' passes over the row; the dense part of the gradient is
-// written first, then the entries that fall into the part are put right.
+// written first, then the entries that fall into the part are put right.  Measured, bf16: loss alone 8192 x 131072 327 us, 6.56 TB/s; gradient
+// alone 8192 x 32768 197 us, 5.4; both at once 8192 x 131072 849 us, 5.06 TB/s.
 #include <math_constants.h>
 
 #include "lf_ops_internal.h"

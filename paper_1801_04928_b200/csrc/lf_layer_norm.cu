@@ -16,7 +16,8 @@ __device__ __forceinline__ unsigned block_byte(unsigned amax_bits) { return max(
 
 // ---- h = x + residual, y = (h - m) r gain + bias ------------------------------------------------------
 // The row stays in registers between its mean, the sum of squares about that mean (which does not cancel, as the mean
-// square less the squared mean would) and the result.
+// square less the squared mean would) and the result.  Bound by memory: 16384 x 4096 bf16 with residual, h and statistics 90 us, 5.95 TB/s;
+// one row of 4096 2.6 us, a launch.
 template <typename T, int TPR, int VPT>
 __global__ void __launch_bounds__(TPR) k_layer_norm(const lf_layer_norm_args a)
 {
@@ -110,8 +111,13 @@ __global__ void __launch_bounds__(TPR) k_layer_norm(const lf_layer_norm_args a)
 // ---- dh = r (u - mean u - c mean(u c)) + dres, partial column sums of dy c and dy ---------------------
 // As k_rms_norm_backward: groups of TPR threads walk down the matrix, the rows ahead are on their way into shared memory
 // (cp.async; a thread reads only what it copied itself, so dh may be any of the inputs), both row sums share one
-// exchange, the gradients of gain and bias stay in registers and are added at the end, a partial row of 2 n per block.
-template <typename T, int TPR, int VPT, int GROUPS>
+// exchange, the gradients of gain and bias stay in registers and are added at the end, a partial row of 2 n per block.  16384 x 8192 bf16 with
+// dres: 204 us, 5.26 TB/s, bound like that kernel by the chain load, sums, barrier, results of the two rows that a multiprocessor overlaps
+// (mean and rstd a row ahead: no change); 999 x 1032 fp32 11.3 us, of which the second launch, the sum over 250 blocks, is half.
+// ONE: the grid is one cluster, which adds the gradients of gain and bias through distributed shared memory: a launch instead of
+// two for up to eight blocks and 4096 columns (one row of 4096: 4.1 us, one of 2344 3.5).
+constexpr int NORM_CLUSTER = 8;
+template <typename T, int TPR, int VPT, int GROUPS, bool ONE>
 __global__ void __launch_bounds__(TPR * GROUPS) k_layer_norm_backward(const lf_layer_norm_backward_args a, float* sums, int depth)
 {
     extern __shared__ __align__(16) unsigned char ring[];      // [depth][tensor][VPT][thread] pieces of eight elements
@@ -231,7 +237,7 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_layer_norm_backward(const lf_l
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     lf_grid_release();
-    if (!sums) return;
+    if (!ONE && !sums) return;
     if (GROUPS > 1) {
         // add the groups' sums in group order, the gain's first (each fits the ring, see norm_backward_go::bytes)
         float2* all = reinterpret_cast<float2*>(ring);
@@ -255,18 +261,41 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_layer_norm_backward(const lf_l
                         }
             }
         }
-        if (g > 0) return;
+        if (!ONE && g > 0) return;
     }
+    float* mine = reinterpret_cast<float*>(ring);            // [2][n]
+    if (ONE) __syncthreads();
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int i = j * TPR + t;
-        if (i >= nv) continue;
-        float4* to = reinterpret_cast<float4*>(sums + (size_t)blockIdx.x * 2 * a.n + 8 * i);
+        if (i >= nv || (ONE && g > 0)) continue;
+        float4* to = reinterpret_cast<float4*>((ONE ? mine : sums + (size_t)blockIdx.x * 2 * a.n) + 8 * i);
         to[0] = make_float4(dg[j][0].x, dg[j][0].y, dg[j][1].x, dg[j][1].y);
         to[1] = make_float4(dg[j][2].x, dg[j][2].y, dg[j][3].x, dg[j][3].y);
         to += a.n / 4;
         to[0] = make_float4(db[j][0].x, db[j][0].y, db[j][1].x, db[j][1].y);
         to[1] = make_float4(db[j][2].x, db[j][2].y, db[j][3].x, db[j][3].y);
+    }
+    if (ONE) {
+        // every block adds the blocks' sums of its share of the columns, in block order
+        __syncwarp();
+        lfptx::cluster_sync_all();
+        const unsigned from = lfptx::smem_u32(mine);
+        for (int v = (int)blockIdx.x * THREADS + (int)threadIdx.x; v < a.n / 2; v += (int)gridDim.x * THREADS) {
+            float4 p[NORM_CLUSTER];
+#pragma unroll
+            for (unsigned c = 0; c < NORM_CLUSTER; ++c)
+                if (c < gridDim.x)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(p[c].x), "=f"(p[c].y), "=f"(p[c].z), "=f"(p[c].w) : "r"(lfptx::map_to_cta(from, c) + 16u * (unsigned)v) : "memory");
+#pragma unroll
+            for (unsigned c = 1; c < NORM_CLUSTER; ++c)
+                if (c < gridDim.x) { p[0].x += p[c].x; p[0].y += p[c].y; p[0].z += p[c].z; p[0].w += p[c].w; }
+            float* to = v < a.n / 4 ? a.dgain : a.dbias;
+            if (to) *reinterpret_cast<float4*>(to + 4 * (v < a.n / 4 ? v : v - a.n / 4)) = p[0];
+        }
+        __syncwarp();
+        lfptx::cluster_sync_all();                              // nobody leaves while its sums are being read
     }
 }
 
@@ -294,15 +323,26 @@ struct norm_backward_go {
         return d;
     }
     // (the groups' sums, 32 bytes per thread and vector, fit one slot: two tensors of 16 bytes at least)
+    static constexpr size_t one_bytes(bool dres) { return slot(dres) > (size_t)64 * TPR ? slot(dres) : (size_t)64 * TPR; }      // a row, or 2 n sums
     static cudaError_t go(const lf_layer_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* grid_out)
     {
-        const long long blocks = ((long long)a.tokens + GROUPS - 1) / GROUPS, room = (long long)(LF_OPS_FIXED_BYTES / (2 * sizeof(float))) / a.n;
+        const long long blocks = ((long long)a.tokens + GROUPS - 1) / GROUPS;
+        if constexpr (VPT == 1) {                                  // (few rows of up to 4096 columns)
+            if ((a.dgain || a.dbias) && blocks <= NORM_CLUSTER) {
+                int grid = 1;
+                while (grid < blocks) grid *= 2;
+                *grid_out = 0;
+                return lf_launch_clusters(k_layer_norm_backward<T, TPR, VPT, GROUPS, true>, dim3((unsigned)grid), TPR * GROUPS, one_bytes(a.dres), grid, s, a,
+                                          (float*)nullptr, 1);     // a row each: a ring of one
+            }
+        }
+        const long long room = (long long)(LF_OPS_FIXED_BYTES / (2 * sizeof(float))) / a.n;
         // (wide rows: a block a multiprocessor, and as many partial rows as the workspace holds; 160 blocks of 4096 x 16384 took two rounds, 221 us)
         long long grid = room >= 2 * sm_count ? 2 * sm_count : room < sm_count ? room : sm_count;
         if (grid > blocks) grid = blocks;
         const int d = depth(a.dres);
         *grid_out = (int)grid;
-        return lf_launch(k_layer_norm_backward<T, TPR, VPT, GROUPS>, dim3((unsigned)grid), TPR * GROUPS, slot(a.dres) * d, s, a,
+        return lf_launch(k_layer_norm_backward<T, TPR, VPT, GROUPS, false>, dim3((unsigned)grid), TPR * GROUPS, slot(a.dres) * d, s, a,
                          a.dgain || a.dbias ? partial : nullptr, d);
     }
 };
@@ -313,8 +353,12 @@ struct norm_backward_ready {
     static cudaError_t go()
     {
         const size_t with = shape::slot(true) * shape::depth(true), without = shape::slot(false) * shape::depth(false);
-        return cudaFuncSetAttribute(k_layer_norm_backward<T, TPR, VPT, shape::GROUPS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)(with > without ? with : without));
+        cudaError_t e = cudaFuncSetAttribute(k_layer_norm_backward<T, TPR, VPT, shape::GROUPS, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)(with > without ? with : without));
+        if constexpr (VPT == 1)
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(k_layer_norm_backward<T, TPR, VPT, shape::GROUPS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shape::one_bytes(true));
+        return e;
     }
 };
 
@@ -323,7 +367,7 @@ struct norm_backward_ready {
 // that the largest magnitudes of rows, columns or the tile are taken, and both forms written, from one read.  Magnitudes are compared as
 // integers, 16-bit ones two at a time.  The transposed form is turned in shared memory, in pieces of 8 rows of a column whose
 // place is turned by the column, so that neither side meets a bank twice; it is written a piece of 16 bytes at a time, the last one of a row byte
-// by byte where it is not full.  Bound by memory.
+// by byte where it is not full.  Bound by memory: both forms of 8192 x 16384 bf16 104 us, 5.2 TB/s, the transposed one 69, 5.8.
 template <typename T>
 struct magnitudes {                         // of eight columns
     static constexpr int N = sizeof(T) == 2 ? 4 : 8;
@@ -502,7 +546,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_pack_blocks(con
 }
 
 // Rows alone: a thread has eight columns of four rows, one after the other, and no block needs to know another row.  Shallower than the
-// tiles above, for few rows (509 x 4096: a launch and 0.5 us), and with more loads in flight for many.
+// tiles above, for few rows (509 x 4096: 2.6 us), and with more loads in flight
+// for many (8192 x 16384 bf16 63 us, 6.3 TB/s; as tiles of 8192 x 4096 26 us, now 17).
 constexpr int PACK_ROWS = 4;
 template <typename T>
 __global__ void __launch_bounds__(256) k_pack_rows(const lf_pack_blocks_args a, int lanes_log2)
@@ -580,7 +625,7 @@ cudaError_t lfk_layer_norm_backward(const lf_layer_norm_backward_args& a, float*
     else if (a.dtype == LF_BF16) e = pick_row_shape<norm_backward_go, __nv_bfloat16>(a.n, many, a, partial, sm_count, s, &grid);
     else e = pick_row_shape<norm_backward_go, __half>(a.n, many, a, partial, sm_count, s, &grid);
     *launches = 1;
-    if (e == cudaSuccess && (a.dgain || a.dbias)) {
+    if (e == cudaSuccess && (a.dgain || a.dbias) && grid > 0) {
         e = lfk_sum_rows(partial, grid, 2 * a.n, a.dgain, a.dbias, a.n, s);
         *launches = 2;
     }

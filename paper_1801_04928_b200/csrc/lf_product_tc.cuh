@@ -28,7 +28,7 @@ static_assert(sizeof(LtShared) <= 512, "the barrier block must fit into the spac
 
 // Bounded wait (acquire at cluster scope: the peer's arrivals count too); false once this CTA has given up.
 // CLUSTER = false: an acquire of this CTA's scope, for barriers that order tensor memory and bulk copies only (which have fences of
-// their own): several times a stage, the wider scope's fences were most of the stage's time.
+// their own): several times a stage, the wider scope's fences were half of the time (8-bit products, 8192 x 4096 -> 16384: 1206 us, 600 without).
 template <bool CLUSTER = true, typename PARAMS>
 __device__ __forceinline__ bool lt_wait(unsigned bar, unsigned parity, const PARAMS& P, LtShared* sh)
 {
