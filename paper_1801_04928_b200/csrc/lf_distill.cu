@@ -26,6 +26,7 @@ using namespace lfrow;
 
 constexpr int DT_ROW_THREADS = 256;             // for the row; beside them a warp for the teacher's entries and the loss
 constexpr int DT_THREADS = DT_ROW_THREADS + 32;
+constexpr int DT_TABLE_LOG2 = 10, DT_TABLE_ROUNDS = 12;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
 constexpr float DT_LARGE_LSE = 1024.f;          // from here on lse in fp32 is off by 3e-5, so much of the gradient
@@ -252,7 +253,7 @@ __device__ __forceinline__ void gather(const entries& e, const lf_distill_args& 
     }
     __syncwarp();
 }
-__device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a)
+__device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a, short* table)
 {
     const int lane = threadIdx.x & 31;
     const float inv_t = 1.0f / a.temperature, top = e.facts->top;
@@ -268,24 +269,41 @@ __device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a
     for (int k = lane; k < a.top; k += 32) e.p[k] = e.at[k] >= 0 ? e.p[k] * inv : 0.f;
     if (lane == 0) e.facts->sum = sum;
     __syncwarp();
-    // several entries on one element: the first adds them up, in their order
+    // Several entries on one element: the first adds them up, in their order.  Whether there are any is found with a table: an entry
+    // leaves its number at its element's place there and looks who is there then: itself, or an entry on the same element, or on another
+    // one, and then it tries again with the others that did, by another multiplier.  (Every entry against every other: 102 of them took longer than a row of 5249.)
+    bool several = false;
+    unsigned mult = 2654435769u;
+    for (int k = lane; k < a.top; k += 32) e.total[k] = e.p[k];
+    for (int round = 0, left = 1; left && !several; ++round, mult = mult * 5u + 0x9E3779B8u) {
+        left = 0;
+        for (int k = lane; k < a.top; k += 32)
+            if (e.at[k] >= 0 && (round == 0 || e.total[k] < 0.f)) table[(mult * (unsigned)e.at[k]) >> (32 - DT_TABLE_LOG2)] = (short)k;
+        __syncwarp();
+        for (int k = lane; k < a.top; k += 32) {
+            const int at = e.at[k];
+            if (at < 0 || (round > 0 && !(e.total[k] < 0.f))) continue;
+            const int there = table[(mult * (unsigned)at) >> (32 - DT_TABLE_LOG2)];
+            const bool again = there != k && e.at[there] != at;
+            several |= there != k && !again;
+            left |= again;
+            e.total[k] = again ? -1.f : e.p[k];             // (a mark: weights are not below zero)
+        }
+        left = __any_sync(0xFFFFFFFFu, left);
+        several = __any_sync(0xFFFFFFFFu, several) || round == DT_TABLE_ROUNDS;
+        __syncwarp();
+    }
+    if (!several) return;
     for (int k = lane; k < a.top; k += 32) {
         const int at = e.at[k];
-        float total = e.p[k];
-        int others = 0;
-#pragma unroll 8
-        for (int j = 0; j < a.top; ++j) others += e.at[j] == at;
-        if (others > 1) {
-            bool first = true;
-            total = 0.f;
-            for (int j = 0; j < a.top; ++j)
-                if (e.at[j] == at) {
-                    total += e.p[j];
-                    first &= j >= k;
-                }
-            if (!first) total = -1.f;
-        }
-        e.total[k] = total;
+        bool first = at >= 0;
+        float total = 0.f;
+        for (int j = 0; j < a.top; ++j)
+            if (e.at[j] == at) {
+                total += e.p[j];
+                first &= j >= k;
+            }
+        e.total[k] = first ? total : -1.f;
     }
 }
 // The loss, by one warp.  A weight p that fp32 does not tell from zero has no part in it, whatever logit it falls on.
@@ -419,6 +437,7 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
 {
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
+    __shared__ short table[1 << DT_TABLE_LOG2];
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
     const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
@@ -436,7 +455,7 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
         online_edge<T>(o, z, mine, c);
     } else if (part == 0) {
         gather<T>(ent, a, token, z);
-        weigh(ent, a);
+        weigh(ent, a, table);
     }
     __syncwarp();
     o.join_row(warp_ms, row_warp, parts, c);
@@ -456,6 +475,7 @@ __global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf
 {
     extern __shared__ __align__(16) unsigned char space[];     // staged pieces, entries
     __shared__ entry_facts facts;
+    __shared__ short table[1 << DT_TABLE_LOG2];
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
     const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
     const bool row_warp = tid < DT_ROW_THREADS;
@@ -488,7 +508,7 @@ __global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf
     const float w = a.weight ? a.weight[token] : 1.f, wt = w * a.temperature, m = o.m;
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !facts.any;
     if (!row_warp) {
-        weigh(ent, a);
+        weigh(ent, a, table);
     } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
         gradient_pieces<T, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
@@ -517,6 +537,7 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
 {
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
+    __shared__ short table[1 << DT_TABLE_LOG2];
     __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
     const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
@@ -527,7 +548,7 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
     lf_grid_release();
     if (!row_warp) gather<T>(ent, a, token, z);
     if (a.dz == a.z) __syncthreads();      // the entries' logits have been read
-    if (!row_warp) weigh(ent, a);
+    if (!row_warp) weigh(ent, a, table);
     const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], c = LOG2E / a.temperature;
     const bool large = fabsf(lse) >= DT_LARGE_LSE;
     if (large && part > 0) return;
