@@ -33,9 +33,9 @@ __device__ __forceinline__ void copy16(unsigned dst, const void* src, int valid)
 template <typename OUT>
 __device__ __forceinline__ float as_float(const void* p, size_t at) { return (float)static_cast<const OUT*>(p)[at]; }
 
-// TT: blocks of eight rows of a (1 or 2); B_ROWS: a scale for each row of b
+// TT: blocks of eight rows of a (1 or 2); B_ROWS: a scale for each row of b; share: warps to a tile
 template <typename OUT, int TT, int WARPS, bool B_ROWS>
-__global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_product_blocks_args p, int rows)
+__global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_product_blocks_args p, int rows, int share)
 {
     // [tile parity][warp][row of a][column]: 33 words keep the lanes of a fragment on different banks; before it the
     // ring: [step][piece][thread] pieces of 16 bytes, each copied and read by one thread only
@@ -45,7 +45,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_produc
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int M = p.tokens, N = p.n_out, K = p.n_in;
     const int tiles = (N + rows - 1) / rows, steps = (K + BS_STEP - 1) / BS_STEP, blocks = (K + 127) >> 7;
-    const int c0 = (int)((long long)steps * warp / WARPS), c1 = (int)((long long)steps * (warp + 1) / WARPS);
+    const int groups = WARPS / share, group = share == WARPS ? 0 : warp / share, member = warp - group * share;
+    const int first = blockIdx.x * groups + group, stride = gridDim.x * groups;
+    // (steps are 2^24 at most)
+    const int c0 = share == WARPS ? steps * member / WARPS : steps * member / share, c1 = share == WARPS ? steps * (member + 1) / WARPS : steps * (member + 1) / share;
     const unsigned my_ring = lfptx::smem_u32(bs_raw) + threadIdx.x * 16;
 
     const unsigned char* xp[TT];
@@ -56,7 +59,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_produc
         xp[j] = p.a + (xv[j] ? (size_t)(j * 8 + g) * p.ld_a + 16 * t : 0);
     }
     // the step that is fetched next
-    int f_tile = blockIdx.x, f_c = c0;
+    int f_tile = first, f_c = c0;
     const unsigned char* wp[4];
     bool wv[4];
     auto rows_of = [&]() {
@@ -75,7 +78,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_produc
             for (int r = 0; r < 4; ++r) copy16<false>(dst + r * (THREADS * 16), kv && wv[r] ? wp[r] + k : p.b, wv[r] ? kv : 0);
 #pragma unroll
             for (int j = 0; j < TT; ++j) copy16<true>(dst + (4 + j) * (THREADS * 16), kv && xv[j] ? xp[j] + k : p.a, xv[j] ? kv : 0);
-            if (++f_c == c1) { f_c = c0; f_tile += gridDim.x; rows_of(); }
+            if (++f_c == c1) { f_c = c0; f_tile += stride; rows_of(); }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -94,18 +97,19 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_produc
     };
     rows_of();
     // The first tile of b into L2 while the kernel before this one runs.  What that one still writes there it writes into L2 as
-    // well, so nothing is read too early; the tile itself is read after the wait.
-    if (threadIdx.x < (unsigned)rows && blockIdx.x * rows + threadIdx.x < (unsigned)N) {
+    // well, so nothing is read too early; the tile itself is read after the wait.  (Not where it is the only one: 4096 -> 4096 5.8 us with, 5.5
+    // without; 4096 -> 32768 28.1 and 29.6.)
+    if (tiles > stride && member == 0 && lane < rows && first * rows + lane < N) {
         const int bytes = min(K & ~15, BS_PREFETCH);
-        if (bytes) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.b + (size_t)(blockIdx.x * rows + threadIdx.x) * p.ld_b), "r"(bytes) : "memory");
+        if (bytes) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.b + (size_t)(first * rows + lane) * p.ld_b), "r"(bytes) : "memory");
     }
     lf_grid_wait();
     lf_grid_release();
 #pragma unroll
     for (int d = 0; d < BS_DEPTH - 1; ++d) fetch(d);
-    if (c0 < c1) scales_of(blockIdx.x, c0 >> 1);
+    if (c0 < c1) scales_of(first, c0 >> 1);
     int parity = 0, slot = 0;
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, parity ^= 1) {
+    for (int tile = first; tile < tiles; tile += stride, parity ^= 1) {
         float sum[2][TT][4];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -118,7 +122,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_produc
                 s = s_next;
                 const int next = (c >> 1) + 1;
                 if (2 * next < c1) scales_of(tile, next);
-                else if (tile + (int)gridDim.x < tiles) scales_of(tile + gridDim.x, c0 >> 1);
+                else if (tile + stride < tiles) scales_of(tile + stride, c0 >> 1);
             }
             fetch(slot == 0 ? BS_DEPTH - 1 : slot - 1);
             asm volatile("cp.async.wait_group %0;" ::"n"(BS_DEPTH - 1) : "memory");
@@ -146,14 +150,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_blocks_stream(const lf_produc
             for (int j = 0; j < TT; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) red[parity][warp][j * 8 + 2 * t + (i & 1)][m * 16 + g + 8 * (i >> 1)] = sum[m][j][i];
-        __syncthreads();
+        if (share > 1) lfptx::bar_sync(1 + group, share * 32);             // the tile's warps
+        else __syncwarp();
         // a warp takes a row of a at a time, a lane a column; the sums are added in warp order
         const int col = tile * rows + lane;
-        for (int tok = warp; tok < TT * 8 && tok < M; tok += WARPS) {
+        for (int tok = member; tok < TT * 8 && tok < M; tok += share) {
             if (lane >= rows || col >= N) continue;
             float v = 0.f;
+            if (share == WARPS) {
 #pragma unroll
-            for (int i = 0; i < WARPS; ++i) v += red[parity][i][tok][lane];
+                for (int i = 0; i < WARPS; ++i) v += red[parity][i][tok][lane];
+            } else {
+#pragma unroll 4
+                for (int i = group * share; i < (group + 1) * share; ++i) v += red[parity][i][tok][lane];
+            }
             if (p.bias) v += p.bias[col];
             if (p.add) v += as_float<OUT>(p.add, (size_t)tok * p.ld_add + col);
             static_cast<OUT*>(p.d)[(size_t)tok * p.ld_d + col] = (OUT)v;
@@ -185,12 +195,22 @@ constexpr size_t stream_smem() { return (size_t)BS_DEPTH * (4 + TT) * WARPS * 32
 template <typename OUT, int TT, int WARPS>
 cudaError_t stream_go(const lf_product_blocks_args& a, int sm_count, cudaStream_t s)
 {
-    const int waves = (a.n_out + BS_ROWS * sm_count - 1) / (BS_ROWS * sm_count);
-    int rows = (a.n_out + sm_count * waves - 1) / (sm_count * waves);          // tiles come out even over the multiprocessors
+    // Warps to a tile: as many as have four steps each, and more where there are too few tiles for the others.  (A tile's end costs
+    // its warps a meeting: one row, 968 -> 42800 15.8 us with all 16 to a tile, 13.2 with four; but warps at work on one tile read its rows
+    // in longer pieces: one row, 8192 -> 65536 91 us with all 16 to a tile, 109 with one.)
+    const int steps = (a.n_in + BS_STEP - 1) / BS_STEP, tiles32 = (a.n_out + BS_ROWS - 1) / BS_ROWS;
+    int share = 1;
+    while (share < WARPS && (steps / share > 4 || (long long)tiles32 * share < (long long)sm_count * WARPS)) {
+        ++share;
+        while (WARPS % share) ++share;
+    }
+    const int groups = sm_count * (WARPS / share);
+    const int waves = (a.n_out + BS_ROWS * groups - 1) / (BS_ROWS * groups);
+    int rows = (a.n_out + groups * waves - 1) / (groups * waves);              // tiles come out even over the groups
     if (rows < 8) rows = 8;                                                    // a load covers eight rows
-    const int tiles = (a.n_out + rows - 1) / rows;
+    const int tiles = (a.n_out + rows - 1) / rows, blocks = (tiles + WARPS / share - 1) / (WARPS / share);
     return lf_launch(a.b_tiles ? k_blocks_stream<OUT, TT, WARPS, false> : k_blocks_stream<OUT, TT, WARPS, true>,
-                     dim3((unsigned)(tiles < sm_count ? tiles : sm_count)), WARPS * 32, stream_smem<TT, WARPS>(), s, a, rows);
+                     dim3((unsigned)(blocks < sm_count ? blocks : sm_count)), WARPS * 32, stream_smem<TT, WARPS>(), s, a, rows, share);
 }
 template <typename OUT>
 cudaError_t stream_of(const lf_product_blocks_args& a, int sm_count, cudaStream_t s)

@@ -24,13 +24,16 @@ namespace {
 
 using namespace lfrow;
 
-constexpr int DT_ROW_THREADS = 256;             // for the row; beside them a warp for the teacher's entries and the loss
-constexpr int DT_THREADS = DT_ROW_THREADS + 32;
+// Threads for a row (RT in what follows): 256, or 64 where rows are short; beside them a warp for the teacher's entries and the loss.
+constexpr int DT_LONG = 256, DT_SHORT = 64;
 constexpr int DT_TABLE_LOG2 = 10, DT_TABLE_ROUNDS = 12;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
 constexpr float DT_LARGE_LSE = 1024.f;          // from here on lse in fp32 is off by 3e-5, so much of the gradient
-constexpr int DT_BLOCKS = 6;                    // of the joint kernel per multiprocessor
+// Rows up to here are short, where there are so many tokens that a row need not be cut; up to twice as much (the joint kernel: half as much again)
+// where there are eight for a multiprocessor.  Measured, us, short against long: both at once 5554 x 5249 f16 42 and 71, 8192 x 12000 bf16 94
+// and 101, 8192 x 16384 131 and 114; loss 8192 x 16384 50 and 70, 400 x 30000 11.8 and 10.0; gradient 8192 x 16384 95 and 113, 8192 x 30000 190 and 167.
+constexpr int DT_SHORT_BYTES = 16 * 1024;
 constexpr int DT_PART_BYTES = 32 * 1024;        // of a row that a block of the joint kernel has, where eight parts are enough
 constexpr int DT_STAGE_BYTES = DT_PART_BYTES;   // at most of a part that stays in shared memory
 
@@ -164,9 +167,10 @@ struct online {
     }
     // Over the row's warps of all blocks of a cluster: every warp leaves its own, and after one barrier takes all of them, the same ones on a lane.
     // `mine`: this warp has a share of the row.
+    template <int RT>
     __device__ __forceinline__ void join_row(float2* warp_ms, bool mine, int parts, float c)
     {
-        constexpr int WARPS = DT_ROW_THREADS / 32, EACH = WARPS * DT_MAX_PARTS / 32;
+        constexpr int WARPS = RT / 32, EACH = (WARPS * DT_MAX_PARTS + 31) / 32;
         const int lane = threadIdx.x & 31;
         if (mine) {
             join_lanes(c);
@@ -221,15 +225,17 @@ struct entries {                       // the teacher's, of one token
         total = z + top;
     }
 };
-// By one warp, in two steps: what is read of the row, and what follows from it.  A sum over lanes adds in a fixed order.
+// By one warp, in two steps: what is read of the row (the logits of elements [e0, e1)), and what follows from it.  A sum over lanes adds in a fixed order.
 template <typename T>
-__device__ __forceinline__ void gather(const entries& e, const lf_distill_args& a, int token, const T* z)
+__device__ __forceinline__ void gather(const entries& e, const lf_distill_args& a, int token, const T* z, long long e0, long long e1)
 {
     const int lane = threadIdx.x & 31;
     const int* index = a.index + (size_t)token * a.top;
     const float* value = a.value + (size_t)token * a.top;
     float top = -CUDART_INF_F;
     int bad = 0, any = 0;
+    // (the list first, then the logits, several loads of each under way)
+#pragma unroll 4
     for (int k = lane; k < a.top; k += 32) {
         const int i = index[k];
         const float t = value[k];
@@ -239,8 +245,12 @@ __device__ __forceinline__ void gather(const entries& e, const lf_distill_args& 
         any |= there;
         e.at[k] = there && !beyond ? i : -1;
         e.t[k] = there ? t : -CUDART_INF_F;
-        e.z[k] = there && !beyond ? (float)z[i] : 0.f;
         if (there) top = fmaxf(top, t);
+    }
+#pragma unroll 4
+    for (int k = lane; k < a.top; k += 32) {
+        const int i = e.at[k];
+        e.z[k] = i >= e0 && i < e1 ? (float)z[i] : 0.f;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -324,10 +334,10 @@ __device__ __forceinline__ void loss_of(const entries& e, const lf_distill_args&
     }
 }
 // By the row's threads: dz of the entries that fall on elements [e0, e1)
-template <typename T, typename F>
+template <typename T, int RT, typename F>
 __device__ __forceinline__ void put_right(const entries& e, int top, long long e0, long long e1, T* dz, float wt, F q_of)
 {
-    for (int k = threadIdx.x; k < top; k += DT_ROW_THREADS) {
+    for (int k = threadIdx.x; k < top; k += RT) {
         const int at = e.at[k];
         // (NaN, the weight of a list that holds one, is no number below zero)
         if (at >= e0 && at < e1 && !(e.total[k] < 0.f)) dz[at] = (T)(wt * (q_of(e.z[k]) - e.total[k]));
@@ -361,27 +371,27 @@ __device__ __forceinline__ void gradient_piece(float (&v)[16 / sizeof(T)], uint4
     }
 }
 // pieces [first, last) of a part's dz, a thread's of them, from pieces that `at` gives, BATCH of them before the first is used
-template <typename T, int BATCH, typename F>
+template <typename T, int RT, int BATCH, typename F>
 __device__ __forceinline__ void gradient_pieces(T* to, int first, int last, float m, float c, float f, bool aligned, F at)
 {
-    constexpr int N = 16 / (int)sizeof(T), STEP = DT_ROW_THREADS * BATCH;
+    constexpr int N = 16 / (int)sizeof(T), STEP = RT * BATCH;
     float v[N];
     int i = first + (int)threadIdx.x;
     if (aligned) {
-        for (; i + STEP - DT_ROW_THREADS < last; i += STEP) {
+        for (; i + STEP - RT < last; i += STEP) {
             uint4 r[BATCH];
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) r[u] = at(i + u * DT_ROW_THREADS);
+            for (int u = 0; u < BATCH; ++u) r[u] = at(i + u * RT);
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
                 gradient_piece<T>(v, r[u], m, c, f);
                 piece16<T> o;
                 o.set(v);
-                reinterpret_cast<uint4*>(to)[i + u * DT_ROW_THREADS] = o.u;
+                reinterpret_cast<uint4*>(to)[i + u * RT] = o.u;
             }
         }
     }
-    for (; i < last; i += DT_ROW_THREADS) {
+    for (; i < last; i += RT) {
         gradient_piece<T>(v, at(i), m, c, f);
         store_piece<T>(to + (long long)i * N, v, aligned);
     }
@@ -394,34 +404,34 @@ __device__ __forceinline__ void gradient_edge(T* dz, const T* z, const part_of<T
         dz[at] = (T)(f * ex2(((float)z[at] - m) * c));
     }
 }
-template <typename T>
+template <typename T, int RT>
 __device__ __forceinline__ void fill_part(T* dz, const part_of<T>& mine, float with, bool aligned)
 {
     float v[16 / sizeof(T)];
 #pragma unroll
     for (int k = 0; k < 16 / (int)sizeof(T); ++k) v[k] = with;
-    for (int i = threadIdx.x; i < mine.pieces; i += DT_ROW_THREADS) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
+    for (int i = threadIdx.x; i < mine.pieces; i += RT) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
     if ((int)threadIdx.x < mine.edge) dz[mine.at_edge(threadIdx.x)] = (T)with;
 }
-template <typename T>
-__device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool aligned) { fill_part<T>(dz, mine, 0.f, aligned); }
+template <typename T, int RT>
+__device__ __forceinline__ void zero_part(T* dz, const part_of<T>& mine, bool aligned) { fill_part<T, RT>(dz, mine, 0.f, aligned); }
 
 // pieces [first, last) of a part, a thread's of them, from pieces that `at` gives, DT_UNROLL at a time
-template <typename T, typename F>
+template <typename T, int RT, typename F>
 __device__ __forceinline__ void online_pieces(online& o, int first, int last, float c, F at)
 {
-    constexpr int STEP = DT_ROW_THREADS * DT_UNROLL;
+    constexpr int STEP = RT * DT_UNROLL;
     uint4 r[DT_UNROLL];
     int i = first + (int)threadIdx.x;
-    for (; i + STEP - DT_ROW_THREADS < last; i += STEP) {
+    for (; i + STEP - RT < last; i += STEP) {
 #pragma unroll
-        for (int u = 0; u < DT_UNROLL; ++u) r[u] = at(i + u * DT_ROW_THREADS);
+        for (int u = 0; u < DT_UNROLL; ++u) r[u] = at(i + u * RT);
         o.add<T>(r, c);
     }
     if (i < last) {
         const unsigned none = minus_infinity(T());
 #pragma unroll
-        for (int u = 0; u < DT_UNROLL; ++u) r[u] = i + u * DT_ROW_THREADS < last ? at(i + u * DT_ROW_THREADS) : make_uint4(none, none, none, none);
+        for (int u = 0; u < DT_UNROLL; ++u) r[u] = i + u * RT < last ? at(i + u * RT) : make_uint4(none, none, none, none);
         o.add<T>(r, c);
     }
 }
@@ -432,33 +442,33 @@ __device__ __forceinline__ void online_edge(online& o, const T* z, const part_of
 }
 
 // Loss and lse of a token's row; a cluster of 2^log2 blocks has a token, each of them `per` elements.
-template <typename T>
-__global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a, int log2, long long per)
+template <typename T, int RT>
+__global__ void __launch_bounds__(RT + 32) k_distill(const lf_distill_args a, int log2, long long per)
 {
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
     __shared__ short table[1 << DT_TABLE_LOG2];
-    __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
+    __shared__ float2 warp_ms[RT / 32];
     const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     const part_of<T> mine(z, a.vocab, part, per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
     const float c = LOG2E / a.temperature;
-    const bool row_warp = tid < DT_ROW_THREADS;
+    const bool row_warp = tid < RT;
     const entries ent(space, a.top, &facts);
     lf_grid_wait();
     lf_grid_release();
     online o;
     o.clear();
     if (row_warp) {
-        online_pieces<T>(o, 0, mine.pieces, c, [&](int i) { return ld16(from + i); });
+        online_pieces<T, RT>(o, 0, mine.pieces, c, [&](int i) { return ld16(from + i); });
         online_edge<T>(o, z, mine, c);
     } else if (part == 0) {
-        gather<T>(ent, a, token, z);
+        gather<T>(ent, a, token, z, 0, a.vocab);
         weigh(ent, a, table);
     }
     __syncwarp();
-    o.join_row(warp_ms, row_warp, parts, c);
+    o.join_row<RT>(warp_ms, row_warp, parts, c);
     if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     if (part == 0 && !row_warp) loss_of(ent, a, token, o.m, o.s);
     __syncwarp();
@@ -470,15 +480,15 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill(const lf_distill_args a,
 // some load while others add or store: 8192 x 131072 bf16 849 us, 5.06 TB/s, with six blocks to a multiprocessor (five: 938, four: 1072); persistent
 // ones with the next part on its way 1345, a row to a block that reads it again from L2 1154.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
 // the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
-template <typename T>
-__global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf_distill_args a, int log2, long long per, int staged)
+template <typename T, int RT>
+__global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_both(const lf_distill_args a, int log2, long long per, int staged)
 {
     extern __shared__ __align__(16) unsigned char space[];     // staged pieces, entries
     __shared__ entry_facts facts;
     __shared__ short table[1 << DT_TABLE_LOG2];
-    __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
+    __shared__ float2 warp_ms[RT / 32];
     const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
-    const bool row_warp = tid < DT_ROW_THREADS;
+    const bool row_warp = tid < RT;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     const part_of<T> mine(z, a.vocab, part, per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
@@ -492,17 +502,17 @@ __global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf
     o.clear();
     if (row_warp) {
         // (a thread reads what it copied itself)
-        for (int i = tid; i < kept; i += DT_ROW_THREADS) cp_async16(lfptx::smem_u32(own + i), from + i);
+        for (int i = tid; i < kept; i += RT) cp_async16(lfptx::smem_u32(own + i), from + i);
         asm volatile("cp.async.commit_group;" ::: "memory");
-        online_pieces<T>(o, kept, mine.pieces, c, [&](int i) { return ld16(from + i); });
+        online_pieces<T, RT>(o, kept, mine.pieces, c, [&](int i) { return ld16(from + i); });
         online_edge<T>(o, z, mine, c);
         asm volatile("cp.async.wait_all;" ::: "memory");
-        online_pieces<T>(o, 0, kept, c, [&](int i) { return own[i]; });
+        online_pieces<T, RT>(o, 0, kept, c, [&](int i) { return own[i]; });
     } else {
-        gather<T>(ent, a, token, z);
+        gather<T>(ent, a, token, z, part == 0 ? 0 : mine.e0, part == 0 ? a.vocab : mine.e1);       // (the first part has the loss)
     }
     __syncwarp();
-    o.join_row(warp_ms, row_warp, parts, c);                     // (every part has read the logits that its entries need)
+    o.join_row<RT>(warp_ms, row_warp, parts, c);                     // (every part has read the logits that its entries need)
     if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
     const float w = a.weight ? a.weight[token] : 1.f, wt = w * a.temperature, m = o.m;
@@ -511,17 +521,17 @@ __global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf
         weigh(ent, a, table);
     } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
-        gradient_pieces<T, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
-        gradient_pieces<T, 1>(dz + mine.body, kept, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
+        gradient_pieces<T, RT, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
+        gradient_pieces<T, RT, 1>(dz + mine.body, kept, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
         gradient_edge<T>(dz, z, mine, m, c, f);
     } else {
-        zero_part<T>(dz, mine, aligned);
+        zero_part<T, RT>(dz, mine, aligned);
     }
     __syncthreads();
     if (row_warp) {
         if (!none) {
             const float inv_s = 1.0f / o.s;
-            put_right<T>(ent, a.top, mine.e0, mine.e1, dz, facts.bad ? CUDART_NAN_F : wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
+            put_right<T, RT>(ent, a.top, mine.e0, mine.e1, dz, facts.bad ? CUDART_NAN_F : wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
         }
     } else if (part == 0) {
         loss_of(ent, a, token, o.m, o.s);
@@ -532,31 +542,31 @@ __global__ void __launch_bounds__(DT_THREADS, DT_BLOCKS) k_distill_both(const lf
 
 // dz from z and lse: no part of a row needs to know another.  Where lse is so large that fp32 does not hold enough of
 // its fraction (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
-template <typename T>
-__global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distill_args a, int parts, long long per)
+template <typename T, int RT>
+__global__ void __launch_bounds__(RT + 32) k_distill_backward(const lf_distill_args a, int parts, long long per)
 {
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
     __shared__ short table[1 << DT_TABLE_LOG2];
-    __shared__ float2 warp_ms[DT_ROW_THREADS / 32];
+    __shared__ float2 warp_ms[RT / 32];
     const int token = blockIdx.x / parts, part = blockIdx.x - token * parts, tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     T* dz = static_cast<T*>(a.dz) + (size_t)token * a.ld_dz;
-    const bool row_warp = tid < DT_ROW_THREADS;
+    const bool row_warp = tid < RT;
     const entries ent(space, a.top, &facts);
     lf_grid_wait();
     lf_grid_release();
-    if (!row_warp) gather<T>(ent, a, token, z);
-    if (a.dz == a.z) __syncthreads();      // the entries' logits have been read
-    if (!row_warp) weigh(ent, a, table);
     const float w = a.weight ? a.weight[token] : 1.f, lse = a.lse[token], c = LOG2E / a.temperature;
     const bool large = fabsf(lse) >= DT_LARGE_LSE;
     if (large && part > 0) return;
     const part_of<T> mine(z, a.vocab, part, large ? (1ll << 40) : per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
+    if (!row_warp) gather<T>(ent, a, token, z, mine.e0, mine.e1);
+    if (a.dz == a.z) __syncthreads();      // the entries' logits have been read
+    if (!row_warp) weigh(ent, a, table);
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
     if (w == 0.f) {
-        if (row_warp) zero_part<T>(dz, mine, aligned);
+        if (row_warp) zero_part<T, RT>(dz, mine, aligned);
         return;
     }
     const float wt = w * a.temperature;
@@ -565,24 +575,24 @@ __global__ void __launch_bounds__(DT_THREADS) k_distill_backward(const lf_distil
         online o;
         o.clear();
         if (row_warp) {
-            online_pieces<T>(o, 0, mine.pieces, c, [&](int i) { return ld16(from + i); });
+            online_pieces<T, RT>(o, 0, mine.pieces, c, [&](int i) { return ld16(from + i); });
             online_edge<T>(o, z, mine, c);
         }
         __syncwarp();
-        o.join_row(warp_ms, row_warp, 1, c);
+        o.join_row<RT>(warp_ms, row_warp, 1, c);
         m = o.m;
         scale = 1.0f / o.s;
     }
     const float f = wt * scale;
     if (row_warp) {
-        gradient_pieces<T, DT_UNROLL>(dz + mine.body, 0, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
+        gradient_pieces<T, RT, DT_UNROLL>(dz + mine.body, 0, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
         gradient_edge<T>(dz, z, mine, m, c, f);
     }
     __syncthreads();
     if (!row_warp) return;
-    if (!facts.any) zero_part<T>(dz, mine, aligned);               // (rare: what was written is written again)
-    else if (facts.bad) fill_part<T>(dz, mine, CUDART_NAN_F, aligned);
-    else put_right<T>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
+    if (!facts.any) zero_part<T, RT>(dz, mine, aligned);               // (rare: what was written is written again)
+    else if (facts.bad) fill_part<T, RT>(dz, mine, CUDART_NAN_F, aligned);
+    else put_right<T, RT>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
 }
 
 // elements of a part, whole pieces
@@ -606,12 +616,18 @@ template <typename T>
 cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
 {
     const int log2 = parts_log2(a, sm_count, a.dz ? DT_PART_BYTES : 1ll << 40), parts = 1 << log2;
+    const long long row = (long long)a.vocab * (long long)sizeof(T);
+    const bool brief = log2 == 0 && (row <= DT_SHORT_BYTES || (a.tokens >= 8 * sm_count && row <= DT_SHORT_BYTES / 2 * (a.dz ? 3 : 4)));
     const dim3 grid((unsigned)((long long)a.tokens << log2));
     const long long per = per_part<T>(a, parts);
-    if (!a.dz) return lf_launch_clusters(k_distill<T>, grid, DT_THREADS, entries::bytes(a.top), parts, s, a, log2, per);
+    if (!a.dz)
+        return brief ? lf_launch(k_distill<T, DT_SHORT>, grid, DT_SHORT + 32, entries::bytes(a.top), s, a, log2, per)
+                     : lf_launch_clusters(k_distill<T, DT_LONG>, grid, DT_LONG + 32, entries::bytes(a.top), parts, s, a, log2, per);
     const long long bytes = per * (long long)sizeof(T);
     const int staged = (int)((bytes < DT_STAGE_BYTES ? bytes : DT_STAGE_BYTES) / 16);
-    return lf_launch_clusters(k_distill_both<T>, grid, DT_THREADS, (size_t)staged * 16 + entries::bytes(a.top), parts, s, a, log2, per, staged);
+    const size_t smem = (size_t)staged * 16 + entries::bytes(a.top);
+    return brief ? lf_launch(k_distill_both<T, DT_SHORT>, grid, DT_SHORT + 32, smem, s, a, log2, per, staged)
+                 : lf_launch_clusters(k_distill_both<T, DT_LONG>, grid, DT_LONG + 32, smem, parts, s, a, log2, per, staged);
 }
 template <typename T>
 cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
@@ -619,12 +635,15 @@ cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStre
     const long long bytes = (long long)a.vocab * sizeof(T);
     long long parts = (bytes + 65535) / 65536;                    // (16 pieces a thread)
     while ((long long)a.tokens * parts < 2 * sm_count && bytes / parts > 4096) parts *= 2;
-    return lf_launch(k_distill_backward<T>, dim3((unsigned)((long long)a.tokens * parts)), DT_THREADS, entries::bytes(a.top), s, a, (int)parts, per_part<T>(a, parts));
+    const dim3 grid((unsigned)((long long)a.tokens * parts));
+    return parts == 1 && (bytes <= DT_SHORT_BYTES || (a.tokens >= 8 * sm_count && bytes <= 2 * DT_SHORT_BYTES))
+               ? lf_launch(k_distill_backward<T, DT_SHORT>, grid, DT_SHORT + 32, entries::bytes(a.top), s, a, 1, per_part<T>(a, 1))
+               : lf_launch(k_distill_backward<T, DT_LONG>, grid, DT_LONG + 32, entries::bytes(a.top), s, a, (int)parts, per_part<T>(a, parts));
 }
 template <typename T>
 bool distill_ready()
 {
-    return cudaFuncSetAttribute(k_distill_both<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(DT_STAGE_BYTES + entries::bytes(LF_DISTILL_MAX_TOP))) == cudaSuccess;
+    return cudaFuncSetAttribute(k_distill_both<T, DT_LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(DT_STAGE_BYTES + entries::bytes(LF_DISTILL_MAX_TOP))) == cudaSuccess;
 }
 
 }  // namespace
