@@ -13,7 +13,7 @@
 // written too, a part keeps what it has read in shared memory, so that the row is read from memory once.
 // The teacher's entries and the loss are one warp's work, beside the others' passes over the row; the dense part of the gradient is
 // written first, then the entries that fall into the part are put right.  Measured, bf16: loss alone 8192 x 131072 327 us, 6.56 TB/s; gradient
-// alone 8192 x 32768 197 us, 5.4; both at once 8192 x 131072 849 us, 5.06 TB/s.
+// alone 8192 x 32768 167 us, 6.4; both at once 8192 x 131072 805 us, 5.34 TB/s.
 #include <math_constants.h>
 
 #include "lf_ops_internal.h"
@@ -26,6 +26,7 @@ using namespace lfrow;
 
 // Threads for a row (RT in what follows): 256, or 64 where rows are short; beside them a warp for the teacher's entries and the loss.
 constexpr int DT_LONG = 256, DT_SHORT = 64;
+constexpr int DT_GATHER = 4;                    // entries of a lane at once
 constexpr int DT_TABLE_LOG2 = 10, DT_TABLE_ROUNDS = 12;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
@@ -234,23 +235,33 @@ __device__ __forceinline__ void gather(const entries& e, const lf_distill_args& 
     const float* value = a.value + (size_t)token * a.top;
     float top = -CUDART_INF_F;
     int bad = 0, any = 0;
-    // (the list first, then the logits, several loads of each under way)
-#pragma unroll 4
-    for (int k = lane; k < a.top; k += 32) {
-        const int i = index[k];
-        const float t = value[k];
-        const bool there = i >= 0 && t != -CUDART_INF_F;
-        const bool beyond = there && i >= a.vocab;
-        bad |= beyond;
-        any |= there;
-        e.at[k] = there && !beyond ? i : -1;
-        e.t[k] = there ? t : -CUDART_INF_F;
-        if (there) top = fmaxf(top, t);
-    }
-#pragma unroll 4
-    for (int k = lane; k < a.top; k += 32) {
-        const int i = e.at[k];
-        e.z[k] = i >= e0 && i < e1 ? (float)z[i] : 0.f;
+    // (several entries of a lane at once: their places, then their logits)
+    for (int k0 = lane; k0 < a.top; k0 += 32 * DT_GATHER) {
+        int at[DT_GATHER];
+        float t[DT_GATHER], l[DT_GATHER];
+#pragma unroll
+        for (int u = 0; u < DT_GATHER; ++u) {
+            const bool in = k0 + 32 * u < a.top;
+            at[u] = in ? index[k0 + 32 * u] : -1;
+            t[u] = in ? value[k0 + 32 * u] : -CUDART_INF_F;
+        }
+#pragma unroll
+        for (int u = 0; u < DT_GATHER; ++u) {
+            l[u] = at[u] >= e0 && at[u] < e1 ? (float)z[at[u]] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < DT_GATHER; ++u) {
+            const int k = k0 + 32 * u;
+            if (k >= a.top) break;
+            const bool there = at[u] >= 0 && t[u] != -CUDART_INF_F;
+            const bool beyond = there && at[u] >= a.vocab;
+            bad |= beyond;
+            any |= there;
+            e.at[k] = there && !beyond ? at[u] : -1;
+            e.t[k] = there ? t[u] : -CUDART_INF_F;
+            e.z[k] = there ? l[u] : 0.f;
+            if (there) top = fmaxf(top, t[u]);
+        }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -263,7 +274,7 @@ __device__ __forceinline__ void gather(const entries& e, const lf_distill_args& 
     }
     __syncwarp();
 }
-__device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a, short* table)
+__device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a)
 {
     const int lane = threadIdx.x & 31;
     const float inv_t = 1.0f / a.temperature, top = e.facts->top;
@@ -279,13 +290,24 @@ __device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a
     for (int k = lane; k < a.top; k += 32) e.p[k] = e.at[k] >= 0 ? e.p[k] * inv : 0.f;
     if (lane == 0) e.facts->sum = sum;
     __syncwarp();
+}
+// What the gradient needs beside, by the same warp.
+__device__ __forceinline__ void gather_totals(const entries& e, const lf_distill_args& a, short* table)
+{
+    const int lane = threadIdx.x & 31;
     // Several entries on one element: the first adds them up, in their order.  Whether there are any is found with a table: an entry
     // leaves its number at its element's place there and looks who is there then: itself, or an entry on the same element, or on another
     // one, and then it tries again with the others that did, by another multiplier.  (Every entry against every other: 102 of them took longer than a row of 5249.)
+    // (A lane each: the lanes are compared at once.)
     bool several = false;
     unsigned mult = 2654435769u;
     for (int k = lane; k < a.top; k += 32) e.total[k] = e.p[k];
-    for (int round = 0, left = 1; left && !several; ++round, mult = mult * 5u + 0x9E3779B8u) {
+    if (a.top <= 32) {
+        const int at = lane < a.top ? e.at[lane] : -1;
+        const unsigned same = __match_any_sync(0xFFFFFFFFu, at);
+        several = __any_sync(0xFFFFFFFFu, at >= 0 && (same & (same - 1)) != 0);
+    }
+    for (int round = 0, left = a.top > 32; left && !several; ++round, mult = mult * 5u + 0x9E3779B8u) {
         left = 0;
         for (int k = lane; k < a.top; k += 32)
             if (e.at[k] >= 0 && (round == 0 || e.total[k] < 0.f)) table[(mult * (unsigned)e.at[k]) >> (32 - DT_TABLE_LOG2)] = (short)k;
@@ -442,12 +464,13 @@ __device__ __forceinline__ void online_edge(online& o, const T* z, const part_of
 }
 
 // Loss and lse of a token's row; a cluster of 2^log2 blocks has a token, each of them `per` elements.
+// (Registers: left to itself the compiler takes 32 of them for long rows and has fewer loads under way: 64 x 50001 f32 7.4 us, with room for 56 6.1;
+// the short rows' blocks want to be many: 8192 x 8000 bf16 33.6 us with 56, 32.5 with 40.)
 template <typename T, int RT>
-__global__ void __launch_bounds__(RT + 32) k_distill(const lf_distill_args a, int log2, long long per)
+__global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill(const lf_distill_args a, int log2, long long per)
 {
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
-    __shared__ short table[1 << DT_TABLE_LOG2];
     __shared__ float2 warp_ms[RT / 32];
     const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
@@ -465,7 +488,7 @@ __global__ void __launch_bounds__(RT + 32) k_distill(const lf_distill_args a, in
         online_edge<T>(o, z, mine, c);
     } else if (part == 0) {
         gather<T>(ent, a, token, z, 0, a.vocab);
-        weigh(ent, a, table);
+        weigh(ent, a);
     }
     __syncwarp();
     o.join_row<RT>(warp_ms, row_warp, parts, c);
@@ -477,7 +500,7 @@ __global__ void __launch_bounds__(RT + 32) k_distill(const lf_distill_args a, in
 
 // The same and the gradient, with z read once from memory: a part of a row stays in shared memory between the sums and the
 // gradient (`staged` pieces of it; what is more, of rows beyond 8 * 32 KB, is read again).  Blocks are small and many, so that
-// some load while others add or store: 8192 x 131072 bf16 849 us, 5.06 TB/s, with six blocks to a multiprocessor (five: 938, four: 1072); persistent
+// some load while others add or store: 8192 x 131072 bf16 849 us with six blocks to a multiprocessor (five: 938, four: 1072), 805 since the lists are read several entries at once; persistent
 // ones with the next part on its way 1345, a row to a block that reads it again from L2 1154.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
 // the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
 template <typename T, int RT>
@@ -518,7 +541,8 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
     const float w = a.weight ? a.weight[token] : 1.f, wt = w * a.temperature, m = o.m;
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !facts.any;
     if (!row_warp) {
-        weigh(ent, a, table);
+        weigh(ent, a);
+        gather_totals(ent, a, table);
     } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
         gradient_pieces<T, RT, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
@@ -543,7 +567,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
 // dz from z and lse: no part of a row needs to know another.  Where lse is so large that fp32 does not hold enough of
 // its fraction (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
 template <typename T, int RT>
-__global__ void __launch_bounds__(RT + 32) k_distill_backward(const lf_distill_args a, int parts, long long per)
+__global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill_backward(const lf_distill_args a, int parts, long long per)
 {
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
@@ -563,7 +587,10 @@ __global__ void __launch_bounds__(RT + 32) k_distill_backward(const lf_distill_a
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
     if (!row_warp) gather<T>(ent, a, token, z, mine.e0, mine.e1);
     if (a.dz == a.z) __syncthreads();      // the entries' logits have been read
-    if (!row_warp) weigh(ent, a, table);
+    if (!row_warp) {
+        weigh(ent, a);
+        gather_totals(ent, a, table);
+    }
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
     if (w == 0.f) {
         if (row_warp) zero_part<T, RT>(dz, mine, aligned);
