@@ -296,6 +296,23 @@ def test_product_forms(ops, M, N, K, kw):
     _product(ops, M, N, K, F16, False, **kw)
 
 
+@pytest.mark.parametrize("tiles", [True, False])
+@pytest.mark.parametrize("M,N,K", [(5, 520, 1200), (16, 4104, 200), (100, 520, 4104), (200, 1032, 200), (2100, 2056, 200), (0, 8, 8), (40, 16, 0)])
+def test_product_adds_in_place(ops, M, N, K, tiles):
+    """`add` may be the very matrix that the result goes to: the bits of a call with one of its own."""
+    g = _gen(M + N + K)
+    for dtype in (BF16, F16):
+        qa, sa, qb, sb = _operands(g, M, N, K, tiles and K > 0)
+        add, d, own = Out(M, N, dtype, N + 16), Out(M, N, dtype, N + 16), Out(M, N, dtype, N + 16)
+        add.t.copy_(_rand(g, M, N, std=10.0))
+        own.t.copy_(add.t)
+        ops.product_blocks(qa.t, sa, qb.t, sb, d.t, add=add.t)
+        ops.product_blocks(qa.t, sa, qb.t, sb, own.t, add=own.t)
+        ops.sync()
+        own.check()
+        assert torch.equal(own.t, d.t) and bool((own.t != add.t).any()) == (M > 0 and K > 0)
+
+
 @pytest.mark.parametrize("M", [3, 40])
 def test_product_of_nothing(ops, M):
     for dtype in DTYPES:
@@ -622,6 +639,34 @@ def test_captured_and_replayed_on_another_stream():
             for k in keys:
                 assert torch.equal(b[k], want[seed - 1][k]), (seed, k)
         del graph
+
+
+def test_two_handles_at_once():
+    """Two handles on two streams, each with a workspace of its own, their kernels side by side: the bits of one after the other."""
+    cases = [(16, 1032, 4104, 40), (300, 2056, 3000, 64)]
+    with lf.Operators() as plain:
+        want = []
+        for sizes in cases:
+            b = _buffers(*sizes)
+            _run_all(plain, *sizes, b)
+            plain.sync()
+            want.append({k: v.clone() for k, v in b.items()})
+    streams = [torch.cuda.Stream() for _ in cases]
+    handles = [lf.Operators(stream=s.cuda_stream) for s in streams]
+    try:
+        bufs = [_buffers(*sizes) for sizes in cases]
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for ops, sizes, b in zip(handles, cases, bufs):
+                _run_all(ops, *sizes, b)
+        for ops in handles:
+            ops.sync()
+        for b, w in zip(bufs, want):
+            for k in ("h", "y", "z", "loss", "lse", "dz", "dy", "gw", "dh", "dg", "db"):
+                assert torch.equal(b[k], w[k]), k
+    finally:
+        for ops in handles:
+            ops.close()
 
 
 def test_results_do_not_depend_on_timing(ops):
