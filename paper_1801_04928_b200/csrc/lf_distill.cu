@@ -13,7 +13,9 @@
 // written too, a part keeps what it has read in shared memory, so that the row is read from memory once.
 // The teacher's entries and the loss are one warp's work, beside the others' passes over the row; the dense part of the gradient is
 // written first, then the entries that fall into the part are put right.  Measured, bf16: loss alone 8192 x 131072 327 us, 6.56 TB/s; gradient
-// alone 8192 x 32768 167 us, 6.4; both at once 8192 x 131072 805 us, 5.34 TB/s.
+// alone 8192 x 32768 167 us, 6.4; both at once 8192 x 131072 with 64 entries a token 815 us, 5.27 TB/s.
+#include <algorithm>
+
 #include <math_constants.h>
 
 #include "lf_ops_internal.h"
@@ -26,7 +28,6 @@ using namespace lfrow;
 
 // Threads for a row (RT in what follows): 256, or 64 where rows are short; beside them a warp for the teacher's entries and the loss.
 constexpr int DT_LONG = 256, DT_SHORT = 64;
-constexpr int DT_GATHER = 4;                    // entries of a lane at once
 constexpr int DT_TABLE_LOG2 = 10, DT_TABLE_ROUNDS = 12;
 constexpr int DT_UNROLL = 4;                    // pieces of 16 bytes that a thread has in flight
 constexpr int DT_MAX_PARTS = 8;                 // blocks of a cluster
@@ -37,6 +38,7 @@ constexpr float DT_LARGE_LSE = 1024.f;          // from here on lse in fp32 is o
 constexpr int DT_SHORT_BYTES = 16 * 1024;
 constexpr int DT_PART_BYTES = 32 * 1024;        // of a row that a block of the joint kernel has, where eight parts are enough
 constexpr int DT_STAGE_BYTES = DT_PART_BYTES;   // at most of a part that stays in shared memory
+constexpr int DT_ROOM_BYTES = 227 * 1024 / 6 - 1024 - 2304;    // of shared memory for a block of six, beside its variables and what every block takes
 
 // ---- 16 bytes of a row -------------------------------------------------------------------------------
 template <typename T>
@@ -208,15 +210,17 @@ struct entry_facts {                   // of a token's entries
     double sum;                        // P
     float top;                         // t_m
     int any, bad;                      // entries at all; an index beyond the vocabulary
+    int mine;                          // entries in this part of the row
 };
 struct entries {                       // the teacher's, of one token
     int* at;                           // -1: not there
     float* p;                          // 0: not there
     float* t;                          // the teacher's logit
     float* z;                          // the student's
-    float* total;                      // of the first entry on an element: what all of them have; of others < 0
+    float* total;                      // of the first of this part's entries on an element: what all of them have; of others < 0
+    short* mine;                       // this part's entries, in their order
     entry_facts* facts;
-    __host__ __device__ static constexpr size_t bytes(int top) { return (size_t)top * 20; }
+    __host__ __device__ static constexpr size_t bytes(int top) { return (size_t)top * 22; }
     __device__ __forceinline__ entries(void* space, int top, entry_facts* f) : facts(f)
     {
         at = static_cast<int*>(space);
@@ -224,45 +228,56 @@ struct entries {                       // the teacher's, of one token
         t = p + top;
         z = t + top;
         total = z + top;
+        mine = reinterpret_cast<short*>(total + top);
     }
 };
-// By one warp, in two steps: what is read of the row (the logits of elements [e0, e1)), and what follows from it.  A sum over lanes adds in a fixed order.
+__device__ __forceinline__ void copy4(void* to, const void* from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(lfptx::smem_u32(to)), "l"(from) : "memory");
+}
+// whether the four bytes that an element lies in are the row's
 template <typename T>
-__device__ __forceinline__ void gather(const entries& e, const lf_distill_args& a, int token, const T* z, long long e0, long long e1)
+__device__ __forceinline__ bool in_word(const T* z, int at, int vocab)
+{
+    if (sizeof(T) == 4) return true;
+    return (reinterpret_cast<uintptr_t>(z + at) & 2) ? at > 0 : at + 1 < vocab;
+}
+// By one warp, in steps: what is read of the row (the logits of elements [e0, e1)) and which entries are of the part [p0, p1), ...
+template <typename T>
+__device__ __forceinline__ void gather(const entries& e, const lf_distill_args& a, int token, const T* z, long long e0, long long e1, long long p0, long long p1)
 {
     const int lane = threadIdx.x & 31;
     const int* index = a.index + (size_t)token * a.top;
     const float* value = a.value + (size_t)token * a.top;
     float top = -CUDART_INF_F;
-    int bad = 0, any = 0;
-    // (several entries of a lane at once: their places, then their logits)
-    for (int k0 = lane; k0 < a.top; k0 += 32 * DT_GATHER) {
-        int at[DT_GATHER];
-        float t[DT_GATHER], l[DT_GATHER];
-#pragma unroll
-        for (int u = 0; u < DT_GATHER; ++u) {
-            const bool in = k0 + 32 * u < a.top;
-            at[u] = in ? index[k0 + 32 * u] : -1;
-            t[u] = in ? value[k0 + 32 * u] : -CUDART_INF_F;
-        }
-#pragma unroll
-        for (int u = 0; u < DT_GATHER; ++u) {
-            l[u] = at[u] >= e0 && at[u] < e1 ? (float)z[at[u]] : 0.f;
-        }
-#pragma unroll
-        for (int u = 0; u < DT_GATHER; ++u) {
-            const int k = k0 + 32 * u;
-            if (k >= a.top) break;
-            const bool there = at[u] >= 0 && t[u] != -CUDART_INF_F;
-            const bool beyond = there && at[u] >= a.vocab;
-            bad |= beyond;
-            any |= there;
-            e.at[k] = there && !beyond ? at[u] : -1;
-            e.t[k] = there ? t[u] : -CUDART_INF_F;
-            e.z[k] = there ? l[u] : 0.f;
-            if (there) top = fmaxf(top, t[u]);
+    int bad = 0, any = 0, mine = 0;
+    // (copies without registers: the whole list is under way at once, then all the logits, so that its length costs no further trip to memory)
+    for (int k = lane; k < a.top; k += 32) {
+        copy4(e.at + k, index + k);
+        copy4(e.t + k, value + k);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int first = 0; first < a.top; first += 32) {
+        const int k = first + lane, at = k < a.top ? e.at[k] : -1;
+        const float t = k < a.top ? e.t[k] : -CUDART_INF_F;
+        const bool there = at >= 0 && t != -CUDART_INF_F, here = there && at >= p0 && at < p1;
+        const unsigned all_here = __ballot_sync(0xFFFFFFFFu, here);
+        if (here) e.mine[mine + __popc(all_here & ((1u << lane) - 1u))] = (short)k;
+        mine += __popc(all_here);
+        bad |= there && at >= a.vocab;
+        any |= there;
+        if (there) top = fmaxf(top, t);
+        if (k < a.top) {
+            if (!there) e.t[k] = -CUDART_INF_F;
+            if (there && at >= e0 && at < e1) {
+                if (in_word(z, at, a.vocab)) copy4(e.z + k, reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(z + at) & ~(uintptr_t)3));
+                else e.z[k] = (float)z[at];
+            } else {
+                e.z[k] = 0.f;
+            }
         }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     bad = __any_sync(0xFFFFFFFFu, bad);
@@ -271,50 +286,66 @@ __device__ __forceinline__ void gather(const entries& e, const lf_distill_args& 
         e.facts->any = any;
         e.facts->bad = bad;
         e.facts->top = top;
+        e.facts->mine = mine;
     }
     __syncwarp();
 }
-__device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a)
+// ... the weights (a sum over lanes adds in a fixed order) and, where four bytes hold two logits, the one that is meant, ...
+template <typename T>
+__device__ __forceinline__ void weigh(const entries& e, const lf_distill_args& a, const T* z, long long e0, long long e1)
 {
     const int lane = threadIdx.x & 31;
     const float inv_t = 1.0f / a.temperature, top = e.facts->top;
     double sum = 0.0;
+#pragma unroll 4
     for (int k = lane; k < a.top; k += 32) {
         const float p = e.t[k] != -CUDART_INF_F ? expf((e.t[k] - top) * inv_t) : 0.f;
         sum += (double)p;
         e.p[k] = p;
+        if constexpr (sizeof(T) == 2) {
+            const int at = e.at[k];
+            if (at >= e0 && at < e1 && e.t[k] != -CUDART_INF_F && in_word(z, at, a.vocab)) {
+                const float2 f = unpack2(__float_as_uint(e.z[k]), T());
+                e.z[k] = (reinterpret_cast<uintptr_t>(z + at) & 2) ? f.y : f.x;
+            }
+        }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
     const float inv = 1.0f / (float)sum;
-    for (int k = lane; k < a.top; k += 32) e.p[k] = e.at[k] >= 0 ? e.p[k] * inv : 0.f;
+#pragma unroll 4
+    for (int k = lane; k < a.top; k += 32) e.p[k] *= inv;
     if (lane == 0) e.facts->sum = sum;
     __syncwarp();
 }
-// What the gradient needs beside, by the same warp.
-__device__ __forceinline__ void gather_totals(const entries& e, const lf_distill_args& a, short* table)
+// ... and what each element of the part has of them, for the gradient.
+__device__ __forceinline__ void gather_totals(const entries& e, short* table)
 {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, mine = e.facts->mine;
     // Several entries on one element: the first adds them up, in their order.  Whether there are any is found with a table: an entry
     // leaves its number at its element's place there and looks who is there then: itself, or an entry on the same element, or on another
     // one, and then it tries again with the others that did, by another multiplier.  (Every entry against every other: 102 of them took longer than a row of 5249.)
     // (A lane each: the lanes are compared at once.)
     bool several = false;
     unsigned mult = 2654435769u;
-    for (int k = lane; k < a.top; k += 32) e.total[k] = e.p[k];
-    if (a.top <= 32) {
-        const int at = lane < a.top ? e.at[lane] : -1;
+    for (int i = lane; i < mine; i += 32) e.total[e.mine[i]] = e.p[e.mine[i]];
+    if (mine <= 32) {
+        const int at = lane < mine ? e.at[e.mine[lane]] : -1;
         const unsigned same = __match_any_sync(0xFFFFFFFFu, at);
         several = __any_sync(0xFFFFFFFFu, at >= 0 && (same & (same - 1)) != 0);
     }
-    for (int round = 0, left = a.top > 32; left && !several; ++round, mult = mult * 5u + 0x9E3779B8u) {
+    for (int round = 0, left = mine > 32; left && !several; ++round, mult = mult * 5u + 0x9E3779B8u) {
         left = 0;
-        for (int k = lane; k < a.top; k += 32)
-            if (e.at[k] >= 0 && (round == 0 || e.total[k] < 0.f)) table[(mult * (unsigned)e.at[k]) >> (32 - DT_TABLE_LOG2)] = (short)k;
+#pragma unroll 2
+        for (int i = lane; i < mine; i += 32) {
+            const int k = e.mine[i];
+            if (round == 0 || e.total[k] < 0.f) table[(mult * (unsigned)e.at[k]) >> (32 - DT_TABLE_LOG2)] = (short)k;
+        }
         __syncwarp();
-        for (int k = lane; k < a.top; k += 32) {
-            const int at = e.at[k];
-            if (at < 0 || (round > 0 && !(e.total[k] < 0.f))) continue;
+#pragma unroll 2
+        for (int i = lane; i < mine; i += 32) {
+            const int k = e.mine[i], at = e.at[k];
+            if (round > 0 && !(e.total[k] < 0.f)) continue;
             const int there = table[(mult * (unsigned)at) >> (32 - DT_TABLE_LOG2)];
             const bool again = there != k && e.at[there] != at;
             several |= there != k && !again;
@@ -326,15 +357,17 @@ __device__ __forceinline__ void gather_totals(const entries& e, const lf_distill
         __syncwarp();
     }
     if (!several) return;
-    for (int k = lane; k < a.top; k += 32) {
-        const int at = e.at[k];
-        bool first = at >= 0;
+    for (int i = lane; i < mine; i += 32) {
+        const int k = e.mine[i], at = e.at[k];
+        bool first = true;
         float total = 0.f;
-        for (int j = 0; j < a.top; ++j)
+        for (int o = 0; o < mine; ++o) {
+            const int j = e.mine[o];
             if (e.at[j] == at) {
                 total += e.p[j];
                 first &= j >= k;
             }
+        }
         e.total[k] = first ? total : -1.f;
     }
 }
@@ -357,12 +390,13 @@ __device__ __forceinline__ void loss_of(const entries& e, const lf_distill_args&
 }
 // By the row's threads: dz of the entries that fall on elements [e0, e1)
 template <typename T, int RT, typename F>
-__device__ __forceinline__ void put_right(const entries& e, int top, long long e0, long long e1, T* dz, float wt, F q_of)
+__device__ __forceinline__ void put_right(const entries& e, T* dz, float wt, F q_of)
 {
-    for (int k = threadIdx.x; k < top; k += RT) {
-        const int at = e.at[k];
+    const int mine = e.facts->mine;
+    for (int i = threadIdx.x; i < mine; i += RT) {
+        const int k = e.mine[i];
         // (NaN, the weight of a list that holds one, is no number below zero)
-        if (at >= e0 && at < e1 && !(e.total[k] < 0.f)) dz[at] = (T)(wt * (q_of(e.z[k]) - e.total[k]));
+        if (!(e.total[k] < 0.f)) dz[e.at[k]] = (T)(wt * (q_of(e.z[k]) - e.total[k]));
     }
 }
 template <typename T>
@@ -487,8 +521,8 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill(con
         online_pieces<T, RT>(o, 0, mine.pieces, c, [&](int i) { return ld16(from + i); });
         online_edge<T>(o, z, mine, c);
     } else if (part == 0) {
-        gather<T>(ent, a, token, z, 0, a.vocab);
-        weigh(ent, a);
+        gather<T>(ent, a, token, z, 0, a.vocab, 0, 0);
+        weigh<T>(ent, a, z, 0, a.vocab);
     }
     __syncwarp();
     o.join_row<RT>(warp_ms, row_warp, parts, c);
@@ -500,7 +534,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill(con
 
 // The same and the gradient, with z read once from memory: a part of a row stays in shared memory between the sums and the
 // gradient (`staged` pieces of it; what is more, of rows beyond 8 * 32 KB, is read again).  Blocks are small and many, so that
-// some load while others add or store: 8192 x 131072 bf16 849 us with six blocks to a multiprocessor (five: 938, four: 1072), 805 since the lists are read several entries at once; persistent
+// some load while others add or store: 8192 x 131072 bf16 849 us with six blocks to a multiprocessor (five: 938, four: 1072), 815 since a part looks after its own entries only; persistent
 // ones with the next part on its way 1345, a row to a block that reads it again from L2 1154.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
 // the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
 template <typename T, int RT>
@@ -532,7 +566,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
         asm volatile("cp.async.wait_all;" ::: "memory");
         online_pieces<T, RT>(o, 0, kept, c, [&](int i) { return own[i]; });
     } else {
-        gather<T>(ent, a, token, z, part == 0 ? 0 : mine.e0, part == 0 ? a.vocab : mine.e1);       // (the first part has the loss)
+        gather<T>(ent, a, token, z, part == 0 ? 0 : mine.e0, part == 0 ? a.vocab : mine.e1, mine.e0, mine.e1);       // (the first part has the loss)
     }
     __syncwarp();
     o.join_row<RT>(warp_ms, row_warp, parts, c);                     // (every part has read the logits that its entries need)
@@ -541,8 +575,8 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
     const float w = a.weight ? a.weight[token] : 1.f, wt = w * a.temperature, m = o.m;
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !facts.any;
     if (!row_warp) {
-        weigh(ent, a);
-        gather_totals(ent, a, table);
+        weigh<T>(ent, a, z, part == 0 ? 0 : mine.e0, part == 0 ? a.vocab : mine.e1);
+        gather_totals(ent, table);
     } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
         gradient_pieces<T, RT, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
@@ -555,7 +589,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
     if (row_warp) {
         if (!none) {
             const float inv_s = 1.0f / o.s;
-            put_right<T, RT>(ent, a.top, mine.e0, mine.e1, dz, facts.bad ? CUDART_NAN_F : wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
+            put_right<T, RT>(ent, dz, facts.bad ? CUDART_NAN_F : wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
         }
     } else if (part == 0) {
         loss_of(ent, a, token, o.m, o.s);
@@ -585,11 +619,11 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill_bac
     if (large && part > 0) return;
     const part_of<T> mine(z, a.vocab, part, large ? (1ll << 40) : per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-    if (!row_warp) gather<T>(ent, a, token, z, mine.e0, mine.e1);
+    if (!row_warp) gather<T>(ent, a, token, z, mine.e0, mine.e1, mine.e0, mine.e1);
     if (a.dz == a.z) __syncthreads();      // the entries' logits have been read
     if (!row_warp) {
-        weigh(ent, a);
-        gather_totals(ent, a, table);
+        weigh<T>(ent, a, z, mine.e0, mine.e1);
+        gather_totals(ent, table);
     }
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0;
     if (w == 0.f) {
@@ -619,7 +653,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill_bac
     if (!row_warp) return;
     if (!facts.any) zero_part<T, RT>(dz, mine, aligned);               // (rare: what was written is written again)
     else if (facts.bad) fill_part<T, RT>(dz, mine, CUDART_NAN_F, aligned);
-    else put_right<T, RT>(ent, a.top, mine.e0, mine.e1, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
+    else put_right<T, RT>(ent, dz, wt, [&](float zk) { return scale * ex2((zk - m) * c); });
 }
 
 // elements of a part, whole pieces
@@ -651,7 +685,9 @@ cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
         return brief ? lf_launch(k_distill<T, DT_SHORT>, grid, DT_SHORT + 32, entries::bytes(a.top), s, a, log2, per)
                      : lf_launch_clusters(k_distill<T, DT_LONG>, grid, DT_LONG + 32, entries::bytes(a.top), parts, s, a, log2, per);
     const long long bytes = per * (long long)sizeof(T);
-    const int staged = (int)((bytes < DT_STAGE_BYTES ? bytes : DT_STAGE_BYTES) / 16);
+    // (long lists take room from the row, not from the six blocks: 8192 x 131072 with 300 entries 1257 us when they did)
+    const long long most = brief ? DT_STAGE_BYTES : std::min((long long)DT_STAGE_BYTES, (DT_ROOM_BYTES - (long long)entries::bytes(a.top)) / 16 * 16);
+    const int staged = (int)((bytes < most ? bytes : most) / 16);
     const size_t smem = (size_t)staged * 16 + entries::bytes(a.top);
     return brief ? lf_launch(k_distill_both<T, DT_SHORT>, grid, DT_SHORT + 32, smem, s, a, log2, per, staged)
                  : lf_launch_clusters(k_distill_both<T, DT_LONG>, grid, DT_LONG + 32, smem, parts, s, a, log2, per, staged);
