@@ -242,7 +242,8 @@ __device__ __forceinline__ bool in_word(const T* z, int at, int vocab)
     if (sizeof(T) == 4) return true;
     return (reinterpret_cast<uintptr_t>(z + at) & 2) ? at > 0 : at + 1 < vocab;
 }
-// By one warp, in steps: what is read of the row (the logits of elements [e0, e1)) and which entries are of the part [p0, p1), ...
+// By one warp, in steps: what is read of the row (the logits of elements [e0, e1); of 16-bit ones the four bytes that they lie in, where the row has both
+// halves) and which entries are of the part [p0, p1), ...
 template <typename T>
 __device__ __forceinline__ void gather(const entries& e, const lf_distill_args& a, int token, const T* z, long long e0, long long e1, long long p0, long long p1)
 {
@@ -325,11 +326,10 @@ __device__ __forceinline__ void gather_totals(const entries& e, short* table)
     // Several entries on one element: the first adds them up, in their order.  Whether there are any is found with a table: an entry
     // leaves its number at its element's place there and looks who is there then: itself, or an entry on the same element, or on another
     // one, and then it tries again with the others that did, by another multiplier.  (Every entry against every other: 102 of them took longer than a row of 5249.)
-    // (A lane each: the lanes are compared at once.)
     bool several = false;
     unsigned mult = 2654435769u;
     for (int i = lane; i < mine; i += 32) e.total[e.mine[i]] = e.p[e.mine[i]];
-    if (mine <= 32) {
+    if (mine <= 32) {                      // a lane each, compared at once
         const int at = lane < mine ? e.at[e.mine[lane]] : -1;
         const unsigned same = __match_any_sync(0xFFFFFFFFu, at);
         several = __any_sync(0xFFFFFFFFu, at >= 0 && (same & (same - 1)) != 0);
