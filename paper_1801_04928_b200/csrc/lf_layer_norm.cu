@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_layer_norm_backward(const lf_l
         else if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
-        const float2 mr = f2(-mean * r), rr = f2(r);         // c = h r - m r
+        const float2 minus_m = f2(-mean), rr = f2(r);        // c = (h - m) r: the difference first (h r - m r cancels where the mean is larger than the deviation)
         float2 su2 = f2(0.f), sc2 = f2(0.f);
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_layer_norm_backward(const lf_l
             for (int k = 0; k < 8; k += 2) {
                 const float2 u = mul2(make_float2(gn[k], gn[k + 1]), make_float2(y[k], y[k + 1]));
                 su2 = add2(su2, u);
-                sc2 = fma2(u, fma2(make_float2(h[k], h[k + 1]), rr, mr), sc2);
+                sc2 = fma2(u, mul2(add2(make_float2(h[k], h[k + 1]), minus_m), rr), sc2);
             }
         }
         float su = su2.x + su2.y, sc = sc2.x + sc2.y;
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(TPR * GROUPS) k_layer_norm_backward(const lf_l
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
                 const float2 yk = make_float2(y[k], y[k + 1]);
-                const float2 c = fma2(make_float2(h[k], h[k + 1]), rr, mr);
+                const float2 c = mul2(add2(make_float2(h[k], h[k + 1]), minus_m), rr);
                 dg[j][k / 2] = fma2(yk, c, dg[j][k / 2]);
                 db[j][k / 2] = add2(yk, db[j][k / 2]);
                 const float2 in = fma2(c, mc, fma2(make_float2(gn[k], gn[k + 1]), yk, mu));       // u - mean u - c mean(u c)

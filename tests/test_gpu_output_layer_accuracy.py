@@ -1,0 +1,72 @@
+"""Accuracy of layer norm's gradient and of the loss against a teacher where means, offsets and low temperatures make fp32 numbers
+cancel: bounds that a form which subtracts first keeps, and one that subtracts rounded products or logarithms does not."""
+import math
+
+import pytest
+import torch
+
+import operators_ref as R
+import output_layer_ref as O
+import paper_1801_04928_b200 as lf
+from test_gpu_operators import Out, _gen, _rand
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+DTYPES = [F32, BF16, F16]
+U = O.U
+
+
+@pytest.fixture(scope="module")
+def ops():
+    with lf.Operators() as o:
+        yield o
+
+
+# ---- the norm's gradient --------------------------------------------------------------------------------
+
+def _norm_backward(ops, dy, h, gain, mean, rstd):
+    """Results and bounds.  c = (h - m) r is a difference and a product: two roundings of c itself, whatever the mean.  Sums of a row are
+    64 additions in a row at most, of a column a hundredth of the rows and 64."""
+    M, n = h.shape
+    dh, dg, db = Out(M, n, h.dtype), Out(1, n, F32), Out(1, n, F32)
+    ops.layer_norm_backward(dy, h, gain, mean, rstd, dh.t, dg.t, db.t)
+    ops.sync()
+    for o in (dh, dg, db):
+        o.check()
+    (rh, rg, rb), _ = O.layer_norm_backward(dy, h, gain, mean, rstd)
+    u, r = dy.to(R.D) * gain.to(R.D), rstd.to(R.D)[:, None]
+    c = (h.to(R.D) - mean.to(R.D)[:, None]) * r
+    mu, mc = u.mean(1, keepdim=True), (u * c).mean(1, keepdim=True)
+    c_err = 2.001 * U * c.abs()
+    mu_err = 66 * U * u.abs().mean(1, keepdim=True)
+    mc_err = 66 * U * (u * c).abs().mean(1, keepdim=True) + (u.abs() * c_err).mean(1, keepdim=True)
+    dh_err = r * (4 * U * (u.abs() + mu.abs() + (c * mc).abs()) + mu_err + c.abs() * mc_err + c_err * mc.abs())
+    adds = (M / 100 + 64) * U
+    dg_err = adds * (dy.to(R.D) * c).abs().sum(0) + (dy.abs() * c_err).sum(0)
+    R.check("dh", dh.t, rh, R.rounded(rh, h.dtype, dh_err))
+    R.check("dgain", dg.t[0], rg, R.rounded(rg, F32, dg_err))
+    R.check("dbias", db.t[0], rb, R.rounded(rb, F32, adds * dy.to(R.D).abs().sum(0)))
+    return dh.t, dg.t[0], db.t[0]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shift", [0.5, 300.0, -5000.0])
+@pytest.mark.parametrize("M,n", [(1, 8), (5, 264), (31, 1032), (17, 8192), (301, 512), (400, 2056), (299, 16384)])
+def test_norm_gradient_of_shifted_rows(ops, M, n, shift, dtype):
+    g = _gen(M + n)
+    h, dy = (_rand(g, M, n, std=2.0) + shift).to(dtype), _rand(g, M, n, std=0.1).to(dtype)
+    hd = h.to(R.D)
+    mean = hd.mean(1).float()
+    rstd = (1 / torch.sqrt(hd.var(1, unbiased=False) + 1e-5)).float()
+    _norm_backward(ops, dy, h, 1 + _rand(g, n, std=0.2), mean, rstd)
+
+
+@pytest.mark.parametrize("M,n", [(3, 264), (40, 1032), (700, 520)])
+def test_norm_gradient_of_constant_rows(ops, M, n):
+    """h - m is 0, so the gain's gradient is nothing but zeros."""
+    g = _gen(n)
+    h = torch.linspace(-1000.3, 777.7, M, device="cuda")[:, None].expand(M, n).contiguous()
+    rstd = torch.full((M,), 1e-5 ** -0.5, device="cuda")
+    _, dg, _ = _norm_backward(ops, _rand(g, M, n), h, 1 + _rand(g, n, std=0.2), h[:, 0].contiguous(), rstd)
+    assert bool((dg == 0).all())
