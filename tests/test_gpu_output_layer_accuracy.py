@@ -70,3 +70,35 @@ def test_norm_gradient_of_constant_rows(ops, M, n):
     rstd = torch.full((M,), 1e-5 ** -0.5, device="cuda")
     _, dg, _ = _norm_backward(ops, _rand(g, M, n), h, 1 + _rand(g, n, std=0.2), h[:, 0].contiguous(), rstd)
     assert bool((dg == 0).all())
+
+
+# ---- the loss -------------------------------------------------------------------------------------------
+
+def _loss(ops, z, index, value, tau, kind, weight=None):
+    """(loss, dz) by one call or by two."""
+    loss, lse, dz = Out(1, z.shape[0], F32), Out(1, z.shape[0], F32), Out(*z.shape, z.dtype)
+    given = dict(weight=weight, temperature=tau)
+    ops.distill(z, index, value, loss.t, lse.t, dz=dz.t if kind == "both" else None, **given)
+    if kind == "two calls":
+        ops.distill_backward(z, index, value, lse.t, dz.t, **given)
+    ops.sync()
+    for o in (loss, lse, dz):
+        o.check()
+    return loss.t[0], dz.t
+
+
+@pytest.mark.parametrize("kind", ["both", "two calls"])
+@pytest.mark.parametrize("V,top", [(700, 40), (40000, 40), (3001, 512)])
+@pytest.mark.parametrize("tau", [1.0, 0.5, 0.7])
+def test_weights_of_the_teacher(ops, tau, V, top, kind):
+    """Where the student gives the entries no mass at all, dz is -T p: p is rounded once, and so is the product, whatever the entries' span."""
+    g = _gen(V)
+    M = 5
+    z = torch.full((M, V), -300.0, device="cuda")
+    z[:, 3] = 0.0
+    index = torch.stack([4 + torch.randperm(V - 4, generator=g, device="cuda")[:top] for _ in range(M)]).int()
+    value = -60.0 * tau * torch.rand(M, top, generator=g, device="cuda")
+    _, dz = _loss(ops, z, index, value, tau, kind)
+    tau32 = torch.tensor(tau, dtype=F32).item()                   # T as it is handed over
+    p = torch.softmax(value.to(R.D) / tau32, 1)
+    R.check("dz", dz.gather(1, index.long()), -tau32 * p, 2.001 * U * tau32 * p + 2.0 ** -149)
