@@ -613,7 +613,8 @@ typedef struct lf_distill_args {
     const float* value;              /* [tokens][top], the teacher's logits                    */
     const float* weight;             /* [tokens] or NULL (1): the token's weight; lf_distill_backward: times the gradient of its loss */
     float* loss;                     /* [tokens]; not used by lf_distill_backward              */
-    float* lse;                      /* [tokens]; lf_distill: written, or NULL; lf_distill_backward: read */
+    float* lse;                      /* [tokens]; lf_distill: written, or NULL; lf_distill_backward: read (of 16-bit logits; its
+                                      * rounding would show in an fp32 dz, whose rows are summed again) */
     void* dz; long long ld_dz;       /* [tokens][vocab], as z; lf_distill: or NULL (gradient of the sum of the losses).  May be z itself, same stride */
 } lf_distill_args;                   /* index, value, weight, loss, lse: at the boundary of an element */
 

@@ -37,8 +37,11 @@ constexpr float DT_LARGE_LSE = 1024.f;          // from here on lse in fp32 is o
 // and 101, 8192 x 16384 131 and 114; loss 8192 x 16384 50 and 70, 400 x 30000 11.8 and 10.0; gradient 8192 x 16384 95 and 113, 8192 x 30000 190 and 167.
 constexpr int DT_SHORT_BYTES = 16 * 1024;
 constexpr int DT_PART_BYTES = 32 * 1024;        // of a row that a block of the joint kernel has, where eight parts are enough
-constexpr int DT_STAGE_BYTES = DT_PART_BYTES;   // at most of a part that stays in shared memory
-constexpr int DT_ROOM_BYTES = 227 * 1024 / 6 - 1024 - 2304;    // of shared memory for a block of six, beside its variables and what every block takes
+// The same of the gradient alone (fp32 logits), which needs no more blocks than there are multiprocessors: 64 x 50001 in four parts 7.5 us, in eight of 32 KB 10.9;
+// 1000 x 30000 43.8 and 49.5, 400 x 131072 78 and 94.
+constexpr int DT_ALONE_BYTES = 64 * 1024;
+// of shared memory for one of so many blocks, beside its variables and what every block takes
+constexpr int dt_room(int blocks) { return 227 * 1024 / blocks - 1024 - 2304; }
 
 // ---- 16 bytes of a row -------------------------------------------------------------------------------
 template <typename T>
@@ -548,8 +551,8 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill(con
     if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
 }
 
-// The same and the gradient, with z read once from memory: a part of a row stays in shared memory between the sums and the
-// gradient (`staged` pieces of it; what is more, of rows beyond 8 * 32 KB, is read again).  Blocks are small and many, so that
+// The same and the gradient, or (loss NULL) the gradient alone, with z read once from memory: a part of a row stays in shared memory between the sums and the
+// gradient (`staged` pieces of it; what is more, of rows beyond eight parts, is read again).  Blocks are small and many, so that
 // some load while others add or store: 8192 x 131072 bf16 849 us with six blocks to a multiprocessor (five: 938, four: 1072), 815 since a part looks after its own entries only; persistent
 // ones with the next part on its way 1345, a row to a block that reads it again from L2 1154.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
 // the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
@@ -561,7 +564,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
     __shared__ short table[1 << DT_TABLE_LOG2];
     __shared__ float2 warp_ms[RT / 32];
     const int parts = 1 << log2, token = blockIdx.x >> log2, part = blockIdx.x & (parts - 1), tid = threadIdx.x;
-    const bool row_warp = tid < RT;
+    const bool row_warp = tid < RT, whole = part == 0 && a.loss;      // the first part has the loss
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     const part_of<T> mine(z, a.vocab, part, per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
@@ -582,7 +585,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
         asm volatile("cp.async.wait_all;" ::: "memory");
         online_pieces<T, RT>(o, 0, kept, c, [&](int i) { return own[i]; });
     } else {
-        gather<T>(ent, a, token, z, part == 0 ? 0 : mine.e0, part == 0 ? a.vocab : mine.e1, mine.e0, mine.e1);       // (the first part has the loss)
+        gather<T>(ent, a, token, z, whole ? 0 : mine.e0, whole ? a.vocab : mine.e1, mine.e0, mine.e1);
     }
     __syncwarp();
     o.join_row<RT>(warp_ms, row_warp, parts, c);                     // (every part has read the logits that its entries need)
@@ -591,7 +594,7 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
     const float w = a.weight ? a.weight[token] : 1.f, wt = w * a.temperature, m = o.m;
     const bool aligned = (reinterpret_cast<uintptr_t>(dz + mine.body) & 15u) == 0, none = w == 0.f || !facts.any;
     if (!row_warp) {
-        weigh<T>(ent, a, z, part == 0 ? 0 : mine.e0, part == 0 ? a.vocab : mine.e1);
+        weigh<T>(ent, a, z, whole ? 0 : mine.e0, whole ? a.vocab : mine.e1);
         gather_totals(ent, table);
     } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
@@ -607,18 +610,22 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
             const float inv_s = 1.0f / o.s;
             put_right<T, RT>(ent, dz, facts.bad ? CUDART_NAN_F : wt, [&](float zk) { return inv_s * ex2((zk - m) * c); });
         }
-    } else if (part == 0) {
+    } else if (whole) {
         loss_of(ent, a, token, o.m, o.s);
     }
     __syncwarp();
     if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // nobody leaves while its sums are being read
 }
 
-// dz from z and lse: no part of a row needs to know another.  Where lse is so large that fp32 does not hold enough of
+// dz from z and lse, 16-bit logits: no part of a row needs to know another.  Where lse is so large that fp32 does not hold enough of
 // its fraction (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
+// (Of fp32 logits, lse as an fp32 number is never good enough: its rounding, 2^-24 of itself, is in every q of the row, 5e-7 for an lse of 11 and 1.5e-5 for one of
+// 260, where q is good for 1e-7.  Their maximum and sum are taken again, by k_distill_both without a loss: 8192 x 32768 352 us, from lse 328; 64 x 50001 7.6 and
+// 4.9; 2048 x 131072 373 and 324; a row that eight parts do not hold is read twice, 64 x 600001 139 and 55.)
 template <typename T, int RT>
 __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill_backward(const lf_distill_args a, int parts, long long per)
 {
+    static_assert(sizeof(T) == 2, "fp32 logits: k_distill_both");
     extern __shared__ __align__(16) unsigned char space[];
     __shared__ entry_facts facts;
     __shared__ short table[1 << DT_TABLE_LOG2];
@@ -679,20 +686,21 @@ long long per_part(const lf_distill_args& a, long long parts)
     constexpr long long N = 16 / (long long)sizeof(T);
     return ((a.vocab + parts - 1) / parts + N - 1) / N * N;
 }
-// Blocks of a cluster, as a power of two: enough to fill the device and to have `most` bytes at most, up to eight; parts of fewer than 4 KB
+// Blocks of a cluster, as a power of two: enough for `blocks` of them and to have `most` bytes at most, up to eight; parts of fewer than 4 KB
 // are not worth a meeting.
-int parts_log2(const lf_distill_args& a, int sm_count, long long most)
+int parts_log2(const lf_distill_args& a, long long blocks, long long most)
 {
     const long long bytes = (long long)a.vocab * (a.dtype == LF_F32 ? 4 : 2);
     int n = 0;
-    while ((1 << n) < DT_MAX_PARTS && (bytes >> n) > 4096 && ((bytes >> n) > most || ((long long)a.tokens << n) < 2 * sm_count)) ++n;
+    while ((1 << n) < DT_MAX_PARTS && (bytes >> n) > 4096 && ((bytes >> n) > most || ((long long)a.tokens << n) < blocks)) ++n;
     return n;
 }
 
 template <typename T>
 cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
 {
-    const int log2 = parts_log2(a, sm_count, a.dz ? DT_PART_BYTES : 1ll << 40), parts = 1 << log2;
+    const int part_bytes = a.loss ? DT_PART_BYTES : DT_ALONE_BYTES;
+    const int log2 = parts_log2(a, a.loss ? 2 * sm_count : sm_count, a.dz ? part_bytes : 1ll << 40), parts = 1 << log2;
     const long long row = (long long)a.vocab * (long long)sizeof(T);
     const bool brief = log2 == 0 && (row <= DT_SHORT_BYTES || (a.tokens >= 8 * sm_count && row <= DT_SHORT_BYTES / 2 * (a.dz ? 3 : 4)));
     const dim3 grid((unsigned)((long long)a.tokens << log2));
@@ -701,8 +709,8 @@ cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
         return brief ? lf_launch(k_distill<T, DT_SHORT>, grid, DT_SHORT + 32, entries::bytes(a.top), s, a, log2, per)
                      : lf_launch_clusters(k_distill<T, DT_LONG>, grid, DT_LONG + 32, entries::bytes(a.top), parts, s, a, log2, per);
     const long long bytes = per * (long long)sizeof(T);
-    // (long lists take room from the row, not from the six blocks: 8192 x 131072 with 300 entries 1257 us when they did)
-    const long long most = brief ? DT_STAGE_BYTES : std::min((long long)DT_STAGE_BYTES, (DT_ROOM_BYTES - (long long)entries::bytes(a.top)) / 16 * 16);
+    // (long lists take room from the row, not from the six, or alone three, blocks: 8192 x 131072 with 300 entries 1257 us when they did)
+    const long long most = brief ? part_bytes : std::min((long long)part_bytes, (dt_room(a.loss ? 6 : 3) - (long long)entries::bytes(a.top)) / 16 * 16);
     const int staged = (int)((bytes < most ? bytes : most) / 16);
     const size_t smem = (size_t)staged * 16 + entries::bytes(a.top);
     return brief ? lf_launch(k_distill_both<T, DT_SHORT>, grid, DT_SHORT + 32, smem, s, a, log2, per, staged)
@@ -722,7 +730,7 @@ cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStre
 template <typename T>
 bool distill_ready()
 {
-    return cudaFuncSetAttribute(k_distill_both<T, DT_LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(DT_STAGE_BYTES + entries::bytes(LF_DISTILL_MAX_TOP))) == cudaSuccess;
+    return cudaFuncSetAttribute(k_distill_both<T, DT_LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, dt_room(sizeof(T) == 4 ? 3 : 6)) == cudaSuccess;
 }
 
 }  // namespace
@@ -740,7 +748,11 @@ cudaError_t lfk_distill(const lf_distill_args& a, int sm_count, cudaStream_t s)
 }
 cudaError_t lfk_distill_backward(const lf_distill_args& a, int sm_count, cudaStream_t s)
 {
-    if (a.dtype == LF_F32) return distill_backward_of<float>(a, sm_count, s);
+    if (a.dtype == LF_F32) {
+        lf_distill_args alone = a;
+        alone.loss = alone.lse = nullptr;
+        return distill_of<float>(alone, sm_count, s);
+    }
     if (a.dtype == LF_BF16) return distill_backward_of<__nv_bfloat16>(a, sm_count, s);
     return distill_backward_of<__half>(a, sm_count, s);
 }

@@ -102,3 +102,34 @@ def test_weights_of_the_teacher(ops, tau, V, top, kind):
     tau32 = torch.tensor(tau, dtype=F32).item()                   # T as it is handed over
     p = torch.softmax(value.to(R.D) / tau32, 1)
     R.check("dz", dz.gather(1, index.long()), -tau32 * p, 2.001 * U * tau32 * p + 2.0 ** -149)
+
+
+def _student(g, M, V, std):
+    return _rand(g, M, V, std=std)
+
+
+@pytest.mark.parametrize("kind", ["both", "two calls"])
+@pytest.mark.parametrize("M,V", [(16, 1000), (12, 5000), (10, 20001), (9, 50001), (9, 131072), (300, 9000)])
+@pytest.mark.parametrize("tau,shift", [(1.0, 0.0), (1.0, 60.0), (1.0, -250.0), (1.0, 900.0), (0.05, 30.0), (3.0, 5000.0)])
+def test_gradient_of_shifted_logits(ops, M, V, tau, shift, kind):
+    """An offset of a row changes nothing: q is as good as its largest logit and the sum of the differences' exponentials are, however large
+    lse is, whose rounding to fp32 alone would be 2^-24 |lse|."""
+    g = _gen(V)
+    z = _student(g, M, V, 2.0 * tau) + shift
+    index = torch.randint(0, V, (M, 3), generator=g, device="cuda").int()
+    value = _rand(g, M, 3) * tau
+    _, dz = _loss(ops, z, index, value, tau, kind)
+    tau32 = torch.tensor(tau, dtype=F32).item()
+    x = z.to(R.D) / tau32
+    d = x.amax(1, keepdim=True) - x
+    q = torch.softmax(x, 1)
+    p = torch.softmax(value.to(R.D) / tau32, 1)
+    mass = torch.zeros_like(q).scatter_add_(1, index.long(), p)
+    ref = tau32 * (q - mass)
+    # e^((z - m) / T): the difference, log2(e) / T (2 U) and their product, and 4 U of the function
+    e_err = 4 * U * d + 4 * U
+    # the sum: of a thread at most seven times 16 terms, seven additions and a change of the maximum each (4 U and once more the terms' own), then 13 over
+    # lanes, warps and parts with two more changes
+    s_err = (q * (2 * e_err)).sum(1, keepdim=True) + (7 * 7 + 13 + 9 * 4) * U
+    err = tau32 * (q * (e_err + s_err + 4 * U) + mass * 4 * U) + 3 * U * ref.abs() + 2.0 ** -120
+    R.check("dz", dz, ref, err)
