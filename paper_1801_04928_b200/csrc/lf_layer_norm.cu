@@ -421,7 +421,7 @@ template <typename T, bool TILES, bool TURN>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_pack_blocks(const lf_pack_blocks_args a)
 {
     typedef magnitudes<T> mags;
-    __shared__ unsigned col_max[TURN || TILES ? 8 : 1][TURN || TILES ? 16 * mags::N : 1];
+    __shared__ __align__(16) unsigned col_max[TURN || TILES ? 8 : 1][TURN || TILES ? 16 * mags::N : 1];
     __shared__ __align__(16) unsigned char turned[TURN ? 128 * 128 : 16];
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, warp = threadIdx.x >> 5;
     const unsigned nbx = ((unsigned)a.n + 127) / 128, nby = ((unsigned)a.tokens + 127) / 128;

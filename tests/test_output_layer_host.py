@@ -4,6 +4,7 @@ handles and arguments answer with an error code, tensors that do not fit are ref
 import ctypes
 import math
 import os
+import re
 import subprocess
 
 import pytest
@@ -116,3 +117,22 @@ def test_reference_of_the_norm_gradient():
     got, _ = O.layer_norm_backward(dy, h, gain, m[:, 0], r[:, 0])
     for a, b in zip(got, want):
         assert (a - b).abs().max() < 1e-12
+
+
+def test_shared_arrays_that_are_read_in_vectors_are_aligned():
+    """An array in shared memory promises its element's alignment and no more: one that is accessed 8 or 16 bytes at a time says so."""
+    wide = {"uint4": 16, "int4": 16, "float4": 16, "uint2": 8, "int2": 8, "float2": 8}
+    own = {"float4": 16, "uint4": 16, "float2": 8, "uint2": 8, "unsigned long long": 8, "double": 8}
+    csrc, seen = os.path.join(ROOT, "paper_1801_04928_b200", "csrc"), 0
+    for name in sorted(os.listdir(csrc)):
+        text = open(os.path.join(csrc, name)).read()
+        # a name may be declared in several kernels: the least promise of a file counts
+        promised = {}
+        for align, kind, array in re.findall(r"__shared__\s+(?:__align__\((\d+)\)\s+)?((?:unsigned long long|unsigned char|\w+))\s+(\w+)\[", text):
+            has = max(int(align or 1), own.get(kind, 4 if kind in ("float", "int", "unsigned") else 1))
+            promised[array] = min(has, promised.get(array, 1024))
+        for kind, array in re.findall(r"reinterpret_cast<(?:const\s+)?(\w+)\s*\*>\(\s*&?(\w+)", text):
+            if kind in wide and array in promised:
+                seen += 1
+                assert promised[array] >= wide[kind], f"{name}: {array} promises {promised[array]} bytes and is accessed as {kind}"
+    assert seen >= 5
