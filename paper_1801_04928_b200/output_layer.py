@@ -24,6 +24,10 @@ def blocks(n: int) -> int:
     return (n + 127) // 128
 
 
+def pitch(n: int) -> int:
+    return (n + 15) // 16 * 16
+
+
 class OutputLayer:
     """Weights, gradients and the buffers of one layer for at most `tokens` tokens.  `width` and `vocab`: multiples of 8."""
 
@@ -35,7 +39,7 @@ class OutputLayer:
             return torch.empty(shape, dtype=dt, device=device)
 
         def packed(rows, n):                                 # e4m3 rows begin on 16-byte boundaries
-            return new(rows, (n + 15) // 16 * 16, dt=torch.uint8)[:, :n]
+            return new(rows * pitch(n), dt=torch.uint8).view(rows, pitch(n))[:, :n]
 
         f32 = torch.float32
         self.ops, self.dtype, self.width, self.vocab = ops, dtype, width, vocab
@@ -48,40 +52,52 @@ class OutputLayer:
         # what the forward pass keeps: h, its statistics and u
         self.h, self.u, self.du = new(tokens, width), new(tokens, width), new(tokens, width)
         self.mean, self.rstd = new(tokens, dt=f32), new(tokens, dt=f32)
-        self._packed, self._scales = packed, lambda *shape: new(*shape, dt=f32)
-        self._forms = {}
+        # the 8-bit forms of u and of the logits' gradient: storage for all `tokens`, which smaller batches have a part of
+        self.tokens, self._new, self._storage, self._views = tokens, new, {}, {}
 
     def refresh(self):
         self.ops.pack_tiles(self.master["w"], **self.w)
 
-    def forms(self, m: int):
-        """8-bit buffers for m tokens (scales are [blocks, m], so they go by the number)."""
-        if m not in self._forms:
-            p, s, n, v = self._packed, self._scales, self.width, self.vocab
-            self._forms[m] = dict(u=dict(q=p(m, n), s=s(blocks(n), m), qt=p(n, m), st=s(blocks(m), n)),
-                                  dz=dict(q=p(m, v), s=s(blocks(v), m), qt=p(v, m), st=s(blocks(m), v)))
-        return self._forms[m]
+    def _cut(self, name: str, m: int, n: int):
+        """An [m, n] matrix in 8 bits, as it lies (q, s) or, where the name ends in t, transposed (qt, st), in the storage of that name."""
+        turned, most = name.endswith("t"), self.tokens
+        if name not in self._storage:
+            self._storage[name] = (self._new(n * pitch(most) if turned else most * pitch(n), dt=torch.uint8),
+                                   self._new(blocks(most) * n if turned else blocks(n) * most, dt=torch.float32))
+        q, s = self._storage[name]
+        rows, cols = (n, m) if turned else (m, n)
+        return q[:rows * pitch(cols)].view(rows, pitch(cols))[:, :cols], s[:blocks(cols) * rows].view(blocks(cols), rows)
+
+    def form(self, name: str, m: int):
+        """8-bit matrix and scales for m tokens: "u" and "ut", "dz" and "dzt" (scales are [blocks, m], so they go by the number)."""
+        if not 0 <= m <= self.tokens:
+            raise ValueError(f"{m} tokens in a layer that was made for {self.tokens}")
+        if (name, m) not in self._views:
+            self._views[name, m] = self._cut(name, m, self.width if name.startswith("u") else self.vocab)
+        return self._views[name, m]
 
     def forward(self, x, r, z, keep: bool = True):
         """z = layer(x + r); with `keep` also what backward() reads."""
         m, p = x.shape[0], self.master
-        u8 = self.forms(m)["u"]
+        uq, us = self.form("u", m)
         if keep:
-            self.ops.layer_norm(x, p["gain"], p["shift"], self.u[:m], residual=r, h=self.h[:m], q=u8["q"], s=u8["s"], mean=self.mean[:m], rstd=self.rstd[:m])
+            self.ops.layer_norm(x, p["gain"], p["shift"], self.u[:m], residual=r, h=self.h[:m], q=uq, s=us, mean=self.mean[:m], rstd=self.rstd[:m])
         else:
-            self.ops.layer_norm(x, p["gain"], p["shift"], residual=r, q=u8["q"], s=u8["s"])
-        self.ops.product_blocks(u8["q"], u8["s"], self.w["q"], self.w["s"], z)
+            self.ops.layer_norm(x, p["gain"], p["shift"], residual=r, q=uq, s=us)
+        self.ops.product_blocks(uq, us, self.w["q"], self.w["s"], z)
 
     def backward(self, z, index, value, loss, dh, weight=None, temperature: float = 1.0):
         """loss [tokens], the gradients of all parameters (self.grad) and dh, from the logits of the last forward pass,
         which the gradient of the losses' sum with respect to them replaces."""
         m, g = z.shape[0], self.grad
-        f = self.forms(m)
+        dzq, dzs = self.form("dz", m)
+        dzqt, dzst = self.form("dzt", m)
+        uqt, ust = self.form("ut", m)
         self.ops.distill(z, index, value, loss, weight=weight, dz=z, temperature=temperature)
-        self.ops.pack_blocks(z, **f["dz"])
-        self.ops.pack_blocks(self.u[:m], qt=f["u"]["qt"], st=f["u"]["st"])
-        self.ops.product_blocks(f["dz"]["qt"], f["dz"]["st"], f["u"]["qt"], f["u"]["st"], g["w"])
-        self.ops.product_blocks(f["dz"]["q"], f["dz"]["s"], self.w["qt"], self.w["st"], self.du[:m])
+        self.ops.pack_blocks(z, q=dzq, s=dzs, qt=dzqt, st=dzst)
+        self.ops.pack_blocks(self.u[:m], qt=uqt, st=ust)
+        self.ops.product_blocks(dzqt, dzst, uqt, ust, g["w"])
+        self.ops.product_blocks(dzq, dzs, self.w["qt"], self.w["st"], self.du[:m])
         self.ops.layer_norm_backward(self.du[:m], self.h[:m], self.master["gain"], self.mean[:m], self.rstd[:m], dh, g["gain"], g["shift"])
 
     def step(self, rate: float):

@@ -136,3 +136,57 @@ def test_shared_arrays_that_are_read_in_vectors_are_aligned():
                 seen += 1
                 assert promised[array] >= wide[kind], f"{name}: {array} promises {promised[array]} bytes and is accessed as {kind}"
     assert seen >= 5
+
+
+class _Recorder:
+    """Stands in for the operators: keeps the tensors that each call is given."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*a, **k):
+            self.calls.append((name, [t for t in (*a, *k.values()) if isinstance(t, torch.Tensor)]))
+        return call
+
+
+def _steps(layer, tokens, width, vocab, sizes, backward=True):
+    z, x = torch.zeros(tokens, vocab), torch.zeros(tokens, width)
+    index, value, loss = torch.zeros(tokens, 2, dtype=torch.int32), torch.zeros(tokens, 2), torch.zeros(tokens)
+    for m in sizes:
+        layer.forward(x[:m], x[:m], z[:m], keep=backward)
+        if backward:
+            layer.backward(z[:m], index[:m], value[:m], loss[:m], x[:m])
+
+
+def test_output_layer_keeps_buffers_for_its_tokens_once(monkeypatch):
+    from paper_1801_04928_b200.output_layer import OutputLayer
+    made, empty = [], torch.empty
+
+    def counted(*a, **k):
+        made.append(empty(*a, **k))
+        return made[-1]
+    monkeypatch.setattr(torch, "empty", counted)
+
+    def bytes_for(sizes, backward=True):
+        made.clear()
+        ops = _Recorder()
+        _steps(OutputLayer(ops, 40, 72, 264, device="cpu"), 40, 72, 264, sizes, backward)
+        return sum(t.untyped_storage().nbytes() for t in made), ops
+    most, _ = bytes_for([40])
+    for sizes in (range(40, 0, -1), [*range(1, 41), *range(1, 41)]):
+        got, ops = bytes_for(sizes)
+        assert got == most, (got, most)
+    # every view is what the operators take: scales contiguous, rows of bytes 16 bytes apart or a multiple, from a 16-byte boundary
+    for name, ts in ops.calls:
+        for t in ts:
+            if t.dtype == torch.uint8:
+                assert t.stride(1) == 1 and t.stride(0) % 16 == 0 and t.data_ptr() % 16 == 0, name
+            elif t.dim() == 2 and t.dtype == torch.float32:
+                assert t.is_contiguous(), name
+    # tokens without a backward pass have no use for the gradient's forms: z's in 8 bits, both ways, and u's turned
+    gradient = (40 * 272 + 264 * 48 + 72 * 48) + 4 * (3 * 40 + 264 + 72)
+    assert bytes_for([1, 40], backward=False)[0] == most - gradient
+    layer = OutputLayer(_Recorder(), 40, 72, 264, device="cpu")
+    with pytest.raises(ValueError):
+        layer.forward(torch.zeros(41, 72), torch.zeros(41, 72), torch.zeros(41, 264), keep=False)
