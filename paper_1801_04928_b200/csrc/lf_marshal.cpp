@@ -453,6 +453,9 @@ PyObject* m_product_blocks(PyObject*, PyObject* const* v, Py_ssize_t nargs)
     return c.answer(reinterpret_cast<decltype(&lf_product_blocks)>(address(v[0]))(static_cast<lf_ops*>(address(v[1])), &a));
 }
 
+// entries in the order of the indices: their shape, or one dimension (a matrix of as many entries the other way round is in another order)
+bool listed_as(const at::Tensor& value, const at::Tensor& index) { return value.dim() == 1 || value.sizes() == index.sizes(); }
+
 // distill(f, ops, z, index, value, loss, lse, weight, dz, temperature, device); distill_backward the same, loss None
 template <bool BACKWARD>
 PyObject* distill_any(PyObject* const* v, Py_ssize_t nargs)
@@ -473,6 +476,7 @@ PyObject* distill_any(PyObject* const* v, Py_ssize_t nargs)
     const float* lse_in = nullptr;
     const bool ok = c.mat(v[2], "z", a.tokens, a.vocab, st, &a.z, &a.ld_z) && (rows == a.tokens || c.refuse("index", c.said(*index) + ", a row for each of z's needed")) &&
                     c.flat(v[3], "index", n, at::kInt, &a.index) && c.flat(v[4], "value", n, at::kFloat, &a.value) &&
+                    (v[4] == Py_None || listed_as(THPVariable_Unpack(v[4]), *index) || c.refuse("value", c.said(THPVariable_Unpack(v[4])) + ", the shape of index needed")) &&
                     c.flat(v[5], "loss", a.tokens, at::kFloat, &a.loss) &&
                     (BACKWARD ? c.flat(v[6], "lse", a.tokens, at::kFloat, &lse_in) : c.flat(v[6], "lse", a.tokens, at::kFloat, &a.lse)) &&
                     c.flat(v[7], "weight", a.tokens, at::kFloat, &a.weight) && c.mat(v[8], "dz", a.tokens, a.vocab, st, &a.dz, &a.ld_dz);

@@ -133,3 +133,19 @@ def test_gradient_of_shifted_logits(ops, M, V, tau, shift, kind):
     s_err = (q * (2 * e_err)).sum(1, keepdim=True) + (7 * 7 + 13 + 9 * 4) * U
     err = tau32 * (q * (e_err + s_err + 4 * U) + mass * 4 * U) + 3 * U * ref.abs() + 2.0 ** -120
     R.check("dz", dz, ref, err)
+
+
+def test_entries_in_another_order_are_refused(ops):
+    """As many values as indices, but a row for each entry instead of each token."""
+    z, index, value = _rand(_gen(1), 4, 50), torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.zeros(4, 3, device="cuda")
+    loss, lse, dz = torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.empty(4, 50, device="cuda")
+    for bad in (value.t().contiguous(), value.view(2, 6), value.view(4, 3, 1)):
+        with pytest.raises(lf.LeapfrogError) as e:
+            ops.distill(z, index, bad, loss, lse)
+        assert e.value.status == lf.LF_EINVAL and "argument value" in str(e.value)
+        with pytest.raises(lf.LeapfrogError) as e:
+            ops.distill_backward(z, index, bad, lse, dz)
+        assert e.value.status == lf.LF_EINVAL
+    ops.distill(z, index, value.view(-1), loss, lse)
+    ops.distill_backward(z, index, value, lse, dz)
+    ops.sync()
