@@ -833,3 +833,89 @@ def test_output_layer_runs():
     d = (one[0].double() - z[5].double()).abs()
     assert bool((d <= 2 * 2.0 ** -8 * z[5].double().abs() + 1e-4).all())
     ops.close()
+
+
+OUTPUTS = ("h", "y", "mean", "rstd", "q", "s", "yqt", "yst", "wq", "ws", "wqt", "wst", "z", "loss", "lse", "dz", "dq", "ds", "dqt", "dst", "dy", "gw", "dh", "dg", "db")
+
+
+def test_every_run_gives_the_same_bits(ops):
+    """Each of the runs, all that they write, the 8-bit matrices too: outputs are cleared before a run and compared after it."""
+    for sizes in ((16, 1032, 4104, 40), (300, 2056, 3000, 64)):
+        b = _buffers(*sizes)
+        _run_all(ops, *sizes, b)
+        first = {k: b[k].clone() for k in OUTPUTS}
+        different = torch.zeros(len(OUTPUTS), dtype=torch.int64, device="cuda")
+        for _ in range(20):
+            for k in OUTPUTS:
+                b[k].zero_()
+            _run_all(ops, *sizes, b)
+            different += torch.stack([(b[k] != first[k]).sum() for k in OUTPUTS])
+        ops.sync()
+        assert all(bool(first[k].float().isfinite().all()) for k in OUTPUTS)
+        assert not bool(different.any()), dict(zip(OUTPUTS, different.tolist()))
+
+
+def test_two_handles_at_once_in_every_round():
+    """As the runs of two handles side by side, each round of them compared."""
+    cases = [(16, 1032, 4104, 40), (300, 2056, 3000, 64)]
+    with lf.Operators() as plain:
+        want = []
+        for sizes in cases:
+            b = _buffers(*sizes)
+            _run_all(plain, *sizes, b)
+            plain.sync()
+            want.append({k: b[k].clone() for k in OUTPUTS})
+    streams = [torch.cuda.Stream() for _ in cases]
+    handles = [lf.Operators(stream=s.cuda_stream) for s in streams]
+    try:
+        bufs = [_buffers(*sizes) for sizes in cases]
+        different = [torch.zeros(len(OUTPUTS), dtype=torch.int64, device="cuda") for _ in cases]
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for ops, sizes, b in zip(handles, cases, bufs):
+                _run_all(ops, *sizes, b)
+            for s, b, w, d in zip(streams, bufs, want, different):
+                with torch.cuda.stream(s):
+                    d += torch.stack([(b[k] != w[k]).sum() for k in OUTPUTS])
+                    for k in OUTPUTS:
+                        b[k].zero_()
+        torch.cuda.synchronize()
+        for d in different:
+            assert not bool(d.any()), dict(zip(OUTPUTS, d.tolist()))
+    finally:
+        for ops in handles:
+            ops.close()
+
+
+@pytest.mark.parametrize("tokens,width,vocab,temperature", [(300, 264, 1000, 2.0), (40, 512, 2504, 1.0)])
+def test_output_layer_gradients_against_automatic_differentiation(tokens, width, vocab, temperature):
+    """From the loss to the parameters and the layer's input, all of it differentiated in 64 bits.  An e4m3 number is off by 2^-4 of itself at most, 3.6 % in the mean
+    square, a sum of products of two by 5.1 % of its terms' root sum of squares; the logits (of deviation 1.4: x + r has unit variance after the norm, w's
+    rows unit length, the gain 1.2) carry 7 % into the softmax, and the gradient one or two more such products: 10 %, and a factor of two for terms that cancel."""
+    from paper_1801_04928_b200.output_layer import OutputLayer
+    g = _gen(vocab)
+    with lf.Operators() as ops:
+        layer = OutputLayer(ops, tokens, width, vocab, seed=tokens)
+        layer.master["gain"].add_(_rand(g, width, std=0.2))
+        layer.master["shift"].add_(_rand(g, width, std=0.2))
+        x, r = _rand(g, tokens, width, dtype=BF16), _rand(g, tokens, width, dtype=BF16)
+        index, value = _teacher(g, tokens, vocab, 7)
+        weight = torch.rand(tokens, generator=g, device="cuda")
+        z, loss, dh = torch.empty(tokens, vocab, dtype=BF16, device="cuda"), torch.empty(tokens, device="cuda"), torch.empty_like(x)
+        layer.forward(x, r, z)
+        layer.backward(z, index, value, loss, dh, weight=weight, temperature=temperature)
+        ops.sync()
+    leaves = [t.to(R.D).requires_grad_(True) for t in (layer.master["w"], layer.master["gain"], layer.master["shift"], x)]
+    w, gain, shift, xd = leaves
+    h = xd + r.to(R.D)
+    c = h - h.mean(1, keepdim=True)
+    u = c / torch.sqrt((c * c).mean(1, keepdim=True) + 1e-5) * gain + shift
+    logq = torch.log_softmax(u @ w.t() / temperature, 1).gather(1, index.clamp(min=0).long())
+    p = torch.softmax(value.to(R.D) / temperature, 1)
+    assert bool((index >= 0).all())
+    each = weight.to(R.D) * temperature ** 2 * (p * (p.log() - logq)).sum(1)
+    want = torch.autograd.grad(each.sum(), leaves)
+    assert (loss - each).norm() <= 0.2 * each.norm()
+    for name, got, ref in zip(("w", "gain", "shift", "x"), (layer.grad["w"], layer.grad["gain"], layer.grad["shift"], dh), want):
+        off = ((got.to(R.D) - ref).norm() / ref.norm()).item()
+        assert off <= 0.2, (name, off)

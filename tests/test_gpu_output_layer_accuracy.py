@@ -149,3 +149,31 @@ def test_entries_in_another_order_are_refused(ops):
     ops.distill(z, index, value.view(-1), loss, lse)
     ops.distill_backward(z, index, value, lse, dz)
     ops.sync()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [40, 5000, 70001])
+def test_gradient_far_from_zero_by_two_calls(ops, V, dtype):
+    """Rows at the type's lowest number and at -60000, where no fp32 lse holds a fraction: every row, and q to its own rounding."""
+    g = _gen(V)
+    z = torch.full((3, V), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+    z[1] = -60000.0
+    z[1, ::2] = -60000.0 + (32 if dtype == F16 else 256)
+    z[2, 7:] = 0
+    index, value = torch.randint(7, V, (3, 5), generator=g, device="cuda").int(), _rand(g, 3, 5)
+    q, p = torch.softmax(z.to(R.D), 1), torch.softmax(value.to(R.D), 1)
+    mass = torch.zeros_like(q).scatter_add_(1, index.long(), p)
+    ref = q - mass
+    # differences are 0 or far below any that counts: what is left are the sum (of a thread 7 * 17 additions and changes of the maximum at most where eight parts have
+    # the row, 17 times as many where a block has it alone) and a few roundings; weights of 16-bit logits are off by their argument's 3 U and 6 more
+    adds = 7 * 11 + 13 + 9 * 4
+    if dtype != F32:
+        adds = (V // (16 * 256) + 7) * 11 + 13 + 9 * 4
+    err = q * (adds + 12) * U + mass * (9 + 3 * value.abs().max()) * U
+    for in_place in (False, True):
+        loss, lse = torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+        to = z.clone()
+        ops.distill(z, index, value, loss, lse)
+        ops.distill_backward(to if in_place else z, index, value, lse, to)
+        ops.sync()
+        R.check("dz", to, ref, R.rounded(ref, dtype, err))
