@@ -739,11 +739,11 @@ int lb_choose(const lf_ops* o, const lf_product_blocks_args& a, int n_k)
     const double rows = a.tokens < 128 ? a.tokens / 128.0 : 1.0;
     int best = 1;
     double least = 1e30;
-    for (int splits = 1; splits <= 8 && splits <= n_k; splits *= 2) {
+    for (int i = 0, splits = 1; splits <= 8 && splits <= n_k; ++i, splits *= 2) {
+        if (o->max_block_splits[i] == 0) continue;
         const double part = (double)((n_k + splits - 1) / splits);
         const double meet = splits > 1 ? 1500.0 + 65536.0 * rows * (splits - 1) / splits / 14.0 : 0.0;
-        const int at_once = splits == 8 ? 120 : splits == 4 ? 132 : o->sm_count;      // resident clusters
-        const double cycles = waves(m128 * n128 * splits, at_once) * (part * 600.0 + meet + 9000.0);
+        const double cycles = waves(m128 * n128 * splits, o->max_block_splits[i]) * (part * 600.0 + meet + 9000.0);
         if (cycles < least) { least = cycles; best = splits; }
     }
     if (o->max_block_pairs > 0 && waves(tiles, o->max_block_pairs) * (n_k * 750.0 + 4000.0) + 10000.0 < least) best = 0;
@@ -755,20 +755,26 @@ int lb_choose(const lf_ops* o, const lf_product_blocks_args& a, int n_k)
 int lf_blocks_tc_init(lf_ops* o)
 {
     o->max_block_pairs = -1;
+    for (int& n : o->max_block_splits) n = -1;
     for (int type = 0; type < 3; ++type)
         for (int rows = 0; rows < 2; ++rows) {
             const int out = type == 0 ? LF_F32 : type == 1 ? LF_BF16 : LF_F16;
-            for (int splits = 1; splits <= 8; splits *= 2)
-                if (cudaFuncSetAttribute(lb_pick(out, rows, splits), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LBS_SMEM) != cudaSuccess) return LF_ECUDA;
-            const lb_kernel f = lb_pick(out, rows, 0);
-            if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LB_SMEM) != cudaSuccess) return LF_ECUDA;
-            cudaLaunchConfig_t cfg;
-            cudaLaunchAttribute at[2];
-            lt_cluster_config(&cfg, at, 32, lb_threads(rows != 0), 2, LB_SMEM, nullptr);
-            int n = 0;
-            if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return LF_ECUDA;
-            if (o->max_block_pairs < 0 || n < o->max_block_pairs) o->max_block_pairs = n;
+            // opts a kernel in; least: clusters of it that are resident at once, or fewer of another one
+            auto resident = [&](lb_kernel f, int threads, int cluster, size_t smem, int* least) {
+                cudaLaunchConfig_t cfg;
+                cudaLaunchAttribute at[2];
+                lt_cluster_config(&cfg, at, 32, threads, cluster, smem, nullptr);
+                int n = 0;
+                if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+                    cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess) return false;
+                if (*least < 0 || n < *least) *least = n;
+                return true;
+            };
+            for (int i = 0; i < 4; ++i)
+                if (!resident(lb_pick(out, rows, 1 << i), LBS_THREADS, 1 << i, LBS_SMEM, &o->max_block_splits[i])) return LF_ECUDA;
+            if (!resident(lb_pick(out, rows, 0), lb_threads(rows != 0), 2, LB_SMEM, &o->max_block_pairs)) return LF_ECUDA;
         }
+    for (int i = 0; i < 4; ++i) o->max_block_splits[i] <<= i;              // blocks
     return LF_OK;
 }
 

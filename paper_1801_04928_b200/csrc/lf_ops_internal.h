@@ -13,6 +13,7 @@ struct lf_ops {
     int max_pairs;              // CTA pairs of the 256 x 256 tile kernels that are resident at once (0: none)
     int max_pair_splits;        // resident clusters of the split pair kernels
     int max_block_pairs;        // CTA pairs of the 8-bit kernels that are resident at once
+    int max_block_splits[4];    // blocks of its split tiles in 1, 2, 4 and 8 parts (clusters) that are
     cudaStream_t stream;
     unsigned char* ws;          // workspace: fixed part first, then the unpacked layer input
     size_t ws_bytes;
