@@ -37,9 +37,10 @@ constexpr float DT_LARGE_LSE = 1024.f;          // from here on lse in fp32 is o
 // and 101, 8192 x 16384 131 and 114; loss 8192 x 16384 50 and 70, 400 x 30000 11.8 and 10.0; gradient 8192 x 16384 95 and 113, 8192 x 30000 190 and 167.
 constexpr int DT_SHORT_BYTES = 16 * 1024;
 constexpr int DT_PART_BYTES = 32 * 1024;        // of a row that a block of the joint kernel has, where eight parts are enough
-// The same of the gradient alone (fp32 logits), which needs no more blocks than there are multiprocessors: 64 x 50001 in four parts 7.5 us, in eight of 32 KB 10.9;
-// 1000 x 30000 43.8 and 49.5, 400 x 131072 78 and 94.
+// The same of the gradient alone (fp32 logits), which needs no more blocks than there are multiprocessors: through shared memory 64 x 50001 in four parts 7.5 us, in
+// eight of 32 KB 10.9; 1000 x 30000 43.8 and 49.5, 400 x 131072 78 and 94.
 constexpr int DT_ALONE_BYTES = 64 * 1024;
+constexpr int DT_HELD = DT_ALONE_BYTES / (16 * DT_UNROLL * DT_LONG);         // so much in a thread's registers
 // of shared memory for one of so many blocks, beside its variables and what every block takes
 constexpr int dt_room(int blocks) { return 227 * 1024 / blocks - 1024 - 2304; }
 
@@ -556,8 +557,11 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill(con
 // some load while others add or store: 8192 x 131072 bf16 849 us with six blocks to a multiprocessor (five: 938, four: 1072), 815 since a part looks after its own entries only; persistent
 // ones with the next part on its way 1345, a row to a block that reads it again from L2 1154.  The warp with the teacher's entries is waited for where it has read the row, which dz may be, and at
 // the end: a list of nothing, or an index beyond the vocabulary, is rare enough for the part to be written again.
-template <typename T, int RT>
-__global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_both(const lf_distill_args a, int log2, long long per, int staged)
+// HELD: a thread holds so many times DT_UNROLL pieces in registers instead, of fp32 rows whose gradient alone is wanted and that are all at work at once: their
+// blocks need not be small, and no multiprocessor has to divide its memory differently for them than for the loss before them (both calls on other rows each time:
+// 64 x 50001 15.2 us, through shared memory 19.3; 148 x 16000 11.3 and 14.2; not all at once, 2048 x 131072, 611 and 583).
+template <typename T, int RT, int HELD>
+__global__ void __launch_bounds__(RT + 32, HELD ? 2 : RT == DT_LONG ? 6 : 16) k_distill_both(const lf_distill_args a, int log2, long long per, int staged)
 {
     extern __shared__ __align__(16) unsigned char space[];     // staged pieces, entries
     __shared__ entry_facts facts;
@@ -568,7 +572,8 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
     const T* z = static_cast<const T*>(a.z) + (size_t)token * a.ld_z;
     const part_of<T> mine(z, a.vocab, part, per);
     const uint4* from = reinterpret_cast<const uint4*>(z + mine.body);
-    const int kept = min(staged, mine.pieces);
+    const int kept = min(HELD ? HELD * DT_UNROLL * RT : staged, mine.pieces);
+    uint4 held[HELD ? HELD : 1][DT_UNROLL];
     const float c = LOG2E / a.temperature;
     uint4* own = reinterpret_cast<uint4*>(space);
     const entries ent(space + (size_t)staged * 16, a.top, &facts);
@@ -577,13 +582,30 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
     online o;
     o.clear();
     if (row_warp) {
-        // (a thread reads what it copied itself)
-        for (int i = tid; i < kept; i += RT) cp_async16(lfptx::smem_u32(own + i), from + i);
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if constexpr (HELD > 0) {
+            const unsigned none = minus_infinity(T());
+#pragma unroll
+            for (int k = 0; k < HELD; ++k)
+#pragma unroll
+                for (int u = 0; u < DT_UNROLL; ++u) {
+                    const int i = tid + (k * DT_UNROLL + u) * RT;
+                    held[k][u] = i < kept ? ld16(from + i) : make_uint4(none, none, none, none);
+                }
+        } else {
+            // (a thread reads what it copied itself)
+            for (int i = tid; i < kept; i += RT) cp_async16(lfptx::smem_u32(own + i), from + i);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
         online_pieces<T, RT>(o, kept, mine.pieces, c, [&](int i) { return ld16(from + i); });
         online_edge<T>(o, z, mine, c);
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        online_pieces<T, RT>(o, 0, kept, c, [&](int i) { return own[i]; });
+        if constexpr (HELD > 0) {
+#pragma unroll
+            for (int k = 0; k < HELD; ++k)
+                if (tid + k * DT_UNROLL * RT < kept) o.add<T>(held[k], c);
+        } else {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            online_pieces<T, RT>(o, 0, kept, c, [&](int i) { return own[i]; });
+        }
     } else {
         gather<T>(ent, a, token, z, whole ? 0 : mine.e0, whole ? a.vocab : mine.e1, mine.e0, mine.e1);
     }
@@ -598,7 +620,19 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
         gather_totals(ent, table);
     } else if (!none) {
         const float f = facts.bad ? CUDART_NAN_F : wt / o.s;
-        gradient_pieces<T, RT, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
+        if constexpr (HELD > 0) {
+#pragma unroll
+            for (int k = 0; k < HELD; ++k)
+#pragma unroll
+                for (int u = 0; u < DT_UNROLL; ++u) {
+                    const int i = tid + (k * DT_UNROLL + u) * RT;
+                    float v[16 / sizeof(T)];
+                    gradient_piece<T>(v, held[k][u], m, c, f);
+                    if (i < kept) store_piece<T>(dz + mine.body + (long long)i * (16 / (int)sizeof(T)), v, aligned);
+                }
+        } else {
+            gradient_pieces<T, RT, 1>(dz + mine.body, 0, kept, m, c, f, aligned, [&](int i) { return own[i]; });
+        }
         gradient_pieces<T, RT, 1>(dz + mine.body, kept, mine.pieces, m, c, f, aligned, [&](int i) { return ld16(from + i); });
         gradient_edge<T>(dz, z, mine, m, c, f);
     } else {
@@ -620,8 +654,8 @@ __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 6 : 16) k_distill_bot
 // dz from z and lse, 16-bit logits: no part of a row needs to know another.  Where lse is so large that fp32 does not hold enough of
 // its fraction (a row of nothing but a type's lowest number), the first part takes the whole row, with its own maximum and sum.
 // (Of fp32 logits, lse as an fp32 number is never good enough: its rounding, 2^-24 of itself, is in every q of the row, 5e-7 for an lse of 11 and 1.5e-5 for one of
-// 260, where q is good for 1e-7.  Their maximum and sum are taken again, by k_distill_both without a loss: 8192 x 32768 352 us, from lse 328; 64 x 50001 7.6 and
-// 4.9; 2048 x 131072 373 and 324; a row that eight parts do not hold is read twice, 64 x 600001 139 and 55.)
+// 260, where q is good for 1e-7.  Their maximum and sum are taken again, by k_distill_both without a loss.  Both calls on other rows each time: 64 x 50001 15.2 us,
+// from lse 14.5; 1 x 50001 7.4 and 6.4; 8192 x 32768 565 and 501; 2048 x 131072 583 and 495.  A row that eight parts do not hold is read twice: 64 x 600001 139 for 55.)
 template <typename T, int RT>
 __global__ void __launch_bounds__(RT + 32, RT == DT_LONG ? 4 : 16) k_distill_backward(const lf_distill_args a, int parts, long long per)
 {
@@ -697,8 +731,10 @@ int parts_log2(const lf_distill_args& a, long long blocks, long long most)
 }
 
 template <typename T>
-cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
+cudaError_t distill_of(const lf_ops* o, const lf_distill_args& a)
 {
+    const int sm_count = o->sm_count;
+    const cudaStream_t s = o->stream;
     const int part_bytes = a.loss ? DT_PART_BYTES : DT_ALONE_BYTES;
     const int log2 = parts_log2(a, a.loss ? 2 * sm_count : sm_count, a.dz ? part_bytes : 1ll << 40), parts = 1 << log2;
     const long long row = (long long)a.vocab * (long long)sizeof(T);
@@ -709,16 +745,21 @@ cudaError_t distill_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
         return brief ? lf_launch(k_distill<T, DT_SHORT>, grid, DT_SHORT + 32, entries::bytes(a.top), s, a, log2, per)
                      : lf_launch_clusters(k_distill<T, DT_LONG>, grid, DT_LONG + 32, entries::bytes(a.top), parts, s, a, log2, per);
     const long long bytes = per * (long long)sizeof(T);
+    if constexpr (sizeof(T) == 4)
+        if (!a.loss && !brief && bytes <= DT_ALONE_BYTES && a.tokens <= o->max_held_rows[log2])
+            return lf_launch_clusters(k_distill_both<T, DT_LONG, DT_HELD>, grid, DT_LONG + 32, entries::bytes(a.top), parts, s, a, log2, per, 0);
     // (long lists take room from the row, not from the six, or alone three, blocks: 8192 x 131072 with 300 entries 1257 us when they did)
     const long long most = brief ? part_bytes : std::min((long long)part_bytes, (dt_room(a.loss ? 6 : 3) - (long long)entries::bytes(a.top)) / 16 * 16);
     const int staged = (int)((bytes < most ? bytes : most) / 16);
     const size_t smem = (size_t)staged * 16 + entries::bytes(a.top);
-    return brief ? lf_launch(k_distill_both<T, DT_SHORT>, grid, DT_SHORT + 32, smem, s, a, log2, per, staged)
-                 : lf_launch_clusters(k_distill_both<T, DT_LONG>, grid, DT_LONG + 32, smem, parts, s, a, log2, per, staged);
+    return brief ? lf_launch(k_distill_both<T, DT_SHORT, 0>, grid, DT_SHORT + 32, smem, s, a, log2, per, staged)
+                 : lf_launch_clusters(k_distill_both<T, DT_LONG, 0>, grid, DT_LONG + 32, smem, parts, s, a, log2, per, staged);
 }
 template <typename T>
-cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStream_t s)
+cudaError_t distill_backward_of(const lf_ops* o, const lf_distill_args& a)
 {
+    const int sm_count = o->sm_count;
+    const cudaStream_t s = o->stream;
     const long long bytes = (long long)a.vocab * sizeof(T);
     long long parts = (bytes + 65535) / 65536;                    // (16 pieces a thread)
     while ((long long)a.tokens * parts < 2 * sm_count && bytes / parts > 4096) parts *= 2;
@@ -730,29 +771,43 @@ cudaError_t distill_backward_of(const lf_distill_args& a, int sm_count, cudaStre
 template <typename T>
 bool distill_ready()
 {
-    return cudaFuncSetAttribute(k_distill_both<T, DT_LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, dt_room(sizeof(T) == 4 ? 3 : 6)) == cudaSuccess;
+    return cudaFuncSetAttribute(k_distill_both<T, DT_LONG, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, dt_room(sizeof(T) == 4 ? 3 : 6)) == cudaSuccess;
 }
 
 }  // namespace
 
-int lf_distill_init()
+int lf_distill_init(lf_ops* o)
 {
+    for (int i = 0; i < 4; ++i) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at[1];
+        cfg.gridDim = dim3(8);
+        cfg.blockDim = dim3(DT_LONG + 32);
+        cfg.dynamicSmemBytes = entries::bytes(LF_DISTILL_MAX_TOP);
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = 1u << i;
+        at[0].val.clusterDim.y = 1;
+        at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&o->max_held_rows[i], k_distill_both<float, DT_LONG, DT_HELD>, &cfg) != cudaSuccess) return LF_ECUDA;
+    }
     return distill_ready<float>() && distill_ready<__nv_bfloat16>() && distill_ready<__half>() ? LF_OK : LF_ECUDA;
 }
 
-cudaError_t lfk_distill(const lf_distill_args& a, int sm_count, cudaStream_t s)
+cudaError_t lfk_distill(const lf_ops* o, const lf_distill_args& a)
 {
-    if (a.dtype == LF_F32) return distill_of<float>(a, sm_count, s);
-    if (a.dtype == LF_BF16) return distill_of<__nv_bfloat16>(a, sm_count, s);
-    return distill_of<__half>(a, sm_count, s);
+    if (a.dtype == LF_F32) return distill_of<float>(o, a);
+    if (a.dtype == LF_BF16) return distill_of<__nv_bfloat16>(o, a);
+    return distill_of<__half>(o, a);
 }
-cudaError_t lfk_distill_backward(const lf_distill_args& a, int sm_count, cudaStream_t s)
+cudaError_t lfk_distill_backward(const lf_ops* o, const lf_distill_args& a)
 {
     if (a.dtype == LF_F32) {
         lf_distill_args alone = a;
         alone.loss = alone.lse = nullptr;
-        return distill_of<float>(alone, sm_count, s);
+        return distill_of<float>(o, alone);
     }
-    if (a.dtype == LF_BF16) return distill_backward_of<__nv_bfloat16>(a, sm_count, s);
-    return distill_backward_of<__half>(a, sm_count, s);
+    if (a.dtype == LF_BF16) return distill_backward_of<__nv_bfloat16>(o, a);
+    return distill_backward_of<__half>(o, a);
 }

@@ -121,7 +121,7 @@ int lf_ops_create(lf_ops** out, long long workspace_bytes)
     // (the memsets are only queued, on a stream that the handle's own need not wait for)
     ok = ok && cudaStreamSynchronize(nullptr) == cudaSuccess;
     ok = ok && lf_product_tc_init(o) == LF_OK && lf_linear_stream_init() == LF_OK && lf_rows_init() == LF_OK && lf_layer_norm_init() == LF_OK &&
-         lf_blocks_tc_init(o) == LF_OK && lf_blocks_stream_init() == LF_OK && lf_distill_init() == LF_OK;
+         lf_blocks_tc_init(o) == LF_OK && lf_blocks_stream_init() == LF_OK && lf_distill_init(o) == LF_OK;
     if (!ok) {
         const cudaError_t e = cudaGetLastError();
         lf_ops_destroy(o);
@@ -460,7 +460,7 @@ int lf_distill(lf_ops* o, const lf_distill_args* args)
     o->stats.launches = 0;
     if (a.tokens == 0) return LF_OK;
     a.ld_z = ld_or(a.ld_z, a.vocab); a.ld_dz = ld_or(a.ld_dz, a.vocab);
-    LF_OPS_TRY(o, lfk_distill(a, o->sm_count, o->stream));
+    LF_OPS_TRY(o, lfk_distill(o, a));
     o->stats.launches = 1;
     return LF_OK;
 }
@@ -476,7 +476,7 @@ int lf_distill_backward(lf_ops* o, const lf_distill_args* args)
     o->stats.launches = 0;
     if (a.tokens == 0) return LF_OK;
     a.ld_z = ld_or(a.ld_z, a.vocab); a.ld_dz = ld_or(a.ld_dz, a.vocab);
-    LF_OPS_TRY(o, lfk_distill_backward(a, o->sm_count, o->stream));
+    LF_OPS_TRY(o, lfk_distill_backward(o, a));
     o->stats.launches = 1;
     return LF_OK;
 }

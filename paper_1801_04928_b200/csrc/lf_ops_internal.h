@@ -14,6 +14,7 @@ struct lf_ops {
     int max_pair_splits;        // resident clusters of the split pair kernels
     int max_block_pairs;        // CTA pairs of the 8-bit kernels that are resident at once
     int max_block_splits[4];    // blocks of its split tiles in 1, 2, 4 and 8 parts (clusters) that are
+    int max_held_rows[4];       // rows of logits, each held in registers by 1, 2, 4 and 8 blocks, that are
     cudaStream_t stream;
     unsigned char* ws;          // workspace: fixed part first, then the unpacked layer input
     size_t ws_bytes;
@@ -109,9 +110,9 @@ int lf_layer_norm_init();
 cudaError_t lfk_layer_norm(const lf_layer_norm_args& a, int sm_count, cudaStream_t s);
 cudaError_t lfk_layer_norm_backward(const lf_layer_norm_backward_args& a, float* partial, int sm_count, cudaStream_t s, int* launches);
 cudaError_t lfk_pack_blocks(const lf_pack_blocks_args& a, bool tiles, cudaStream_t s);
-int lf_distill_init();
-cudaError_t lfk_distill(const lf_distill_args& a, int sm_count, cudaStream_t s);
-cudaError_t lfk_distill_backward(const lf_distill_args& a, int sm_count, cudaStream_t s);
+int lf_distill_init(lf_ops* o);
+cudaError_t lfk_distill(const lf_ops* o, const lf_distill_args& a);
+cudaError_t lfk_distill_backward(const lf_ops* o, const lf_distill_args& a);
 
 // ---- matrix products -----------------------------------------------------------------------------
 // What a product is for: which operands are transposed and what its epilogue does.
