@@ -1,7 +1,5 @@
 """Accuracy of layer norm's gradient and of the loss against a teacher where means, offsets and low temperatures make fp32 numbers
 cancel: bounds that a form which subtracts first keeps, and one that subtracts rounded products or logarithms does not."""
-import math
-
 import pytest
 import torch
 
@@ -177,3 +175,29 @@ def test_gradient_far_from_zero_by_two_calls(ops, V, dtype):
         ops.distill_backward(to if in_place else z, index, value, lse, to)
         ops.sync()
         R.check("dz", to, ref, R.rounded(ref, dtype, err))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("M,V", [(60, 20001), (300, 20001), (320, 30000)])
+def test_longest_lists_of_many_rows(ops, M, V, in_place):
+    """512 entries beside parts of rows that are held in registers or take most of a block's shared memory: each way the same gradient."""
+    g = _gen(M)
+    z = _student(g, M, V, 2.0)
+    index, value = torch.rand(M, V, generator=g, device="cuda").topk(512, 1).indices.int(), _rand(g, M, 512)
+    weight = torch.rand(M, generator=g, device="cuda")
+    _, dz = _loss(ops, z, index, value, 1.0, "both", weight)
+    loss, lse = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    to = z.clone()
+    ops.distill(z, index, value, loss, lse, weight=weight)
+    ops.distill_backward(to if in_place else z, index, value, lse, to, weight=weight)
+    ops.sync()
+    w = weight.to(R.D)[:, None]
+    q, p = torch.softmax(z.to(R.D), 1), torch.softmax(value.to(R.D), 1)
+    mass = torch.zeros_like(q).scatter_add_(1, index.long(), p)
+    d = z.to(R.D).amax(1, keepdim=True) - z.to(R.D)
+    # as for shifted logits; the weight is one more rounding
+    e_err = 4 * U * d + 4 * U
+    s_err = (q * (2 * e_err)).sum(1, keepdim=True) + (7 * 7 + 13 + 9 * 4) * U
+    err = w * (q * (e_err + s_err + 5 * U) + mass * 5 * U) + 3 * U * (w * (q - mass)).abs() + 2.0 ** -120
+    for got in (dz, to):
+        R.check("dz", got, w * (q - mass), err)
